@@ -279,6 +279,63 @@ int tr_profile_read(tr_ctx *ctx, double *ms_total, double *ms_empty_pairs, int64
  * dependent kernels. */
 int tr_profile_chain(void *hip_stream, int32_t *buf, int32_t workgroups, int32_t launches);
 
+/* ------------------------------------------------------------------ losses over the vocabulary
+ *
+ * What the small model learns from: the tokens that were emitted, and the large model's logits for the tokens it was asked for
+ * (the more of the large model's answers the small one gives by itself, the fewer tokens are routed). Both losses are functions of hidden rows (the exposed
+ * last-layer hidden state of Section 3.3, i.e. what the LM head multiplies) and of an LM head, need no context, and come with their gradients to both.
+ * Logits are never kept: they exist block by block, and in the gradients as pieces of the vocabulary in the workspace.
+ *
+ * z[n][v] = hidden[n] . weight[v] / T;  lse[n] = log sum_v exp z[n][v];  p = exp(z - lse).
+ *   cross entropy (T = 1): loss[n] = lse[n] - z[n][ids[n]]
+ *   distillation:          loss[n] = T^2 sum_j q_j (log q_j - (z[n][ids[n][j]] - lse[n])), q = softmax over the row's entries of teacher[n][j] / T:
+ *                          T^2 times the divergence of the student's distribution from the teacher's, the latter taken as nothing but its listed entries
+ *   gradients: with y = (ids[n] listed once with share 1 | the shares q), d loss[n] / d (hidden[n] . weight[v]) = T (p[v] - y[v]), weighed by grad_loss[n]
+ *
+ * Rows that do not count: cross entropy, ids[n] < 0; distillation, rows without entries. An entry is an id in [0, vocab) whose teacher logit is not
+ * -infinity; other ids (padding; a teacher whose padded vocabulary is longer) are left out of the row's softmax. Rows that do not count have loss and lse 0 and
+ * zero gradients, and take no part in d_weight, whatever their hidden rows hold. Cross entropy with ids[n] >= vocab: loss and lse NaN, no gradient. Rows of
+ * grad_loss 0 take no part in the gradients. An id listed twice in a row counts with both shares.
+ *
+ * Sums, softmax statistics and the losses are 32-bit throughout. Types: hidden and weight both TR_BF16, both TR_F32, or hidden TR_F32 (as tr_out.hidden) over
+ * a TR_BF16 head; gradients have the type of what they are to. With bf16 hidden rows the pieces of p - y are rounded to bf16 once.
+ * The same inputs give the same bits.
+ *
+ * Errors: TR_ERR_INVALID_ARG, TR_ERR_SHAPE (unsupported types or sizes), TR_ERR_CAPACITY (more rows or entries than configured, workspace too small), before
+ * anything is enqueued; TR_ERR_HIP. Calls only enqueue. Calls that share a workspace must be ordered with respect to each other; nothing in it
+ * outlives a call. rows may be 0 (d_weight is then cleared). */
+typedef struct tr_loss_config {
+    int32_t max_rows, dim, vocab;         /* 1 .. 2^20 rows, 1 .. 65536 features, 1 .. 2^24 entries */
+    int32_t hidden_dtype, weight_dtype;   /* TR_F32 / TR_BF16 */
+    int32_t max_entries;                  /* entries per row of distillation calls, 1 .. 1024 */
+} tr_loss_config;
+
+/* DEVICE pointers, aligned to their elements. */
+typedef struct tr_loss_rows {
+    const void *hidden, *weight;              /* [rows][dim], [vocab][dim] */
+    int64_t hidden_stride, weight_stride;     /* elements from row to row, >= dim */
+    const int32_t *ids;                       /* [rows] | [rows][entries] */
+    const float *teacher;                     /* [rows][entries] logits; distillation only */
+    int32_t rows, entries;                    /* entries: distillation only */
+    float temperature;                        /* > 0; distillation only */
+} tr_loss_rows;
+
+typedef struct tr_loss_grads {                /* DEVICE; either may be NULL: not computed */
+    void *d_hidden, *d_weight;                /* [rows][dim] in hidden_dtype, [vocab][dim] in weight_dtype */
+    int64_t d_hidden_stride, d_weight_stride;
+} tr_loss_grads;
+
+/* Bytes of device workspace (256-byte aligned, owned by the caller) the calls below need; 0 if the configuration is not supported. */
+size_t tr_loss_workspace_bytes(const tr_loss_config *cfg);
+/* loss, lse: DEVICE float [rows]. */
+int tr_cross_entropy(const tr_loss_config *cfg, void *workspace, size_t workspace_bytes, void *hip_stream, const tr_loss_rows *in, float *loss, float *lse);
+int tr_distill(const tr_loss_config *cfg, void *workspace, size_t workspace_bytes, void *hip_stream, const tr_loss_rows *in, float *loss, float *lse);
+/* lse: as the loss call on the same inputs left it; grad_loss: DEVICE float [rows], weight of each row's loss. */
+int tr_cross_entropy_grad(const tr_loss_config *cfg, void *workspace, size_t workspace_bytes, void *hip_stream, const tr_loss_rows *in, const float *lse,
+                          const float *grad_loss, const tr_loss_grads *out);
+int tr_distill_grad(const tr_loss_config *cfg, void *workspace, size_t workspace_bytes, void *hip_stream, const tr_loss_rows *in, const float *lse,
+                    const float *grad_loss, const tr_loss_grads *out);
+
 const char *tr_last_error(const tr_ctx *ctx);
 
 #ifdef __cplusplus

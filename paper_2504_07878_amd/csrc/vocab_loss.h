@@ -1,0 +1,90 @@
+// Losses over the vocabulary: what the host side (vocab_loss_api.hip) and the kernels share.
+//
+// z[r][v] = k * hidden[r] . weight[v] (k = 1 / temperature), lse[r] = log sum_v exp z[r][v]. A row's loss compares softmax(z) with shares q over a few
+// listed entries of the vocabulary: one entry of share 1 (cross entropy), or the softmax of a teacher's logits (distillation). The gradient to the
+// products hidden . weight is g (p - q) per temperature, p = exp(z - lse); it exists only in pieces of the vocabulary, as a matrix G of the piece's p - q.
+//
+// Only rows that count take part: they are listed once per call (`idx`) and everything behind works on that list, so that masked rows cost nothing and
+// whatever their hidden rows hold reaches neither gradient.
+#pragma once
+#include "tr_internal.h"
+
+namespace tr {
+
+struct LossHead {     // [count or 0, rows given, largest |weight of a row| as float bits, 0]
+    int count, rows;
+    float scale;
+    int pad;
+};
+
+struct LossArgs {
+    const void *hidden, *weight;
+    long long hs, ws;             // elements from row to row
+    int hdt, wdt;                 // DT_*
+    int rows, dim, vocab, entries;
+    const int *ids;               // [rows][entries]
+    const float *teacher;         // [rows][entries], NULL: every row's one entry has share 1
+    float temperature;
+    const float *grad;            // [rows] weights of the rows' losses (gradients only)
+    float *loss, *lse;            // [rows]; gradients read lse
+    void *d_hidden, *d_weight;    // either may be NULL
+    long long dhs, dws;
+    // workspace
+    LossHead *head;
+    int *idx;                     // [n_pad] rows that count, in order
+    unsigned char *state;         // [rows] ROW_*
+    float2 *part;                 // [blocks of the vocabulary][n_pad] running softmax (see Running)
+    float *value;                 // [n_pad][entries] products of the listed entries, then p - q
+    void *G;                      // [n_pad][piece]
+    float *acc;                   // [splits][n_pad][d_pad] sums of the gradient to the hidden rows
+    void *hp, *hw;                // [n_pad][d_pad] rows that count, and the same by their share of the largest weight (bf16 products)
+    void *wp;                     // [piece][d_pad] rows of the head where they cannot be read as they lie
+    int n_pad, d_pad, piece, splits;
+    int n_block;                  // rows per block (bf16 products)
+    bool direct;                  // the head is read as it lies (bf16 products): rows on 16 bytes, whole steps of 64 features
+};
+
+enum { ROW_SKIP = 0, ROW_COUNTS = 1, ROW_BAD = 2 };
+
+constexpr int LOSS_MAX_ENTRIES = 1024;
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
+// Rows that count, their list, zeros (NaN for an id at or past the vocabulary) for the others.
+void launch_loss_rows(hipStream_t s, const LossArgs &a);
+// lse and loss of the rows that count from `parts` running softmaxes each.
+void launch_loss_finish(hipStream_t s, const LossArgs &a, int parts);
+// From the products of the listed entries: p - q, and their places in G for one piece of the vocabulary.
+void launch_loss_values(hipStream_t s, const LossArgs &a);
+void launch_loss_scatter(hipStream_t s, const LossArgs &a, int v0, int vn, bool g_bf16);
+// The gradient to the hidden rows from `splits` sums, weighed and rounded; zeros for rows that do not count.
+void launch_loss_hidden_grad(hipStream_t s, const LossArgs &a, int splits);
+
+// Products of the listed entries, each the bits that the softmax's own products have: a probability near 1 and its logit then agree, and what is left of
+// 1 - p and of lse - z is not the difference of two roundings.
+void launch_f32_entries(hipStream_t s, const LossArgs &a);
+void launch_bf16_entries(hipStream_t s, const LossArgs &a);
+
+// Products on 32-bit matrix instructions, operands of either type and any stride (vocab_loss_f32_kernels.hip). Blocks of 128 x 128.
+constexpr int F32_BLOCK = 128;
+void launch_f32_softmax(hipStream_t s, const LossArgs &a);
+void launch_f32_probabilities(hipStream_t s, const LossArgs &a, int v0, int vn);
+void launch_f32_hidden_grad(hipStream_t s, const LossArgs &a, int v0, int vn, bool first);
+void launch_f32_weight_grad(hipStream_t s, const LossArgs &a, int v0, int vn);
+
+// bf16 rows and head (vocab_loss_bf16_kernels.hip): blocks of 256 vocabulary entries or features.
+constexpr int BF16_BLOCK = 256;
+void launch_bf16_pack_rows(hipStream_t s, const LossArgs &a);
+void launch_bf16_pack_head(hipStream_t s, const LossArgs &a, int v0, int vn);
+void launch_bf16_softmax(hipStream_t s, const LossArgs &a, int v0, int vn);
+void launch_bf16_probabilities(hipStream_t s, const LossArgs &a, int v0, int vn);
+void launch_bf16_hidden_grad(hipStream_t s, const LossArgs &a, int v0, int vn, bool first);
+void launch_bf16_weight_grad(hipStream_t s, const LossArgs &a, int v0, int vn);
+// splits of the sums of the gradient to `count` hidden rows, at most a.splits (both sides)
+__host__ __device__ inline int bf16_splits(const LossArgs &a, int count)
+{
+    const int tiles = (count + a.n_block - 1) / a.n_block * (a.d_pad / BF16_BLOCK + (a.d_pad % BF16_BLOCK ? 1 : 0));
+    const int n = 256 / (tiles ? tiles : 1);
+    return n < 1 ? 1 : n < a.splits ? n : a.splits;
+}
+
+}  // namespace tr

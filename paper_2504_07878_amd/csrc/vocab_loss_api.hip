@@ -1,0 +1,152 @@
+// Host side of the losses over the vocabulary: checks, workspace and the order of launches behind tr_cross_entropy, tr_distill and their gradients.
+#include "../../include/tokroute.h"
+#include "vocab_loss.h"
+
+#include <algorithm>
+#include <cmath>
+
+using namespace tr;
+
+namespace {
+
+size_t up(size_t v, size_t to) { return (v + to - 1) / to * to; }
+
+constexpr int MAX_ROWS = 1 << 20, MAX_DIM = 1 << 16, MAX_VOCAB = 1 << 24;
+
+bool config_ok(const tr_loss_config *c)
+{
+    if (!c || c->max_rows < 1 || c->max_rows > MAX_ROWS || c->dim < 1 || c->dim > MAX_DIM || c->vocab < 1 || c->vocab > MAX_VOCAB) return false;
+    if (c->max_entries < 1 || c->max_entries > LOSS_MAX_ENTRIES) return false;
+    return (c->hidden_dtype == TR_F32 && (c->weight_dtype == TR_F32 || c->weight_dtype == TR_BF16)) || (c->hidden_dtype == TR_BF16 && c->weight_dtype == TR_BF16);
+}
+
+// Where everything lies in the workspace, for a configuration; the sizes of a call's own launches follow from its rows, never beyond these.
+struct Plan {
+    int n_pad, d_pad, piece, splits;
+    size_t head, idx, state, part, value, G, acc, total;
+};
+
+Plan plan_of(const tr_loss_config *c)
+{
+    Plan p{};
+    const size_t g_size = 4;
+    p.n_pad = (int)up(c->max_rows, F32_BLOCK);
+    p.d_pad = (int)up(c->dim, F32_BLOCK);
+    const size_t vocab = up(c->vocab, F32_BLOCK);
+    p.piece = (int)std::min(vocab, std::max<size_t>(2048, (256u << 20) / g_size / p.n_pad / F32_BLOCK * F32_BLOCK));
+    const int tiles = p.n_pad / F32_BLOCK * (p.d_pad / F32_BLOCK);
+    p.splits = std::max(1, std::min(512 / tiles, p.piece / 256));
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t was = at; at += up(bytes, 256); return was; };
+    p.head = take(sizeof(LossHead));
+    p.idx = take((size_t)p.n_pad * 4);
+    p.state = take(c->max_rows);
+    p.part = take(vocab / F32_BLOCK * p.n_pad * sizeof(float2));
+    p.value = take((size_t)p.n_pad * c->max_entries * 4);
+    p.G = take((size_t)p.n_pad * p.piece * g_size);
+    p.acc = take((size_t)p.splits * p.n_pad * p.d_pad * 4);
+    p.total = at;
+    return p;
+}
+
+// Checks what every call has in common and fills in the arguments; TR_OK or an error, before anything is enqueued.
+int arguments(const tr_loss_config *c, const tr_loss_rows *in, void *ws, size_t ws_bytes, bool teacher, LossArgs &a, Plan &p)
+{
+    if (!c || !in || !ws) return TR_ERR_INVALID_ARG;
+    if (!config_ok(c)) return TR_ERR_SHAPE;
+    p = plan_of(c);
+    if (ws_bytes < p.total) return TR_ERR_CAPACITY;
+    if (in->rows > c->max_rows) return TR_ERR_CAPACITY;
+    if (in->rows < 0 || (reinterpret_cast<uintptr_t>(ws) & 255)) return TR_ERR_INVALID_ARG;
+    if (!in->weight || (in->rows && (!in->hidden || !in->ids || (teacher && !in->teacher)))) return TR_ERR_INVALID_ARG;
+    if (in->hidden_stride < c->dim || in->weight_stride < c->dim) return TR_ERR_INVALID_ARG;
+    if (teacher && (in->entries < 1 || !(in->temperature > 0.f) || !std::isfinite(in->temperature))) return TR_ERR_INVALID_ARG;
+    if (teacher && in->entries > c->max_entries) return TR_ERR_CAPACITY;
+    const auto size = [](int dt) { return dt == TR_BF16 ? 2u : 4u; };
+    if (reinterpret_cast<uintptr_t>(in->hidden) % size(c->hidden_dtype) || reinterpret_cast<uintptr_t>(in->weight) % size(c->weight_dtype)) return TR_ERR_INVALID_ARG;
+    char *const b = (char *)ws;
+    a = LossArgs{};
+    a.hidden = in->hidden; a.weight = in->weight; a.hs = in->hidden_stride; a.ws = in->weight_stride;
+    a.hdt = c->hidden_dtype == TR_BF16 ? DT_BF16 : DT_F32; a.wdt = c->weight_dtype == TR_BF16 ? DT_BF16 : DT_F32;
+    a.rows = in->rows; a.dim = c->dim; a.vocab = c->vocab;
+    a.entries = teacher ? in->entries : 1; a.ids = in->ids; a.teacher = teacher ? in->teacher : nullptr; a.temperature = teacher ? in->temperature : 1.f;
+    a.head = (LossHead *)(b + p.head); a.idx = (int *)(b + p.idx); a.state = (unsigned char *)(b + p.state); a.part = (float2 *)(b + p.part);
+    a.value = (float *)(b + p.value); a.G = b + p.G; a.acc = (float *)(b + p.acc);
+    a.n_pad = p.n_pad; a.d_pad = p.d_pad; a.piece = p.piece; a.splits = p.splits;
+    return TR_OK;
+}
+
+int enqueued() { return hipGetLastError() == hipSuccess ? TR_OK : TR_ERR_HIP; }
+
+int forward(const tr_loss_config *c, void *ws, size_t ws_bytes, void *stream, const tr_loss_rows *in, float *loss, float *lse, bool teacher)
+{
+    LossArgs a;
+    Plan p;
+    if (const int e = arguments(c, in, ws, ws_bytes, teacher, a, p)) return e;
+    if (a.rows && (!loss || !lse)) return TR_ERR_INVALID_ARG;
+    if (!a.rows) return TR_OK;
+    a.loss = loss; a.lse = lse;
+    hipStream_t s = (hipStream_t)stream;
+    launch_loss_rows(s, a);
+    launch_f32_softmax(s, a);
+    launch_f32_entries(s, a);
+    launch_loss_finish(s, a, (a.vocab + F32_BLOCK - 1) / F32_BLOCK);
+    return enqueued();
+}
+
+int backward(const tr_loss_config *c, void *ws, size_t ws_bytes, void *stream, const tr_loss_rows *in, const float *lse, const float *grad_loss, const tr_loss_grads *out, bool teacher)
+{
+    LossArgs a;
+    Plan p;
+    if (const int e = arguments(c, in, ws, ws_bytes, teacher, a, p)) return e;
+    if (!out || (a.rows && (!lse || !grad_loss))) return TR_ERR_INVALID_ARG;
+    if ((out->d_hidden && out->d_hidden_stride < c->dim) || (out->d_weight && out->d_weight_stride < c->dim)) return TR_ERR_INVALID_ARG;
+    const auto size = [](int dt) { return dt == TR_BF16 ? 2u : 4u; };
+    if (reinterpret_cast<uintptr_t>(out->d_hidden) % size(c->hidden_dtype) || reinterpret_cast<uintptr_t>(out->d_weight) % size(c->weight_dtype)) return TR_ERR_INVALID_ARG;
+    if (!out->d_hidden && !out->d_weight) return TR_OK;
+    a.lse = const_cast<float *>(lse); a.grad = grad_loss;
+    a.d_hidden = out->d_hidden; a.dhs = out->d_hidden_stride; a.d_weight = out->d_weight; a.dws = out->d_weight_stride;
+    hipStream_t s = (hipStream_t)stream;
+    launch_loss_rows(s, a);
+    launch_f32_entries(s, a);
+    launch_loss_values(s, a);
+    for (int v0 = 0; v0 < a.vocab; v0 += a.piece) {
+        const int vn = std::min(a.piece, a.vocab - v0);
+        launch_f32_probabilities(s, a, v0, vn);
+        launch_loss_scatter(s, a, v0, vn, false);
+        if (a.d_hidden) launch_f32_hidden_grad(s, a, v0, vn, v0 == 0);
+        if (a.d_weight) launch_f32_weight_grad(s, a, v0, vn);
+    }
+    if (a.d_hidden) launch_loss_hidden_grad(s, a, a.splits);
+    return enqueued();
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t tr_loss_workspace_bytes(const tr_loss_config *cfg) { return config_ok(cfg) ? plan_of(cfg).total : 0; }
+
+int tr_cross_entropy(const tr_loss_config *cfg, void *workspace, size_t workspace_bytes, void *hip_stream, const tr_loss_rows *in, float *loss, float *lse)
+{
+    return forward(cfg, workspace, workspace_bytes, hip_stream, in, loss, lse, false);
+}
+
+int tr_cross_entropy_grad(const tr_loss_config *cfg, void *workspace, size_t workspace_bytes, void *hip_stream, const tr_loss_rows *in, const float *lse,
+                          const float *grad_loss, const tr_loss_grads *out)
+{
+    return backward(cfg, workspace, workspace_bytes, hip_stream, in, lse, grad_loss, out, false);
+}
+
+int tr_distill(const tr_loss_config *cfg, void *workspace, size_t workspace_bytes, void *hip_stream, const tr_loss_rows *in, float *loss, float *lse)
+{
+    return forward(cfg, workspace, workspace_bytes, hip_stream, in, loss, lse, true);
+}
+
+int tr_distill_grad(const tr_loss_config *cfg, void *workspace, size_t workspace_bytes, void *hip_stream, const tr_loss_rows *in, const float *lse,
+                    const float *grad_loss, const tr_loss_grads *out)
+{
+    return backward(cfg, workspace, workspace_bytes, hip_stream, in, lse, grad_loss, out, true);
+}
+
+}  // extern "C"

@@ -1,0 +1,92 @@
+// What becomes of a block of products in the losses over the vocabulary. All products are computed transposed: the accumulator registers of a lane run
+// along the output's contiguous dimension (runs of 8: tile_feature) and the lanes along its rows, so that a row's softmax needs one exchange between
+// lanes, and stores are whole runs.
+#pragma once
+#include "mfma_common.h"
+#include "vocab_loss.h"
+
+namespace tr {
+
+__device__ __forceinline__ void run_of(const f32x16 &c, int h, float (&v)[8])
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = c[8 * h + e];
+}
+
+__device__ __forceinline__ void store_run(float *p, const float (&v)[8])
+{
+    reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+__device__ __forceinline__ uint32_t two_bf16(float a, float b)
+{
+    const f32x2 x = {a, b};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+}
+__device__ __forceinline__ void store_run(bf16_t *p, const float (&v)[8])
+{
+    *reinterpret_cast<uint4 *>(p) = make_uint4(two_bf16(v[0], v[1]), two_bf16(v[2], v[3]), two_bf16(v[4], v[5]), two_bf16(v[6], v[7]));
+}
+__device__ __forceinline__ void store_one(float *p, float v) { *p = v; }
+__device__ __forceinline__ void store_one(bf16_t *p, float v) { *p = (bf16_t)two_bf16(v, 0.f); }
+__device__ __forceinline__ float load_one(const float *p) { return *p; }
+__device__ __forceinline__ float load_one(const bf16_t *p) { return __uint_as_float((uint32_t)*p << 16); }
+
+// A running softmax is (m, s): s = sum of 2^(k c - m) over the products c seen, k = log2(e) / T, m a whole number at least the largest k c (-inf: none seen).
+// Since m is whole, moving a sum to another m is exact, and k c - m is rounded once (fma), relative to itself: what is near the top keeps all its bits.
+__device__ __forceinline__ float whole_above(float top) { return ceilf(top); }
+__device__ __forceinline__ float term(float c, float k, float m) { return __builtin_amdgcn_exp2f(fmaf(c, k, -m)); }
+__device__ __forceinline__ float2 join(float2 a, float2 b)
+{
+    const float m = fmaxf(a.x, b.x), at = m == -INFINITY ? 0.f : m;
+    return make_float2(m, a.y * __builtin_amdgcn_exp2f(a.x - at) + b.y * __builtin_amdgcn_exp2f(b.x - at));
+}
+
+// A block's part of every row's softmax over vocabulary entries m0 .. (those at or past V do not exist): wavefront (wm, wn) of WM x WN holds MI x NI
+// accumulators. red: LDS, WM * WN * NI * 32 float2.
+template <int WM, int WN, int MI, int NI>
+__device__ __forceinline__ void softmax_part(const f32x16 (&c)[MI][NI], float2 *red, float2 *part /* of this block's vocabulary, [row] */, int m0, int V, float k2, int wm, int wn)
+{
+    const int lane = threadIdx.x & 63, hf = lane >> 5, col = lane & 31;
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi) {
+            const int base = m0 + (wm * MI + mi) * 32;
+            if (base + 32 <= V) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) top = fmaxf(top, c[mi][ni][r]);
+            } else {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) top = base + 16 * (r >> 3) + 8 * hf + (r & 7) < V ? fmaxf(top, c[mi][ni][r]) : top;
+            }
+        }
+        top = whole_above(top * k2);
+        const float at = top == -INFINITY ? 0.f : top;
+        float sum = 0.f;
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi) {
+            const int base = m0 + (wm * MI + mi) * 32;
+            if (base + 32 <= V) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) sum += term(c[mi][ni][r], k2, at);
+            } else {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) sum += base + 16 * (r >> 3) + 8 * hf + (r & 7) < V ? term(c[mi][ni][r], k2, at) : 0.f;
+            }
+        }
+        const float2 mine = make_float2(top, sum), other = make_float2(__shfl_xor(top, 32), __shfl_xor(sum, 32));
+        const float2 both = hf ? join(other, mine) : join(mine, other);
+        if (hf == 0) red[(wm * WN + wn) * NI * 32 + ni * 32 + col] = both;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < WN * NI * 32; i += WM * WN * 64) {
+        float2 t = red[i];
+#pragma unroll
+        for (int w = 1; w < WM; ++w) t = join(t, red[w * WN * NI * 32 + i]);
+        part[i] = t;
+    }
+}
+
+}  // namespace tr

@@ -25,7 +25,7 @@ KERNEL_FAMILIES = ("setup", "prep", "qkv", "attention", "oproj", "gateup", "down
 
 EXPORTS = ["tr_workspace_bytes", "tr_create", "tr_destroy", "tr_prefill", "tr_decode_step", "tr_decode_step_dev", "tr_decode_step_active", "tr_extend", "tr_tail", "tr_tail_noalloc", "tr_set_threshold",
            "tr_set_mode", "tr_set_shared", "tr_seq_len", "tr_seq_truncate", "tr_seq_fork", "tr_seq_load_kv", "tr_counters_ptr", "tr_profile_enable", "tr_profile_select",
-           "tr_profile_read", "tr_profile_chain", "tr_last_error"]
+           "tr_profile_read", "tr_profile_chain", "tr_last_error", "tr_loss_workspace_bytes", "tr_cross_entropy", "tr_cross_entropy_grad", "tr_distill", "tr_distill_grad"]
 
 
 class tr_config(C.Structure):
@@ -37,6 +37,19 @@ class tr_config(C.Structure):
 
 
 _PP = C.POINTER(C.c_void_p)
+
+
+class tr_loss_config(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("max_rows", "dim", "vocab", "hidden_dtype", "weight_dtype", "max_entries")]
+
+
+class tr_loss_rows(C.Structure):
+    _fields_ = [("hidden", C.c_void_p), ("weight", C.c_void_p), ("hidden_stride", C.c_int64), ("weight_stride", C.c_int64), ("ids", C.c_void_p),
+                ("teacher", C.c_void_p), ("rows", C.c_int32), ("entries", C.c_int32), ("temperature", C.c_float)]
+
+
+class tr_loss_grads(C.Structure):
+    _fields_ = [("d_hidden", C.c_void_p), ("d_weight", C.c_void_p), ("d_hidden_stride", C.c_int64), ("d_weight_stride", C.c_int64)]
 
 
 class tr_weights(C.Structure):
@@ -83,6 +96,12 @@ def load_library():
         L.tr_profile_select.argtypes = [vp, i32]
         L.tr_profile_read.argtypes = [vp, C.POINTER(C.c_double), C.POINTER(C.c_double), C.POINTER(C.c_int64)]
         L.tr_profile_chain.argtypes = [vp, vp, i32, i32]
+        lc, lr, sz = C.POINTER(tr_loss_config), C.POINTER(tr_loss_rows), C.c_size_t
+        L.tr_loss_workspace_bytes.argtypes = [lc]; L.tr_loss_workspace_bytes.restype = sz
+        for f in (L.tr_cross_entropy, L.tr_distill):
+            f.argtypes = [lc, vp, sz, vp, lr, vp, vp]
+        for f in (L.tr_cross_entropy_grad, L.tr_distill_grad):
+            f.argtypes = [lc, vp, sz, vp, lr, vp, vp, C.POINTER(tr_loss_grads)]
         L.tr_last_error.argtypes = [vp]; L.tr_last_error.restype = C.c_char_p
         _lib = L
     return _lib

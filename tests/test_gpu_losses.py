@@ -1,0 +1,424 @@
+"""Losses over the vocabulary (tr_cross_entropy, tr_distill and their gradients) against their definition in 64 bits, on the same inputs.
+
+Tolerances, from the arithmetic: u = 2^-24 is a rounding to fp32, b = 2^-8 one to bf16 (8 significant bits).
+  * A product hidden . weight of d terms, summed in fp32 in any order: |dz| <= Z = (4 sqrt(d) + 4) u max_v sum_k |h_k w_k| (rounding errors add up like a random
+    walk; 4 of its standard deviations), over T. lse moves by no more than its largest dz, and by the roundings of exp, log and the sum: 16 u (1 + |lse|).
+    loss = T^2 sum_j q_j (log q_j - z_j + lse): T^2 (2 Z + 16 u (1 + |lse| + max |log q| + max |z_j|)).
+  * p = exp(z - lse) is off by a factor of 1 +- (2 Z + 16 u (1 + |lse|)), y by 1 +- 16 u (1 + max |log q|); with bf16 rows p - y is rounded to bf16 once: b |p - y| more. So an element of a gradient,
+    a sum of K terms |p - y| x, is off by at most the sum of these times |x|, plus (4 sqrt(K) + 4) u sum |(p - y) x| of summing, plus b (or u) of the result for the last rounding; the
+    gradient of the head with rows of unequal weight has one more rounding of the weighed rows to bf16.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+U, B = 2.0 ** -24, 2.0 ** -8
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+@pytest.fixture(scope="module")
+def losses():
+    from paper_2504_07878_amd import losses as m
+    from paper_2504_07878_amd import tokroute
+    tokroute.load_library()
+    return m
+
+
+def make(n, d, v, ht, wt, entries=0, seed=0, scale=1.0, masked=0.3, pad=(0, 0), even=False):
+    """Hidden rows N(0, 1), head N(0, (2 scale / sqrt d)^2), so that logits have a standard deviation of 2 scale; a row's first entry pulls it up."""
+    g = torch.Generator().manual_seed(seed)
+    h = torch.randn((n, d + pad[0]), generator=g)[:, :d]
+    w = torch.randn((v, d + pad[1]), generator=g)[:, :d] * (2.0 * scale / math.sqrt(d))
+    ids = torch.randint(0, v, (n, max(entries, 1)), generator=g)
+    h = h + w[ids[:, 0]] * (torch.rand((n, 1), generator=g) * math.sqrt(d))
+    off = torch.rand(n, generator=g) < masked
+    t = {"hidden": _strided(h, ht, pad[0]), "weight": _strided(w, wt, pad[1])}
+    if entries:
+        teacher = 3.0 * torch.randn((n, entries), generator=g)
+        ids[torch.rand((n, entries), generator=g) < 0.2] = -1
+        ids[off] = -5
+        t |= {"ids": ids.int().cuda(), "teacher": teacher.cuda()}
+    else:
+        ids[off] = -1
+        t["targets"] = ids[:, 0].int().cuda()
+    t["grad_loss"] = (torch.ones(n) / n if even else torch.randn(n, generator=g)).cuda()
+    return t
+
+
+def _strided(x, dtype, pad):
+    room = torch.full((x.shape[0], x.shape[1] + pad), float("nan"), dtype=dtype, device="cuda")   # what lies between rows is not read
+    room[:, :x.shape[1]] = x.to(dtype).cuda()
+    return room[:, :x.shape[1]]
+
+
+def shares(t, v, temperature):
+    """(q [n][entries], log q, counts [n]) of every row in 64 bits, numpy"""
+    if "targets" in t:
+        ids = t["targets"].cpu().numpy()[:, None]
+        ok = (ids >= 0) & (ids < v)
+        return ids, ok, ok.astype(np.float64), np.zeros(ids.shape)
+    ids, x = t["ids"].cpu().numpy(), t["teacher"].double().cpu().numpy()
+    ok = (ids >= 0) & (ids < v) & (x != -np.inf)
+    with np.errstate(invalid="ignore", divide="ignore"):
+        x = np.where(ok, x, -np.inf)
+        top = np.where(ok.any(1, keepdims=True), x.max(1, keepdims=True), 0.0)
+        e = np.where(ok, np.exp((x - top) / temperature), 0.0)
+        total = e.sum(1, keepdims=True)
+        q = e / np.where(total > 0, total, 1.0)
+        lq = np.where(ok, (x - top) / temperature, 0.0) - np.log(np.where(total > 0, total, 1.0))
+    return ids, ok, q, lq
+
+
+def definition(t, temperature=1.0):
+    """loss, lse, gradients, and the bounds on each that the module's head derives; numpy, 64 bits."""
+    h, w = t["hidden"].double().cpu().numpy(), t["weight"].double().cpu().numpy()
+    n, d, v = h.shape[0], h.shape[1], w.shape[0]
+    ids, ok, q, lq = shares(t, v, temperature)
+    on = ok.any(1)
+    g = np.where(on, t["grad_loss"].double().cpu().numpy(), 0.0)
+    h = np.where(on[:, None], h, 0.0)
+    z = h @ w.T / temperature
+    top = z.max(1, keepdims=True)
+    lse = (top + np.log(np.exp(z - top).sum(1, keepdims=True)))[:, 0]
+    zj = np.take_along_axis(z, np.where(ok, ids, 0), 1)
+    T2 = temperature * temperature
+    loss = T2 * np.where(ok & (q > 0), q * (lq - zj + lse[:, None]), 0.0).sum(1)
+    Z = (4 * math.sqrt(d) + 4) * U * (np.abs(h) @ np.abs(w).T).max(1) / temperature
+    listed = np.where(ok & (q > 0), np.abs(lq), 0.0).max(1)
+    own = 2 * Z + 16 * U * (1 + np.abs(lse))
+    out = {"loss": np.where(on, loss, 0.0), "lse": np.where(on, lse, 0.0)}
+    bound = {"lse": Z + 16 * U * (1 + np.abs(lse)), "loss": T2 * (own + 16 * U * (1 + listed + np.where(ok, np.abs(zj), 0.0).max(1)))}
+    p = np.exp(z - lse[:, None])
+    y = np.zeros_like(p)
+    np.add.at(y, (np.arange(n)[:, None].repeat(ids.shape[1], 1)[ok], ids[ok]), q[ok])
+    dz = g[:, None] * temperature * np.where(on[:, None], p - y, 0.0)
+    weigh = np.abs(g)[:, None] * temperature * on[:, None]
+    half = t["hidden"].dtype == BF16
+    off = weigh * (p * own[:, None] + y * 16 * U * (1 + listed)[:, None]) + (B if half else 2 * U) * np.abs(dz)
+    out |= {"d_hidden": dz @ w, "d_weight": dz.T @ h}
+    uneven = half and np.unique(np.abs(g[on & (g != 0)])).size > 1
+    last = {"d_hidden": B if half else U, "d_weight": B if t["weight"].dtype == BF16 else U}
+    bound["d_hidden"] = off @ np.abs(w) + (4 * math.sqrt(v) + 4) * U * (np.abs(dz) @ np.abs(w))
+    bound["d_weight"] = off.T @ np.abs(h) + ((4 * math.sqrt(max(1, n)) + 8) * U + (B if uneven else 0.0)) * (np.abs(dz).T @ np.abs(h))
+    for k, r in last.items():
+        bound[k] += r * (np.abs(out[k]) + bound[k]) + 1e-38
+    return out, bound
+
+
+def call(losses, t, temperature=1.0, plan=None, **kw):
+    n, d = t["hidden"].shape
+    if "targets" in t:
+        plan = plan or losses.VocabLoss(max(n, 1), d, t["weight"].shape[0], t["hidden"].dtype, t["weight"].dtype)
+        loss, lse = plan.cross_entropy(t["hidden"], t["weight"], t["targets"])
+        dh, dw = plan.cross_entropy_grad(t["hidden"], t["weight"], t["targets"], lse, t["grad_loss"], **kw)
+    else:
+        plan = plan or losses.VocabLoss(max(n, 1), d, t["weight"].shape[0], t["hidden"].dtype, t["weight"].dtype, max_entries=t["ids"].shape[1])
+        loss, lse = plan.distill(t["hidden"], t["weight"], t["ids"], t["teacher"], temperature)
+        dh, dw = plan.distill_grad(t["hidden"], t["weight"], t["ids"], t["teacher"], temperature, lse, t["grad_loss"], **kw)
+    return {"loss": loss, "lse": lse, "d_hidden": dh, "d_weight": dw}
+
+
+def check(got, t, temperature=1.0, what=("loss", "lse", "d_hidden", "d_weight")):
+    want, bound = definition(t, temperature)
+    for k in what:
+        x = got[k].double().cpu().numpy()
+        assert x.shape == want[k].shape, k
+        over = ~(np.abs(x - want[k]) <= bound[k])
+        assert not over.any(), (k, int(over.sum()), float(np.max(np.abs(x - want[k]) / bound[k])), np.argwhere(over)[:4].tolist())
+
+
+# rows, features, vocabulary: one of each, sizes about the edges of blocks and pieces, odd ones, and the tiny model's
+SIZES = [(1, 1, 1), (1, 8, 2), (3, 64, 100), (33, 65, 127), (64, 128, 257), (65, 200, 1000), (130, 256, 4096), (257, 192, 777), (300, 896, 1500), (127, 333, 5003), (520, 64, 129)]
+TYPES = [(F32, F32), (F32, BF16), (BF16, BF16)]
+
+
+@pytest.mark.parametrize("types", TYPES, ids=["f32", "f32_rows", "bf16"])
+@pytest.mark.parametrize("size", SIZES, ids=str)
+def test_cross_entropy(losses, size, types):
+    t = make(*size, *types, seed=sum(size))
+    check(call(losses, t), t)
+
+
+@pytest.mark.parametrize("types", TYPES, ids=["f32", "f32_rows", "bf16"])
+@pytest.mark.parametrize("size,entries,temperature", [((1, 8, 2), 1, 1.0), ((3, 64, 100), 5, 2.0), ((65, 200, 1000), 64, 0.5), ((130, 256, 4096), 33, 1.5), ((300, 896, 1500), 16, 4.0),
+                                                      ((40, 77, 3000), 1024, 2.0), ((257, 64, 777), 3, 1.0)], ids=str)
+def test_distill(losses, size, entries, temperature, types):
+    t = make(*size, *types, entries=entries, seed=sum(size) + entries)
+    check(call(losses, t, temperature), t, temperature)
+
+
+@pytest.mark.parametrize("types", TYPES, ids=["f32", "f32_rows", "bf16"])
+def test_every_row_counts_with_the_same_weight(losses, types):
+    t = make(200, 192, 1111, *types, masked=0.0, even=True)
+    check(call(losses, t), t)
+
+
+@pytest.mark.parametrize("types", TYPES, ids=["f32", "f32_rows", "bf16"])
+@pytest.mark.parametrize("pad", [(1, 3), (8, 16), (5, 0)], ids=str)
+def test_strided_rows(losses, types, pad):
+    """Rows of larger matrices: what lies between them (NaN here) is neither read nor written over."""
+    t = make(70, 192, 500, *types, pad=pad, seed=3)
+    room_h, room_w = (torch.full((m, 192 + 5), 7.0, dtype=dt, device="cuda") for m, dt in ((70, types[0]), (500, types[1])))
+    got = call(losses, t, d_hidden=room_h[:, :192], d_weight=room_w[:, :192])
+    check(got, t)
+    assert (room_h[:, 192:] == 7).all() and (room_w[:, 192:] == 7).all()
+
+
+@pytest.mark.parametrize("types", TYPES, ids=["f32", "f32_rows", "bf16"])
+@pytest.mark.parametrize("entries", [0, 4])
+def test_rows_that_do_not_count_may_hold_anything(losses, types, entries):
+    t = make(90, 128, 300, *types, entries=entries, masked=0.5, seed=4)
+    clean = call(losses, t)
+    off = (t["targets"] < 0) if entries == 0 else (t["ids"] < 0).all(1)
+    assert off.any() and not off.all()
+    for junk in (float("nan"), float("inf"), torch.finfo(types[0]).min):
+        t["hidden"][off] = junk
+        got = call(losses, t)
+        for k in got:
+            assert torch.equal(got[k], clean[k]), (junk, k)
+        for k in ("loss", "lse", "d_hidden"):
+            assert (got[k][off] == 0).all()
+
+
+@pytest.mark.parametrize("types", TYPES, ids=["f32", "f32_rows", "bf16"])
+@pytest.mark.parametrize("entries", [0, 3])
+def test_no_row_counts(losses, types, entries):
+    t = make(37, 64, 200, *types, entries=entries, masked=1.1)
+    got = call(losses, t)
+    for k in got:
+        assert (got[k] == 0).all(), k
+
+
+@pytest.mark.parametrize("types", TYPES, ids=["f32", "f32_rows", "bf16"])
+def test_no_rows(losses, types):
+    t = make(4, 64, 200, *types)
+    none = {k: (v if k == "weight" else v[:0]) for k, v in t.items()}
+    plan = losses.VocabLoss(4, 64, 200, *types)
+    dw = torch.full((200, 64), 3.0, dtype=types[1], device="cuda")
+    got = call(losses, none, plan=plan, d_weight=dw)
+    assert got["loss"].numel() == 0 and got["d_hidden"].shape == (0, 64) and (dw == 0).all()
+
+
+def test_ids_past_the_vocabulary(losses):
+    """Cross entropy: the row is NaN and gives no gradient. Distillation: such entries are left out (a teacher's padded vocabulary)."""
+    t = make(20, 64, 100, BF16, BF16, masked=0.0)
+    bad = t | {"targets": t["targets"].clone()}
+    bad["targets"][7], bad["targets"][11] = 100, 2 ** 31 - 1
+    got = call(losses, bad)
+    assert got["loss"][[7, 11]].isnan().all() and got["loss"].isnan().sum() == 2 and (got["d_hidden"][[7, 11]] == 0).all()
+    skip = t | {"targets": bad["targets"].where(bad["targets"] < 100, torch.tensor(-1, dtype=torch.int32, device="cuda"))}
+    want = call(losses, skip)
+    assert torch.equal(got["d_weight"], want["d_weight"])
+    t = make(20, 64, 100, BF16, BF16, entries=6, masked=0.0)
+    t["ids"][:, 2] = 100
+    t["ids"][5] = torch.tensor([100, 101, 2 ** 31 - 1, 100, -1, -2 ** 31], device="cuda")
+    got = call(losses, t, 2.0)
+    check(got, t, 2.0)
+    assert got["loss"][5] == 0 and (got["d_hidden"][5] == 0).all()
+
+
+@pytest.mark.parametrize("types", TYPES, ids=["f32", "f32_rows", "bf16"])
+def test_teacher_logits_at_the_ends_of_their_range(losses, types):
+    t = make(12, 64, 100, *types, entries=4, masked=0.0, seed=6)
+    t["ids"] = torch.arange(48, dtype=torch.int32, device="cuda").reshape(12, 4)
+    low = torch.finfo(F32).min
+    t["teacher"][0] = low                                                        # all at the lowest value: equal shares
+    t["teacher"][1] = torch.tensor([low, 1.0, 2.0, low])
+    t["teacher"][2] = torch.tensor([-math.inf, 1.0, -math.inf, 0.0])             # -inf: no entry
+    t["teacher"][3] = -math.inf                                                  # none left: the row does not count
+    t["teacher"][4] = torch.tensor([3e38, -3e38, 0.0, 1.0])
+    for temperature in (0.25, 1.0, 3.0):
+        got = call(losses, t, temperature)
+        check(got, t, temperature)
+        assert got["loss"][3] == 0 and (got["d_hidden"][3] == 0).all()
+
+
+@pytest.mark.parametrize("types", TYPES, ids=["f32", "f32_rows", "bf16"])
+def test_ids_listed_twice(losses, types):
+    t = make(30, 64, 50, *types, entries=8, masked=0.0, seed=7)
+    t["ids"][:, 4:] = t["ids"][:, :4]
+    t["ids"][3] = 9
+    check(call(losses, t), t)
+
+
+@pytest.mark.parametrize("types", TYPES, ids=["f32", "f32_rows", "bf16"])
+def test_logits_far_apart(losses, types):
+    """Logits of a standard deviation of 200: exp of them overflows by itself, and most probabilities are 0."""
+    t = make(40, 128, 700, *types, scale=100.0, seed=8)
+    check(call(losses, t), t, what=("loss", "lse"))
+    t = make(40, 128, 700, *types, scale=5.0, seed=8)
+    check(call(losses, t), t)
+
+
+def test_infinite_and_nan_inputs_that_count_show(losses):
+    for types in TYPES:
+        t = make(6, 64, 90, *types, masked=0.0)
+        t["hidden"][2, 5] = float("nan")
+        got = call(losses, t)
+        assert got["loss"].isnan().nonzero().flatten().tolist() == [2]
+        assert got["d_hidden"][2].isnan().all() and not got["d_hidden"][[0, 1, 3, 4, 5]].isnan().any()
+        t = make(6, 64, 90, *types, masked=0.0)
+        t["weight"][89, 0] = float("nan")
+        assert call(losses, t)["loss"].isnan().all()
+
+
+@pytest.mark.parametrize("types", TYPES, ids=["f32", "f32_rows", "bf16"])
+def test_rows_of_weight_zero_are_left_out_of_the_gradients(losses, types):
+    t = make(50, 64, 300, *types, masked=0.0, seed=9)
+    t["grad_loss"][::3] = 0
+    got = call(losses, t)
+    check(got, t)
+    assert (got["d_hidden"][::3] == 0).all()
+
+
+@pytest.mark.parametrize("types", TYPES, ids=["f32", "f32_rows", "bf16"])
+def test_either_gradient_alone_and_the_same_bits_again(losses, types):
+    t = make(150, 192, 2100, *types, entries=5, seed=10)
+    plan = losses.VocabLoss(400, 192, 2100, *types, max_entries=9)      # larger than the call
+    both = call(losses, t, 2.0, plan=plan)
+    check(both, t, 2.0)
+    plan.workspace.fill_(255)                                            # nothing in it outlives a call
+    again = call(losses, t, 2.0, plan=plan)
+    for k in both:
+        assert torch.equal(both[k], again[k]), k
+    only = call(losses, t, 2.0, plan=plan, d_weight=False)
+    assert only["d_weight"] is None and torch.equal(only["d_hidden"], both["d_hidden"])
+    only = call(losses, t, 2.0, plan=plan, d_hidden=False)
+    assert only["d_hidden"] is None and torch.equal(only["d_weight"], both["d_weight"])
+
+
+@pytest.mark.parametrize("entries", [0, 6])
+def test_gradients_against_differences(losses, entries):
+    """Central differences of the fp32 loss along a random direction of unit length: step e = 0.05. Truncation: e^2 / 6 times the third derivative; of a log-sum-exp of
+    logits whose slopes along the direction are s, that is at most 6 max|s|^3: e^2 max|s|^3 per row of weight 1. Rounding: 2 times the loss's own bound, over 2 e."""
+    t = make(9, 48, 120, F32, F32, entries=entries, seed=11)
+    temperature = 1.0 if not entries else 1.5
+    got = call(losses, t, temperature)
+    w = t["grad_loss"].double()
+    gen, e = torch.Generator(device="cuda").manual_seed(5), 0.05
+    for name, grad in (("hidden", got["d_hidden"]), ("weight", got["d_weight"])):
+        for _ in range(4):
+            u = torch.randn(t[name].shape, device="cuda", generator=gen)
+            u = (u / u.norm()).contiguous()
+            at = [dict(t) | {name: t[name] + s * e * u} for s in (1, -1)]
+            up, down = (float((call(losses, x, temperature)["loss"].double() * w).sum()) for x in at)
+            slope = ((u @ t["weight"].T) if name == "hidden" else (t["hidden"] @ u.T)).abs().amax(1).double() / temperature
+            _, bound = definition(t, temperature)
+            tol = float((w.abs() * (temperature ** 2 * e * e * slope ** 3)).sum()) + float((w.abs().cpu().numpy() * bound["loss"]).sum()) / e * 1.5
+            want = (up - down) / (2 * e)
+            assert abs(float((grad.double() * u.double()).sum()) - want) <= tol, (name, want, tol)
+
+
+@pytest.mark.parametrize("entries", [0, 6])
+def test_autograd(losses, entries):
+    t = make(60, 128, 400, BF16, BF16, entries=entries, seed=12)
+    want = call(losses, t, 1.0 if not entries else 2.0)
+    h, w = t["hidden"].clone().requires_grad_(), t["weight"].clone().requires_grad_()
+    plan = losses.VocabLoss(60, 128, 400, max_entries=max(1, entries))
+    loss = losses.distill(plan, h, w, t["ids"], t["teacher"], 2.0) if entries else losses.cross_entropy(plan, h, w, t["targets"])
+    (loss * t["grad_loss"]).sum().backward()
+    assert torch.equal(loss, want["loss"]) and torch.equal(h.grad, want["d_hidden"]) and torch.equal(w.grad, want["d_weight"])
+    w2 = t["weight"].clone().requires_grad_()                       # a frozen model's rows: only the head's gradient
+    loss = losses.cross_entropy(plan, t["hidden"], w2, t["targets"]) if not entries else losses.distill(plan, t["hidden"], w2, t["ids"], t["teacher"], 2.0)
+    (loss * t["grad_loss"]).sum().backward()
+    assert torch.equal(w2.grad, want["d_weight"])
+
+
+@pytest.mark.parametrize("types", [(F32, F32), (BF16, BF16)], ids=["f32", "bf16"])
+def test_another_stream_and_a_captured_graph(losses, types):
+    """Captured once and replayed on inputs that change in place, with eager work between the replays."""
+    t = make(100, 128, 1500, *types, entries=4, seed=13)
+    plan = losses.VocabLoss(100, 128, 1500, *types, max_entries=4)
+    want = call(losses, t, 2.0, plan=plan)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = call(losses, t, 2.0, plan=plan)
+    torch.cuda.current_stream().wait_stream(side)
+    for k in want:
+        assert torch.equal(got[k], want[k]), k
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        rec = call(losses, t, 2.0, plan=plan)
+    for turn in range(4):
+        fresh = make(100, 128, 1500, *types, entries=4, seed=20 + turn)
+        for k, v in fresh.items():
+            t[k].copy_(v)
+        want = call(losses, t, 2.0, plan=plan)
+        graph.replay()
+        torch.cuda.synchronize()
+        for k in want:
+            assert torch.equal(rec[k], want[k]), (turn, k)
+
+
+def test_refusals(losses):
+    from paper_2504_07878_amd import tokroute as tr
+    t = make(8, 64, 100, BF16, BF16)
+    plan = losses.VocabLoss(8, 64, 100, max_entries=2)
+    ce = lambda **kw: call(losses, t | kw, plan=plan)   # noqa: E731
+    for bad in (dict(hidden=t["hidden"].float()), dict(hidden=t["hidden"][:, :63]), dict(hidden=t["hidden"].t()), dict(weight=t["weight"][:99]), dict(weight=t["weight"].float()),
+                dict(targets=t["targets"].long()), dict(targets=t["targets"][:7]), dict(targets=t["targets"].cpu()), dict(grad_loss=t["grad_loss"].double()), dict(hidden=t["hidden"].cpu())):
+        with pytest.raises(ValueError):
+            ce(**bad)
+    with pytest.raises(ValueError):
+        losses.VocabLoss(8, 64, 100, torch.float16, torch.bfloat16)
+
+    def code(f):
+        with pytest.raises(tr.TokrouteError) as e:
+            f()
+        return e.value.code
+
+    assert code(lambda: losses.VocabLoss(8, 64, 100, BF16, F32)) == tr.ERR_SHAPE
+    for args in ((0, 64, 100), (8, 0, 100), (8, 64, 0), (8, 70000, 100), (1 << 21, 64, 100)):
+        assert code(lambda: losses.VocabLoss(*args)) == tr.ERR_SHAPE
+    assert code(lambda: losses.VocabLoss(8, 64, 100, max_entries=1025)) == tr.ERR_SHAPE
+    assert code(lambda: ce(hidden=t["hidden"][:1].expand(8, 64))) == tr.ERR_INVALID_ARG       # rows on top of each other
+    more = make(9, 64, 100, BF16, BF16)
+    assert code(lambda: call(losses, more, plan=plan)) == tr.ERR_CAPACITY
+    d = make(8, 64, 100, BF16, BF16, entries=3)
+    assert code(lambda: call(losses, d, plan=plan)) == tr.ERR_CAPACITY
+    d = make(8, 64, 100, BF16, BF16, entries=2)
+    for temperature in (0.0, -1.0, math.nan, math.inf):
+        assert code(lambda: call(losses, d, temperature, plan=plan)) == tr.ERR_INVALID_ARG
+    empty = d | {"ids": d["ids"][:, :0].contiguous(), "teacher": d["teacher"][:, :0].contiguous()}
+    assert code(lambda: call(losses, empty, plan=plan)) == tr.ERR_INVALID_ARG
+    import ctypes as C
+    lib, rows = plan.lib, plan._rows(t["hidden"], t["weight"], t["targets"])
+    out = torch.empty(8, device="cuda")
+    go = lambda ws, size, cfg=plan.cfg, r=rows, o=out.data_ptr(): lib.tr_cross_entropy(C.byref(cfg), ws, size, None, C.byref(r), o, o)   # noqa: E731
+    ws, size = plan.workspace.data_ptr(), plan.workspace.numel()
+    assert go(ws, size - 1) == tr.ERR_CAPACITY and go(ws + 8, size) == tr.ERR_INVALID_ARG and go(None, size) == tr.ERR_INVALID_ARG and go(ws, size, o=None) == tr.ERR_INVALID_ARG
+    odd = plan._rows(t["hidden"], t["weight"], t["targets"]); odd.weight += 1
+    assert go(ws, size, r=odd) == tr.ERR_INVALID_ARG
+    odd = plan._rows(t["hidden"], t["weight"], t["targets"]); odd.rows = -1
+    assert go(ws, size, r=odd) == tr.ERR_INVALID_ARG
+    none = tr.tr_loss_grads(None, None, 64, 64)
+    assert lib.tr_cross_entropy_grad(C.byref(plan.cfg), ws, size, None, C.byref(rows), out.data_ptr(), out.data_ptr(), C.byref(none)) == tr.OK    # nothing asked for
+    assert lib.tr_cross_entropy_grad(C.byref(plan.cfg), ws, size, None, C.byref(rows), out.data_ptr(), None, C.byref(none)) == tr.ERR_INVALID_ARG
+    call(losses, t, plan=plan)["loss"].cpu()                                                 # and the plan still works
+
+
+def test_sizes_of_the_small_models_head(losses):
+    """The real vocabulary, several pieces of it; rows past one block of them; against the definition on the GPU in 64 bits (loss of all rows, gradients by norm:
+    the bf16 roundings of this module's head, which add up at random over elements, 2^-9 / sqrt(3) relative in the mean each, three of them at most)."""
+    n, d, v = 300, 896, 151936
+    g = torch.Generator(device="cuda").manual_seed(1)
+    w = (torch.randn((v, d), device="cuda", generator=g) * 0.02).bfloat16()
+    ids = torch.randint(0, v, (n,), device="cuda", generator=g)
+    h = (torch.randn((n, d), device="cuda", generator=g) + w[ids].float() * 50 * torch.rand((n, 1), device="cuda", generator=g)).bfloat16()
+    t = {"hidden": h, "weight": w, "targets": torch.where(torch.arange(n, device="cuda") % 4 > 0, ids, -1).int(), "grad_loss": torch.rand(n, device="cuda", generator=g)}
+    got = call(losses, t)
+    on = t["targets"] >= 0
+    z = h.double() @ w.double().t()
+    lse = torch.logsumexp(z, 1)
+    loss = torch.where(on, lse - z.gather(1, ids[:, None])[:, 0], 0.0)
+    assert float((got["loss"].double() - loss).abs().max()) < 1e-4        # Z of the module's head: 125 u times sum |h w| < 30
+    dz = torch.exp(z - lse[:, None])
+    dz[torch.arange(n, device="cuda"), ids] -= 1
+    dz *= (t["grad_loss"].double() * on)[:, None]
+    for k, want in (("d_hidden", dz @ w.double()), ("d_weight", dz.t().contiguous() @ h.double())):
+        assert float((got[k].double() - want).norm() / want.norm()) < 3 * 2.0 ** -9 / math.sqrt(3), k
