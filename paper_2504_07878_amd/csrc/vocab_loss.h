@@ -2,7 +2,8 @@
 //
 // z[r][v] = k * hidden[r] . weight[v] (k = 1 / temperature), lse[r] = log sum_v exp z[r][v]. A row's loss compares softmax(z) with shares q over a few
 // listed entries of the vocabulary: one entry of share 1 (cross entropy), or the softmax of a teacher's logits (distillation). The gradient to the
-// products hidden . weight is g (p - q) per temperature, p = exp(z - lse); it exists only in pieces of the vocabulary, as a matrix G of the piece's p - q.
+// products hidden . weight is T g (p - q), p = exp(z - lse), g the row's weight; it exists only in pieces of the vocabulary, as a matrix G of the piece's
+// g / max |g| (p - q).
 //
 // Only rows that count take part: they are listed once per call (`idx`) and everything behind works on that list, so that masked rows cost nothing and
 // whatever their hidden rows hold reaches neither gradient.
@@ -34,10 +35,10 @@ struct LossArgs {
     int *idx;                     // [n_pad] rows that count, in order
     unsigned char *state;         // [rows] ROW_*
     float2 *part;                 // [blocks of the vocabulary][n_pad] running softmax (see Running)
-    float *value;                 // [n_pad][entries] products of the listed entries, then p - q
+    float *value;                 // [n_pad][entries] products of the listed entries, then what G has there
     void *G;                      // [n_pad][piece]
-    float *acc;                   // [splits][n_pad][d_pad] sums of the gradient to the hidden rows
-    void *hp, *hw;                // [n_pad][d_pad] rows that count, and the same by their share of the largest weight (bf16 products)
+    float *acc;                   // [splits][n_pad, or the blocks that count (bf16)][d_pad] sums of the gradient to the hidden rows
+    void *hp;                     // [n_pad][d_pad] rows that count (bf16 products)
     void *wp;                     // [piece][d_pad] rows of the head where they cannot be read as they lie
     int n_pad, d_pad, piece, splits;
     int n_block;                  // rows per block (bf16 products)
@@ -53,11 +54,11 @@ constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 void launch_loss_rows(hipStream_t s, const LossArgs &a);
 // lse and loss of the rows that count from `parts` running softmaxes each.
 void launch_loss_finish(hipStream_t s, const LossArgs &a, int parts);
-// From the products of the listed entries: p - q, and their places in G for one piece of the vocabulary.
+// From the products of the listed entries: what G has for them, and their places in G for one piece of the vocabulary.
 void launch_loss_values(hipStream_t s, const LossArgs &a);
 void launch_loss_scatter(hipStream_t s, const LossArgs &a, int v0, int vn, bool g_bf16);
-// The gradient to the hidden rows from `splits` sums, weighed and rounded; zeros for rows that do not count.
-void launch_loss_hidden_grad(hipStream_t s, const LossArgs &a, int splits);
+// The gradient to the hidden rows from the splits' sums (as the bf16 or the f32 products leave them), weighed and rounded; zeros for rows that do not count.
+void launch_loss_hidden_grad(hipStream_t s, const LossArgs &a, bool bf16);
 
 // Products of the listed entries, each the bits that the softmax's own products have: a probability near 1 and its logit then agree, and what is left of
 // 1 - p and of lse - z is not the difference of two roundings.
@@ -79,7 +80,8 @@ void launch_bf16_softmax(hipStream_t s, const LossArgs &a, int v0, int vn);
 void launch_bf16_probabilities(hipStream_t s, const LossArgs &a, int v0, int vn);
 void launch_bf16_hidden_grad(hipStream_t s, const LossArgs &a, int v0, int vn, bool first);
 void launch_bf16_weight_grad(hipStream_t s, const LossArgs &a, int v0, int vn);
-// splits of the sums of the gradient to `count` hidden rows, at most a.splits (both sides)
+__host__ __device__ inline int bf16_rows(const LossArgs &a, int count) { return (count + a.n_block - 1) / a.n_block * a.n_block; }   // whole blocks
+// splits of the sums of the gradient to `count` hidden rows, at most a.splits
 __host__ __device__ inline int bf16_splits(const LossArgs &a, int count)
 {
     const int tiles = (count + a.n_block - 1) / a.n_block * (a.d_pad / BF16_BLOCK + (a.d_pad % BF16_BLOCK ? 1 : 0));

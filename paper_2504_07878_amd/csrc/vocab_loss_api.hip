@@ -23,28 +23,40 @@ bool config_ok(const tr_loss_config *c)
 // Where everything lies in the workspace, for a configuration; the sizes of a call's own launches follow from its rows, never beyond these.
 struct Plan {
     int n_pad, d_pad, piece, splits;
-    size_t head, idx, state, part, value, G, acc, total;
+    size_t head, idx, state, part, value, G, acc, hp, wp, total;
 };
 
+bool is_bf16(const tr_loss_config *c) { return c->hidden_dtype == TR_BF16; }   // the products that run on bf16 matrix instructions
+
+// Rows of G times its columns stay at 256 MB or less (what the caches beyond L2 hold, so that a piece is read back from there), but a piece has 2048 columns at least.
+// Splits of the sums of the gradient to the hidden rows: as many as give every compute unit a block.
 Plan plan_of(const tr_loss_config *c)
 {
     Plan p{};
-    const size_t g_size = 4;
-    p.n_pad = (int)up(c->max_rows, F32_BLOCK);
-    p.d_pad = (int)up(c->dim, F32_BLOCK);
-    const size_t vocab = up(c->vocab, F32_BLOCK);
-    p.piece = (int)std::min(vocab, std::max<size_t>(2048, (256u << 20) / g_size / p.n_pad / F32_BLOCK * F32_BLOCK));
-    const int tiles = p.n_pad / F32_BLOCK * (p.d_pad / F32_BLOCK);
-    p.splits = std::max(1, std::min(512 / tiles, p.piece / 256));
+    const bool half = is_bf16(c);
+    const int block = half ? BF16_BLOCK : F32_BLOCK;
+    const size_t g_size = half ? 2 : 4;
+    p.n_pad = (int)up(c->max_rows, block);
+    p.d_pad = (int)up(c->dim, half ? 64 : F32_BLOCK);
+    const size_t vocab = up(c->vocab, block);
+    p.piece = (int)std::min(vocab, std::max<size_t>(2048, (256u << 20) / g_size / p.n_pad / block * block));
+    const int tiles = (int)(up(p.d_pad, block) / block) * (half ? 1 : p.n_pad / F32_BLOCK);
+    p.splits = std::max(1, std::min((half ? 256 : 512) / tiles, p.piece / 256));
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t was = at; at += up(bytes, 256); return was; };
     p.head = take(sizeof(LossHead));
     p.idx = take((size_t)p.n_pad * 4);
     p.state = take(c->max_rows);
-    p.part = take(vocab / F32_BLOCK * p.n_pad * sizeof(float2));
+    p.part = take(vocab / block * p.n_pad * sizeof(float2));
     p.value = take((size_t)p.n_pad * c->max_entries * 4);
     p.G = take((size_t)p.n_pad * p.piece * g_size);
-    p.acc = take((size_t)p.splits * p.n_pad * p.d_pad * 4);
+    // bf16: (blocks along the rows) * splits * (blocks along the features) <= 256, or splits = 1
+    const size_t sums = half ? std::max<size_t>(p.n_pad, (size_t)(256 / std::min(256, tiles)) * BF16_BLOCK) : (size_t)p.splits * p.n_pad;
+    p.acc = take(sums * p.d_pad * 4);
+    if (half) {
+        p.hp = take((size_t)p.n_pad * p.d_pad * 2);
+        p.wp = take((size_t)p.piece * p.d_pad * 2);
+    }
     p.total = at;
     return p;
 }
@@ -72,6 +84,11 @@ int arguments(const tr_loss_config *c, const tr_loss_rows *in, void *ws, size_t 
     a.entries = teacher ? in->entries : 1; a.ids = in->ids; a.teacher = teacher ? in->teacher : nullptr; a.temperature = teacher ? in->temperature : 1.f;
     a.head = (LossHead *)(b + p.head); a.idx = (int *)(b + p.idx); a.state = (unsigned char *)(b + p.state); a.part = (float2 *)(b + p.part);
     a.value = (float *)(b + p.value); a.G = b + p.G; a.acc = (float *)(b + p.acc);
+    if (is_bf16(c)) {
+        a.hp = b + p.hp; a.wp = b + p.wp;
+        a.n_block = a.rows <= 64 ? 64 : a.rows <= 128 ? 128 : 256;
+        a.direct = a.dim % 64 == 0 && a.ws % 8 == 0 && a.ws < (1 << 22) && (reinterpret_cast<uintptr_t>(a.weight) & 15) == 0;
+    }
     a.n_pad = p.n_pad; a.d_pad = p.d_pad; a.piece = p.piece; a.splits = p.splits;
     return TR_OK;
 }
@@ -88,9 +105,19 @@ int forward(const tr_loss_config *c, void *ws, size_t ws_bytes, void *stream, co
     a.loss = loss; a.lse = lse;
     hipStream_t s = (hipStream_t)stream;
     launch_loss_rows(s, a);
-    launch_f32_softmax(s, a);
-    launch_f32_entries(s, a);
-    launch_loss_finish(s, a, (a.vocab + F32_BLOCK - 1) / F32_BLOCK);
+    if (is_bf16(c)) {
+        launch_bf16_pack_rows(s, a);
+        for (int v0 = 0, vn; v0 < a.vocab; v0 += vn) {
+            vn = a.direct ? a.vocab : std::min(a.piece, a.vocab - v0);
+            if (!a.direct) launch_bf16_pack_head(s, a, v0, vn);
+            launch_bf16_softmax(s, a, v0, vn);
+        }
+        launch_bf16_entries(s, a);
+    } else {
+        launch_f32_softmax(s, a);
+        launch_f32_entries(s, a);
+    }
+    launch_loss_finish(s, a, (a.vocab + (is_bf16(c) ? BF16_BLOCK : F32_BLOCK) - 1) / (is_bf16(c) ? BF16_BLOCK : F32_BLOCK));
     return enqueued();
 }
 
@@ -108,16 +135,30 @@ int backward(const tr_loss_config *c, void *ws, size_t ws_bytes, void *stream, c
     a.d_hidden = out->d_hidden; a.dhs = out->d_hidden_stride; a.d_weight = out->d_weight; a.dws = out->d_weight_stride;
     hipStream_t s = (hipStream_t)stream;
     launch_loss_rows(s, a);
-    launch_f32_entries(s, a);
+    const bool half = is_bf16(c);
+    if (half && a.rows) {
+        launch_bf16_pack_rows(s, a);
+        launch_bf16_entries(s, a);
+    } else if (a.rows) launch_f32_entries(s, a);
     launch_loss_values(s, a);
     for (int v0 = 0; v0 < a.vocab; v0 += a.piece) {
         const int vn = std::min(a.piece, a.vocab - v0);
-        launch_f32_probabilities(s, a, v0, vn);
-        launch_loss_scatter(s, a, v0, vn, false);
-        if (a.d_hidden) launch_f32_hidden_grad(s, a, v0, vn, v0 == 0);
-        if (a.d_weight) launch_f32_weight_grad(s, a, v0, vn);
+        if (half) {
+            if (a.rows) {
+                if (!a.direct) launch_bf16_pack_head(s, a, v0, vn);
+                launch_bf16_probabilities(s, a, v0, vn);
+                launch_loss_scatter(s, a, v0, vn, true);
+                if (a.d_hidden) launch_bf16_hidden_grad(s, a, v0, vn, v0 == 0);
+            }
+            if (a.d_weight) launch_bf16_weight_grad(s, a, v0, vn);
+        } else {
+            launch_f32_probabilities(s, a, v0, vn);
+            launch_loss_scatter(s, a, v0, vn, false);
+            if (a.d_hidden) launch_f32_hidden_grad(s, a, v0, vn, v0 == 0);
+            if (a.d_weight) launch_f32_weight_grad(s, a, v0, vn);
+        }
     }
-    if (a.d_hidden) launch_loss_hidden_grad(s, a, a.splits);
+    if (a.d_hidden) launch_loss_hidden_grad(s, a, half);
     return enqueued();
 }
 

@@ -5,7 +5,7 @@
 // both operands go through registers into LDS as [k][row], the next step's are requested before this step's products. Three products:
 //   softmax, probabilities: m = vocabulary entry, n = row that counts, k = feature
 //   gradient to the hidden rows: m = feature, n = row, k = vocabulary entry of the piece; summed over the pieces in `acc`, one sum per split of k
-//   gradient to the head: m = feature, n = vocabulary entry, k = row; rows weighed as they are read
+//   gradient to the head: m = feature, n = vocabulary entry, k = row
 #include "vocab_loss_epilogues.h"
 
 namespace tr {
@@ -35,15 +35,10 @@ struct PieceRows {                             // G[n][k]
     const float *g; int ld, count, vn;
     __device__ __forceinline__ float at(int n, int k) const { return n < count && k < vn ? g[(size_t)n * ld + k] : 0.f; }
 };
-template <class HT> struct HiddenColumns {     // weight of the row * hidden[idx[k]][m]
+template <class HT> struct HiddenColumns {     // hidden[idx[k]][m]
     static constexpr bool contiguous_k = false;
-    const HT *h; long long hs; const int *idx; const float *grad; int count, d; float rscale;
-    __device__ __forceinline__ float at(int m, int k) const
-    {
-        if (m >= d || k >= count) return 0.f;
-        const int r = idx[k];
-        return (grad[r] * rscale) * load_one(h + r * hs + m);
-    }
+    const HT *h; long long hs; const int *idx; int count, d;
+    __device__ __forceinline__ float at(int m, int k) const { return m < d && k < count ? load_one(h + idx[k] * hs + m) : 0.f; }
 };
 struct PieceColumns {                          // G[k][n]
     static constexpr bool contiguous_k = false;
@@ -141,9 +136,9 @@ template <class HT, class WT> __global__ __launch_bounds__(256) void f32_probabi
     each_run(c, [&](int n, int m, float (&v)[8]) {
         n += n0; m += m0;
         if (n >= count) return;
-        const float lse = a.lse[a.idx[n]];
+        const float lse = a.lse[a.idx[n]], weight = a.grad[a.idx[n]] / a.head->scale;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = m + e < vn ? expf(fmaf(v[e], k, -lse)) : 0.f;
+        for (int e = 0; e < 8; ++e) v[e] = m + e < vn ? weight * expf(fmaf(v[e], k, -lse)) : 0.f;
         store_run((float *)a.G + (size_t)n * a.piece + m, v);
     });
 }
@@ -174,12 +169,11 @@ template <class HT, class WT> __global__ __launch_bounds__(256) void f32_weight_
 {
     __shared__ Tiles sm;
     const int m0 = blockIdx.x * F32_BLOCK, n0 = blockIdx.y * F32_BLOCK, count = a.head->count;
-    const float scale = a.head->scale;
-    const HiddenColumns<HT> A{(const HT *)a.hidden, a.hs, a.idx, a.grad, count, a.dim, 1.0f / scale};
+    const HiddenColumns<HT> A{(const HT *)a.hidden, a.hs, a.idx, count, a.dim};
     const PieceColumns B{(const float *)a.G, a.piece, count, vn};
     f32x16 c[2][2];
     products(A, B, m0, n0, 0, count, sm, c);
-    const float k = scale * a.temperature;
+    const float k = a.head->scale * a.temperature;
     each_run(c, [&](int n, int m, float (&v)[8]) {
         n += n0; m += m0;
         if (n >= vn) return;
@@ -232,8 +226,7 @@ int blocks(int n) { return (n + F32_BLOCK - 1) / F32_BLOCK; }
 
 template <class Go> void by_types(const LossArgs &a, Go go)
 {
-    if (a.hdt == DT_BF16) go(bf16_t{}, bf16_t{});
-    else if (a.wdt == DT_BF16) go(float{}, bf16_t{});
+    if (a.wdt == DT_BF16) go(float{}, bf16_t{});
     else go(float{}, float{});
 }
 

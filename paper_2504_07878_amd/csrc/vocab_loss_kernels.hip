@@ -28,8 +28,9 @@ __global__ __launch_bounds__(256) void loss_state_kernel(LossArgs a)
     a.state[r] = (unsigned char)st;
 }
 
-// One workgroup lists the rows that count, in order, 1024 rows at a time; the rows that do not get their loss here. The largest |weight| of a row that counts
-// is what the rows' weights are taken relative to in the gradient of the head: rows of equal weight then enter it unchanged.
+// One workgroup lists the rows that count, in order, 1024 rows at a time; the rows that do not get their loss here. The rows' weights in the
+// gradients are taken relative to the largest |weight|, by which the gradients are multiplied at the end: with equal weights G then holds p - q itself, whose
+// 0 - 1 has no rounding.
 __global__ __launch_bounds__(1024) void loss_list_kernel(LossArgs a)
 {
     __shared__ int sums[16];
@@ -142,14 +143,14 @@ __global__ __launch_bounds__(256) void loss_finish_kernel(LossArgs a, int parts)
     }
 }
 
-// p - q of every listed entry of a row from its product (an id listed twice: p less both shares, in both places)
+// p - q of every listed entry of a row from its product (an id listed twice: p less both shares, in both places), by the row's weight
 template <bool TEACHER>
 __global__ __launch_bounds__(256) void loss_values_kernel(LossArgs a)
 {
     const int i = blockIdx.x;
     if (i >= a.head->count) return;
     const int r = a.idx[i];
-    const float lse = a.lse[r], k = 1.0f / a.temperature;
+    const float lse = a.lse[r], k = 1.0f / a.temperature, weight = a.grad[r] / a.head->scale;
     const Shares sh = shares_of<TEACHER>(a, r);
     const long long at0 = (long long)r * a.entries;
     for (int j = threadIdx.x; j < a.entries; j += 256) {
@@ -162,7 +163,7 @@ __global__ __launch_bounds__(256) void loss_values_kernel(LossArgs a)
                 if (a.ids[at0 + o] == id && entry_counts<TEACHER>(a, at0 + o)) q += expf((a.teacher[at0 + o] - sh.top) / a.temperature) / sh.total;
         }
         float &v = a.value[(size_t)i * a.entries + j];
-        v = expf(fmaf(v, k, -lse)) - q;
+        v = weight * (expf(fmaf(v, k, -lse)) - q);
     }
 }
 
@@ -207,18 +208,19 @@ void launch_loss_scatter(hipStream_t s, const LossArgs &a, int v0, int vn, bool 
 
 // ------------------------------------------------------------------ gradient to the hidden rows
 
-// rows that do not count are cleared by `clear`, the others written from their sums (in order of the splits)
-template <class HT>
-__global__ __launch_bounds__(256) void hidden_grad_kernel(LossArgs a, int splits)
+// a workgroup writes the i-th row that counts from its sums, in order of the splits, and clears row i if that does not count
+template <class HT, bool BF16>
+__global__ __launch_bounds__(256) void hidden_grad_kernel(LossArgs a)
 {
-    const int i = blockIdx.x;
-    if (i < a.head->count) {
-        const int r = a.idx[i];
-        const float c = a.grad[r] * a.temperature;
+    const int i = blockIdx.x, count = a.head->count;
+    if (i < count) {
+        const int r = a.idx[i], splits = BF16 ? bf16_splits(a, count) : a.splits;
+        const size_t apart = (size_t)(BF16 ? bf16_rows(a, count) : a.n_pad) * a.d_pad;
+        const float c = a.head->scale * a.temperature;
         HT *out = (HT *)a.d_hidden + (long long)r * a.dhs;
         for (int j = threadIdx.x; j < a.dim; j += 256) {
             float v = 0.f;
-            for (int p = 0; p < splits; ++p) v += a.acc[((size_t)p * a.n_pad + i) * a.d_pad + j];
+            for (int p = 0; p < splits; ++p) v += a.acc[p * apart + (size_t)i * a.d_pad + j];
             store_one(out + j, c * v);
         }
     }
@@ -228,11 +230,11 @@ __global__ __launch_bounds__(256) void hidden_grad_kernel(LossArgs a, int splits
     }
 }
 
-void launch_loss_hidden_grad(hipStream_t s, const LossArgs &a, int splits)
+void launch_loss_hidden_grad(hipStream_t s, const LossArgs &a, bool bf16)
 {
     if (!a.rows) return;
-    if (a.hdt == DT_BF16) hipLaunchKernelGGL((hidden_grad_kernel<bf16_t>), dim3(a.rows), dim3(256), 0, s, a, splits);
-    else hipLaunchKernelGGL((hidden_grad_kernel<float>), dim3(a.rows), dim3(256), 0, s, a, splits);
+    if (bf16) hipLaunchKernelGGL((hidden_grad_kernel<bf16_t, true>), dim3(a.rows), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((hidden_grad_kernel<float, false>), dim3(a.rows), dim3(256), 0, s, a);
 }
 
 }  // namespace tr
