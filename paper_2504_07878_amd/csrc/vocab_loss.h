@@ -34,13 +34,13 @@ struct LossArgs {
     LossHead *head;
     int *idx;                     // [n_pad] rows that count, in order
     unsigned char *state;         // [rows] ROW_*
-    float2 *part;                 // [blocks of the vocabulary][n_pad] running softmax (see Running)
+    float2 *part;                 // [parts of the vocabulary][part_ld] running softmaxes
     float *value;                 // [n_pad][entries] products of the listed entries, then what G has there
     void *G;                      // [n_pad][piece]
     float *acc;                   // [splits][n_pad, or the blocks that count (bf16)][d_pad] sums of the gradient to the hidden rows
     void *hp;                     // [n_pad][d_pad] rows that count (bf16 products)
     void *wp;                     // [piece][d_pad] rows of the head where they cannot be read as they lie
-    int n_pad, d_pad, piece, splits;
+    int n_pad, d_pad, piece, splits, part_ld;
     int n_block;                  // rows per block (bf16 products)
     bool direct;                  // the head is read as it lies (bf16 products): rows on 16 bytes, whole steps of 64 features
 };
@@ -77,6 +77,7 @@ constexpr int BF16_BLOCK = 256;
 void launch_bf16_pack_rows(hipStream_t s, const LossArgs &a);
 void launch_bf16_pack_head(hipStream_t s, const LossArgs &a, int v0, int vn);
 void launch_bf16_softmax(hipStream_t s, const LossArgs &a, int v0, int vn);
+int bf16_softmax_parts(const LossArgs &a);
 void launch_bf16_probabilities(hipStream_t s, const LossArgs &a, int v0, int vn);
 void launch_bf16_hidden_grad(hipStream_t s, const LossArgs &a, int v0, int vn, bool first);
 void launch_bf16_weight_grad(hipStream_t s, const LossArgs &a, int v0, int vn);

@@ -47,7 +47,7 @@ Plan plan_of(const tr_loss_config *c)
     p.head = take(sizeof(LossHead));
     p.idx = take((size_t)p.n_pad * 4);
     p.state = take(c->max_rows);
-    p.part = take(vocab / block * p.n_pad * sizeof(float2));
+    p.part = take(vocab / block * 2 * p.n_pad * sizeof(float2));   // two wavefronts' parts a block of 256 rows; four of 128 or eight of 64
     p.value = take((size_t)p.n_pad * c->max_entries * 4);
     p.G = take((size_t)p.n_pad * p.piece * g_size);
     // bf16: (blocks along the rows) * splits * (blocks along the features) <= 256, or splits = 1
@@ -84,12 +84,13 @@ int arguments(const tr_loss_config *c, const tr_loss_rows *in, void *ws, size_t 
     a.entries = teacher ? in->entries : 1; a.ids = in->ids; a.teacher = teacher ? in->teacher : nullptr; a.temperature = teacher ? in->temperature : 1.f;
     a.head = (LossHead *)(b + p.head); a.idx = (int *)(b + p.idx); a.state = (unsigned char *)(b + p.state); a.part = (float2 *)(b + p.part);
     a.value = (float *)(b + p.value); a.G = b + p.G; a.acc = (float *)(b + p.acc);
+    a.n_pad = a.part_ld = p.n_pad; a.d_pad = p.d_pad; a.piece = p.piece; a.splits = p.splits;
     if (is_bf16(c)) {
         a.hp = b + p.hp; a.wp = b + p.wp;
         a.n_block = a.rows <= 64 ? 64 : a.rows <= 128 ? 128 : 256;
+        if (a.n_block < 256) a.part_ld = a.n_block;   // more parts, of fewer rows
         a.direct = a.dim % 64 == 0 && a.ws % 8 == 0 && a.ws < (1 << 22) && (reinterpret_cast<uintptr_t>(a.weight) & 15) == 0;
     }
-    a.n_pad = p.n_pad; a.d_pad = p.d_pad; a.piece = p.piece; a.splits = p.splits;
     return TR_OK;
 }
 
@@ -117,7 +118,7 @@ int forward(const tr_loss_config *c, void *ws, size_t ws_bytes, void *stream, co
         launch_f32_softmax(s, a);
         launch_f32_entries(s, a);
     }
-    launch_loss_finish(s, a, (a.vocab + (is_bf16(c) ? BF16_BLOCK : F32_BLOCK) - 1) / (is_bf16(c) ? BF16_BLOCK : F32_BLOCK));
+    launch_loss_finish(s, a, is_bf16(c) ? bf16_softmax_parts(a) : (a.vocab + F32_BLOCK - 1) / F32_BLOCK * 2);
     return enqueued();
 }
 

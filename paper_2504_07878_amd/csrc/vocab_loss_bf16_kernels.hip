@@ -19,27 +19,35 @@ namespace {
 constexpr int BK = 64;                 // k per step
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 
+__device__ __forceinline__ int wavefront() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+
 __device__ __forceinline__ void load_to_lds(uint32_t lds, uint32_t lane_off, const char *base)
 {
     asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"{m0}"(lds), "v"(lane_off), "s"(base) : "memory");
 }
-// own loads have landed, own LDS reads are done, then the workgroup's barrier
-__device__ __forceinline__ void landed_and_barrier()
+// own loads but the youngest N have landed, own LDS reads are done, then the workgroup's barrier
+template <int N> __device__ __forceinline__ void landed_and_barrier()
 {
     asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt((0 & 15) | (7 << 4) | (0 << 8));   // vmcnt 0, expcnt 7 (no wait), lgkmcnt 0
+    __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (0 << 8) | ((N >> 4) << 14));   // vmcnt N, expcnt 7 (no wait), lgkmcnt 0
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
 
-// One operand's tile of T rows of its dimension x 64 k in LDS. KC: k contiguous in memory, LDS [row][64 k]; otherwise [64 k][T]. FEAT: rows are read in
-// the order of the matrix instruction's output runs (tile_feature). WAVES share the copying.
-template <int T, bool KC, bool FEAT, int WAVES> struct Tile {
+// How the pieces of a line of a tile are permuted (exclusive or). LDS has 64 banks of 4 bytes: the 16 lanes that a 16-byte read serves at a time have to meet 16
+// different pieces of 256 bytes, two lines of 64 k; the 32 lanes of an 8-byte read 8 different pieces of 32 bytes, from 4 lines of 16 columns twice. (Keyed by the
+// lowest bits of the line instead, half of all LDS cycles were conflicts.)
+__device__ __forceinline__ int row_key(int row) { return (row >> 1) & 7; }
+__device__ __forceinline__ int k_key(int k) { return ((k & 3) << 1) ^ ((k >> 3) & 1); }
+
+__device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14)); }   // lgkmcnt 0
+template <int N> __device__ __forceinline__ void wait_all_but() { __builtin_amdgcn_s_waitcnt(N | (7 << 4) | (0 << 8)); }   // vmcnt N < 16 and lgkmcnt 0
+
+// One operand's tile of T rows of its dimension x 64 k in LDS. KC: k contiguous in memory, LDS [row][64 k]; otherwise [64 k][T]. WAVES share the copying.
+template <int T, bool KC, int WAVES> struct Tile {
     static constexpr int BYTES = T * BK * 2, COPIES = BYTES / 1024 / WAVES;
     static_assert(BYTES % (1024 * WAVES) == 0, "whole copies");
-    static constexpr int MASK = T >= 256 ? 7 : T / 16 - 1;   // 32-byte pieces of a row of T elements that are permuted
-
-    static __device__ __forceinline__ int key(int row) { return FEAT ? (row & 3) | ((row >> 1) & 4) : row & 7; }
+    static_assert(KC || T >= 128, "eight pieces of 32 bytes a line");
 
     uint32_t off[COPIES], krow[COPIES];
     const char *base;
@@ -48,7 +56,7 @@ template <int T, bool KC, bool FEAT, int WAVES> struct Tile {
     // p: element (first row, first k) of the operand; ld: elements from one line of memory to the next; limit: rows (KC) or columns that exist from p on
     __device__ __forceinline__ void init(const bf16_t *p, long long ld_elems, int limit)
     {
-        const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+        const int lane = threadIdx.x & 63, w = wavefront();
         base = (const char *)p;
         ld = (uint32_t)ld_elems * 2;
         advance = KC ? BK * 2 : BK * ld;
@@ -56,11 +64,11 @@ template <int T, bool KC, bool FEAT, int WAVES> struct Tile {
         for (int q = 0; q < COPIES; ++q) {
             const int g = w * COPIES + q;
             if (KC) {
-                const int row = g * 8 + (lane >> 3), piece = (lane & 7) ^ key(row);
+                const int row = g * 8 + (lane >> 3), piece = (lane & 7) ^ row_key(row);
                 off[q] = (uint32_t)min(row, limit - 1) * ld + piece * 16;
                 krow[q] = 0;
             } else {
-                const int at = g * 1024 + lane * 16, k = at / (T * 2), in = at % (T * 2), piece = (in >> 5) ^ (k & MASK), col = piece * 16 + ((in >> 4) & 1) * 8;
+                const int at = g * 1024 + lane * 16, k = at / (T * 2), in = at % (T * 2), piece = (in >> 5) ^ k_key(k), col = piece * 16 + ((in >> 4) & 1) * 8;
                 krow[q] = k;
                 off[q] = (uint32_t)min(col, limit - 8) * 2;
             }
@@ -69,28 +77,28 @@ template <int T, bool KC, bool FEAT, int WAVES> struct Tile {
     // copies of the next step into LDS at byte `lds`; kleft: lines that are left (read only where k runs from row to row)
     __device__ __forceinline__ void issue(uint32_t lds, int kleft)
     {
-        const int w = threadIdx.x >> 6;
+        const int w = wavefront();
 #pragma unroll
         for (int q = 0; q < COPIES; ++q) {
             uint32_t o = off[q];
             if (!KC) o += min(krow[q], (uint32_t)(kleft - 1)) * ld;
-            load_to_lds(__builtin_amdgcn_readfirstlane(lds + (w * COPIES + q) * 1024), o, base);
+            load_to_lds(lds + (w * COPIES + q) * 1024, o, base);
         }
         base += advance;
     }
 };
 
-// Reads matrix operands from a tile: N of them, of 32 rows each, from row r0 on; step kk of 16 k.
+// Reads matrix operands from a tile: N of them, of 32 rows each, from row r0 on; step kk of 16 k. FEAT: rows in the order of the matrix instruction's output
+// runs (tile_feature).
 template <int T, bool KC, bool FEAT, int N> struct Reader {
-    static constexpr int MASK = T >= 256 ? 7 : T / 16 - 1;
-    uint32_t at[KC ? 4 : 2 * N];
+    uint32_t at[KC ? BK / 16 : 2 * N];
     __device__ __forceinline__ void init(int r0)
     {
         const int lane = threadIdx.x & 63, hf = lane >> 5;
         if (KC) {
-            const int in = lane & 31, row = r0 + (FEAT ? tile_feature(in) : in), key = FEAT ? (row & 3) | ((row >> 1) & 4) : row & 7;
+            const int in = lane & 31, row = r0 + (FEAT ? tile_feature(in) : in), key = row_key(row);
 #pragma unroll
-            for (int kk = 0; kk < 4; ++kk) at[kk] = row * (BK * 2) + (((kk * 2 + hf) ^ key) << 4);
+            for (int kk = 0; kk < BK / 16; ++kk) at[kk] = row * (BK * 2) + (((kk * 2 + hf) ^ key) << 4);
         } else {
             // groups of 16 lanes turn 4 (k) x 16 elements; lane 4 r + c brings k = r, columns of quad c, and gets its own column's four k
             const int g = (lane >> 4) & 1, r = (lane >> 2) & 3, c = lane & 3, quad = FEAT ? 2 * (c & 1) + (c >> 1) : c;
@@ -99,7 +107,7 @@ template <int T, bool KC, bool FEAT, int N> struct Reader {
 #pragma unroll
                 for (int n = 0; n < N; ++n) {
                     const int k = 4 * t + r, piece = (r0 >> 4) + 2 * n + g;
-                    at[t * N + n] = (8 * hf + k) * (T * 2) + ((piece ^ (k & MASK)) << 5) + quad * 8;
+                    at[t * N + n] = (8 * hf + k) * (T * 2) + ((piece ^ k_key(8 * hf + k)) << 5) + quad * 8;
                 }
         }
     }
@@ -119,12 +127,13 @@ template <int T, bool KC, bool FEAT, int N> struct Reader {
     }
 };
 
-// Block of WM x WN wavefronts, each MI x NI accumulators; A_KC, B_KC: where the operands have k contiguous.
-template <int WM_, int WN_, int MI_, int NI_, bool A_KC, bool B_KC> struct Block {
+// One block by WM x WN wavefronts, each MI x NI accumulators; A_KC, B_KC: where the operands have k contiguous. A ring of STAGES steps in LDS, one barrier a
+// step; the matrix operands of 16 k are read one such step ahead. For blocks of few rows, which are bound by reading the head.
+template <int WM_, int WN_, int MI_, int NI_, int STAGES, bool A_KC, bool B_KC> struct Block {
     static constexpr int WM = WM_, WN = WN_, MI = MI_, NI = NI_, WAVES = WM * WN, TM = WM * MI * 32, TN = WN * NI * 32;
-    using TA = Tile<TM, A_KC, true, WAVES>;
-    using TB = Tile<TN, B_KC, false, WAVES>;
-    static constexpr int STAGE = TA::BYTES + TB::BYTES, LDS = 2 * STAGE;
+    using TA = Tile<TM, A_KC, WAVES>;
+    using TB = Tile<TN, B_KC, WAVES>;
+    static constexpr int STAGE = TA::BYTES + TB::BYTES, LDS = STAGES * STAGE;
 
     TA a;
     TB b;
@@ -133,7 +142,7 @@ template <int WM_, int WN_, int MI_, int NI_, bool A_KC, bool B_KC> struct Block
     // K: k in all; whole steps are copied, and what lies past K in the last has to be zero in one operand and finite in the other
     __device__ __forceinline__ void run(uint32_t lds, int K)
     {
-        const int w = threadIdx.x >> 6, wm = w / WN, wn = w % WN, steps = (K + BK - 1) / BK;
+        const int w = wavefront(), wm = w / WN, wn = w % WN, steps = (K + BK - 1) / BK;
 #pragma unroll
         for (int i = 0; i < MI; ++i)
 #pragma unroll
@@ -158,12 +167,17 @@ template <int WM_, int WN_, int MI_, int NI_, bool A_KC, bool B_KC> struct Block
 #pragma unroll
                 for (int j = 0; j < NI; ++j) c[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xa[p][i], xb[p][j], c[i][j], 0, 0, 0);
         };
-        issue(0);
-        landed_and_barrier();
-        if (steps > 1) issue(1);
+        constexpr int COPIES = TA::COPIES + TB::COPIES;
+        int next = 0;
+#pragma unroll
+        for (int p = 0; p < STAGES; ++p)
+            if (p < steps) issue(next++);
+        if (steps >= STAGES) landed_and_barrier<(STAGES - 1) * COPIES>();
+        else landed_and_barrier<0>();
         uint32_t at = lds;
         ra.template read<0>(at, xa[0]);
         rb.template read<0>(at + TA::BYTES, xb[0]);
+        int stage = 0;
 #pragma unroll 1
         for (int s = 0; s < steps; ++s) {
             ra.template read<1>(at, xa[1]); rb.template read<1>(at + TA::BYTES, xb[1]);
@@ -173,47 +187,62 @@ template <int WM_, int WN_, int MI_, int NI_, bool A_KC, bool B_KC> struct Block
             ra.template read<3>(at, xa[1]); rb.template read<3>(at + TA::BYTES, xb[1]);
             multiply(0);
             // every wavefront holds the step's last operands: its buffer is free, and the next step's has landed
-            landed_and_barrier();
-            if (s + 2 < steps) issue(s & 1);
-            at = lds + ((s + 1) & 1) * STAGE;
+            if (s + STAGES <= steps) landed_and_barrier<(STAGES - 2) * COPIES>();
+            else landed_and_barrier<0>();
+            if (s + STAGES < steps) issue(stage);
+            stage = stage + 1 < STAGES ? stage + 1 : 0;
+            at = lds + stage * STAGE;
             if (s + 1 < steps) { ra.template read<0>(at, xa[0]); rb.template read<0>(at + TA::BYTES, xb[0]); }
             multiply(1);
         }
     }
 
-    // f(accumulator along n, n, first m of a run of 8, the run)
-    template <class F> __device__ __forceinline__ void each_run(F f) const
-    {
-        const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, wm = w / WN, wn = w % WN;
-#pragma unroll
-        for (int j = 0; j < NI; ++j)
-#pragma unroll
-            for (int i = 0; i < MI; ++i)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    float v[8];
-                    run_of(c[i][j], h, v);
-                    f(j, (wn * NI + j) * 32 + (lane & 31), (wm * MI + i) * 32 + 16 * h + 8 * (lane >> 5), v);
-                }
-    }
 };
+
+// f(accumulator along n, n, first m of a run of 8, the run) of a wavefront's part of a block
+template <int WN, int MI, int NI, class F> __device__ __forceinline__ void each_run(const f32x16 (&c)[MI][NI], F f)
+{
+    const int lane = threadIdx.x & 63, w = wavefront(), wm = w / WN, wn = w % WN;
+#pragma unroll
+    for (int j = 0; j < NI; ++j)
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float v[8];
+                run_of(c[i][j], h, v);
+                f(j, (wn * NI + j) * 32 + (lane & 31), (wm * MI + i) * 32 + 16 * h + 8 * (lane >> 5), v);
+            }
+}
 
 extern __shared__ char dynamic_lds[];
 __device__ __forceinline__ uint32_t lds_start() { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)dynamic_lds; }
 
-// Which block a workgroup computes. Workgroup b runs on XCD b mod 8, whose workgroups take a contiguous piece of an order that walks groups of GN blocks along n and, in
-// a group, along m: those that run at a time share GN tiles of one operand and a few of the other in the XCD's L2. false: none.
-constexpr int GN = 8;
-__device__ __forceinline__ bool block_of(int mb, int nb, int &m, int &n)
-{
-    const int items = mb * nb, per = (items + 7) >> 3, at = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-    if ((int)(blockIdx.x >> 3) >= per || at >= items) return false;
-    const int group = at / (GN * mb), in = at - group * GN * mb, width = min(GN, nb - group * GN);
-    m = in / width;
-    n = group * GN + in % width;
-    return true;
-}
-dim3 grid_of(int mb, int nb) { return dim3((mb * nb + 7) / 8 * 8); }
+// The order in which blocks are taken. Workgroup b runs on XCD b mod 8, whose workgroups take a contiguous piece of an order that walks groups of GN blocks along n
+// and, in a group, along m: those that run at a time share GN tiles of one operand and a few of the other in the XCD's L2.
+#ifndef XGN
+#define XGN 8
+#endif
+constexpr int GN = XGN;
+struct Order {
+    int mb, nb, items, per;
+    __device__ __forceinline__ Order(int mb_, int nb_) : mb(mb_), nb(nb_), items(mb_ * nb_), per((mb_ * nb_ + 7) >> 3) {}
+    __device__ __forceinline__ int first() const { return (blockIdx.x & 7) * per + (blockIdx.x >> 3); }
+    __device__ __forceinline__ int end() const { return min(items, ((int)(blockIdx.x & 7) + 1) * per); }
+    __device__ __forceinline__ void at(int i, int &m, int &n) const
+    {
+        const int group = i / (GN * mb), in = i - group * GN * mb, width = min(GN, nb - group * GN);
+        m = in / width;
+        n = group * GN + in - m * width;
+    }
+};
+
+// Where a block's operands lie.
+struct Place {
+    const bf16_t *a, *b;
+    long long lda, ldb;
+    int a_limit, b_limit, K, m, n, split;
+};
 
 __device__ __forceinline__ const bf16_t *head_rows(const LossArgs &a, int v0, long long &ld)
 {
@@ -221,108 +250,281 @@ __device__ __forceinline__ const bf16_t *head_rows(const LossArgs &a, int v0, lo
     return a.direct ? (const bf16_t *)a.weight + (long long)v0 * a.ws : (const bf16_t *)a.wp;
 }
 
-template <int TN> struct ByRows;    // blocks along the rows: 256 x TN
-template <> struct ByRows<256> { template <bool A, bool B> using of = Block<2, 4, 4, 2, A, B>; };
-template <> struct ByRows<128> { template <bool A, bool B> using of = Block<4, 2, 2, 2, A, B>; };
-template <> struct ByRows<64> { template <bool A, bool B> using of = Block<8, 1, 1, 2, A, B>; };
-
-template <int TN> __global__ __launch_bounds__(512) void bf16_softmax_kernel(LossArgs a, int v0, int vn)
-{
-    using Bl = typename ByRows<TN>::template of<true, true>;
-    __shared__ float2 red[Bl::WAVES * Bl::NI * 32];
-    const int count = a.head->count;
-    int m, n;
-    if (!block_of((vn + Bl::TM - 1) / Bl::TM, (count + TN - 1) / TN, m, n)) return;
-    Bl bl;
-    long long ld;
-    const bf16_t *w = head_rows(a, v0, ld);
-    bl.a.init(w + m * Bl::TM * ld, ld, vn - m * Bl::TM);
-    bl.b.init((const bf16_t *)a.hp + (size_t)n * TN * a.d_pad, a.d_pad, TN);
-    bl.run(lds_start(), a.d_pad);
-    const int wv = threadIdx.x >> 6;
-    softmax_part<Bl::WM, Bl::WN, Bl::MI, Bl::NI>(bl.c, red, a.part + (size_t)(v0 / Bl::TM + m) * a.n_pad + n * TN, m * Bl::TM, vn, LOG2E / a.temperature, wv / Bl::WN, wv % Bl::WN);
-}
-
-template <int TN> __global__ __launch_bounds__(512) void bf16_probabilities_kernel(LossArgs a, int v0, int vn)
-{
-    using Bl = typename ByRows<TN>::template of<true, true>;
-    const int count = a.head->count;
-    int m, n;
-    if (!block_of((vn + Bl::TM - 1) / Bl::TM, (count + TN - 1) / TN, m, n)) return;
-    Bl bl;
-    long long ld;
-    const bf16_t *w = head_rows(a, v0, ld);
-    bl.a.init(w + m * Bl::TM * ld, ld, vn - m * Bl::TM);
-    bl.b.init((const bf16_t *)a.hp + (size_t)n * TN * a.d_pad, a.d_pad, TN);
-    bl.run(lds_start(), a.d_pad);
-    const float k2 = LOG2E / a.temperature;
-    const int lane = threadIdx.x & 63, wn = (threadIdx.x >> 6) % Bl::WN;
-    float lse2[Bl::NI], weight[Bl::NI];
-#pragma unroll
-    for (int j = 0; j < Bl::NI; ++j) {
-        const int row = n * TN + (wn * Bl::NI + j) * 32 + (lane & 31);
-        lse2[j] = row < count ? a.lse[a.idx[row]] * LOG2E : 0.f;
-        weight[j] = row < count ? a.grad[a.idx[row]] / a.head->scale : 0.f;
+// What a kernel does: blocks of TM x TN, the place of block (m, n), and what becomes of a wavefront's accumulators.
+template <int TM, int TN> struct Logits {
+    static constexpr bool A_KC = true, B_KC = true;
+    const LossArgs &a;
+    int v0, vn, count;
+    __device__ __forceinline__ Logits(const LossArgs &a_, int v0_, int vn_, int) : a(a_), v0(v0_), vn(vn_), count(a_.head->count) {}
+    __device__ __forceinline__ Order order() const { return Order((vn + TM - 1) / TM, (count + TN - 1) / TN); }
+    __device__ __forceinline__ Place place(int m, int n) const
+    {
+        Place p;
+        p.a = head_rows(a, v0, p.lda) + (long long)m * TM * (a.direct ? a.ws : a.d_pad);
+        p.b = (const bf16_t *)a.hp + (size_t)n * TN * a.d_pad;
+        p.ldb = a.d_pad; p.a_limit = vn - m * TM; p.b_limit = TN; p.K = a.d_pad; p.m = m; p.n = n;
+        return p;
     }
-    bl.each_run([&](int j, int i, int v, float (&x)[8]) {   // rows that do not count and entries that do not exist: zeros, which the next products read
-        const int row = n * TN + i;
-        v += m * Bl::TM;
+};
+
+template <int TM, int TN> struct Softmax : Logits<TM, TN> {
+    using Logits<TM, TN>::Logits;
+    template <int WM, int WN, int MI, int NI> __device__ __forceinline__ void done(const Place &p, const f32x16 (&c)[MI][NI])
+    {
+        const LossArgs &a = this->a;
+        const int w = wavefront(), wm = w / WN, wn = w % WN;
+        softmax_part(c, a.part + ((size_t)(this->v0 / TM + p.m) * WM + wm) * a.part_ld + p.n * TN + wn * NI * 32, p.m * TM + wm * MI * 32, this->vn, LOG2E / a.temperature);
+    }
+};
+
+template <int TM, int TN> struct Probabilities : Logits<TM, TN> {
+    using Logits<TM, TN>::Logits;
+    int have = -1;               // rows whose lse and weight are held
+    float lse2[2], weight[2];
+    template <int WM, int WN, int MI, int NI> __device__ __forceinline__ void done(const Place &p, const f32x16 (&c)[MI][NI])
+    {
+        const LossArgs &a = this->a;
+        const int wn = wavefront() % WN;
+        if (p.n != have) {
+            have = p.n;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = row < count && v + e < vn ? weight[j] * term(x[e], k2, lse2[j]) : 0.f;
-        store_run((bf16_t *)a.G + (size_t)row * a.piece + v, x);
-    });
+            for (int j = 0; j < NI; ++j) {
+                const int row = p.n * TN + (wn * NI + j) * 32 + (threadIdx.x & 31);
+                lse2[j] = row < this->count ? a.lse[a.idx[row]] * LOG2E : 0.f;
+                weight[j] = row < this->count ? a.grad[a.idx[row]] / a.head->scale : 0.f;
+            }
+        }
+        const float k2 = LOG2E / a.temperature;
+        const bool inside = p.m * TM + TM <= this->vn && p.n * TN + TN <= this->count;
+        each_run<WN>(c, [&](int j, int i, int v, float (&x)[8]) {
+            const int row = p.n * TN + i;
+            v += p.m * TM;
+            // rows that do not count and entries that do not exist: zeros, which the next products read
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = inside || (row < this->count && v + e < this->vn) ? weight[j] * term(x[e], k2, lse2[j]) : 0.f;
+            store_run((bf16_t *)a.G + (size_t)row * a.piece + v, x);
+        });
+    }
+};
+
+template <int TM, int TN> struct HiddenGrad {
+    static constexpr bool A_KC = false, B_KC = true;
+    const LossArgs &a;
+    int v0, vn, first, count, mb, splits, per;
+    __device__ __forceinline__ HiddenGrad(const LossArgs &a_, int v0_, int vn_, int first_) : a(a_), v0(v0_), vn(vn_), first(first_), count(a_.head->count)
+    {
+        mb = (a.d_pad + TM - 1) / TM;
+        splits = bf16_splits(a, count);
+        per = ((vn + splits - 1) / splits + 63) / 64 * 64;
+    }
+    __device__ __forceinline__ Order order() const { return Order(mb * splits, (count + TN - 1) / TN); }
+    __device__ __forceinline__ Place place(int m, int n) const
+    {
+        Place p;
+        p.split = m / mb; p.m = m - p.split * mb; p.n = n;
+        const int k0 = min(vn, p.split * per);
+        p.K = min(vn, k0 + per) - k0;
+        p.a = head_rows(a, v0, p.lda);
+        p.a += k0 * p.lda + p.m * TM; p.a_limit = a.d_pad - p.m * TM;
+        p.b = (const bf16_t *)a.G + (size_t)n * TN * a.piece + k0; p.ldb = a.piece; p.b_limit = TN;
+        return p;
+    }
+    template <int WM, int WN, int MI, int NI> __device__ __forceinline__ void done(const Place &p, const f32x16 (&c)[MI][NI])
+    {
+        each_run<WN>(c, [&](int, int i, int d, float (&x)[8]) {
+            d += p.m * TM;
+            if (d >= a.d_pad) return;
+            float *to = a.acc + ((size_t)p.split * bf16_rows(a, count) + p.n * TN + i) * a.d_pad + d;
+            if (!first) {
+                const float4 u = reinterpret_cast<const float4 *>(to)[0], w = reinterpret_cast<const float4 *>(to)[1];
+                x[0] += u.x; x[1] += u.y; x[2] += u.z; x[3] += u.w; x[4] += w.x; x[5] += w.y; x[6] += w.z; x[7] += w.w;
+            }
+            store_run(to, x);
+        });
+    }
+};
+
+template <int TM, int TN> struct WeightGrad {
+    static constexpr bool A_KC = false, B_KC = false;
+    const LossArgs &a;
+    int v0, vn;
+    __device__ __forceinline__ WeightGrad(const LossArgs &a_, int v0_, int vn_, int) : a(a_), v0(v0_), vn(vn_) {}
+    __device__ __forceinline__ Order order() const { return Order((a.d_pad + TM - 1) / TM, (vn + TN - 1) / TN); }
+    __device__ __forceinline__ Place place(int m, int n) const
+    {
+        Place p;
+        p.m = m; p.n = n; p.K = (a.head->count + 63) / 64 * 64;      // G and the rows are zero from the last row that counts to there
+        p.a = (const bf16_t *)a.hp + m * TM; p.lda = a.d_pad; p.a_limit = a.d_pad - m * TM;
+        p.b = (const bf16_t *)a.G + n * TN; p.ldb = a.piece; p.b_limit = a.piece - n * TN;
+        return p;
+    }
+    template <int WM, int WN, int MI, int NI> __device__ __forceinline__ void done(const Place &p, const f32x16 (&c)[MI][NI])
+    {
+        const float k = a.head->scale * a.temperature;
+        const bool whole = ((reinterpret_cast<uintptr_t>(a.d_weight) | (uintptr_t)(a.dws * 2)) & 15) == 0;
+        each_run<WN>(c, [&](int, int i, int d, float (&x)[8]) {
+            const int v = p.n * TN + i;
+            d += p.m * TM;
+            if (v >= vn || d >= a.dim) return;
+            bf16_t *to = (bf16_t *)a.d_weight + (long long)(v0 + v) * a.dws + d;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] *= k;
+            if (whole && d + 8 <= a.dim) store_run(to, x);
+            else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) if (d + e < a.dim) store_one(to + e, x[e]);
+            }
+        });
+    }
+};
+
+// One block a workgroup.
+template <template <int, int> class Job_, class Bl> __global__ __launch_bounds__(512) void block_kernel(LossArgs a, int v0, int vn, int flag)
+{
+    Job_<Bl::TM, Bl::TN> job(a, v0, vn, flag);
+    const Order o = job.order();
+    const int i = o.first();
+    if (i >= o.end()) return;
+    int m, n;
+    o.at(i, m, n);
+    const Place p = job.place(m, n);
+    Bl bl;
+    bl.a.init(p.a, p.lda, p.a_limit);
+    bl.b.init(p.b, p.ldb, p.b_limit);
+    bl.run(lds_start(), p.K);
+    job.template done<Bl::WM, Bl::WN, Bl::MI, Bl::NI>(p, bl.c);
 }
 
-template <int TN> __global__ __launch_bounds__(512) void bf16_hidden_grad_kernel(LossArgs a, int v0, int vn, int first)
+// Blocks of 256 x 256, one workgroup a compute unit, block after block, the copies never stopping. 8 wavefronts of 128 x 64; the first four and the last four (one of each
+// on every SIMD) take turns: while one reads its matrix operands of 32 k from LDS, the other's matrix instructions run. LDS holds five tiles, a step's two, A's of the next
+// two steps and B's of the next: A (the operand that comes from beyond L2 more often) has two steps of time to arrive, B one.
+template <template <int, int> class Job_> __global__ __launch_bounds__(512) void turns_kernel(LossArgs a, int v0, int vn, int flag)
 {
-    using Bl = typename ByRows<TN>::template of<false, true>;
-    const int count = a.head->count, nb = (count + TN - 1) / TN, mb = (a.d_pad + Bl::TM - 1) / Bl::TM, splits = bf16_splits(a, count);
-    int m, n;
-    if (!block_of(mb * splits, nb, m, n)) return;
-    const int split = m / mb, per = ((vn + splits - 1) / splits + BK - 1) / BK * BK, k0 = min(vn, split * per), k1 = min(vn, k0 + per);
-    m -= split * mb;
-    Bl bl;
-    long long ld;
-    const bf16_t *w = head_rows(a, v0, ld);
-    bl.a.init(w + k0 * ld + m * Bl::TM, ld, a.d_pad - m * Bl::TM);
-    bl.b.init((const bf16_t *)a.G + (size_t)n * TN * a.piece + k0, a.piece, TN);
-    bl.run(lds_start(), k1 - k0);
-    bl.each_run([&](int, int i, int d, float (&x)[8]) {
-        d += m * Bl::TM;
-        if (d >= a.d_pad) return;
-        float *to = a.acc + ((size_t)split * bf16_rows(a, count) + n * TN + i) * a.d_pad + d;
-        if (!first) {
-            const float4 p = reinterpret_cast<const float4 *>(to)[0], q = reinterpret_cast<const float4 *>(to)[1];
-            x[0] += p.x; x[1] += p.y; x[2] += p.z; x[3] += p.w; x[4] += q.x; x[5] += q.y; x[6] += q.z; x[7] += q.w;
-        }
-        store_run(to, x);
-    });
-}
+    constexpr int WM = 2, WN = 4, MI = 4, NI = 2, T = 256, TILES = 5;
+    using Job = Job_<T, T>;
+    using TA = Tile<T, Job::A_KC, 8>;
+    using TB = Tile<T, Job::B_KC, 8>;
+    Job job(a, v0, vn, flag);
+    const Order o = job.order();
+    const int end = o.end(), stride = gridDim.x >> 3, w = wavefront();
+    if (o.first() >= end) return;
+    const bool second = w >= 4;
+    const uint32_t lds = lds_start();
 
-__global__ __launch_bounds__(512) void bf16_weight_grad_kernel(LossArgs a, int v0, int vn)
-{
-    using Bl = Block<2, 4, 4, 2, false, false>;
-    int m, n;
-    if (!block_of((a.d_pad + Bl::TM - 1) / Bl::TM, (vn + Bl::TN - 1) / Bl::TN, m, n)) return;
-    Bl bl;
-    bl.a.init((const bf16_t *)a.hp + m * Bl::TM, a.d_pad, a.d_pad - m * Bl::TM);
-    bl.b.init((const bf16_t *)a.G + n * Bl::TN, a.piece, a.piece - n * Bl::TN);
-    bl.run(lds_start(), (a.head->count + BK - 1) / BK * BK);
-    const float k = a.head->scale * a.temperature;
-    const bool whole = ((reinterpret_cast<uintptr_t>(a.d_weight) | (uintptr_t)(a.dws * 2)) & 15) == 0;
-    bl.each_run([&](int, int i, int d, float (&x)[8]) {
-        const int v = n * Bl::TN + i;
-        d += m * Bl::TM;
-        if (v >= vn || d >= a.dim) return;
-        bf16_t *to = (bf16_t *)a.d_weight + (long long)(v0 + v) * a.dws + d;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] *= k;
-        if (whole && d + 8 <= a.dim) store_run(to, x);
-        else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) if (d + e < a.dim) store_one(to + e, x[e]);
+    // the copies: an operand's next step, of this block or of the next that has any
+    TA ta;
+    TB tb;
+    int ia = o.first(), ib = ia, steps_a, steps_b, left_a, left_b;
+    auto open_a = [&] {
+        for (steps_a = 0; ia < end; ia += stride) {
+            int m, n;
+            o.at(ia, m, n);
+            const Place p = job.place(m, n);
+            if (p.K > 0) { steps_a = (p.K + BK - 1) / BK; left_a = p.K; ta.init(p.a, p.lda, p.a_limit); break; }
         }
-    });
+    };
+    auto open_b = [&] {
+        for (steps_b = 0; ib < end; ib += stride) {
+            int m, n;
+            o.at(ib, m, n);
+            const Place p = job.place(m, n);
+            if (p.K > 0) { steps_b = (p.K + BK - 1) / BK; left_b = p.K; tb.init(p.b, p.ldb, p.b_limit); break; }
+        }
+    };
+    uint32_t to = lds;            // the next free tile
+    auto turn = [&](uint32_t &t, int by) { t += by * TA::BYTES; t = t >= lds + TILES * TA::BYTES ? t - TILES * TA::BYTES : t; };
+    auto copy_a = [&] {
+        ta.issue(to, left_a);
+        turn(to, 1);
+        left_a -= BK;
+        if (--steps_a == 0) { ia += stride; open_a(); }
+    };
+    auto copy_b = [&] {
+        tb.issue(to, left_b);
+        turn(to, 1);
+        left_b -= BK;
+        if (--steps_b == 0) { ib += stride; open_b(); }
+    };
+    auto barrier = [] {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("" ::: "memory");
+    };
+
+    open_a();
+    open_b();
+    if (steps_a) {
+        copy_a();
+        copy_b();
+        if (steps_a) copy_a();    // two steps ahead of B from here on, as far as there are steps
+        else turn(to, 1);
+    }
+    landed_and_barrier<0>();
+    if (second) barrier();
+
+    Reader<T, Job::A_KC, true, MI> ra;
+    Reader<T, Job::B_KC, false, NI> rb;
+    ra.init(w / WN * MI * 32);
+    rb.init(w % WN * NI * 32);
+    f32x16 c[MI][NI];
+    bf16x8 xa[2][MI], xb[2][NI];
+    auto products = [&] {
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < NI; ++j) c[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xa[q][i], xb[q][j], c[i][j], 0, 0, 0);
+        __builtin_amdgcn_s_setprio(0);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    uint32_t at_a = lds, at_b = lds + TA::BYTES;
+#pragma unroll 1
+    for (int item = o.first(); item < end; item += stride) {
+        int m, n;
+        o.at(item, m, n);
+        const Place p = job.place(m, n);
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) c[i][j][r] = 0.f;
+#pragma unroll 1
+        for (int s = (p.K + BK - 1) / BK; s; --s) {
+            ra.template read<0>(at_a, xa[0]); rb.template read<0>(at_b, xb[0]);
+            ra.template read<1>(at_a, xa[1]); rb.template read<1>(at_b, xb[1]);
+            // the tiles of the step before are free: everyone has read them
+            if (steps_b) copy_b();
+            const bool ahead = steps_a > 0;
+            if (ahead) copy_a();
+            wait_lds();
+            barrier();
+            products();
+            barrier();
+            ra.template read<2>(at_a, xa[0]); rb.template read<2>(at_b, xb[0]);
+            ra.template read<3>(at_a, xa[1]); rb.template read<3>(at_b, xb[1]);
+            // before the barrier after which the next step is read: both its tiles are there, A's of the step after may be under way
+            if (second) {
+                if (ahead) wait_all_but<TA::COPIES>();
+                else wait_all_but<0>();
+            } else wait_lds();
+            barrier();
+            products();
+            if (!second) {
+                if (ahead) wait_all_but<TA::COPIES>();
+                else wait_all_but<0>();
+            }
+            barrier();
+            turn(at_a, 2);
+            turn(at_b, 2);
+        }
+        job.template done<WM, WN, MI, NI>(p, c);
+    }
+    if (!second) barrier();
 }
 
 // Rows that count, one after the other, whole steps long; zeros up to the end of the last block.
@@ -391,11 +593,14 @@ template <class... P, class... A> void launch(void (*kernel)(P...), dim3 grid, i
     hipLaunchKernelGGL(kernel, grid, dim3(512), lds, s, args...);
 }
 
-template <class Go> void by_block(const LossArgs &a, Go go)
+template <template <int, int> class Job> void launch_job(hipStream_t s, const LossArgs &a, int v0, int vn, int flag, int mb)
 {
-    if (a.n_block == 64) go(std::integral_constant<int, 64>{});
-    else if (a.n_block == 128) go(std::integral_constant<int, 128>{});
-    else go(std::integral_constant<int, 256>{});
+    constexpr bool A = Job<256, 64>::A_KC, B = Job<256, 64>::B_KC;
+    using Small = Block<8, 1, 1, 2, 3, A, B>;       // 256 x 64
+    using Middle = Block<4, 2, 2, 2, 3, A, B>;      // 256 x 128
+    if (a.n_block == 64) launch(block_kernel<Job, Small>, dim3(up_div(mb, 8) * 8), Small::LDS, s, a, v0, vn, flag);
+    else if (a.n_block == 128) launch(block_kernel<Job, Middle>, dim3(up_div(mb, 8) * 8), Middle::LDS, s, a, v0, vn, flag);
+    else launch(turns_kernel<Job>, dim3(256), 5 * 256 * BK * 2, s, a, v0, vn, flag);
 }
 
 }  // namespace
@@ -415,36 +620,18 @@ void launch_bf16_entries(hipStream_t s, const LossArgs &a)
     hipLaunchKernelGGL(bf16_entries_kernel, dim3((unsigned)(((long long)a.rows * a.entries + 31) / 32)), dim3(64), 0, s, a);
 }
 
-void launch_bf16_softmax(hipStream_t s, const LossArgs &a, int v0, int vn)
-{
-    by_block(a, [&](auto t) {
-        constexpr int TN = decltype(t)::value;
-        launch(bf16_softmax_kernel<TN>, grid_of(up_div(vn, BF16_BLOCK), up_div(a.rows, TN)), ByRows<TN>::template of<true, true>::LDS, s, a, v0, vn);
-    });
-}
+void launch_bf16_softmax(hipStream_t s, const LossArgs &a, int v0, int vn) { launch_job<Softmax>(s, a, v0, vn, 0, up_div(vn, BF16_BLOCK)); }
 
-void launch_bf16_probabilities(hipStream_t s, const LossArgs &a, int v0, int vn)
-{
-    by_block(a, [&](auto t) {
-        constexpr int TN = decltype(t)::value;
-        launch(bf16_probabilities_kernel<TN>, grid_of(up_div(vn, BF16_BLOCK), up_div(a.rows, TN)), ByRows<TN>::template of<true, true>::LDS, s, a, v0, vn);
-    });
-}
+int bf16_softmax_parts(const LossArgs &a) { return up_div(a.vocab, BF16_BLOCK) * (a.n_block == 64 ? 8 : a.n_block == 128 ? 4 : 2); }
+
+void launch_bf16_probabilities(hipStream_t s, const LossArgs &a, int v0, int vn) { launch_job<Probabilities>(s, a, v0, vn, 0, up_div(vn, BF16_BLOCK)); }
 
 void launch_bf16_hidden_grad(hipStream_t s, const LossArgs &a, int v0, int vn, bool first)
 {
-    by_block(a, [&](auto t) {
-        constexpr int TN = decltype(t)::value;
-        // the rows that count, and with them the splits, are known on the device: the largest product of the two over any count
-        const int mb = up_div(a.d_pad, BF16_BLOCK), most = std::max(mb * up_div(a.rows, TN), std::min(256, mb * up_div(a.rows, TN) * a.splits));
-        launch(bf16_hidden_grad_kernel<TN>, grid_of(most, 1), ByRows<TN>::template of<false, true>::LDS, s, a, v0, vn, (int)first);
-    });
+    const int mb = up_div(a.d_pad, BF16_BLOCK);
+    launch_job<HiddenGrad>(s, a, v0, vn, first, std::max(mb, std::min(256, mb * a.splits)));
 }
 
-void launch_bf16_weight_grad(hipStream_t s, const LossArgs &a, int v0, int vn)
-{
-    using Bl = Block<2, 4, 4, 2, false, false>;
-    launch(bf16_weight_grad_kernel, grid_of(up_div(a.d_pad, Bl::TM), up_div(vn, Bl::TN)), Bl::LDS, s, a, v0, vn);
-}
+void launch_bf16_weight_grad(hipStream_t s, const LossArgs &a, int v0, int vn) { launch(turns_kernel<WeightGrad>, dim3(256), 5 * 256 * BK * 2, s, a, v0, vn, 0); }
 
 }  // namespace tr

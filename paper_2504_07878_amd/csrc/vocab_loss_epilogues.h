@@ -42,10 +42,9 @@ __device__ __forceinline__ float2 join(float2 a, float2 b)
     return make_float2(m, a.y * __builtin_amdgcn_exp2f(a.x - at) + b.y * __builtin_amdgcn_exp2f(b.x - at));
 }
 
-// A block's part of every row's softmax over vocabulary entries m0 .. (those at or past V do not exist): wavefront (wm, wn) of WM x WN holds MI x NI
-// accumulators. red: LDS, WM * WN * NI * 32 float2.
-template <int WM, int WN, int MI, int NI>
-__device__ __forceinline__ void softmax_part(const f32x16 (&c)[MI][NI], float2 *red, float2 *part /* of this block's vocabulary, [row] */, int m0, int V, float k2, int wm, int wn)
+// A wavefront's part of its rows' softmax: MI x NI accumulators over vocabulary entries m0 .. (those at or past V do not exist); part: of its first row.
+template <int MI, int NI>
+__device__ __forceinline__ void softmax_part(const f32x16 (&c)[MI][NI], float2 *part, int m0, int V, float k2)
 {
     const int lane = threadIdx.x & 63, hf = lane >> 5, col = lane & 31;
 #pragma unroll
@@ -53,7 +52,7 @@ __device__ __forceinline__ void softmax_part(const f32x16 (&c)[MI][NI], float2 *
         float top = -INFINITY;
 #pragma unroll
         for (int mi = 0; mi < MI; ++mi) {
-            const int base = m0 + (wm * MI + mi) * 32;
+            const int base = m0 + mi * 32;
             if (base + 32 <= V) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) top = fmaxf(top, c[mi][ni][r]);
@@ -62,12 +61,13 @@ __device__ __forceinline__ void softmax_part(const f32x16 (&c)[MI][NI], float2 *
                 for (int r = 0; r < 16; ++r) top = base + 16 * (r >> 3) + 8 * hf + (r & 7) < V ? fmaxf(top, c[mi][ni][r]) : top;
             }
         }
+        top = fmaxf(top, __shfl_xor(top, 32));
         top = whole_above(top * k2);
         const float at = top == -INFINITY ? 0.f : top;
         float sum = 0.f;
 #pragma unroll
         for (int mi = 0; mi < MI; ++mi) {
-            const int base = m0 + (wm * MI + mi) * 32;
+            const int base = m0 + mi * 32;
             if (base + 32 <= V) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) sum += term(c[mi][ni][r], k2, at);
@@ -76,16 +76,8 @@ __device__ __forceinline__ void softmax_part(const f32x16 (&c)[MI][NI], float2 *
                 for (int r = 0; r < 16; ++r) sum += base + 16 * (r >> 3) + 8 * hf + (r & 7) < V ? term(c[mi][ni][r], k2, at) : 0.f;
             }
         }
-        const float2 mine = make_float2(top, sum), other = make_float2(__shfl_xor(top, 32), __shfl_xor(sum, 32));
-        const float2 both = hf ? join(other, mine) : join(mine, other);
-        if (hf == 0) red[(wm * WN + wn) * NI * 32 + ni * 32 + col] = both;
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < WN * NI * 32; i += WM * WN * 64) {
-        float2 t = red[i];
-#pragma unroll
-        for (int w = 1; w < WM; ++w) t = join(t, red[w * WN * NI * 32 + i]);
-        part[i] = t;
+        sum += __shfl_xor(sum, 32);
+        if (hf == 0) part[ni * 32 + col] = make_float2(top, sum);
     }
 }
 

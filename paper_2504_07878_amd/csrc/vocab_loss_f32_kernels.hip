@@ -112,7 +112,6 @@ template <class F> __device__ __forceinline__ void each_run(const f32x16 (&c)[2]
 template <class HT, class WT> __global__ __launch_bounds__(256) void f32_softmax_kernel(LossArgs a)
 {
     __shared__ Tiles sm;
-    __shared__ float2 red[256];
     const int m0 = blockIdx.x * F32_BLOCK, n0 = blockIdx.y * F32_BLOCK, count = a.head->count;
     if (n0 >= count) return;
     const HeadRows<WT> A{(const WT *)a.weight, a.ws, 0, a.vocab, a.dim};
@@ -120,7 +119,7 @@ template <class HT, class WT> __global__ __launch_bounds__(256) void f32_softmax
     f32x16 c[2][2];
     products(A, B, m0, n0, 0, a.dim, sm, c);
     const int w = threadIdx.x >> 6;
-    softmax_part<2, 2, 2, 2>(c, red, a.part + (size_t)blockIdx.x * a.n_pad + n0, m0, a.vocab, LOG2E / a.temperature, w >> 1, w & 1);
+    softmax_part(c, a.part + ((size_t)blockIdx.x * 2 + (w >> 1)) * a.part_ld + n0 + (w & 1) * 64, m0 + (w >> 1) * 64, a.vocab, LOG2E / a.temperature);
 }
 
 template <class HT, class WT> __global__ __launch_bounds__(256) void f32_probabilities_kernel(LossArgs a, int v0, int vn)

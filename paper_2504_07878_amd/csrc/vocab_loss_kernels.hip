@@ -115,7 +115,7 @@ __global__ __launch_bounds__(256) void loss_finish_kernel(LossArgs a, int parts)
     if (i >= a.head->count) return;
     const int r = a.idx[i];
     float2 t = make_float2(-INFINITY, 0.f);
-    for (int p = threadIdx.x; p < parts; p += 256) t = join(t, a.part[(size_t)p * a.n_pad + i]);
+    for (int p = threadIdx.x; p < parts; p += 256) t = join(t, a.part[(size_t)p * a.part_ld + i]);
     for (int o = 32; o; o >>= 1) {
         const float2 u = make_float2(__shfl_xor(t.x, o), __shfl_xor(t.y, o));
         t = lane & o ? join(u, t) : join(t, u);
