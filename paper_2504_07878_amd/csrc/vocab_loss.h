@@ -12,11 +12,15 @@
 
 namespace tr {
 
-struct LossHead {     // [count or 0, rows given, largest |weight of a row| as float bits, 0]
-    int count, rows;
-    float scale;
+struct LossHead {
+    int count;      // rows that count
+    int half;       // > 0: rows of G in pairs, see below
+    float scale;    // largest |weight| of a row that counts
     int pad;
 };
+// Pairs: with 128 rows or fewer (bf16 products) G has a second row for every row, `half` (64 or 128) rows further on, with what rounding the first to bf16 left, and the
+// packed rows are there twice. The products are bound by the head's bytes then, so the second half costs little, and few rows average few roundings.
+constexpr int PAIR_ROWS = 128;
 
 struct LossArgs {
     const void *hidden, *weight;
@@ -36,11 +40,12 @@ struct LossArgs {
     unsigned char *state;         // [rows] ROW_*
     float2 *part;                 // [parts of the vocabulary][part_ld] running softmaxes
     float *value;                 // [n_pad][entries] products of the listed entries, then what G has there
-    void *G;                      // [n_pad][piece]
+    void *G;                      // [n_pad][g_ld], a piece's columns; lines are not a power of two apart, so that a column's do not meet in one memory channel
     float *acc;                   // [splits][n_pad, or the blocks that count (bf16)][d_pad] sums of the gradient to the hidden rows
     void *hp;                     // [n_pad][d_pad] rows that count (bf16 products)
     void *wp;                     // [piece][d_pad] rows of the head where they cannot be read as they lie
-    int n_pad, d_pad, piece, splits, part_ld;
+    int n_pad, d_pad, piece, g_ld, splits, part_ld;
+    int pairs;                    // rows may be in pairs (gradients, bf16 products)
     int n_block;                  // rows per block (bf16 products)
     bool direct;                  // the head is read as it lies (bf16 products): rows on 16 bytes, whole steps of 64 features
 };
@@ -50,15 +55,15 @@ enum { ROW_SKIP = 0, ROW_COUNTS = 1, ROW_BAD = 2 };
 constexpr int LOSS_MAX_ENTRIES = 1024;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
-// Rows that count, their list, zeros (NaN for an id at or past the vocabulary) for the others.
+// Rows that count, their list, zeros (NaN for an id at or past the vocabulary) for the others; the rows packed for bf16 products.
 void launch_loss_rows(hipStream_t s, const LossArgs &a);
 // lse and loss of the rows that count from `parts` running softmaxes each.
 void launch_loss_finish(hipStream_t s, const LossArgs &a, int parts);
-// From the products of the listed entries: what G has for them, and their places in G for one piece of the vocabulary.
-void launch_loss_values(hipStream_t s, const LossArgs &a);
-void launch_loss_scatter(hipStream_t s, const LossArgs &a, int v0, int vn, bool g_bf16);
+// From the products of the listed entries: what G has for them, and their places in G for one piece of the vocabulary (place: both at once, for a vocabulary of one piece).
+void launch_loss_values(hipStream_t s, const LossArgs &a, bool place);
+void launch_loss_scatter(hipStream_t s, const LossArgs &a, int v0, int vn);
 // The gradient to the hidden rows from the splits' sums (as the bf16 or the f32 products leave them), weighed and rounded; zeros for rows that do not count.
-void launch_loss_hidden_grad(hipStream_t s, const LossArgs &a, bool bf16);
+void launch_loss_hidden_grad(hipStream_t s, const LossArgs &a);
 
 // Products of the listed entries, each the bits that the softmax's own products have: a probability near 1 and its logit then agree, and what is left of
 // 1 - p and of lse - z is not the difference of two roundings.
@@ -74,20 +79,25 @@ void launch_f32_weight_grad(hipStream_t s, const LossArgs &a, int v0, int vn);
 
 // bf16 rows and head (vocab_loss_bf16_kernels.hip): blocks of 256 vocabulary entries or features.
 constexpr int BF16_BLOCK = 256;
-void launch_bf16_pack_rows(hipStream_t s, const LossArgs &a);
 void launch_bf16_pack_head(hipStream_t s, const LossArgs &a, int v0, int vn);
-void launch_bf16_softmax(hipStream_t s, const LossArgs &a, int v0, int vn);
+// entries: the listed entries' products too, in the same launch (blocks of fewer than 256 rows only)
+void launch_bf16_softmax(hipStream_t s, const LossArgs &a, int v0, int vn, bool entries);
 int bf16_softmax_parts(const LossArgs &a);
-void launch_bf16_probabilities(hipStream_t s, const LossArgs &a, int v0, int vn);
+void launch_bf16_probabilities(hipStream_t s, const LossArgs &a, int v0, int vn, bool entries);
 void launch_bf16_hidden_grad(hipStream_t s, const LossArgs &a, int v0, int vn, bool first);
 void launch_bf16_weight_grad(hipStream_t s, const LossArgs &a, int v0, int vn);
-__host__ __device__ inline int bf16_rows(const LossArgs &a, int count) { return (count + a.n_block - 1) / a.n_block * a.n_block; }   // whole blocks
-// splits of the sums of the gradient to `count` hidden rows, at most a.splits
-__host__ __device__ inline int bf16_splits(const LossArgs &a, int count)
+#ifdef __HIPCC__
+__host__ __device__ inline int bf16_products_rows(int count, int half) { return half ? 2 * half : count; }
+__host__ __device__ inline int bf16_rows(const LossArgs &a, int rows) { return (rows + a.n_block - 1) / a.n_block * a.n_block; }   // whole blocks
+// Splits of the sums of the gradient to `rows` rows (of products), at most a.splits. With 8 or more the k's of an eighth of them lie on one XCD: every XCD reads its own part of
+// the head, once, and of G. Enough for every compute unit to have a block; none where there are many blocks anyway.
+__host__ __device__ inline int bf16_splits(const LossArgs &a, int rows)
 {
-    const int tiles = (count + a.n_block - 1) / a.n_block * (a.d_pad / BF16_BLOCK + (a.d_pad % BF16_BLOCK ? 1 : 0));
-    const int n = 256 / (tiles ? tiles : 1);
-    return n < 1 ? 1 : n < a.splits ? n : a.splits;
+    const int tiles = (rows + a.n_block - 1) / a.n_block * ((a.d_pad + BF16_BLOCK - 1) / BF16_BLOCK);
+    if (tiles >= 1024 || a.splits < 2) return 1;
+    const int n = tiles >= 32 ? 8 : 32 / (tiles ? tiles : 1) * 8;
+    return n < a.splits ? n : a.splits >= 8 ? a.splits / 8 * 8 : a.splits;
 }
+#endif
 
 }  // namespace tr

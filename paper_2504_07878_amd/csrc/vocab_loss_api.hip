@@ -22,13 +22,14 @@ bool config_ok(const tr_loss_config *c)
 
 // Where everything lies in the workspace, for a configuration; the sizes of a call's own launches follow from its rows, never beyond these.
 struct Plan {
-    int n_pad, d_pad, piece, splits;
+    int n_pad, d_pad, piece, g_ld, splits;
     size_t head, idx, state, part, value, G, acc, hp, wp, total;
 };
 
 bool is_bf16(const tr_loss_config *c) { return c->hidden_dtype == TR_BF16; }   // the products that run on bf16 matrix instructions
 
-// Rows of G times its columns stay at 256 MB or less (what the caches beyond L2 hold, so that a piece is read back from there), but a piece has 2048 columns at least.
+// G stays at 512 MB or less, but a piece has 2048 columns at least. (6144 of 8192 rows x 151936 x 896, all products of the gradients, pieces of 128 / 256 / 512 / 1024 MB:
+// 7.1 / 5.9 / 5.8 / 5.7 ms.)
 // Splits of the sums of the gradient to the hidden rows: as many as give every compute unit a block.
 Plan plan_of(const tr_loss_config *c)
 {
@@ -39,9 +40,10 @@ Plan plan_of(const tr_loss_config *c)
     p.n_pad = (int)up(c->max_rows, block);
     p.d_pad = (int)up(c->dim, half ? 64 : F32_BLOCK);
     const size_t vocab = up(c->vocab, block);
-    p.piece = (int)std::min(vocab, std::max<size_t>(2048, (256u << 20) / g_size / p.n_pad / block * block));
-    const int tiles = (int)(up(p.d_pad, block) / block) * (half ? 1 : p.n_pad / F32_BLOCK);
-    p.splits = std::max(1, std::min((half ? 256 : 512) / tiles, p.piece / 256));
+    p.piece = (int)std::min(vocab, std::max<size_t>(2048, (512u << 20) / g_size / p.n_pad / block * block));
+    p.g_ld = p.piece + 128;
+    const int mb = (int)(up(p.d_pad, block) / block), few = std::max(1, p.piece / 256);
+    p.splits = half ? std::min(few, std::max(1, 32 / mb) * 8) : std::max(1, std::min(512 / (mb * (p.n_pad / F32_BLOCK)), few));
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t was = at; at += up(bytes, 256); return was; };
     p.head = take(sizeof(LossHead));
@@ -49,10 +51,11 @@ Plan plan_of(const tr_loss_config *c)
     p.state = take(c->max_rows);
     p.part = take(vocab / block * 2 * p.n_pad * sizeof(float2));   // two wavefronts' parts a block of 256 rows; four of 128 or eight of 64
     p.value = take((size_t)p.n_pad * c->max_entries * 4);
-    p.G = take((size_t)p.n_pad * p.piece * g_size);
-    // bf16: (blocks along the rows) * splits * (blocks along the features) <= 256, or splits = 1
-    const size_t sums = half ? std::max<size_t>(p.n_pad, (size_t)(256 / std::min(256, tiles)) * BF16_BLOCK) : (size_t)p.splits * p.n_pad;
-    p.acc = take(sums * p.d_pad * 4);
+    p.G = take((size_t)p.n_pad * p.g_ld * g_size);
+    // bf16, rows of all splits (bf16_splits): blocks * splits <= 256 where there are fewer than 32 blocks, 8 splits up to 1024 blocks, one from there on
+    const size_t sums = (size_t)p.splits * p.n_pad, most = std::max({(size_t)std::min(p.splits, 8) * std::min<size_t>(p.n_pad, 1024 / mb * BF16_BLOCK + BF16_BLOCK),
+                                                                     (size_t)(256 / mb + 1) * BF16_BLOCK, (size_t)p.n_pad});
+    p.acc = take((half ? std::min(sums, most) : sums) * p.d_pad * 4);
     if (half) {
         p.hp = take((size_t)p.n_pad * p.d_pad * 2);
         p.wp = take((size_t)p.piece * p.d_pad * 2);
@@ -62,7 +65,7 @@ Plan plan_of(const tr_loss_config *c)
 }
 
 // Checks what every call has in common and fills in the arguments; TR_OK or an error, before anything is enqueued.
-int arguments(const tr_loss_config *c, const tr_loss_rows *in, void *ws, size_t ws_bytes, bool teacher, LossArgs &a, Plan &p)
+int arguments(const tr_loss_config *c, const tr_loss_rows *in, void *ws, size_t ws_bytes, bool teacher, bool gradient, LossArgs &a, Plan &p)
 {
     if (!c || !in || !ws) return TR_ERR_INVALID_ARG;
     if (!config_ok(c)) return TR_ERR_SHAPE;
@@ -84,10 +87,12 @@ int arguments(const tr_loss_config *c, const tr_loss_rows *in, void *ws, size_t 
     a.entries = teacher ? in->entries : 1; a.ids = in->ids; a.teacher = teacher ? in->teacher : nullptr; a.temperature = teacher ? in->temperature : 1.f;
     a.head = (LossHead *)(b + p.head); a.idx = (int *)(b + p.idx); a.state = (unsigned char *)(b + p.state); a.part = (float2 *)(b + p.part);
     a.value = (float *)(b + p.value); a.G = b + p.G; a.acc = (float *)(b + p.acc);
-    a.n_pad = a.part_ld = p.n_pad; a.d_pad = p.d_pad; a.piece = p.piece; a.splits = p.splits;
+    a.n_pad = a.part_ld = p.n_pad; a.d_pad = p.d_pad; a.piece = p.piece; a.g_ld = p.g_ld; a.splits = p.splits;
     if (is_bf16(c)) {
         a.hp = b + p.hp; a.wp = b + p.wp;
-        a.n_block = a.rows <= 64 ? 64 : a.rows <= 128 ? 128 : 256;
+        a.pairs = gradient;
+        const int rows = gradient && a.rows <= PAIR_ROWS ? 2 * a.rows : a.rows;
+        a.n_block = rows <= 64 && !gradient ? 64 : rows <= 128 ? 128 : 256;
         if (a.n_block < 256) a.part_ld = a.n_block;   // more parts, of fewer rows
         a.direct = a.dim % 64 == 0 && a.ws % 8 == 0 && a.ws < (1 << 22) && (reinterpret_cast<uintptr_t>(a.weight) & 15) == 0;
     }
@@ -100,20 +105,20 @@ int forward(const tr_loss_config *c, void *ws, size_t ws_bytes, void *stream, co
 {
     LossArgs a;
     Plan p;
-    if (const int e = arguments(c, in, ws, ws_bytes, teacher, a, p)) return e;
+    if (const int e = arguments(c, in, ws, ws_bytes, teacher, false, a, p)) return e;
     if (a.rows && (!loss || !lse)) return TR_ERR_INVALID_ARG;
     if (!a.rows) return TR_OK;
     a.loss = loss; a.lse = lse;
     hipStream_t s = (hipStream_t)stream;
     launch_loss_rows(s, a);
     if (is_bf16(c)) {
-        launch_bf16_pack_rows(s, a);
+        const bool along = a.n_block < 256;     // the listed entries in the same launch
         for (int v0 = 0, vn; v0 < a.vocab; v0 += vn) {
             vn = a.direct ? a.vocab : std::min(a.piece, a.vocab - v0);
             if (!a.direct) launch_bf16_pack_head(s, a, v0, vn);
-            launch_bf16_softmax(s, a, v0, vn);
+            launch_bf16_softmax(s, a, v0, vn, along && v0 == 0);
         }
-        launch_bf16_entries(s, a);
+        if (!along) launch_bf16_entries(s, a);
     } else {
         launch_f32_softmax(s, a);
         launch_f32_entries(s, a);
@@ -126,7 +131,7 @@ int backward(const tr_loss_config *c, void *ws, size_t ws_bytes, void *stream, c
 {
     LossArgs a;
     Plan p;
-    if (const int e = arguments(c, in, ws, ws_bytes, teacher, a, p)) return e;
+    if (const int e = arguments(c, in, ws, ws_bytes, teacher, true, a, p)) return e;
     if (!out || (a.rows && (!lse || !grad_loss))) return TR_ERR_INVALID_ARG;
     if ((out->d_hidden && out->d_hidden_stride < c->dim) || (out->d_weight && out->d_weight_stride < c->dim)) return TR_ERR_INVALID_ARG;
     const auto size = [](int dt) { return dt == TR_BF16 ? 2u : 4u; };
@@ -136,30 +141,32 @@ int backward(const tr_loss_config *c, void *ws, size_t ws_bytes, void *stream, c
     a.d_hidden = out->d_hidden; a.dhs = out->d_hidden_stride; a.d_weight = out->d_weight; a.dws = out->d_weight_stride;
     hipStream_t s = (hipStream_t)stream;
     launch_loss_rows(s, a);
-    const bool half = is_bf16(c);
-    if (half && a.rows) {
-        launch_bf16_pack_rows(s, a);
-        launch_bf16_entries(s, a);
-    } else if (a.rows) launch_f32_entries(s, a);
-    launch_loss_values(s, a);
+    const bool half = is_bf16(c), one = a.piece >= a.vocab, along = half && one && a.n_block < 256;
+    if (a.rows && !along) {
+        if (half) launch_bf16_entries(s, a);
+        else launch_f32_entries(s, a);
+        if (!one) launch_loss_values(s, a, false);
+    }
     for (int v0 = 0; v0 < a.vocab; v0 += a.piece) {
         const int vn = std::min(a.piece, a.vocab - v0);
-        if (half) {
-            if (a.rows) {
+        if (a.rows) {
+            if (half) {
                 if (!a.direct) launch_bf16_pack_head(s, a, v0, vn);
-                launch_bf16_probabilities(s, a, v0, vn);
-                launch_loss_scatter(s, a, v0, vn, true);
-                if (a.d_hidden) launch_bf16_hidden_grad(s, a, v0, vn, v0 == 0);
+                launch_bf16_probabilities(s, a, v0, vn, along);
+            } else launch_f32_probabilities(s, a, v0, vn);
+            if (one) launch_loss_values(s, a, true);
+            else launch_loss_scatter(s, a, v0, vn);
+            if (a.d_hidden) {
+                if (half) launch_bf16_hidden_grad(s, a, v0, vn, v0 == 0);
+                else launch_f32_hidden_grad(s, a, v0, vn, v0 == 0);
             }
-            if (a.d_weight) launch_bf16_weight_grad(s, a, v0, vn);
-        } else {
-            launch_f32_probabilities(s, a, v0, vn);
-            launch_loss_scatter(s, a, v0, vn, false);
-            if (a.d_hidden) launch_f32_hidden_grad(s, a, v0, vn, v0 == 0);
-            if (a.d_weight) launch_f32_weight_grad(s, a, v0, vn);
+        }
+        if (a.d_weight) {
+            if (half) launch_bf16_weight_grad(s, a, v0, vn);
+            else launch_f32_weight_grad(s, a, v0, vn);
         }
     }
-    if (a.d_hidden) launch_loss_hidden_grad(s, a, half);
+    if (a.d_hidden) launch_loss_hidden_grad(s, a);
     return enqueued();
 }
 

@@ -225,10 +225,14 @@ __device__ __forceinline__ uint32_t lds_start() { return (uint32_t)(uintptr_t)(_
 #endif
 constexpr int GN = XGN;
 struct Order {
-    int mb, nb, items, per;
-    __device__ __forceinline__ Order(int mb_, int nb_) : mb(mb_), nb(nb_), items(mb_ * nb_), per((mb_ * nb_ + 7) >> 3) {}
-    __device__ __forceinline__ int first() const { return (blockIdx.x & 7) * per + (blockIdx.x >> 3); }
-    __device__ __forceinline__ int end() const { return min(items, ((int)(blockIdx.x & 7) + 1) * per); }
+    int mb, nb, first, end;      // first of this workgroup (of an XCD's first few), end of its XCD's
+    __device__ __forceinline__ Order(int mb_, int nb_, int b) : mb(mb_), nb(nb_)
+    {
+        const int items = mb * nb, per = (items + 7) >> 3;
+        first = (b & 7) * per + (b >> 3);
+        end = min(items, ((b & 7) + 1) * per);
+    }
+    __device__ __forceinline__ Order() {}
     __device__ __forceinline__ void at(int i, int &m, int &n) const
     {
         const int group = i / (GN * mb), in = i - group * GN * mb, width = min(GN, nb - group * GN);
@@ -241,7 +245,7 @@ struct Order {
 struct Place {
     const bf16_t *a, *b;
     long long lda, ldb;
-    int a_limit, b_limit, K, m, n, split;
+    int a_limit, b_limit, n_limit, K, m, n, split;   // n_limit: rows of the product that exist from n's block on
 };
 
 __device__ __forceinline__ const bf16_t *head_rows(const LossArgs &a, int v0, long long &ld)
@@ -250,19 +254,22 @@ __device__ __forceinline__ const bf16_t *head_rows(const LossArgs &a, int v0, lo
     return a.direct ? (const bf16_t *)a.weight + (long long)v0 * a.ws : (const bf16_t *)a.wp;
 }
 
-// What a kernel does: blocks of TM x TN, the place of block (m, n), and what becomes of a wavefront's accumulators.
+// What a kernel does: its blocks of TM x TN and their order, the place of block i, and what becomes of a wavefront's accumulators.
 template <int TM, int TN> struct Logits {
     static constexpr bool A_KC = true, B_KC = true;
     const LossArgs &a;
-    int v0, vn, count;
-    __device__ __forceinline__ Logits(const LossArgs &a_, int v0_, int vn_, int) : a(a_), v0(v0_), vn(vn_), count(a_.head->count) {}
-    __device__ __forceinline__ Order order() const { return Order((vn + TM - 1) / TM, (count + TN - 1) / TN); }
-    __device__ __forceinline__ Place place(int m, int n) const
+    int v0, vn, count, half, rows;
+    Order o;
+    __device__ __forceinline__ Logits(const LossArgs &a_, int v0_, int vn_, int, int b)
+        : a(a_), v0(v0_), vn(vn_), count(a_.head->count), half(a_.grad ? a_.head->half : 0), rows(bf16_products_rows(count, half)), o((vn + TM - 1) / TM, (rows + TN - 1) / TN, b) {}
+    __device__ __forceinline__ Place place(int i) const
     {
         Place p;
-        p.a = head_rows(a, v0, p.lda) + (long long)m * TM * (a.direct ? a.ws : a.d_pad);
-        p.b = (const bf16_t *)a.hp + (size_t)n * TN * a.d_pad;
-        p.ldb = a.d_pad; p.a_limit = vn - m * TM; p.b_limit = TN; p.K = a.d_pad; p.m = m; p.n = n;
+        o.at(i, p.m, p.n);
+        p.a = head_rows(a, v0, p.lda);
+        p.a += (long long)p.m * TM * p.lda;
+        p.b = (const bf16_t *)a.hp + (size_t)p.n * TN * a.d_pad;
+        p.ldb = a.d_pad; p.a_limit = vn - p.m * TM; p.b_limit = TN; p.n_limit = rows - p.n * TN; p.K = a.d_pad;
         return p;
     }
 };
@@ -280,16 +287,16 @@ template <int TM, int TN> struct Softmax : Logits<TM, TN> {
 template <int TM, int TN> struct Probabilities : Logits<TM, TN> {
     using Logits<TM, TN>::Logits;
     int have = -1;               // rows whose lse and weight are held
-    float lse2[2], weight[2];
+    float lse2[2], weight[2];    // (weight 0: a row that is none)
     template <int WM, int WN, int MI, int NI> __device__ __forceinline__ void done(const Place &p, const f32x16 (&c)[MI][NI])
     {
         const LossArgs &a = this->a;
-        const int wn = wavefront() % WN;
+        const int first = p.n * TN + wavefront() % WN * NI * 32, half = this->half;
         if (p.n != have) {
             have = p.n;
 #pragma unroll
             for (int j = 0; j < NI; ++j) {
-                const int row = p.n * TN + (wn * NI + j) * 32 + (threadIdx.x & 31);
+                const int at = first + j * 32 + (threadIdx.x & 31), row = half && at >= half ? at - half : at;
                 lse2[j] = row < this->count ? a.lse[a.idx[row]] * LOG2E : 0.f;
                 weight[j] = row < this->count ? a.grad[a.idx[row]] / a.head->scale : 0.f;
             }
@@ -297,44 +304,66 @@ template <int TM, int TN> struct Probabilities : Logits<TM, TN> {
         const float k2 = LOG2E / a.temperature;
         const bool inside = p.m * TM + TM <= this->vn && p.n * TN + TN <= this->count;
         each_run<WN>(c, [&](int j, int i, int v, float (&x)[8]) {
-            const int row = p.n * TN + i;
+            const int at = p.n * TN + i, row = half && at >= half ? at - half : at;
             v += p.m * TM;
             // rows that do not count and entries that do not exist: zeros, which the next products read
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = inside || (row < this->count && v + e < this->vn) ? weight[j] * term(x[e], k2, lse2[j]) : 0.f;
-            store_run((bf16_t *)a.G + (size_t)row * a.piece + v, x);
+            if (half && first + j * 32 >= half) {      // a pair's second: what rounding leaves
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    const uint32_t hi = two_bf16(x[e], x[e + 1]);
+                    x[e] -= __uint_as_float(hi << 16);
+                    x[e + 1] -= __uint_as_float(hi & 0xffff0000u);
+                }
+            }
+            store_run((bf16_t *)a.G + (size_t)at * a.g_ld + v, x);
         });
     }
 };
 
+// Every sum over the piece's vocabulary in `splits` parts. With 8 or more, part s belongs to XCD s / (splits / 8), which takes all blocks of its parts.
 template <int TM, int TN> struct HiddenGrad {
     static constexpr bool A_KC = false, B_KC = true;
     const LossArgs &a;
-    int v0, vn, first, count, mb, splits, per;
-    __device__ __forceinline__ HiddenGrad(const LossArgs &a_, int v0_, int vn_, int first_) : a(a_), v0(v0_), vn(vn_), first(first_), count(a_.head->count)
+    int v0, vn, first, mb, nb, rows, splits, per, tiles;
+    Order o;
+    __device__ __forceinline__ HiddenGrad(const LossArgs &a_, int v0_, int vn_, int first_, int b) : a(a_), v0(v0_), vn(vn_), first(first_)
     {
+        rows = bf16_products_rows(a.head->count, a.head->half);
         mb = (a.d_pad + TM - 1) / TM;
-        splits = bf16_splits(a, count);
+        nb = (rows + TN - 1) / TN;
+        tiles = mb * nb;
+        splits = bf16_splits(a, rows);
         per = ((vn + splits - 1) / splits + 63) / 64 * 64;
+        o = Order(mb, nb * splits, b);
+        if (splits >= 8) {
+            const int own = tiles * (splits >> 3);
+            o.first = (b & 7) * own + (b >> 3);
+            o.end = ((b & 7) + 1) * own;
+        }
     }
-    __device__ __forceinline__ Order order() const { return Order(mb * splits, (count + TN - 1) / TN); }
-    __device__ __forceinline__ Place place(int m, int n) const
+    __device__ __forceinline__ Place place(int i) const
     {
         Place p;
-        p.split = m / mb; p.m = m - p.split * mb; p.n = n;
+        p.split = i / tiles;
+        Order one = o;
+        one.nb = nb;
+        one.at(i - p.split * tiles, p.m, p.n);
         const int k0 = min(vn, p.split * per);
         p.K = min(vn, k0 + per) - k0;
         p.a = head_rows(a, v0, p.lda);
         p.a += k0 * p.lda + p.m * TM; p.a_limit = a.d_pad - p.m * TM;
-        p.b = (const bf16_t *)a.G + (size_t)n * TN * a.piece + k0; p.ldb = a.piece; p.b_limit = TN;
+        p.b = (const bf16_t *)a.G + (size_t)p.n * TN * a.g_ld + k0; p.ldb = a.g_ld; p.b_limit = TN; p.n_limit = rows - p.n * TN;
         return p;
     }
     template <int WM, int WN, int MI, int NI> __device__ __forceinline__ void done(const Place &p, const f32x16 (&c)[MI][NI])
     {
+        if (!first && p.K == 0) return;
         each_run<WN>(c, [&](int, int i, int d, float (&x)[8]) {
             d += p.m * TM;
             if (d >= a.d_pad) return;
-            float *to = a.acc + ((size_t)p.split * bf16_rows(a, count) + p.n * TN + i) * a.d_pad + d;
+            float *to = a.acc + ((size_t)p.split * bf16_rows(a, rows) + p.n * TN + i) * a.d_pad + d;
             if (!first) {
                 const float4 u = reinterpret_cast<const float4 *>(to)[0], w = reinterpret_cast<const float4 *>(to)[1];
                 x[0] += u.x; x[1] += u.y; x[2] += u.z; x[3] += u.w; x[4] += w.x; x[5] += w.y; x[6] += w.z; x[7] += w.w;
@@ -347,15 +376,17 @@ template <int TM, int TN> struct HiddenGrad {
 template <int TM, int TN> struct WeightGrad {
     static constexpr bool A_KC = false, B_KC = false;
     const LossArgs &a;
-    int v0, vn;
-    __device__ __forceinline__ WeightGrad(const LossArgs &a_, int v0_, int vn_, int) : a(a_), v0(v0_), vn(vn_) {}
-    __device__ __forceinline__ Order order() const { return Order((a.d_pad + TM - 1) / TM, (vn + TN - 1) / TN); }
-    __device__ __forceinline__ Place place(int m, int n) const
+    int v0, vn, rows;
+    Order o;
+    __device__ __forceinline__ WeightGrad(const LossArgs &a_, int v0_, int vn_, int, int b)
+        : a(a_), v0(v0_), vn(vn_), rows(bf16_products_rows(a_.head->count, a_.head->half)), o((a_.d_pad + TM - 1) / TM, (vn_ + TN - 1) / TN, b) {}
+    __device__ __forceinline__ Place place(int i) const
     {
         Place p;
-        p.m = m; p.n = n; p.K = (a.head->count + 63) / 64 * 64;      // G and the rows are zero from the last row that counts to there
-        p.a = (const bf16_t *)a.hp + m * TM; p.lda = a.d_pad; p.a_limit = a.d_pad - m * TM;
-        p.b = (const bf16_t *)a.G + n * TN; p.ldb = a.piece; p.b_limit = a.piece - n * TN;
+        o.at(i, p.m, p.n);
+        p.K = (rows + 63) / 64 * 64;      // G and the packed rows are zero from the last row that counts to there
+        p.a = (const bf16_t *)a.hp + p.m * TM; p.lda = a.d_pad; p.a_limit = a.d_pad - p.m * TM;
+        p.b = (const bf16_t *)a.G + p.n * TN; p.ldb = a.g_ld; p.b_limit = a.piece - p.n * TN; p.n_limit = vn - p.n * TN;
         return p;
     }
     template <int WM, int WN, int MI, int NI> __device__ __forceinline__ void done(const Place &p, const f32x16 (&c)[MI][NI])
@@ -378,16 +409,62 @@ template <int TM, int TN> struct WeightGrad {
     }
 };
 
-// One block a workgroup.
-template <template <int, int> class Job_, class Bl> __global__ __launch_bounds__(512) void block_kernel(LossArgs a, int v0, int vn, int flag)
+// Products of listed entries: a wavefront takes 32 of them, its rows of the head against its packed rows, of which only the diagonal is kept: the matrix unit is
+// all but idle in a product this small, and it gives the bits that the same pair has in a block (the same instruction over the same steps of k).
+__device__ __forceinline__ void entries_group(const LossArgs &a, int group)
 {
-    Job_<Bl::TM, Bl::TN> job(a, v0, vn, flag);
-    const Order o = job.order();
-    const int i = o.first();
-    if (i >= o.end()) return;
-    int m, n;
-    o.at(i, m, n);
-    const Place p = job.place(m, n);
+    const int lane = threadIdx.x & 63, e = group * 32 + (lane & 31), hf = lane >> 5, count = a.head->count;
+    if ((long long)group * 32 >= (long long)count * a.entries) return;
+    const int i = e / a.entries, j = e - i * a.entries;
+    bool on = i < count;
+    const bf16_t *h = (const bf16_t *)a.hp, *w = (const bf16_t *)a.weight;
+    if (on) {
+        const int id = a.ids[(long long)a.idx[i] * a.entries + j];
+        on = id >= 0 && id < a.vocab;
+        h += (size_t)i * a.d_pad;
+        if (on) w += id * a.ws;
+    }
+    f32x16 c;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) c[r] = 0.f;
+    constexpr int AT_ONCE = 8;      // steps of 16 k whose loads are requested together
+    for (int k0 = 0; k0 < a.d_pad; k0 += 16 * AT_ONCE) {
+        bf16x8 x[AT_ONCE], y[AT_ONCE];
+#pragma unroll
+        for (int q = 0; q < AT_ONCE; ++q) {
+            const int k = min(k0 + 16 * q, a.d_pad - 16) + 8 * hf;
+            y[q] = *reinterpret_cast<const bf16x8 *>(h + k);
+            if (a.direct) x[q] = *reinterpret_cast<const bf16x8 *>(w + k);
+            else {
+                uint32_t u[4];
+#pragma unroll
+                for (int p = 0; p < 4; ++p) u[p] = (k + 2 * p < a.dim ? (uint32_t)w[k + 2 * p] : 0u) | (k + 2 * p + 1 < a.dim ? (uint32_t)w[k + 2 * p + 1] << 16 : 0u);
+                x[q] = __builtin_bit_cast(bf16x8, make_uint4(u[0], u[1], u[2], u[3]));
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < AT_ONCE; ++q)
+            if (k0 + 16 * q < a.d_pad) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[q], y[q], c, 0, 0, 0);
+    }
+    const int n = lane & 31;   // row m of column n lies in register (m / 8) * 4 + m % 4 of lane n + 32 * (m / 4 % 2)
+    float d = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) d = (n >> 3) * 4 + (n & 3) == r ? c[r] : d;
+    if (on && ((n >> 2) & 1) == hf) a.value[e] = d;
+}
+
+__global__ __launch_bounds__(64) void bf16_entries_kernel(LossArgs a) { entries_group(a, blockIdx.x); }
+
+// One block a workgroup; the first `extra` (a multiple of 8) workgroups take listed entries instead.
+template <template <int, int> class Job_, class Bl> __global__ __launch_bounds__(512) void block_kernel(LossArgs a, int v0, int vn, int flag, int extra)
+{
+    if ((int)blockIdx.x < extra) {
+        entries_group(a, blockIdx.x * Bl::WAVES + wavefront());
+        return;
+    }
+    Job_<Bl::TM, Bl::TN> job(a, v0, vn, flag, blockIdx.x - extra);
+    if (job.o.first >= job.o.end) return;
+    const Place p = job.place(job.o.first);
     Bl bl;
     bl.a.init(p.a, p.lda, p.a_limit);
     bl.b.init(p.b, p.ldb, p.b_limit);
@@ -404,30 +481,25 @@ template <template <int, int> class Job_> __global__ __launch_bounds__(512) void
     using Job = Job_<T, T>;
     using TA = Tile<T, Job::A_KC, 8>;
     using TB = Tile<T, Job::B_KC, 8>;
-    Job job(a, v0, vn, flag);
-    const Order o = job.order();
-    const int end = o.end(), stride = gridDim.x >> 3, w = wavefront();
-    if (o.first() >= end) return;
+    Job job(a, v0, vn, flag, blockIdx.x);
+    const int begin = job.o.first, end = job.o.end, stride = gridDim.x >> 3, w = wavefront();
+    if (begin >= end) return;
     const bool second = w >= 4;
     const uint32_t lds = lds_start();
 
     // the copies: an operand's next step, of this block or of the next that has any
     TA ta;
     TB tb;
-    int ia = o.first(), ib = ia, steps_a, steps_b, left_a, left_b;
+    int ia = begin, ib = begin, steps_a, steps_b, left_a, left_b;
     auto open_a = [&] {
         for (steps_a = 0; ia < end; ia += stride) {
-            int m, n;
-            o.at(ia, m, n);
-            const Place p = job.place(m, n);
+            const Place p = job.place(ia);
             if (p.K > 0) { steps_a = (p.K + BK - 1) / BK; left_a = p.K; ta.init(p.a, p.lda, p.a_limit); break; }
         }
     };
     auto open_b = [&] {
         for (steps_b = 0; ib < end; ib += stride) {
-            int m, n;
-            o.at(ib, m, n);
-            const Place p = job.place(m, n);
+            const Place p = job.place(ib);
             if (p.K > 0) { steps_b = (p.K + BK - 1) / BK; left_b = p.K; tb.init(p.b, p.ldb, p.b_limit); break; }
         }
     };
@@ -483,10 +555,9 @@ template <template <int, int> class Job_> __global__ __launch_bounds__(512) void
     };
     uint32_t at_a = lds, at_b = lds + TA::BYTES;
 #pragma unroll 1
-    for (int item = o.first(); item < end; item += stride) {
-        int m, n;
-        o.at(item, m, n);
-        const Place p = job.place(m, n);
+    for (int item = begin; item < end; item += stride) {
+        const Place p = job.place(item);
+        const bool works = w / WN * MI * 32 < p.a_limit && w % WN * NI * 32 < p.n_limit;   // the last blocks: nothing is multiplied that does not exist
 #pragma unroll
         for (int i = 0; i < MI; ++i)
 #pragma unroll
@@ -495,25 +566,29 @@ template <template <int, int> class Job_> __global__ __launch_bounds__(512) void
                 for (int r = 0; r < 16; ++r) c[i][j][r] = 0.f;
 #pragma unroll 1
         for (int s = (p.K + BK - 1) / BK; s; --s) {
-            ra.template read<0>(at_a, xa[0]); rb.template read<0>(at_b, xb[0]);
-            ra.template read<1>(at_a, xa[1]); rb.template read<1>(at_b, xb[1]);
+            if (works) {
+                ra.template read<0>(at_a, xa[0]); rb.template read<0>(at_b, xb[0]);
+                ra.template read<1>(at_a, xa[1]); rb.template read<1>(at_b, xb[1]);
+            }
             // the tiles of the step before are free: everyone has read them
             if (steps_b) copy_b();
             const bool ahead = steps_a > 0;
             if (ahead) copy_a();
             wait_lds();
             barrier();
-            products();
+            if (works) products();
             barrier();
-            ra.template read<2>(at_a, xa[0]); rb.template read<2>(at_b, xb[0]);
-            ra.template read<3>(at_a, xa[1]); rb.template read<3>(at_b, xb[1]);
+            if (works) {
+                ra.template read<2>(at_a, xa[0]); rb.template read<2>(at_b, xb[0]);
+                ra.template read<3>(at_a, xa[1]); rb.template read<3>(at_b, xb[1]);
+            }
             // before the barrier after which the next step is read: both its tiles are there, A's of the step after may be under way
             if (second) {
                 if (ahead) wait_all_but<TA::COPIES>();
                 else wait_all_but<0>();
             } else wait_lds();
             barrier();
-            products();
+            if (works) products();
             if (!second) {
                 if (ahead) wait_all_but<TA::COPIES>();
                 else wait_all_but<0>();
@@ -527,61 +602,10 @@ template <template <int, int> class Job_> __global__ __launch_bounds__(512) void
     if (!second) barrier();
 }
 
-// Rows that count, one after the other, whole steps long; zeros up to the end of the last block.
-__global__ __launch_bounds__(256) void bf16_pack_rows_kernel(LossArgs a)
-{
-    const int i = blockIdx.x, count = a.head->count;
-    if (i >= (count + BF16_BLOCK - 1) / BF16_BLOCK * BF16_BLOCK) return;
-    const bf16_t *h = (const bf16_t *)a.hidden + (i < count ? a.idx[i] : 0) * a.hs;
-    for (int k = threadIdx.x; k < a.d_pad; k += 256) ((bf16_t *)a.hp)[(size_t)i * a.d_pad + k] = i < count && k < a.dim ? h[k] : (bf16_t)0;
-}
-
 __global__ __launch_bounds__(256) void bf16_pack_head_kernel(LossArgs a, int v0)
 {
     const bf16_t *w = (const bf16_t *)a.weight + (long long)(v0 + blockIdx.x) * a.ws;
     for (int k = threadIdx.x; k < a.d_pad; k += 256) ((bf16_t *)a.wp)[(size_t)blockIdx.x * a.d_pad + k] = k < a.dim ? w[k] : (bf16_t)0;
-}
-
-// Products of listed entries: a wavefront takes 32 of them, its rows of the head against its hidden rows, of which only the diagonal is kept.
-__global__ __launch_bounds__(64) void bf16_entries_kernel(LossArgs a)
-{
-    const int lane = threadIdx.x, e = blockIdx.x * 32 + (lane & 31), hf = lane >> 5, count = a.head->count;
-    if ((long long)blockIdx.x * 32 >= (long long)count * a.entries) return;
-    const int i = e / a.entries, j = e - i * a.entries;
-    bool on = i < count;
-    const bf16_t *h = (const bf16_t *)a.hp, *w = (const bf16_t *)a.weight;
-    if (on) {
-        const int id = a.ids[(long long)a.idx[i] * a.entries + j];
-        on = id >= 0 && id < a.vocab;
-        h += (size_t)i * a.d_pad;
-        if (on) w += id * a.ws;
-    }
-    f32x16 c;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) c[r] = 0.f;
-    if (a.direct) {
-#pragma unroll 8
-        for (int k = 0; k < a.d_pad; k += 16) {
-            const bf16x8 x = *reinterpret_cast<const bf16x8 *>(w + k + 8 * hf), y = *reinterpret_cast<const bf16x8 *>(h + k + 8 * hf);
-            c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, c, 0, 0, 0);
-        }
-    } else {
-        for (int k = 0; k < a.d_pad; k += 16) {
-            uint32_t q[4];
-#pragma unroll
-            for (int p = 0; p < 4; ++p) {
-                const int at = k + 8 * hf + 2 * p;
-                q[p] = (at < a.dim ? (uint32_t)w[at] : 0u) | (at + 1 < a.dim ? (uint32_t)w[at + 1] << 16 : 0u);
-            }
-            const bf16x8 x = __builtin_bit_cast(bf16x8, make_uint4(q[0], q[1], q[2], q[3])), y = *reinterpret_cast<const bf16x8 *>(h + k + 8 * hf);
-            c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, c, 0, 0, 0);
-        }
-    }
-    const int n = lane & 31;   // row m of column n lies in register (m / 8) * 4 + m % 4 of lane n + 32 * (m / 4 % 2)
-    float d = 0.f;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) d = (n >> 3) * 4 + (n & 3) == r ? c[r] : d;
-    if (on && ((n >> 2) & 1) == hf) a.value[e] = d;
 }
 
 int up_div(int n, int by) { return (n + by - 1) / by; }
@@ -593,43 +617,39 @@ template <class... P, class... A> void launch(void (*kernel)(P...), dim3 grid, i
     hipLaunchKernelGGL(kernel, grid, dim3(512), lds, s, args...);
 }
 
-template <template <int, int> class Job> void launch_job(hipStream_t s, const LossArgs &a, int v0, int vn, int flag, int mb)
+int entry_groups(const LossArgs &a) { return (int)(((long long)a.rows * a.entries + 31) / 32); }
+
+// blocks: those of 256 x n_block there can be (one along the rows, where they are smaller than 256); entries: listed entries too, where workgroups take a block each
+template <template <int, int> class Job> void launch_job(hipStream_t s, const LossArgs &a, int v0, int vn, int flag, int blocks, bool entries)
 {
     constexpr bool A = Job<256, 64>::A_KC, B = Job<256, 64>::B_KC;
     using Small = Block<8, 1, 1, 2, 3, A, B>;       // 256 x 64
     using Middle = Block<4, 2, 2, 2, 3, A, B>;      // 256 x 128
-    if (a.n_block == 64) launch(block_kernel<Job, Small>, dim3(up_div(mb, 8) * 8), Small::LDS, s, a, v0, vn, flag);
-    else if (a.n_block == 128) launch(block_kernel<Job, Middle>, dim3(up_div(mb, 8) * 8), Middle::LDS, s, a, v0, vn, flag);
+    const int extra = entries ? up_div(entry_groups(a), 64) * 8 : 0;
+    const dim3 grid(up_div(blocks, 8) * 8 + extra);
+    if (a.n_block == 64) launch(block_kernel<Job, Small>, grid, Small::LDS, s, a, v0, vn, flag, extra);
+    else if (a.n_block == 128) launch(block_kernel<Job, Middle>, grid, Middle::LDS, s, a, v0, vn, flag, extra);
     else launch(turns_kernel<Job>, dim3(256), 5 * 256 * BK * 2, s, a, v0, vn, flag);
 }
 
 }  // namespace
-
-void launch_bf16_pack_rows(hipStream_t s, const LossArgs &a)
-{
-    hipLaunchKernelGGL(bf16_pack_rows_kernel, dim3(up_div(a.rows, BF16_BLOCK) * BF16_BLOCK), dim3(256), 0, s, a);
-}
 
 void launch_bf16_pack_head(hipStream_t s, const LossArgs &a, int v0, int vn)
 {
     hipLaunchKernelGGL(bf16_pack_head_kernel, dim3(vn), dim3(256), 0, s, a, v0);
 }
 
-void launch_bf16_entries(hipStream_t s, const LossArgs &a)
-{
-    hipLaunchKernelGGL(bf16_entries_kernel, dim3((unsigned)(((long long)a.rows * a.entries + 31) / 32)), dim3(64), 0, s, a);
-}
+void launch_bf16_entries(hipStream_t s, const LossArgs &a) { hipLaunchKernelGGL(bf16_entries_kernel, dim3(entry_groups(a)), dim3(64), 0, s, a); }
 
-void launch_bf16_softmax(hipStream_t s, const LossArgs &a, int v0, int vn) { launch_job<Softmax>(s, a, v0, vn, 0, up_div(vn, BF16_BLOCK)); }
+void launch_bf16_softmax(hipStream_t s, const LossArgs &a, int v0, int vn, bool entries) { launch_job<Softmax>(s, a, v0, vn, 0, up_div(vn, BF16_BLOCK), entries); }
 
 int bf16_softmax_parts(const LossArgs &a) { return up_div(a.vocab, BF16_BLOCK) * (a.n_block == 64 ? 8 : a.n_block == 128 ? 4 : 2); }
 
-void launch_bf16_probabilities(hipStream_t s, const LossArgs &a, int v0, int vn) { launch_job<Probabilities>(s, a, v0, vn, 0, up_div(vn, BF16_BLOCK)); }
+void launch_bf16_probabilities(hipStream_t s, const LossArgs &a, int v0, int vn, bool entries) { launch_job<Probabilities>(s, a, v0, vn, 0, up_div(vn, BF16_BLOCK), entries); }
 
 void launch_bf16_hidden_grad(hipStream_t s, const LossArgs &a, int v0, int vn, bool first)
 {
-    const int mb = up_div(a.d_pad, BF16_BLOCK);
-    launch_job<HiddenGrad>(s, a, v0, vn, first, std::max(mb, std::min(256, mb * a.splits)));
+    launch_job<HiddenGrad>(s, a, v0, vn, first, up_div(a.d_pad, BF16_BLOCK) * std::max(a.splits, 1), false);
 }
 
 void launch_bf16_weight_grad(hipStream_t s, const LossArgs &a, int v0, int vn) { launch(turns_kernel<WeightGrad>, dim3(256), 5 * 256 * BK * 2, s, a, v0, vn, 0); }

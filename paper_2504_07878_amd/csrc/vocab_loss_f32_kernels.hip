@@ -138,7 +138,7 @@ template <class HT, class WT> __global__ __launch_bounds__(256) void f32_probabi
         const float lse = a.lse[a.idx[n]], weight = a.grad[a.idx[n]] / a.head->scale;
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = m + e < vn ? weight * expf(fmaf(v[e], k, -lse)) : 0.f;
-        store_run((float *)a.G + (size_t)n * a.piece + m, v);
+        store_run((float *)a.G + (size_t)n * a.g_ld + m, v);
     });
 }
 
@@ -149,7 +149,7 @@ template <class WT> __global__ __launch_bounds__(256) void f32_hidden_grad_kerne
     const int m0 = blockIdx.x * F32_BLOCK, n0 = blockIdx.y * F32_BLOCK, count = a.head->count;
     if (n0 >= count) return;
     const HeadColumns<WT> A{(const WT *)a.weight, a.ws, v0, vn, a.dim};
-    const PieceRows B{(const float *)a.G, a.piece, count, vn};
+    const PieceRows B{(const float *)a.G, a.g_ld, count, vn};
     f32x16 c[2][2];
     products(A, B, m0, n0, min(vn, (int)blockIdx.z * per), min(vn, ((int)blockIdx.z + 1) * per), sm, c);
     each_run(c, [&](int n, int m, float (&v)[8]) {
@@ -169,7 +169,7 @@ template <class HT, class WT> __global__ __launch_bounds__(256) void f32_weight_
     __shared__ Tiles sm;
     const int m0 = blockIdx.x * F32_BLOCK, n0 = blockIdx.y * F32_BLOCK, count = a.head->count;
     const HiddenColumns<HT> A{(const HT *)a.hidden, a.hs, a.idx, count, a.dim};
-    const PieceColumns B{(const float *)a.G, a.piece, count, vn};
+    const PieceColumns B{(const float *)a.G, a.g_ld, count, vn};
     f32x16 c[2][2];
     products(A, B, m0, n0, 0, count, sm, c);
     const float k = a.head->scale * a.temperature;

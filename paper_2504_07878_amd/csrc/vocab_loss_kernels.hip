@@ -1,5 +1,6 @@
 // Losses over the vocabulary: rows, listed entries and sums. Small kernels beside the products; what they compute is in vocab_loss.h.
 #include "vocab_loss_epilogues.h"
+#include <type_traits>
 
 namespace tr {
 
@@ -12,23 +13,106 @@ __device__ __forceinline__ bool entry_counts(const LossArgs &a, long long at)
     return id >= 0 && id < a.vocab && (!TEACHER || a.teacher[at] != -INFINITY);
 }
 
-// A row counts if it has an entry (and, for gradients, a weight). One thread a row: the entries of a row lie together, and the first that counts ends the search.
+// A row counts if it has an entry (and, for gradients, a weight).
+template <bool TEACHER>
+__device__ __forceinline__ int row_state(const LossArgs &a, int r)
+{
+    int st = ROW_SKIP;
+    const long long at = (long long)r * a.entries;
+    if (!TEACHER) {
+        const int id = a.ids[r];
+        st = id < 0 ? ROW_SKIP : id < a.vocab ? ROW_COUNTS : ROW_BAD;
+    } else {
+        for (int j = 0; j < a.entries && st == ROW_SKIP; j += 8) {     // most rows have one among their first
+            bool any = false;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) any |= entry_counts<TEACHER>(a, at + min(j + e, a.entries - 1));
+            if (any) st = ROW_COUNTS;
+        }
+    }
+    if (a.grad && a.grad[r] == 0.f) st = ROW_SKIP;
+    return st;
+}
+
+// weights that cannot be divided by (none, infinite, too small for a reciprocal share) are taken as they are
+__device__ __forceinline__ float usable(float top) { return top > 1e-30f && top < INFINITY ? top : 1.f; }
+__device__ __forceinline__ int half_of(const LossArgs &a, int count) { return !a.pairs || count == 0 || count > PAIR_ROWS ? 0 : count > 64 ? 128 : 64; }
+
+__device__ __forceinline__ void skipped(const LossArgs &a, int r, int st)
+{
+    const float v = st == ROW_BAD ? __uint_as_float(0x7fc00000u) : 0.f;
+    a.loss[r] = v;
+    a.lse[r] = v;
+}
+
+// Row `to` of the packed rows: row `from` that counts (-1: zeros), whole steps long.
+template <class HT> __device__ __forceinline__ void pack_row(const LossArgs &a, int to, int from)
+{
+    if constexpr (sizeof(HT) == 2) {
+        const HT *h = (const HT *)a.hidden + (long long)max(from, 0) * a.hs;
+        bf16_t *p = (bf16_t *)a.hp + (size_t)to * a.d_pad;
+        if (((reinterpret_cast<uintptr_t>(h) | (uintptr_t)(a.hs * 2)) & 15) == 0 && a.dim == a.d_pad) {
+            for (int k = threadIdx.x * 8; k < a.d_pad; k += blockDim.x * 8)
+                *reinterpret_cast<uint4 *>(p + k) = from < 0 ? make_uint4(0, 0, 0, 0) : *reinterpret_cast<const uint4 *>(h + k);
+        } else {
+            for (int k = threadIdx.x; k < a.d_pad; k += blockDim.x) p[k] = from >= 0 && k < a.dim ? h[k] : (bf16_t)0;
+        }
+    }
+}
+
+// Everything at once for few rows: workgroup j finds row j's place by going over the states of all rows, and packs it; the packed rows past the last are cleared, and
+// with pairs the second halves written, by the workgroups from the end.
+template <bool TEACHER, class HT>
+__global__ __launch_bounds__(256) void loss_prepare_kernel(LossArgs a, int packed)
+{
+    __shared__ int before_s[4], count_s[4], own_s;
+    __shared__ float top_s[4];
+    const int j = blockIdx.x, t = threadIdx.x, lane = t & 63, w = t >> 6;
+    int before = 0, count = 0;
+    float top = 0.f;
+    for (int r = t; r < a.rows; r += 256) {
+        const int st = row_state<TEACHER>(a, r);
+        if (r == j) own_s = st;
+        if (st == ROW_COUNTS) {
+            ++count;
+            before += r < j;
+            if (a.grad) { const float g = fabsf(a.grad[r]); top = g > top ? g : top; }
+        }
+    }
+    for (int o = 32; o; o >>= 1) { before += __shfl_xor(before, o); count += __shfl_xor(count, o); top = fmaxf(top, __shfl_xor(top, o)); }
+    if (lane == 0) { before_s[w] = before; count_s[w] = count; top_s[w] = top; }
+    __syncthreads();
+    before = (before_s[0] + before_s[1]) + (before_s[2] + before_s[3]);
+    count = (count_s[0] + count_s[1]) + (count_s[2] + count_s[3]);
+    const int half = half_of(a, count), own = j < a.rows ? own_s : (int)ROW_SKIP;
+    if (j == 0 && t == 0) {
+        a.head->count = count; a.head->half = half;
+        a.head->scale = usable(fmaxf(fmaxf(top_s[0], top_s[1]), fmaxf(top_s[2], top_s[3])));
+    }
+    if (j < a.rows && t == 0) {
+        a.state[j] = (unsigned char)own;
+        if (own == ROW_COUNTS) a.idx[before] = j;
+        else if (!a.grad) skipped(a, j, own);
+    }
+    if (!packed) return;
+    if (own == ROW_COUNTS) {
+        pack_row<HT>(a, before, j);
+        if (half) pack_row<HT>(a, before + half, j);
+    }
+    // rows without anything: [count, half or the end), and with pairs [half + count, the end)
+    const int firsts = half ? half : packed, gap = firsts - count, all = half ? gap + packed - half - count : gap;
+    for (int i = j; i < all; i += gridDim.x) pack_row<HT>(a, i < gap ? count + i : half + count + (i - gap), -1);
+}
+
+// For many rows: their states, one thread a row, ...
 template <bool TEACHER>
 __global__ __launch_bounds__(256) void loss_state_kernel(LossArgs a)
 {
     const int r = blockIdx.x * 256 + threadIdx.x;
-    if (r >= a.rows) return;
-    int st = ROW_SKIP;
-    for (int j = 0; j < a.entries && st == ROW_SKIP; ++j) {
-        const long long at = (long long)r * a.entries + j;
-        if (entry_counts<TEACHER>(a, at)) st = ROW_COUNTS;
-        else if (!TEACHER && a.ids[at] >= a.vocab) st = ROW_BAD;
-    }
-    if (a.grad && a.grad[r] == 0.f) st = ROW_SKIP;
-    a.state[r] = (unsigned char)st;
+    if (r < a.rows) a.state[r] = (unsigned char)row_state<TEACHER>(a, r);
 }
 
-// One workgroup lists the rows that count, in order, 1024 rows at a time; the rows that do not get their loss here. The rows' weights in the
+// ... their list by one workgroup, in order, 1024 rows at a time; the rows that do not count get their loss here. The rows' weights in the
 // gradients are taken relative to the largest |weight|, by which the gradients are multiplied at the end: with equal weights G then holds p - q itself, whose
 // 0 - 1 has no rounding.
 __global__ __launch_bounds__(1024) void loss_list_kernel(LossArgs a)
@@ -54,29 +138,45 @@ __global__ __launch_bounds__(1024) void loss_list_kernel(LossArgs a)
                 const float g = fabsf(a.grad[r]);
                 top = g > top ? g : top;
             }
-        } else if (r < a.rows && !a.grad) {
-            const float v = st == ROW_BAD ? __uint_as_float(0x7fc00000u) : 0.f;
-            a.loss[r] = v;
-            a.lse[r] = v;
-        }
+        } else if (r < a.rows && !a.grad) skipped(a, r, st);
     }
     for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
     if (lane == 0) tops[w] = top;
     __syncthreads();
     if (t == 0) {
         for (int i = 0; i < 16; ++i) top = fmaxf(top, tops[i]);
-        // weights that cannot be divided by (none, infinite, too small for a reciprocal share) are taken as they are
-        a.head->count = before; a.head->rows = a.rows; a.head->scale = top > 1e-30f && top < INFINITY ? top : 1.f;
+        a.head->count = before; a.head->half = half_of(a, before); a.head->scale = usable(top);
     }
+}
+
+// ... and the packed rows, one after the other, zeros up to the end of the last block.
+template <class HT>
+__global__ __launch_bounds__(256) void loss_pack_kernel(LossArgs a)
+{
+    const int i = blockIdx.x, count = a.head->count, half = a.head->half;
+    if (i >= (bf16_products_rows(count, half) + BF16_BLOCK - 1) / BF16_BLOCK * BF16_BLOCK) return;
+    const int row = half && i >= half ? i - half : i;
+    pack_row<HT>(a, i, row < count ? a.idx[row] : -1);
+}
+
+template <bool TEACHER, class HT> static void rows_of(hipStream_t s, const LossArgs &a)
+{
+    const int packed = a.hp ? (a.rows + BF16_BLOCK - 1) / BF16_BLOCK * BF16_BLOCK : 0;
+    if (a.rows <= 1024 && (long long)a.rows * a.entries <= 16384) {
+        const int used = a.rows <= PAIR_ROWS && a.hp ? (a.pairs ? (a.rows <= 64 ? 128 : 256) : (a.rows <= 64 ? 64 : 128)) : packed;   // what the products' blocks read
+        hipLaunchKernelGGL((loss_prepare_kernel<TEACHER, HT>), dim3(a.rows), dim3(256), 0, s, a, used);
+        return;
+    }
+    hipLaunchKernelGGL((loss_state_kernel<TEACHER>), dim3((a.rows + 255) / 256), dim3(256), 0, s, a);
+    hipLaunchKernelGGL(loss_list_kernel, dim3(1), dim3(1024), 0, s, a);
+    if (packed) hipLaunchKernelGGL((loss_pack_kernel<HT>), dim3(packed), dim3(256), 0, s, a);
 }
 
 void launch_loss_rows(hipStream_t s, const LossArgs &a)
 {
-    if (a.rows > 0) {
-        if (a.teacher) hipLaunchKernelGGL((loss_state_kernel<true>), dim3((a.rows + 255) / 256), dim3(256), 0, s, a);
-        else hipLaunchKernelGGL((loss_state_kernel<false>), dim3((a.rows + 255) / 256), dim3(256), 0, s, a);
-    }
-    hipLaunchKernelGGL(loss_list_kernel, dim3(1), dim3(1024), 0, s, a);
+    if (!a.rows) { hipLaunchKernelGGL(loss_list_kernel, dim3(1), dim3(1024), 0, s, a); return; }
+    if (a.teacher) { if (a.hdt == DT_BF16) rows_of<true, bf16_t>(s, a); else rows_of<true, float>(s, a); }
+    else { if (a.hdt == DT_BF16) rows_of<false, bf16_t>(s, a); else rows_of<false, float>(s, a); }
 }
 
 // ------------------------------------------------------------------ listed entries
@@ -104,47 +204,59 @@ __device__ __forceinline__ Shares shares_of(const LossArgs &a, int r)
     }
 }
 
-// A workgroup takes a row: it joins the blocks' running softmaxes, then takes the row's entries. Sums in a fixed order.
+// A workgroup takes ROWS rows that count: 256 / ROWS threads join a row's running softmaxes, then a wavefront takes the row's entries. Sums in a fixed order.
 // lse - z_j = ln 2 (m - k c_j) + log s: no rounding of lse in it.
-template <bool TEACHER>
+template <bool TEACHER, int ROWS>
 __global__ __launch_bounds__(256) void loss_finish_kernel(LossArgs a, int parts)
 {
-    __shared__ float2 joined[4];
-    __shared__ float sums[4];
-    const int i = blockIdx.x, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    if (i >= a.head->count) return;
-    const int r = a.idx[i];
-    float2 t = make_float2(-INFINITY, 0.f);
-    for (int p = threadIdx.x; p < parts; p += 256) t = join(t, a.part[(size_t)p * a.part_ld + i]);
-    for (int o = 32; o; o >>= 1) {
-        const float2 u = make_float2(__shfl_xor(t.x, o), __shfl_xor(t.y, o));
-        t = lane & o ? join(u, t) : join(t, u);
-    }
-    if (lane == 0) joined[w] = t;
+    __shared__ float2 joined[256];
+    const int i0 = blockIdx.x * ROWS, count = a.head->count, t = threadIdx.x, lane = t & 63, w = t >> 6;
+    if (i0 >= count) return;
+    const int mine = i0 + t % ROWS;
+    float2 x = make_float2(-INFINITY, 0.f);
+    if (mine < count)
+        for (int p = t / ROWS; p < parts; p += 256 / ROWS) x = join(x, a.part[(size_t)p * a.part_ld + mine]);
+    joined[t] = x;
     __syncthreads();
-    t = join(join(joined[0], joined[1]), join(joined[2], joined[3]));
-    const float ls = logf(t.y), k2 = LOG2E / a.temperature, at = t.x == -INFINITY ? 0.f : t.x;
-    const Shares sh = shares_of<TEACHER>(a, r);
-    const float ltot = TEACHER ? logf(sh.total) : 0.f;
-    float s = 0.f;
-    for (int j = threadIdx.x; j < a.entries; j += 256) {
-        const long long from = (long long)r * a.entries + j;
-        if (!entry_counts<TEACHER>(a, from)) continue;
-        const float rel = TEACHER ? (a.teacher[from] - sh.top) / a.temperature : 0.f, q = TEACHER ? expf(rel) / sh.total : 1.f;
-        const float left = LN2 * -fmaf(a.value[(size_t)i * a.entries + j], k2, -at) + ls;
-        if (q != 0.f) s += q * ((rel - ltot) + left);
+    for (int o = 128; o >= ROWS; o >>= 1) {
+        if (t < o) joined[t] = join(joined[t], joined[t + o]);
+        __syncthreads();
     }
-    s = sum64(s);
-    if (lane == 0) sums[w] = s;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        a.lse[r] = LN2 * t.x + ls;
-        a.loss[r] = a.temperature * a.temperature * ((sums[0] + sums[1]) + (sums[2] + sums[3]));
+    for (int q = w; q < ROWS && i0 + q < count; q += 4) {
+        const int i = i0 + q, r = a.idx[i];
+        const float2 st = joined[q];
+        const float ls = logf(st.y), k2 = LOG2E / a.temperature, at = st.x == -INFINITY ? 0.f : st.x;
+        const Shares sh = shares_of<TEACHER>(a, r);
+        const float ltot = TEACHER ? logf(sh.total) : 0.f;
+        float s = 0.f;
+        for (int j = lane; j < a.entries; j += 64) {
+            const long long from = (long long)r * a.entries + j;
+            if (!entry_counts<TEACHER>(a, from)) continue;
+            const float rel = TEACHER ? (a.teacher[from] - sh.top) / a.temperature : 0.f, e = TEACHER ? expf(rel) / sh.total : 1.f;
+            const float left = LN2 * -fmaf(a.value[(size_t)i * a.entries + j], k2, -at) + ls;
+            if (e != 0.f) s += e * ((rel - ltot) + left);
+        }
+        s = sum64(s);
+        if (lane == 0) {
+            a.lse[r] = LN2 * st.x + ls;
+            a.loss[r] = a.temperature * a.temperature * s;
+        }
     }
 }
 
-// p - q of every listed entry of a row from its product (an id listed twice: p less both shares, in both places), by the row's weight
-template <bool TEACHER>
+// What G holds for an entry v of row i.
+template <bool BF16> __device__ __forceinline__ void place_entry(const LossArgs &a, int i, int v, float x)
+{
+    if constexpr (BF16) {
+        bf16_t *to = (bf16_t *)a.G + (size_t)i * a.g_ld + v;
+        store_one(to, x);
+        const int half = a.head->half;
+        if (half) { const bf16_t hi = (bf16_t)two_bf16(x, 0.f); store_one(to + (size_t)half * a.g_ld, x - load_one(&hi)); }
+    } else ((float *)a.G)[(size_t)i * a.g_ld + v] = x;
+}
+
+// p - q of every listed entry of a row from its product (an id listed twice: p less both shares, in both places), by the row's weight. PLACE: into G right away.
+template <bool TEACHER, bool PLACE, bool BF16>
 __global__ __launch_bounds__(256) void loss_values_kernel(LossArgs a)
 {
     const int i = blockIdx.x;
@@ -163,11 +275,13 @@ __global__ __launch_bounds__(256) void loss_values_kernel(LossArgs a)
                 if (a.ids[at0 + o] == id && entry_counts<TEACHER>(a, at0 + o)) q += expf((a.teacher[at0 + o] - sh.top) / a.temperature) / sh.total;
         }
         float &v = a.value[(size_t)i * a.entries + j];
-        v = weight * (expf(fmaf(v, k, -lse)) - q);
+        const float x = weight * (expf(fmaf(v, k, -lse)) - q);
+        if (PLACE) place_entry<BF16>(a, i, id, x);
+        else v = x;
     }
 }
 
-template <bool TEACHER, class GT>
+template <bool TEACHER, bool BF16>
 __global__ __launch_bounds__(256) void loss_scatter_kernel(LossArgs a, int v0, int vn)
 {
     const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
@@ -176,65 +290,87 @@ __global__ __launch_bounds__(256) void loss_scatter_kernel(LossArgs a, int v0, i
     const long long from = (long long)a.idx[i] * a.entries + j;
     const int v = a.ids[from] - v0;
     if (v < 0 || v >= vn || !entry_counts<TEACHER>(a, from)) return;
-    store_one((GT *)a.G + (size_t)i * a.piece + v, a.value[at]);
+    place_entry<BF16>(a, i, v, a.value[at]);
 }
 
+// go(there is a teacher, products are bf16)
+template <class Go> static void by_kind(const LossArgs &a, Go go)
+{
+    using Yes = std::integral_constant<bool, true>;
+    using No = std::integral_constant<bool, false>;
+    if (a.teacher) { if (a.hdt == DT_BF16) go(Yes{}, Yes{}); else go(Yes{}, No{}); }
+    else { if (a.hdt == DT_BF16) go(No{}, Yes{}); else go(No{}, No{}); }
+}
+
+// Few rows take a workgroup each, so that their parts are read at once; many take eight, whose parts lie together.
 void launch_loss_finish(hipStream_t s, const LossArgs &a, int parts)
 {
     if (!a.rows) return;
-    if (a.teacher) hipLaunchKernelGGL((loss_finish_kernel<true>), dim3(a.rows), dim3(256), 0, s, a, parts);
-    else hipLaunchKernelGGL((loss_finish_kernel<false>), dim3(a.rows), dim3(256), 0, s, a, parts);
+    by_kind(a, [&](auto t, auto) {
+        if (a.rows <= 256) hipLaunchKernelGGL((loss_finish_kernel<decltype(t)::value, 1>), dim3(a.rows), dim3(256), 0, s, a, parts);
+        else hipLaunchKernelGGL((loss_finish_kernel<decltype(t)::value, 8>), dim3((a.rows + 7) / 8), dim3(256), 0, s, a, parts);
+    });
 }
 
-void launch_loss_values(hipStream_t s, const LossArgs &a)
+void launch_loss_values(hipStream_t s, const LossArgs &a, bool place)
 {
     if (!a.rows) return;
-    if (a.teacher) hipLaunchKernelGGL((loss_values_kernel<true>), dim3(a.rows), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((loss_values_kernel<false>), dim3(a.rows), dim3(256), 0, s, a);
+    by_kind(a, [&](auto t, auto b) {
+        if (place) hipLaunchKernelGGL((loss_values_kernel<decltype(t)::value, true, decltype(b)::value>), dim3(a.rows), dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((loss_values_kernel<decltype(t)::value, false, decltype(b)::value>), dim3(a.rows), dim3(256), 0, s, a);
+    });
 }
 
-void launch_loss_scatter(hipStream_t s, const LossArgs &a, int v0, int vn, bool g_bf16)
+void launch_loss_scatter(hipStream_t s, const LossArgs &a, int v0, int vn)
 {
     if (!a.rows) return;
     const dim3 grid((unsigned)(((long long)a.rows * a.entries + 255) / 256));
-    if (a.teacher) {
-        if (g_bf16) hipLaunchKernelGGL((loss_scatter_kernel<true, bf16_t>), grid, dim3(256), 0, s, a, v0, vn);
-        else hipLaunchKernelGGL((loss_scatter_kernel<true, float>), grid, dim3(256), 0, s, a, v0, vn);
-    } else {
-        if (g_bf16) hipLaunchKernelGGL((loss_scatter_kernel<false, bf16_t>), grid, dim3(256), 0, s, a, v0, vn);
-        else hipLaunchKernelGGL((loss_scatter_kernel<false, float>), grid, dim3(256), 0, s, a, v0, vn);
-    }
+    by_kind(a, [&](auto t, auto b) { hipLaunchKernelGGL((loss_scatter_kernel<decltype(t)::value, decltype(b)::value>), grid, dim3(256), 0, s, a, v0, vn); });
 }
 
 // ------------------------------------------------------------------ gradient to the hidden rows
 
-// a workgroup writes the i-th row that counts from its sums, in order of the splits, and clears row i if that does not count
+// A workgroup takes 256 columns of the i-th row that counts: its wavefronts every fourth split each, in order, joined in a fixed order; and clears those of row i
+// if that does not count.
 template <class HT, bool BF16>
 __global__ __launch_bounds__(256) void hidden_grad_kernel(LossArgs a)
 {
-    const int i = blockIdx.x, count = a.head->count;
+    __shared__ float4 sums[3][64];
+    const int i = blockIdx.x, count = a.head->count, lane = threadIdx.x & 63, w = threadIdx.x >> 6, j = blockIdx.y * 256 + lane * 4;
     if (i < count) {
-        const int r = a.idx[i], splits = BF16 ? bf16_splits(a, count) : a.splits;
-        const size_t apart = (size_t)(BF16 ? bf16_rows(a, count) : a.n_pad) * a.d_pad;
-        const float c = a.head->scale * a.temperature;
-        HT *out = (HT *)a.d_hidden + (long long)r * a.dhs;
-        for (int j = threadIdx.x; j < a.dim; j += 256) {
-            float v = 0.f;
-            for (int p = 0; p < splits; ++p) v += a.acc[p * apart + (size_t)i * a.d_pad + j];
-            store_one(out + j, c * v);
+        const int half = BF16 ? a.head->half : 0, rows = BF16 ? bf16_products_rows(count, half) : a.n_pad, splits = BF16 ? bf16_splits(a, rows) : a.splits;
+        const size_t apart = (size_t)(BF16 ? bf16_rows(a, rows) : rows) * a.d_pad;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        auto add = [&](float4 &to, const float4 u) { to.x += u.x; to.y += u.y; to.z += u.z; to.w += u.w; };
+        if (j < a.d_pad)
+            for (int p = w; p < splits; p += 4) {
+                const float *at = a.acc + p * apart + (size_t)i * a.d_pad + j;
+                add(v, *reinterpret_cast<const float4 *>(at));
+                if (half) add(v, *reinterpret_cast<const float4 *>(at + (size_t)half * a.d_pad));
+            }
+        if (w) sums[w - 1][lane] = v;
+        __syncthreads();
+        if (w == 0) {
+            add(v, sums[0][lane]); add(v, sums[1][lane]); add(v, sums[2][lane]);
+            const float c = a.head->scale * a.temperature, x[4] = {v.x, v.y, v.z, v.w};
+            HT *out = (HT *)a.d_hidden + (long long)a.idx[i] * a.dhs;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) if (j + e < a.dim) store_one(out + j + e, c * x[e]);
         }
     }
-    if (a.state[i] != ROW_COUNTS) {
+    if (a.state[i] != ROW_COUNTS && w == 0) {
         HT *out = (HT *)a.d_hidden + (long long)i * a.dhs;
-        for (int j = threadIdx.x; j < a.dim; j += 256) store_one(out + j, 0.f);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) if (j + e < a.dim) store_one(out + j + e, 0.f);
     }
 }
 
-void launch_loss_hidden_grad(hipStream_t s, const LossArgs &a, bool bf16)
+void launch_loss_hidden_grad(hipStream_t s, const LossArgs &a)
 {
     if (!a.rows) return;
-    if (bf16) hipLaunchKernelGGL((hidden_grad_kernel<bf16_t, true>), dim3(a.rows), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((hidden_grad_kernel<float, false>), dim3(a.rows), dim3(256), 0, s, a);
+    const dim3 grid(a.rows, (a.dim + 255) / 256);
+    if (a.hdt == DT_BF16) hipLaunchKernelGGL((hidden_grad_kernel<bf16_t, true>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((hidden_grad_kernel<float, false>), grid, dim3(256), 0, s, a);
 }
 
 }  // namespace tr
