@@ -49,7 +49,7 @@ Plan plan_of(const tr_loss_config *c)
     p.head = take(sizeof(LossHead));
     p.idx = take((size_t)p.n_pad * 4);
     p.state = take(c->max_rows);
-    p.part = take(vocab / block * 2 * p.n_pad * sizeof(float2));   // two wavefronts' parts a block of 256 rows; four of 128 or eight of 64
+    p.part = take(vocab / block * 2 * p.n_pad * sizeof(float2));   // two wavefronts' parts a block of 256 rows
     p.value = take((size_t)p.n_pad * c->max_entries * 4);
     p.G = take((size_t)p.n_pad * p.g_ld * g_size);
     // bf16, rows of all splits (bf16_splits): blocks * splits <= 256 where there are fewer than 32 blocks, 8 splits up to 1024 blocks, one from there on
@@ -93,7 +93,7 @@ int arguments(const tr_loss_config *c, const tr_loss_rows *in, void *ws, size_t 
         a.pairs = gradient;
         const int rows = gradient && a.rows <= PAIR_ROWS ? 2 * a.rows : a.rows;
         a.n_block = rows <= 64 && !gradient ? 64 : rows <= 128 ? 128 : 256;
-        if (a.n_block < 256) a.part_ld = a.n_block;   // more parts, of fewer rows
+        if (a.n_block < 256) a.part_ld = a.n_block;
         a.direct = a.dim % 64 == 0 && a.ws % 8 == 0 && a.ws < (1 << 22) && (reinterpret_cast<uintptr_t>(a.weight) & 15) == 0;
     }
     return TR_OK;

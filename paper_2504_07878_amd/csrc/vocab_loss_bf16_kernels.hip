@@ -130,7 +130,7 @@ template <int T, bool KC, bool FEAT, int N> struct Reader {
 // One block by WM x WN wavefronts, each MI x NI accumulators; A_KC, B_KC: where the operands have k contiguous. A ring of STAGES steps in LDS, one barrier a
 // step; the matrix operands of 16 k are read one such step ahead. For blocks of few rows, which are bound by reading the head.
 template <int WM_, int WN_, int MI_, int NI_, int STAGES, bool A_KC, bool B_KC> struct Block {
-    static constexpr int WM = WM_, WN = WN_, MI = MI_, NI = NI_, WAVES = WM * WN, TM = WM * MI * 32, TN = WN * NI * 32;
+    static constexpr int WM = WM_, WN = WN_, MI = MI_, NI = NI_, WAVES = WM * WN, TM = WM * MI * 32, TN = WN * NI * 32, STAGES_ = STAGES;
     using TA = Tile<TM, A_KC, WAVES>;
     using TB = Tile<TN, B_KC, WAVES>;
     static constexpr int STAGE = TA::BYTES + TB::BYTES, LDS = STAGES * STAGE;
@@ -274,13 +274,25 @@ template <int TM, int TN> struct Logits {
     }
 };
 
+constexpr int LDS_OF_RING = 144 << 10;      // of stream_kernel at most; behind it what a block's wavefronts exchange
+
 template <int TM, int TN> struct Softmax : Logits<TM, TN> {
     using Logits<TM, TN>::Logits;
     template <int WM, int WN, int MI, int NI> __device__ __forceinline__ void done(const Place &p, const f32x16 (&c)[MI][NI])
     {
         const LossArgs &a = this->a;
         const int w = wavefront(), wm = w / WN, wn = w % WN;
-        softmax_part(c, a.part + ((size_t)(this->v0 / TM + p.m) * WM + wm) * a.part_ld + p.n * TN + wn * NI * 32, p.m * TM + wm * MI * 32, this->vn, LOG2E / a.temperature);
+        if constexpr (WM > 2) {      // few rows: the block's wavefronts join their parts in LDS
+            float2 *red = reinterpret_cast<float2 *>(dynamic_lds + LDS_OF_RING);
+            softmax_part(c, red + wm * TN + wn * NI * 32, p.m * TM + wm * MI * 32, this->vn, LOG2E / a.temperature);
+            __syncthreads();
+            for (int i = threadIdx.x; i < TN; i += WM * WN * 64) {
+                float2 t = red[i];
+#pragma unroll
+                for (int q = 1; q < WM; ++q) t = join(t, red[q * TN + i]);
+                a.part[(size_t)(this->v0 / TM + p.m) * a.part_ld + p.n * TN + i] = t;
+            }
+        } else softmax_part(c, a.part + ((size_t)(this->v0 / TM + p.m) * WM + wm) * a.part_ld + p.n * TN + wn * NI * 32, p.m * TM + wm * MI * 32, this->vn, LOG2E / a.temperature);
     }
 };
 
@@ -393,19 +405,40 @@ template <int TM, int TN> struct WeightGrad {
     {
         const float k = a.head->scale * a.temperature;
         const bool whole = ((reinterpret_cast<uintptr_t>(a.d_weight) | (uintptr_t)(a.dws * 2)) & 15) == 0;
-        each_run<WN>(c, [&](int, int i, int d, float (&x)[8]) {
-            const int v = p.n * TN + i;
-            d += p.m * TM;
-            if (v >= vn || d >= a.dim) return;
-            bf16_t *to = (bf16_t *)a.d_weight + (long long)(v0 + v) * a.dws + d;
+        bf16_t *const out = (bf16_t *)a.d_weight + (long long)(v0 + p.n * TN) * a.dws + p.m * TM;
+        const int vs = vn - p.n * TN, ds = a.dim - p.m * TM;      // what exists of the block
+        if constexpr (TM == 128) {
+            // through LDS, which is free by then, so that a row's stores are whole lines of memory: 16-byte pieces, permuted by the row
+            uint4 *const tile = reinterpret_cast<uint4 *>(dynamic_lds);
+            each_run<WN>(c, [&](int, int i, int d, float (&x)[8]) {
+                tile[i * 16 + ((d >> 3) ^ (i & 15))] = make_uint4(two_bf16(k * x[0], k * x[1]), two_bf16(k * x[2], k * x[3]), two_bf16(k * x[4], k * x[5]), two_bf16(k * x[6], k * x[7]));
+            });
+            __syncthreads();
+#pragma unroll 4
+            for (int at = threadIdx.x; at < TN * 16; at += WM * WN * 64) {
+                const int v = at >> 4, d = (at & 15) * 8;
+                if (v >= vs || d >= ds) continue;
+                const uint4 u = tile[v * 16 + ((at & 15) ^ (v & 15))];
+                bf16_t *to = out + (long long)v * a.dws + d;
+                if (whole && d + 8 <= ds) *reinterpret_cast<uint4 *>(to) = u;
+                else {
+                    const uint32_t q[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] *= k;
-            if (whole && d + 8 <= a.dim) store_run(to, x);
-            else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) if (d + e < a.dim) store_one(to + e, x[e]);
+                    for (int e = 0; e < 8; ++e) if (d + e < ds) to[e] = (bf16_t)(q[e >> 1] >> (16 * (e & 1)));
+                }
             }
-        });
+        } else
+            each_run<WN>(c, [&](int, int i, int d, float (&x)[8]) {
+                if (i >= vs || d >= ds) return;
+                bf16_t *to = out + (long long)i * a.dws + d;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] *= k;
+                if (whole && d + 8 <= ds) store_run(to, x);
+                else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) if (d + e < ds) store_one(to + e, x[e]);
+                }
+            });
     }
 };
 
@@ -435,12 +468,7 @@ __device__ __forceinline__ void entries_group(const LossArgs &a, int group)
             const int k = min(k0 + 16 * q, a.d_pad - 16) + 8 * hf;
             y[q] = *reinterpret_cast<const bf16x8 *>(h + k);
             if (a.direct) x[q] = *reinterpret_cast<const bf16x8 *>(w + k);
-            else {
-                uint32_t u[4];
-#pragma unroll
-                for (int p = 0; p < 4; ++p) u[p] = (k + 2 * p < a.dim ? (uint32_t)w[k + 2 * p] : 0u) | (k + 2 * p + 1 < a.dim ? (uint32_t)w[k + 2 * p + 1] << 16 : 0u);
-                x[q] = __builtin_bit_cast(bf16x8, make_uint4(u[0], u[1], u[2], u[3]));
-            }
+            else x[q] = __builtin_bit_cast(bf16x8, load8(w, k, on ? a.dim : 0));
         }
 #pragma unroll
         for (int q = 0; q < AT_ONCE; ++q)
@@ -455,14 +483,86 @@ __device__ __forceinline__ void entries_group(const LossArgs &a, int group)
 
 __global__ __launch_bounds__(64) void bf16_entries_kernel(LossArgs a) { entries_group(a, blockIdx.x); }
 
-// One block a workgroup; the first `extra` (a multiple of 8) workgroups take listed entries instead.
-template <template <int, int> class Job_, class Bl> __global__ __launch_bounds__(512) void block_kernel(LossArgs a, int v0, int vn, int flag, int extra)
+// Few rows, bound by the head's bytes: one workgroup a compute unit takes block after block, the copies running on across blocks: a ring of steps in LDS, one barrier a
+// step. The first `extra` (a multiple of 8) workgroups take listed entries instead.
+template <template <int, int> class Job_, class Bl> __global__ __launch_bounds__(Bl::WAVES * 64) void stream_kernel(LossArgs a, int v0, int vn, int flag, int extra)
 {
     if ((int)blockIdx.x < extra) {
         entries_group(a, blockIdx.x * Bl::WAVES + wavefront());
         return;
     }
-    Job_<Bl::TM, Bl::TN> job(a, v0, vn, flag, blockIdx.x - extra);
+    constexpr int MI = Bl::MI, NI = Bl::NI, STAGES = Bl::STAGES_, COPIES = Bl::TA::COPIES + Bl::TB::COPIES;
+    using Job = Job_<Bl::TM, Bl::TN>;
+    Job job(a, v0, vn, flag, blockIdx.x - extra);
+    const int begin = job.o.first, end = job.o.end, stride = (gridDim.x - extra) >> 3, w = wavefront();
+    if (begin >= end) return;
+    const uint32_t lds = lds_start();
+    typename Bl::TA ta;
+    typename Bl::TB tb;
+    int item = begin, steps, left, ahead = 0;      // of the copies; steps that are on their way or there
+    auto open = [&] {
+        for (steps = 0; item < end; item += stride) {
+            const Place p = job.place(item);
+            if (p.K > 0) { steps = (p.K + BK - 1) / BK; left = p.K; ta.init(p.a, p.lda, p.a_limit); tb.init(p.b, p.ldb, p.b_limit); break; }
+        }
+    };
+    int to = 0;
+    auto copy = [&] {
+        if (!steps) return;
+        ta.issue(lds + to * Bl::STAGE, left);
+        tb.issue(lds + to * Bl::STAGE + Bl::TA::BYTES, left);
+        to = to + 1 < STAGES ? to + 1 : 0;
+        left -= BK;
+        ++ahead;
+        if (--steps == 0) { item += stride; open(); }
+    };
+    open();
+#pragma unroll
+    for (int q = 0; q < STAGES - 1; ++q) copy();
+    Reader<Bl::TM, Job::A_KC, true, MI> ra;
+    Reader<Bl::TN, Job::B_KC, false, NI> rb;
+    ra.init(w / Bl::WN * MI * 32);
+    rb.init(w % Bl::WN * NI * 32);
+    f32x16 c[MI][NI];
+    int from = 0;
+#pragma unroll 1
+    for (int it = begin; it < end; it += stride) {
+        const Place p = job.place(it);
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) c[i][j][r] = 0.f;
+#pragma unroll 1
+        for (int s = (p.K + BK - 1) / BK; s; --s) {
+            // this step has landed, and everyone has read the one before, whose place is the next copy's
+            if (ahead == STAGES - 1) landed_and_barrier<(STAGES - 2) * COPIES>();
+            else landed_and_barrier<0>();
+            copy();
+            const uint32_t at = lds + from * Bl::STAGE;
+            bf16x8 xa[4][MI], xb[4][NI];
+            ra.template read<0>(at, xa[0]); rb.template read<0>(at + Bl::TA::BYTES, xb[0]);
+            ra.template read<1>(at, xa[1]); rb.template read<1>(at + Bl::TA::BYTES, xb[1]);
+            ra.template read<2>(at, xa[2]); rb.template read<2>(at + Bl::TA::BYTES, xb[2]);
+            ra.template read<3>(at, xa[3]); rb.template read<3>(at + Bl::TA::BYTES, xb[3]);
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int i = 0; i < MI; ++i)
+#pragma unroll
+                    for (int j = 0; j < NI; ++j) c[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xa[q][i], xb[q][j], c[i][j], 0, 0, 0);
+            --ahead;
+            from = from + 1 < STAGES ? from + 1 : 0;
+        }
+        job.template done<Bl::WM, Bl::WN, MI, NI>(p, c);
+    }
+}
+
+// One block a workgroup.
+template <template <int, int> class Job_, class Bl> __global__ __launch_bounds__(Bl::WAVES * 64) void block_kernel(LossArgs a, int v0, int vn, int flag)
+{
+    Job_<Bl::TM, Bl::TN> job(a, v0, vn, flag, blockIdx.x);
     if (job.o.first >= job.o.end) return;
     const Place p = job.place(job.o.first);
     Bl bl;
@@ -602,19 +702,19 @@ template <template <int, int> class Job_> __global__ __launch_bounds__(512) void
     if (!second) barrier();
 }
 
-__global__ __launch_bounds__(256) void bf16_pack_head_kernel(LossArgs a, int v0)
+__global__ __launch_bounds__(128) void bf16_pack_head_kernel(LossArgs a, int v0)
 {
     const bf16_t *w = (const bf16_t *)a.weight + (long long)(v0 + blockIdx.x) * a.ws;
-    for (int k = threadIdx.x; k < a.d_pad; k += 256) ((bf16_t *)a.wp)[(size_t)blockIdx.x * a.d_pad + k] = k < a.dim ? w[k] : (bf16_t)0;
+    for (int k = threadIdx.x * 8; k < a.d_pad; k += 1024) *reinterpret_cast<uint4 *>((bf16_t *)a.wp + (size_t)blockIdx.x * a.d_pad + k) = load8(w, k, a.dim);
 }
 
 int up_div(int n, int by) { return (n + by - 1) / by; }
 
 // a kernel's dynamic LDS beyond 64 KiB has to be allowed once per kernel and device; asking again costs nothing that counts beside a launch
-template <class... P, class... A> void launch(void (*kernel)(P...), dim3 grid, int lds, hipStream_t s, A... args)
+template <class... P, class... A> void launch(void (*kernel)(P...), dim3 grid, int threads, int lds, hipStream_t s, A... args)
 {
     (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    hipLaunchKernelGGL(kernel, grid, dim3(512), lds, s, args...);
+    hipLaunchKernelGGL(kernel, grid, dim3(threads), lds, s, args...);
 }
 
 int entry_groups(const LossArgs &a) { return (int)(((long long)a.rows * a.entries + 31) / 32); }
@@ -626,24 +726,24 @@ template <template <int, int> class Job> void launch_job(hipStream_t s, const Lo
     using Small = Block<8, 1, 1, 2, 3, A, B>;       // 256 x 64
     using Middle = Block<4, 2, 2, 2, 3, A, B>;      // 256 x 128
     const int extra = entries ? up_div(entry_groups(a), 64) * 8 : 0;
-    const dim3 grid(up_div(blocks, 8) * 8 + extra);
-    if (a.n_block == 64) launch(block_kernel<Job, Small>, grid, Small::LDS, s, a, v0, vn, flag, extra);
-    else if (a.n_block == 128) launch(block_kernel<Job, Middle>, grid, Middle::LDS, s, a, v0, vn, flag, extra);
-    else launch(turns_kernel<Job>, dim3(256), 5 * 256 * BK * 2, s, a, v0, vn, flag);
+    const dim3 persistent(256 + extra);
+    if (a.n_block == 64) launch(stream_kernel<Job, Small>, persistent, 512, LDS_OF_RING + 8 * 64 * 8, s, a, v0, vn, flag, extra);
+    else if (a.n_block == 128) launch(stream_kernel<Job, Middle>, persistent, 512, LDS_OF_RING + 8 * 128 * 8, s, a, v0, vn, flag, extra);
+    else launch(turns_kernel<Job>, dim3(256), 512, 5 * 256 * BK * 2, s, a, v0, vn, flag);
 }
 
 }  // namespace
 
 void launch_bf16_pack_head(hipStream_t s, const LossArgs &a, int v0, int vn)
 {
-    hipLaunchKernelGGL(bf16_pack_head_kernel, dim3(vn), dim3(256), 0, s, a, v0);
+    hipLaunchKernelGGL(bf16_pack_head_kernel, dim3(vn), dim3(128), 0, s, a, v0);
 }
 
 void launch_bf16_entries(hipStream_t s, const LossArgs &a) { hipLaunchKernelGGL(bf16_entries_kernel, dim3(entry_groups(a)), dim3(64), 0, s, a); }
 
 void launch_bf16_softmax(hipStream_t s, const LossArgs &a, int v0, int vn, bool entries) { launch_job<Softmax>(s, a, v0, vn, 0, up_div(vn, BF16_BLOCK), entries); }
 
-int bf16_softmax_parts(const LossArgs &a) { return up_div(a.vocab, BF16_BLOCK) * (a.n_block == 64 ? 8 : a.n_block == 128 ? 4 : 2); }
+int bf16_softmax_parts(const LossArgs &a) { return up_div(a.vocab, BF16_BLOCK) * (a.n_block < 256 ? 1 : 2); }
 
 void launch_bf16_probabilities(hipStream_t s, const LossArgs &a, int v0, int vn, bool entries) { launch_job<Probabilities>(s, a, v0, vn, 0, up_div(vn, BF16_BLOCK), entries); }
 
@@ -652,6 +752,15 @@ void launch_bf16_hidden_grad(hipStream_t s, const LossArgs &a, int v0, int vn, b
     launch_job<HiddenGrad>(s, a, v0, vn, first, up_div(a.d_pad, BF16_BLOCK) * std::max(a.splits, 1), false);
 }
 
-void launch_bf16_weight_grad(hipStream_t s, const LossArgs &a, int v0, int vn) { launch(turns_kernel<WeightGrad>, dim3(256), 5 * 256 * BK * 2, s, a, v0, vn, 0); }
+// Few rows make it a matter of writing: blocks of 128 x 128, two a compute unit, one computing while the other's stores drain.
+#ifndef XK
+#define XK 1024
+#endif
+void launch_bf16_weight_grad(hipStream_t s, const LossArgs &a, int v0, int vn)
+{
+    using Bl = Block<2, 2, 2, 2, 2, false, false>;
+    if (a.rows <= XK) launch(block_kernel<WeightGrad, Bl>, dim3(up_div(up_div(a.d_pad, Bl::TM) * up_div(vn, Bl::TN), 8) * 8), 256, Bl::LDS, s, a, v0, vn, 0);
+    else launch(turns_kernel<WeightGrad>, dim3(256), 512, 5 * 256 * BK * 2, s, a, v0, vn, 0);
+}
 
 }  // namespace tr

@@ -32,6 +32,20 @@ __device__ __forceinline__ void store_one(bf16_t *p, float v) { *p = (bf16_t)two
 __device__ __forceinline__ float load_one(const float *p) { return *p; }
 __device__ __forceinline__ float load_one(const bf16_t *p) { return __uint_as_float((uint32_t)*p << 16); }
 
+// elements k .. k + 7 of a bf16 row of d that may begin anywhere; zeros past its end
+__device__ __forceinline__ uint4 load8(const bf16_t *row, int k, int d)
+{
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (k + 8 <= d) __builtin_memcpy(&v, row + k, 16);
+    else {
+        uint32_t q[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) if (k + e < d) q[e >> 1] |= (uint32_t)row[k + e] << (16 * (e & 1));
+        v = make_uint4(q[0], q[1], q[2], q[3]);
+    }
+    return v;
+}
+
 // A running softmax is (m, s): s = sum of 2^(k c - m) over the products c seen, k = log2(e) / T, m a whole number at least the largest k c (-inf: none seen).
 // Since m is whole, moving a sum to another m is exact, and k c - m is rounded once (fma), relative to itself: what is near the top keeps all its bits.
 __device__ __forceinline__ float whole_above(float top) { return ceilf(top); }

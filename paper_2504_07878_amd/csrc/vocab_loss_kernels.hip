@@ -1,5 +1,6 @@
 // Losses over the vocabulary: rows, listed entries and sums. Small kernels beside the products; what they compute is in vocab_loss.h.
 #include "vocab_loss_epilogues.h"
+#include <algorithm>
 #include <type_traits>
 
 namespace tr {
@@ -55,7 +56,7 @@ template <class HT> __device__ __forceinline__ void pack_row(const LossArgs &a, 
             for (int k = threadIdx.x * 8; k < a.d_pad; k += blockDim.x * 8)
                 *reinterpret_cast<uint4 *>(p + k) = from < 0 ? make_uint4(0, 0, 0, 0) : *reinterpret_cast<const uint4 *>(h + k);
         } else {
-            for (int k = threadIdx.x; k < a.d_pad; k += blockDim.x) p[k] = from >= 0 && k < a.dim ? h[k] : (bf16_t)0;
+            for (int k = threadIdx.x * 8; k < a.d_pad; k += blockDim.x * 8) *reinterpret_cast<uint4 *>(p + k) = from < 0 ? make_uint4(0, 0, 0, 0) : load8(h, k, a.dim);
         }
     }
 }
@@ -164,7 +165,7 @@ template <bool TEACHER, class HT> static void rows_of(hipStream_t s, const LossA
     const int packed = a.hp ? (a.rows + BF16_BLOCK - 1) / BF16_BLOCK * BF16_BLOCK : 0;
     if (a.rows <= 1024 && (long long)a.rows * a.entries <= 16384) {
         const int used = a.rows <= PAIR_ROWS && a.hp ? (a.pairs ? (a.rows <= 64 ? 128 : 256) : (a.rows <= 64 ? 64 : 128)) : packed;   // what the products' blocks read
-        hipLaunchKernelGGL((loss_prepare_kernel<TEACHER, HT>), dim3(a.rows), dim3(256), 0, s, a, used);
+        hipLaunchKernelGGL((loss_prepare_kernel<TEACHER, HT>), dim3(std::max(a.rows, used)), dim3(256), 0, s, a, used);
         return;
     }
     hipLaunchKernelGGL((loss_state_kernel<TEACHER>), dim3((a.rows + 255) / 256), dim3(256), 0, s, a);
@@ -215,6 +216,7 @@ __global__ __launch_bounds__(256) void loss_finish_kernel(LossArgs a, int parts)
     const int mine = i0 + t % ROWS;
     float2 x = make_float2(-INFINITY, 0.f);
     if (mine < count)
+#pragma unroll 4
         for (int p = t / ROWS; p < parts; p += 256 / ROWS) x = join(x, a.part[(size_t)p * a.part_ld + mine]);
     joined[t] = x;
     __syncthreads();
@@ -343,6 +345,7 @@ __global__ __launch_bounds__(256) void hidden_grad_kernel(LossArgs a)
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
         auto add = [&](float4 &to, const float4 u) { to.x += u.x; to.y += u.y; to.z += u.z; to.w += u.w; };
         if (j < a.d_pad)
+#pragma unroll 8
             for (int p = w; p < splits; p += 4) {
                 const float *at = a.acc + p * apart + (size_t)i * a.d_pad + j;
                 add(v, *reinterpret_cast<const float4 *>(at));
