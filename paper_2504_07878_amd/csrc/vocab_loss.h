@@ -67,12 +67,13 @@ void launch_loss_hidden_grad(hipStream_t s, const LossArgs &a);
 
 // Products of the listed entries, each the bits that the softmax's own products have: a probability near 1 and its logit then agree, and what is left of
 // 1 - p and of lse - z is not the difference of two roundings.
-void launch_f32_entries(hipStream_t s, const LossArgs &a);
 void launch_bf16_entries(hipStream_t s, const LossArgs &a);
 
-// Products on 32-bit matrix instructions, operands of either type and any stride (vocab_loss_f32_kernels.hip). Blocks of 128 x 128.
-constexpr int F32_BLOCK = 128;
+// Products on 32-bit matrix instructions, operands of either type and any stride (vocab_loss_f32_kernels.hip). Blocks of 64 x 64. The
+// softmax and the first piece's probabilities bring the products of the listed entries.
+constexpr int F32_BLOCK = 64;
 void launch_f32_softmax(hipStream_t s, const LossArgs &a);
+int f32_softmax_parts(const LossArgs &a);
 void launch_f32_probabilities(hipStream_t s, const LossArgs &a, int v0, int vn);
 void launch_f32_hidden_grad(hipStream_t s, const LossArgs &a, int v0, int vn, bool first);
 void launch_f32_weight_grad(hipStream_t s, const LossArgs &a, int v0, int vn);

@@ -23,10 +23,12 @@ bool config_ok(const tr_loss_config *c)
 // Where everything lies in the workspace, for a configuration; the sizes of a call's own launches follow from its rows, never beyond these.
 struct Plan {
     int n_pad, d_pad, piece, g_ld, splits;
+    int planes_ld, planes_piece;   // d_pad and piece of the softmax on rows in planes
     size_t head, idx, state, part, value, G, acc, hp, wp, total;
 };
 
-bool is_bf16(const tr_loss_config *c) { return c->hidden_dtype == TR_BF16; }   // the products that run on bf16 matrix instructions
+bool is_bf16(const tr_loss_config *c) { return c->hidden_dtype == TR_BF16; }                                    // all products run on bf16 matrix instructions
+bool in_planes(const tr_loss_config *c) { return c->hidden_dtype == TR_F32 && c->weight_dtype == TR_BF16; }   // those of the softmax do, on rows in three planes
 
 // G stays at 512 MB or less, but a piece has 2048 columns at least. (6144 of 8192 rows x 151936 x 896, all products of the gradients, pieces of 128 / 256 / 512 / 1024 MB:
 // 7.1 / 5.9 / 5.8 / 5.7 ms.)
@@ -37,13 +39,13 @@ Plan plan_of(const tr_loss_config *c)
     const bool half = is_bf16(c);
     const int block = half ? BF16_BLOCK : F32_BLOCK;
     const size_t g_size = half ? 2 : 4;
-    p.n_pad = (int)up(c->max_rows, block);
+    p.n_pad = (int)up(c->max_rows, BF16_BLOCK);
     p.d_pad = (int)up(c->dim, half ? 64 : F32_BLOCK);
     const size_t vocab = up(c->vocab, block);
     p.piece = (int)std::min(vocab, std::max<size_t>(2048, (512u << 20) / g_size / p.n_pad / block * block));
     p.g_ld = p.piece + 128;
     const int mb = (int)(up(p.d_pad, block) / block), few = std::max(1, p.piece / 256);
-    p.splits = half ? std::min(few, std::max(1, 32 / mb) * 8) : std::max(1, std::min(512 / (mb * (p.n_pad / F32_BLOCK)), few));
+    p.splits = half ? std::min(few, std::max(1, 32 / mb) * 8) : std::max(1, std::min(1024 / (mb * (p.n_pad / F32_BLOCK)), few));
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t was = at; at += up(bytes, 256); return was; };
     p.head = take(sizeof(LossHead));
@@ -56,9 +58,14 @@ Plan plan_of(const tr_loss_config *c)
     const size_t sums = (size_t)p.splits * p.n_pad, most = std::max({(size_t)std::min(p.splits, 8) * std::min<size_t>(p.n_pad, 1024 / mb * BF16_BLOCK + BF16_BLOCK),
                                                                      (size_t)(256 / mb + 1) * BF16_BLOCK, (size_t)p.n_pad});
     p.acc = take((half ? std::min(sums, most) : sums) * p.d_pad * 4);
+    p.planes_ld = (int)up(c->dim, 64);
+    p.planes_piece = (int)std::min(up(c->vocab, BF16_BLOCK), std::max<size_t>(2048, p.piece / BF16_BLOCK * BF16_BLOCK));
     if (half) {
         p.hp = take((size_t)p.n_pad * p.d_pad * 2);
         p.wp = take((size_t)p.piece * p.d_pad * 2);
+    } else if (in_planes(c)) {
+        p.hp = take(up(p.n_pad, BF16_BLOCK) * 3 * p.planes_ld * 2);
+        p.wp = take((size_t)p.planes_piece * p.planes_ld * 2);
     }
     p.total = at;
     return p;
@@ -88,13 +95,16 @@ int arguments(const tr_loss_config *c, const tr_loss_rows *in, void *ws, size_t 
     a.head = (LossHead *)(b + p.head); a.idx = (int *)(b + p.idx); a.state = (unsigned char *)(b + p.state); a.part = (float2 *)(b + p.part);
     a.value = (float *)(b + p.value); a.G = b + p.G; a.acc = (float *)(b + p.acc);
     a.n_pad = a.part_ld = p.n_pad; a.d_pad = p.d_pad; a.piece = p.piece; a.g_ld = p.g_ld; a.splits = p.splits;
+    a.direct = a.dim % 64 == 0 && a.ws % 8 == 0 && a.ws < (1 << 22) && (reinterpret_cast<uintptr_t>(a.weight) & 15) == 0;
     if (is_bf16(c)) {
         a.hp = b + p.hp; a.wp = b + p.wp;
         a.pairs = gradient;
         const int rows = gradient && a.rows <= PAIR_ROWS ? 2 * a.rows : a.rows;
         a.n_block = rows <= 64 && !gradient ? 64 : rows <= 128 ? 128 : 256;
         if (a.n_block < 256) a.part_ld = a.n_block;
-        a.direct = a.dim % 64 == 0 && a.ws % 8 == 0 && a.ws < (1 << 22) && (reinterpret_cast<uintptr_t>(a.weight) & 15) == 0;
+    } else if (in_planes(c) && !gradient) {
+        a.hp = b + p.hp; a.wp = b + p.wp;
+        a.n_block = 64; a.d_pad = p.planes_ld; a.piece = p.planes_piece;
     }
     return TR_OK;
 }
@@ -111,7 +121,8 @@ int forward(const tr_loss_config *c, void *ws, size_t ws_bytes, void *stream, co
     a.loss = loss; a.lse = lse;
     hipStream_t s = (hipStream_t)stream;
     launch_loss_rows(s, a);
-    if (is_bf16(c)) {
+    const bool bf16_products = a.hp != nullptr;
+    if (bf16_products) {
         const bool along = a.n_block < 256;     // the listed entries in the same launch
         for (int v0 = 0, vn; v0 < a.vocab; v0 += vn) {
             vn = a.direct ? a.vocab : std::min(a.piece, a.vocab - v0);
@@ -121,9 +132,8 @@ int forward(const tr_loss_config *c, void *ws, size_t ws_bytes, void *stream, co
         if (!along) launch_bf16_entries(s, a);
     } else {
         launch_f32_softmax(s, a);
-        launch_f32_entries(s, a);
     }
-    launch_loss_finish(s, a, is_bf16(c) ? bf16_softmax_parts(a) : (a.vocab + F32_BLOCK - 1) / F32_BLOCK * 2);
+    launch_loss_finish(s, a, bf16_products ? bf16_softmax_parts(a) : f32_softmax_parts(a));
     return enqueued();
 }
 
@@ -141,21 +151,17 @@ int backward(const tr_loss_config *c, void *ws, size_t ws_bytes, void *stream, c
     a.d_hidden = out->d_hidden; a.dhs = out->d_hidden_stride; a.d_weight = out->d_weight; a.dws = out->d_weight_stride;
     hipStream_t s = (hipStream_t)stream;
     launch_loss_rows(s, a);
-    const bool half = is_bf16(c), one = a.piece >= a.vocab, along = half && one && a.n_block < 256;
-    if (a.rows && !along) {
-        if (half) launch_bf16_entries(s, a);
-        else launch_f32_entries(s, a);
-        if (!one) launch_loss_values(s, a, false);
-    }
+    const bool half = is_bf16(c), one = a.piece >= a.vocab, along = half && a.n_block < 256;
+    if (a.rows && half && !along) launch_bf16_entries(s, a);
     for (int v0 = 0; v0 < a.vocab; v0 += a.piece) {
         const int vn = std::min(a.piece, a.vocab - v0);
         if (a.rows) {
             if (half) {
                 if (!a.direct) launch_bf16_pack_head(s, a, v0, vn);
-                launch_bf16_probabilities(s, a, v0, vn, along);
+                launch_bf16_probabilities(s, a, v0, vn, along && v0 == 0);
             } else launch_f32_probabilities(s, a, v0, vn);
-            if (one) launch_loss_values(s, a, true);
-            else launch_loss_scatter(s, a, v0, vn);
+            if (v0 == 0) launch_loss_values(s, a, one);
+            if (!one) launch_loss_scatter(s, a, v0, vn);
             if (a.d_hidden) {
                 if (half) launch_bf16_hidden_grad(s, a, v0, vn, v0 == 0);
                 else launch_f32_hidden_grad(s, a, v0, vn, v0 == 0);

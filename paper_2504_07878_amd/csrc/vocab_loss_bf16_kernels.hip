@@ -1,4 +1,5 @@
-// Products of the losses over the vocabulary on bf16 matrix instructions: both operands bf16, sums in fp32.
+// Products of the losses over the vocabulary on bf16 matrix instructions: both operands bf16, sums in fp32. The softmax also takes fp32 rows over a bf16 head: a row is
+// then the sum of three bf16 rows (planes), each what the ones before leave, rounded: 24 bits, and every product with the head is exact.
 //
 // Four products, all computed transposed (see vocab_loss_epilogues.h), C[n][m] = sum_k A[m][k] B[n][k]:
 //   softmax, probabilities     m = vocabulary entry, n = row that counts, k = feature: both operands lie with k contiguous
@@ -129,10 +130,11 @@ template <int T, bool KC, bool FEAT, int N> struct Reader {
 
 // One block by WM x WN wavefronts, each MI x NI accumulators; A_KC, B_KC: where the operands have k contiguous. A ring of STAGES steps in LDS, one barrier a
 // step; the matrix operands of 16 k are read one such step ahead. For blocks of few rows, which are bound by reading the head.
-template <int WM_, int WN_, int MI_, int NI_, int STAGES, bool A_KC, bool B_KC> struct Block {
+template <int WM_, int WN_, int MI_, int NI_, int STAGES, bool A_KC, bool B_KC, int PLANES = 1> struct Block {
     static constexpr int WM = WM_, WN = WN_, MI = MI_, NI = NI_, WAVES = WM * WN, TM = WM * MI * 32, TN = WN * NI * 32, STAGES_ = STAGES;
     using TA = Tile<TM, A_KC, WAVES>;
-    using TB = Tile<TN, B_KC, WAVES>;
+    static constexpr int PL = PLANES;
+    using TB = Tile<TN * PL, B_KC, WAVES>;
     static constexpr int STAGE = TA::BYTES + TB::BYTES, LDS = STAGES * STAGE;
 
     TA a;
@@ -268,8 +270,9 @@ template <int TM, int TN> struct Logits {
         o.at(i, p.m, p.n);
         p.a = head_rows(a, v0, p.lda);
         p.a += (long long)p.m * TM * p.lda;
-        p.b = (const bf16_t *)a.hp + (size_t)p.n * TN * a.d_pad;
-        p.ldb = a.d_pad; p.a_limit = vn - p.m * TM; p.b_limit = TN; p.n_limit = rows - p.n * TN; p.K = a.d_pad;
+        const int planes = a.hdt == DT_F32 ? 3 : 1;
+        p.b = (const bf16_t *)a.hp + (size_t)p.n * TN * planes * a.d_pad;
+        p.ldb = a.d_pad; p.a_limit = vn - p.m * TM; p.b_limit = TN * planes; p.n_limit = rows - p.n * TN; p.K = a.d_pad;
         return p;
     }
 };
@@ -444,7 +447,7 @@ template <int TM, int TN> struct WeightGrad {
 
 // Products of listed entries: a wavefront takes 32 of them, its rows of the head against its packed rows, of which only the diagonal is kept: the matrix unit is
 // all but idle in a product this small, and it gives the bits that the same pair has in a block (the same instruction over the same steps of k).
-__device__ __forceinline__ void entries_group(const LossArgs &a, int group)
+template <int PLANES> __device__ __forceinline__ void entries_group(const LossArgs &a, int group)
 {
     const int lane = threadIdx.x & 63, e = group * 32 + (lane & 31), hf = lane >> 5, count = a.head->count;
     if ((long long)group * 32 >= (long long)count * a.entries) return;
@@ -454,25 +457,29 @@ __device__ __forceinline__ void entries_group(const LossArgs &a, int group)
     if (on) {
         const int id = a.ids[(long long)a.idx[i] * a.entries + j];
         on = id >= 0 && id < a.vocab;
-        h += (size_t)i * a.d_pad;
+        h += (size_t)(PLANES == 1 ? i : (i >> 6) * 64 * PLANES + (i & 63)) * a.d_pad;
         if (on) w += id * a.ws;
     }
     f32x16 c;
 #pragma unroll
     for (int r = 0; r < 16; ++r) c[r] = 0.f;
-    constexpr int AT_ONCE = 8;      // steps of 16 k whose loads are requested together
+    constexpr int AT_ONCE = PLANES == 1 ? 8 : 4;      // steps of 16 k whose loads are requested together
     for (int k0 = 0; k0 < a.d_pad; k0 += 16 * AT_ONCE) {
-        bf16x8 x[AT_ONCE], y[AT_ONCE];
+        bf16x8 x[AT_ONCE], y[AT_ONCE][PLANES];
 #pragma unroll
         for (int q = 0; q < AT_ONCE; ++q) {
             const int k = min(k0 + 16 * q, a.d_pad - 16) + 8 * hf;
-            y[q] = *reinterpret_cast<const bf16x8 *>(h + k);
+#pragma unroll
+            for (int l = 0; l < PLANES; ++l) y[q][l] = *reinterpret_cast<const bf16x8 *>(h + (size_t)l * 64 * a.d_pad + k);
             if (a.direct) x[q] = *reinterpret_cast<const bf16x8 *>(w + k);
             else x[q] = __builtin_bit_cast(bf16x8, load8(w, k, on ? a.dim : 0));
         }
 #pragma unroll
         for (int q = 0; q < AT_ONCE; ++q)
-            if (k0 + 16 * q < a.d_pad) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[q], y[q], c, 0, 0, 0);
+            if (k0 + 16 * q < a.d_pad) {
+#pragma unroll
+                for (int l = 0; l < PLANES; ++l) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[q], y[q][l], c, 0, 0, 0);
+            }
     }
     const int n = lane & 31;   // row m of column n lies in register (m / 8) * 4 + m % 4 of lane n + 32 * (m / 4 % 2)
     float d = 0.f;
@@ -481,14 +488,14 @@ __device__ __forceinline__ void entries_group(const LossArgs &a, int group)
     if (on && ((n >> 2) & 1) == hf) a.value[e] = d;
 }
 
-__global__ __launch_bounds__(64) void bf16_entries_kernel(LossArgs a) { entries_group(a, blockIdx.x); }
+__global__ __launch_bounds__(64) void bf16_entries_kernel(LossArgs a) { entries_group<1>(a, blockIdx.x); }
 
 // Few rows, bound by the head's bytes: one workgroup a compute unit takes block after block, the copies running on across blocks: a ring of steps in LDS, one barrier a
 // step. The first `extra` (a multiple of 8) workgroups take listed entries instead.
 template <template <int, int> class Job_, class Bl> __global__ __launch_bounds__(Bl::WAVES * 64) void stream_kernel(LossArgs a, int v0, int vn, int flag, int extra)
 {
     if ((int)blockIdx.x < extra) {
-        entries_group(a, blockIdx.x * Bl::WAVES + wavefront());
+        entries_group<Bl::PL>(a, blockIdx.x * Bl::WAVES + wavefront());
         return;
     }
     constexpr int MI = Bl::MI, NI = Bl::NI, STAGES = Bl::STAGES_, COPIES = Bl::TA::COPIES + Bl::TB::COPIES;
@@ -520,7 +527,8 @@ template <template <int, int> class Job_, class Bl> __global__ __launch_bounds__
 #pragma unroll
     for (int q = 0; q < STAGES - 1; ++q) copy();
     Reader<Bl::TM, Job::A_KC, true, MI> ra;
-    Reader<Bl::TN, Job::B_KC, false, NI> rb;
+    static_assert(Bl::PL == 1 || Bl::WN == 1, "a row's planes belong to one wavefront");
+    Reader<Bl::TN * Bl::PL, Job::B_KC, false, NI * Bl::PL> rb;
     ra.init(w / Bl::WN * MI * 32);
     rb.init(w % Bl::WN * NI * 32);
     f32x16 c[MI][NI];
@@ -541,7 +549,7 @@ template <template <int, int> class Job_, class Bl> __global__ __launch_bounds__
             else landed_and_barrier<0>();
             copy();
             const uint32_t at = lds + from * Bl::STAGE;
-            bf16x8 xa[4][MI], xb[4][NI];
+            bf16x8 xa[4][MI], xb[4][NI * Bl::PL];
             ra.template read<0>(at, xa[0]); rb.template read<0>(at + Bl::TA::BYTES, xb[0]);
             ra.template read<1>(at, xa[1]); rb.template read<1>(at + Bl::TA::BYTES, xb[1]);
             ra.template read<2>(at, xa[2]); rb.template read<2>(at + Bl::TA::BYTES, xb[2]);
@@ -549,9 +557,11 @@ template <template <int, int> class Job_, class Bl> __global__ __launch_bounds__
 #pragma unroll
             for (int q = 0; q < 4; ++q)
 #pragma unroll
-                for (int i = 0; i < MI; ++i)
+                for (int l = 0; l < Bl::PL; ++l)
 #pragma unroll
-                    for (int j = 0; j < NI; ++j) c[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xa[q][i], xb[q][j], c[i][j], 0, 0, 0);
+                    for (int i = 0; i < MI; ++i)
+#pragma unroll
+                        for (int j = 0; j < NI; ++j) c[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xa[q][i], xb[q][l * NI + j], c[i][j], 0, 0, 0);
             --ahead;
             from = from + 1 < STAGES ? from + 1 : 0;
         }
@@ -719,14 +729,20 @@ template <class... P, class... A> void launch(void (*kernel)(P...), dim3 grid, i
 
 int entry_groups(const LossArgs &a) { return (int)(((long long)a.rows * a.entries + 31) / 32); }
 
-// blocks: those of 256 x n_block there can be (one along the rows, where they are smaller than 256); entries: listed entries too, where workgroups take a block each
-template <template <int, int> class Job> void launch_job(hipStream_t s, const LossArgs &a, int v0, int vn, int flag, int blocks, bool entries)
+// entries: listed entries too, where there are few rows or fp32 ones
+template <template <int, int> class Job> void launch_job(hipStream_t s, const LossArgs &a, int v0, int vn, int flag, bool entries)
 {
     constexpr bool A = Job<256, 64>::A_KC, B = Job<256, 64>::B_KC;
     using Small = Block<8, 1, 1, 2, 3, A, B>;       // 256 x 64
     using Middle = Block<4, 2, 2, 2, 3, A, B>;      // 256 x 128
     const int extra = entries ? up_div(entry_groups(a), 64) * 8 : 0;
     const dim3 persistent(256 + extra);
+    if constexpr (std::is_same_v<Job<256, 64>, Softmax<256, 64>>)
+        if (a.hdt == DT_F32) {
+            using Planes = Block<8, 1, 1, 2, 2, A, B, 3>;
+            launch(stream_kernel<Job, Planes>, persistent, 512, LDS_OF_RING + 8 * 64 * 8, s, a, v0, vn, flag, extra);
+            return;
+        }
     if (a.n_block == 64) launch(stream_kernel<Job, Small>, persistent, 512, LDS_OF_RING + 8 * 64 * 8, s, a, v0, vn, flag, extra);
     else if (a.n_block == 128) launch(stream_kernel<Job, Middle>, persistent, 512, LDS_OF_RING + 8 * 128 * 8, s, a, v0, vn, flag, extra);
     else launch(turns_kernel<Job>, dim3(256), 512, 5 * 256 * BK * 2, s, a, v0, vn, flag);
@@ -741,15 +757,15 @@ void launch_bf16_pack_head(hipStream_t s, const LossArgs &a, int v0, int vn)
 
 void launch_bf16_entries(hipStream_t s, const LossArgs &a) { hipLaunchKernelGGL(bf16_entries_kernel, dim3(entry_groups(a)), dim3(64), 0, s, a); }
 
-void launch_bf16_softmax(hipStream_t s, const LossArgs &a, int v0, int vn, bool entries) { launch_job<Softmax>(s, a, v0, vn, 0, up_div(vn, BF16_BLOCK), entries); }
+void launch_bf16_softmax(hipStream_t s, const LossArgs &a, int v0, int vn, bool entries) { launch_job<Softmax>(s, a, v0, vn, 0, entries); }
 
 int bf16_softmax_parts(const LossArgs &a) { return up_div(a.vocab, BF16_BLOCK) * (a.n_block < 256 ? 1 : 2); }
 
-void launch_bf16_probabilities(hipStream_t s, const LossArgs &a, int v0, int vn, bool entries) { launch_job<Probabilities>(s, a, v0, vn, 0, up_div(vn, BF16_BLOCK), entries); }
+void launch_bf16_probabilities(hipStream_t s, const LossArgs &a, int v0, int vn, bool entries) { launch_job<Probabilities>(s, a, v0, vn, 0, entries); }
 
 void launch_bf16_hidden_grad(hipStream_t s, const LossArgs &a, int v0, int vn, bool first)
 {
-    launch_job<HiddenGrad>(s, a, v0, vn, first, up_div(a.d_pad, BF16_BLOCK) * std::max(a.splits, 1), false);
+    launch_job<HiddenGrad>(s, a, v0, vn, first, false);
 }
 
 // Few rows make it a matter of writing: blocks of 128 x 128, two a compute unit, one computing while the other's stores drain.

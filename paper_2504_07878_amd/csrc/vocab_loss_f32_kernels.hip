@@ -1,8 +1,9 @@
 // Products of the losses over the vocabulary on 32-bit matrix instructions: operands of either storage type, any stride and alignment, widened where they
 // are read; used wherever an operand is fp32.
 //
-// A workgroup of 4 wavefronts (2 x 2, each 2 x 2 accumulators of 32 x 32) computes a 128 x 128 block of C[n][m] = sum_k A[m][k] B[n][k], 16 k at a time:
-// both operands go through registers into LDS as [k][row], the next step's are requested before this step's products. Three products:
+// A workgroup of 4 wavefronts (2 x 2, an accumulator of 32 x 32 each) computes a 64 x 64 block of C[n][m] = sum_k A[m][k] B[n][k] in steps of 32 k: both operands
+// go through registers into LDS as [row][k], one step ahead, in two buffers. A lane reads four k at a time: k = 8 g + 4 (lane / 32) + j for the j-th product of group g.
+// Small blocks, since models of this type are small: they have to fill the chip. Three products:
 //   softmax, probabilities: m = vocabulary entry, n = row that counts, k = feature
 //   gradient to the hidden rows: m = feature, n = row, k = vocabulary entry of the piece; summed over the pieces in `acc`, one sum per split of k
 //   gradient to the head: m = feature, n = vocabulary entry, k = row
@@ -12,125 +13,184 @@ namespace tr {
 
 namespace {
 
-constexpr int BK = 16, PITCH = F32_BLOCK + 4;
+constexpr int BK = 32, PITCH = BK + 4;       // 16-byte reads of 16 rows meet 16 different places of the 64 banks
 
-// operands: at(row of the block's dimension, k) or 0 beyond either. CONTIGUOUS_K: how threads are laid over a tile, so that neighbours read neighbours.
-template <class WT> struct HeadRows {          // weight[v][k]
-    static constexpr bool contiguous_k = true;
-    const WT *w; long long ws; int v0, vn, d;
-    __device__ __forceinline__ float at(int m, int k) const { return m < vn && k < d ? load_one(w + (v0 + m) * ws + k) : 0.f; }
-};
-template <class HT> struct HiddenRows {        // hidden[idx[n]][k]
-    static constexpr bool contiguous_k = true;
-    const HT *h; long long hs; const int *idx; int count, d;
-    __device__ __forceinline__ float at(int n, int k) const { return n < count && k < d ? load_one(h + idx[n] * hs + k) : 0.f; }
-};
-template <class WT> struct HeadColumns {       // weight[k][m]
-    static constexpr bool contiguous_k = false;
-    const WT *w; long long ws; int v0, vn, d;
-    __device__ __forceinline__ float at(int m, int k) const { return m < d && k < vn ? load_one(w + (v0 + k) * ws + m) : 0.f; }
-};
-struct PieceRows {                             // G[n][k]
-    static constexpr bool contiguous_k = true;
-    const float *g; int ld, count, vn;
-    __device__ __forceinline__ float at(int n, int k) const { return n < count && k < vn ? g[(size_t)n * ld + k] : 0.f; }
-};
-template <class HT> struct HiddenColumns {     // hidden[idx[k]][m]
-    static constexpr bool contiguous_k = false;
-    const HT *h; long long hs; const int *idx; int count, d;
-    __device__ __forceinline__ float at(int m, int k) const { return m < d && k < count ? load_one(h + idx[k] * hs + m) : 0.f; }
-};
-struct PieceColumns {                          // G[k][n]
-    static constexpr bool contiguous_k = false;
-    const float *g; int ld, count, vn;
-    __device__ __forceinline__ float at(int n, int k) const { return n < vn && k < count ? g[(size_t)k * ld + n] : 0.f; }
-};
-
-struct Tiles { float a[BK * PITCH], b[BK * PITCH]; };
-
-template <class Op> __device__ __forceinline__ void read8(const Op &op, int row0, int k0, float (&v)[8])
+// eight elements of a line from j on, as fp32; zeros at or past `limit` and where there is no line. `wide`: the line lies on 16 bytes
+__device__ __forceinline__ void eight_of(const float *line, int j, int limit, bool wide, float (&v)[8])
 {
-    const int t = threadIdx.x;
+    if (line && wide && j + 8 <= limit) {
+        const float4 x = *reinterpret_cast<const float4 *>(line + j), y = *reinterpret_cast<const float4 *>(line + j + 4);
+        v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
+    } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        v[e] = Op::contiguous_k ? op.at(row0 + (t >> 1), k0 + (t & 1) * 8 + e) : op.at(row0 + (t & 15) * 8 + e, k0 + (t >> 4));
+        for (int e = 0; e < 8; ++e) v[e] = line && j + e < limit ? line[j + e] : 0.f;
+    }
 }
-template <class Op> __device__ __forceinline__ void write8(float *lds, const float (&v)[8])
+__device__ __forceinline__ void eight_of(const bf16_t *line, int j, int limit, bool, float (&v)[8])
 {
-    const int t = threadIdx.x;
+    const uint4 u = line ? load8(line, j, limit) : make_uint4(0, 0, 0, 0);
+    const uint32_t q[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-    for (int e = 0; e < 8; ++e) lds[Op::contiguous_k ? ((t & 1) * 8 + e) * PITCH + (t >> 1) : (t >> 4) * PITCH + (t & 15) * 8 + e] = v[e];
+    for (int e = 0; e < 4; ++e) { v[2 * e] = __uint_as_float(q[e] << 16); v[2 * e + 1] = __uint_as_float(q[e] & 0xffff0000u); }
 }
 
-// c = products of the block at (m0, n0) over k in [k_lo, k_hi), whole steps unless k_hi is the operands' end
-template <class A, class B> __device__ __forceinline__ void products(const A &a, const B &b, int m0, int n0, int k_lo, int k_hi, Tiles &sm, f32x16 (&c)[2][2])
+template <class T> __device__ __forceinline__ void four_of(const T *line, int j, int limit, bool wide, float (&v)[4])
 {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, wm = w >> 1, wn = w & 1;
-    const int arow = wm * 64 + tile_feature(lane & 31), brow = wn * 64 + (lane & 31), kk = lane >> 5;
+    if (line && wide && j + 4 <= limit) {
+        if constexpr (sizeof(T) == 4) {
+            const float4 x = *reinterpret_cast<const float4 *>(line + j);
+            v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+        } else {
+            const uint2 u = *reinterpret_cast<const uint2 *>(line + j);
+            v[0] = __uint_as_float(u.x << 16); v[1] = __uint_as_float(u.x & 0xffff0000u); v[2] = __uint_as_float(u.y << 16); v[3] = __uint_as_float(u.y & 0xffff0000u);
+        }
+    } else {
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+        for (int e = 0; e < 4; ++e) v[e] = line && j + e < limit ? load_one(line + j + e) : 0.f;
+    }
+}
+
+// An operand is lines of memory: line o has elements 0 .. limit - 1. ALONG_K: a line is a row of the operand (k runs along it); otherwise it is one k.
+template <class T> struct Lines {              // line o at p + o * ld, o < lines
+    const T *p; long long ld; int lines, limit; bool wide;
+    __device__ __forceinline__ Lines(const void *p_, long long ld_, int lines_, int limit_) : p((const T *)p_), ld(ld_), lines(lines_), limit(limit_)
+    {
+        wide = ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * sizeof(T))) & 15) == 0;
+    }
+    __device__ __forceinline__ void read(int o, int j, float (&v)[8]) const { eight_of(o < lines ? p + o * ld : nullptr, j, limit, wide, v); }
+};
+template <class T> struct ListedLines {        // line o at p + list[o] * ld
+    Lines<T> l; const int *list;
+    __device__ __forceinline__ void read(int o, int j, float (&v)[8]) const { eight_of(o < l.lines ? l.p + list[o] * l.ld : nullptr, j, l.limit, l.wide, v); }
+};
+
+struct Tiles { float a[2][F32_BLOCK * PITCH], b[2][F32_BLOCK * PITCH]; };
+
+// a thread's eight elements of a tile (64 x 32): of a row, or of a k
+template <bool ALONG_K, class Op> __device__ __forceinline__ void read_tile(const Op &op, int row0, int k0, float (&v)[8])
+{
+    const int t = threadIdx.x;
+    if (ALONG_K) op.read(row0 + (t >> 2), k0 + (t & 3) * 8, v);
+    else op.read(k0 + (t >> 3), row0 + (t & 7) * 8, v);
+}
+template <bool ALONG_K> __device__ __forceinline__ void write_tile(float *lds, const float (&v)[8])
+{
+    const int t = threadIdx.x;
+    if (ALONG_K) store_run(lds + (t >> 2) * PITCH + (t & 3) * 8, v);
+    else {
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int e = 0; e < 8; ++e) lds[((t & 7) * 8 + e) * PITCH + (t >> 3)] = v[e];
+    }
+}
+
+// c = this wavefront's products of the block at (m0, n0) over k in [k_lo, k_hi), whole steps unless k_hi is the operands' end
+template <bool A_ALONG, bool B_ALONG, class A, class B>
+__device__ __forceinline__ void products(const A &a, const B &b, int m0, int n0, int k_lo, int k_hi, Tiles &sm, f32x16 (&c)[1][1])
+{
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int arow = (w >> 1) * 32 + tile_feature(lane & 31), brow = (w & 1) * 32 + (lane & 31), at = (lane >> 5) * 4;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) c[i][j][r] = 0.f;
+    for (int r = 0; r < 16; ++r) c[0][0][r] = 0.f;
+    if (k_lo >= k_hi) return;
     float va[8], vb[8];
-    if (k_lo < k_hi) { read8(a, m0, k_lo, va); read8(b, n0, k_lo, vb); }
-    for (int k = k_lo; k < k_hi; k += BK) {
-        __syncthreads();
-        write8<A>(sm.a, va); write8<B>(sm.b, vb);
-        __syncthreads();
-        if (k + BK < k_hi) { read8(a, m0, k + BK, va); read8(b, n0, k + BK, vb); }
+    read_tile<A_ALONG>(a, m0, k_lo, va);
+    read_tile<B_ALONG>(b, n0, k_lo, vb);
+    int buf = 0;
+    for (int k = k_lo; k < k_hi; k += BK, buf ^= 1) {
+        write_tile<A_ALONG>(sm.a[buf], va);
+        write_tile<B_ALONG>(sm.b[buf], vb);
+        __syncthreads();        // (the other buffer's readers are past it when it is written again)
+        if (k + BK < k_hi) { read_tile<A_ALONG>(a, m0, k + BK, va); read_tile<B_ALONG>(b, n0, k + BK, vb); }
 #pragma unroll
-        for (int s = 0; s < BK; s += 2) {
-            float x[2], y[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) { x[i] = sm.a[(s + kk) * PITCH + arow + 32 * i]; y[i] = sm.b[(s + kk) * PITCH + brow + 32 * i]; }
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) c[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i], y[j], c[i][j], 0, 0, 0);
+        for (int g = 0; g < BK; g += 8) {
+            const float4 x = *reinterpret_cast<const float4 *>(sm.a[buf] + arow * PITCH + g + at), y = *reinterpret_cast<const float4 *>(sm.b[buf] + brow * PITCH + g + at);
+            c[0][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(x.x, y.x, c[0][0], 0, 0, 0);
+            c[0][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(x.y, y.y, c[0][0], 0, 0, 0);
+            c[0][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(x.z, y.z, c[0][0], 0, 0, 0);
+            c[0][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(x.w, y.w, c[0][0], 0, 0, 0);
         }
     }
 }
 
 // f(n, first m of a run of 8, the run) for every run of the block
-template <class F> __device__ __forceinline__ void each_run(const f32x16 (&c)[2][2], F f)
+template <class F> __device__ __forceinline__ void each_run(const f32x16 (&c)[1][1], F f)
 {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, wm = w >> 1, wn = w & 1;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int h = 0; h < 2; ++h) {
+        float v[8];
+        run_of(c[0][0], h, v);
+        f((w & 1) * 32 + (lane & 31), (w >> 1) * 32 + 16 * h + 8 * (lane >> 5), v);
+    }
+}
+
+// Products of listed entries: a wavefront takes 32 of them, its rows of the head against its hidden rows, of which only the diagonal is kept (the matrix unit
+// is all but idle in a product this small, and it gives the bits that the same pair has in a block: the same instructions over the same steps of k).
+template <class HT, class WT> __device__ __forceinline__ void entries_group(const LossArgs &a, int group)
+{
+    const int lane = threadIdx.x & 63, e = group * 32 + (lane & 31), hf = lane >> 5, count = a.head->count;
+    if ((long long)group * 32 >= (long long)count * a.entries) return;
+    const int i = e / a.entries, j = e - i * a.entries;
+    const HT *h = nullptr;
+    const WT *w = nullptr;
+    if (i < count) {
+        const int r = a.idx[i], id = a.ids[(long long)r * a.entries + j];
+        if (id >= 0 && id < a.vocab) { h = (const HT *)a.hidden + r * a.hs; w = (const WT *)a.weight + id * a.ws; }
+    }
+    const bool hw = ((reinterpret_cast<uintptr_t>(a.hidden) | (uintptr_t)(a.hs * sizeof(HT))) & 15) == 0, ww = ((reinterpret_cast<uintptr_t>(a.weight) | (uintptr_t)(a.ws * sizeof(WT))) & 15) == 0;
+    f32x16 c;
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+    for (int r = 0; r < 16; ++r) c[r] = 0.f;
+    constexpr int AT_ONCE = 8;       // groups of 8 k whose loads are requested together
+    for (int k0 = 0; k0 < a.dim; k0 += 8 * AT_ONCE) {
+        float x[AT_ONCE][4], y[AT_ONCE][4];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                float v[8];
-                run_of(c[i][j], h, v);
-                f(wn * 64 + j * 32 + (lane & 31), wm * 64 + i * 32 + 16 * h + 8 * (lane >> 5), v);
+        for (int g = 0; g < AT_ONCE; ++g) { four_of(w, k0 + 8 * g + 4 * hf, a.dim, ww, x[g]); four_of(h, k0 + 8 * g + 4 * hf, a.dim, hw, y[g]); }
+#pragma unroll
+        for (int g = 0; g < AT_ONCE; ++g)
+            if (k0 + 8 * g < a.dim) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) c = __builtin_amdgcn_mfma_f32_32x32x2f32(x[g][q], y[g][q], c, 0, 0, 0);
             }
+    }
+    // row m of column n lies in register (m / 8) * 4 + m % 4 of lane n + 32 * (m / 4 % 2)
+    const int n = lane & 31;
+    float d = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) d = (n >> 3) * 4 + (n & 3) == r ? c[r] : d;
+    if (w && ((n >> 2) & 1) == hf) a.value[e] = d;
 }
 
-template <class HT, class WT> __global__ __launch_bounds__(256) void f32_softmax_kernel(LossArgs a)
+// The first `extra` workgroups along x, of the first row of them, take listed entries.
+template <class HT, class WT> __global__ __launch_bounds__(256) void f32_softmax_kernel(LossArgs a, int extra)
 {
     __shared__ Tiles sm;
-    const int m0 = blockIdx.x * F32_BLOCK, n0 = blockIdx.y * F32_BLOCK, count = a.head->count;
+    const int m0 = ((int)blockIdx.x - extra) * F32_BLOCK, n0 = blockIdx.y * F32_BLOCK, count = a.head->count, w = threadIdx.x >> 6;
+    if (m0 < 0) {
+        if (n0 == 0) entries_group<HT, WT>(a, blockIdx.x * 4 + w);
+        return;
+    }
     if (n0 >= count) return;
-    const HeadRows<WT> A{(const WT *)a.weight, a.ws, 0, a.vocab, a.dim};
-    const HiddenRows<HT> B{(const HT *)a.hidden, a.hs, a.idx, count, a.dim};
-    f32x16 c[2][2];
-    products(A, B, m0, n0, 0, a.dim, sm, c);
-    const int w = threadIdx.x >> 6;
-    softmax_part(c, a.part + ((size_t)blockIdx.x * 2 + (w >> 1)) * a.part_ld + n0 + (w & 1) * 64, m0 + (w >> 1) * 64, a.vocab, LOG2E / a.temperature);
+    const Lines<WT> A(a.weight, a.ws, a.vocab, a.dim);
+    const ListedLines<HT> B{Lines<HT>(a.hidden, a.hs, count, a.dim), a.idx};
+    f32x16 c[1][1];
+    products<true, true>(A, B, m0, n0, 0, a.dim, sm, c);
+    softmax_part(c, a.part + ((size_t)(m0 / F32_BLOCK) * 2 + (w >> 1)) * a.part_ld + n0 + (w & 1) * 32, m0 + (w >> 1) * 32, a.vocab, LOG2E / a.temperature);
 }
 
-template <class HT, class WT> __global__ __launch_bounds__(256) void f32_probabilities_kernel(LossArgs a, int v0, int vn)
+template <class HT, class WT> __global__ __launch_bounds__(256) void f32_probabilities_kernel(LossArgs a, int v0, int vn, int extra)
 {
     __shared__ Tiles sm;
-    const int m0 = blockIdx.x * F32_BLOCK, n0 = blockIdx.y * F32_BLOCK, count = a.head->count;
+    const int m0 = ((int)blockIdx.x - extra) * F32_BLOCK, n0 = blockIdx.y * F32_BLOCK, count = a.head->count;
+    if (m0 < 0) {
+        if (n0 == 0) entries_group<HT, WT>(a, blockIdx.x * 4 + (threadIdx.x >> 6));
+        return;
+    }
     if (n0 >= count) return;
-    const HeadRows<WT> A{(const WT *)a.weight, a.ws, v0, vn, a.dim};
-    const HiddenRows<HT> B{(const HT *)a.hidden, a.hs, a.idx, count, a.dim};
-    f32x16 c[2][2];
-    products(A, B, m0, n0, 0, a.dim, sm, c);
+    const Lines<WT> A((const WT *)a.weight + (long long)v0 * a.ws, a.ws, vn, a.dim);
+    const ListedLines<HT> B{Lines<HT>(a.hidden, a.hs, count, a.dim), a.idx};
+    f32x16 c[1][1];
+    products<true, true>(A, B, m0, n0, 0, a.dim, sm, c);
     const float k = 1.0f / a.temperature;
     each_run(c, [&](int n, int m, float (&v)[8]) {
         n += n0; m += m0;
@@ -148,10 +208,10 @@ template <class WT> __global__ __launch_bounds__(256) void f32_hidden_grad_kerne
     __shared__ Tiles sm;
     const int m0 = blockIdx.x * F32_BLOCK, n0 = blockIdx.y * F32_BLOCK, count = a.head->count;
     if (n0 >= count) return;
-    const HeadColumns<WT> A{(const WT *)a.weight, a.ws, v0, vn, a.dim};
-    const PieceRows B{(const float *)a.G, a.g_ld, count, vn};
-    f32x16 c[2][2];
-    products(A, B, m0, n0, min(vn, (int)blockIdx.z * per), min(vn, ((int)blockIdx.z + 1) * per), sm, c);
+    const Lines<WT> A((const WT *)a.weight + (long long)v0 * a.ws, a.ws, vn, a.dim);
+    const Lines<float> B(a.G, a.g_ld, count, vn);
+    f32x16 c[1][1];
+    products<false, true>(A, B, m0, n0, min(vn, (int)blockIdx.z * per), min(vn, ((int)blockIdx.z + 1) * per), sm, c);
     each_run(c, [&](int n, int m, float (&v)[8]) {
         n += n0; m += m0;
         if (m >= a.d_pad) return;
@@ -168,60 +228,28 @@ template <class HT, class WT> __global__ __launch_bounds__(256) void f32_weight_
 {
     __shared__ Tiles sm;
     const int m0 = blockIdx.x * F32_BLOCK, n0 = blockIdx.y * F32_BLOCK, count = a.head->count;
-    const HiddenColumns<HT> A{(const HT *)a.hidden, a.hs, a.idx, count, a.dim};
-    const PieceColumns B{(const float *)a.G, a.g_ld, count, vn};
-    f32x16 c[2][2];
-    products(A, B, m0, n0, 0, count, sm, c);
+    const ListedLines<HT> A{Lines<HT>(a.hidden, a.hs, count, a.dim), a.idx};
+    const Lines<float> B(a.G, a.g_ld, count, vn);
+    f32x16 c[1][1];
+    products<false, false>(A, B, m0, n0, 0, count, sm, c);
     const float k = a.head->scale * a.temperature;
+    const bool wide = ((reinterpret_cast<uintptr_t>(a.d_weight) | (uintptr_t)(a.dws * sizeof(WT))) & 15) == 0;
     each_run(c, [&](int n, int m, float (&v)[8]) {
         n += n0; m += m0;
         if (n >= vn) return;
         WT *to = (WT *)a.d_weight + (long long)(v0 + n) * a.dws + m;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) if (m + e < a.dim) store_one(to + e, k * v[e]);
+        for (int e = 0; e < 8; ++e) v[e] *= k;
+        if (wide && m + 8 <= a.dim) store_run(to, v);
+        else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) if (m + e < a.dim) store_one(to + e, v[e]);
+        }
     });
 }
 
-// Products of listed entries: a wavefront takes 32 of them, its rows of the head against its hidden rows, of which only the diagonal is kept (the matrix unit
-// is all but idle in a product this small, and it gives the bits that the same pair has in a block: the same instruction over the same steps of k).
-template <class HT, class WT> __global__ __launch_bounds__(64) void f32_entries_kernel(LossArgs a)
-{
-    const int lane = threadIdx.x, e = blockIdx.x * 32 + (lane & 31), kk = lane >> 5, count = a.head->count;
-    if ((long long)blockIdx.x * 32 >= (long long)count * a.entries) return;
-    const int i = e / a.entries, j = e - i * a.entries;
-    const HT *h = (const HT *)a.hidden;
-    const WT *w = (const WT *)a.weight;
-    bool on = i < count;
-    if (on) {
-        const int r = a.idx[i], id = a.ids[(long long)r * a.entries + j];
-        on = id >= 0 && id < a.vocab;
-        h += r * a.hs;
-        if (on) w += id * a.ws;
-    }
-    f32x16 c;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) c[r] = 0.f;
-    for (int k = 0; k < a.dim; k += BK) {
-        float x[BK / 2], y[BK / 2];
-#pragma unroll
-        for (int s = 0; s < BK / 2; ++s) {
-            const int at = k + 2 * s + kk;
-            const bool in = on && at < a.dim;
-            x[s] = in ? load_one(w + at) : 0.f;
-            y[s] = in ? load_one(h + at) : 0.f;
-        }
-#pragma unroll
-        for (int s = 0; s < BK / 2; ++s) c = __builtin_amdgcn_mfma_f32_32x32x2f32(x[s], y[s], c, 0, 0, 0);
-    }
-    // row m of column n lies in register (m / 8) * 4 + m % 4 of lane n + 32 * (m / 4 % 2)
-    const int n = lane & 31;
-    float d = 0.f;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) d = (n >> 3) * 4 + (n & 3) == r ? c[r] : d;
-    if (on && ((n >> 2) & 1) == kk) a.value[e] = d;
-}
-
 int blocks(int n) { return (n + F32_BLOCK - 1) / F32_BLOCK; }
+int entry_blocks(const LossArgs &a) { return (int)(((long long)a.rows * a.entries + 127) / 128); }
 
 template <class Go> void by_types(const LossArgs &a, Go go)
 {
@@ -233,31 +261,24 @@ template <class Go> void by_types(const LossArgs &a, Go go)
 
 void launch_f32_softmax(hipStream_t s, const LossArgs &a)
 {
-    if (!a.rows) return;
     by_types(a, [&](auto ht, auto wt) {
-        hipLaunchKernelGGL((f32_softmax_kernel<decltype(ht), decltype(wt)>), dim3(blocks(a.vocab), blocks(a.rows)), dim3(256), 0, s, a);
+        const int extra = entry_blocks(a);
+        hipLaunchKernelGGL((f32_softmax_kernel<decltype(ht), decltype(wt)>), dim3(extra + blocks(a.vocab), blocks(a.rows)), dim3(256), 0, s, a, extra);
     });
 }
 
-void launch_f32_entries(hipStream_t s, const LossArgs &a)
-{
-    if (!a.rows) return;
-    by_types(a, [&](auto ht, auto wt) {
-        hipLaunchKernelGGL((f32_entries_kernel<decltype(ht), decltype(wt)>), dim3((unsigned)(((long long)a.rows * a.entries + 31) / 32)), dim3(64), 0, s, a);
-    });
-}
+int f32_softmax_parts(const LossArgs &a) { return blocks(a.vocab) * 2; }
 
 void launch_f32_probabilities(hipStream_t s, const LossArgs &a, int v0, int vn)
 {
-    if (!a.rows) return;
     by_types(a, [&](auto ht, auto wt) {
-        hipLaunchKernelGGL((f32_probabilities_kernel<decltype(ht), decltype(wt)>), dim3(blocks(vn), blocks(a.rows)), dim3(256), 0, s, a, v0, vn);
+        const int extra = v0 == 0 ? entry_blocks(a) : 0;
+        hipLaunchKernelGGL((f32_probabilities_kernel<decltype(ht), decltype(wt)>), dim3(extra + blocks(vn), blocks(a.rows)), dim3(256), 0, s, a, v0, vn, extra);
     });
 }
 
 void launch_f32_hidden_grad(hipStream_t s, const LossArgs &a, int v0, int vn, bool first)
 {
-    if (!a.rows) return;
     const int per = ((vn + a.splits - 1) / a.splits + BK - 1) / BK * BK;   // whole steps
     const dim3 grid(blocks(a.dim), blocks(a.rows), a.splits);
     if (a.wdt == DT_BF16) hipLaunchKernelGGL((f32_hidden_grad_kernel<bf16_t>), grid, dim3(256), 0, s, a, v0, vn, per, first);

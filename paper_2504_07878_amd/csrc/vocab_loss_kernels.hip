@@ -46,17 +46,24 @@ __device__ __forceinline__ void skipped(const LossArgs &a, int r, int st)
     a.lse[r] = v;
 }
 
-// Row `to` of the packed rows: row `from` that counts (-1: zeros), whole steps long.
+// Row `to` of the packed rows: row `from` that counts (-1: zeros), whole steps long. fp32 rows: blocks of 64 rows x 3 planes, a plane being what the ones
+// before it leave, rounded to bf16.
 template <class HT> __device__ __forceinline__ void pack_row(const LossArgs &a, int to, int from)
 {
+    const HT *h = (const HT *)a.hidden + (long long)max(from, 0) * a.hs;
     if constexpr (sizeof(HT) == 2) {
-        const HT *h = (const HT *)a.hidden + (long long)max(from, 0) * a.hs;
         bf16_t *p = (bf16_t *)a.hp + (size_t)to * a.d_pad;
-        if (((reinterpret_cast<uintptr_t>(h) | (uintptr_t)(a.hs * 2)) & 15) == 0 && a.dim == a.d_pad) {
-            for (int k = threadIdx.x * 8; k < a.d_pad; k += blockDim.x * 8)
-                *reinterpret_cast<uint4 *>(p + k) = from < 0 ? make_uint4(0, 0, 0, 0) : *reinterpret_cast<const uint4 *>(h + k);
-        } else {
-            for (int k = threadIdx.x * 8; k < a.d_pad; k += blockDim.x * 8) *reinterpret_cast<uint4 *>(p + k) = from < 0 ? make_uint4(0, 0, 0, 0) : load8(h, k, a.dim);
+        for (int k = threadIdx.x * 8; k < a.d_pad; k += blockDim.x * 8) *reinterpret_cast<uint4 *>(p + k) = from < 0 ? make_uint4(0, 0, 0, 0) : load8(h, k, a.dim);
+    } else {
+        bf16_t *p = (bf16_t *)a.hp + (size_t)((to >> 6) * 192 + (to & 63)) * a.d_pad;
+        for (int k = threadIdx.x; k < a.d_pad; k += blockDim.x) {
+            float v = from >= 0 && k < a.dim ? h[k] : 0.f;
+#pragma unroll
+            for (int l = 0; l < 3; ++l) {
+                const bf16_t b = (bf16_t)two_bf16(v, 0.f);
+                p[(size_t)l * 64 * a.d_pad + k] = b;
+                v -= load_one(&b);
+            }
         }
     }
 }
@@ -164,7 +171,7 @@ template <bool TEACHER, class HT> static void rows_of(hipStream_t s, const LossA
 {
     const int packed = a.hp ? (a.rows + BF16_BLOCK - 1) / BF16_BLOCK * BF16_BLOCK : 0;
     if (a.rows <= 1024 && (long long)a.rows * a.entries <= 16384) {
-        const int used = a.rows <= PAIR_ROWS && a.hp ? (a.pairs ? (a.rows <= 64 ? 128 : 256) : (a.rows <= 64 ? 64 : 128)) : packed;   // what the products' blocks read
+        const int used = !a.hp ? 0 : a.n_block < 256 ? (a.rows + a.n_block - 1) / a.n_block * a.n_block : packed;   // what the products' blocks read
         hipLaunchKernelGGL((loss_prepare_kernel<TEACHER, HT>), dim3(std::max(a.rows, used)), dim3(256), 0, s, a, used);
         return;
     }
