@@ -67,7 +67,7 @@ void launch_loss_hidden_grad(hipStream_t s, const LossArgs &a);
 
 // Products of the listed entries, each the bits that the softmax's own products have: a probability near 1 and its logit then agree, and what is left of
 // 1 - p and of lse - z is not the difference of two roundings.
-void launch_bf16_entries(hipStream_t s, const LossArgs &a);
+void launch_bf16_entries(hipStream_t s, const LossArgs &a, bool packed);   // packed: a.wp holds the whole head
 
 // Products on 32-bit matrix instructions, operands of either type and any stride (vocab_loss_f32_kernels.hip). Blocks of 64 x 64. The
 // softmax and the first piece's probabilities bring the products of the listed entries.
@@ -90,14 +90,19 @@ void launch_bf16_weight_grad(hipStream_t s, const LossArgs &a, int v0, int vn);
 #ifdef __HIPCC__
 __host__ __device__ inline int bf16_products_rows(int count, int half) { return half ? 2 * half : count; }
 __host__ __device__ inline int bf16_rows(const LossArgs &a, int rows) { return (rows + a.n_block - 1) / a.n_block * a.n_block; }   // whole blocks
-// Splits of the sums of the gradient to `rows` rows (of products), at most a.splits. With 8 or more the k's of an eighth of them lie on one XCD: every XCD reads its own part of
-// the head, once, and of G. Enough for every compute unit to have a block; none where there are many blocks anyway.
+// Splits of the sums of the gradient to `rows` rows (of products), a power of two, at most a.splits: those for which a workgroup a compute unit is done first, when it takes
+// `tiles` * n blocks, 256 at a time, of (steps / n + SPLIT_COST) steps of 64 k each; the sums' reading and writing costs a block about as much as that many steps.
+// (6144 rows x 151936 x 896, 8 splits instead of 2: 2097 -> 1999 us; 2048 x 152064 x 3584: 2114 -> 2347 us, so 2.)
+constexpr int SPLIT_COST = 16;
 __host__ __device__ inline int bf16_splits(const LossArgs &a, int rows)
 {
-    const int tiles = (rows + a.n_block - 1) / a.n_block * ((a.d_pad + BF16_BLOCK - 1) / BF16_BLOCK);
-    if (tiles >= 1024 || a.splits < 2) return 1;
-    const int n = tiles >= 32 ? 8 : 32 / (tiles ? tiles : 1) * 8;
-    return n < a.splits ? n : a.splits >= 8 ? a.splits / 8 * 8 : a.splits;
+    const int tiles = (rows + a.n_block - 1) / a.n_block * ((a.d_pad + BF16_BLOCK - 1) / BF16_BLOCK), steps = (a.piece + 63) / 64;
+    int best = 1, least = 0x7fffffff;
+    for (int n = 1; n <= a.splits && (n <= 8 || tiles * n <= 256) && (n == 1 || tiles < 1024); n *= 2) {
+        const int time = (tiles * n + 255) / 256 * ((steps + n - 1) / n + SPLIT_COST);
+        if (time < least) { least = time; best = n; }
+    }
+    return best;
 }
 #endif
 

@@ -129,7 +129,7 @@ int forward(const tr_loss_config *c, void *ws, size_t ws_bytes, void *stream, co
             if (!a.direct) launch_bf16_pack_head(s, a, v0, vn);
             launch_bf16_softmax(s, a, v0, vn, along && v0 == 0);
         }
-        if (!along) launch_bf16_entries(s, a);
+        if (!along) launch_bf16_entries(s, a, !a.direct && a.piece >= a.vocab);
     } else {
         launch_f32_softmax(s, a);
     }
@@ -152,12 +152,14 @@ int backward(const tr_loss_config *c, void *ws, size_t ws_bytes, void *stream, c
     hipStream_t s = (hipStream_t)stream;
     launch_loss_rows(s, a);
     const bool half = is_bf16(c), one = a.piece >= a.vocab, along = half && a.n_block < 256;
-    if (a.rows && half && !along) launch_bf16_entries(s, a);
+    const bool whole = half && a.rows && !a.direct && one;      // the head is packed once, whole
+    if (whole) launch_bf16_pack_head(s, a, 0, a.vocab);
+    if (a.rows && half && !along) launch_bf16_entries(s, a, whole);
     for (int v0 = 0; v0 < a.vocab; v0 += a.piece) {
         const int vn = std::min(a.piece, a.vocab - v0);
         if (a.rows) {
             if (half) {
-                if (!a.direct) launch_bf16_pack_head(s, a, v0, vn);
+                if (!a.direct && !whole) launch_bf16_pack_head(s, a, v0, vn);
                 launch_bf16_probabilities(s, a, v0, vn, along && v0 == 0);
             } else launch_f32_probabilities(s, a, v0, vn);
             if (v0 == 0) launch_loss_values(s, a, one);

@@ -285,8 +285,8 @@ template <int TM, int TN> struct Softmax : Logits<TM, TN> {
     {
         const LossArgs &a = this->a;
         const int w = wavefront(), wm = w / WN, wn = w % WN;
-        if constexpr (WM > 2) {      // few rows: the block's wavefronts join their parts in LDS
-            float2 *red = reinterpret_cast<float2 *>(dynamic_lds + LDS_OF_RING);
+        if constexpr (WM > 2 || TM == 128) {      // few rows or small blocks: the wavefronts join their parts in LDS
+            float2 *red = reinterpret_cast<float2 *>(dynamic_lds + (TM == 128 ? 0 : LDS_OF_RING));   // (block_kernel: its LDS is free by then)
             softmax_part(c, red + wm * TN + wn * NI * 32, p.m * TM + wm * MI * 32, this->vn, LOG2E / a.temperature);
             __syncthreads();
             for (int i = threadIdx.x; i < TN; i += WM * WN * 64) {
@@ -317,27 +317,43 @@ template <int TM, int TN> struct Probabilities : Logits<TM, TN> {
             }
         }
         const float k2 = LOG2E / a.temperature;
-        const bool inside = p.m * TM + TM <= this->vn && p.n * TN + TN <= this->count;
-        each_run<WN>(c, [&](int j, int i, int v, float (&x)[8]) {
-            const int at = p.n * TN + i, row = half && at >= half ? at - half : at;
-            v += p.m * TM;
-            // rows that do not count and entries that do not exist: zeros, which the next products read
+        const int lane = threadIdx.x & 63, v0 = p.m * TM + wavefront() / WN * MI * 32, there = this->vn - v0 - 8 * (lane >> 5);   // entries that exist from this lane's first on
+        const int needed = (this->rows + 63) / 64 * 64;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = inside || (row < this->count && v + e < this->vn) ? weight[j] * term(x[e], k2, lse2[j]) : 0.f;
-            if (half && first + j * 32 >= half) {      // a pair's second: what rounding leaves
+        for (int j = 0; j < NI; ++j) {
+            const int at = first + j * 32;
+            if (at >= needed) continue;               // (the products read whole steps of 64 rows)
+            const bool second = half && at >= half;   // of a pair: what rounding leaves
+            bf16_t *to = (bf16_t *)a.G + (size_t)(at + (lane & 31)) * a.g_ld + v0 + 8 * (lane >> 5);
 #pragma unroll
-                for (int e = 0; e < 8; e += 2) {
-                    const uint32_t hi = two_bf16(x[e], x[e + 1]);
-                    x[e] -= __uint_as_float(hi << 16);
-                    x[e + 1] -= __uint_as_float(hi & 0xffff0000u);
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float x[8];
+                    run_of(c[i][j], h, x);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = weight[j] * term(x[e], k2, lse2[j]);
+                    // rows that do not count and entries that do not exist: zeros, which the next products read
+                    if (this->vn < p.m * TM + TM || this->rows < p.n * TN + TN || half) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) x[e] = weight[j] != 0.f && i * 32 + 16 * h + e < there ? x[e] : 0.f;
+                    }
+                    if (second) {
+#pragma unroll
+                        for (int e = 0; e < 8; e += 2) {
+                            const uint32_t hi = two_bf16(x[e], x[e + 1]);
+                            x[e] -= __uint_as_float(hi << 16);
+                            x[e + 1] -= __uint_as_float(hi & 0xffff0000u);
+                        }
+                    }
+                    store_run(to + i * 32 + 16 * h, x);
                 }
-            }
-            store_run((bf16_t *)a.G + (size_t)at * a.g_ld + v, x);
-        });
+        }
     }
 };
 
-// Every sum over the piece's vocabulary in `splits` parts. With 8 or more, part s belongs to XCD s / (splits / 8), which takes all blocks of its parts.
+// Every sum over the piece's vocabulary in `splits` parts (a power of two). A part belongs to 8 / splits XCDs, which share its blocks, or an XCD has splits / 8 whole parts: what an
+// XCD reads of the head and of G, it reads alone, or with few.
 template <int TM, int TN> struct HiddenGrad {
     static constexpr bool A_KC = false, B_KC = true;
     const LossArgs &a;
@@ -351,20 +367,23 @@ template <int TM, int TN> struct HiddenGrad {
         tiles = mb * nb;
         splits = bf16_splits(a, rows);
         per = ((vn + splits - 1) / splits + 63) / 64 * 64;
-        o = Order(mb, nb * splits, b);
+        o.mb = mb; o.nb = nb;
+        const int x = b & 7, j = b >> 3;
         if (splits >= 8) {
             const int own = tiles * (splits >> 3);
-            o.first = (b & 7) * own + (b >> 3);
-            o.end = ((b & 7) + 1) * own;
+            o.first = x * own + j;
+            o.end = (x + 1) * own;
+        } else {
+            const int sharing = 8 / splits, own = (tiles + sharing - 1) / sharing, of = x / sharing * tiles;
+            o.first = of + x % sharing * own + j;
+            o.end = of + min(tiles, (x % sharing + 1) * own);
         }
     }
     __device__ __forceinline__ Place place(int i) const
     {
         Place p;
         p.split = i / tiles;
-        Order one = o;
-        one.nb = nb;
-        one.at(i - p.split * tiles, p.m, p.n);
+        o.at(i - p.split * tiles, p.m, p.n);
         const int k0 = min(vn, p.split * per);
         p.K = min(vn, k0 + per) - k0;
         p.a = head_rows(a, v0, p.lda);
@@ -375,16 +394,25 @@ template <int TM, int TN> struct HiddenGrad {
     template <int WM, int WN, int MI, int NI> __device__ __forceinline__ void done(const Place &p, const f32x16 (&c)[MI][NI])
     {
         if (!first && p.K == 0) return;
-        each_run<WN>(c, [&](int, int i, int d, float (&x)[8]) {
-            d += p.m * TM;
-            if (d >= a.d_pad) return;
-            float *to = a.acc + ((size_t)p.split * bf16_rows(a, rows) + p.n * TN + i) * a.d_pad + d;
-            if (!first) {
-                const float4 u = reinterpret_cast<const float4 *>(to)[0], w = reinterpret_cast<const float4 *>(to)[1];
-                x[0] += u.x; x[1] += u.y; x[2] += u.z; x[3] += u.w; x[4] += w.x; x[5] += w.y; x[6] += w.z; x[7] += w.w;
+        const int lane = threadIdx.x & 63, w = wavefront(), d0 = p.m * TM + w / WN * MI * 32 + 8 * (lane >> 5);
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+            float *to = a.acc + ((size_t)p.split * bf16_rows(a, rows) + p.n * TN + (w % WN * NI + j) * 32 + (lane & 31)) * a.d_pad + d0;
+#pragma unroll
+            for (int i = 0; i < MI; ++i) {
+                if (d0 + i * 32 >= a.d_pad) break;       // (d_pad: a multiple of 64)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float x[8];
+                    run_of(c[i][j], h, x);
+                    if (!first) {
+                        const float4 u = reinterpret_cast<const float4 *>(to + i * 32 + 16 * h)[0], v = reinterpret_cast<const float4 *>(to + i * 32 + 16 * h)[1];
+                        x[0] += u.x; x[1] += u.y; x[2] += u.z; x[3] += u.w; x[4] += v.x; x[5] += v.y; x[6] += v.z; x[7] += v.w;
+                    }
+                    store_run(to + i * 32 + 16 * h, x);
+                }
             }
-            store_run(to, x);
-        });
+        }
     }
 };
 
@@ -430,56 +458,81 @@ template <int TM, int TN> struct WeightGrad {
                     for (int e = 0; e < 8; ++e) if (d + e < ds) to[e] = (bf16_t)(q[e >> 1] >> (16 * (e & 1)));
                 }
             }
-        } else
-            each_run<WN>(c, [&](int, int i, int d, float (&x)[8]) {
-                if (i >= vs || d >= ds) return;
-                bf16_t *to = out + (long long)i * a.dws + d;
+        } else {
+            const int lane = threadIdx.x & 63, w = wavefront(), d0 = w / WN * MI * 32 + 8 * (lane >> 5);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] *= k;
-                if (whole && d + 8 <= ds) store_run(to, x);
-                else {
+            for (int j = 0; j < NI; ++j) {
+                const int v = (w % WN * NI + j) * 32 + (lane & 31);
+                if (v >= vs) continue;
+                bf16_t *to = out + (long long)v * a.dws + d0;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) if (d + e < ds) store_one(to + e, x[e]);
-                }
-            });
+                for (int i = 0; i < MI; ++i)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int d = i * 32 + 16 * h;
+                        float x[8];
+                        run_of(c[i][j], h, x);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) x[e] *= k;
+                        if (whole && d0 + d + 8 <= ds) store_run(to + d, x);
+                        else {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) if (d0 + d + e < ds) store_one(to + d + e, x[e]);
+                        }
+                    }
+            }
+        }
     }
 };
 
 // Products of listed entries: a wavefront takes 32 of them, its rows of the head against its packed rows, of which only the diagonal is kept: the matrix unit is
 // all but idle in a product this small, and it gives the bits that the same pair has in a block (the same instruction over the same steps of k).
-template <int PLANES> __device__ __forceinline__ void entries_group(const LossArgs &a, int group)
+template <int PLANES> __device__ __forceinline__ void entries_group(const LossArgs &a, int group, bool packed)   // packed: the whole head is
 {
     const int lane = threadIdx.x & 63, e = group * 32 + (lane & 31), hf = lane >> 5, count = a.head->count;
     if ((long long)group * 32 >= (long long)count * a.entries) return;
     const int i = e / a.entries, j = e - i * a.entries;
     bool on = i < count;
-    const bf16_t *h = (const bf16_t *)a.hp, *w = (const bf16_t *)a.weight;
+    const bf16_t *h = (const bf16_t *)a.hp, *w = packed ? (const bf16_t *)a.wp : (const bf16_t *)a.weight;
     if (on) {
         const int id = a.ids[(long long)a.idx[i] * a.entries + j];
         on = id >= 0 && id < a.vocab;
         h += (size_t)(PLANES == 1 ? i : (i >> 6) * 64 * PLANES + (i & 63)) * a.d_pad;
-        if (on) w += id * a.ws;
+        if (on) w = packed ? (const bf16_t *)a.wp + (size_t)id * a.d_pad : w + id * a.ws;
     }
     f32x16 c;
 #pragma unroll
     for (int r = 0; r < 16; ++r) c[r] = 0.f;
-    constexpr int AT_ONCE = PLANES == 1 ? 8 : 4;      // steps of 16 k whose loads are requested together
-    for (int k0 = 0; k0 < a.d_pad; k0 += 16 * AT_ONCE) {
-        bf16x8 x[AT_ONCE], y[AT_ONCE][PLANES];
+    // N steps of 16 k, their loads requested together; ANYWHERE: the head's row may begin anywhere, PART: and end within the steps
+    auto steps = [&](auto n, auto anywhere, auto part, int k0) {
+        constexpr int N = decltype(n)::value;
+        bf16x8 x[N], y[N][PLANES];
 #pragma unroll
-        for (int q = 0; q < AT_ONCE; ++q) {
-            const int k = min(k0 + 16 * q, a.d_pad - 16) + 8 * hf;
+        for (int q = 0; q < N; ++q) {
+            const int k = k0 + 16 * q + 8 * hf;
+            if constexpr (decltype(part)::value) x[q] = __builtin_bit_cast(bf16x8, load8(w, k, on ? a.dim : 0));
+            else if constexpr (decltype(anywhere)::value) __builtin_memcpy(&x[q], w + k, 16);
+            else x[q] = *reinterpret_cast<const bf16x8 *>(w + k);
 #pragma unroll
             for (int l = 0; l < PLANES; ++l) y[q][l] = *reinterpret_cast<const bf16x8 *>(h + (size_t)l * 64 * a.d_pad + k);
-            if (a.direct) x[q] = *reinterpret_cast<const bf16x8 *>(w + k);
-            else x[q] = __builtin_bit_cast(bf16x8, load8(w, k, on ? a.dim : 0));
         }
 #pragma unroll
-        for (int q = 0; q < AT_ONCE; ++q)
-            if (k0 + 16 * q < a.d_pad) {
+        for (int q = 0; q < N; ++q)
 #pragma unroll
-                for (int l = 0; l < PLANES; ++l) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[q], y[q][l], c, 0, 0, 0);
-            }
+            for (int l = 0; l < PLANES; ++l) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[q], y[q][l], c, 0, 0, 0);
+    };
+    using Yes = std::true_type;
+    using No = std::false_type;
+    constexpr int MOST = PLANES == 1 ? 14 : 8;
+    using Many = std::integral_constant<int, MOST>;
+    using One = std::integral_constant<int, 1>;
+    int k = 0;
+    if (a.direct || packed) {
+        for (; k + 16 * MOST <= a.d_pad; k += 16 * MOST) steps(Many{}, No{}, No{}, k);
+        for (; k < a.d_pad; k += 16) steps(One{}, No{}, No{}, k);
+    } else {
+        for (; k + 16 * MOST <= a.dim; k += 16 * MOST) steps(Many{}, Yes{}, No{}, k);
+        for (; k < a.d_pad; k += 16) steps(One{}, Yes{}, Yes{}, k);
     }
     const int n = lane & 31;   // row m of column n lies in register (m / 8) * 4 + m % 4 of lane n + 32 * (m / 4 % 2)
     float d = 0.f;
@@ -488,14 +541,14 @@ template <int PLANES> __device__ __forceinline__ void entries_group(const LossAr
     if (on && ((n >> 2) & 1) == hf) a.value[e] = d;
 }
 
-__global__ __launch_bounds__(64) void bf16_entries_kernel(LossArgs a) { entries_group<1>(a, blockIdx.x); }
+__global__ __launch_bounds__(64) void bf16_entries_kernel(LossArgs a, bool packed) { entries_group<1>(a, blockIdx.x, packed); }
 
 // Few rows, bound by the head's bytes: one workgroup a compute unit takes block after block, the copies running on across blocks: a ring of steps in LDS, one barrier a
 // step. The first `extra` (a multiple of 8) workgroups take listed entries instead.
 template <template <int, int> class Job_, class Bl> __global__ __launch_bounds__(Bl::WAVES * 64) void stream_kernel(LossArgs a, int v0, int vn, int flag, int extra)
 {
     if ((int)blockIdx.x < extra) {
-        entries_group<Bl::PL>(a, blockIdx.x * Bl::WAVES + wavefront());
+        entries_group<Bl::PL>(a, blockIdx.x * Bl::WAVES + wavefront(), !a.direct && vn == a.vocab);
         return;
     }
     constexpr int MI = Bl::MI, NI = Bl::NI, STAGES = Bl::STAGES_, COPIES = Bl::TA::COPIES + Bl::TB::COPIES;
@@ -729,6 +782,12 @@ template <class... P, class... A> void launch(void (*kernel)(P...), dim3 grid, i
 
 int entry_groups(const LossArgs &a) { return (int)(((long long)a.rows * a.entries + 31) / 32); }
 
+template <bool A_KC, bool B_KC> using Quarter = Block<2, 2, 2, 2, 2, A_KC, B_KC>;      // 128 x 128, two a compute unit
+
+// Where blocks of 256 x 256 would leave half of the chip without one, those of 128 x 128 are four times as many (1021 rows x 5003 x 1001: softmax 30 -> XX us).
+int product_rows(const LossArgs &a) { return a.pairs ? std::max(a.rows, 2 * PAIR_ROWS) : a.rows; }     // at most
+bool small_blocks(int m, int n) { return up_div(m, 256) * up_div(n, 256) <= 128; }
+
 // entries: listed entries too, where there are few rows or fp32 ones
 template <template <int, int> class Job> void launch_job(hipStream_t s, const LossArgs &a, int v0, int vn, int flag, bool entries)
 {
@@ -745,7 +804,9 @@ template <template <int, int> class Job> void launch_job(hipStream_t s, const Lo
         }
     if (a.n_block == 64) launch(stream_kernel<Job, Small>, persistent, 512, LDS_OF_RING + 8 * 64 * 8, s, a, v0, vn, flag, extra);
     else if (a.n_block == 128) launch(stream_kernel<Job, Middle>, persistent, 512, LDS_OF_RING + 8 * 128 * 8, s, a, v0, vn, flag, extra);
-    else launch(turns_kernel<Job>, dim3(256), 512, 5 * 256 * BK * 2, s, a, v0, vn, flag);
+    else if (Job<256, 64>::A_KC && small_blocks(vn, product_rows(a))) {
+        if constexpr (A) launch(block_kernel<Job, Quarter<A, B>>, dim3(up_div(up_div(vn, 128) * up_div(product_rows(a), 128), 8) * 8), 256, Quarter<A, B>::LDS, s, a, v0, vn, flag);
+    } else launch(turns_kernel<Job>, dim3(256), 512, 5 * 256 * BK * 2, s, a, v0, vn, flag);
 }
 
 }  // namespace
@@ -755,11 +816,11 @@ void launch_bf16_pack_head(hipStream_t s, const LossArgs &a, int v0, int vn)
     hipLaunchKernelGGL(bf16_pack_head_kernel, dim3(vn), dim3(128), 0, s, a, v0);
 }
 
-void launch_bf16_entries(hipStream_t s, const LossArgs &a) { hipLaunchKernelGGL(bf16_entries_kernel, dim3(entry_groups(a)), dim3(64), 0, s, a); }
+void launch_bf16_entries(hipStream_t s, const LossArgs &a, bool packed) { hipLaunchKernelGGL(bf16_entries_kernel, dim3(entry_groups(a)), dim3(64), 0, s, a, packed); }
 
 void launch_bf16_softmax(hipStream_t s, const LossArgs &a, int v0, int vn, bool entries) { launch_job<Softmax>(s, a, v0, vn, 0, entries); }
 
-int bf16_softmax_parts(const LossArgs &a) { return up_div(a.vocab, BF16_BLOCK) * (a.n_block < 256 ? 1 : 2); }
+int bf16_softmax_parts(const LossArgs &a) { return a.n_block < 256 ? up_div(a.vocab, BF16_BLOCK) : a.direct || a.piece >= a.vocab ? (small_blocks(a.vocab, product_rows(a)) ? up_div(a.vocab, 128) : up_div(a.vocab, BF16_BLOCK) * 2) : up_div(a.vocab, BF16_BLOCK) * 2; }
 
 void launch_bf16_probabilities(hipStream_t s, const LossArgs &a, int v0, int vn, bool entries) { launch_job<Probabilities>(s, a, v0, vn, 0, entries); }
 
@@ -774,7 +835,7 @@ void launch_bf16_hidden_grad(hipStream_t s, const LossArgs &a, int v0, int vn, b
 #endif
 void launch_bf16_weight_grad(hipStream_t s, const LossArgs &a, int v0, int vn)
 {
-    using Bl = Block<2, 2, 2, 2, 2, false, false>;
+    using Bl = Quarter<false, false>;
     if (a.rows <= XK) launch(block_kernel<WeightGrad, Bl>, dim3(up_div(up_div(a.d_pad, Bl::TM) * up_div(vn, Bl::TN), 8) * 8), 256, Bl::LDS, s, a, v0, vn, 0);
     else launch(turns_kernel<WeightGrad>, dim3(256), 512, 5 * 256 * BK * 2, s, a, v0, vn, 0);
 }

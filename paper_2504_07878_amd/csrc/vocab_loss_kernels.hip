@@ -339,48 +339,56 @@ void launch_loss_scatter(hipStream_t s, const LossArgs &a, int v0, int vn)
 
 // ------------------------------------------------------------------ gradient to the hidden rows
 
-// A workgroup takes 256 columns of the i-th row that counts: its wavefronts every fourth split each, in order, joined in a fixed order; and clears those of row i
-// if that does not count.
-template <class HT, bool BF16>
+// A workgroup takes ROWS rows that count, 256 columns of each: 4 / ROWS wavefronts a row take every such split each, in order, joined in a fixed order. It also clears those
+// of the rows of the same numbers that do not count.
+template <class HT, bool BF16, int ROWS>
 __global__ __launch_bounds__(256) void hidden_grad_kernel(LossArgs a)
 {
-    __shared__ float4 sums[3][64];
-    const int i = blockIdx.x, count = a.head->count, lane = threadIdx.x & 63, w = threadIdx.x >> 6, j = blockIdx.y * 256 + lane * 4;
+    __shared__ float4 sums[4][64];
+    constexpr int SHARE = 4 / ROWS;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, i = blockIdx.x * ROWS + w / SHARE, part = w % SHARE, count = a.head->count, j = blockIdx.y * 256 + lane * 4;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](float4 &to, const float4 u) { to.x += u.x; to.y += u.y; to.z += u.z; to.w += u.w; };
+    auto store = [&](int r, const float (&x)[4]) {
+        HT *out = (HT *)a.d_hidden + (long long)r * a.dhs + j;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) if (j + e < a.dim) store_one(out + e, x[e]);
+    };
     if (i < count) {
         const int half = BF16 ? a.head->half : 0, rows = BF16 ? bf16_products_rows(count, half) : a.n_pad, splits = BF16 ? bf16_splits(a, rows) : a.splits;
         const size_t apart = (size_t)(BF16 ? bf16_rows(a, rows) : rows) * a.d_pad;
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        auto add = [&](float4 &to, const float4 u) { to.x += u.x; to.y += u.y; to.z += u.z; to.w += u.w; };
-        if (j < a.d_pad)
+        const float *at = a.acc + (size_t)i * a.d_pad + j;
+        if (j < a.d_pad) {
 #pragma unroll 8
-            for (int p = w; p < splits; p += 4) {
-                const float *at = a.acc + p * apart + (size_t)i * a.d_pad + j;
-                add(v, *reinterpret_cast<const float4 *>(at));
-                if (half) add(v, *reinterpret_cast<const float4 *>(at + (size_t)half * a.d_pad));
+            for (int p = part; p < splits; p += SHARE) add(v, *reinterpret_cast<const float4 *>(at + p * apart));
+            if (half) {
+                at += (size_t)half * a.d_pad;
+#pragma unroll 8
+                for (int p = part; p < splits; p += SHARE) add(v, *reinterpret_cast<const float4 *>(at + p * apart));
             }
-        if (w) sums[w - 1][lane] = v;
-        __syncthreads();
-        if (w == 0) {
-            add(v, sums[0][lane]); add(v, sums[1][lane]); add(v, sums[2][lane]);
-            const float c = a.head->scale * a.temperature, x[4] = {v.x, v.y, v.z, v.w};
-            HT *out = (HT *)a.d_hidden + (long long)a.idx[i] * a.dhs;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) if (j + e < a.dim) store_one(out + j + e, c * x[e]);
         }
     }
-    if (a.state[i] != ROW_COUNTS && w == 0) {
-        HT *out = (HT *)a.d_hidden + (long long)i * a.dhs;
+    if constexpr (SHARE > 1) {
+        sums[w][lane] = v;
+        __syncthreads();
 #pragma unroll
-        for (int e = 0; e < 4; ++e) if (j + e < a.dim) store_one(out + j + e, 0.f);
+        for (int q = 1; q < SHARE; ++q) if (part == 0) add(v, sums[w + q][lane]);
+    }
+    if (part == 0) {
+        const float k = a.head->scale * a.temperature, x[4] = {k * v.x, k * v.y, k * v.z, k * v.w}, none[4] = {0.f, 0.f, 0.f, 0.f};
+        if (i < count) store(a.idx[i], x);
+        if (i < a.rows && a.state[i] != ROW_COUNTS) store(i, none);
     }
 }
 
 void launch_loss_hidden_grad(hipStream_t s, const LossArgs &a)
 {
     if (!a.rows) return;
-    const dim3 grid(a.rows, (a.dim + 255) / 256);
-    if (a.hdt == DT_BF16) hipLaunchKernelGGL((hidden_grad_kernel<bf16_t, true>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((hidden_grad_kernel<float, false>), grid, dim3(256), 0, s, a);
+    const int ny = (a.dim + 255) / 256;
+    if (a.hdt == DT_BF16) {
+        if (a.rows <= 512) hipLaunchKernelGGL((hidden_grad_kernel<bf16_t, true, 1>), dim3(a.rows, ny), dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((hidden_grad_kernel<bf16_t, true, 4>), dim3((a.rows + 3) / 4, ny), dim3(256), 0, s, a);
+    } else hipLaunchKernelGGL((hidden_grad_kernel<float, false, 1>), dim3(a.rows, ny), dim3(256), 0, s, a);
 }
 
 }  // namespace tr
