@@ -18,7 +18,7 @@ struct LossHead {
     float scale;    // largest |weight| of a row that counts
     int pad;
 };
-// Pairs: with 128 rows or fewer (bf16 products) G has a second row for every row, `half` (64 or 128) rows further on, with what rounding the first to bf16 left, and the
+// Pairs: with 128 rows or fewer (bf16 products) G has a second row for every row, `half` (32, 64 or 128) rows further on, with what rounding the first to bf16 left, and the
 // packed rows are there twice. The products are bound by the head's bytes then, so the second half costs little, and few rows average few roundings.
 constexpr int PAIR_ROWS = 128;
 

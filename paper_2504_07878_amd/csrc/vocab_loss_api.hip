@@ -100,7 +100,7 @@ int arguments(const tr_loss_config *c, const tr_loss_rows *in, void *ws, size_t 
         a.hp = b + p.hp; a.wp = b + p.wp;
         a.pairs = gradient;
         const int rows = gradient && a.rows <= PAIR_ROWS ? 2 * a.rows : a.rows;
-        a.n_block = rows <= 64 && !gradient ? 64 : rows <= 128 ? 128 : 256;
+        a.n_block = rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
         if (a.n_block < 256) a.part_ld = a.n_block;
     } else if (in_planes(c) && !gradient) {
         a.hp = b + p.hp; a.wp = b + p.wp;

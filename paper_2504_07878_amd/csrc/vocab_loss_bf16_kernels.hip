@@ -169,6 +169,22 @@ template <int WM_, int WN_, int MI_, int NI_, int STAGES, bool A_KC, bool B_KC, 
 #pragma unroll
                 for (int j = 0; j < NI; ++j) c[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xa[p][i], xb[p][j], c[i][j], 0, 0, 0);
         };
+        if constexpr (STAGES == 1) {
+#pragma unroll 1
+            for (int s = 0; s < steps; ++s) {
+                issue(0);
+                landed_and_barrier<0>();
+                ra.template read<0>(lds, xa[0]); rb.template read<0>(lds + TA::BYTES, xb[0]);
+                ra.template read<1>(lds, xa[1]); rb.template read<1>(lds + TA::BYTES, xb[1]);
+                multiply(0);
+                ra.template read<2>(lds, xa[0]); rb.template read<2>(lds + TA::BYTES, xb[0]);
+                multiply(1);
+                ra.template read<3>(lds, xa[1]); rb.template read<3>(lds + TA::BYTES, xb[1]);
+                multiply(0);
+                landed_and_barrier<0>();
+                multiply(1);
+            }
+        } else {
         constexpr int COPIES = TA::COPIES + TB::COPIES;
         int next = 0;
 #pragma unroll
@@ -196,6 +212,7 @@ template <int WM_, int WN_, int MI_, int NI_, int STAGES, bool A_KC, bool B_KC, 
             at = lds + stage * STAGE;
             if (s + 1 < steps) { ra.template read<0>(at, xa[0]); rb.template read<0>(at + TA::BYTES, xb[0]); }
             multiply(1);
+        }
         }
     }
 
@@ -426,7 +443,8 @@ template <int TM, int TN> struct WeightGrad {
     __device__ __forceinline__ Place place(int i) const
     {
         Place p;
-        o.at(i, p.m, p.n);
+        p.n = i / o.mb;                   // all blocks of some rows of the head before the next rows: whole rows are written at a time
+        p.m = i - p.n * o.mb;
         p.K = (rows + 63) / 64 * 64;      // G and the packed rows are zero from the last row that counts to there
         p.a = (const bf16_t *)a.hp + p.m * TM; p.lda = a.d_pad; p.a_limit = a.d_pad - p.m * TM;
         p.b = (const bf16_t *)a.G + p.n * TN; p.ldb = a.g_ld; p.b_limit = a.piece - p.n * TN; p.n_limit = vn - p.n * TN;
@@ -795,7 +813,8 @@ template <template <int, int> class Job> void launch_job(hipStream_t s, const Lo
     using Small = Block<8, 1, 1, 2, 3, A, B>;       // 256 x 64
     using Middle = Block<4, 2, 2, 2, 3, A, B>;      // 256 x 128
     const int extra = entries ? up_div(entry_groups(a), 64) * 8 : 0;
-    const dim3 persistent(256 + extra);
+    // a workgroup a compute unit: a few of them take entries only, since the head's bytes come as fast without them
+    const dim3 persistent(extra <= 64 ? 256 : 256 + extra);
     if constexpr (std::is_same_v<Job<256, 64>, Softmax<256, 64>>)
         if (a.hdt == DT_F32) {
             using Planes = Block<8, 1, 1, 2, 2, A, B, 3>;
@@ -829,14 +848,14 @@ void launch_bf16_hidden_grad(hipStream_t s, const LossArgs &a, int v0, int vn, b
     launch_job<HiddenGrad>(s, a, v0, vn, first, false);
 }
 
-// Few rows make it a matter of writing: blocks of 128 x 128, two a compute unit, one computing while the other's stores drain.
-#ifndef XK
-#define XK 1024
-#endif
+// Blocks of 256 x 256 or, several a compute unit, of 128 x 128 in one step's LDS: while one loads or stores another multiplies. Small ones for few rows, where it is a matter of
+// writing (300 of 500 rows x 151936 x 896: 145 us against 165), and up to more rows where the last large ones would be half empty (3072 of 4096 rows x 896 features: 902 against
+// 976 us; but 6144 of 8192 rows 1956 against 1854, and 2048 rows x 3584 features 2399 against 2287).
 void launch_bf16_weight_grad(hipStream_t s, const LossArgs &a, int v0, int vn)
 {
-    using Bl = Quarter<false, false>;
-    if (a.rows <= XK) launch(block_kernel<WeightGrad, Bl>, dim3(up_div(up_div(a.d_pad, Bl::TM) * up_div(vn, Bl::TN), 8) * 8), 256, Bl::LDS, s, a, v0, vn, 0);
+    using Bl = Block<2, 2, 2, 2, 1, false, false>;
+    const int over = a.d_pad % 256;
+    if (a.rows <= (over && over <= 128 ? 4096 : 1024)) launch(block_kernel<WeightGrad, Bl>, dim3(up_div(up_div(a.d_pad, Bl::TM) * up_div(vn, Bl::TN), 8) * 8), 256, Bl::LDS, s, a, v0, vn, 0);
     else launch(turns_kernel<WeightGrad>, dim3(256), 512, 5 * 256 * BK * 2, s, a, v0, vn, 0);
 }
 
