@@ -569,41 +569,60 @@ template <template <int, int> class Job_, class Bl> __global__ __launch_bounds__
         entries_group<Bl::PL>(a, blockIdx.x * Bl::WAVES + wavefront(), !a.direct && vn == a.vocab);
         return;
     }
-    constexpr int MI = Bl::MI, NI = Bl::NI, STAGES = Bl::STAGES_, COPIES = Bl::TA::COPIES + Bl::TB::COPIES;
+    constexpr int MI = Bl::MI, NI = Bl::NI;
+    constexpr int A_TILES = 3, B_TILES = Bl::PL > 1 ? 2 : 3;     // rings of both operands; B's (the rows, in L2) may be shorter
+    constexpr int UNDER_WAY = A_TILES == B_TILES ? Bl::TA::COPIES + Bl::TB::COPIES : Bl::TA::COPIES;   // copies that may be, when a step's last have landed
+    static_assert(A_TILES * Bl::TA::BYTES + B_TILES * Bl::TB::BYTES <= LDS_OF_RING, "LDS");
     using Job = Job_<Bl::TM, Bl::TN>;
     Job job(a, v0, vn, flag, blockIdx.x - extra);
     const int begin = job.o.first, end = job.o.end, stride = (gridDim.x - extra) >> 3, w = wavefront();
     if (begin >= end) return;
-    const uint32_t lds = lds_start();
+    const uint32_t lds_a = lds_start(), lds_b = lds_a + A_TILES * Bl::TA::BYTES;
     typename Bl::TA ta;
     typename Bl::TB tb;
-    int item = begin, steps, left, ahead = 0;      // of the copies; steps that are on their way or there
-    auto open = [&] {
-        for (steps = 0; item < end; item += stride) {
-            const Place p = job.place(item);
-            if (p.K > 0) { steps = (p.K + BK - 1) / BK; left = p.K; ta.init(p.a, p.lda, p.a_limit); tb.init(p.b, p.ldb, p.b_limit); break; }
+    int item_a = begin, item_b = begin, steps_a, steps_b, left_a, left_b, to_a = 0, to_b = 0;      // of the copies
+    auto open_a = [&] {
+        for (steps_a = 0; item_a < end; item_a += stride) {
+            const Place p = job.place(item_a);
+            if (p.K > 0) { steps_a = (p.K + BK - 1) / BK; left_a = p.K; ta.init(p.a, p.lda, p.a_limit); break; }
         }
     };
-    int to = 0;
-    auto copy = [&] {
-        if (!steps) return;
-        ta.issue(lds + to * Bl::STAGE, left);
-        tb.issue(lds + to * Bl::STAGE + Bl::TA::BYTES, left);
-        to = to + 1 < STAGES ? to + 1 : 0;
-        left -= BK;
-        ++ahead;
-        if (--steps == 0) { item += stride; open(); }
+    auto open_b = [&] {
+        for (steps_b = 0; item_b < end; item_b += stride) {
+            const Place p = job.place(item_b);
+            if (p.K > 0) { steps_b = (p.K + BK - 1) / BK; left_b = p.K; tb.init(p.b, p.ldb, p.b_limit); break; }
+        }
     };
-    open();
+    auto copy_a = [&] {       // whether there was one
+        if (!steps_a) return false;
+        ta.issue(lds_a + to_a * Bl::TA::BYTES, left_a);
+        to_a = to_a + 1 < A_TILES ? to_a + 1 : 0;
+        left_a -= BK;
+        if (--steps_a == 0) { item_a += stride; open_a(); }
+        return true;
+    };
+    auto copy_b = [&] {
+        if (!steps_b) return;
+        tb.issue(lds_b + to_b * Bl::TB::BYTES, left_b);
+        to_b = to_b + 1 < B_TILES ? to_b + 1 : 0;
+        left_b -= BK;
+        if (--steps_b == 0) { item_b += stride; open_b(); }
+    };
+    open_a();
+    open_b();
+    bool full = false;        // the copies that may be under way are
 #pragma unroll
-    for (int q = 0; q < STAGES - 1; ++q) copy();
+    for (int q = 0; q < A_TILES - 1; ++q) {
+        if (q >= A_TILES - B_TILES) copy_b();
+        full = copy_a();
+    }
     Reader<Bl::TM, Job::A_KC, true, MI> ra;
     static_assert(Bl::PL == 1 || Bl::WN == 1, "a row's planes belong to one wavefront");
     Reader<Bl::TN * Bl::PL, Job::B_KC, false, NI * Bl::PL> rb;
     ra.init(w / Bl::WN * MI * 32);
     rb.init(w % Bl::WN * NI * 32);
     f32x16 c[MI][NI];
-    int from = 0;
+    int from_a = 0, from_b = 0;
 #pragma unroll 1
     for (int it = begin; it < end; it += stride) {
         const Place p = job.place(it);
@@ -615,16 +634,17 @@ template <template <int, int> class Job_, class Bl> __global__ __launch_bounds__
                 for (int r = 0; r < 16; ++r) c[i][j][r] = 0.f;
 #pragma unroll 1
         for (int s = (p.K + BK - 1) / BK; s; --s) {
-            // this step has landed, and everyone has read the one before, whose place is the next copy's
-            if (ahead == STAGES - 1) landed_and_barrier<(STAGES - 2) * COPIES>();
+            // this step has landed, and everyone has read the one before, whose places are the next copies'
+            if (full) landed_and_barrier<UNDER_WAY>();
             else landed_and_barrier<0>();
-            copy();
-            const uint32_t at = lds + from * Bl::STAGE;
+            copy_b();
+            full = copy_a();
+            const uint32_t at_a = lds_a + from_a * Bl::TA::BYTES, at_b = lds_b + from_b * Bl::TB::BYTES;
             bf16x8 xa[4][MI], xb[4][NI * Bl::PL];
-            ra.template read<0>(at, xa[0]); rb.template read<0>(at + Bl::TA::BYTES, xb[0]);
-            ra.template read<1>(at, xa[1]); rb.template read<1>(at + Bl::TA::BYTES, xb[1]);
-            ra.template read<2>(at, xa[2]); rb.template read<2>(at + Bl::TA::BYTES, xb[2]);
-            ra.template read<3>(at, xa[3]); rb.template read<3>(at + Bl::TA::BYTES, xb[3]);
+            ra.template read<0>(at_a, xa[0]); rb.template read<0>(at_b, xb[0]);
+            ra.template read<1>(at_a, xa[1]); rb.template read<1>(at_b, xb[1]);
+            ra.template read<2>(at_a, xa[2]); rb.template read<2>(at_b, xb[2]);
+            ra.template read<3>(at_a, xa[3]); rb.template read<3>(at_b, xb[3]);
 #pragma unroll
             for (int q = 0; q < 4; ++q)
 #pragma unroll
@@ -633,8 +653,8 @@ template <template <int, int> class Job_, class Bl> __global__ __launch_bounds__
                     for (int i = 0; i < MI; ++i)
 #pragma unroll
                         for (int j = 0; j < NI; ++j) c[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xa[q][i], xb[q][l * NI + j], c[i][j], 0, 0, 0);
-            --ahead;
-            from = from + 1 < STAGES ? from + 1 : 0;
+            from_a = from_a + 1 < A_TILES ? from_a + 1 : 0;
+            from_b = from_b + 1 < B_TILES ? from_b + 1 : 0;
         }
         job.template done<Bl::WM, Bl::WN, MI, NI>(p, c);
     }
