@@ -5,12 +5,17 @@
 //   softmax, probabilities     m = vocabulary entry, n = row that counts, k = feature: both operands lie with k contiguous
 //   gradient to the rows       m = feature, n = row, k = vocabulary entry of the piece: A is the head, whose k runs from row to row; B = G, k contiguous
 //   gradient to the head       m = feature, n = vocabulary entry, k = row: both operands have k from row to row
-// A workgroup computes a block of 256 (m) x 256, 128 or 64 (n) in steps of 64 k. Both operands of a step are copied to LDS by direct loads, as they lie in
-// memory, one step ahead; an operand with k from row to row is turned where it is read (the transposing LDS read). Within a tile the 16-byte pieces of a row (or
-// the 32-byte pieces, where k runs from row to row) are permuted by the row, on the way in through the lanes' addresses, so that reads meet no bank conflicts.
-// The matrix operands of 16 k are read into registers one such step ahead, across the steps' barriers too.
+// All in steps of 64 k. Both operands of a step are copied to LDS by direct loads, as they lie in memory; an operand with k from row to row is turned where it is read
+// (the transposing LDS read). Within a tile the 16-byte pieces of a line (or the 32-byte pieces, where k runs from row to row) are permuted by the line, on the way in through
+// the lanes' addresses, so that reads meet no bank conflicts. Three schedules:
+//   turns_kernel    blocks of 256 x 256, for more than 128 rows. Bound by the chip's power: 6144 rows x 151936 x 896 (8192, three quarters of them counting) take 1550 us for the
+//                   softmax, 1.08 PFLOP/s with the matrix pipes 57 % busy at 1.83 GHz; 2048 rows x 152064 x 3584 1870 us, 1.19 PFLOP/s (a library product of 8192^3: 1.30, of
+//                   4096 x 151936 x 896: 0.98). The clock falls as the pipes get busier, so that schedules that fill them better gain less than they fill.
+//   stream_kernel   blocks of 256 x 64 or 128, for fewer rows. Bound by the head's bytes: 272 MB in 50 us, 5.4 TB/s, what copies reach here.
+//   block_kernel    blocks of 128 x 128, where there are few blocks, and for the gradient to the head of few rows.
 #include "vocab_loss_epilogues.h"
 #include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 namespace tr {
@@ -46,6 +51,7 @@ template <int N> __device__ __forceinline__ void wait_all_but() { __builtin_amdg
 
 // One operand's tile of T rows of its dimension x 64 k in LDS. KC: k contiguous in memory, LDS [row][64 k]; otherwise [64 k][T]. WAVES share the copying.
 template <int T, bool KC, int WAVES> struct Tile {
+    static constexpr bool K_CONTIGUOUS = KC;
     static constexpr int BYTES = T * BK * 2, COPIES = BYTES / 1024 / WAVES;
     static_assert(BYTES % (1024 * WAVES) == 0, "whole copies");
     static_assert(KC || T >= 128, "eight pieces of 32 bytes a line");
@@ -128,13 +134,18 @@ template <int T, bool KC, bool FEAT, int N> struct Reader {
     }
 };
 
-// One block by WM x WN wavefronts, each MI x NI accumulators; A_KC, B_KC: where the operands have k contiguous. A ring of STAGES steps in LDS, one barrier a
-// step; the matrix operands of 16 k are read one such step ahead. For blocks of few rows, which are bound by reading the head.
-template <int WM_, int WN_, int MI_, int NI_, int STAGES, bool A_KC, bool B_KC, int PLANES = 1> struct Block {
-    static constexpr int WM = WM_, WN = WN_, MI = MI_, NI = NI_, WAVES = WM * WN, TM = WM * MI * 32, TN = WN * NI * 32, STAGES_ = STAGES;
+// WM x WN wavefronts, each MI x NI accumulators; A_KC, B_KC: where the operands have k contiguous. PLANES rows of B for every column.
+template <int WM_, int WN_, int MI_, int NI_, bool A_KC, bool B_KC, int PLANES = 1> struct Shape {
+    static constexpr int WM = WM_, WN = WN_, MI = MI_, NI = NI_, WAVES = WM * WN, TM = WM * MI * 32, TN = WN * NI * 32, PL = PLANES;
     using TA = Tile<TM, A_KC, WAVES>;
-    static constexpr int PL = PLANES;
     using TB = Tile<TN * PL, B_KC, WAVES>;
+};
+
+// One block: STAGES steps in LDS, one barrier a step; the matrix operands of 16 k are read one such step ahead, across the barriers too (STAGES > 1).
+template <int STAGES, class S> struct Block : S {
+    using S::WM; using S::WN; using S::MI; using S::NI; using S::TM; using S::TN;
+    using TA = typename S::TA;
+    using TB = typename S::TB;
     static constexpr int STAGE = TA::BYTES + TB::BYTES, LDS = STAGES * STAGE;
 
     TA a;
@@ -152,8 +163,8 @@ template <int WM_, int WN_, int MI_, int NI_, int STAGES, bool A_KC, bool B_KC, 
 #pragma unroll
                 for (int r = 0; r < 16; ++r) c[i][j][r] = 0.f;
         if (!steps) return;
-        Reader<TM, A_KC, true, MI> ra;
-        Reader<TN, B_KC, false, NI> rb;
+        Reader<TM, TA::K_CONTIGUOUS, true, MI> ra;
+        Reader<TN, TB::K_CONTIGUOUS, false, NI> rb;
         ra.init(wm * MI * 32);
         rb.init(wn * NI * 32);
         int left = K;
@@ -185,40 +196,38 @@ template <int WM_, int WN_, int MI_, int NI_, int STAGES, bool A_KC, bool B_KC, 
                 multiply(1);
             }
         } else {
-        constexpr int COPIES = TA::COPIES + TB::COPIES;
-        int next = 0;
+            constexpr int COPIES = TA::COPIES + TB::COPIES;
 #pragma unroll
-        for (int p = 0; p < STAGES; ++p)
-            if (p < steps) issue(next++);
-        if (steps >= STAGES) landed_and_barrier<(STAGES - 1) * COPIES>();
-        else landed_and_barrier<0>();
-        uint32_t at = lds;
-        ra.template read<0>(at, xa[0]);
-        rb.template read<0>(at + TA::BYTES, xb[0]);
-        int stage = 0;
-#pragma unroll 1
-        for (int s = 0; s < steps; ++s) {
-            ra.template read<1>(at, xa[1]); rb.template read<1>(at + TA::BYTES, xb[1]);
-            multiply(0);
-            ra.template read<2>(at, xa[0]); rb.template read<2>(at + TA::BYTES, xb[0]);
-            multiply(1);
-            ra.template read<3>(at, xa[1]); rb.template read<3>(at + TA::BYTES, xb[1]);
-            multiply(0);
-            // every wavefront holds the step's last operands: its buffer is free, and the next step's has landed
-            if (s + STAGES <= steps) landed_and_barrier<(STAGES - 2) * COPIES>();
+            for (int p = 0; p < STAGES; ++p)
+                if (p < steps) issue(p);
+            if (steps >= STAGES) landed_and_barrier<(STAGES - 1) * COPIES>();
             else landed_and_barrier<0>();
-            if (s + STAGES < steps) issue(stage);
-            stage = stage + 1 < STAGES ? stage + 1 : 0;
-            at = lds + stage * STAGE;
-            if (s + 1 < steps) { ra.template read<0>(at, xa[0]); rb.template read<0>(at + TA::BYTES, xb[0]); }
-            multiply(1);
-        }
+            uint32_t at = lds;
+            ra.template read<0>(at, xa[0]);
+            rb.template read<0>(at + TA::BYTES, xb[0]);
+            int stage = 0;
+#pragma unroll 1
+            for (int s = 0; s < steps; ++s) {
+                ra.template read<1>(at, xa[1]); rb.template read<1>(at + TA::BYTES, xb[1]);
+                multiply(0);
+                ra.template read<2>(at, xa[0]); rb.template read<2>(at + TA::BYTES, xb[0]);
+                multiply(1);
+                ra.template read<3>(at, xa[1]); rb.template read<3>(at + TA::BYTES, xb[1]);
+                multiply(0);
+                // every wavefront holds the step's last operands: its place is free, and the next step's has landed
+                if (s + STAGES <= steps) landed_and_barrier<(STAGES - 2) * COPIES>();
+                else landed_and_barrier<0>();
+                if (s + STAGES < steps) issue(stage);
+                stage = stage + 1 < STAGES ? stage + 1 : 0;
+                at = lds + stage * STAGE;
+                if (s + 1 < steps) { ra.template read<0>(at, xa[0]); rb.template read<0>(at + TA::BYTES, xb[0]); }
+                multiply(1);
+            }
         }
     }
-
 };
 
-// f(accumulator along n, n, first m of a run of 8, the run) of a wavefront's part of a block
+// f(n, first m of a run of 8, the run) of a wavefront's part of a block
 template <int WN, int MI, int NI, class F> __device__ __forceinline__ void each_run(const f32x16 (&c)[MI][NI], F f)
 {
     const int lane = threadIdx.x & 63, w = wavefront(), wm = w / WN, wn = w % WN;
@@ -230,7 +239,7 @@ template <int WN, int MI, int NI, class F> __device__ __forceinline__ void each_
             for (int h = 0; h < 2; ++h) {
                 float v[8];
                 run_of(c[i][j], h, v);
-                f(j, (wn * NI + j) * 32 + (lane & 31), (wm * MI + i) * 32 + 16 * h + 8 * (lane >> 5), v);
+                f((wn * NI + j) * 32 + (lane & 31), (wm * MI + i) * 32 + 16 * h + 8 * (lane >> 5), v);
             }
 }
 
@@ -239,10 +248,7 @@ __device__ __forceinline__ uint32_t lds_start() { return (uint32_t)(uintptr_t)(_
 
 // The order in which blocks are taken. Workgroup b runs on XCD b mod 8, whose workgroups take a contiguous piece of an order that walks groups of GN blocks along n
 // and, in a group, along m: those that run at a time share GN tiles of one operand and a few of the other in the XCD's L2.
-#ifndef XGN
-#define XGN 8
-#endif
-constexpr int GN = XGN;
+constexpr int GN = 8;        // (4 and 6: the same within 2 %)
 struct Order {
     int mb, nb, first, end;      // first of this workgroup (of an XCD's first few), end of its XCD's
     __device__ __forceinline__ Order(int mb_, int nb_, int b) : mb(mb_), nb(nb_)
@@ -459,7 +465,7 @@ template <int TM, int TN> struct WeightGrad {
         if constexpr (TM == 128) {
             // through LDS, which is free by then, so that a row's stores are whole lines of memory: 16-byte pieces, permuted by the row
             uint4 *const tile = reinterpret_cast<uint4 *>(dynamic_lds);
-            each_run<WN>(c, [&](int, int i, int d, float (&x)[8]) {
+            each_run<WN>(c, [&](int i, int d, float (&x)[8]) {
                 tile[i * 16 + ((d >> 3) ^ (i & 15))] = make_uint4(two_bf16(k * x[0], k * x[1]), two_bf16(k * x[2], k * x[3]), two_bf16(k * x[4], k * x[5]), two_bf16(k * x[6], k * x[7]));
             });
             __syncthreads();
@@ -561,25 +567,25 @@ template <int PLANES> __device__ __forceinline__ void entries_group(const LossAr
 
 __global__ __launch_bounds__(64) void bf16_entries_kernel(LossArgs a, bool packed) { entries_group<1>(a, blockIdx.x, packed); }
 
-// Few rows, bound by the head's bytes: one workgroup a compute unit takes block after block, the copies running on across blocks: a ring of steps in LDS, one barrier a
-// step. The first `extra` (a multiple of 8) workgroups take listed entries instead.
-template <template <int, int> class Job_, class Bl> __global__ __launch_bounds__(Bl::WAVES * 64) void stream_kernel(LossArgs a, int v0, int vn, int flag, int extra)
+// Few rows, bound by the head's bytes: one workgroup a compute unit takes block after block, the copies running on across blocks (a workgroup a block: 78 us for one row over
+// 151936 x 896, so 63): rings of both operands' steps in LDS, one barrier a step. The first `extra` (a multiple of 8) workgroups take listed entries instead.
+template <template <int, int> class Job_, class Sh> __global__ __launch_bounds__(Sh::WAVES * 64) void stream_kernel(LossArgs a, int v0, int vn, int flag, int extra)
 {
     if ((int)blockIdx.x < extra) {
-        entries_group<Bl::PL>(a, blockIdx.x * Bl::WAVES + wavefront(), !a.direct && vn == a.vocab);
+        entries_group<Sh::PL>(a, blockIdx.x * Sh::WAVES + wavefront(), !a.direct && vn == a.vocab);
         return;
     }
-    constexpr int MI = Bl::MI, NI = Bl::NI;
-    constexpr int A_TILES = 3, B_TILES = Bl::PL > 1 ? 2 : 3;     // rings of both operands; B's (the rows, in L2) may be shorter
-    constexpr int UNDER_WAY = A_TILES == B_TILES ? Bl::TA::COPIES + Bl::TB::COPIES : Bl::TA::COPIES;   // copies that may be, when a step's last have landed
-    static_assert(A_TILES * Bl::TA::BYTES + B_TILES * Bl::TB::BYTES <= LDS_OF_RING, "LDS");
-    using Job = Job_<Bl::TM, Bl::TN>;
+    constexpr int MI = Sh::MI, NI = Sh::NI;
+    constexpr int A_TILES = 3, B_TILES = Sh::PL > 1 ? 2 : 3;     // rings of both operands; B's (the rows, in L2) may be shorter
+    constexpr int UNDER_WAY = A_TILES == B_TILES ? Sh::TA::COPIES + Sh::TB::COPIES : Sh::TA::COPIES;   // copies that may be, when a step's last have landed
+    static_assert(A_TILES * Sh::TA::BYTES + B_TILES * Sh::TB::BYTES <= LDS_OF_RING, "LDS");
+    using Job = Job_<Sh::TM, Sh::TN>;
     Job job(a, v0, vn, flag, blockIdx.x - extra);
     const int begin = job.o.first, end = job.o.end, stride = (gridDim.x - extra) >> 3, w = wavefront();
     if (begin >= end) return;
-    const uint32_t lds_a = lds_start(), lds_b = lds_a + A_TILES * Bl::TA::BYTES;
-    typename Bl::TA ta;
-    typename Bl::TB tb;
+    const uint32_t lds_a = lds_start(), lds_b = lds_a + A_TILES * Sh::TA::BYTES;
+    typename Sh::TA ta;
+    typename Sh::TB tb;
     int item_a = begin, item_b = begin, steps_a, steps_b, left_a, left_b, to_a = 0, to_b = 0;      // of the copies
     auto open_a = [&] {
         for (steps_a = 0; item_a < end; item_a += stride) {
@@ -595,7 +601,7 @@ template <template <int, int> class Job_, class Bl> __global__ __launch_bounds__
     };
     auto copy_a = [&] {       // whether there was one
         if (!steps_a) return false;
-        ta.issue(lds_a + to_a * Bl::TA::BYTES, left_a);
+        ta.issue(lds_a + to_a * Sh::TA::BYTES, left_a);
         to_a = to_a + 1 < A_TILES ? to_a + 1 : 0;
         left_a -= BK;
         if (--steps_a == 0) { item_a += stride; open_a(); }
@@ -603,7 +609,7 @@ template <template <int, int> class Job_, class Bl> __global__ __launch_bounds__
     };
     auto copy_b = [&] {
         if (!steps_b) return;
-        tb.issue(lds_b + to_b * Bl::TB::BYTES, left_b);
+        tb.issue(lds_b + to_b * Sh::TB::BYTES, left_b);
         to_b = to_b + 1 < B_TILES ? to_b + 1 : 0;
         left_b -= BK;
         if (--steps_b == 0) { item_b += stride; open_b(); }
@@ -616,11 +622,11 @@ template <template <int, int> class Job_, class Bl> __global__ __launch_bounds__
         if (q >= A_TILES - B_TILES) copy_b();
         full = copy_a();
     }
-    Reader<Bl::TM, Job::A_KC, true, MI> ra;
-    static_assert(Bl::PL == 1 || Bl::WN == 1, "a row's planes belong to one wavefront");
-    Reader<Bl::TN * Bl::PL, Job::B_KC, false, NI * Bl::PL> rb;
-    ra.init(w / Bl::WN * MI * 32);
-    rb.init(w % Bl::WN * NI * 32);
+    Reader<Sh::TM, Job::A_KC, true, MI> ra;
+    static_assert(Sh::PL == 1 || Sh::WN == 1, "a row's planes belong to one wavefront");
+    Reader<Sh::TN * Sh::PL, Job::B_KC, false, NI * Sh::PL> rb;
+    ra.init(w / Sh::WN * MI * 32);
+    rb.init(w % Sh::WN * NI * 32);
     f32x16 c[MI][NI];
     int from_a = 0, from_b = 0;
 #pragma unroll 1
@@ -639,8 +645,8 @@ template <template <int, int> class Job_, class Bl> __global__ __launch_bounds__
             else landed_and_barrier<0>();
             copy_b();
             full = copy_a();
-            const uint32_t at_a = lds_a + from_a * Bl::TA::BYTES, at_b = lds_b + from_b * Bl::TB::BYTES;
-            bf16x8 xa[4][MI], xb[4][NI * Bl::PL];
+            const uint32_t at_a = lds_a + from_a * Sh::TA::BYTES, at_b = lds_b + from_b * Sh::TB::BYTES;
+            bf16x8 xa[4][MI], xb[4][NI * Sh::PL];
             ra.template read<0>(at_a, xa[0]); rb.template read<0>(at_b, xb[0]);
             ra.template read<1>(at_a, xa[1]); rb.template read<1>(at_b, xb[1]);
             ra.template read<2>(at_a, xa[2]); rb.template read<2>(at_b, xb[2]);
@@ -648,7 +654,7 @@ template <template <int, int> class Job_, class Bl> __global__ __launch_bounds__
 #pragma unroll
             for (int q = 0; q < 4; ++q)
 #pragma unroll
-                for (int l = 0; l < Bl::PL; ++l)
+                for (int l = 0; l < Sh::PL; ++l)
 #pragma unroll
                     for (int i = 0; i < MI; ++i)
 #pragma unroll
@@ -656,7 +662,7 @@ template <template <int, int> class Job_, class Bl> __global__ __launch_bounds__
             from_a = from_a + 1 < A_TILES ? from_a + 1 : 0;
             from_b = from_b + 1 < B_TILES ? from_b + 1 : 0;
         }
-        job.template done<Bl::WM, Bl::WN, MI, NI>(p, c);
+        job.template done<Sh::WM, Sh::WN, MI, NI>(p, c);
     }
 }
 
@@ -673,7 +679,8 @@ template <template <int, int> class Job_, class Bl> __global__ __launch_bounds__
     job.template done<Bl::WM, Bl::WN, Bl::MI, Bl::NI>(p, bl.c);
 }
 
-// Blocks of 256 x 256, one workgroup a compute unit, block after block, the copies never stopping. 8 wavefronts of 128 x 64; the first four and the last four (one of each
+// Blocks of 256 x 256, one workgroup a compute unit, block after block, the copies never stopping (softmax of 2048 rows x 152064 x 3584, a workgroup a block: 1977 us; in turns:
+// 1881; copies running on: 1835). 8 wavefronts of 128 x 64; the first four and the last four (one of each
 // on every SIMD) take turns: while one reads its matrix operands of 32 k from LDS, the other's matrix instructions run. LDS holds five tiles, a step's two, A's of the next
 // two steps and B's of the next: A (the operand that comes from beyond L2 more often) has two steps of time to arrive, B one.
 template <template <int, int> class Job_> __global__ __launch_bounds__(512) void turns_kernel(LossArgs a, int v0, int vn, int flag)
@@ -811,18 +818,22 @@ __global__ __launch_bounds__(128) void bf16_pack_head_kernel(LossArgs a, int v0)
 
 int up_div(int n, int by) { return (n + by - 1) / by; }
 
-// a kernel's dynamic LDS beyond 64 KiB has to be allowed once per kernel and device; asking again costs nothing that counts beside a launch
-template <class... P, class... A> void launch(void (*kernel)(P...), dim3 grid, int threads, int lds, hipStream_t s, A... args)
+// (A kernel's dynamic LDS beyond 64 KiB has to be allowed once per device.)
+template <auto KERNEL, class... A> void launch(dim3 grid, int threads, int lds, hipStream_t s, A... args)
 {
-    (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    hipLaunchKernelGGL(kernel, grid, dim3(threads), lds, s, args...);
+    static std::atomic<uint64_t> allowed{0};
+    int device = 0;
+    (void)hipGetDevice(&device);
+    const uint64_t bit = device < 64 ? 1ull << device : 0;
+    if (!(allowed.load(std::memory_order_relaxed) & bit) && hipFuncSetAttribute(reinterpret_cast<const void *>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess)
+        allowed.fetch_or(bit, std::memory_order_relaxed);
+    hipLaunchKernelGGL(KERNEL, grid, dim3(threads), lds, s, args...);
 }
 
 int entry_groups(const LossArgs &a) { return (int)(((long long)a.rows * a.entries + 31) / 32); }
 
-template <bool A_KC, bool B_KC> using Quarter = Block<2, 2, 2, 2, 2, A_KC, B_KC>;      // 128 x 128, two a compute unit
-
-// Where blocks of 256 x 256 would leave half of the chip without one, those of 128 x 128 are four times as many (1021 rows x 5003 x 1001: softmax 30 -> XX us).
+// Where blocks of 256 x 256 would leave half of the chip without one, those of 128 x 128 (two a compute unit) are four times as many: 817 of 1021 rows x 5003 x 1001, softmax
+// 30 -> 19 us. With more blocks the large ones are faster: 300 of 500 rows x 151936 x 896 139 us against 141, 2048 x 152064 x 3584 1.9 ms against 2.2.
 int product_rows(const LossArgs &a) { return a.pairs ? std::max(a.rows, 2 * PAIR_ROWS) : a.rows; }     // at most
 bool small_blocks(int m, int n) { return up_div(m, 256) * up_div(n, 256) <= 128; }
 
@@ -830,22 +841,23 @@ bool small_blocks(int m, int n) { return up_div(m, 256) * up_div(n, 256) <= 128;
 template <template <int, int> class Job> void launch_job(hipStream_t s, const LossArgs &a, int v0, int vn, int flag, bool entries)
 {
     constexpr bool A = Job<256, 64>::A_KC, B = Job<256, 64>::B_KC;
-    using Small = Block<8, 1, 1, 2, 3, A, B>;       // 256 x 64
-    using Middle = Block<4, 2, 2, 2, 3, A, B>;      // 256 x 128
     const int extra = entries ? up_div(entry_groups(a), 64) * 8 : 0;
     // a workgroup a compute unit: a few of them take entries only, since the head's bytes come as fast without them
     const dim3 persistent(extra <= 64 ? 256 : 256 + extra);
-    if constexpr (std::is_same_v<Job<256, 64>, Softmax<256, 64>>)
-        if (a.hdt == DT_F32) {
-            using Planes = Block<8, 1, 1, 2, 2, A, B, 3>;
-            launch(stream_kernel<Job, Planes>, persistent, 512, LDS_OF_RING + 8 * 64 * 8, s, a, v0, vn, flag, extra);
-            return;
+    const auto stream = [&](auto shape) {
+        using Sh = decltype(shape);
+        launch<stream_kernel<Job, Sh>>(persistent, 512, LDS_OF_RING + Sh::WM * Sh::TN * (int)sizeof(float2), s, a, v0, vn, flag, extra);
+    };
+    if (a.hdt == DT_F32) {
+        if constexpr (std::is_same_v<Job<256, 64>, Softmax<256, 64>>) stream(Shape<8, 1, 1, 2, A, B, 3>{});
+    } else if (a.n_block == 64) stream(Shape<8, 1, 1, 2, A, B>{});
+    else if (a.n_block == 128) stream(Shape<4, 2, 2, 2, A, B>{});
+    else if (A && small_blocks(vn, product_rows(a))) {
+        if constexpr (A) {
+            using Bl = Block<2, Shape<2, 2, 2, 2, A, B>>;
+            launch<block_kernel<Job, Bl>>(dim3(up_div(up_div(vn, Bl::TM) * up_div(product_rows(a), Bl::TN), 8) * 8), 256, Bl::LDS, s, a, v0, vn, flag);
         }
-    if (a.n_block == 64) launch(stream_kernel<Job, Small>, persistent, 512, LDS_OF_RING + 8 * 64 * 8, s, a, v0, vn, flag, extra);
-    else if (a.n_block == 128) launch(stream_kernel<Job, Middle>, persistent, 512, LDS_OF_RING + 8 * 128 * 8, s, a, v0, vn, flag, extra);
-    else if (Job<256, 64>::A_KC && small_blocks(vn, product_rows(a))) {
-        if constexpr (A) launch(block_kernel<Job, Quarter<A, B>>, dim3(up_div(up_div(vn, 128) * up_div(product_rows(a), 128), 8) * 8), 256, Quarter<A, B>::LDS, s, a, v0, vn, flag);
-    } else launch(turns_kernel<Job>, dim3(256), 512, 5 * 256 * BK * 2, s, a, v0, vn, flag);
+    } else launch<turns_kernel<Job>>(dim3(256), 512, 5 * 256 * BK * 2, s, a, v0, vn, flag);
 }
 
 }  // namespace
@@ -859,7 +871,8 @@ void launch_bf16_entries(hipStream_t s, const LossArgs &a, bool packed) { hipLau
 
 void launch_bf16_softmax(hipStream_t s, const LossArgs &a, int v0, int vn, bool entries) { launch_job<Softmax>(s, a, v0, vn, 0, entries); }
 
-int bf16_softmax_parts(const LossArgs &a) { return a.n_block < 256 ? up_div(a.vocab, BF16_BLOCK) : a.direct || a.piece >= a.vocab ? (small_blocks(a.vocab, product_rows(a)) ? up_div(a.vocab, 128) : up_div(a.vocab, BF16_BLOCK) * 2) : up_div(a.vocab, BF16_BLOCK) * 2; }
+// (blocks of 256 x 256 leave two parts each, those of 128 x 128 one, in the same places)
+int bf16_softmax_parts(const LossArgs &a) { return up_div(a.vocab, a.n_block < 256 ? BF16_BLOCK : BF16_BLOCK / 2); }
 
 void launch_bf16_probabilities(hipStream_t s, const LossArgs &a, int v0, int vn, bool entries) { launch_job<Probabilities>(s, a, v0, vn, 0, entries); }
 
@@ -869,14 +882,14 @@ void launch_bf16_hidden_grad(hipStream_t s, const LossArgs &a, int v0, int vn, b
 }
 
 // Blocks of 256 x 256 or, several a compute unit, of 128 x 128 in one step's LDS: while one loads or stores another multiplies. Small ones for few rows, where it is a matter of
-// writing (300 of 500 rows x 151936 x 896: 145 us against 165), and up to more rows where the last large ones would be half empty (3072 of 4096 rows x 896 features: 902 against
-// 976 us; but 6144 of 8192 rows 1956 against 1854, and 2048 rows x 3584 features 2399 against 2287).
+// writing (300 of 500 rows x 151936 x 896: 145 us against 165), and up to more rows where the last large ones would be half empty (896 features, 4096 rows, three quarters of them
+// counting: 902 against 976 us; but 8192 rows 1956 against 1854, and 2048 rows x 3584 features 2399 against 2287).
 void launch_bf16_weight_grad(hipStream_t s, const LossArgs &a, int v0, int vn)
 {
-    using Bl = Block<2, 2, 2, 2, 1, false, false>;
+    using Bl = Block<1, Shape<2, 2, 2, 2, false, false>>;
     const int over = a.d_pad % 256;
-    if (a.rows <= (over && over <= 128 ? 4096 : 1024)) launch(block_kernel<WeightGrad, Bl>, dim3(up_div(up_div(a.d_pad, Bl::TM) * up_div(vn, Bl::TN), 8) * 8), 256, Bl::LDS, s, a, v0, vn, 0);
-    else launch(turns_kernel<WeightGrad>, dim3(256), 512, 5 * 256 * BK * 2, s, a, v0, vn, 0);
+    if (a.rows <= (over && over <= 128 ? 4096 : 1024)) launch<block_kernel<WeightGrad, Bl>>(dim3(up_div(up_div(a.d_pad, Bl::TM) * up_div(vn, Bl::TN), 8) * 8), 256, Bl::LDS, s, a, v0, vn, 0);
+    else launch<turns_kernel<WeightGrad>>(dim3(256), 512, 5 * 256 * BK * 2, s, a, v0, vn, 0);
 }
 
 }  // namespace tr
