@@ -23,26 +23,25 @@ bool config_ok(const tr_loss_config *c)
 // Where everything lies in the workspace, for a configuration; the sizes of a call's own launches follow from its rows, never beyond these.
 struct Plan {
     int n_pad, d_pad, piece, g_ld, splits;
-    int planes_ld, planes_piece;   // d_pad and piece of the softmax on rows in planes
+    int packed;        // columns of a piece whose head is packed
     size_t head, idx, state, part, value, G, acc, hp, wp, total;
 };
 
 bool is_bf16(const tr_loss_config *c) { return c->hidden_dtype == TR_BF16; }                                    // all products run on bf16 matrix instructions
 bool in_planes(const tr_loss_config *c) { return c->hidden_dtype == TR_F32 && c->weight_dtype == TR_BF16; }   // those of the softmax do, on rows in three planes
 
-// G stays at 512 MB or less, but a piece has 2048 columns at least. (6144 of 8192 rows x 151936 x 896, all products of the gradients, pieces of 128 / 256 / 512 / 1024 MB:
-// 7.1 / 5.9 / 5.8 / 5.7 ms.)
-// Splits of the sums of the gradient to the hidden rows: as many as give every compute unit a block.
+// G stays at 512 MB or less, but a piece has 2048 columns at least (8192 rows x 151936 x 896, three quarters of the rows counting, all products of the gradients, pieces of
+// 128 / 256 / 512 / 1024 MB: 7.1 / 5.9 / 5.8 / 5.7 ms); where the head is packed, that stays at 128 MB or less.
 Plan plan_of(const tr_loss_config *c)
 {
     Plan p{};
     const bool half = is_bf16(c);
     const int block = half ? BF16_BLOCK : F32_BLOCK;
-    const size_t g_size = half ? 2 : 4;
+    const size_t g_size = half ? 2 : 4, whole = up(c->vocab, BF16_BLOCK), steps = up(c->dim, 64);
     p.n_pad = (int)up(c->max_rows, BF16_BLOCK);
-    p.d_pad = (int)up(c->dim, half ? 64 : F32_BLOCK);
-    const size_t vocab = up(c->vocab, block);
-    p.piece = (int)std::min(vocab, std::max<size_t>(2048, (512u << 20) / g_size / p.n_pad / block * block));
+    p.d_pad = (int)steps;
+    p.piece = (int)std::min(whole, std::max<size_t>(2048, (512u << 20) / g_size / p.n_pad / BF16_BLOCK * BF16_BLOCK));
+    p.packed = (int)std::min(whole, std::max<size_t>(2048, (128u << 20) / 2 / steps / BF16_BLOCK * BF16_BLOCK));
     p.g_ld = p.piece + 128;
     const int mb = (int)(up(p.d_pad, block) / block), few = std::max(1, p.piece / 256);
     p.splits = half ? std::min(few, std::max(1, 32 / mb) * 8) : std::max(1, std::min(1024 / (mb * (p.n_pad / F32_BLOCK)), few));
@@ -51,21 +50,16 @@ Plan plan_of(const tr_loss_config *c)
     p.head = take(sizeof(LossHead));
     p.idx = take((size_t)p.n_pad * 4);
     p.state = take(c->max_rows);
-    p.part = take(vocab / block * 2 * p.n_pad * sizeof(float2));   // two wavefronts' parts a block of 256 rows
+    p.part = take((half ? whole / BF16_BLOCK * 2 : in_planes(c) ? whole / BF16_BLOCK : whole / F32_BLOCK * 2) * p.n_pad * sizeof(float2));
     p.value = take((size_t)p.n_pad * c->max_entries * 4);
     p.G = take((size_t)p.n_pad * p.g_ld * g_size);
     // bf16, rows of all splits (bf16_splits): blocks * splits <= 256 where there are fewer than 32 blocks, 8 splits up to 1024 blocks, one from there on
     const size_t sums = (size_t)p.splits * p.n_pad, most = std::max({(size_t)std::min(p.splits, 8) * std::min<size_t>(p.n_pad, 1024 / mb * BF16_BLOCK + BF16_BLOCK),
                                                                      (size_t)(256 / mb + 1) * BF16_BLOCK, (size_t)p.n_pad});
     p.acc = take((half ? std::min(sums, most) : sums) * p.d_pad * 4);
-    p.planes_ld = (int)up(c->dim, 64);
-    p.planes_piece = (int)std::min(up(c->vocab, BF16_BLOCK), std::max<size_t>(2048, p.piece / BF16_BLOCK * BF16_BLOCK));
-    if (half) {
-        p.hp = take((size_t)p.n_pad * p.d_pad * 2);
-        p.wp = take((size_t)p.piece * p.d_pad * 2);
-    } else if (in_planes(c)) {
-        p.hp = take(up(p.n_pad, BF16_BLOCK) * 3 * p.planes_ld * 2);
-        p.wp = take((size_t)p.planes_piece * p.planes_ld * 2);
+    if (half || in_planes(c)) {
+        p.hp = take((size_t)p.n_pad * (half ? 1 : 3) * steps * 2);
+        p.wp = take((size_t)p.packed * steps * 2);
     }
     p.total = at;
     return p;
@@ -96,15 +90,13 @@ int arguments(const tr_loss_config *c, const tr_loss_rows *in, void *ws, size_t 
     a.value = (float *)(b + p.value); a.G = b + p.G; a.acc = (float *)(b + p.acc);
     a.n_pad = a.part_ld = p.n_pad; a.d_pad = p.d_pad; a.piece = p.piece; a.g_ld = p.g_ld; a.splits = p.splits;
     a.direct = a.dim % 64 == 0 && a.ws % 8 == 0 && a.ws < (1 << 22) && (reinterpret_cast<uintptr_t>(a.weight) & 15) == 0;
-    if (is_bf16(c)) {
+    if (is_bf16(c) || (in_planes(c) && !gradient)) {
         a.hp = b + p.hp; a.wp = b + p.wp;
         a.pairs = gradient;
         const int rows = gradient && a.rows <= PAIR_ROWS ? 2 * a.rows : a.rows;
-        a.n_block = rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
-        if (a.n_block < 256) a.part_ld = a.n_block;
-    } else if (in_planes(c) && !gradient) {
-        a.hp = b + p.hp; a.wp = b + p.wp;
-        a.n_block = 64; a.d_pad = p.planes_ld; a.piece = p.planes_piece;
+        a.n_block = rows <= 64 || in_planes(c) ? 64 : rows <= 128 ? 128 : 256;
+        if (a.n_block < 256 && !in_planes(c)) a.part_ld = a.n_block;
+        if (!a.direct) a.piece = std::min(p.piece, p.packed);
     }
     return TR_OK;
 }

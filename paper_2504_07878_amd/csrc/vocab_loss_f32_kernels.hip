@@ -1,9 +1,10 @@
-// Products of the losses over the vocabulary on 32-bit matrix instructions: operands of either storage type, any stride and alignment, widened where they
-// are read; used wherever an operand is fp32.
+// Products of the losses over the vocabulary on 32-bit matrix instructions: fp32 rows and a head of either type, any stride and alignment, widened where they
+// are read. (The softmax of fp32 rows over a bf16 head has faster ones, on three bf16 rows for each.)
 //
 // A workgroup of 4 wavefronts (2 x 2, an accumulator of 32 x 32 each) computes a 64 x 64 block of C[n][m] = sum_k A[m][k] B[n][k] in steps of 32 k: both operands
 // go through registers into LDS as [row][k], one step ahead, in two buffers. A lane reads four k at a time: k = 8 g + 4 (lane / 32) + j for the j-th product of group g.
-// Small blocks, since models of this type are small: they have to fill the chip. Three products:
+// Small blocks, since models of this type are small: they have to fill the chip. Bound by latency there: 133 of 190 rows x 4096 x 256 take 21 us for the softmax, 13 and 11 us for
+// the gradients (blocks of 128 x 128, 16 k a step, in one buffer: 52, 40 and 33). Three products:
 //   softmax, probabilities: m = vocabulary entry, n = row that counts, k = feature
 //   gradient to the hidden rows: m = feature, n = row, k = vocabulary entry of the piece; summed over the pieces in `acc`, one sum per split of k
 //   gradient to the head: m = feature, n = vocabulary entry, k = row
@@ -126,18 +127,18 @@ template <class F> __device__ __forceinline__ void each_run(const f32x16 (&c)[1]
 
 // Products of listed entries: a wavefront takes 32 of them, its rows of the head against its hidden rows, of which only the diagonal is kept (the matrix unit
 // is all but idle in a product this small, and it gives the bits that the same pair has in a block: the same instructions over the same steps of k).
-template <class HT, class WT> __device__ __forceinline__ void entries_group(const LossArgs &a, int group)
+template <class WT> __device__ __forceinline__ void entries_group(const LossArgs &a, int group)
 {
     const int lane = threadIdx.x & 63, e = group * 32 + (lane & 31), hf = lane >> 5, count = a.head->count;
     if ((long long)group * 32 >= (long long)count * a.entries) return;
     const int i = e / a.entries, j = e - i * a.entries;
-    const HT *h = nullptr;
+    const float *h = nullptr;
     const WT *w = nullptr;
     if (i < count) {
         const int r = a.idx[i], id = a.ids[(long long)r * a.entries + j];
-        if (id >= 0 && id < a.vocab) { h = (const HT *)a.hidden + r * a.hs; w = (const WT *)a.weight + id * a.ws; }
+        if (id >= 0 && id < a.vocab) { h = (const float *)a.hidden + r * a.hs; w = (const WT *)a.weight + id * a.ws; }
     }
-    const bool hw = ((reinterpret_cast<uintptr_t>(a.hidden) | (uintptr_t)(a.hs * sizeof(HT))) & 15) == 0, ww = ((reinterpret_cast<uintptr_t>(a.weight) | (uintptr_t)(a.ws * sizeof(WT))) & 15) == 0;
+    const bool hw = ((reinterpret_cast<uintptr_t>(a.hidden) | (uintptr_t)(a.hs * 4)) & 15) == 0, ww = ((reinterpret_cast<uintptr_t>(a.weight) | (uintptr_t)(a.ws * sizeof(WT))) & 15) == 0;
     f32x16 c;
 #pragma unroll
     for (int r = 0; r < 16; ++r) c[r] = 0.f;
@@ -162,33 +163,33 @@ template <class HT, class WT> __device__ __forceinline__ void entries_group(cons
 }
 
 // The first `extra` workgroups along x, of the first row of them, take listed entries.
-template <class HT, class WT> __global__ __launch_bounds__(256) void f32_softmax_kernel(LossArgs a, int extra)
+__global__ __launch_bounds__(256) void f32_softmax_kernel(LossArgs a, int extra)
 {
     __shared__ Tiles sm;
     const int m0 = ((int)blockIdx.x - extra) * F32_BLOCK, n0 = blockIdx.y * F32_BLOCK, count = a.head->count, w = threadIdx.x >> 6;
     if (m0 < 0) {
-        if (n0 == 0) entries_group<HT, WT>(a, blockIdx.x * 4 + w);
+        if (n0 == 0) entries_group<float>(a, blockIdx.x * 4 + w);
         return;
     }
     if (n0 >= count) return;
-    const Lines<WT> A(a.weight, a.ws, a.vocab, a.dim);
-    const ListedLines<HT> B{Lines<HT>(a.hidden, a.hs, count, a.dim), a.idx};
+    const Lines<float> A(a.weight, a.ws, a.vocab, a.dim);
+    const ListedLines<float> B{Lines<float>(a.hidden, a.hs, count, a.dim), a.idx};
     f32x16 c[1][1];
     products<true, true>(A, B, m0, n0, 0, a.dim, sm, c);
     softmax_part(c, a.part + ((size_t)(m0 / F32_BLOCK) * 2 + (w >> 1)) * a.part_ld + n0 + (w & 1) * 32, m0 + (w >> 1) * 32, a.vocab, LOG2E / a.temperature);
 }
 
-template <class HT, class WT> __global__ __launch_bounds__(256) void f32_probabilities_kernel(LossArgs a, int v0, int vn, int extra)
+template <class WT> __global__ __launch_bounds__(256) void f32_probabilities_kernel(LossArgs a, int v0, int vn, int extra)
 {
     __shared__ Tiles sm;
     const int m0 = ((int)blockIdx.x - extra) * F32_BLOCK, n0 = blockIdx.y * F32_BLOCK, count = a.head->count;
     if (m0 < 0) {
-        if (n0 == 0) entries_group<HT, WT>(a, blockIdx.x * 4 + (threadIdx.x >> 6));
+        if (n0 == 0) entries_group<WT>(a, blockIdx.x * 4 + (threadIdx.x >> 6));
         return;
     }
     if (n0 >= count) return;
     const Lines<WT> A((const WT *)a.weight + (long long)v0 * a.ws, a.ws, vn, a.dim);
-    const ListedLines<HT> B{Lines<HT>(a.hidden, a.hs, count, a.dim), a.idx};
+    const ListedLines<float> B{Lines<float>(a.hidden, a.hs, count, a.dim), a.idx};
     f32x16 c[1][1];
     products<true, true>(A, B, m0, n0, 0, a.dim, sm, c);
     const float k = 1.0f / a.temperature;
@@ -224,11 +225,11 @@ template <class WT> __global__ __launch_bounds__(256) void f32_hidden_grad_kerne
     });
 }
 
-template <class HT, class WT> __global__ __launch_bounds__(256) void f32_weight_grad_kernel(LossArgs a, int v0, int vn)
+template <class WT> __global__ __launch_bounds__(256) void f32_weight_grad_kernel(LossArgs a, int v0, int vn)
 {
     __shared__ Tiles sm;
     const int m0 = blockIdx.x * F32_BLOCK, n0 = blockIdx.y * F32_BLOCK, count = a.head->count;
-    const ListedLines<HT> A{Lines<HT>(a.hidden, a.hs, count, a.dim), a.idx};
+    const ListedLines<float> A{Lines<float>(a.hidden, a.hs, count, a.dim), a.idx};
     const Lines<float> B(a.G, a.g_ld, count, vn);
     f32x16 c[1][1];
     products<false, false>(A, B, m0, n0, 0, count, sm, c);
@@ -251,45 +252,41 @@ template <class HT, class WT> __global__ __launch_bounds__(256) void f32_weight_
 int blocks(int n) { return (n + F32_BLOCK - 1) / F32_BLOCK; }
 int entry_blocks(const LossArgs &a) { return (int)(((long long)a.rows * a.entries + 127) / 128); }
 
-template <class Go> void by_types(const LossArgs &a, Go go)
+template <class Go> void by_head(const LossArgs &a, Go go)
 {
-    if (a.wdt == DT_BF16) go(float{}, bf16_t{});
-    else go(float{}, float{});
+    if (a.wdt == DT_BF16) go(bf16_t{});
+    else go(float{});
 }
 
 }  // namespace
 
 void launch_f32_softmax(hipStream_t s, const LossArgs &a)
 {
-    by_types(a, [&](auto ht, auto wt) {
-        const int extra = entry_blocks(a);
-        hipLaunchKernelGGL((f32_softmax_kernel<decltype(ht), decltype(wt)>), dim3(extra + blocks(a.vocab), blocks(a.rows)), dim3(256), 0, s, a, extra);
-    });
+    const int extra = entry_blocks(a);
+    hipLaunchKernelGGL(f32_softmax_kernel, dim3(extra + blocks(a.vocab), blocks(a.rows)), dim3(256), 0, s, a, extra);
 }
 
 int f32_softmax_parts(const LossArgs &a) { return blocks(a.vocab) * 2; }
 
 void launch_f32_probabilities(hipStream_t s, const LossArgs &a, int v0, int vn)
 {
-    by_types(a, [&](auto ht, auto wt) {
+    by_head(a, [&](auto wt) {
         const int extra = v0 == 0 ? entry_blocks(a) : 0;
-        hipLaunchKernelGGL((f32_probabilities_kernel<decltype(ht), decltype(wt)>), dim3(extra + blocks(vn), blocks(a.rows)), dim3(256), 0, s, a, v0, vn, extra);
+        hipLaunchKernelGGL((f32_probabilities_kernel<decltype(wt)>), dim3(extra + blocks(vn), blocks(a.rows)), dim3(256), 0, s, a, v0, vn, extra);
     });
 }
 
 void launch_f32_hidden_grad(hipStream_t s, const LossArgs &a, int v0, int vn, bool first)
 {
-    const int per = ((vn + a.splits - 1) / a.splits + BK - 1) / BK * BK;   // whole steps
-    const dim3 grid(blocks(a.dim), blocks(a.rows), a.splits);
-    if (a.wdt == DT_BF16) hipLaunchKernelGGL((f32_hidden_grad_kernel<bf16_t>), grid, dim3(256), 0, s, a, v0, vn, per, first);
-    else hipLaunchKernelGGL((f32_hidden_grad_kernel<float>), grid, dim3(256), 0, s, a, v0, vn, per, first);
+    by_head(a, [&](auto wt) {
+        const int per = ((vn + a.splits - 1) / a.splits + BK - 1) / BK * BK;   // whole steps
+        hipLaunchKernelGGL((f32_hidden_grad_kernel<decltype(wt)>), dim3(blocks(a.dim), blocks(a.rows), a.splits), dim3(256), 0, s, a, v0, vn, per, (int)first);
+    });
 }
 
 void launch_f32_weight_grad(hipStream_t s, const LossArgs &a, int v0, int vn)
 {
-    by_types(a, [&](auto ht, auto wt) {
-        hipLaunchKernelGGL((f32_weight_grad_kernel<decltype(ht), decltype(wt)>), dim3(blocks(a.dim), blocks(vn)), dim3(256), 0, s, a, v0, vn);
-    });
+    by_head(a, [&](auto wt) { hipLaunchKernelGGL((f32_weight_grad_kernel<decltype(wt)>), dim3(blocks(a.dim), blocks(vn)), dim3(256), 0, s, a, v0, vn); });
 }
 
 }  // namespace tr
