@@ -8,9 +8,9 @@
 // All in steps of 64 k. Both operands of a step are copied to LDS by direct loads, as they lie in memory; an operand with k from row to row is turned where it is read
 // (the transposing LDS read). Within a tile the 16-byte pieces of a line (or the 32-byte pieces, where k runs from row to row) are permuted by the line, on the way in through
 // the lanes' addresses, so that reads meet no bank conflicts. Three schedules:
-//   turns_kernel    blocks of 256 x 256, for more than 128 rows. Bound by the chip's power: 6144 rows x 151936 x 896 (8192, three quarters of them counting) take 1550 us for the
-//                   softmax, 1.08 PFLOP/s with the matrix pipes 57 % busy at 1.83 GHz; 2048 rows x 152064 x 3584 1870 us, 1.19 PFLOP/s (a library product of 8192^3: 1.30, of
-//                   4096 x 151936 x 896: 0.98). The clock falls as the pipes get busier, so that schedules that fill them better gain less than they fill.
+//   turns_kernel    blocks of 256 x 256, for more than 128 rows. Bound by the chip's power: 6144 rows x 151936 x 896 (8192, three quarters of them counting) take 1530 us for the
+//                   softmax, 1.09 PFLOP/s; 2048 rows x 152064 x 3584 1780 us, 1.25 PFLOP/s (a library product of 8192^3: 1.30, of 4096 x 151936 x 896: 0.98). The clock falls
+//                   as the pipes get busier, so that schedules that fill them better gain less than they fill.
 //   stream_kernel   blocks of 256 x 64 or 128, for fewer rows. Bound by the head's bytes: 272 MB in 50 us, 5.4 TB/s, what copies reach here.
 //   block_kernel    blocks of 128 x 128, where there are few blocks, and for the gradient to the head of few rows.
 #include "vocab_loss_epilogues.h"
@@ -24,6 +24,7 @@ namespace {
 
 constexpr int BK = 64;                 // k per step
 typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
 
 __device__ __forceinline__ int wavefront() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 
@@ -40,17 +41,23 @@ template <int N> __device__ __forceinline__ void landed_and_barrier()
     asm volatile("" ::: "memory");
 }
 
+// Matrix instructions of 16 x 16 x 32: in registers alone they sustain 1.97 PFLOP/s on random data where those of 32 x 32 x 16 sustain 1.74 (the chip's power bounds both), since
+// they move half as much of the accumulators (softmax of 2048 rows x 152064 x 3584: 1867 -> 1780 us). An operand is 16 rows x 32 k, lane l holding k = 8 (l / 16) .. + 7 of row l mod 16; lane l of the result holds rows 4 (l / 16) .. + 3 of
+// column l mod 16. Where m lies along memory in the result and k contiguous in A, A's rows are taken in pairs of operands over 32 rows, row 4 a + e of the first being 8 a + e and of
+// the second 8 a + 4 + e, so that a lane's results of a pair are 8 in a run.
+
 // How the pieces of a line of a tile are permuted (exclusive or). LDS has 64 banks of 4 bytes: the 16 lanes that a 16-byte read serves at a time have to meet 16
-// different pieces of 256 bytes, two lines of 64 k; the 32 lanes of an 8-byte read 8 different pieces of 32 bytes, from 4 lines of 16 columns twice. (Keyed by the
+// different pieces of 256 bytes, two lines of 64 k; the 32 lanes of an 8-byte read 8 different pieces of 32 bytes, from 8 lines of one column. (Keyed by the
 // lowest bits of the line instead, half of all LDS cycles were conflicts.)
-__device__ __forceinline__ int row_key(int row) { return (row >> 1) & 7; }
+template <bool PAIRED> __device__ __forceinline__ int row_key(int row) { return PAIRED ? ((row >> 1) & 1) | ((row >> 2) & 6) : (row >> 1) & 7; }
 __device__ __forceinline__ int k_key(int k) { return ((k & 3) << 1) ^ ((k >> 3) & 1); }
 
 __device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14)); }   // lgkmcnt 0
 template <int N> __device__ __forceinline__ void wait_all_but() { __builtin_amdgcn_s_waitcnt(N | (7 << 4) | (0 << 8)); }   // vmcnt N < 16 and lgkmcnt 0
 
-// One operand's tile of T rows of its dimension x 64 k in LDS. KC: k contiguous in memory, LDS [row][64 k]; otherwise [64 k][T]. WAVES share the copying.
-template <int T, bool KC, int WAVES> struct Tile {
+// One operand's tile of T rows of its dimension x 64 k in LDS. KC: k contiguous in memory, LDS [row][64 k]; otherwise [64 k][T]. PAIRED: rows are read
+// in pairs of operands. WAVES share the copying.
+template <int T, bool KC, bool PAIRED, int WAVES> struct Tile {
     static constexpr bool K_CONTIGUOUS = KC;
     static constexpr int BYTES = T * BK * 2, COPIES = BYTES / 1024 / WAVES;
     static_assert(BYTES % (1024 * WAVES) == 0, "whole copies");
@@ -71,7 +78,7 @@ template <int T, bool KC, int WAVES> struct Tile {
         for (int q = 0; q < COPIES; ++q) {
             const int g = w * COPIES + q;
             if (KC) {
-                const int row = g * 8 + (lane >> 3), piece = (lane & 7) ^ row_key(row);
+                const int row = g * 8 + (lane >> 3), piece = (lane & 7) ^ row_key<PAIRED>(row);
                 off[q] = (uint32_t)min(row, limit - 1) * ld + piece * 16;
                 krow[q] = 0;
             } else {
@@ -95,27 +102,24 @@ template <int T, bool KC, int WAVES> struct Tile {
     }
 };
 
-// Reads matrix operands from a tile: N of them, of 32 rows each, from row r0 on; step kk of 16 k. FEAT: rows in the order of the matrix instruction's output
-// runs (tile_feature).
-template <int T, bool KC, bool FEAT, int N> struct Reader {
-    uint32_t at[KC ? BK / 16 : 2 * N];
+// Reads matrix operands from a tile: N of them, of 16 rows each, from row r0 on (a multiple of 16 N); step KK of 32 k.
+template <int T, bool KC, bool PAIRED, int N> struct Reader {
+    uint32_t at[2];
     __device__ __forceinline__ void init(int r0)
     {
-        const int lane = threadIdx.x & 63, hf = lane >> 5;
+        const int lane = threadIdx.x & 63, in = lane & 15, g = lane >> 4;
         if (KC) {
-            const int in = lane & 31, row = r0 + (FEAT ? tile_feature(in) : in), key = row_key(row);
+            const int row = r0 + (PAIRED ? 8 * (in >> 2) + (in & 3) : in);
 #pragma unroll
-            for (int kk = 0; kk < BK / 16; ++kk) at[kk] = row * (BK * 2) + (((kk * 2 + hf) ^ key) << 4);
+            for (int kk = 0; kk < 2; ++kk) at[kk] = row * (BK * 2) + (((kk * 4 + g) ^ row_key<PAIRED>(row)) << 4);
         } else {
             // groups of 16 lanes turn 4 (k) x 16 elements; lane 4 r + c brings k = r, columns of quad c, and gets its own column's four k
-            const int g = (lane >> 4) & 1, r = (lane >> 2) & 3, c = lane & 3, quad = FEAT ? 2 * (c & 1) + (c >> 1) : c;
+            const int r = in >> 2, c = in & 3;
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int n = 0; n < N; ++n) {
-                    const int k = 4 * t + r, piece = (r0 >> 4) + 2 * n + g;
-                    at[t * N + n] = (8 * hf + k) * (T * 2) + ((piece ^ k_key(8 * hf + k)) << 5) + quad * 8;
-                }
+            for (int t = 0; t < 2; ++t) {
+                const int k = 8 * g + 4 * t + r;
+                at[t] = k * (T * 2) + (((r0 >> 4) ^ k_key(k)) << 5) + c * 8;
+            }
         }
     }
     template <int KK> __device__ __forceinline__ void read(uint32_t lds, bf16x8 (&o)[N]) const
@@ -123,50 +127,67 @@ template <int T, bool KC, bool FEAT, int N> struct Reader {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             if constexpr (KC) {
-                o[n] = *reinterpret_cast<const __attribute__((address_space(3))) bf16x8 *>(lds + at[KK] + n * 32 * BK * 2);
+                const int rows = PAIRED ? (n >> 1) * 32 + (n & 1) * 4 : n * 16;      // (the key is the same there)
+                o[n] = *reinterpret_cast<const __attribute__((address_space(3))) bf16x8 *>(lds + at[KK] + rows * BK * 2);
             } else {
                 typedef __attribute__((address_space(3))) s16x4 *lp;
-                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lp>(lds + at[n] + KK * 16 * T * 2));
-                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lp>(lds + at[N + n] + KK * 16 * T * 2));
+                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lp>(lds + (at[0] ^ (n << 5)) + KK * 32 * T * 2));
+                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lp>(lds + (at[1] ^ (n << 5)) + KK * 32 * T * 2));
                 o[n] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
             }
         }
     }
 };
 
+template <int MI, int NI> __device__ __forceinline__ void clear(f32x4 (&c)[MI][NI])
+{
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j) c[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+}
+
+// c += a b, `PLANES` operands of b for every column in turn
+template <int MI, int NI, int PLANES> __device__ __forceinline__ void multiply(f32x4 (&c)[MI][NI], const bf16x8 (&a)[MI], const bf16x8 (&b)[NI * PLANES])
+{
+#pragma unroll
+    for (int l = 0; l < PLANES; ++l)
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j) c[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[l * NI + j], c[i][j], 0, 0, 0);
+}
+
 // WM x WN wavefronts, each MI x NI accumulators; A_KC, B_KC: where the operands have k contiguous. PLANES rows of B for every column.
 template <int WM_, int WN_, int MI_, int NI_, bool A_KC, bool B_KC, int PLANES = 1> struct Shape {
-    static constexpr int WM = WM_, WN = WN_, MI = MI_, NI = NI_, WAVES = WM * WN, TM = WM * MI * 32, TN = WN * NI * 32, PL = PLANES;
-    using TA = Tile<TM, A_KC, WAVES>;
-    using TB = Tile<TN * PL, B_KC, WAVES>;
+    static constexpr int WM = WM_, WN = WN_, MI = MI_, NI = NI_, WAVES = WM * WN, TM = WM * MI * 16, TN = WN * NI * 16, PL = PLANES;
+    using TA = Tile<TM, A_KC, A_KC, WAVES>;
+    using TB = Tile<TN * PL, B_KC, false, WAVES>;
+    using RA = Reader<TM, A_KC, A_KC, MI>;
+    using RB = Reader<TN * PL, B_KC, false, NI * PL>;
 };
 
-// One block: STAGES steps in LDS, one barrier a step; the matrix operands of 16 k are read one such step ahead, across the barriers too (STAGES > 1).
+// One block: STAGES steps in LDS, one barrier a step; the matrix operands of 32 k are read one such step ahead, across the barriers too (STAGES > 1).
 template <int STAGES, class S> struct Block : S {
     using S::WM; using S::WN; using S::MI; using S::NI; using S::TM; using S::TN;
     using TA = typename S::TA;
     using TB = typename S::TB;
-    static constexpr int STAGE = TA::BYTES + TB::BYTES, LDS = STAGES * STAGE;
+    static constexpr int STAGE = TA::BYTES + TB::BYTES, LDS = STAGES * STAGE, AT_ONCE = STAGES == 1 ? 4 : 3;   // (workgroups a compute unit)
 
     TA a;
     TB b;
-    f32x16 c[MI][NI];
+    f32x4 c[MI][NI];
 
     // K: k in all; whole steps are copied, and what lies past K in the last has to be zero in one operand and finite in the other
     __device__ __forceinline__ void run(uint32_t lds, int K)
     {
         const int w = wavefront(), wm = w / WN, wn = w % WN, steps = (K + BK - 1) / BK;
-#pragma unroll
-        for (int i = 0; i < MI; ++i)
-#pragma unroll
-            for (int j = 0; j < NI; ++j)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) c[i][j][r] = 0.f;
+        clear(c);
         if (!steps) return;
-        Reader<TM, TA::K_CONTIGUOUS, true, MI> ra;
-        Reader<TN, TB::K_CONTIGUOUS, false, NI> rb;
-        ra.init(wm * MI * 32);
-        rb.init(wn * NI * 32);
+        typename S::RA ra;
+        typename S::RB rb;
+        ra.init(wm * MI * 16);
+        rb.init(wn * NI * 16);
         int left = K;
         auto issue = [&](int stage) {
             a.issue(lds + stage * STAGE, left);
@@ -174,26 +195,16 @@ template <int STAGES, class S> struct Block : S {
             left -= BK;
         };
         bf16x8 xa[2][MI], xb[2][NI];
-        auto multiply = [&](int p) {
-#pragma unroll
-            for (int i = 0; i < MI; ++i)
-#pragma unroll
-                for (int j = 0; j < NI; ++j) c[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xa[p][i], xb[p][j], c[i][j], 0, 0, 0);
-        };
         if constexpr (STAGES == 1) {
 #pragma unroll 1
             for (int s = 0; s < steps; ++s) {
                 issue(0);
                 landed_and_barrier<0>();
                 ra.template read<0>(lds, xa[0]); rb.template read<0>(lds + TA::BYTES, xb[0]);
-                ra.template read<1>(lds, xa[1]); rb.template read<1>(lds + TA::BYTES, xb[1]);
-                multiply(0);
-                ra.template read<2>(lds, xa[0]); rb.template read<2>(lds + TA::BYTES, xb[0]);
-                multiply(1);
-                ra.template read<3>(lds, xa[1]); rb.template read<3>(lds + TA::BYTES, xb[1]);
-                multiply(0);
+                multiply<MI, NI, 1>(c, xa[0], xb[0]);
+                ra.template read<1>(lds, xa[0]); rb.template read<1>(lds + TA::BYTES, xb[0]);
                 landed_and_barrier<0>();
-                multiply(1);
+                multiply<MI, NI, 1>(c, xa[0], xb[0]);
             }
         } else {
             constexpr int COPIES = TA::COPIES + TB::COPIES;
@@ -209,11 +220,7 @@ template <int STAGES, class S> struct Block : S {
 #pragma unroll 1
             for (int s = 0; s < steps; ++s) {
                 ra.template read<1>(at, xa[1]); rb.template read<1>(at + TA::BYTES, xb[1]);
-                multiply(0);
-                ra.template read<2>(at, xa[0]); rb.template read<2>(at + TA::BYTES, xb[0]);
-                multiply(1);
-                ra.template read<3>(at, xa[1]); rb.template read<3>(at + TA::BYTES, xb[1]);
-                multiply(0);
+                multiply<MI, NI, 1>(c, xa[0], xb[0]);
                 // every wavefront holds the step's last operands: its place is free, and the next step's has landed
                 if (s + STAGES <= steps) landed_and_barrier<(STAGES - 2) * COPIES>();
                 else landed_and_barrier<0>();
@@ -221,27 +228,11 @@ template <int STAGES, class S> struct Block : S {
                 stage = stage + 1 < STAGES ? stage + 1 : 0;
                 at = lds + stage * STAGE;
                 if (s + 1 < steps) { ra.template read<0>(at, xa[0]); rb.template read<0>(at + TA::BYTES, xb[0]); }
-                multiply(1);
+                multiply<MI, NI, 1>(c, xa[1], xb[1]);
             }
         }
     }
 };
-
-// f(n, first m of a run of 8, the run) of a wavefront's part of a block
-template <int WN, int MI, int NI, class F> __device__ __forceinline__ void each_run(const f32x16 (&c)[MI][NI], F f)
-{
-    const int lane = threadIdx.x & 63, w = wavefront(), wm = w / WN, wn = w % WN;
-#pragma unroll
-    for (int j = 0; j < NI; ++j)
-#pragma unroll
-        for (int i = 0; i < MI; ++i)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                float v[8];
-                run_of(c[i][j], h, v);
-                f((wn * NI + j) * 32 + (lane & 31), (wm * MI + i) * 32 + 16 * h + 8 * (lane >> 5), v);
-            }
-}
 
 extern __shared__ char dynamic_lds[];
 __device__ __forceinline__ uint32_t lds_start() { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)dynamic_lds; }
@@ -304,13 +295,21 @@ constexpr int LDS_OF_RING = 144 << 10;      // of stream_kernel at most; behind 
 
 template <int TM, int TN> struct Softmax : Logits<TM, TN> {
     using Logits<TM, TN>::Logits;
-    template <int WM, int WN, int MI, int NI> __device__ __forceinline__ void done(const Place &p, const f32x16 (&c)[MI][NI])
+    template <int WM, int WN, int MI, int NI> __device__ __forceinline__ void done(const Place &p, const f32x4 (&c)[MI][NI])
     {
         const LossArgs &a = this->a;
-        const int w = wavefront(), wm = w / WN, wn = w % WN;
-        if constexpr (WM > 2 || TM == 128) {      // few rows or small blocks: the wavefronts join their parts in LDS
-            float2 *red = reinterpret_cast<float2 *>(dynamic_lds + (TM == 128 ? 0 : LDS_OF_RING));   // (block_kernel: its LDS is free by then)
-            softmax_part(c, red + wm * TN + wn * NI * 32, p.m * TM + wm * MI * 32, this->vn, LOG2E / a.temperature);
+        const int lane = threadIdx.x & 63, w = wavefront(), wm = w / WN, wn = w % WN, m = p.m * TM + wm * MI * 16 + 8 * (lane >> 4);
+        float2 *red = reinterpret_cast<float2 *>(dynamic_lds + (TM == 128 ? 0 : LDS_OF_RING)) + wm * TN + wn * NI * 16;   // (block_kernel: its LDS is free by then)
+        constexpr bool JOIN = WM > 2 || TM == 128;       // few rows or small blocks: the wavefronts join their parts in LDS
+        float2 *to = JOIN ? red : a.part + ((size_t)(this->v0 / TM + p.m) * WM + wm) * a.part_ld + p.n * TN + wn * NI * 16;
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+            const float2 t = column_softmax<MI * 4>([&](int i) { return c[(i >> 3) * 2 + ((i >> 2) & 1)][j][i & 3]; }, [](int i) { return (i >> 3) * 32 + (i & 7); }, this->vn - m,
+                                                    LOG2E / a.temperature, 16);
+            if (lane < 16) to[j * 16 + lane] = t;
+        }
+        if constexpr (JOIN) {
+            red -= wm * TN + wn * NI * 16;
             __syncthreads();
             for (int i = threadIdx.x; i < TN; i += WM * WN * 64) {
                 float2 t = red[i];
@@ -318,59 +317,57 @@ template <int TM, int TN> struct Softmax : Logits<TM, TN> {
                 for (int q = 1; q < WM; ++q) t = join(t, red[q * TN + i]);
                 a.part[(size_t)(this->v0 / TM + p.m) * a.part_ld + p.n * TN + i] = t;
             }
-        } else softmax_part(c, a.part + ((size_t)(this->v0 / TM + p.m) * WM + wm) * a.part_ld + p.n * TN + wn * NI * 32, p.m * TM + wm * MI * 32, this->vn, LOG2E / a.temperature);
+        }
     }
 };
 
 template <int TM, int TN> struct Probabilities : Logits<TM, TN> {
     using Logits<TM, TN>::Logits;
     int have = -1;               // rows whose lse and weight are held
-    float lse2[2], weight[2];    // (weight 0: a row that is none)
-    template <int WM, int WN, int MI, int NI> __device__ __forceinline__ void done(const Place &p, const f32x16 (&c)[MI][NI])
+    float lse2[4], weight[4];    // (weight 0: a row that is none)
+    template <int WM, int WN, int MI, int NI> __device__ __forceinline__ void done(const Place &p, const f32x4 (&c)[MI][NI])
     {
+        static_assert(NI <= 4, "rows held");
         const LossArgs &a = this->a;
-        const int first = p.n * TN + wavefront() % WN * NI * 32, half = this->half;
+        const int lane = threadIdx.x & 63, w = wavefront(), first = p.n * TN + w % WN * NI * 16, half = this->half;
         if (p.n != have) {
             have = p.n;
 #pragma unroll
             for (int j = 0; j < NI; ++j) {
-                const int at = first + j * 32 + (threadIdx.x & 31), row = half && at >= half ? at - half : at;
+                const int at = first + j * 16 + (lane & 15), row = half && at >= half ? at - half : at;
                 lse2[j] = row < this->count ? a.lse[a.idx[row]] * LOG2E : 0.f;
                 weight[j] = row < this->count ? a.grad[a.idx[row]] / a.head->scale : 0.f;
             }
         }
         const float k2 = LOG2E / a.temperature;
-        const int lane = threadIdx.x & 63, v0 = p.m * TM + wavefront() / WN * MI * 32, there = this->vn - v0 - 8 * (lane >> 5);   // entries that exist from this lane's first on
+        const int v0 = p.m * TM + w / WN * MI * 16 + 8 * (lane >> 4), there = this->vn - v0;   // entries that exist from this lane's first on
         const int needed = (this->rows + 63) / 64 * 64;
 #pragma unroll
         for (int j = 0; j < NI; ++j) {
-            const int at = first + j * 32;
+            const int at = first + j * 16;
             if (at >= needed) continue;               // (the products read whole steps of 64 rows)
             const bool second = half && at >= half;   // of a pair: what rounding leaves
-            bf16_t *to = (bf16_t *)a.G + (size_t)(at + (lane & 31)) * a.g_ld + v0 + 8 * (lane >> 5);
+            bf16_t *to = (bf16_t *)a.G + (size_t)(at + (lane & 15)) * a.g_ld + v0;
 #pragma unroll
-            for (int i = 0; i < MI; ++i)
+            for (int i = 0; i < MI; i += 2) {
+                float x[8];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    float x[8];
-                    run_of(c[i][j], h, x);
+                for (int e = 0; e < 8; ++e) x[e] = weight[j] * term(c[i + (e >> 2)][j][e & 3], k2, lse2[j]);
+                // rows that do not count and entries that do not exist: zeros, which the next products read
+                if (this->vn < p.m * TM + TM || this->rows < p.n * TN + TN || half) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = weight[j] * term(x[e], k2, lse2[j]);
-                    // rows that do not count and entries that do not exist: zeros, which the next products read
-                    if (this->vn < p.m * TM + TM || this->rows < p.n * TN + TN || half) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) x[e] = weight[j] != 0.f && i * 32 + 16 * h + e < there ? x[e] : 0.f;
-                    }
-                    if (second) {
-#pragma unroll
-                        for (int e = 0; e < 8; e += 2) {
-                            const uint32_t hi = two_bf16(x[e], x[e + 1]);
-                            x[e] -= __uint_as_float(hi << 16);
-                            x[e + 1] -= __uint_as_float(hi & 0xffff0000u);
-                        }
-                    }
-                    store_run(to + i * 32 + 16 * h, x);
+                    for (int e = 0; e < 8; ++e) x[e] = weight[j] != 0.f && i * 16 + e < there ? x[e] : 0.f;
                 }
+                if (second) {
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2) {
+                        const uint32_t hi = two_bf16(x[e], x[e + 1]);
+                        x[e] -= __uint_as_float(hi << 16);
+                        x[e + 1] -= __uint_as_float(hi & 0xffff0000u);
+                    }
+                }
+                store_run(to + i * 16, x);
+            }
         }
     }
 };
@@ -414,26 +411,22 @@ template <int TM, int TN> struct HiddenGrad {
         p.b = (const bf16_t *)a.G + (size_t)p.n * TN * a.g_ld + k0; p.ldb = a.g_ld; p.b_limit = TN; p.n_limit = rows - p.n * TN;
         return p;
     }
-    template <int WM, int WN, int MI, int NI> __device__ __forceinline__ void done(const Place &p, const f32x16 (&c)[MI][NI])
+    template <int WM, int WN, int MI, int NI> __device__ __forceinline__ void done(const Place &p, const f32x4 (&c)[MI][NI])
     {
         if (!first && p.K == 0) return;
-        const int lane = threadIdx.x & 63, w = wavefront(), d0 = p.m * TM + w / WN * MI * 32 + 8 * (lane >> 5);
+        const int lane = threadIdx.x & 63, w = wavefront(), d0 = p.m * TM + w / WN * MI * 16;
 #pragma unroll
         for (int j = 0; j < NI; ++j) {
-            float *to = a.acc + ((size_t)p.split * bf16_rows(a, rows) + p.n * TN + (w % WN * NI + j) * 32 + (lane & 31)) * a.d_pad + d0;
+            float *to = a.acc + ((size_t)p.split * bf16_rows(a, rows) + p.n * TN + (w % WN * NI + j) * 16 + (lane & 15)) * a.d_pad + d0 + 4 * (lane >> 4);
 #pragma unroll
             for (int i = 0; i < MI; ++i) {
-                if (d0 + i * 32 >= a.d_pad) break;       // (d_pad: a multiple of 64)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    float x[8];
-                    run_of(c[i][j], h, x);
-                    if (!first) {
-                        const float4 u = reinterpret_cast<const float4 *>(to + i * 32 + 16 * h)[0], v = reinterpret_cast<const float4 *>(to + i * 32 + 16 * h)[1];
-                        x[0] += u.x; x[1] += u.y; x[2] += u.z; x[3] += u.w; x[4] += v.x; x[5] += v.y; x[6] += v.z; x[7] += v.w;
-                    }
-                    store_run(to + i * 32 + 16 * h, x);
+                if (d0 + i * 16 >= a.d_pad) break;       // (d_pad: a multiple of 64)
+                float4 x = make_float4(c[i][j][0], c[i][j][1], c[i][j][2], c[i][j][3]);
+                if (!first) {
+                    const float4 u = *reinterpret_cast<const float4 *>(to + i * 16);
+                    x.x += u.x; x.y += u.y; x.z += u.z; x.w += u.w;
                 }
+                *reinterpret_cast<float4 *>(to + i * 16) = x;
             }
         }
     }
@@ -456,24 +449,31 @@ template <int TM, int TN> struct WeightGrad {
         p.b = (const bf16_t *)a.G + p.n * TN; p.ldb = a.g_ld; p.b_limit = a.piece - p.n * TN; p.n_limit = vn - p.n * TN;
         return p;
     }
-    template <int WM, int WN, int MI, int NI> __device__ __forceinline__ void done(const Place &p, const f32x16 (&c)[MI][NI])
+    template <int WM, int WN, int MI, int NI> __device__ __forceinline__ void done(const Place &p, const f32x4 (&c)[MI][NI])
     {
         const float k = a.head->scale * a.temperature;
         const bool whole = ((reinterpret_cast<uintptr_t>(a.d_weight) | (uintptr_t)(a.dws * 2)) & 15) == 0;
         bf16_t *const out = (bf16_t *)a.d_weight + (long long)(v0 + p.n * TN) * a.dws + p.m * TM;
         const int vs = vn - p.n * TN, ds = a.dim - p.m * TM;      // what exists of the block
+        const int lane = threadIdx.x & 63, w = wavefront(), d0 = w / WN * MI * 16 + 4 * (lane >> 4);
+        auto rounded = [&](int i, int j) { return make_uint2(two_bf16(k * c[i][j][0], k * c[i][j][1]), two_bf16(k * c[i][j][2], k * c[i][j][3])); };
         if constexpr (TM == 128) {
             // through LDS, which is free by then, so that a row's stores are whole lines of memory: 16-byte pieces, permuted by the row
-            uint4 *const tile = reinterpret_cast<uint4 *>(dynamic_lds);
-            each_run<WN>(c, [&](int i, int d, float (&x)[8]) {
-                tile[i * 16 + ((d >> 3) ^ (i & 15))] = make_uint4(two_bf16(k * x[0], k * x[1]), two_bf16(k * x[2], k * x[3]), two_bf16(k * x[4], k * x[5]), two_bf16(k * x[6], k * x[7]));
-            });
+#pragma unroll
+            for (int j = 0; j < NI; ++j) {
+                const int v = (w % WN * NI + j) * 16 + (lane & 15);
+#pragma unroll
+                for (int i = 0; i < MI; ++i) {
+                    const int d = d0 + i * 16;
+                    *reinterpret_cast<uint2 *>(dynamic_lds + v * (TM * 2) + (((d >> 3) ^ (v & 15)) << 4) + (d & 4) * 2) = rounded(i, j);
+                }
+            }
             __syncthreads();
 #pragma unroll 4
             for (int at = threadIdx.x; at < TN * 16; at += WM * WN * 64) {
                 const int v = at >> 4, d = (at & 15) * 8;
                 if (v >= vs || d >= ds) continue;
-                const uint4 u = tile[v * 16 + ((at & 15) ^ (v & 15))];
+                const uint4 u = *reinterpret_cast<const uint4 *>(dynamic_lds + v * (TM * 2) + (((at & 15) ^ (v & 15)) << 4));
                 bf16_t *to = out + (long long)v * a.dws + d;
                 if (whole && d + 8 <= ds) *reinterpret_cast<uint4 *>(to) = u;
                 else {
@@ -483,38 +483,32 @@ template <int TM, int TN> struct WeightGrad {
                 }
             }
         } else {
-            const int lane = threadIdx.x & 63, w = wavefront(), d0 = w / WN * MI * 32 + 8 * (lane >> 5);
 #pragma unroll
             for (int j = 0; j < NI; ++j) {
-                const int v = (w % WN * NI + j) * 32 + (lane & 31);
+                const int v = (w % WN * NI + j) * 16 + (lane & 15);
                 if (v >= vs) continue;
                 bf16_t *to = out + (long long)v * a.dws + d0;
 #pragma unroll
-                for (int i = 0; i < MI; ++i)
+                for (int i = 0; i < MI; ++i) {
+                    const uint2 u = rounded(i, j);
+                    if (whole && d0 + i * 16 + 4 <= ds) *reinterpret_cast<uint2 *>(to + i * 16) = u;
+                    else {
+                        const uint32_t q[2] = {u.x, u.y};
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int d = i * 32 + 16 * h;
-                        float x[8];
-                        run_of(c[i][j], h, x);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) x[e] *= k;
-                        if (whole && d0 + d + 8 <= ds) store_run(to + d, x);
-                        else {
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) if (d0 + d + e < ds) store_one(to + d + e, x[e]);
-                        }
+                        for (int e = 0; e < 4; ++e) if (d0 + i * 16 + e < ds) to[i * 16 + e] = (bf16_t)(q[e >> 1] >> (16 * (e & 1)));
                     }
+                }
             }
         }
     }
 };
 
-// Products of listed entries: a wavefront takes 32 of them, its rows of the head against its packed rows, of which only the diagonal is kept: the matrix unit is
+// Products of listed entries: a wavefront takes 16 of them, its rows of the head against its packed rows, of which only the diagonal is kept: the matrix unit is
 // all but idle in a product this small, and it gives the bits that the same pair has in a block (the same instruction over the same steps of k).
 template <int PLANES> __device__ __forceinline__ void entries_group(const LossArgs &a, int group, bool packed)   // packed: the whole head is
 {
-    const int lane = threadIdx.x & 63, e = group * 32 + (lane & 31), hf = lane >> 5, count = a.head->count;
-    if ((long long)group * 32 >= (long long)count * a.entries) return;
+    const int lane = threadIdx.x & 63, e = group * 16 + (lane & 15), g = lane >> 4, count = a.head->count;
+    if ((long long)group * 16 >= (long long)count * a.entries) return;
     const int i = e / a.entries, j = e - i * a.entries;
     bool on = i < count;
     const bf16_t *h = (const bf16_t *)a.hp, *w = packed ? (const bf16_t *)a.wp : (const bf16_t *)a.weight;
@@ -524,16 +518,14 @@ template <int PLANES> __device__ __forceinline__ void entries_group(const LossAr
         h += (size_t)(PLANES == 1 ? i : (i >> 6) * 64 * PLANES + (i & 63)) * a.d_pad;
         if (on) w = packed ? (const bf16_t *)a.wp + (size_t)id * a.d_pad : w + id * a.ws;
     }
-    f32x16 c;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) c[r] = 0.f;
-    // N steps of 16 k, their loads requested together; ANYWHERE: the head's row may begin anywhere, PART: and end within the steps
+    f32x4 c = {0.f, 0.f, 0.f, 0.f};
+    // N steps of 32 k, their loads requested together; ANYWHERE: the head's row may begin anywhere, PART: and end within the steps
     auto steps = [&](auto n, auto anywhere, auto part, int k0) {
         constexpr int N = decltype(n)::value;
         bf16x8 x[N], y[N][PLANES];
 #pragma unroll
         for (int q = 0; q < N; ++q) {
-            const int k = k0 + 16 * q + 8 * hf;
+            const int k = k0 + 32 * q + 8 * g;
             if constexpr (decltype(part)::value) x[q] = __builtin_bit_cast(bf16x8, load8(w, k, on ? a.dim : 0));
             else if constexpr (decltype(anywhere)::value) __builtin_memcpy(&x[q], w + k, 16);
             else x[q] = *reinterpret_cast<const bf16x8 *>(w + k);
@@ -543,7 +535,7 @@ template <int PLANES> __device__ __forceinline__ void entries_group(const LossAr
 #pragma unroll
         for (int q = 0; q < N; ++q)
 #pragma unroll
-            for (int l = 0; l < PLANES; ++l) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[q], y[q][l], c, 0, 0, 0);
+            for (int l = 0; l < PLANES; ++l) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[q], y[q][l], c, 0, 0, 0);
     };
     using Yes = std::true_type;
     using No = std::false_type;
@@ -552,17 +544,15 @@ template <int PLANES> __device__ __forceinline__ void entries_group(const LossAr
     using One = std::integral_constant<int, 1>;
     int k = 0;
     if (a.direct || packed) {
-        for (; k + 16 * MOST <= a.d_pad; k += 16 * MOST) steps(Many{}, No{}, No{}, k);
-        for (; k < a.d_pad; k += 16) steps(One{}, No{}, No{}, k);
+        for (; k + 32 * MOST <= a.d_pad; k += 32 * MOST) steps(Many{}, No{}, No{}, k);
+        for (; k < a.d_pad; k += 32) steps(One{}, No{}, No{}, k);
     } else {
-        for (; k + 16 * MOST <= a.dim; k += 16 * MOST) steps(Many{}, Yes{}, No{}, k);
-        for (; k < a.d_pad; k += 16) steps(One{}, Yes{}, Yes{}, k);
+        for (; k + 32 * MOST <= a.dim; k += 32 * MOST) steps(Many{}, Yes{}, No{}, k);
+        for (; k < a.d_pad; k += 32) steps(One{}, Yes{}, Yes{}, k);
     }
-    const int n = lane & 31;   // row m of column n lies in register (m / 8) * 4 + m % 4 of lane n + 32 * (m / 4 % 2)
-    float d = 0.f;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) d = (n >> 3) * 4 + (n & 3) == r ? c[r] : d;
-    if (on && ((n >> 2) & 1) == hf) a.value[e] = d;
+    const int n = lane & 15;
+    const float d = n & 2 ? (n & 1 ? c[3] : c[2]) : (n & 1 ? c[1] : c[0]);
+    if (on && n >> 2 == g) a.value[e] = d;
 }
 
 __global__ __launch_bounds__(64) void bf16_entries_kernel(LossArgs a, bool packed) { entries_group<1>(a, blockIdx.x, packed); }
@@ -622,22 +612,17 @@ template <template <int, int> class Job_, class Sh> __global__ __launch_bounds__
         if (q >= A_TILES - B_TILES) copy_b();
         full = copy_a();
     }
-    Reader<Sh::TM, Job::A_KC, true, MI> ra;
     static_assert(Sh::PL == 1 || Sh::WN == 1, "a row's planes belong to one wavefront");
-    Reader<Sh::TN * Sh::PL, Job::B_KC, false, NI * Sh::PL> rb;
-    ra.init(w / Sh::WN * MI * 32);
-    rb.init(w % Sh::WN * NI * 32);
-    f32x16 c[MI][NI];
+    typename Sh::RA ra;
+    typename Sh::RB rb;
+    ra.init(w / Sh::WN * MI * 16);
+    rb.init(w % Sh::WN * NI * 16);
+    f32x4 c[MI][NI];
     int from_a = 0, from_b = 0;
 #pragma unroll 1
     for (int it = begin; it < end; it += stride) {
         const Place p = job.place(it);
-#pragma unroll
-        for (int i = 0; i < MI; ++i)
-#pragma unroll
-            for (int j = 0; j < NI; ++j)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) c[i][j][r] = 0.f;
+        clear(c);
 #pragma unroll 1
         for (int s = (p.K + BK - 1) / BK; s; --s) {
             // this step has landed, and everyone has read the one before, whose places are the next copies'
@@ -646,19 +631,11 @@ template <template <int, int> class Job_, class Sh> __global__ __launch_bounds__
             copy_b();
             full = copy_a();
             const uint32_t at_a = lds_a + from_a * Sh::TA::BYTES, at_b = lds_b + from_b * Sh::TB::BYTES;
-            bf16x8 xa[4][MI], xb[4][NI * Sh::PL];
+            bf16x8 xa[2][MI], xb[2][NI * Sh::PL];
             ra.template read<0>(at_a, xa[0]); rb.template read<0>(at_b, xb[0]);
             ra.template read<1>(at_a, xa[1]); rb.template read<1>(at_b, xb[1]);
-            ra.template read<2>(at_a, xa[2]); rb.template read<2>(at_b, xb[2]);
-            ra.template read<3>(at_a, xa[3]); rb.template read<3>(at_b, xb[3]);
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-#pragma unroll
-                for (int l = 0; l < Sh::PL; ++l)
-#pragma unroll
-                    for (int i = 0; i < MI; ++i)
-#pragma unroll
-                        for (int j = 0; j < NI; ++j) c[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xa[q][i], xb[q][l * NI + j], c[i][j], 0, 0, 0);
+            multiply<MI, NI, Sh::PL>(c, xa[0], xb[0]);
+            multiply<MI, NI, Sh::PL>(c, xa[1], xb[1]);
             from_a = from_a + 1 < A_TILES ? from_a + 1 : 0;
             from_b = from_b + 1 < B_TILES ? from_b + 1 : 0;
         }
@@ -666,8 +643,9 @@ template <template <int, int> class Job_, class Sh> __global__ __launch_bounds__
     }
 }
 
-// One block a workgroup.
-template <template <int, int> class Job_, class Bl> __global__ __launch_bounds__(Bl::WAVES * 64) void block_kernel(LossArgs a, int v0, int vn, int flag)
+// One block a workgroup. As many of them a compute unit as LDS has room for hide each other's copies: their registers are bounded for that (gradient to the head of 500 rows,
+// 151936 x 896: 198 us where the compiler's choice left room for two, 138 with four).
+template <template <int, int> class Job_, class Bl> __global__ __launch_bounds__(Bl::WAVES * 64, Bl::AT_ONCE) void block_kernel(LossArgs a, int v0, int vn, int flag)
 {
     Job_<Bl::TM, Bl::TN> job(a, v0, vn, flag, blockIdx.x);
     if (job.o.first >= job.o.end) return;
@@ -685,10 +663,11 @@ template <template <int, int> class Job_, class Bl> __global__ __launch_bounds__
 // two steps and B's of the next: A (the operand that comes from beyond L2 more often) has two steps of time to arrive, B one.
 template <template <int, int> class Job_> __global__ __launch_bounds__(512) void turns_kernel(LossArgs a, int v0, int vn, int flag)
 {
-    constexpr int WM = 2, WN = 4, MI = 4, NI = 2, T = 256, TILES = 5;
+    constexpr int WM = 2, WN = 4, MI = 8, NI = 4, T = 256, TILES = 5;
     using Job = Job_<T, T>;
-    using TA = Tile<T, Job::A_KC, 8>;
-    using TB = Tile<T, Job::B_KC, 8>;
+    using Sh = Shape<WM, WN, MI, NI, Job::A_KC, Job::B_KC>;
+    using TA = typename Sh::TA;
+    using TB = typename Sh::TB;
     Job job(a, v0, vn, flag, blockIdx.x);
     const int begin = job.o.first, end = job.o.end, stride = gridDim.x >> 3, w = wavefront();
     if (begin >= end) return;
@@ -744,20 +723,15 @@ template <template <int, int> class Job_> __global__ __launch_bounds__(512) void
     landed_and_barrier<0>();
     if (second) barrier();
 
-    Reader<T, Job::A_KC, true, MI> ra;
-    Reader<T, Job::B_KC, false, NI> rb;
-    ra.init(w / WN * MI * 32);
-    rb.init(w % WN * NI * 32);
-    f32x16 c[MI][NI];
-    bf16x8 xa[2][MI], xb[2][NI];
+    typename Sh::RA ra;
+    typename Sh::RB rb;
+    ra.init(w / WN * MI * 16);
+    rb.init(w % WN * NI * 16);
+    f32x4 c[MI][NI];
+    bf16x8 xa[MI], xb[NI];
     auto products = [&] {
         __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-        for (int q = 0; q < 2; ++q)
-#pragma unroll
-            for (int i = 0; i < MI; ++i)
-#pragma unroll
-                for (int j = 0; j < NI; ++j) c[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xa[q][i], xb[q][j], c[i][j], 0, 0, 0);
+        multiply<MI, NI, 1>(c, xa, xb);
         __builtin_amdgcn_s_setprio(0);
         __builtin_amdgcn_sched_barrier(0);
     };
@@ -765,18 +739,13 @@ template <template <int, int> class Job_> __global__ __launch_bounds__(512) void
 #pragma unroll 1
     for (int item = begin; item < end; item += stride) {
         const Place p = job.place(item);
-        const bool works = w / WN * MI * 32 < p.a_limit && w % WN * NI * 32 < p.n_limit;   // the last blocks: nothing is multiplied that does not exist
-#pragma unroll
-        for (int i = 0; i < MI; ++i)
-#pragma unroll
-            for (int j = 0; j < NI; ++j)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) c[i][j][r] = 0.f;
+        const bool works = w / WN * MI * 16 < p.a_limit && w % WN * NI * 16 < p.n_limit;   // the last blocks: nothing is multiplied that does not exist
+        clear(c);
 #pragma unroll 1
         for (int s = (p.K + BK - 1) / BK; s; --s) {
             if (works) {
-                ra.template read<0>(at_a, xa[0]); rb.template read<0>(at_b, xb[0]);
-                ra.template read<1>(at_a, xa[1]); rb.template read<1>(at_b, xb[1]);
+                ra.template read<0>(at_a, xa);
+                rb.template read<0>(at_b, xb);
             }
             // the tiles of the step before are free: everyone has read them
             if (steps_b) copy_b();
@@ -787,8 +756,8 @@ template <template <int, int> class Job_> __global__ __launch_bounds__(512) void
             if (works) products();
             barrier();
             if (works) {
-                ra.template read<2>(at_a, xa[0]); rb.template read<2>(at_b, xb[0]);
-                ra.template read<3>(at_a, xa[1]); rb.template read<3>(at_b, xb[1]);
+                ra.template read<1>(at_a, xa);
+                rb.template read<1>(at_b, xb);
             }
             // before the barrier after which the next step is read: both its tiles are there, A's of the step after may be under way
             if (second) {
@@ -830,7 +799,7 @@ template <auto KERNEL, class... A> void launch(dim3 grid, int threads, int lds, 
     hipLaunchKernelGGL(KERNEL, grid, dim3(threads), lds, s, args...);
 }
 
-int entry_groups(const LossArgs &a) { return (int)(((long long)a.rows * a.entries + 31) / 32); }
+int entry_groups(const LossArgs &a) { return (int)(((long long)a.rows * a.entries + 15) / 16); }
 
 // Where blocks of 256 x 256 would leave half of the chip without one, those of 128 x 128 (two a compute unit) are four times as many: 817 of 1021 rows x 5003 x 1001, softmax
 // 30 -> 19 us. With more blocks the large ones are faster: 300 of 500 rows x 151936 x 896 139 us against 141, 2048 x 152064 x 3584 1.9 ms against 2.2.
@@ -849,12 +818,12 @@ template <template <int, int> class Job> void launch_job(hipStream_t s, const Lo
         launch<stream_kernel<Job, Sh>>(persistent, 512, LDS_OF_RING + Sh::WM * Sh::TN * (int)sizeof(float2), s, a, v0, vn, flag, extra);
     };
     if (a.hdt == DT_F32) {
-        if constexpr (std::is_same_v<Job<256, 64>, Softmax<256, 64>>) stream(Shape<8, 1, 1, 2, A, B, 3>{});
-    } else if (a.n_block == 64) stream(Shape<8, 1, 1, 2, A, B>{});
-    else if (a.n_block == 128) stream(Shape<4, 2, 2, 2, A, B>{});
+        if constexpr (std::is_same_v<Job<256, 64>, Softmax<256, 64>>) stream(Shape<8, 1, 2, 4, A, B, 3>{});
+    } else if (a.n_block == 64) stream(Shape<8, 1, 2, 4, A, B>{});
+    else if (a.n_block == 128) stream(Shape<4, 2, 4, 4, A, B>{});
     else if (A && small_blocks(vn, product_rows(a))) {
         if constexpr (A) {
-            using Bl = Block<2, Shape<2, 2, 2, 2, A, B>>;
+            using Bl = Block<2, Shape<2, 2, 4, 4, A, B>>;
             launch<block_kernel<Job, Bl>>(dim3(up_div(up_div(vn, Bl::TM) * up_div(product_rows(a), Bl::TN), 8) * 8), 256, Bl::LDS, s, a, v0, vn, flag);
         }
     } else launch<turns_kernel<Job>>(dim3(256), 512, 5 * 256 * BK * 2, s, a, v0, vn, flag);
@@ -886,7 +855,7 @@ void launch_bf16_hidden_grad(hipStream_t s, const LossArgs &a, int v0, int vn, b
 // counting: 902 against 976 us; but 8192 rows 1956 against 1854, and 2048 rows x 3584 features 2399 against 2287).
 void launch_bf16_weight_grad(hipStream_t s, const LossArgs &a, int v0, int vn)
 {
-    using Bl = Block<1, Shape<2, 2, 2, 2, false, false>>;
+    using Bl = Block<1, Shape<2, 2, 4, 4, false, false>>;
     const int over = a.d_pad % 256;
     if (a.rows <= (over && over <= 128 ? 4096 : 1024)) launch<block_kernel<WeightGrad, Bl>>(dim3(up_div(up_div(a.d_pad, Bl::TM) * up_div(vn, Bl::TN), 8) * 8), 256, Bl::LDS, s, a, v0, vn, 0);
     else launch<turns_kernel<WeightGrad>>(dim3(256), 512, 5 * 256 * BK * 2, s, a, v0, vn, 0);

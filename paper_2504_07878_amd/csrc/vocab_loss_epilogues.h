@@ -56,43 +56,30 @@ __device__ __forceinline__ float2 join(float2 a, float2 b)
     return make_float2(m, a.y * __builtin_amdgcn_exp2f(a.x - at) + b.y * __builtin_amdgcn_exp2f(b.x - at));
 }
 
-// A wavefront's part of its rows' softmax: MI x NI accumulators over vocabulary entries m0 .. (those at or past V do not exist); part: of its first row.
-template <int MI, int NI>
-__device__ __forceinline__ void softmax_part(const f32x16 (&c)[MI][NI], float2 *part, int m0, int V, float k2)
+// The running softmax of a lane's N products of one row, value(i) at vocabulary entry first + offset(i), joined with those of the lanes `apart`, 2 apart, ... from it; entries at
+// or past `left` from first on do not exist.
+template <int N, class Value, class Offset> __device__ __forceinline__ float2 column_softmax(Value value, Offset offset, int left, float k2, int apart)
 {
-    const int lane = threadIdx.x & 63, hf = lane >> 5, col = lane & 31;
+    float top = -INFINITY, sum = 0.f;
+    if (left >= offset(N - 1) + 1) {
 #pragma unroll
-    for (int ni = 0; ni < NI; ++ni) {
-        float top = -INFINITY;
+        for (int i = 0; i < N; ++i) top = fmaxf(top, value(i));
+    } else {
 #pragma unroll
-        for (int mi = 0; mi < MI; ++mi) {
-            const int base = m0 + mi * 32;
-            if (base + 32 <= V) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) top = fmaxf(top, c[mi][ni][r]);
-            } else {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) top = base + 16 * (r >> 3) + 8 * hf + (r & 7) < V ? fmaxf(top, c[mi][ni][r]) : top;
-            }
-        }
-        top = fmaxf(top, __shfl_xor(top, 32));
-        top = whole_above(top * k2);
-        const float at = top == -INFINITY ? 0.f : top;
-        float sum = 0.f;
-#pragma unroll
-        for (int mi = 0; mi < MI; ++mi) {
-            const int base = m0 + mi * 32;
-            if (base + 32 <= V) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) sum += term(c[mi][ni][r], k2, at);
-            } else {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) sum += base + 16 * (r >> 3) + 8 * hf + (r & 7) < V ? term(c[mi][ni][r], k2, at) : 0.f;
-            }
-        }
-        sum += __shfl_xor(sum, 32);
-        if (hf == 0) part[ni * 32 + col] = make_float2(top, sum);
+        for (int i = 0; i < N; ++i) top = offset(i) < left ? fmaxf(top, value(i)) : top;
     }
+    for (int o = apart; o < 64; o *= 2) top = fmaxf(top, __shfl_xor(top, o));
+    top = whole_above(top * k2);
+    const float at = top == -INFINITY ? 0.f : top;
+    if (left >= offset(N - 1) + 1) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum += term(value(i), k2, at);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum += offset(i) < left ? term(value(i), k2, at) : 0.f;
+    }
+    for (int o = apart; o < 64; o *= 2) sum += __shfl_xor(sum, o);
+    return make_float2(top, sum);
 }
 
 }  // namespace tr

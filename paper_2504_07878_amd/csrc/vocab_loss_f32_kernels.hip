@@ -176,7 +176,9 @@ __global__ __launch_bounds__(256) void f32_softmax_kernel(LossArgs a, int extra)
     const ListedLines<float> B{Lines<float>(a.hidden, a.hs, count, a.dim), a.idx};
     f32x16 c[1][1];
     products<true, true>(A, B, m0, n0, 0, a.dim, sm, c);
-    softmax_part(c, a.part + ((size_t)(m0 / F32_BLOCK) * 2 + (w >> 1)) * a.part_ld + n0 + (w & 1) * 32, m0 + (w >> 1) * 32, a.vocab, LOG2E / a.temperature);
+    const int lane = threadIdx.x & 63, m = m0 + (w >> 1) * 32 + 8 * (lane >> 5);
+    const float2 t = column_softmax<16>([&](int i) { return c[0][0][i]; }, [](int i) { return 16 * (i >> 3) + (i & 7); }, a.vocab - m, LOG2E / a.temperature, 32);
+    if (lane < 32) a.part[((size_t)(m0 / F32_BLOCK) * 2 + (w >> 1)) * a.part_ld + n0 + (w & 1) * 32 + lane] = t;
 }
 
 template <class WT> __global__ __launch_bounds__(256) void f32_probabilities_kernel(LossArgs a, int v0, int vn, int extra)
