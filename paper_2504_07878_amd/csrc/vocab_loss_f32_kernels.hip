@@ -2,85 +2,158 @@
 // are read. (The softmax of fp32 rows over a bf16 head has faster ones, on three bf16 rows for each.)
 //
 // A workgroup of 4 wavefronts (2 x 2, an accumulator of 32 x 32 each) computes a 64 x 64 block of C[n][m] = sum_k A[m][k] B[n][k] in steps of 32 k: both operands
-// go through registers into LDS as [row][k], one step ahead, in two buffers. A lane reads four k at a time: k = 8 g + 4 (lane / 32) + j for the j-th product of group g.
-// Small blocks, since models of this type are small: they have to fill the chip. Bound by latency there: 133 of 190 rows x 4096 x 256 take 21 us for the softmax, 13 and 11 us for
-// the gradients (blocks of 128 x 128, 16 k a step, in one buffer: 52, 40 and 33). Three products:
+// go through registers into LDS as [row][k], two steps ahead, in two buffers. A lane reads four k at a time: k = 8 g + 4 (lane / 32) + j for the j-th product of group g.
+// Small blocks, since models of this type are small: they have to fill the chip. Bound by latency there: 133 of 190 rows x 4096 x 256 take 11 us for the softmax, 13 and 10 us for
+// the gradients (5 us of each for a single step; blocks of 128 x 128, 16 k a step, in one buffer: 52, 40 and 33; one step ahead, and loads that waited for each other: 21, 13
+// and 11, 19 of the first for the listed entries). Three products:
 //   softmax, probabilities: m = vocabulary entry, n = row that counts, k = feature
 //   gradient to the hidden rows: m = feature, n = row, k = vocabulary entry of the piece; summed over the pieces in `acc`, one sum per split of k
 //   gradient to the head: m = feature, n = vocabulary entry, k = row
 #include "vocab_loss_epilogues.h"
+#include <type_traits>
 
 namespace tr {
 
 namespace {
 
+typedef __attribute__((ext_vector_type(4))) float f32x4;
 constexpr int BK = 32, PITCH = BK + 4;       // 16-byte reads of 16 rows meet 16 different places of the 64 banks
 
-// eight elements of a line from j on, as fp32; zeros at or past `limit` and where there is no line. `wide`: the line lies on 16 bytes
-__device__ __forceinline__ void eight_of(const float *line, int j, int limit, bool wide, float (&v)[8])
+// N elements of a line from p on, which lies on 16 bytes and has them, as fp32
+template <int N> __device__ __forceinline__ void widened(const float *p, float (&v)[N])
 {
-    if (line && wide && j + 8 <= limit) {
-        const float4 x = *reinterpret_cast<const float4 *>(line + j), y = *reinterpret_cast<const float4 *>(line + j + 4);
-        v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
-    } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = line && j + e < limit ? line[j + e] : 0.f;
+    for (int q = 0; q < N; q += 4) {
+        const f32x4 x = *reinterpret_cast<const f32x4 *>(p + q);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[q + e] = x[e];
     }
 }
-__device__ __forceinline__ void eight_of(const bf16_t *line, int j, int limit, bool, float (&v)[8])
+template <int N> __device__ __forceinline__ void widened(const bf16_t *p, float (&v)[N])
 {
-    const uint4 u = line ? load8(line, j, limit) : make_uint4(0, 0, 0, 0);
-    const uint32_t q[4] = {u.x, u.y, u.z, u.w};
+    uint32_t u[N / 2];
+    if constexpr (N == 8) *reinterpret_cast<uint4 *>(u) = *reinterpret_cast<const uint4 *>(p);
+    else *reinterpret_cast<uint2 *>(u) = *reinterpret_cast<const uint2 *>(p);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) { v[2 * e] = __uint_as_float(q[e] << 16); v[2 * e + 1] = __uint_as_float(q[e] & 0xffff0000u); }
+    for (int q = 0; q < N; q += 2) { v[q] = __uint_as_float(u[q / 2] << 16); v[q + 1] = __uint_as_float(u[q / 2] & 0xffff0000u); }
 }
-
-template <class T> __device__ __forceinline__ void four_of(const T *line, int j, int limit, bool wide, float (&v)[4])
+// ... from j on, wherever it lies; zeros at or past `limit` and where there is no line
+template <int N, class T> __device__ __forceinline__ void widened(const T *line, int j, int limit, bool wide, float (&v)[N])
 {
-    if (line && wide && j + 4 <= limit) {
-        if constexpr (sizeof(T) == 4) {
-            const float4 x = *reinterpret_cast<const float4 *>(line + j);
-            v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
-        } else {
-            const uint2 u = *reinterpret_cast<const uint2 *>(line + j);
-            v[0] = __uint_as_float(u.x << 16); v[1] = __uint_as_float(u.x & 0xffff0000u); v[2] = __uint_as_float(u.y << 16); v[3] = __uint_as_float(u.y & 0xffff0000u);
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = line && j + e < limit ? load_one(line + j + e) : 0.f;
-    }
-}
-
-// An operand is lines of memory: line o has elements 0 .. limit - 1. ALONG_K: a line is a row of the operand (k runs along it); otherwise it is one k.
-template <class T> struct Lines {              // line o at p + o * ld, o < lines
-    const T *p; long long ld; int lines, limit; bool wide;
-    __device__ __forceinline__ Lines(const void *p_, long long ld_, int lines_, int limit_) : p((const T *)p_), ld(ld_), lines(lines_), limit(limit_)
-    {
-        wide = ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * sizeof(T))) & 15) == 0;
-    }
-    __device__ __forceinline__ void read(int o, int j, float (&v)[8]) const { eight_of(o < lines ? p + o * ld : nullptr, j, limit, wide, v); }
-};
-template <class T> struct ListedLines {        // line o at p + list[o] * ld
-    Lines<T> l; const int *list;
-    __device__ __forceinline__ void read(int o, int j, float (&v)[8]) const { eight_of(o < l.lines ? l.p + list[o] * l.ld : nullptr, j, l.limit, l.wide, v); }
-};
-
-struct Tiles { float a[2][F32_BLOCK * PITCH], b[2][F32_BLOCK * PITCH]; };
-
-// a thread's eight elements of a tile (64 x 32): of a row, or of a k
-template <bool ALONG_K, class Op> __device__ __forceinline__ void read_tile(const Op &op, int row0, int k0, float (&v)[8])
-{
-    const int t = threadIdx.x;
-    if (ALONG_K) op.read(row0 + (t >> 2), k0 + (t & 3) * 8, v);
-    else op.read(k0 + (t >> 3), row0 + (t & 7) * 8, v);
-}
-template <bool ALONG_K> __device__ __forceinline__ void write_tile(float *lds, const float (&v)[8])
-{
-    const int t = threadIdx.x;
-    if (ALONG_K) store_run(lds + (t >> 2) * PITCH + (t & 3) * 8, v);
+    if (line && wide && j + N <= limit) widened(line + j, v);
     else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) lds[((t & 7) * 8 + e) * PITCH + (t >> 3)] = v[e];
+        for (int e = 0; e < N; ++e) v[e] = line && j + e < limit ? load_one(line + j + e) : 0.f;
+    }
+}
+
+// An operand is lines of memory: line o, o < lines, has elements 0 .. limit - 1 from p + o * ld on, with a list from p + list[o] * ld. ALONG_K: a line is a row of the
+// operand (k runs along it); otherwise it is one k. wide: lines lie on 16 bytes; regular: eight elements are there or not together.
+template <class T, bool LISTED = false> struct Lines {
+    const T *p; long long ld; int lines, limit; const int *list; bool wide, regular;
+    __device__ __forceinline__ Lines(const void *p_, long long ld_, int lines_, int limit_, const int *list_ = nullptr) : p((const T *)p_), ld(ld_), lines(lines_), limit(limit_), list(list_)
+    {
+        wide = ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * sizeof(T))) & 15) == 0;
+        regular = wide && limit % 8 == 0;
+    }
+    __device__ __forceinline__ int place(int o) const { return LISTED ? list[min(o, lines - 1)] : min(o, lines - 1); }    // of line o, or of the last
+};
+
+struct alignas(16) Tiles { float a[2][F32_BLOCK * PITCH], b[2][F32_BLOCK * PITCH]; };
+
+// A thread's eight elements of the tiles (64 x 32) from row0 on, step after step from k0 on: of a row, or of a k (whose place is read a step ahead); zeros where there
+// is nothing. REGULAR: read as they are, under no condition, from the nearest place that is there, and widened when they are used: until then nothing waits for them.
+template <bool ALONG_K, bool REGULAR, class Op> struct Steps {
+    using T = std::remove_const_t<std::remove_pointer_t<decltype(Op::p)>>;
+    struct Read { f32x4 u[sizeof(T) == 4 || !REGULAR ? 2 : 1]; bool there; };
+    const Op &op;
+    int place, line, along;
+    __device__ __forceinline__ Steps(const Op &op_, int row0, int k0) : op(op_)
+    {
+        const int t = threadIdx.x;
+        line = ALONG_K ? row0 + (t >> 2) : k0 + (t >> 3);
+        along = ALONG_K ? k0 + (t & 3) * 8 : row0 + (t & 7) * 8;
+        place = op.place(line);
+    }
+    __device__ __forceinline__ void next(Read &r)
+    {
+        const T *at = op.p + place * op.ld;
+        r.there = line < op.lines && along < op.limit;
+        if constexpr (REGULAR) {
+            at += min(along, op.limit - 8);
+            r.u[0] = *reinterpret_cast<const f32x4 *>(at);
+            if constexpr (sizeof(T) == 4) r.u[1] = *reinterpret_cast<const f32x4 *>(at + 4);
+        } else {
+            float v[8];
+            widened(r.there ? at : nullptr, along, op.limit, op.wide, v);
+            r.u[0] = f32x4{v[0], v[1], v[2], v[3]};
+            r.u[1] = f32x4{v[4], v[5], v[6], v[7]};
+        }
+        if (ALONG_K) along += BK;
+        else { line += BK; place = op.place(line); }
+    }
+    static __device__ __forceinline__ void values(const Read &r, float (&v)[8])
+    {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if constexpr (sizeof(T) == 4 || !REGULAR) v[e] = r.u[e >> 2][e & 3];
+            else v[e] = __uint_as_float(e & 1 ? __float_as_uint(r.u[0][e >> 1]) & 0xffff0000u : __float_as_uint(r.u[0][e >> 1]) << 16);
+            v[e] = r.there ? v[e] : 0.f;
+        }
+    }
+    static __device__ __forceinline__ void write(float *lds, const Read &r)
+    {
+        float v[8];
+        values(r, v);
+        const int t = threadIdx.x;
+        if (ALONG_K) {
+            f32x4 *to = reinterpret_cast<f32x4 *>(lds + (t >> 2) * PITCH + (t & 3) * 8);
+            to[0] = f32x4{v[0], v[1], v[2], v[3]};
+            to[1] = f32x4{v[4], v[5], v[6], v[7]};
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) lds[((t & 7) * 8 + e) * PITCH + (t >> 3)] = v[e];
+        }
+    }
+};
+// own LDS accesses are done, then the workgroup's barrier; loads may be under way
+__device__ __forceinline__ void lds_barrier()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));   // lgkmcnt 0
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+template <bool A_ALONG, bool B_ALONG, bool REGULAR, class A, class B>
+__device__ __forceinline__ void products_of(const A &a, const B &b, int m0, int n0, int k_lo, int k_hi, Tiles &sm, f32x16 (&c)[1][1])
+{
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int arow = (w >> 1) * 32 + tile_feature(lane & 31), brow = (w & 1) * 32 + (lane & 31), at = (lane >> 5) * 4;
+    Steps<A_ALONG, REGULAR, A> from_a(a, m0, k_lo);
+    Steps<B_ALONG, REGULAR, B> from_b(b, n0, k_lo);
+    typename Steps<A_ALONG, REGULAR, A>::Read ra[2];
+    typename Steps<B_ALONG, REGULAR, B>::Read rb[2];
+    from_a.next(ra[0]); from_b.next(rb[0]);
+    from_a.next(ra[1]); from_b.next(rb[1]);
+    const auto step = [&](auto buffer) {
+        constexpr int buf = decltype(buffer)::value;
+        from_a.write(sm.a[buf], ra[buf]);
+        from_b.write(sm.b[buf], rb[buf]);
+        lds_barrier();          // (the other buffer's readers are past it when it is written again)
+        from_a.next(ra[buf]); from_b.next(rb[buf]);     // (past the end: for nobody)
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int g = 0; g < BK; g += 8) {
+            const f32x4 x = *reinterpret_cast<const f32x4 *>(sm.a[buf] + arow * PITCH + g + at), y = *reinterpret_cast<const f32x4 *>(sm.b[buf] + brow * PITCH + g + at);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) c[0][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[q], y[q], c[0][0], 0, 0, 0);
+        }
+    };
+    for (int k = k_lo;; k += 2 * BK) {
+        step(std::integral_constant<int, 0>{});
+        if (k + BK >= k_hi) break;
+        step(std::integral_constant<int, 1>{});
+        if (k + 2 * BK >= k_hi) break;
     }
 }
 
@@ -88,29 +161,11 @@ template <bool ALONG_K> __device__ __forceinline__ void write_tile(float *lds, c
 template <bool A_ALONG, bool B_ALONG, class A, class B>
 __device__ __forceinline__ void products(const A &a, const B &b, int m0, int n0, int k_lo, int k_hi, Tiles &sm, f32x16 (&c)[1][1])
 {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int arow = (w >> 1) * 32 + tile_feature(lane & 31), brow = (w & 1) * 32 + (lane & 31), at = (lane >> 5) * 4;
 #pragma unroll
     for (int r = 0; r < 16; ++r) c[0][0][r] = 0.f;
     if (k_lo >= k_hi) return;
-    float va[8], vb[8];
-    read_tile<A_ALONG>(a, m0, k_lo, va);
-    read_tile<B_ALONG>(b, n0, k_lo, vb);
-    int buf = 0;
-    for (int k = k_lo; k < k_hi; k += BK, buf ^= 1) {
-        write_tile<A_ALONG>(sm.a[buf], va);
-        write_tile<B_ALONG>(sm.b[buf], vb);
-        __syncthreads();        // (the other buffer's readers are past it when it is written again)
-        if (k + BK < k_hi) { read_tile<A_ALONG>(a, m0, k + BK, va); read_tile<B_ALONG>(b, n0, k + BK, vb); }
-#pragma unroll
-        for (int g = 0; g < BK; g += 8) {
-            const float4 x = *reinterpret_cast<const float4 *>(sm.a[buf] + arow * PITCH + g + at), y = *reinterpret_cast<const float4 *>(sm.b[buf] + brow * PITCH + g + at);
-            c[0][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(x.x, y.x, c[0][0], 0, 0, 0);
-            c[0][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(x.y, y.y, c[0][0], 0, 0, 0);
-            c[0][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(x.z, y.z, c[0][0], 0, 0, 0);
-            c[0][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(x.w, y.w, c[0][0], 0, 0, 0);
-        }
-    }
+    if (a.regular && b.regular) products_of<A_ALONG, B_ALONG, true>(a, b, m0, n0, k_lo, k_hi, sm, c);
+    else products_of<A_ALONG, B_ALONG, false>(a, b, m0, n0, k_lo, k_hi, sm, c);
 }
 
 // f(n, first m of a run of 8, the run) for every run of the block
@@ -132,34 +187,44 @@ template <class WT> __device__ __forceinline__ void entries_group(const LossArgs
     const int lane = threadIdx.x & 63, e = group * 32 + (lane & 31), hf = lane >> 5, count = a.head->count;
     if ((long long)group * 32 >= (long long)count * a.entries) return;
     const int i = e / a.entries, j = e - i * a.entries;
-    const float *h = nullptr;
-    const WT *w = nullptr;
-    if (i < count) {
+    bool on = i < count;
+    const float *h = (const float *)a.hidden;         // (a lane without an entry reads what is there, for nobody)
+    const WT *w = (const WT *)a.weight;
+    if (on) {
         const int r = a.idx[i], id = a.ids[(long long)r * a.entries + j];
-        if (id >= 0 && id < a.vocab) { h = (const float *)a.hidden + r * a.hs; w = (const WT *)a.weight + id * a.ws; }
+        h += r * a.hs;
+        on = id >= 0 && id < a.vocab;
+        if (on) w += id * a.ws;
     }
-    const bool hw = ((reinterpret_cast<uintptr_t>(a.hidden) | (uintptr_t)(a.hs * 4)) & 15) == 0, ww = ((reinterpret_cast<uintptr_t>(a.weight) | (uintptr_t)(a.ws * sizeof(WT))) & 15) == 0;
+    const bool wide = ((reinterpret_cast<uintptr_t>(a.hidden) | (uintptr_t)(a.hs * 4) | reinterpret_cast<uintptr_t>(a.weight) | (uintptr_t)(a.ws * sizeof(WT))) & 15) == 0;
     f32x16 c;
 #pragma unroll
     for (int r = 0; r < 16; ++r) c[r] = 0.f;
-    constexpr int AT_ONCE = 8;       // groups of 8 k whose loads are requested together
-    for (int k0 = 0; k0 < a.dim; k0 += 8 * AT_ONCE) {
-        float x[AT_ONCE][4], y[AT_ONCE][4];
+    constexpr int AT_ONCE = 16;      // groups of 8 k whose loads are requested together
+    float x[AT_ONCE][4], y[AT_ONCE][4];
+    const auto multiply = [&](int g) {
 #pragma unroll
-        for (int g = 0; g < AT_ONCE; ++g) { four_of(w, k0 + 8 * g + 4 * hf, a.dim, ww, x[g]); four_of(h, k0 + 8 * g + 4 * hf, a.dim, hw, y[g]); }
+        for (int q = 0; q < 4; ++q) c = __builtin_amdgcn_mfma_f32_32x32x2f32(x[g][q], y[g][q], c, 0, 0, 0);
+    };
+    int k0 = 0;
+    if (wide)
+        for (; k0 + 8 * AT_ONCE <= a.dim; k0 += 8 * AT_ONCE) {
 #pragma unroll
-        for (int g = 0; g < AT_ONCE; ++g)
-            if (k0 + 8 * g < a.dim) {
+            for (int g = 0; g < AT_ONCE; ++g) { widened(w + k0 + 8 * g + 4 * hf, x[g]); widened(h + k0 + 8 * g + 4 * hf, y[g]); }
 #pragma unroll
-                for (int q = 0; q < 4; ++q) c = __builtin_amdgcn_mfma_f32_32x32x2f32(x[g][q], y[g][q], c, 0, 0, 0);
-            }
+            for (int g = 0; g < AT_ONCE; ++g) multiply(g);
+        }
+    for (; k0 < a.dim; k0 += 8) {
+        widened(w, k0 + 4 * hf, a.dim, wide, x[0]);
+        widened(h, k0 + 4 * hf, a.dim, wide, y[0]);
+        multiply(0);
     }
     // row m of column n lies in register (m / 8) * 4 + m % 4 of lane n + 32 * (m / 4 % 2)
     const int n = lane & 31;
     float d = 0.f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) d = (n >> 3) * 4 + (n & 3) == r ? c[r] : d;
-    if (w && ((n >> 2) & 1) == hf) a.value[e] = d;
+    if (on && ((n >> 2) & 1) == hf) a.value[e] = d;
 }
 
 // The first `extra` workgroups along x, of the first row of them, take listed entries.
@@ -173,7 +238,7 @@ __global__ __launch_bounds__(256) void f32_softmax_kernel(LossArgs a, int extra)
     }
     if (n0 >= count) return;
     const Lines<float> A(a.weight, a.ws, a.vocab, a.dim);
-    const ListedLines<float> B{Lines<float>(a.hidden, a.hs, count, a.dim), a.idx};
+    const Lines<float, true> B(a.hidden, a.hs, count, a.dim, a.idx);
     f32x16 c[1][1];
     products<true, true>(A, B, m0, n0, 0, a.dim, sm, c);
     const int lane = threadIdx.x & 63, m = m0 + (w >> 1) * 32 + 8 * (lane >> 5);
@@ -191,7 +256,7 @@ template <class WT> __global__ __launch_bounds__(256) void f32_probabilities_ker
     }
     if (n0 >= count) return;
     const Lines<WT> A((const WT *)a.weight + (long long)v0 * a.ws, a.ws, vn, a.dim);
-    const ListedLines<float> B{Lines<float>(a.hidden, a.hs, count, a.dim), a.idx};
+    const Lines<float, true> B(a.hidden, a.hs, count, a.dim, a.idx);
     f32x16 c[1][1];
     products<true, true>(A, B, m0, n0, 0, a.dim, sm, c);
     const float k = 1.0f / a.temperature;
@@ -212,7 +277,7 @@ template <class WT> __global__ __launch_bounds__(256) void f32_hidden_grad_kerne
     const int m0 = blockIdx.x * F32_BLOCK, n0 = blockIdx.y * F32_BLOCK, count = a.head->count;
     if (n0 >= count) return;
     const Lines<WT> A((const WT *)a.weight + (long long)v0 * a.ws, a.ws, vn, a.dim);
-    const Lines<float> B(a.G, a.g_ld, count, vn);
+    const Lines<float> B(a.G, a.g_ld, count, (vn + 7) & ~7);      // (G is zero from vn on to the end of a block)
     f32x16 c[1][1];
     products<false, true>(A, B, m0, n0, min(vn, (int)blockIdx.z * per), min(vn, ((int)blockIdx.z + 1) * per), sm, c);
     each_run(c, [&](int n, int m, float (&v)[8]) {
@@ -231,8 +296,8 @@ template <class WT> __global__ __launch_bounds__(256) void f32_weight_grad_kerne
 {
     __shared__ Tiles sm;
     const int m0 = blockIdx.x * F32_BLOCK, n0 = blockIdx.y * F32_BLOCK, count = a.head->count;
-    const ListedLines<float> A{Lines<float>(a.hidden, a.hs, count, a.dim), a.idx};
-    const Lines<float> B(a.G, a.g_ld, count, vn);
+    const Lines<float, true> A(a.hidden, a.hs, count, a.dim, a.idx);
+    const Lines<float> B(a.G, a.g_ld, count, (vn + 7) & ~7);      // (G is zero from vn on to the end of a block)
     f32x16 c[1][1];
     products<false, false>(A, B, m0, n0, 0, count, sm, c);
     const float k = a.head->scale * a.temperature;
