@@ -11,7 +11,8 @@ template <bool TEACHER>
 __device__ __forceinline__ bool entry_counts(const LossArgs &a, long long at)
 {
     const int id = a.ids[at];
-    return id >= 0 && id < a.vocab && (!TEACHER || a.teacher[at] != -INFINITY);
+    const float t = TEACHER ? a.teacher[at] : 0.f;         // (read at the same time)
+    return (id >= 0) & (id < a.vocab) & (t != -INFINITY);
 }
 
 // A row counts if it has an entry (and, for gradients, a weight).
@@ -217,23 +218,19 @@ __device__ __forceinline__ Shares shares_of(const LossArgs &a, int r)
 template <bool TEACHER, int ROWS>
 __global__ __launch_bounds__(256) void loss_finish_kernel(LossArgs a, int parts)
 {
-    __shared__ float2 joined[256];
-    const int i0 = blockIdx.x * ROWS, count = a.head->count, t = threadIdx.x, lane = t & 63, w = t >> 6;
-    if (i0 >= count) return;
-    const int mine = i0 + t % ROWS;
+    __shared__ float2 joined[4][ROWS];
+    const int i0 = blockIdx.x * ROWS, t = threadIdx.x, lane = t & 63, w = t >> 6, mine = min(i0 + t % ROWS, a.rows - 1);
     float2 x = make_float2(-INFINITY, 0.f);
-    if (mine < count)
 #pragma unroll 4
-        for (int p = t / ROWS; p < parts; p += 256 / ROWS) x = join(x, a.part[(size_t)p * a.part_ld + mine]);
-    joined[t] = x;
+    for (int p = t / ROWS; p < parts; p += 256 / ROWS) x = join(x, a.part[(size_t)p * a.part_ld + mine]);    // (of a row that does not count: for nobody)
+    const int count = a.head->count;
+    if (i0 >= count) return;
+    for (int o = ROWS; o < 64; o *= 2) x = join(x, make_float2(__shfl_xor(x.x, o), __shfl_xor(x.y, o)));
+    if (lane < ROWS) joined[w][lane] = x;
     __syncthreads();
-    for (int o = 128; o >= ROWS; o >>= 1) {
-        if (t < o) joined[t] = join(joined[t], joined[t + o]);
-        __syncthreads();
-    }
     for (int q = w; q < ROWS && i0 + q < count; q += 4) {
         const int i = i0 + q, r = a.idx[i];
-        const float2 st = joined[q];
+        const float2 st = join(join(joined[0][q], joined[1][q]), join(joined[2][q], joined[3][q]));
         const float ls = logf(st.y), k2 = LOG2E / a.temperature, at = st.x == -INFINITY ? 0.f : st.x;
         const Shares sh = shares_of<TEACHER>(a, r);
         const float ltot = TEACHER ? logf(sh.total) : 0.f;
@@ -268,21 +265,33 @@ template <bool BF16> __device__ __forceinline__ void place_entry(const LossArgs 
 template <bool TEACHER, bool PLACE, bool BF16>
 __global__ __launch_bounds__(256) void loss_values_kernel(LossArgs a)
 {
-    const int i = blockIdx.x;
+    const int i = blockIdx.x, lane = threadIdx.x & 63;
     if (i >= a.head->count) return;
     const int r = a.idx[i];
     const float lse = a.lse[r], k = 1.0f / a.temperature, weight = a.grad[r] / a.head->scale;
     const Shares sh = shares_of<TEACHER>(a, r);
     const long long at0 = (long long)r * a.entries;
-    for (int j = threadIdx.x; j < a.entries; j += 256) {
-        if (!entry_counts<TEACHER>(a, at0 + j)) continue;
-        const int id = a.ids[at0 + j];
+    for (int j0 = threadIdx.x - lane; j0 < a.entries; j0 += 256) {
+        const int j = j0 + lane;
+        const bool on = j < a.entries && entry_counts<TEACHER>(a, at0 + j);
+        const int id = on ? a.ids[at0 + j] : -1;
         float q = 1.f;
         if (TEACHER) {
+            // a wavefront's 64 shares at a time, each handed to all its lanes
             q = 0.f;
-            for (int o = 0; o < a.entries; ++o)
-                if (a.ids[at0 + o] == id && entry_counts<TEACHER>(a, at0 + o)) q += expf((a.teacher[at0 + o] - sh.top) / a.temperature) / sh.total;
+            for (int o0 = 0; o0 < a.entries; o0 += 64) {
+                const int o = o0 + lane;
+                const bool other = o < a.entries && entry_counts<TEACHER>(a, at0 + o);
+                const int others = other ? a.ids[at0 + o] : -1;
+                const float share = other ? expf((a.teacher[at0 + o] - sh.top) / a.temperature) / sh.total : 0.f;
+                for (int n = 0; n < min(64, a.entries - o0); ++n) {
+                    const int same = __shfl(others, n);
+                    const float its = __shfl(share, n);
+                    q += same == id ? its : 0.f;
+                }
+            }
         }
+        if (!on) continue;
         float &v = a.value[(size_t)i * a.entries + j];
         const float x = weight * (expf(fmaf(v, k, -lse)) - q);
         if (PLACE) place_entry<BF16>(a, i, id, x);
