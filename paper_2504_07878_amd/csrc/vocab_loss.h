@@ -84,6 +84,7 @@ void launch_bf16_pack_head(hipStream_t s, const LossArgs &a, int v0, int vn);
 // entries: the listed entries' products too, in the same launch (blocks of fewer than 256 rows only)
 void launch_bf16_softmax(hipStream_t s, const LossArgs &a, int v0, int vn, bool entries);
 int bf16_softmax_parts(const LossArgs &a);
+bool bf16_takes_entries(const LossArgs &a, int vn);      // the softmax and the probabilities of a piece of vn entries take the listed ones along
 void launch_bf16_probabilities(hipStream_t s, const LossArgs &a, int v0, int vn, bool entries);
 void launch_bf16_hidden_grad(hipStream_t s, const LossArgs &a, int v0, int vn, bool first);
 void launch_bf16_weight_grad(hipStream_t s, const LossArgs &a, int v0, int vn);

@@ -115,9 +115,10 @@ int forward(const tr_loss_config *c, void *ws, size_t ws_bytes, void *stream, co
     launch_loss_rows(s, a);
     const bool bf16_products = a.hp != nullptr;
     if (bf16_products) {
-        const bool along = a.n_block < 256;     // the listed entries in the same launch
+        const int most = a.direct ? a.vocab : std::min(a.piece, a.vocab);
+        const bool along = bf16_takes_entries(a, most);
         for (int v0 = 0, vn; v0 < a.vocab; v0 += vn) {
-            vn = a.direct ? a.vocab : std::min(a.piece, a.vocab - v0);
+            vn = std::min(most, a.vocab - v0);
             if (!a.direct) launch_bf16_pack_head(s, a, v0, vn);
             launch_bf16_softmax(s, a, v0, vn, along && v0 == 0);
         }
@@ -143,7 +144,7 @@ int backward(const tr_loss_config *c, void *ws, size_t ws_bytes, void *stream, c
     a.d_hidden = out->d_hidden; a.dhs = out->d_hidden_stride; a.d_weight = out->d_weight; a.dws = out->d_weight_stride;
     hipStream_t s = (hipStream_t)stream;
     launch_loss_rows(s, a);
-    const bool half = is_bf16(c), one = a.piece >= a.vocab, along = half && a.n_block < 256;
+    const bool half = is_bf16(c), one = a.piece >= a.vocab, along = half && bf16_takes_entries(a, std::min(a.piece, a.vocab));
     const bool whole = half && a.rows && !a.direct && one;      // the head is packed once, whole
     if (whole) launch_bf16_pack_head(s, a, 0, a.vocab);
     if (a.rows && half && !along) launch_bf16_entries(s, a, whole);

@@ -432,6 +432,8 @@ template <int TM, int TN> struct HiddenGrad {
     }
 };
 
+__host__ __device__ inline bool on_16_bytes(const LossArgs &a) { return ((reinterpret_cast<uintptr_t>(a.d_weight) | (uintptr_t)(a.dws * 2)) & 15) == 0; }   // the head's gradient is
+
 template <int TM, int TN> struct WeightGrad {
     static constexpr bool A_KC = false, B_KC = false;
     const LossArgs &a;
@@ -452,7 +454,6 @@ template <int TM, int TN> struct WeightGrad {
     template <int WM, int WN, int MI, int NI> __device__ __forceinline__ void done(const Place &p, const f32x4 (&c)[MI][NI])
     {
         const float k = a.head->scale * a.temperature;
-        const bool whole = ((reinterpret_cast<uintptr_t>(a.d_weight) | (uintptr_t)(a.dws * 2)) & 15) == 0;
         bf16_t *const out = (bf16_t *)a.d_weight + (long long)(v0 + p.n * TN) * a.dws + p.m * TM;
         const int vs = vn - p.n * TN, ds = a.dim - p.m * TM;      // what exists of the block
         const int lane = threadIdx.x & 63, w = wavefront(), d0 = w / WN * MI * 16 + 4 * (lane >> 4);
@@ -469,13 +470,21 @@ template <int TM, int TN> struct WeightGrad {
                 }
             }
             __syncthreads();
+            if (!on_16_bytes(a)) {        // an element a lane, side by side (817 rows x 5003 x 1001: 28 us where a lane stored eight in a row)
+#pragma unroll 4
+                for (int at = threadIdx.x; at < TN * TM; at += WM * WN * 64) {
+                    const int v = at / TM, d = at % TM;
+                    if (v < vs && d < ds) out[(long long)v * a.dws + d] = *reinterpret_cast<const bf16_t *>(dynamic_lds + v * (TM * 2) + (((d >> 3) ^ (v & 15)) << 4) + (d & 7) * 2);
+                }
+                return;
+            }
 #pragma unroll 4
             for (int at = threadIdx.x; at < TN * 16; at += WM * WN * 64) {
                 const int v = at >> 4, d = (at & 15) * 8;
                 if (v >= vs || d >= ds) continue;
                 const uint4 u = *reinterpret_cast<const uint4 *>(dynamic_lds + v * (TM * 2) + (((at & 15) ^ (v & 15)) << 4));
                 bf16_t *to = out + (long long)v * a.dws + d;
-                if (whole && d + 8 <= ds) *reinterpret_cast<uint4 *>(to) = u;
+                if (d + 8 <= ds) *reinterpret_cast<uint4 *>(to) = u;
                 else {
                     const uint32_t q[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
@@ -491,7 +500,7 @@ template <int TM, int TN> struct WeightGrad {
 #pragma unroll
                 for (int i = 0; i < MI; ++i) {
                     const uint2 u = rounded(i, j);
-                    if (whole && d0 + i * 16 + 4 <= ds) *reinterpret_cast<uint2 *>(to + i * 16) = u;
+                    if (d0 + i * 16 + 4 <= ds) *reinterpret_cast<uint2 *>(to + i * 16) = u;      // (a gradient on 16 bytes: launch_bf16_weight_grad)
                     else {
                         const uint32_t q[2] = {u.x, u.y};
 #pragma unroll
@@ -561,15 +570,16 @@ __global__ __launch_bounds__(64) void bf16_entries_kernel(LossArgs a, bool packe
 // 151936 x 896, so 63): rings of both operands' steps in LDS, one barrier a step. The first `extra` (a multiple of 8) workgroups take listed entries instead.
 template <template <int, int> class Job_, class Sh> __global__ __launch_bounds__(Sh::WAVES * 64) void stream_kernel(LossArgs a, int v0, int vn, int flag, int extra)
 {
-    if ((int)blockIdx.x < extra) {
-        entries_group<Sh::PL>(a, blockIdx.x * Sh::WAVES + wavefront(), !a.direct && vn == a.vocab);
-        return;
-    }
+    using Job = Job_<Sh::TM, Sh::TN>;
+    if constexpr (Job::A_KC)
+        if ((int)blockIdx.x < extra) {
+            entries_group<Sh::PL>(a, blockIdx.x * Sh::WAVES + wavefront(), !a.direct && vn == a.vocab);
+            return;
+        }
     constexpr int MI = Sh::MI, NI = Sh::NI;
     constexpr int A_TILES = 3, B_TILES = Sh::PL > 1 ? 2 : 3;     // rings of both operands; B's (the rows, in L2) may be shorter
     constexpr int UNDER_WAY = A_TILES == B_TILES ? Sh::TA::COPIES + Sh::TB::COPIES : Sh::TA::COPIES;   // copies that may be, when a step's last have landed
     static_assert(A_TILES * Sh::TA::BYTES + B_TILES * Sh::TB::BYTES <= LDS_OF_RING, "LDS");
-    using Job = Job_<Sh::TM, Sh::TN>;
     Job job(a, v0, vn, flag, blockIdx.x - extra);
     const int begin = job.o.first, end = job.o.end, stride = (gridDim.x - extra) >> 3, w = wavefront();
     if (begin >= end) return;
@@ -643,11 +653,17 @@ template <template <int, int> class Job_, class Sh> __global__ __launch_bounds__
     }
 }
 
-// One block a workgroup. As many of them a compute unit as LDS has room for hide each other's copies: their registers are bounded for that (gradient to the head of 500 rows,
+// One block a workgroup, the first `extra` (a multiple of 8) take listed entries. As many of them a compute unit as LDS has room for hide each other's copies: their registers are bounded for that (gradient to the head of 500 rows,
 // 151936 x 896: 198 us where the compiler's choice left room for two, 138 with four).
-template <template <int, int> class Job_, class Bl> __global__ __launch_bounds__(Bl::WAVES * 64, Bl::AT_ONCE) void block_kernel(LossArgs a, int v0, int vn, int flag)
+template <template <int, int> class Job_, class Bl> __global__ __launch_bounds__(Bl::WAVES * 64, Bl::AT_ONCE) void block_kernel(LossArgs a, int v0, int vn, int flag, int extra)
 {
-    Job_<Bl::TM, Bl::TN> job(a, v0, vn, flag, blockIdx.x);
+    using Job = Job_<Bl::TM, Bl::TN>;
+    if constexpr (Job::A_KC)
+        if ((int)blockIdx.x < extra) {
+            entries_group<1>(a, blockIdx.x * Bl::WAVES + wavefront(), !a.direct && vn == a.vocab);
+            return;
+        }
+    Job job(a, v0, vn, flag, blockIdx.x - extra);
     if (job.o.first >= job.o.end) return;
     const Place p = job.place(job.o.first);
     Bl bl;
@@ -806,15 +822,15 @@ int entry_groups(const LossArgs &a) { return (int)(((long long)a.rows * a.entrie
 int product_rows(const LossArgs &a) { return a.pairs ? std::max(a.rows, 2 * PAIR_ROWS) : a.rows; }     // at most
 bool small_blocks(int m, int n) { return up_div(m, 256) * up_div(n, 256) <= 128; }
 
-// entries: listed entries too, where there are few rows or fp32 ones
+// entries: listed entries too
 template <template <int, int> class Job> void launch_job(hipStream_t s, const LossArgs &a, int v0, int vn, int flag, bool entries)
 {
     constexpr bool A = Job<256, 64>::A_KC, B = Job<256, 64>::B_KC;
-    const int extra = entries ? up_div(entry_groups(a), 64) * 8 : 0;
-    // a workgroup a compute unit: a few of them take entries only, since the head's bytes come as fast without them
-    const dim3 persistent(extra <= 64 ? 256 : 256 + extra);
     const auto stream = [&](auto shape) {
         using Sh = decltype(shape);
+        const int extra = entries ? up_div(entry_groups(a), 64) * 8 : 0;
+        // a workgroup a compute unit: a few of them take entries only, since the head's bytes come as fast without them
+        const dim3 persistent(extra <= 64 ? 256 : 256 + extra);
         launch<stream_kernel<Job, Sh>>(persistent, 512, LDS_OF_RING + Sh::WM * Sh::TN * (int)sizeof(float2), s, a, v0, vn, flag, extra);
     };
     if (a.hdt == DT_F32) {
@@ -824,7 +840,8 @@ template <template <int, int> class Job> void launch_job(hipStream_t s, const Lo
     else if (A && small_blocks(vn, product_rows(a))) {
         if constexpr (A) {
             using Bl = Block<2, Shape<2, 2, 4, 4, A, B>>;
-            launch<block_kernel<Job, Bl>>(dim3(up_div(up_div(vn, Bl::TM) * up_div(product_rows(a), Bl::TN), 8) * 8), 256, Bl::LDS, s, a, v0, vn, flag);
+            const int own = entries ? up_div(entry_groups(a), 32) * 8 : 0;
+            launch<block_kernel<Job, Bl>>(dim3(own + up_div(up_div(vn, Bl::TM) * up_div(product_rows(a), Bl::TN), 8) * 8), 256, Bl::LDS, s, a, v0, vn, flag, own);
         }
     } else launch<turns_kernel<Job>>(dim3(256), 512, 5 * 256 * BK * 2, s, a, v0, vn, flag);
 }
@@ -840,6 +857,10 @@ void launch_bf16_entries(hipStream_t s, const LossArgs &a, bool packed) { hipLau
 
 void launch_bf16_softmax(hipStream_t s, const LossArgs &a, int v0, int vn, bool entries) { launch_job<Softmax>(s, a, v0, vn, 0, entries); }
 
+// Which launches take the listed entries along: those of few rows, or of small blocks (two launches less of 6 us each, 817 of 1021 rows x 5003 x 1001). Beside many large blocks
+// a launch of their own costs nothing, and would keep the persistent workgroups waiting.
+bool bf16_takes_entries(const LossArgs &a, int vn) { return a.n_block < 256 || small_blocks(vn, product_rows(a)); }
+
 // (blocks of 256 x 256 leave two parts each, those of 128 x 128 one, in the same places)
 int bf16_softmax_parts(const LossArgs &a) { return up_div(a.vocab, a.n_block < 256 ? BF16_BLOCK : BF16_BLOCK / 2); }
 
@@ -852,12 +873,13 @@ void launch_bf16_hidden_grad(hipStream_t s, const LossArgs &a, int v0, int vn, b
 
 // Blocks of 256 x 256 or, several a compute unit, of 128 x 128 in one step's LDS: while one loads or stores another multiplies. Small ones for few rows, where it is a matter of
 // writing (300 of 500 rows x 151936 x 896: 145 us against 165), and up to more rows where the last large ones would be half empty (896 features, 4096 rows, three quarters of them
-// counting: 902 against 976 us; but 8192 rows 1956 against 1854, and 2048 rows x 3584 features 2399 against 2287).
+// counting: 902 against 976 us; but 8192 rows 1956 against 1854, and 2048 rows x 3584 features 2399 against 2287);
+// and where rows of the gradient do not lie on 16 bytes, since only they bring whole lines of it together (all gradients of 2048 rows x 32000 x 1001: 483 us against 517).
 void launch_bf16_weight_grad(hipStream_t s, const LossArgs &a, int v0, int vn)
 {
     using Bl = Block<1, Shape<2, 2, 4, 4, false, false>>;
     const int over = a.d_pad % 256;
-    if (a.rows <= (over && over <= 128 ? 4096 : 1024)) launch<block_kernel<WeightGrad, Bl>>(dim3(up_div(up_div(a.d_pad, Bl::TM) * up_div(vn, Bl::TN), 8) * 8), 256, Bl::LDS, s, a, v0, vn, 0);
+    if (!on_16_bytes(a) || a.rows <= (over && over <= 128 ? 4096 : 1024)) launch<block_kernel<WeightGrad, Bl>>(dim3(up_div(up_div(a.d_pad, Bl::TM) * up_div(vn, Bl::TN), 8) * 8), 256, Bl::LDS, s, a, v0, vn, 0, 0);
     else launch<turns_kernel<WeightGrad>>(dim3(256), 512, 5 * 256 * BK * 2, s, a, v0, vn, 0);
 }
 
