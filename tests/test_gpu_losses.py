@@ -422,3 +422,22 @@ def test_sizes_of_the_small_models_head(losses):
     dz *= (t["grad_loss"].double() * on)[:, None]
     for k, want in (("d_hidden", dz @ w.double()), ("d_weight", dz.t().contiguous() @ h.double())):
         assert float((got[k].double() - want).norm() / want.norm()) < 3 * 2.0 ** -9 / math.sqrt(3), k
+
+
+@pytest.mark.parametrize("size,entries", [((1500, 200, 6000), 0), ((1500, 200, 6000), 3), ((1200, 201, 1300), 0), ((4400, 304, 500), 0), ((90, 200, 12000), 70)], ids=str)
+def test_many_rows(losses, size, entries):
+    """Large blocks whose last ones are partly empty, along the rows, the features and the vocabulary; a head whose rows do not lie on 16 bytes; more entries than lanes."""
+    t = make(*size, BF16, BF16, entries=entries, seed=sum(size), even=True)
+    check(call(losses, t, 2.0 if entries else 1.0), t, 2.0 if entries else 1.0)
+
+
+@pytest.mark.parametrize("types", TYPES, ids=["f32", "f32_rows", "bf16"])
+@pytest.mark.parametrize("dim,entries", [(72, 0), (128, 0), (72, 5), (128, 5)])
+def test_the_vocabulary_in_pieces(losses, dim, entries, types):
+    """A workspace for so many rows that a piece has 2048 entries; the same bits of the loss as from one that takes the vocabulary whole."""
+    t = make(90, dim, 5000, *types, entries=entries, seed=31)
+    plan = losses.VocabLoss(130000, dim, 5000, *types, max_entries=max(entries, 1))
+    got = call(losses, t, 1.5 if entries else 1.0, plan=plan)
+    check(got, t, 1.5 if entries else 1.0)
+    whole = call(losses, t, 1.5 if entries else 1.0)
+    assert torch.equal(got["loss"], whole["loss"]) and torch.equal(got["lse"], whole["lse"])
