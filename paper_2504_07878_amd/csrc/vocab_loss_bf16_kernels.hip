@@ -882,15 +882,16 @@ void launch_bf16_hidden_grad(hipStream_t s, const LossArgs &a, int v0, int vn, b
     launch_job<HiddenGrad>(s, a, v0, vn, first, false);
 }
 
-// Blocks of 256 x 256 or, several a compute unit, of 128 x 128 in one step's LDS: while one loads or stores another multiplies. Small ones for few rows, where it is a matter of
-// writing (300 of 500 rows x 151936 x 896: 145 us against 165), and up to more rows where the last large ones would be half empty (896 features, 4096 rows, three quarters of them
-// counting: 902 against 976 us; but 8192 rows 1956 against 1854, and 2048 rows x 3584 features 2399 against 2287);
-// and where rows of the gradient do not lie on 16 bytes, since only they bring whole lines of it together (all gradients of 2048 rows x 32000 x 1001: 483 us against 517).
+// Blocks of 256 x 256 or, several a compute unit, of 128 x 128 in one step's LDS: while one loads or stores another multiplies. Small ones
+//   for few rows, where it is a matter of writing (300 of 500 rows x 151936 x 896: 139 us against 189; 1200 rows x 64000 x 3584 would be 1160 against 1073);
+//   up to more rows for narrow heads whose last large blocks would be half empty (896 features, 4096 rows, three quarters of them counting: 850 against 960 us, 2048 rows x 64000 x 640
+//   383 against 392; but 8192 rows x 64000 x 896 1930 against 1840, 2048 x 64000 x 1024 610 against 602, 8192 x 64000 x 1344 3040 against 2610);
+//   and where rows of the gradient do not lie on 16 bytes, since only they bring whole lines of it together (all gradients of 2048 rows x 32000 x 1001: 483 us against 517).
 void launch_bf16_weight_grad(hipStream_t s, const LossArgs &a, int v0, int vn)
 {
     using Bl = Block<1, Shape<2, 2, 4, 4, false, false>>;
-    const int over = a.d_pad % 256;
-    if (!on_16_bytes(a) || a.rows <= (over && over <= 128 ? 4096 : 1024)) launch<block_kernel<WeightGrad, Bl>>(dim3(up_div(up_div(a.d_pad, Bl::TM) * up_div(vn, Bl::TN), 8) * 8), 256, Bl::LDS, s, a, v0, vn, 0, 0);
+    const bool half_empty = a.d_pad < 1024 && a.d_pad % 256 && a.d_pad % 256 <= 128;
+    if (!on_16_bytes(a) || a.rows <= (half_empty ? 4096 : 1024)) launch<block_kernel<WeightGrad, Bl>>(dim3(up_div(up_div(a.d_pad, Bl::TM) * up_div(vn, Bl::TN), 8) * 8), 256, Bl::LDS, s, a, v0, vn, 0, 0);
     else launch<turns_kernel<WeightGrad>>(dim3(256), 512, 5 * 256 * BK * 2, s, a, v0, vn, 0);
 }
 
