@@ -93,7 +93,7 @@ __host__ __device__ inline int bf16_products_rows(int count, int half) { return 
 __host__ __device__ inline int bf16_rows(const LossArgs &a, int rows) { return (rows + a.n_block - 1) / a.n_block * a.n_block; }   // whole blocks
 // Splits of the sums of the gradient to `rows` rows (of products), a power of two, at most a.splits: those for which a workgroup a compute unit is done first, when it takes
 // `tiles` * n blocks, 256 at a time, of (steps / n + SPLIT_COST) steps of 64 k each; the sums' reading and writing costs a block about as much as that many steps.
-// (6144 rows x 151936 x 896, 8 splits instead of 2: 2097 -> 1999 us; 2048 x 152064 x 3584: 2114 -> 2347 us, so 2.)
+// (6144 rows x 151936 x 896, 8 splits instead of 2: 2060 -> 1890 us; 2048 x 152064 x 3584: 2114 -> 2347 us, so 2.)
 constexpr int SPLIT_COST = 16;
 __host__ __device__ inline int bf16_splits(const LossArgs &a, int rows)
 {

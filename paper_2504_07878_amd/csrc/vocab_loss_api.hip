@@ -31,7 +31,7 @@ bool is_bf16(const tr_loss_config *c) { return c->hidden_dtype == TR_BF16; }    
 bool in_planes(const tr_loss_config *c) { return c->hidden_dtype == TR_F32 && c->weight_dtype == TR_BF16; }   // those of the softmax do, on rows in three planes
 
 // G stays at 512 MB or less, but a piece has 2048 columns at least (8192 rows x 151936 x 896, three quarters of the rows counting, all products of the gradients, pieces of
-// 128 / 256 / 512 / 1024 MB: 7.1 / 5.9 / 5.8 / 5.7 ms); where the head is packed, that stays at 128 MB or less.
+// 256 / 512 / 1024 MB: 5.60 / 5.45 / 5.42 ms); where the head is packed, that stays at 128 MB or less.
 Plan plan_of(const tr_loss_config *c)
 {
     Plan p{};

@@ -42,9 +42,9 @@ template <int N> __device__ __forceinline__ void landed_and_barrier()
 }
 
 // Matrix instructions of 16 x 16 x 32: in registers alone they sustain 1.97 PFLOP/s on random data where those of 32 x 32 x 16 sustain 1.74 (the chip's power bounds both), since
-// they move half as much of the accumulators (softmax of 2048 rows x 152064 x 3584: 1867 -> 1780 us). An operand is 16 rows x 32 k, lane l holding k = 8 (l / 16) .. + 7 of row l mod 16; lane l of the result holds rows 4 (l / 16) .. + 3 of
-// column l mod 16. Where m lies along memory in the result and k contiguous in A, A's rows are taken in pairs of operands over 32 rows, row 4 a + e of the first being 8 a + e and of
-// the second 8 a + 4 + e, so that a lane's results of a pair are 8 in a run.
+// they move half as much of the accumulators (softmax of 2048 rows x 152064 x 3584: 1867 -> 1780 us). An operand is 16 rows x 32 k, lane l holding k = 8 (l / 16) .. + 7 of row
+// l mod 16; lane l of the result holds rows 4 (l / 16) .. + 3 of column l mod 16. Where m lies along memory in the result and k contiguous in A, A's rows are taken in pairs of
+// operands over 32 rows, row 4 a + e of the first being 8 a + e and of the second 8 a + 4 + e, so that a lane's results of a pair are 8 in a run.
 
 // How the pieces of a line of a tile are permuted (exclusive or). LDS has 64 banks of 4 bytes: the 16 lanes that a 16-byte read serves at a time have to meet 16
 // different pieces of 256 bytes, two lines of 64 k; the 32 lanes of an 8-byte read 8 different pieces of 32 bytes, from 8 lines of one column. (Keyed by the
@@ -427,7 +427,7 @@ template <int TM, int TN> struct HiddenGrad {
         }
     }
     // what the products are added to: the sums of the pieces before, all read at once (added at the end instead, a few at a time, as
-    // registers allow: 6144 rows x 151936 x 896 in five pieces 2005 us, so 1910)
+    // registers allow: 6144 rows x 151936 x 896 in five pieces 2005 us, so 1890)
     template <int WN, int MI, int NI> __device__ __forceinline__ void start(const Place &p, f32x4 (&c)[MI][NI]) const
     {
         clear(c);
@@ -664,8 +664,8 @@ template <template <int, int> class Job_, class Sh> __global__ __launch_bounds__
     }
 }
 
-// One block a workgroup, the first `extra` (a multiple of 8) take listed entries. As many of them a compute unit as LDS has room for hide each other's copies: their registers are bounded for that (gradient to the head of 500 rows,
-// 151936 x 896: 198 us where the compiler's choice left room for two, 138 with four).
+// One block a workgroup, the first `extra` (a multiple of 8) take listed entries. As many of them a compute unit as LDS has room for hide each other's copies: their registers
+// are bounded for that (gradient to the head of 300 of 500 rows, 151936 x 896: 198 us where the compiler's choice left room for two, 138 with four).
 template <template <int, int> class Job_, class Bl> __global__ __launch_bounds__(Bl::WAVES * 64, Bl::AT_ONCE) void block_kernel(LossArgs a, int v0, int vn, int flag, int extra)
 {
     using Job = Job_<Bl::TM, Bl::TN>;
@@ -685,7 +685,7 @@ template <template <int, int> class Job_, class Bl> __global__ __launch_bounds__
 }
 
 // Blocks of 256 x 256, one workgroup a compute unit, block after block, the copies never stopping (softmax of 2048 rows x 152064 x 3584, a workgroup a block: 1977 us; in turns:
-// 1881; copies running on: 1835). 8 wavefronts of 128 x 64; the first four and the last four (one of each
+// 1881; copies running on: 1835; 1780 with the present instructions). 8 wavefronts of 128 x 64; the first four and the last four (one of each
 // on every SIMD) take turns: while one reads its matrix operands of 32 k from LDS, the other's matrix instructions run. LDS holds five tiles, a step's two, A's of the next
 // two steps and B's of the next: A (the operand that comes from beyond L2 more often) has two steps of time to arrive, B one.
 template <template <int, int> class Job_> __global__ __launch_bounds__(512) void turns_kernel(LossArgs a, int v0, int vn, int flag)
@@ -828,8 +828,9 @@ template <auto KERNEL, class... A> void launch(dim3 grid, int threads, int lds, 
 
 int entry_groups(const LossArgs &a) { return (int)(((long long)a.rows * a.entries + 15) / 16); }
 
-// Where blocks of 256 x 256 would leave half of the chip without one, those of 128 x 128 (two a compute unit) are four times as many: 817 of 1021 rows x 5003 x 1001, softmax
-// 30 -> 19 us. With more blocks the large ones are faster: 300 of 500 rows x 151936 x 896 139 us against 141, 2048 x 152064 x 3584 1.9 ms against 2.2.
+// Where blocks of 256 x 256 would leave half of the chip without one, those of 128 x 128 (three a compute unit) are four times as many: 817 of 1021 rows x 5003 x 1001, softmax
+// 30 -> 20 us. With more blocks the large ones are faster: 6144 x 151936 x 896 1545 us against 1793, 2048 x 152064 x 3584
+// 1796 against 2106 (300 of 500 rows x 151936 x 896, softmax and probabilities: 291 both ways).
 int product_rows(const LossArgs &a) { return a.pairs ? std::max(a.rows, 2 * PAIR_ROWS) : a.rows; }     // at most
 bool small_blocks(int m, int n) { return up_div(m, 256) * up_div(n, 256) <= 128; }
 
@@ -891,7 +892,8 @@ void launch_bf16_weight_grad(hipStream_t s, const LossArgs &a, int v0, int vn)
 {
     using Bl = Block<1, Shape<2, 2, 4, 4, false, false>>;
     const bool half_empty = a.d_pad < 1024 && a.d_pad % 256 && a.d_pad % 256 <= 128;
-    if (!on_16_bytes(a) || a.rows <= (half_empty ? 4096 : 1024)) launch<block_kernel<WeightGrad, Bl>>(dim3(up_div(up_div(a.d_pad, Bl::TM) * up_div(vn, Bl::TN), 8) * 8), 256, Bl::LDS, s, a, v0, vn, 0, 0);
+    const int blocks = up_div(a.d_pad, Bl::TM) * up_div(vn, Bl::TN);
+    if (!on_16_bytes(a) || a.rows <= (half_empty ? 4096 : 1024)) launch<block_kernel<WeightGrad, Bl>>(dim3(up_div(blocks, 8) * 8), 256, Bl::LDS, s, a, v0, vn, 0, 0);
     else launch<turns_kernel<WeightGrad>>(dim3(256), 512, 5 * 256 * BK * 2, s, a, v0, vn, 0);
 }
 
