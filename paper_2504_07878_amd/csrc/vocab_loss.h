@@ -22,6 +22,9 @@ struct LossHead {
 // packed rows are there twice. The products are bound by the head's bytes then, so the second half costs little, and few rows average few roundings.
 constexpr int PAIR_ROWS = 128;
 
+// What the probabilities of a row of products need (gradients, bf16 products); rows that are none have weight 0.
+struct alignas(16) LossRow { float lse, weight; int target, none; };    // target: cross entropy's entry
+
 struct LossArgs {
     const void *hidden, *weight;
     long long hs, ws;             // elements from row to row
@@ -43,6 +46,7 @@ struct LossArgs {
     void *G;                      // [n_pad][g_ld], a piece's columns; lines are not a power of two apart, so that a column's do not meet in one memory channel
     float *acc;                   // [splits][n_pad, or the blocks that count (bf16)][d_pad] sums of the gradient to the hidden rows
     void *hp;                     // [n_pad][d_pad] rows that count (bf16 products)
+    LossRow *row;                 // [n_pad] theirs
     void *wp;                     // [piece][d_pad] rows of the head where they cannot be read as they lie
     int n_pad, d_pad, piece, g_ld, splits, part_ld;
     int pairs;                    // rows may be in pairs (gradients, bf16 products)
@@ -75,8 +79,7 @@ constexpr int F32_BLOCK = 64;
 void launch_f32_softmax(hipStream_t s, const LossArgs &a);
 int f32_softmax_parts(const LossArgs &a);
 void launch_f32_probabilities(hipStream_t s, const LossArgs &a, int v0, int vn);
-void launch_f32_hidden_grad(hipStream_t s, const LossArgs &a, int v0, int vn, bool first);
-void launch_f32_weight_grad(hipStream_t s, const LossArgs &a, int v0, int vn);
+void launch_f32_gradients(hipStream_t s, const LossArgs &a, int v0, int vn, bool first);     // those asked for
 
 // bf16 rows and head (vocab_loss_bf16_kernels.hip): blocks of 256 vocabulary entries or features.
 constexpr int BF16_BLOCK = 256;

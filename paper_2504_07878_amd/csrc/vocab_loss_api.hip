@@ -24,7 +24,7 @@ bool config_ok(const tr_loss_config *c)
 struct Plan {
     int n_pad, d_pad, piece, g_ld, splits;
     int packed;        // columns of a piece whose head is packed
-    size_t head, idx, state, part, value, G, acc, hp, wp, total;
+    size_t head, idx, state, part, value, G, acc, hp, wp, row, total;
 };
 
 bool is_bf16(const tr_loss_config *c) { return c->hidden_dtype == TR_BF16; }                                    // all products run on bf16 matrix instructions
@@ -60,6 +60,7 @@ Plan plan_of(const tr_loss_config *c)
     if (half || in_planes(c)) {
         p.hp = take((size_t)p.n_pad * (half ? 1 : 3) * steps * 2);
         p.wp = take((size_t)p.packed * steps * 2);
+        p.row = take((size_t)p.n_pad * sizeof(LossRow));
     }
     p.total = at;
     return p;
@@ -91,7 +92,7 @@ int arguments(const tr_loss_config *c, const tr_loss_rows *in, void *ws, size_t 
     a.n_pad = a.part_ld = p.n_pad; a.d_pad = p.d_pad; a.piece = p.piece; a.g_ld = p.g_ld; a.splits = p.splits;
     a.direct = a.dim % 64 == 0 && a.ws % 8 == 0 && a.ws < (1 << 22) && (reinterpret_cast<uintptr_t>(a.weight) & 15) == 0;
     if (is_bf16(c) || (in_planes(c) && !gradient)) {
-        a.hp = b + p.hp; a.wp = b + p.wp;
+        a.hp = b + p.hp; a.wp = b + p.wp; a.row = (LossRow *)(b + p.row);
         a.pairs = gradient;
         const int rows = gradient && a.rows <= PAIR_ROWS ? 2 * a.rows : a.rows;
         a.n_block = rows <= 64 || in_planes(c) ? 64 : rows <= 128 ? 128 : 256;
@@ -144,10 +145,11 @@ int backward(const tr_loss_config *c, void *ws, size_t ws_bytes, void *stream, c
     a.d_hidden = out->d_hidden; a.dhs = out->d_hidden_stride; a.d_weight = out->d_weight; a.dws = out->d_weight_stride;
     hipStream_t s = (hipStream_t)stream;
     launch_loss_rows(s, a);
-    const bool half = is_bf16(c), one = a.piece >= a.vocab, along = half && bf16_takes_entries(a, std::min(a.piece, a.vocab));
+    // a teacher's entries are placed in G; cross entropy's one a row falls to whoever computes that place
+    const bool half = is_bf16(c), one = a.piece >= a.vocab, along = half && teacher && bf16_takes_entries(a, std::min(a.piece, a.vocab));
     const bool whole = half && a.rows && !a.direct && one;      // the head is packed once, whole
     if (whole) launch_bf16_pack_head(s, a, 0, a.vocab);
-    if (a.rows && half && !along) launch_bf16_entries(s, a, whole);
+    if (a.rows && half && teacher && !along) launch_bf16_entries(s, a, whole);
     for (int v0 = 0; v0 < a.vocab; v0 += a.piece) {
         const int vn = std::min(a.piece, a.vocab - v0);
         if (a.rows) {
@@ -155,17 +157,12 @@ int backward(const tr_loss_config *c, void *ws, size_t ws_bytes, void *stream, c
                 if (!a.direct && !whole) launch_bf16_pack_head(s, a, v0, vn);
                 launch_bf16_probabilities(s, a, v0, vn, along && v0 == 0);
             } else launch_f32_probabilities(s, a, v0, vn);
-            if (v0 == 0) launch_loss_values(s, a, one);
-            if (!one) launch_loss_scatter(s, a, v0, vn);
-            if (a.d_hidden) {
-                if (half) launch_bf16_hidden_grad(s, a, v0, vn, v0 == 0);
-                else launch_f32_hidden_grad(s, a, v0, vn, v0 == 0);
-            }
+            if (teacher && v0 == 0) launch_loss_values(s, a, one);
+            if (teacher && !one) launch_loss_scatter(s, a, v0, vn);
+            if (half && a.d_hidden) launch_bf16_hidden_grad(s, a, v0, vn, v0 == 0);
         }
-        if (a.d_weight) {
-            if (half) launch_bf16_weight_grad(s, a, v0, vn);
-            else launch_f32_weight_grad(s, a, v0, vn);
-        }
+        if (!half) launch_f32_gradients(s, a, v0, vn, v0 == 0);
+        else if (a.d_weight) launch_bf16_weight_grad(s, a, v0, vn);
     }
     if (a.d_hidden) launch_loss_hidden_grad(s, a);
     return enqueued();

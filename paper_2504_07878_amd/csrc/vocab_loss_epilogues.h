@@ -82,4 +82,13 @@ template <int N, class Value, class Offset> __device__ __forceinline__ float2 co
     return make_float2(top, sum);
 }
 
+// p - 1 of cross entropy's own entry, at place `at` of a run of products c(0) .. c(7), weighed
+template <class Product> __device__ __forceinline__ float less_one(Product c, unsigned at, float weight, float lse)
+{
+    float z = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) z = at == e ? c(e) : z;
+    return weight * (expf(z - lse) - 1.f);
+}
+
 }  // namespace tr

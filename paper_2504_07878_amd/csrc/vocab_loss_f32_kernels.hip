@@ -3,9 +3,9 @@
 //
 // A workgroup of 4 wavefronts (2 x 2, an accumulator of 32 x 32 each) computes a 64 x 64 block of C[n][m] = sum_k A[m][k] B[n][k] in steps of 32 k: both operands
 // go through registers into LDS as [row][k], two steps ahead, in two buffers. A lane reads four k at a time: k = 8 g + 4 (lane / 32) + j for the j-th product of group g.
-// Small blocks, since models of this type are small: they have to fill the chip. Bound by latency there: 133 of 190 rows x 4096 x 256 take 11 us for the softmax, 13 and 10 us for
-// the gradients (5 us of each for a single step; blocks of 128 x 128, 16 k a step, in one buffer: 52, 40 and 33; one step ahead, and loads that waited for each other: 21, 13
-// and 11, 19 of the first for the listed entries). Three products:
+// Small blocks, since models of this type are small: they have to fill the chip. Bound by latency there: 133 of 190 rows x 4096 x 256 take 11 us for the softmax, 16 us for
+// both gradients (5 us for a single step; blocks of 128 x 128, 16 k a step, in one buffer, the gradients apart: 52, 40 and 33; one step ahead, and loads that waited for each
+// other: 21, 13 and 11, 19 of the first for the listed entries). 1024 rows x 32768 x 896: 97 TFLOP/s (a library product 112 to 141). Three products:
 //   softmax, probabilities: m = vocabulary entry, n = row that counts, k = feature
 //   gradient to the hidden rows: m = feature, n = row, k = vocabulary entry of the piece; summed over the pieces in `acc`, one sum per split of k
 //   gradient to the head: m = feature, n = vocabulary entry, k = row
@@ -264,26 +264,32 @@ template <class WT> __global__ __launch_bounds__(256) void f32_probabilities_ker
         n += n0; m += m0;
         if (n >= count) return;
         const float lse = a.lse[a.idx[n]], weight = a.grad[a.idx[n]] / a.head->scale;
+        float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = m + e < vn ? weight * expf(fmaf(v[e], k, -lse)) : 0.f;
-        store_run((float *)a.G + (size_t)n * a.g_ld + m, v);
+        for (int e = 0; e < 8; ++e) x[e] = m + e < vn ? weight * expf(fmaf(v[e], k, -lse)) : 0.f;
+        const unsigned own = a.teacher ? ~0u : (unsigned)(a.ids[a.idx[n]] - v0 - m);
+        if (own < 8) {
+            const float own_x = less_one([&](int e) { return v[e]; }, own, weight, lse);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = own == e ? own_x : x[e];
+        }
+        store_run((float *)a.G + (size_t)n * a.g_ld + m, x);
     });
 }
 
-// blockIdx.z: split of the piece's vocabulary, its sums in acc[split]
-template <class WT> __global__ __launch_bounds__(256) void f32_hidden_grad_kernel(LossArgs a, int v0, int vn, int per, int first)
+// split: of the piece's vocabulary, its sums in acc[split]
+template <class WT> __device__ __forceinline__ void hidden_grad(const LossArgs &a, int v0, int vn, int per, int first, int m0, int n0, int split, Tiles &sm)
 {
-    __shared__ Tiles sm;
-    const int m0 = blockIdx.x * F32_BLOCK, n0 = blockIdx.y * F32_BLOCK, count = a.head->count;
+    const int count = a.head->count;
     if (n0 >= count) return;
     const Lines<WT> A((const WT *)a.weight + (long long)v0 * a.ws, a.ws, vn, a.dim);
     const Lines<float> B(a.G, a.g_ld, count, (vn + 7) & ~7);      // (G is zero from vn on to the end of a block)
     f32x16 c[1][1];
-    products<false, true>(A, B, m0, n0, min(vn, (int)blockIdx.z * per), min(vn, ((int)blockIdx.z + 1) * per), sm, c);
+    products<false, true>(A, B, m0, n0, min(vn, split * per), min(vn, (split + 1) * per), sm, c);
     each_run(c, [&](int n, int m, float (&v)[8]) {
         n += n0; m += m0;
         if (m >= a.d_pad) return;
-        float *to = a.acc + ((size_t)blockIdx.z * a.n_pad + n) * a.d_pad + m;
+        float *to = a.acc + ((size_t)split * a.n_pad + n) * a.d_pad + m;
         if (!first) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] += to[e];
@@ -292,10 +298,9 @@ template <class WT> __global__ __launch_bounds__(256) void f32_hidden_grad_kerne
     });
 }
 
-template <class WT> __global__ __launch_bounds__(256) void f32_weight_grad_kernel(LossArgs a, int v0, int vn)
+template <class WT> __device__ __forceinline__ void weight_grad(const LossArgs &a, int v0, int vn, int m0, int n0, Tiles &sm)
 {
-    __shared__ Tiles sm;
-    const int m0 = blockIdx.x * F32_BLOCK, n0 = blockIdx.y * F32_BLOCK, count = a.head->count;
+    const int count = a.head->count;
     const Lines<float, true> A(a.hidden, a.hs, count, a.dim, a.idx);
     const Lines<float> B(a.G, a.g_ld, count, (vn + 7) & ~7);      // (G is zero from vn on to the end of a block)
     f32x16 c[1][1];
@@ -314,6 +319,16 @@ template <class WT> __global__ __launch_bounds__(256) void f32_weight_grad_kerne
             for (int e = 0; e < 8; ++e) if (m + e < a.dim) store_one(to + e, v[e]);
         }
     });
+}
+
+// Both gradients of a piece in one launch: the first `hidden` workgroups (mb x nb blocks of every split) take the rows', the others the head's. Small models' launches are short
+// and wait for each other (133 of 190 rows x 4096 x 256: 12 and 10 us apart, 16 together).
+template <class WT> __global__ __launch_bounds__(256) void f32_gradients_kernel(LossArgs a, int v0, int vn, int per, int first, int hidden, int mb, int nb)
+{
+    __shared__ Tiles sm;
+    const int b = blockIdx.x;
+    if (b < hidden) hidden_grad<WT>(a, v0, vn, per, first, b % mb * F32_BLOCK, b / mb % nb * F32_BLOCK, b / (mb * nb), sm);
+    else weight_grad<WT>(a, v0, vn, (b - hidden) % mb * F32_BLOCK, (b - hidden) / mb * F32_BLOCK, sm);
 }
 
 int blocks(int n) { return (n + F32_BLOCK - 1) / F32_BLOCK; }
@@ -338,22 +353,19 @@ int f32_softmax_parts(const LossArgs &a) { return blocks(a.vocab) * 2; }
 void launch_f32_probabilities(hipStream_t s, const LossArgs &a, int v0, int vn)
 {
     by_head(a, [&](auto wt) {
-        const int extra = v0 == 0 ? entry_blocks(a) : 0;
+        const int extra = v0 == 0 && a.teacher ? entry_blocks(a) : 0;
         hipLaunchKernelGGL((f32_probabilities_kernel<decltype(wt)>), dim3(extra + blocks(vn), blocks(a.rows)), dim3(256), 0, s, a, v0, vn, extra);
     });
 }
 
-void launch_f32_hidden_grad(hipStream_t s, const LossArgs &a, int v0, int vn, bool first)
+void launch_f32_gradients(hipStream_t s, const LossArgs &a, int v0, int vn, bool first)
 {
     by_head(a, [&](auto wt) {
         const int per = ((vn + a.splits - 1) / a.splits + BK - 1) / BK * BK;   // whole steps
-        hipLaunchKernelGGL((f32_hidden_grad_kernel<decltype(wt)>), dim3(blocks(a.dim), blocks(a.rows), a.splits), dim3(256), 0, s, a, v0, vn, per, (int)first);
+        const int mb = blocks(a.dim), nb = blocks(a.rows), hidden = a.d_hidden && a.rows ? mb * nb * a.splits : 0;
+        const int all = hidden + (a.d_weight ? mb * blocks(vn) : 0);
+        if (all) hipLaunchKernelGGL((f32_gradients_kernel<decltype(wt)>), dim3(all), dim3(256), 0, s, a, v0, vn, per, (int)first, hidden, mb, nb);
     });
-}
-
-void launch_f32_weight_grad(hipStream_t s, const LossArgs &a, int v0, int vn)
-{
-    by_head(a, [&](auto wt) { hipLaunchKernelGGL((f32_weight_grad_kernel<decltype(wt)>), dim3(blocks(a.dim), blocks(vn)), dim3(256), 0, s, a, v0, vn); });
 }
 
 }  // namespace tr

@@ -69,6 +69,13 @@ template <class HT> __device__ __forceinline__ void pack_row(const LossArgs &a, 
     }
 }
 
+__device__ __forceinline__ void describe_row(const LossArgs &a, int to, int from, float scale)
+{
+    LossRow x{0.f, 0.f, -1, 0};
+    if (from >= 0) x = LossRow{a.lse[from], a.grad[from] / scale, a.teacher ? -1 : a.ids[from], 0};
+    a.row[to] = x;
+}
+
 // Everything at once for few rows: workgroup j finds row j's place by going over the states of all rows, and packs it; the packed rows past the last are cleared, and
 // with pairs the second halves written, by the workgroups from the end.
 template <bool TEACHER, class HT>
@@ -94,9 +101,11 @@ __global__ __launch_bounds__(256) void loss_prepare_kernel(LossArgs a, int packe
     before = (before_s[0] + before_s[1]) + (before_s[2] + before_s[3]);
     count = (count_s[0] + count_s[1]) + (count_s[2] + count_s[3]);
     const int half = half_of(a, count), own = j < a.rows ? own_s : (int)ROW_SKIP;
+    const float scale = usable(fmaxf(fmaxf(top_s[0], top_s[1]), fmaxf(top_s[2], top_s[3])));
+    const bool describes = a.grad && t == 0;
     if (j == 0 && t == 0) {
         a.head->count = count; a.head->half = half;
-        a.head->scale = usable(fmaxf(fmaxf(top_s[0], top_s[1]), fmaxf(top_s[2], top_s[3])));
+        a.head->scale = scale;
     }
     if (j < a.rows && t == 0) {
         a.state[j] = (unsigned char)own;
@@ -105,12 +114,18 @@ __global__ __launch_bounds__(256) void loss_prepare_kernel(LossArgs a, int packe
     }
     if (!packed) return;
     if (own == ROW_COUNTS) {
-        pack_row<HT>(a, before, j);
-        if (half) pack_row<HT>(a, before + half, j);
+        for (int at = before; at <= before + half; at += half ? half : 1) {
+            pack_row<HT>(a, at, j);
+            if (describes) describe_row(a, at, j, scale);
+        }
     }
     // rows without anything: [count, half or the end), and with pairs [half + count, the end)
     const int firsts = half ? half : packed, gap = firsts - count, all = half ? gap + packed - half - count : gap;
-    for (int i = j; i < all; i += gridDim.x) pack_row<HT>(a, i < gap ? count + i : half + count + (i - gap), -1);
+    for (int i = j; i < all; i += gridDim.x) {
+        const int at = i < gap ? count + i : half + count + (i - gap);
+        pack_row<HT>(a, at, -1);
+        if (describes) describe_row(a, at, -1, scale);
+    }
 }
 
 // For many rows: their states, one thread a row, ...
@@ -165,7 +180,9 @@ __global__ __launch_bounds__(256) void loss_pack_kernel(LossArgs a)
     const int i = blockIdx.x, count = a.head->count, half = a.head->half;
     if (i >= (bf16_products_rows(count, half) + BF16_BLOCK - 1) / BF16_BLOCK * BF16_BLOCK) return;
     const int row = half && i >= half ? i - half : i;
-    pack_row<HT>(a, i, row < count ? a.idx[row] : -1);
+    const int from = row < count ? a.idx[row] : -1;
+    pack_row<HT>(a, i, from);
+    if (a.grad && threadIdx.x == 0) describe_row(a, i, from, a.head->scale);
 }
 
 template <bool TEACHER, class HT> static void rows_of(hipStream_t s, const LossArgs &a)
@@ -261,34 +278,30 @@ template <bool BF16> __device__ __forceinline__ void place_entry(const LossArgs 
     } else ((float *)a.G)[(size_t)i * a.g_ld + v] = x;
 }
 
-// p - q of every listed entry of a row from its product (an id listed twice: p less both shares, in both places), by the row's weight. PLACE: into G right away.
-template <bool TEACHER, bool PLACE, bool BF16>
+// p - q of every listed entry of a teacher's from its product (an id listed twice: p less both shares, in both places), by the row's weight. PLACE: into G right away.
+template <bool PLACE, bool BF16>
 __global__ __launch_bounds__(256) void loss_values_kernel(LossArgs a)
 {
     const int i = blockIdx.x, lane = threadIdx.x & 63;
     if (i >= a.head->count) return;
     const int r = a.idx[i];
     const float lse = a.lse[r], k = 1.0f / a.temperature, weight = a.grad[r] / a.head->scale;
-    const Shares sh = shares_of<TEACHER>(a, r);
+    const Shares sh = shares_of<true>(a, r);
     const long long at0 = (long long)r * a.entries;
     for (int j0 = threadIdx.x - lane; j0 < a.entries; j0 += 256) {
         const int j = j0 + lane;
-        const bool on = j < a.entries && entry_counts<TEACHER>(a, at0 + j);
+        const bool on = j < a.entries && entry_counts<true>(a, at0 + j);
         const int id = on ? a.ids[at0 + j] : -1;
-        float q = 1.f;
-        if (TEACHER) {
-            // a wavefront's 64 shares at a time, each handed to all its lanes
-            q = 0.f;
-            for (int o0 = 0; o0 < a.entries; o0 += 64) {
-                const int o = o0 + lane;
-                const bool other = o < a.entries && entry_counts<TEACHER>(a, at0 + o);
-                const int others = other ? a.ids[at0 + o] : -1;
-                const float share = other ? expf((a.teacher[at0 + o] - sh.top) / a.temperature) / sh.total : 0.f;
-                for (int n = 0; n < min(64, a.entries - o0); ++n) {
-                    const int same = __shfl(others, n);
-                    const float its = __shfl(share, n);
-                    q += same == id ? its : 0.f;
-                }
+        float q = 0.f;
+        for (int o0 = 0; o0 < a.entries; o0 += 64) {       // a wavefront's 64 shares at a time, each handed to all its lanes
+            const int o = o0 + lane;
+            const bool other = o < a.entries && entry_counts<true>(a, at0 + o);
+            const int others = other ? a.ids[at0 + o] : -1;
+            const float share = other ? expf((a.teacher[at0 + o] - sh.top) / a.temperature) / sh.total : 0.f;
+            for (int n = 0; n < min(64, a.entries - o0); ++n) {
+                const int same = __shfl(others, n);
+                const float its = __shfl(share, n);
+                q += same == id ? its : 0.f;
             }
         }
         if (!on) continue;
@@ -299,7 +312,7 @@ __global__ __launch_bounds__(256) void loss_values_kernel(LossArgs a)
     }
 }
 
-template <bool TEACHER, bool BF16>
+template <bool BF16>
 __global__ __launch_bounds__(256) void loss_scatter_kernel(LossArgs a, int v0, int vn)
 {
     const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
@@ -307,43 +320,39 @@ __global__ __launch_bounds__(256) void loss_scatter_kernel(LossArgs a, int v0, i
     if (i >= a.head->count) return;
     const long long from = (long long)a.idx[i] * a.entries + j;
     const int v = a.ids[from] - v0;
-    if (v < 0 || v >= vn || !entry_counts<TEACHER>(a, from)) return;
+    if (v < 0 || v >= vn || !entry_counts<true>(a, from)) return;
     place_entry<BF16>(a, i, v, a.value[at]);
-}
-
-// go(there is a teacher, products are bf16)
-template <class Go> static void by_kind(const LossArgs &a, Go go)
-{
-    using Yes = std::integral_constant<bool, true>;
-    using No = std::integral_constant<bool, false>;
-    if (a.teacher) { if (a.hdt == DT_BF16) go(Yes{}, Yes{}); else go(Yes{}, No{}); }
-    else { if (a.hdt == DT_BF16) go(No{}, Yes{}); else go(No{}, No{}); }
 }
 
 // Few rows take a workgroup each, so that their parts are read at once; many take eight, whose parts lie together.
 void launch_loss_finish(hipStream_t s, const LossArgs &a, int parts)
 {
     if (!a.rows) return;
-    by_kind(a, [&](auto t, auto) {
-        if (a.rows <= 256) hipLaunchKernelGGL((loss_finish_kernel<decltype(t)::value, 1>), dim3(a.rows), dim3(256), 0, s, a, parts);
-        else hipLaunchKernelGGL((loss_finish_kernel<decltype(t)::value, 8>), dim3((a.rows + 7) / 8), dim3(256), 0, s, a, parts);
-    });
+    const auto go = [&](auto teacher) {
+        if (a.rows <= 256) hipLaunchKernelGGL((loss_finish_kernel<decltype(teacher)::value, 1>), dim3(a.rows), dim3(256), 0, s, a, parts);
+        else hipLaunchKernelGGL((loss_finish_kernel<decltype(teacher)::value, 8>), dim3((a.rows + 7) / 8), dim3(256), 0, s, a, parts);
+    };
+    if (a.teacher) go(std::true_type{});
+    else go(std::false_type{});
 }
 
 void launch_loss_values(hipStream_t s, const LossArgs &a, bool place)
 {
     if (!a.rows) return;
-    by_kind(a, [&](auto t, auto b) {
-        if (place) hipLaunchKernelGGL((loss_values_kernel<decltype(t)::value, true, decltype(b)::value>), dim3(a.rows), dim3(256), 0, s, a);
-        else hipLaunchKernelGGL((loss_values_kernel<decltype(t)::value, false, decltype(b)::value>), dim3(a.rows), dim3(256), 0, s, a);
-    });
+    const auto go = [&](auto bf16) {
+        if (place) hipLaunchKernelGGL((loss_values_kernel<true, decltype(bf16)::value>), dim3(a.rows), dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((loss_values_kernel<false, decltype(bf16)::value>), dim3(a.rows), dim3(256), 0, s, a);
+    };
+    if (a.hdt == DT_BF16) go(std::true_type{});
+    else go(std::false_type{});
 }
 
 void launch_loss_scatter(hipStream_t s, const LossArgs &a, int v0, int vn)
 {
     if (!a.rows) return;
     const dim3 grid((unsigned)(((long long)a.rows * a.entries + 255) / 256));
-    by_kind(a, [&](auto t, auto b) { hipLaunchKernelGGL((loss_scatter_kernel<decltype(t)::value, decltype(b)::value>), grid, dim3(256), 0, s, a, v0, vn); });
+    if (a.hdt == DT_BF16) hipLaunchKernelGGL(loss_scatter_kernel<true>, grid, dim3(256), 0, s, a, v0, vn);
+    else hipLaunchKernelGGL(loss_scatter_kernel<false>, grid, dim3(256), 0, s, a, v0, vn);
 }
 
 // ------------------------------------------------------------------ gradient to the hidden rows
