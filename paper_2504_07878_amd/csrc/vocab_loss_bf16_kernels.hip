@@ -449,8 +449,6 @@ template <int TM, int TN> struct HiddenGrad {
     }
 };
 
-__host__ __device__ inline bool on_16_bytes(const LossArgs &a) { return ((reinterpret_cast<uintptr_t>(a.d_weight) | (uintptr_t)(a.dws * 2)) & 15) == 0; }   // the head's gradient is
-
 template <int TM, int TN> struct WeightGrad {
     static constexpr bool A_KC = false, B_KC = false;
     const LossArgs &a;
@@ -488,21 +486,13 @@ template <int TM, int TN> struct WeightGrad {
                 }
             }
             __syncthreads();
-            if (!on_16_bytes(a)) {        // an element a lane, side by side (817 rows x 5003 x 1001: 28 us where a lane stored eight in a row)
-#pragma unroll 4
-                for (int at = threadIdx.x; at < TN * TM; at += WM * WN * 64) {
-                    const int v = at / TM, d = at % TM;
-                    if (v < vs && d < ds) out[(long long)v * a.dws + d] = *reinterpret_cast<const bf16_t *>(dynamic_lds + v * (TM * 2) + (((d >> 3) ^ (v & 15)) << 4) + (d & 7) * 2);
-                }
-                return;
-            }
 #pragma unroll 4
             for (int at = threadIdx.x; at < TN * 16; at += WM * WN * 64) {
                 const int v = at >> 4, d = (at & 15) * 8;
                 if (v >= vs || d >= ds) continue;
                 const uint4 u = *reinterpret_cast<const uint4 *>(dynamic_lds + v * (TM * 2) + (((at & 15) ^ (v & 15)) << 4));
                 bf16_t *to = out + (long long)v * a.dws + d;
-                if (d + 8 <= ds) *reinterpret_cast<uint4 *>(to) = u;
+                if (d + 8 <= ds) store_bits(to, u);
                 else {
                     const uint32_t q[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
@@ -518,7 +508,7 @@ template <int TM, int TN> struct WeightGrad {
 #pragma unroll
                 for (int i = 0; i < MI; ++i) {
                     const uint2 u = rounded(i, j);
-                    if (d0 + i * 16 + 4 <= ds) *reinterpret_cast<uint2 *>(to + i * 16) = u;      // (a gradient on 16 bytes: launch_bf16_weight_grad)
+                    if (d0 + i * 16 + 4 <= ds) store_bits(to + i * 16, u);
                     else {
                         const uint32_t q[2] = {u.x, u.y};
 #pragma unroll
@@ -894,14 +884,13 @@ void launch_bf16_hidden_grad(hipStream_t s, const LossArgs &a, int v0, int vn, b
 // Blocks of 256 x 256 or, several a compute unit, of 128 x 128 in one step's LDS: while one loads or stores another multiplies. Small ones
 //   for few rows, where it is a matter of writing (300 of 500 rows x 151936 x 896: 139 us against 189; 1200 rows x 64000 x 3584 would be 1160 against 1073);
 //   up to more rows for narrow heads whose last large blocks would be half empty (896 features, 4096 rows, three quarters of them counting: 850 against 960 us, 2048 rows x 64000 x 640
-//   383 against 392; but 8192 rows x 64000 x 896 1930 against 1840, 2048 x 64000 x 1024 610 against 602, 8192 x 64000 x 1344 3040 against 2610);
-//   and where rows of the gradient do not lie on 16 bytes, since only they bring whole lines of it together (all gradients of 2048 rows x 32000 x 1001: 483 us against 517).
+//   383 against 392; but 8192 rows x 64000 x 896 1930 against 1840, 2048 x 64000 x 1024 610 against 602, 8192 x 64000 x 1344 3040 against 2610).
 void launch_bf16_weight_grad(hipStream_t s, const LossArgs &a, int v0, int vn)
 {
     using Bl = Block<1, Shape<2, 2, 4, 4, false, false>>;
     const bool half_empty = a.d_pad < 1024 && a.d_pad % 256 && a.d_pad % 256 <= 128;
     const int blocks = up_div(a.d_pad, Bl::TM) * up_div(vn, Bl::TN);
-    if (!on_16_bytes(a) || a.rows <= (half_empty ? 4096 : 1024)) launch<block_kernel<WeightGrad, Bl>>(dim3(up_div(blocks, 8) * 8), 256, Bl::LDS, s, a, v0, vn, 0, 0);
+    if (a.rows <= (half_empty ? 4096 : 1024)) launch<block_kernel<WeightGrad, Bl>>(dim3(up_div(blocks, 8) * 8), 256, Bl::LDS, s, a, v0, vn, 0, 0);
     else launch<turns_kernel<WeightGrad>>(dim3(256), 512, 5 * 256 * BK * 2, s, a, v0, vn, 0);
 }
 

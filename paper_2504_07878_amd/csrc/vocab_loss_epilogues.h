@@ -13,10 +13,12 @@ __device__ __forceinline__ void run_of(const f32x16 &c, int h, float (&v)[8])
     for (int e = 0; e < 8; ++e) v[e] = c[8 * h + e];
 }
 
+// (stores of 8 and 16 bytes need no alignment in global memory: rows of odd length)
+template <class U, class T> __device__ __forceinline__ void store_bits(T *p, const U &u) { __builtin_memcpy(p, &u, sizeof(U)); }
 __device__ __forceinline__ void store_run(float *p, const float (&v)[8])
 {
-    reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-    reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+    store_bits(p, make_float4(v[0], v[1], v[2], v[3]));
+    store_bits(p + 4, make_float4(v[4], v[5], v[6], v[7]));
 }
 __device__ __forceinline__ uint32_t two_bf16(float a, float b)
 {
@@ -25,7 +27,7 @@ __device__ __forceinline__ uint32_t two_bf16(float a, float b)
 }
 __device__ __forceinline__ void store_run(bf16_t *p, const float (&v)[8])
 {
-    *reinterpret_cast<uint4 *>(p) = make_uint4(two_bf16(v[0], v[1]), two_bf16(v[2], v[3]), two_bf16(v[4], v[5]), two_bf16(v[6], v[7]));
+    store_bits(p, make_uint4(two_bf16(v[0], v[1]), two_bf16(v[2], v[3]), two_bf16(v[4], v[5]), two_bf16(v[6], v[7])));
 }
 __device__ __forceinline__ void store_one(float *p, float v) { *p = v; }
 __device__ __forceinline__ void store_one(bf16_t *p, float v) { *p = (bf16_t)two_bf16(v, 0.f); }

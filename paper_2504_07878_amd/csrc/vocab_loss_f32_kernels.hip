@@ -19,53 +19,52 @@ namespace {
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 constexpr int BK = 32, PITCH = BK + 4;       // 16-byte reads of 16 rows meet 16 different places of the 64 banks
 
-// N elements of a line from p on, which lies on 16 bytes and has them, as fp32
-template <int N> __device__ __forceinline__ void widened(const float *p, float (&v)[N])
+// Loads of 16 or 8 bytes from any element on (global loads need no alignment here): lines of odd length need them (gradients of 58 rows x 10911 x 1397 over a bf16 head: element
+// by element, under conditions, 252 us, so 121; with 1400 features 97).
+typedef f32x4 __attribute__((aligned(2))) loose16;
+typedef __attribute__((ext_vector_type(2), aligned(2))) uint32_t loose8;
+
+// four elements of a line from p on, as fp32
+__device__ __forceinline__ void four_of(const float *p, float (&v)[4])
 {
+    const f32x4 x = *reinterpret_cast<const loose16 *>(p);
 #pragma unroll
-    for (int q = 0; q < N; q += 4) {
-        const f32x4 x = *reinterpret_cast<const f32x4 *>(p + q);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[q + e] = x[e];
-    }
+    for (int e = 0; e < 4; ++e) v[e] = x[e];
 }
-template <int N> __device__ __forceinline__ void widened(const bf16_t *p, float (&v)[N])
+__device__ __forceinline__ void four_of(const bf16_t *p, float (&v)[4])
 {
-    uint32_t u[N / 2];
-    if constexpr (N == 8) *reinterpret_cast<uint4 *>(u) = *reinterpret_cast<const uint4 *>(p);
-    else *reinterpret_cast<uint2 *>(u) = *reinterpret_cast<const uint2 *>(p);
-#pragma unroll
-    for (int q = 0; q < N; q += 2) { v[q] = __uint_as_float(u[q / 2] << 16); v[q + 1] = __uint_as_float(u[q / 2] & 0xffff0000u); }
+    const loose8 u = *reinterpret_cast<const loose8 *>(p);
+    v[0] = __uint_as_float(u.x << 16); v[1] = __uint_as_float(u.x & 0xffff0000u); v[2] = __uint_as_float(u.y << 16); v[3] = __uint_as_float(u.y & 0xffff0000u);
 }
-// ... from j on, wherever it lies; zeros at or past `limit` and where there is no line
-template <int N, class T> __device__ __forceinline__ void widened(const T *line, int j, int limit, bool wide, float (&v)[N])
+// N from j on, zeros at or past `limit`: elements one by one, under no condition, which would have each load wait for the one before
+template <int N, class T> __device__ __forceinline__ void some_of(const T *line, int j, int limit, float (&v)[N])
 {
-    if (line && wide && j + N <= limit) widened(line + j, v);
-    else {
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = line && j + e < limit ? load_one(line + j + e) : 0.f;
-    }
+    for (int e = 0; e < N; ++e) v[e] = load_one(line + min(j + e, limit - 1));
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = j + e < limit ? v[e] : 0.f;
 }
 
 // An operand is lines of memory: line o, o < lines, has elements 0 .. limit - 1 from p + o * ld on, with a list from p + list[o] * ld. ALONG_K: a line is a row of the
-// operand (k runs along it); otherwise it is one k. wide: lines lie on 16 bytes; regular: eight elements are there or not together.
+// operand (k runs along it); otherwise it is one k.
 template <class T, bool LISTED = false> struct Lines {
-    const T *p; long long ld; int lines, limit; const int *list; bool wide, regular;
-    __device__ __forceinline__ Lines(const void *p_, long long ld_, int lines_, int limit_, const int *list_ = nullptr) : p((const T *)p_), ld(ld_), lines(lines_), limit(limit_), list(list_)
-    {
-        wide = ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * sizeof(T))) & 15) == 0;
-        regular = wide && limit % 8 == 0;
-    }
+    const T *p; long long ld; int lines, limit; const int *list;
+    __device__ __forceinline__ Lines(const void *p_, long long ld_, int lines_, int limit_, const int *list_ = nullptr) : p((const T *)p_), ld(ld_), lines(lines_), limit(limit_), list(list_) {}
     __device__ __forceinline__ int place(int o) const { return LISTED ? list[min(o, lines - 1)] : min(o, lines - 1); }    // of line o, or of the last
 };
 
 struct alignas(16) Tiles { float a[2][F32_BLOCK * PITCH], b[2][F32_BLOCK * PITCH]; };
 
+// How an operand's eight elements in a run are read: where lines are multiples of eight long, they are there or not together; otherwise the last ones of a line are read from where
+// eight are left, and moved down; lines shorter than eight element by element.
+enum { EIGHTS, MOVED, SINGLES };
+
 // A thread's eight elements of the tiles (64 x 32) from row0 on, step after step from k0 on: of a row, or of a k (whose place is read a step ahead); zeros where there
-// is nothing. REGULAR: read as they are, under no condition, from the nearest place that is there, and widened when they are used: until then nothing waits for them.
-template <bool ALONG_K, bool REGULAR, class Op> struct Steps {
+// is nothing. Read as they are, under no condition, from the nearest place that is there, and widened when they are used: until then nothing waits for them.
+template <bool ALONG_K, int HOW, class Op> struct Steps {
     using T = std::remove_const_t<std::remove_pointer_t<decltype(Op::p)>>;
-    struct Read { f32x4 u[sizeof(T) == 4 || !REGULAR ? 2 : 1]; bool there; };
+    static constexpr bool RAW = sizeof(T) == 2 && HOW != SINGLES;
+    struct Read { f32x4 u[RAW ? 1 : 2]; int down; };     // down: places to move by, 8: nothing is there
     const Op &op;
     int place, line, along;
     __device__ __forceinline__ Steps(const Op &op_, int row0, int k0) : op(op_)
@@ -78,16 +77,17 @@ template <bool ALONG_K, bool REGULAR, class Op> struct Steps {
     __device__ __forceinline__ void next(Read &r)
     {
         const T *at = op.p + place * op.ld;
-        r.there = line < op.lines && along < op.limit;
-        if constexpr (REGULAR) {
-            at += min(along, op.limit - 8);
-            r.u[0] = *reinterpret_cast<const f32x4 *>(at);
-            if constexpr (sizeof(T) == 4) r.u[1] = *reinterpret_cast<const f32x4 *>(at + 4);
-        } else {
+        if constexpr (HOW == SINGLES) {
             float v[8];
-            widened(r.there ? at : nullptr, along, op.limit, op.wide, v);
+            some_of(at, along, op.limit, v);
             r.u[0] = f32x4{v[0], v[1], v[2], v[3]};
             r.u[1] = f32x4{v[4], v[5], v[6], v[7]};
+            r.down = line < op.lines ? 0 : 8;
+        } else {
+            const int from = min(along, op.limit - 8);
+            r.u[0] = *reinterpret_cast<const loose16 *>(at + from);
+            if constexpr (!RAW) r.u[1] = *reinterpret_cast<const loose16 *>(at + from + 4);
+            r.down = line < op.lines ? along - from : 8;
         }
         if (ALONG_K) along += BK;
         else { line += BK; place = op.place(line); }
@@ -96,9 +96,15 @@ template <bool ALONG_K, bool REGULAR, class Op> struct Steps {
     {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            if constexpr (sizeof(T) == 4 || !REGULAR) v[e] = r.u[e >> 2][e & 3];
+            if constexpr (!RAW) v[e] = r.u[e >> 2][e & 3];
             else v[e] = __uint_as_float(e & 1 ? __float_as_uint(r.u[0][e >> 1]) & 0xffff0000u : __float_as_uint(r.u[0][e >> 1]) << 16);
-            v[e] = r.there ? v[e] : 0.f;
+            v[e] = r.down < 8 ? v[e] : 0.f;
+        }
+        if constexpr (HOW == MOVED) {
+#pragma unroll
+            for (int by = 4; by; by >>= 1)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = !(r.down & by) ? v[e] : e + by < 8 ? v[e + by < 8 ? e + by : e] : 0.f;
         }
     }
     static __device__ __forceinline__ void write(float *lds, const Read &r)
@@ -124,15 +130,15 @@ __device__ __forceinline__ void lds_barrier()
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
-template <bool A_ALONG, bool B_ALONG, bool REGULAR, class A, class B>
+template <bool A_ALONG, bool B_ALONG, int HOW, class A, class B>
 __device__ __forceinline__ void products_of(const A &a, const B &b, int m0, int n0, int k_lo, int k_hi, Tiles &sm, f32x16 (&c)[1][1])
 {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const int arow = (w >> 1) * 32 + tile_feature(lane & 31), brow = (w & 1) * 32 + (lane & 31), at = (lane >> 5) * 4;
-    Steps<A_ALONG, REGULAR, A> from_a(a, m0, k_lo);
-    Steps<B_ALONG, REGULAR, B> from_b(b, n0, k_lo);
-    typename Steps<A_ALONG, REGULAR, A>::Read ra[2];
-    typename Steps<B_ALONG, REGULAR, B>::Read rb[2];
+    Steps<A_ALONG, HOW, A> from_a(a, m0, k_lo);
+    Steps<B_ALONG, HOW, B> from_b(b, n0, k_lo);
+    typename Steps<A_ALONG, HOW, A>::Read ra[2];
+    typename Steps<B_ALONG, HOW, B>::Read rb[2];
     from_a.next(ra[0]); from_b.next(rb[0]);
     from_a.next(ra[1]); from_b.next(rb[1]);
     const auto step = [&](auto buffer) {
@@ -164,8 +170,9 @@ __device__ __forceinline__ void products(const A &a, const B &b, int m0, int n0,
 #pragma unroll
     for (int r = 0; r < 16; ++r) c[0][0][r] = 0.f;
     if (k_lo >= k_hi) return;
-    if (a.regular && b.regular) products_of<A_ALONG, B_ALONG, true>(a, b, m0, n0, k_lo, k_hi, sm, c);
-    else products_of<A_ALONG, B_ALONG, false>(a, b, m0, n0, k_lo, k_hi, sm, c);
+    if (((a.limit | b.limit) & 7) == 0) products_of<A_ALONG, B_ALONG, EIGHTS>(a, b, m0, n0, k_lo, k_hi, sm, c);
+    else if (min(a.limit, b.limit) >= 8) products_of<A_ALONG, B_ALONG, MOVED>(a, b, m0, n0, k_lo, k_hi, sm, c);
+    else products_of<A_ALONG, B_ALONG, SINGLES>(a, b, m0, n0, k_lo, k_hi, sm, c);
 }
 
 // f(n, first m of a run of 8, the run) for every run of the block
@@ -196,7 +203,6 @@ template <class WT> __device__ __forceinline__ void entries_group(const LossArgs
         on = id >= 0 && id < a.vocab;
         if (on) w += id * a.ws;
     }
-    const bool wide = ((reinterpret_cast<uintptr_t>(a.hidden) | (uintptr_t)(a.hs * 4) | reinterpret_cast<uintptr_t>(a.weight) | (uintptr_t)(a.ws * sizeof(WT))) & 15) == 0;
     f32x16 c;
 #pragma unroll
     for (int r = 0; r < 16; ++r) c[r] = 0.f;
@@ -207,16 +213,20 @@ template <class WT> __device__ __forceinline__ void entries_group(const LossArgs
         for (int q = 0; q < 4; ++q) c = __builtin_amdgcn_mfma_f32_32x32x2f32(x[g][q], y[g][q], c, 0, 0, 0);
     };
     int k0 = 0;
-    if (wide)
-        for (; k0 + 8 * AT_ONCE <= a.dim; k0 += 8 * AT_ONCE) {
+    for (; k0 + 8 * AT_ONCE <= a.dim; k0 += 8 * AT_ONCE) {
 #pragma unroll
-            for (int g = 0; g < AT_ONCE; ++g) { widened(w + k0 + 8 * g + 4 * hf, x[g]); widened(h + k0 + 8 * g + 4 * hf, y[g]); }
+        for (int g = 0; g < AT_ONCE; ++g) { four_of(w + k0 + 8 * g + 4 * hf, x[g]); four_of(h + k0 + 8 * g + 4 * hf, y[g]); }
 #pragma unroll
-            for (int g = 0; g < AT_ONCE; ++g) multiply(g);
-        }
-    for (; k0 < a.dim; k0 += 8) {
-        widened(w, k0 + 4 * hf, a.dim, wide, x[0]);
-        widened(h, k0 + 4 * hf, a.dim, wide, y[0]);
+        for (int g = 0; g < AT_ONCE; ++g) multiply(g);
+    }
+    for (; k0 + 8 <= a.dim; k0 += 8) {
+        four_of(w + k0 + 4 * hf, x[0]);
+        four_of(h + k0 + 4 * hf, y[0]);
+        multiply(0);
+    }
+    if (k0 < a.dim) {
+        some_of(w, k0 + 4 * hf, a.dim, x[0]);
+        some_of(h, k0 + 4 * hf, a.dim, y[0]);
         multiply(0);
     }
     // row m of column n lies in register (m / 8) * 4 + m % 4 of lane n + 32 * (m / 4 % 2)
@@ -306,14 +316,13 @@ template <class WT> __device__ __forceinline__ void weight_grad(const LossArgs &
     f32x16 c[1][1];
     products<false, false>(A, B, m0, n0, 0, count, sm, c);
     const float k = a.head->scale * a.temperature;
-    const bool wide = ((reinterpret_cast<uintptr_t>(a.d_weight) | (uintptr_t)(a.dws * sizeof(WT))) & 15) == 0;
     each_run(c, [&](int n, int m, float (&v)[8]) {
         n += n0; m += m0;
         if (n >= vn) return;
         WT *to = (WT *)a.d_weight + (long long)(v0 + n) * a.dws + m;
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] *= k;
-        if (wide && m + 8 <= a.dim) store_run(to, v);
+        if (m + 8 <= a.dim) store_run(to, v);
         else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) if (m + e < a.dim) store_one(to + e, v[e]);

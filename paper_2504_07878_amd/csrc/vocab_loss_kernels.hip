@@ -369,8 +369,13 @@ __global__ __launch_bounds__(256) void hidden_grad_kernel(LossArgs a)
     auto add = [&](float4 &to, const float4 u) { to.x += u.x; to.y += u.y; to.z += u.z; to.w += u.w; };
     auto store = [&](int r, const float (&x)[4]) {
         HT *out = (HT *)a.d_hidden + (long long)r * a.dhs + j;
+        if (j + 4 <= a.dim) {
+            if constexpr (sizeof(HT) == 2) store_bits(out, make_uint2(two_bf16(x[0], x[1]), two_bf16(x[2], x[3])));
+            else store_bits(out, make_float4(x[0], x[1], x[2], x[3]));
+        } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) if (j + e < a.dim) store_one(out + e, x[e]);
+            for (int e = 0; e < 4; ++e) if (j + e < a.dim) store_one(out + e, x[e]);
+        }
     };
     if (i < count) {
         const int half = BF16 ? a.head->half : 0, rows = BF16 ? bf16_products_rows(count, half) : a.n_pad, splits = BF16 ? bf16_splits(a, rows) : a.splits;
