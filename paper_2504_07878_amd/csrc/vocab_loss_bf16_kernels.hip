@@ -804,10 +804,13 @@ template <template <int, int> class Job_> __global__ __launch_bounds__(512) void
     if (!second) barrier();
 }
 
-__global__ __launch_bounds__(128) void bf16_pack_head_kernel(LossArgs a, int v0)
+// (a thread takes eight elements, wherever rows begin: 28958 rows of 126 18 us with a workgroup a row, so 6)
+__global__ __launch_bounds__(256) void bf16_pack_head_kernel(LossArgs a, int v0, int vn)
 {
-    const bf16_t *w = (const bf16_t *)a.weight + (long long)(v0 + blockIdx.x) * a.ws;
-    for (int k = threadIdx.x * 8; k < a.d_pad; k += 1024) *reinterpret_cast<uint4 *>((bf16_t *)a.wp + (size_t)blockIdx.x * a.d_pad + k) = load8(w, k, a.dim);
+    const int eights = a.d_pad / 8;
+    const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
+    const int v = (int)(at / eights), k = (int)(at - (long long)v * eights) * 8;
+    if (v < vn) *reinterpret_cast<uint4 *>((bf16_t *)a.wp + (size_t)v * a.d_pad + k) = load8((const bf16_t *)a.weight + (v0 + v) * a.ws, k, a.dim);
 }
 
 int up_div(int n, int by) { return (n + by - 1) / by; }
@@ -860,7 +863,7 @@ template <template <int, int> class Job> void launch_job(hipStream_t s, const Lo
 
 void launch_bf16_pack_head(hipStream_t s, const LossArgs &a, int v0, int vn)
 {
-    hipLaunchKernelGGL(bf16_pack_head_kernel, dim3(vn), dim3(128), 0, s, a, v0);
+    hipLaunchKernelGGL(bf16_pack_head_kernel, dim3((unsigned)(((long long)vn * (a.d_pad / 8) + 255) / 256)), dim3(256), 0, s, a, v0, vn);
 }
 
 void launch_bf16_entries(hipStream_t s, const LossArgs &a, bool packed) { hipLaunchKernelGGL(bf16_entries_kernel, dim3(entry_groups(a)), dim3(64), 0, s, a, packed); }
@@ -882,6 +885,7 @@ void launch_bf16_hidden_grad(hipStream_t s, const LossArgs &a, int v0, int vn, b
 }
 
 // Blocks of 256 x 256 or, several a compute unit, of 128 x 128 in one step's LDS: while one loads or stores another multiplies. Small ones
+//   where there are few (small_blocks: 1280 rows x 275 x 1366 38 -> 24 us);
 //   for few rows, where it is a matter of writing (300 of 500 rows x 151936 x 896: 139 us against 189; 1200 rows x 64000 x 3584 would be 1160 against 1073);
 //   up to more rows for narrow heads whose last large blocks would be half empty (896 features, 4096 rows, three quarters of them counting: 850 against 960 us, 2048 rows x 64000 x 640
 //   383 against 392; but 8192 rows x 64000 x 896 1930 against 1840, 2048 x 64000 x 1024 610 against 602, 8192 x 64000 x 1344 3040 against 2610).
@@ -890,7 +894,7 @@ void launch_bf16_weight_grad(hipStream_t s, const LossArgs &a, int v0, int vn)
     using Bl = Block<1, Shape<2, 2, 4, 4, false, false>>;
     const bool half_empty = a.d_pad < 1024 && a.d_pad % 256 && a.d_pad % 256 <= 128;
     const int blocks = up_div(a.d_pad, Bl::TM) * up_div(vn, Bl::TN);
-    if (a.rows <= (half_empty ? 4096 : 1024)) launch<block_kernel<WeightGrad, Bl>>(dim3(up_div(blocks, 8) * 8), 256, Bl::LDS, s, a, v0, vn, 0, 0);
+    if (a.rows <= (half_empty ? 4096 : 1024) || small_blocks(a.d_pad, vn)) launch<block_kernel<WeightGrad, Bl>>(dim3(up_div(blocks, 8) * 8), 256, Bl::LDS, s, a, v0, vn, 0, 0);
     else launch<turns_kernel<WeightGrad>>(dim3(256), 512, 5 * 256 * BK * 2, s, a, v0, vn, 0);
 }
 
