@@ -95,8 +95,11 @@ int arguments(const tr_loss_config *c, const tr_loss_rows *in, void *ws, size_t 
         a.hp = b + p.hp; a.wp = b + p.wp; a.row = (LossRow *)(b + p.row);
         a.pairs = gradient;
         const int rows = gradient && a.rows <= PAIR_ROWS ? 2 * a.rows : a.rows;
-        a.n_block = rows <= 64 || in_planes(c) ? 64 : rows <= 128 ? 128 : 256;
-        if (a.n_block < 256 && !in_planes(c)) a.part_ld = a.n_block;
+        // Few rows in blocks of 256 entries x 64 or 128 rows, up to 256 rows (151936 x 896, 160 rows, blocks of 256 instead: gradients 316 us against 297; 300 rows 423 against 425).
+        // Losses of small heads, where that leaves most compute units without a block, in small ones (100 rows x 30000 x 512: 21 -> 17 us; gradients would be 53 -> 59).
+        const bool small = !gradient && c->vocab <= 128 * BF16_BLOCK;
+        a.n_block = rows <= 64 || in_planes(c) ? 64 : rows <= 256 && !small ? 128 : 256;
+        if (rows <= a.n_block && a.n_block < 256 && !in_planes(c)) a.part_ld = a.n_block;
         if (!a.direct) a.piece = std::min(p.piece, p.packed);
     }
     return TR_OK;

@@ -38,7 +38,7 @@ __device__ __forceinline__ int row_state(const LossArgs &a, int r)
 
 // weights that cannot be divided by (none, infinite, too small for a reciprocal share) are taken as they are
 __device__ __forceinline__ float usable(float top) { return top > 1e-30f && top < INFINITY ? top : 1.f; }
-__device__ __forceinline__ int half_of(const LossArgs &a, int count) { return !a.pairs || count == 0 || count > PAIR_ROWS ? 0 : count > 64 ? 128 : count > 32 ? 64 : 32; }
+__device__ __forceinline__ int half_of(const LossArgs &a, int count) { return !a.pairs || count == 0 || count > PAIR_ROWS ? 0 : PAIR_ROWS; }
 
 __device__ __forceinline__ void skipped(const LossArgs &a, int r, int st)
 {
