@@ -8,9 +8,9 @@
 // All in steps of 64 k. Both operands of a step are copied to LDS by direct loads, as they lie in memory; an operand with k from row to row is turned where it is read
 // (the transposing LDS read). Within a tile the 16-byte pieces of a line (or the 32-byte pieces, where k runs from row to row) are permuted by the line, on the way in through
 // the lanes' addresses, so that reads meet no bank conflicts. Three schedules:
-//   turns_kernel    blocks of 256 x 256, for more than 256 rows. Bound by the chip's power: 6144 rows x 151936 x 896 (8192, three quarters of them counting) take 1530 us for the
-//                   softmax, 1.09 PFLOP/s; 2048 rows x 152064 x 3584 1780 us, 1.25 PFLOP/s (a library product of 8192^3: 1.30, of 4096 x 151936 x 896: 0.98). The clock falls
-//                   as the pipes get busier, so that schedules that fill them better gain less than they fill.
+//   turns_kernel    blocks of 256 x 256, for more than 256 rows. 6144 rows x 151936 x 896 (8192, three quarters of them counting) take 1510 us for the softmax, 1.11 PFLOP/s with
+//                   the matrix pipes 52 % busy at 2.0 GHz; 2048 rows x 152064 x 3584 1790 us, 1.25 PFLOP/s, 61 % at 1.9 GHz (a library product of 8192^3: 1.30, of
+//                   4096 x 151936 x 896: 0.98). Bound by power and copies together, 1.6 us a step, and by what lies between two blocks, 5 us: the exponentials.
 //   stream_kernel   blocks of 256 x 64 or 128, for fewer rows. Bound by the head's bytes: 272 MB in 50 us, 5.4 TB/s, what copies reach here.
 //   block_kernel    blocks of 128 x 128, where there are few blocks, and for the gradient to the head of few rows.
 #include "vocab_loss_epilogues.h"
