@@ -35,6 +35,7 @@ def collect(slm, llm, prompts, tokens, top: int = 16):
 
 def adapt_head(head, hidden, ids, teacher, targets, steps: int = 20, rate: float = None, share: float = 0.5, temperature: float = 2.0):
     """Gradient descent on the LM head [vocab][d] (float32 or bfloat16): `share` of the loss is distillation, the rest cross entropy, both means over the rows that count.
+
     hidden: float32 as `collect` gives them, or bfloat16, with which the gradients over a bfloat16 head run on bf16 matrix instructions, several times as fast.
     rate: None takes 1 / (mean |hidden|^2 / 2), the inverse of a bound on the curvature of both losses in the head (a softmax's second derivative is at most 1/2; T^2 makes
     up for 1/T twice), with which every step goes down. Returns (new head in the head's type, losses of the steps as a list of floats). Updates are kept in fp32.
