@@ -441,3 +441,26 @@ def test_the_vocabulary_in_pieces(losses, dim, entries, types):
     check(got, t, 1.5 if entries else 1.0)
     whole = call(losses, t, 1.5 if entries else 1.0)
     assert torch.equal(got["loss"], whole["loss"]) and torch.equal(got["lse"], whole["lse"])
+
+
+@pytest.mark.parametrize("types", TYPES, ids=["f32", "f32_rows", "bf16"])
+@pytest.mark.parametrize("size", [(40, 131, 300), (150, 200, 700), (5, 7, 9)], ids=str)
+def test_rows_that_begin_at_any_element(losses, size, types):
+    """Inputs and gradients three elements into their rows' room: the same bits as from tensors by themselves, and nothing beside them is written over."""
+    n, d, v = size
+    t = make(n, d, v, *types, seed=41)
+    want = call(losses, t)
+    check(want, t)
+
+    def inside(x):
+        room = torch.full((x.shape[0], d + 6), 5.0, dtype=x.dtype, device="cuda")
+        room[:, 3:3 + d] = x
+        return room, room[:, 3:3 + d]
+
+    (_, hidden), (_, weight) = inside(t["hidden"]), inside(t["weight"])
+    (room_h, d_hidden), (room_w, d_weight) = inside(torch.zeros_like(t["hidden"])), inside(torch.zeros_like(t["weight"]))
+    got = call(losses, t | {"hidden": hidden, "weight": weight}, d_hidden=d_hidden, d_weight=d_weight)
+    for k in want:
+        assert torch.equal(got[k], want[k]), k
+    for room in (room_h, room_w):
+        assert (room[:, :3] == 5).all() and (room[:, 3 + d:] == 5).all()
