@@ -46,7 +46,7 @@ struct LossArgs {
     float *value;                 // [n_pad][entries] products of the listed entries, then what G has there
     void *G;                      // [n_pad][g_ld], a piece's columns; lines are not a power of two apart, so that a column's do not meet in one memory channel
     float *acc;                   // [splits][n_pad, or the blocks that count (bf16)][d_pad] sums of the gradient to the hidden rows
-    void *hp;                     // [n_pad][d_pad] rows that count (bf16 products)
+    void *hp;                     // [n_pad][d_pad] rows that count (bf16 products), fp32 rows in three planes
     LossRow *row;                 // [n_pad] theirs
     void *wp;                     // [piece][d_pad] rows of the head where they cannot be read as they lie
     int n_pad, d_pad, piece, g_ld, splits, part_ld;
@@ -70,11 +70,11 @@ void launch_loss_scatter(hipStream_t s, const LossArgs &a, int v0, int vn);
 // The gradient to the hidden rows from the splits' sums (as the bf16 or the f32 products leave them), weighed and rounded; zeros for rows that do not count.
 void launch_loss_hidden_grad(hipStream_t s, const LossArgs &a);
 
-// Products of the listed entries, each the bits that the softmax's own products have: a probability near 1 and its logit then agree, and what is left of
-// 1 - p and of lse - z is not the difference of two roundings.
+// Products of the listed entries, each the bits that the softmax's and the probabilities' own products have, for every pair of types: the products' roundings are the same in z and in lse,
+// so that nothing of them is left in lse - z and 1 - p where p is near 1. A loss has no rounding of lse in it either; a gradient is given lse as fp32, and 1 - p keeps that rounding, 2^-24 |lse|.
 void launch_bf16_entries(hipStream_t s, const LossArgs &a, bool packed);   // packed: a.wp holds the whole head
 
-// Products on 32-bit matrix instructions, operands of either type and any stride (vocab_loss_f32_kernels.hip). Blocks of 64 x 64. The
+// Products on 32-bit matrix instructions, any stride (vocab_loss_f32_kernels.hip): fp32 rows and head, the gradients over a bf16 head too. Blocks of 64 x 64. The
 // softmax and the first piece's probabilities bring the products of the listed entries.
 constexpr int F32_BLOCK = 64;
 void launch_f32_softmax(hipStream_t s, const LossArgs &a);
@@ -82,7 +82,7 @@ int f32_softmax_parts(const LossArgs &a);
 void launch_f32_probabilities(hipStream_t s, const LossArgs &a, int v0, int vn);
 void launch_f32_gradients(hipStream_t s, const LossArgs &a, int v0, int vn, bool first);     // those asked for
 
-// bf16 rows and head (vocab_loss_bf16_kernels.hip): blocks of 256 vocabulary entries or features.
+// bf16 rows and head (vocab_loss_bf16_kernels.hip): blocks of 256 vocabulary entries or features. Softmax and probabilities of fp32 rows over a bf16 head too.
 constexpr int BF16_BLOCK = 256;
 void launch_bf16_pack_head(hipStream_t s, const LossArgs &a, int v0, int vn);
 // entries: the listed entries' products too, in the same launch (blocks of fewer than 256 rows only)

@@ -28,7 +28,8 @@ struct Plan {
 };
 
 bool is_bf16(const tr_loss_config *c) { return c->hidden_dtype == TR_BF16; }                                    // all products run on bf16 matrix instructions
-bool in_planes(const tr_loss_config *c) { return c->hidden_dtype == TR_F32 && c->weight_dtype == TR_BF16; }   // those of the softmax do, on rows in three planes
+// those of the softmax and of the probabilities do, on rows in three planes: the gradients take exp(z - lse) of the very products that lse was summed from
+bool in_planes(const tr_loss_config *c) { return c->hidden_dtype == TR_F32 && c->weight_dtype == TR_BF16; }
 
 // G stays at 512 MB or less, but a piece has 2048 columns at least (8192 rows x 151936 x 896, three quarters of the rows counting, all products of the gradients, pieces of
 // 256 / 512 / 1024 MB: 5.60 / 5.45 / 5.42 ms); where the head is packed, that stays at 128 MB or less.
@@ -91,9 +92,9 @@ int arguments(const tr_loss_config *c, const tr_loss_rows *in, void *ws, size_t 
     a.value = (float *)(b + p.value); a.G = b + p.G; a.acc = (float *)(b + p.acc);
     a.n_pad = a.part_ld = p.n_pad; a.d_pad = p.d_pad; a.piece = p.piece; a.g_ld = p.g_ld; a.splits = p.splits;
     a.direct = a.dim % 64 == 0 && a.ws % 8 == 0 && a.ws < (1 << 22) && (reinterpret_cast<uintptr_t>(a.weight) & 15) == 0;
-    if (is_bf16(c) || (in_planes(c) && !gradient)) {
+    if (is_bf16(c) || in_planes(c)) {
         a.hp = b + p.hp; a.wp = b + p.wp; a.row = (LossRow *)(b + p.row);
-        a.pairs = gradient;
+        a.pairs = gradient && is_bf16(c);
         const int rows = gradient && a.rows <= PAIR_ROWS ? 2 * a.rows : a.rows;
         // Few rows in blocks of 256 entries x 64 or 128 rows, up to 256 rows (151936 x 896, 160 rows, blocks of 256 instead: gradients 316 us against 297; 300 rows 423 against 425).
         // Losses of small heads, where that leaves most compute units without a block, in small ones (100 rows x 30000 x 512: 21 -> 17 us; gradients would be 53 -> 59).
@@ -149,14 +150,15 @@ int backward(const tr_loss_config *c, void *ws, size_t ws_bytes, void *stream, c
     hipStream_t s = (hipStream_t)stream;
     launch_loss_rows(s, a);
     // a teacher's entries are placed in G; cross entropy's one a row falls to whoever computes that place
-    const bool half = is_bf16(c), one = a.piece >= a.vocab, along = half && teacher && bf16_takes_entries(a, std::min(a.piece, a.vocab));
-    const bool whole = half && a.rows && !a.direct && one;      // the head is packed once, whole
+    const bool half = is_bf16(c), bf16_products = a.hp != nullptr, one = a.piece >= a.vocab;
+    const bool along = bf16_products && teacher && bf16_takes_entries(a, std::min(a.piece, a.vocab));
+    const bool whole = bf16_products && a.rows && !a.direct && one;      // the head is packed once, whole
     if (whole) launch_bf16_pack_head(s, a, 0, a.vocab);
-    if (a.rows && half && teacher && !along) launch_bf16_entries(s, a, whole);
+    if (a.rows && bf16_products && teacher && !along) launch_bf16_entries(s, a, whole);
     for (int v0 = 0; v0 < a.vocab; v0 += a.piece) {
         const int vn = std::min(a.piece, a.vocab - v0);
         if (a.rows) {
-            if (half) {
+            if (bf16_products) {
                 if (!a.direct && !whole) launch_bf16_pack_head(s, a, v0, vn);
                 launch_bf16_probabilities(s, a, v0, vn, along && v0 == 0);
             } else launch_f32_probabilities(s, a, v0, vn);

@@ -1,5 +1,5 @@
-// Products of the losses over the vocabulary on bf16 matrix instructions: both operands bf16, sums in fp32. The softmax also takes fp32 rows over a bf16 head: a row is
-// then the sum of three bf16 rows (planes), each what the ones before leave, rounded: 24 bits, and every product with the head is exact.
+// Products of the losses over the vocabulary on bf16 matrix instructions: both operands bf16, sums in fp32. The softmax and the probabilities also take fp32 rows over a bf16 head: a row
+// is then the sum of three bf16 rows (planes), each what the ones before leave, rounded: 24 bits, and every product with the head is exact.
 //
 // Four products, all computed transposed (see vocab_loss_epilogues.h), C[n][m] = sum_k A[m][k] B[n][k]:
 //   softmax, probabilities     m = vocabulary entry, n = row that counts, k = feature: both operands lie with k contiguous
@@ -321,8 +321,10 @@ template <int TM, int TN> struct Softmax : Logits<TM, TN> {
     }
 };
 
-template <int TM, int TN> struct Probabilities : Logits<TM, TN> {
+// GT: type of G. With fp32 rows (in planes) it is fp32, and a probability is the exponential that the listed entries have too, from lse as it is: no rounding of lse in units of ln 2.
+template <int TM, int TN, class GT> struct ProbabilitiesIn : Logits<TM, TN> {
     using Logits<TM, TN>::Logits;
+    static constexpr bool PLANES = sizeof(GT) == 4;
     LossRow row[4];
     // the rows' numbers, asked for before the products that they wait for
     template <int WN, int MI, int NI> __device__ __forceinline__ void start(const Place &p, f32x4 (&c)[MI][NI])
@@ -336,7 +338,7 @@ template <int TM, int TN> struct Probabilities : Logits<TM, TN> {
     {
         const LossArgs &a = this->a;
         const int lane = threadIdx.x & 63, w = wavefront(), first = p.n * TN + w % WN * NI * 16, half = this->half;
-        const float k2 = LOG2E / a.temperature;
+        const float k2 = LOG2E / a.temperature, k = 1.0f / a.temperature;
         const int v0 = p.m * TM + w / WN * MI * 16 + 8 * (lane >> 4), there = this->vn - v0;   // entries that exist from this lane's first on
         const int needed = (this->rows + 63) / 64 * 64;
 #pragma unroll
@@ -344,13 +346,16 @@ template <int TM, int TN> struct Probabilities : Logits<TM, TN> {
             const int at = first + j * 16;
             if (at >= needed) continue;               // (the products read whole steps of 64 rows)
             const bool second = half && at >= half;   // of a pair: what rounding leaves
-            bf16_t *to = (bf16_t *)a.G + (size_t)(at + (lane & 15)) * a.g_ld + v0;
+            GT *to = (GT *)a.G + (size_t)(at + (lane & 15)) * a.g_ld + v0;
             const float lse2 = row[j].lse * LOG2E, weight = row[j].weight;
 #pragma unroll
             for (int i = 0; i < MI; i += 2) {
                 float x[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = weight * term(c[i + (e >> 2)][j][e & 3], k2, lse2);
+                for (int e = 0; e < 8; ++e) {
+                    const float product = c[i + (e >> 2)][j][e & 3];
+                    x[e] = weight * (PLANES ? expf(fmaf(product, k, -row[j].lse)) : term(product, k2, lse2));
+                }
                 // rows that do not count and entries that do not exist: zeros, which the next products read
                 if (this->vn < p.m * TM + TM || this->rows < p.n * TN + TN || half) {
 #pragma unroll
@@ -373,12 +378,17 @@ template <int TM, int TN> struct Probabilities : Logits<TM, TN> {
             for (int i = 0; i < MI; i += 2) {
                 if (own - i * 16 >= 8) continue;
                 const float x = less_one([&](int e) { return c[i + (e >> 2)][j][e & 3]; }, own - i * 16, weight, row[j].lse);
-                const bf16_t hi = (bf16_t)two_bf16(x, 0.f);
-                to[own] = second ? (bf16_t)two_bf16(x - load_one(&hi), 0.f) : hi;
+                if constexpr (PLANES) to[own] = x;
+                else {
+                    const bf16_t hi = (bf16_t)two_bf16(x, 0.f);
+                    to[own] = second ? (bf16_t)two_bf16(x - load_one(&hi), 0.f) : hi;
+                }
             }
         }
     }
 };
+template <int TM, int TN> struct Probabilities : ProbabilitiesIn<TM, TN, bf16_t> { using ProbabilitiesIn<TM, TN, bf16_t>::ProbabilitiesIn; };
+template <int TM, int TN> struct PlaneProbabilities : ProbabilitiesIn<TM, TN, float> { using ProbabilitiesIn<TM, TN, float>::ProbabilitiesIn; };
 
 // Every sum over the piece's vocabulary in `splits` parts (a power of two). A part belongs to 8 / splits XCDs, which share its blocks, or an XCD has splits / 8 whole parts: what an
 // XCD reads of the head and of G, it reads alone, or with few.
@@ -846,17 +856,20 @@ template <template <int, int> class Job> void launch_job(hipStream_t s, const Lo
         const dim3 persistent(extra <= 64 ? 256 : 256 + extra);
         launch<stream_kernel<Job, Sh>>(persistent, 512, LDS_OF_RING + Sh::WM * Sh::TN * (int)sizeof(float2), s, a, v0, vn, flag, extra);
     };
-    if (a.hdt == DT_F32) {
-        if constexpr (std::is_same_v<Job<256, 64>, Softmax<256, 64>>) stream(Shape<8, 1, 2, 4, A, B, 3>{});
-    } else if (a.n_block == 64) stream(Shape<8, 1, 2, 4, A, B>{});
-    else if (a.n_block == 128) stream(Shape<4, 2, 4, 4, A, B>{});
-    else if (A && small_blocks(vn, product_rows(a))) {
-        if constexpr (A) {
-            using Bl = Block<2, Shape<2, 2, 4, 4, A, B>>;
-            const int own = entries ? up_div(entry_groups(a), 32) * 8 : 0;
-            launch<block_kernel<Job, Bl>>(dim3(own + up_div(up_div(vn, Bl::TM) * up_div(product_rows(a), Bl::TN), 8) * 8), 256, Bl::LDS, s, a, v0, vn, flag, own);
-        }
-    } else launch<turns_kernel<Job>>(dim3(256), 512, 5 * 256 * BK * 2, s, a, v0, vn, flag);
+    constexpr bool PLANES = std::is_same_v<Job<256, 64>, PlaneProbabilities<256, 64>>;      // a job of fp32 rows alone
+    if constexpr (PLANES || std::is_same_v<Job<256, 64>, Softmax<256, 64>>)
+        if (a.hdt == DT_F32) { stream(Shape<8, 1, 2, 4, A, B, 3>{}); return; }
+    if constexpr (!PLANES) {
+        if (a.n_block == 64) stream(Shape<8, 1, 2, 4, A, B>{});
+        else if (a.n_block == 128) stream(Shape<4, 2, 4, 4, A, B>{});
+        else if (A && small_blocks(vn, product_rows(a))) {
+            if constexpr (A) {
+                using Bl = Block<2, Shape<2, 2, 4, 4, A, B>>;
+                const int own = entries ? up_div(entry_groups(a), 32) * 8 : 0;
+                launch<block_kernel<Job, Bl>>(dim3(own + up_div(up_div(vn, Bl::TM) * up_div(product_rows(a), Bl::TN), 8) * 8), 256, Bl::LDS, s, a, v0, vn, flag, own);
+            }
+        } else launch<turns_kernel<Job>>(dim3(256), 512, 5 * 256 * BK * 2, s, a, v0, vn, flag);
+    }
 }
 
 }  // namespace
@@ -877,7 +890,11 @@ bool bf16_takes_entries(const LossArgs &a, int vn) { return a.n_block < 256 || s
 // (blocks of 256 x 256 leave two parts each, those of 128 x 128 one, in the same places)
 int bf16_softmax_parts(const LossArgs &a) { return up_div(a.vocab, a.n_block < 256 ? BF16_BLOCK : BF16_BLOCK / 2); }
 
-void launch_bf16_probabilities(hipStream_t s, const LossArgs &a, int v0, int vn, bool entries) { launch_job<Probabilities>(s, a, v0, vn, 0, entries); }
+void launch_bf16_probabilities(hipStream_t s, const LossArgs &a, int v0, int vn, bool entries)
+{
+    if (a.hdt == DT_F32) launch_job<PlaneProbabilities>(s, a, v0, vn, 0, entries);
+    else launch_job<Probabilities>(s, a, v0, vn, 0, entries);
+}
 
 void launch_bf16_hidden_grad(hipStream_t s, const LossArgs &a, int v0, int vn, bool first)
 {

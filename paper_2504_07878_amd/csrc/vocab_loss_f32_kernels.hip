@@ -1,5 +1,5 @@
-// Products of the losses over the vocabulary on 32-bit matrix instructions: fp32 rows and a head of either type, any stride and alignment, widened where they
-// are read. (The softmax of fp32 rows over a bf16 head has faster ones, on three bf16 rows for each.)
+// Products of the losses over the vocabulary on 32-bit matrix instructions: fp32 rows and head, and the gradients of fp32 rows over a bf16 head, widened where it is read; any stride and
+// alignment. (The softmax and the probabilities of fp32 rows over a bf16 head have faster ones, on three bf16 rows for each.)
 //
 // A workgroup of 4 wavefronts (2 x 2, an accumulator of 32 x 32 each) computes a 64 x 64 block of C[n][m] = sum_k A[m][k] B[n][k] in steps of 32 k: both operands
 // go through registers into LDS as [row][k], two steps ahead, in two buffers. A lane reads four k at a time: k = 8 g + 4 (lane / 32) + j for the j-th product of group g.
@@ -19,10 +19,9 @@ namespace {
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 constexpr int BK = 32, PITCH = BK + 4;       // 16-byte reads of 16 rows meet 16 different places of the 64 banks
 
-// Loads of 16 or 8 bytes from any element on (global loads need no alignment here): lines of odd length need them (gradients of 58 rows x 10911 x 1397 over a bf16 head: element
+// Loads of 16 bytes from any element on (global loads need no alignment here): lines of odd length need them (gradients of 58 rows x 10911 x 1397 over a bf16 head: element
 // by element, under conditions, 252 us, so 121; with 1400 features 97).
 typedef f32x4 __attribute__((aligned(2))) loose16;
-typedef __attribute__((ext_vector_type(2), aligned(2))) uint32_t loose8;
 
 // four elements of a line from p on, as fp32
 __device__ __forceinline__ void four_of(const float *p, float (&v)[4])
@@ -30,11 +29,6 @@ __device__ __forceinline__ void four_of(const float *p, float (&v)[4])
     const f32x4 x = *reinterpret_cast<const loose16 *>(p);
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = x[e];
-}
-__device__ __forceinline__ void four_of(const bf16_t *p, float (&v)[4])
-{
-    const loose8 u = *reinterpret_cast<const loose8 *>(p);
-    v[0] = __uint_as_float(u.x << 16); v[1] = __uint_as_float(u.x & 0xffff0000u); v[2] = __uint_as_float(u.y << 16); v[3] = __uint_as_float(u.y & 0xffff0000u);
 }
 // N from j on, zeros at or past `limit`: elements one by one, under no condition, which would have each load wait for the one before
 template <int N, class T> __device__ __forceinline__ void some_of(const T *line, int j, int limit, float (&v)[N])
@@ -189,14 +183,14 @@ template <class F> __device__ __forceinline__ void each_run(const f32x16 (&c)[1]
 
 // Products of listed entries: a wavefront takes 32 of them, its rows of the head against its hidden rows, of which only the diagonal is kept (the matrix unit
 // is all but idle in a product this small, and it gives the bits that the same pair has in a block: the same instructions over the same steps of k).
-template <class WT> __device__ __forceinline__ void entries_group(const LossArgs &a, int group)
+__device__ __forceinline__ void entries_group(const LossArgs &a, int group)
 {
     const int lane = threadIdx.x & 63, e = group * 32 + (lane & 31), hf = lane >> 5, count = a.head->count;
     if ((long long)group * 32 >= (long long)count * a.entries) return;
     const int i = e / a.entries, j = e - i * a.entries;
     bool on = i < count;
     const float *h = (const float *)a.hidden;         // (a lane without an entry reads what is there, for nobody)
-    const WT *w = (const WT *)a.weight;
+    const float *w = (const float *)a.weight;
     if (on) {
         const int r = a.idx[i], id = a.ids[(long long)r * a.entries + j];
         h += r * a.hs;
@@ -243,7 +237,7 @@ __global__ __launch_bounds__(256) void f32_softmax_kernel(LossArgs a, int extra)
     __shared__ Tiles sm;
     const int m0 = ((int)blockIdx.x - extra) * F32_BLOCK, n0 = blockIdx.y * F32_BLOCK, count = a.head->count, w = threadIdx.x >> 6;
     if (m0 < 0) {
-        if (n0 == 0) entries_group<float>(a, blockIdx.x * 4 + w);
+        if (n0 == 0) entries_group(a, blockIdx.x * 4 + w);
         return;
     }
     if (n0 >= count) return;
@@ -256,16 +250,16 @@ __global__ __launch_bounds__(256) void f32_softmax_kernel(LossArgs a, int extra)
     if (lane < 32) a.part[((size_t)(m0 / F32_BLOCK) * 2 + (w >> 1)) * a.part_ld + n0 + (w & 1) * 32 + lane] = t;
 }
 
-template <class WT> __global__ __launch_bounds__(256) void f32_probabilities_kernel(LossArgs a, int v0, int vn, int extra)
+__global__ __launch_bounds__(256) void f32_probabilities_kernel(LossArgs a, int v0, int vn, int extra)
 {
     __shared__ Tiles sm;
     const int m0 = ((int)blockIdx.x - extra) * F32_BLOCK, n0 = blockIdx.y * F32_BLOCK, count = a.head->count;
     if (m0 < 0) {
-        if (n0 == 0) entries_group<WT>(a, blockIdx.x * 4 + (threadIdx.x >> 6));
+        if (n0 == 0) entries_group(a, blockIdx.x * 4 + (threadIdx.x >> 6));
         return;
     }
     if (n0 >= count) return;
-    const Lines<WT> A((const WT *)a.weight + (long long)v0 * a.ws, a.ws, vn, a.dim);
+    const Lines<float> A((const float *)a.weight + (long long)v0 * a.ws, a.ws, vn, a.dim);
     const Lines<float, true> B(a.hidden, a.hs, count, a.dim, a.idx);
     f32x16 c[1][1];
     products<true, true>(A, B, m0, n0, 0, a.dim, sm, c);
@@ -361,10 +355,8 @@ int f32_softmax_parts(const LossArgs &a) { return blocks(a.vocab) * 2; }
 
 void launch_f32_probabilities(hipStream_t s, const LossArgs &a, int v0, int vn)
 {
-    by_head(a, [&](auto wt) {
-        const int extra = v0 == 0 && a.teacher ? entry_blocks(a) : 0;
-        hipLaunchKernelGGL((f32_probabilities_kernel<decltype(wt)>), dim3(extra + blocks(vn), blocks(a.rows)), dim3(256), 0, s, a, v0, vn, extra);
-    });
+    const int extra = v0 == 0 && a.teacher ? entry_blocks(a) : 0;
+    hipLaunchKernelGGL(f32_probabilities_kernel, dim3(extra + blocks(vn), blocks(a.rows)), dim3(256), 0, s, a, v0, vn, extra);
 }
 
 void launch_f32_gradients(hipStream_t s, const LossArgs &a, int v0, int vn, bool first)

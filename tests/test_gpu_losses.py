@@ -464,3 +464,55 @@ def test_rows_that_begin_at_any_element(losses, size, types):
         assert torch.equal(got[k], want[k]), k
     for room in (room_h, room_w):
         assert (room[:, :3] == 5).all() and (room[:, 3 + d:] == 5).all()
+
+
+def confident(n, d, v, ht, wt, entries, seed):
+    """Rows whose first entry has 1 - p from 1e-1 to 1e-5: hidden rows N(0, 1) over a head of logits of a standard deviation of 2, moved along the entry's row of the head as far as it takes."""
+    g = torch.Generator().manual_seed(seed)
+    w = (torch.randn((v, d), generator=g) * (2.0 / math.sqrt(d))).to(wt).double()
+    h = torch.randn((n, d), generator=g, dtype=torch.float64)
+    ids = torch.randint(0, v, (n, 1), generator=g) + torch.arange(max(entries, 1)) * (v // max(entries, 1))
+    ids = ids % v
+    left = 10.0 ** -(1 + 4 * torch.rand(n, generator=g, dtype=torch.float64))
+    own = w[ids[:, 0]]
+    z = h @ w.t()
+    others = z.scatter(1, ids[:, :1], -math.inf).logsumexp(1)
+    h = h + own * ((torch.log((1 - left) / left) + others - (h * own).sum(1)) / (own * own).sum(1))[:, None]
+    t = {"hidden": h.to(ht).cuda(), "weight": w.to(wt).cuda(), "grad_loss": torch.ones(n).cuda()}
+    if entries:
+        teacher = -2.0 * torch.arange(entries) - 2.0 * torch.rand((n, entries), generator=g) + torch.where(torch.arange(entries) == 0, 12.0, 0.0)
+        return t | {"ids": ids.int().cuda(), "teacher": teacher.cuda()}
+    return t | {"targets": ids[:, 0].int().contiguous().cuda()}
+
+
+@pytest.mark.parametrize("types", TYPES, ids=["f32", "f32_rows", "bf16"])
+@pytest.mark.parametrize("entries,temperature", [(0, 1.0), (6, 1.0), (6, 2.0)])
+@pytest.mark.parametrize("size", [(256, 896, 2000), (250, 333, 1500), (20, 896, 2000)], ids=str)
+def test_gradients_of_confident_rows(losses, size, entries, temperature, types):
+    """What is left of 1 - p where p is near 1. A product's error dz_v moves p_v by p_v (dz_v - sum_w p_w dz_w), at most 2 Z p_v (1 - p_v) where the products are those that lse was summed
+    from (1 + 4 Z for the second order): nothing of it is left beside a p near 1, where products of another order of summation leave up to Z. Then the roundings, relative to p: lse = ln 2 m + log s in fp32
+    (the product and the sum u each, log 2 u), and again times log2(e) where exponentials to 2 are taken: 4 u |lse|; s, whose largest term has exp2's error (2 u), its argument's (u) and some 50
+    additions of small terms to it (a random walk of u / sqrt 3 each, four standard deviations of it 16 u), expf and p - 1: 24 u in all. Shares as in the head of this module, by entry; bf16 rows' p - y is rounded
+    to bf16 once, and the result to its type."""
+    n, d, v = size
+    t = confident(n, d, v, *types, entries, seed=sum(size) + entries)
+    got = call(losses, t, temperature)
+    h, w = t["hidden"].double().cpu().numpy(), t["weight"].double().cpu().numpy()
+    ids, ok, q, lq = shares(t, v, temperature)
+    z = h @ w.T / temperature
+    top = z.max(1, keepdims=True)
+    lse = top + np.log(np.exp(z - top).sum(1, keepdims=True))
+    p, y, dy = np.exp(z - lse), np.zeros_like(z), np.zeros_like(z)
+    at = (np.arange(n)[:, None].repeat(ids.shape[1], 1), ids)
+    y[at], dy[at] = q, q * 16 * U * (1 + np.abs(lq))
+    Z = (4 * math.sqrt(d) + 4) * U * (np.abs(h) @ np.abs(w).T).max(1, keepdims=True) / temperature
+    half = types[0] == BF16
+    dz = temperature * (p - y)
+    off = temperature * (p * (2 * Z * (1 + 4 * Z) * (1 - p) + U * (4 * np.abs(lse) + 24)) + dy) + (B if half else 2 * U) * np.abs(dz)
+    want = {"d_hidden": dz @ w, "d_weight": dz.T @ h}
+    bound = {"d_hidden": off @ np.abs(w) + (4 * math.sqrt(v) + 4) * U * (np.abs(dz) @ np.abs(w)),
+             "d_weight": off.T @ np.abs(h) + (4 * math.sqrt(n) + 8) * U * (np.abs(dz).T @ np.abs(h))}
+    for k, last in (("d_hidden", B if half else U), ("d_weight", B if types[1] == BF16 else U)):
+        bound[k] += last * (np.abs(want[k]) + bound[k])
+        over = np.abs(got[k].double().cpu().numpy() - want[k]) / bound[k]
+        assert (over <= 1).all(), (k, int((over > 1).sum()), float(over.max()))
