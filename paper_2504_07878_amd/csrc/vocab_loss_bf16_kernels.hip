@@ -535,7 +535,6 @@ template <int TM, int TN> struct WeightGrad {
 template <int PLANES> __device__ __forceinline__ void entries_group(const LossArgs &a, int group, bool packed)   // packed: the whole head is
 {
     const int lane = threadIdx.x & 63, e = group * 16 + (lane & 15), g = lane >> 4, count = a.head->count;
-    if ((long long)group * 16 >= (long long)count * a.entries) return;
     const int i = e / a.entries, j = e - i * a.entries;
     bool on = i < count;
     const bf16_t *h = (const bf16_t *)a.hp, *w = packed ? (const bf16_t *)a.wp : (const bf16_t *)a.weight;
@@ -582,7 +581,14 @@ template <int PLANES> __device__ __forceinline__ void entries_group(const LossAr
     if (on && n >> 2 == g) a.value[e] = d;
 }
 
-__global__ __launch_bounds__(64) void bf16_entries_kernel(LossArgs a, bool packed) { entries_group<1>(a, blockIdx.x, packed); }
+// every `apart`-th group from `first` on
+template <int PLANES> __device__ __forceinline__ void entries_from(const LossArgs &a, int first, int apart, bool packed)
+{
+    const long long all = (long long)a.head->count * a.entries;
+    for (int group = first; (long long)group * 16 < all; group += apart) entries_group<PLANES>(a, group, packed);
+}
+
+__global__ __launch_bounds__(64) void bf16_entries_kernel(LossArgs a, bool packed) { entries_from<1>(a, blockIdx.x, gridDim.x, packed); }
 
 // Few rows, bound by the head's bytes: one workgroup a compute unit takes block after block, the copies running on across blocks (a workgroup a block: 78 us for one row over
 // 151936 x 896, so 63): rings of both operands' steps in LDS, one barrier a step. The first `extra` (a multiple of 8) workgroups take listed entries instead.
@@ -591,7 +597,7 @@ template <template <int, int> class Job_, class Sh> __global__ __launch_bounds__
     using Job = Job_<Sh::TM, Sh::TN>;
     if constexpr (Job::A_KC)
         if ((int)blockIdx.x < extra) {
-            entries_group<Sh::PL>(a, blockIdx.x * Sh::WAVES + wavefront(), !a.direct && vn == a.vocab);
+            entries_from<Sh::PL>(a, blockIdx.x * Sh::WAVES + wavefront(), extra * Sh::WAVES, !a.direct && vn == a.vocab);
             return;
         }
     constexpr int MI = Sh::MI, NI = Sh::NI;
@@ -678,7 +684,7 @@ template <template <int, int> class Job_, class Bl> __global__ __launch_bounds__
     using Job = Job_<Bl::TM, Bl::TN>;
     if constexpr (Job::A_KC)
         if ((int)blockIdx.x < extra) {
-            entries_group<1>(a, blockIdx.x * Bl::WAVES + wavefront(), !a.direct && vn == a.vocab);
+            entries_from<1>(a, blockIdx.x * Bl::WAVES + wavefront(), extra * Bl::WAVES, !a.direct && vn == a.vocab);
             return;
         }
     Job job(a, v0, vn, flag, blockIdx.x - extra);
@@ -837,7 +843,9 @@ template <auto KERNEL, class... A> void launch(dim3 grid, int threads, int lds, 
     hipLaunchKernelGGL(KERNEL, grid, dim3(threads), lds, s, args...);
 }
 
+// Groups of listed entries; 2^20 rows of 1024 are 2^26, more than wavefronts that one launch may have (2^32 threads): beyond MOST_GROUPS a wavefront takes several.
 int entry_groups(const LossArgs &a) { return (int)(((long long)a.rows * a.entries + 15) / 16); }
+constexpr int MOST_GROUPS = 1 << 18;
 
 // Where blocks of 256 x 256 would leave half of the chip without one, those of 128 x 128 (three a compute unit) are four times as many: 817 of 1021 rows x 5003 x 1001, softmax
 // 30 -> 20 us. With more blocks the large ones are faster: 6144 x 151936 x 896 1545 us against 1793, 2048 x 152064 x 3584
@@ -851,7 +859,7 @@ template <template <int, int> class Job> void launch_job(hipStream_t s, const Lo
     constexpr bool A = Job<256, 64>::A_KC, B = Job<256, 64>::B_KC;
     const auto stream = [&](auto shape) {
         using Sh = decltype(shape);
-        const int extra = entries ? up_div(entry_groups(a), 64) * 8 : 0;
+        const int extra = entries ? up_div(std::min(entry_groups(a), MOST_GROUPS), 64) * 8 : 0;
         // a workgroup a compute unit: a few of them take entries only, since the head's bytes come as fast without them
         const dim3 persistent(extra <= 64 ? 256 : 256 + extra);
         launch<stream_kernel<Job, Sh>>(persistent, 512, LDS_OF_RING + Sh::WM * Sh::TN * (int)sizeof(float2), s, a, v0, vn, flag, extra);
@@ -865,7 +873,7 @@ template <template <int, int> class Job> void launch_job(hipStream_t s, const Lo
         else if (A && small_blocks(vn, product_rows(a))) {
             if constexpr (A) {
                 using Bl = Block<2, Shape<2, 2, 4, 4, A, B>>;
-                const int own = entries ? up_div(entry_groups(a), 32) * 8 : 0;
+                const int own = entries ? up_div(std::min(entry_groups(a), MOST_GROUPS), 32) * 8 : 0;
                 launch<block_kernel<Job, Bl>>(dim3(own + up_div(up_div(vn, Bl::TM) * up_div(product_rows(a), Bl::TN), 8) * 8), 256, Bl::LDS, s, a, v0, vn, flag, own);
             }
         } else launch<turns_kernel<Job>>(dim3(256), 512, 5 * 256 * BK * 2, s, a, v0, vn, flag);
@@ -879,7 +887,10 @@ void launch_bf16_pack_head(hipStream_t s, const LossArgs &a, int v0, int vn)
     hipLaunchKernelGGL(bf16_pack_head_kernel, dim3((unsigned)(((long long)vn * (a.d_pad / 8) + 255) / 256)), dim3(256), 0, s, a, v0, vn);
 }
 
-void launch_bf16_entries(hipStream_t s, const LossArgs &a, bool packed) { hipLaunchKernelGGL(bf16_entries_kernel, dim3(entry_groups(a)), dim3(64), 0, s, a, packed); }
+void launch_bf16_entries(hipStream_t s, const LossArgs &a, bool packed)
+{
+    hipLaunchKernelGGL(bf16_entries_kernel, dim3(std::min(entry_groups(a), MOST_GROUPS)), dim3(64), 0, s, a, packed);
+}
 
 void launch_bf16_softmax(hipStream_t s, const LossArgs &a, int v0, int vn, bool entries) { launch_job<Softmax>(s, a, v0, vn, 0, entries); }
 

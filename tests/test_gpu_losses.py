@@ -516,3 +516,30 @@ def test_gradients_of_confident_rows(losses, size, entries, temperature, types):
         bound[k] += last * (np.abs(want[k]) + bound[k])
         over = np.abs(got[k].double().cpu().numpy() - want[k]) / bound[k]
         assert (over <= 1).all(), (k, int((over > 1).sum()), float(over.max()))
+
+
+@pytest.mark.parametrize("types", TYPES[1:], ids=["f32_rows", "bf16"])
+def test_the_most_rows_of_the_most_entries(losses, types):
+    """2^20 rows of 1024 entries, the ends of both ranges: 2^30 entries. Rows take seven values, h = (n mod 7) e, and z = (n mod 7) v / 64 is exact, as are the equal shares, 1 / 1024. What is left are the roundings
+    of exp, log and sums of terms of one sign, of 64 exponentials and of the row's 1024 entries, whose parts q (log q - z + lse) have a size up to 14: (1024 / 64 + 6) u of it for adding 16 a lane and 6 times
+    two lanes, and 16 u (1 + 14) as in the head of this module. The gradient to a row: one feature, sum_v p_v v / 64 - mean over the entries, both up to 1: 64 u each for p and for the sum; with bf16 rows the
+    gradient's elements p - y, of which 64 are summed, are rounded to bf16 once, and so is the result: sum_v |p - y| v / 64 + |result| <= 3 times b."""
+    n, k, v, d = 1 << 20, 1024, 64, 8
+    hidden = torch.zeros((n, d), dtype=types[0], device="cuda")
+    hidden[:, 0] = (torch.arange(n, device="cuda") % 7).to(types[0])
+    weight = torch.zeros((v, d), dtype=types[1], device="cuda")
+    weight[:, 0] = (torch.arange(v, device="cuda") / 64).to(types[1])
+    ids = (torch.arange(k, dtype=torch.int32, device="cuda") % v).expand(n, k).contiguous()
+    teacher = torch.zeros((n, k), device="cuda")
+    plan = losses.VocabLoss(n, d, v, *types, max_entries=k)
+    loss, lse = plan.distill(hidden, weight, ids, teacher)
+    dh, _ = plan.distill_grad(hidden, weight, ids, teacher, 1.0, lse, torch.ones(n, device="cuda"), d_weight=False)
+    z = np.arange(7)[:, None] * (np.arange(v) / 64)
+    want_lse = np.log(np.exp(z).sum(1))
+    want = -math.log(k) - z.mean(1) + want_lse
+    slope = (np.exp(z - want_lse[:, None]) * (np.arange(v) / 64)).sum(1) - (np.arange(v) / 64).mean()
+    row = torch.arange(n, device="cuda") % 7
+    for got, exact, tol in ((lse, want_lse, 16 * U * 8), (loss, want, (22 * 14 + 16 * 15) * U), (dh[:, 0], slope, 128 * U + (3 * B if types[0] == BF16 else 0.0))):
+        off = (got.double() - torch.from_numpy(exact).cuda()[row]).abs().max()
+        assert float(off) <= tol, (float(off), tol)
+    assert (dh[:, 1:] == 0).all()
