@@ -10,6 +10,7 @@
 //   gradient to the hidden rows: m = feature, n = row, k = vocabulary entry of the piece; summed over the pieces in `acc`, one sum per split of k
 //   gradient to the head: m = feature, n = vocabulary entry, k = row
 #include "vocab_loss_epilogues.h"
+#include <algorithm>
 #include <type_traits>
 
 namespace tr {
@@ -231,13 +232,15 @@ __device__ __forceinline__ void entries_group(const LossArgs &a, int group)
     if (on && ((n >> 2) & 1) == hf) a.value[e] = d;
 }
 
-// The first `extra` workgroups along x, of the first row of them, take listed entries.
+// The first `extra` workgroups of the grid's rows take listed entries, as long as there are any.
+__device__ __forceinline__ void entries_of(const LossArgs &a, int extra) { entries_group(a, (blockIdx.y * extra + blockIdx.x) * 4 + (threadIdx.x >> 6)); }
+
 __global__ __launch_bounds__(256) void f32_softmax_kernel(LossArgs a, int extra)
 {
     __shared__ Tiles sm;
     const int m0 = ((int)blockIdx.x - extra) * F32_BLOCK, n0 = blockIdx.y * F32_BLOCK, count = a.head->count, w = threadIdx.x >> 6;
     if (m0 < 0) {
-        if (n0 == 0) entries_group(a, blockIdx.x * 4 + w);
+        entries_of(a, extra);
         return;
     }
     if (n0 >= count) return;
@@ -255,7 +258,7 @@ __global__ __launch_bounds__(256) void f32_probabilities_kernel(LossArgs a, int 
     __shared__ Tiles sm;
     const int m0 = ((int)blockIdx.x - extra) * F32_BLOCK, n0 = blockIdx.y * F32_BLOCK, count = a.head->count;
     if (m0 < 0) {
-        if (n0 == 0) entries_group(a, blockIdx.x * 4 + (threadIdx.x >> 6));
+        entries_of(a, extra);
         return;
     }
     if (n0 >= count) return;
@@ -335,7 +338,12 @@ template <class WT> __global__ __launch_bounds__(256) void f32_gradients_kernel(
 }
 
 int blocks(int n) { return (n + F32_BLOCK - 1) / F32_BLOCK; }
-int entry_blocks(const LossArgs &a) { return (int)(((long long)a.rows * a.entries + 127) / 128); }
+// Workgroups for listed entries in each row of a grid `across` blocks wide. The first rows' take them, those of the others end at once: no more than blocks, or 64, unless it takes more.
+int entry_blocks(const LossArgs &a, int across)
+{
+    const int all = (int)(((long long)a.rows * a.entries + 127) / 128), rows = blocks(a.rows);
+    return std::max((all + rows - 1) / rows, std::min(all, std::max(64, across)));
+}
 
 template <class Go> void by_head(const LossArgs &a, Go go)
 {
@@ -347,7 +355,7 @@ template <class Go> void by_head(const LossArgs &a, Go go)
 
 void launch_f32_softmax(hipStream_t s, const LossArgs &a)
 {
-    const int extra = entry_blocks(a);
+    const int extra = entry_blocks(a, blocks(a.vocab));
     hipLaunchKernelGGL(f32_softmax_kernel, dim3(extra + blocks(a.vocab), blocks(a.rows)), dim3(256), 0, s, a, extra);
 }
 
@@ -355,7 +363,7 @@ int f32_softmax_parts(const LossArgs &a) { return blocks(a.vocab) * 2; }
 
 void launch_f32_probabilities(hipStream_t s, const LossArgs &a, int v0, int vn)
 {
-    const int extra = v0 == 0 && a.teacher ? entry_blocks(a) : 0;
+    const int extra = v0 == 0 && a.teacher ? entry_blocks(a, blocks(vn)) : 0;
     hipLaunchKernelGGL(f32_probabilities_kernel, dim3(extra + blocks(vn), blocks(a.rows)), dim3(256), 0, s, a, v0, vn, extra);
 }
 

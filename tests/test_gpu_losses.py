@@ -518,7 +518,7 @@ def test_gradients_of_confident_rows(losses, size, entries, temperature, types):
         assert (over <= 1).all(), (k, int((over > 1).sum()), float(over.max()))
 
 
-@pytest.mark.parametrize("types", TYPES[1:], ids=["f32_rows", "bf16"])
+@pytest.mark.parametrize("types", TYPES, ids=["f32", "f32_rows", "bf16"])
 def test_the_most_rows_of_the_most_entries(losses, types):
     """2^20 rows of 1024 entries, the ends of both ranges: 2^30 entries. Rows take seven values, h = (n mod 7) e, and z = (n mod 7) v / 64 is exact, as are the equal shares, 1 / 1024. What is left are the roundings
     of exp, log and sums of terms of one sign, of 64 exponentials and of the row's 1024 entries, whose parts q (log q - z + lse) have a size up to 14: (1024 / 64 + 6) u of it for adding 16 a lane and 6 times
