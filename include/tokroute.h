@@ -302,7 +302,7 @@ int tr_profile_chain(void *hip_stream, int32_t *buf, int32_t workgroups, int32_t
  * The same inputs give the same bits.
  *
  * Errors: TR_ERR_INVALID_ARG, TR_ERR_SHAPE (unsupported types or sizes), TR_ERR_CAPACITY (more rows or entries than configured, workspace too small), before
- * anything is enqueued; TR_ERR_HIP. Calls only enqueue. Calls that share a workspace must be ordered with respect to each other; nothing in it
+ * anything is enqueued; TR_ERR_HIP. Calls only enqueue, with the device of the stream and of all pointers current. Calls that share a workspace must be ordered with respect to each other; nothing in it
  * outlives a call. rows may be 0 (d_weight is then cleared). */
 typedef struct tr_loss_config {
     int32_t max_rows, dim, vocab;         /* 1 .. 2^20 rows, 1 .. 65536 features, 1 .. 2^24 entries */

@@ -19,7 +19,7 @@ _DTYPES = {torch.float32: tokroute.F32, torch.bfloat16: tokroute.BF16}
 class VocabLoss:
     """Workspace and sizes of loss calls: up to max_rows hidden rows of `dim` features, a head of `vocab` entries, up to max_entries teacher entries a row.
 
-    Calls enqueue on the current stream; calls of one VocabLoss on different streams must be ordered by the caller, since they share the workspace.
+    Calls enqueue on the current stream of `device`, whichever device is current; calls of one VocabLoss on different streams must be ordered by the caller, since they share the workspace.
     Hidden rows and heads may be strided from row to row; each row is contiguous.
     """
 
@@ -71,13 +71,15 @@ class VocabLoss:
     def _out(self, t, what, n):
         return torch.empty(n, dtype=torch.float32, device=self.workspace.device) if t is None else self._flat(t, what, torch.float32, (n,))
 
-    def _check(self, rc, what):
+    def _call(self, fn, what, *args):
+        with torch.cuda.device(self.workspace.device):     # a default stream is the current device's
+            rc = fn(C.byref(self.cfg), self.workspace.data_ptr(), self.workspace.numel(), self._stream(), *args)
         if rc:
             raise TokrouteError(rc, what)
 
     def _loss(self, fn, what, rows, loss, lse):
         loss, lse = self._out(loss, "loss", rows.rows), self._out(lse, "lse", rows.rows)
-        self._check(fn(C.byref(self.cfg), self.workspace.data_ptr(), self.workspace.numel(), self._stream(), C.byref(rows), loss.data_ptr(), lse.data_ptr()), what)
+        self._call(fn, what, C.byref(rows), loss.data_ptr(), lse.data_ptr())
         return loss, lse
 
     def _grad(self, fn, what, rows, lse, grad_loss, d_hidden, d_weight):
@@ -93,7 +95,7 @@ class VocabLoss:
             out.d_hidden_stride, out.d_hidden = self._matrix(d_hidden, "d_hidden", self.hidden_dtype, c.dim, n), d_hidden.data_ptr()
         if d_weight is not False:
             out.d_weight_stride, out.d_weight = self._matrix(d_weight, "d_weight", self.weight_dtype, c.dim, c.vocab), d_weight.data_ptr()
-        self._check(fn(C.byref(self.cfg), self.workspace.data_ptr(), self.workspace.numel(), self._stream(), C.byref(rows), lse.data_ptr(), grad_loss.data_ptr(), C.byref(out)), what)
+        self._call(fn, what, C.byref(rows), lse.data_ptr(), grad_loss.data_ptr(), C.byref(out))
         return (None if d_hidden is False else d_hidden), (None if d_weight is False else d_weight)
 
     # -- the ABI, same names

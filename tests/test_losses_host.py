@@ -78,3 +78,35 @@ def test_binding_raises_without_a_gpu():
     from paper_2504_07878_amd import losses
     with pytest.raises(RuntimeError, match="no CPU path"):
         losses.VocabLoss(8, 64, 100)
+
+
+def test_calls_run_with_the_workspaces_device_current(tr, monkeypatch):
+    """A default stream is the current device's: every call makes the workspace's current, and only for its time. (Tensors of this machine's memory, and calls that only look at the device.)"""
+    from contextlib import contextmanager
+
+    from paper_2504_07878_amd import losses
+    now, seen = ["another"], []
+
+    @contextmanager
+    def device(d):
+        before, now[0] = now[0], d
+        yield
+        now[0] = before
+
+    def look(*args):
+        seen.append(now[0])
+        return tr.OK
+
+    monkeypatch.setattr(torch.cuda, "device", device)
+    monkeypatch.setattr(losses.VocabLoss, "_matrix", lambda self, t, *_: t.stride(0))
+    monkeypatch.setattr(losses.VocabLoss, "_flat", lambda self, t, *_: t)
+    monkeypatch.setattr(losses.VocabLoss, "_stream", lambda self: seen.append(now[0]))
+    plan = object.__new__(losses.VocabLoss)
+    plan.cfg, plan.workspace, plan.hidden_dtype, plan.weight_dtype = cfg(tr, dim=4, vocab=6), torch.empty(64, dtype=torch.uint8), torch.float32, torch.float32
+    plan.lib = type("Calls", (), {n: staticmethod(look) for n in ("tr_cross_entropy", "tr_cross_entropy_grad", "tr_distill", "tr_distill_grad")})
+    h, w, ids, x, row = torch.zeros(3, 4), torch.zeros(6, 4), torch.zeros((3, 2), dtype=torch.int32), torch.zeros(3, 2), torch.zeros(3)
+    plan.cross_entropy(h, w, ids[:, 0])
+    plan.cross_entropy_grad(h, w, ids[:, 0], row, row)
+    plan.distill(h, w, ids, x)
+    plan.distill_grad(h, w, ids, x, 1.0, row, row)
+    assert seen == [plan.workspace.device] * 8 and now == ["another"]
