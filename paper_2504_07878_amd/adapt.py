@@ -37,15 +37,19 @@ def adapt_head(head, hidden, ids, teacher, targets, steps: int = 20, rate: float
     """Gradient descent on the LM head [vocab][d] (float32 or bfloat16): `share` of the loss is distillation, the rest cross entropy, both means over the rows that count.
 
     hidden: float32 as `collect` gives them, or bfloat16, with which the gradients over a bfloat16 head run on bf16 matrix instructions, several times as fast.
-    rate: None takes 1 / (mean |hidden|^2 / 2), the inverse of a bound on the curvature of both losses in the head (a softmax's second derivative is at most 1/2; T^2 makes
-    up for 1/T twice), with which every step goes down. Returns (new head in the head's type, losses of the steps as a list of floats). Updates are kept in fp32.
+    rate: None takes 1 / (mean |hidden|^2 / 2), each loss's mean over its own rows that count, by its share: the inverse of a bound on the curvature of the loss in the head (a softmax's second
+    derivative is at most 1/2; T^2 makes up for 1/T twice), with which every step of a float32 head goes down (a bfloat16 head's too, but for its rounding). Rows that do not count for a loss (as
+    the losses have it) have no part in any of this, whatever they hold. Returns (new head in the head's type, losses of the steps as a list of floats). Updates are kept in fp32.
     """
     plan = losses.VocabLoss(hidden.shape[0], head.shape[1], head.shape[0], hidden.dtype, head.dtype, max_entries=ids.shape[1], device=head.device)
     master, value = head.float().clone(), []
+    count_ce, count_kd = targets >= 0, ((ids >= 0) & (ids < head.shape[0]) & (teacher != float("-inf"))).any(1)
+    n_ce, n_kd = max(1, int(count_ce.sum())), max(1, int(count_kd.sum()))
     if rate is None:
-        rate = 2.0 / float(hidden.float().square().sum(1).mean())
-    n_ce = max(1, int((targets >= 0).sum()))
-    n_kd = max(1, int(((ids >= 0) & (ids < head.shape[0])).any(1).sum()))
+        square = hidden.float().square().sum(1)
+        mean_ce, mean_kd = (float(square.where(on, torch.zeros_like(square)).sum()) / n for on, n in ((count_ce, n_ce), (count_kd, n_kd)))
+        curvature = (share * mean_kd + (1 - share) * mean_ce) / 2
+        rate = 1.0 / curvature if curvature else 0.0        # (no row that counts, or rows of zeros: no gradient either)
     for _ in range(steps):
         w = master.to(head.dtype, copy=True).requires_grad_()
         loss = share / n_kd * losses.distill(plan, hidden, w, ids, teacher, temperature).sum() + (1 - share) / n_ce * losses.cross_entropy(plan, hidden, w, targets).sum()

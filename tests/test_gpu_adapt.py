@@ -62,3 +62,45 @@ def test_the_tails_confidence_is_the_losses_probability(run):
     plan = losses.VocabLoss(B, s.d_model, s.vocab, torch.float32, torch.float32)
     loss, lse = plan.cross_entropy(out.hidden, slm.dev["tok_emb"], out.token)
     assert torch.allclose(torch.exp(-loss), out.conf, rtol=1e-5, atol=0)
+
+
+def some_rows(n=48, d=256, vocab=500, top=4, seed=5):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    hidden = torch.randn((n, d), device="cuda", generator=g)
+    head = torch.randn((vocab, d), device="cuda", generator=g) * 0.05
+    ids = torch.randint(0, vocab, (n, top), device="cuda", generator=g).int()
+    teacher = torch.randn((n, top), device="cuda", generator=g)
+    return head, hidden, ids, teacher, ids[:, 0].contiguous()
+
+
+@pytest.mark.parametrize("junk", [0.0, float("nan"), float("inf")])
+def test_rows_that_do_not_count_have_no_part_in_the_steps(junk):
+    """Three rows of four count for neither loss: the losses of the steps are those of the others alone (the same sums over the same rows, in blocks of other sizes: fp32 roundings of
+    losses of about 6, 100 u of them, over steps that bring them closer together)."""
+    from paper_2504_07878_amd import adapt
+    head, hidden, ids, teacher, targets = some_rows()
+    off = torch.arange(48, device="cuda") % 4 > 0
+    want = adapt.adapt_head(head, hidden[~off], ids[~off], teacher[~off], targets[~off], steps=30)
+    hidden[off], ids[off], targets[off] = junk, -1, -1
+    got = adapt.adapt_head(head, hidden, ids, teacher, targets, steps=30)
+    assert np.allclose(got[1], want[1], rtol=1e-5, atol=0), (got[1], want[1])
+    assert all(b < a for a, b in zip(got[1], got[1][1:])) and torch.allclose(got[0], want[0], rtol=1e-4, atol=1e-6)
+
+
+def test_rows_without_a_teachers_logits_do_not_count():
+    """Logits of -inf are no entries: a row of nothing else counts like one without ids, and each loss is a mean over its own rows."""
+    from paper_2504_07878_amd import adapt
+    head, hidden, ids, teacher, targets = some_rows()
+    none = ids.clone()
+    none[::3] = -1
+    want = adapt.adapt_head(head, hidden, none, teacher, targets, steps=10)
+    teacher[::3] = float("-inf")
+    got = adapt.adapt_head(head, hidden, ids, teacher, targets, steps=10)
+    assert torch.equal(got[0], want[0]) and got[1] == want[1]
+
+
+def test_no_row_counts():
+    from paper_2504_07878_amd import adapt
+    head, hidden, ids, teacher, targets = some_rows()
+    new, losses = adapt.adapt_head(head, hidden, ids.fill_(-1), teacher, targets.fill_(-1), steps=3)
+    assert torch.equal(new, head) and losses == [0.0] * 3
