@@ -39,10 +39,11 @@ def adapt_head(head, hidden, ids, teacher, targets, steps: int = 20, rate: float
     hidden: float32 as `collect` gives them, or bfloat16, with which the gradients over a bfloat16 head run on bf16 matrix instructions, several times as fast.
     rate: None takes 1 / (mean |hidden|^2 / 2), each loss's mean over its own rows that count, by its share: the inverse of a bound on the curvature of the loss in the head (a softmax's second
     derivative is at most 1/2; T^2 makes up for 1/T twice), with which every step of a float32 head goes down (a bfloat16 head's too, but for its rounding). Rows that do not count for a loss (as
-    the losses have it) have no part in any of this, whatever they hold. Returns (new head in the head's type, losses of the steps as a list of floats). Updates are kept in fp32.
+    the losses have it) have no part in any of this, whatever they hold; nor have targets past the head's vocabulary, tokens that only the large model has. Returns (new head in the head's type, losses of the steps as a list of floats). Updates are kept in fp32.
     """
     plan = losses.VocabLoss(hidden.shape[0], head.shape[1], head.shape[0], hidden.dtype, head.dtype, max_entries=ids.shape[1], device=head.device)
     master, value = head.float().clone(), []
+    targets = targets.where(targets < head.shape[0], torch.full_like(targets, -1))
     count_ce, count_kd = targets >= 0, ((ids >= 0) & (ids < head.shape[0]) & (teacher != float("-inf"))).any(1)
     n_ce, n_kd = max(1, int(count_ce.sum())), max(1, int(count_kd.sum()))
     if rate is None:

@@ -104,3 +104,15 @@ def test_no_row_counts():
     head, hidden, ids, teacher, targets = some_rows()
     new, losses = adapt.adapt_head(head, hidden, ids.fill_(-1), teacher, targets.fill_(-1), steps=3)
     assert torch.equal(new, head) and losses == [0.0] * 3
+
+
+def test_targets_past_the_vocabulary_do_not_count():
+    """Tokens of the large model's longer vocabulary: no target for this head, and no NaN in the steps' losses."""
+    from paper_2504_07878_amd import adapt
+    head, hidden, ids, teacher, targets = some_rows()
+    targets[::5] = -1
+    want = adapt.adapt_head(head, hidden, ids, teacher, targets, steps=10)
+    targets[::5] = torch.tensor([500, 501, 2 ** 31 - 1, 500, 563, 500, 500, 777, 500, 500], dtype=torch.int32, device="cuda")
+    given = targets.clone()
+    got = adapt.adapt_head(head, hidden, ids, teacher, targets, steps=10)
+    assert torch.equal(got[0], want[0]) and got[1] == want[1] and torch.equal(targets, given)
