@@ -11,14 +11,17 @@ import numpy as np
 import torch
 
 from . import losses
+from .tokroute import POST_FINAL_NORM
 
 
 def collect(slm, llm, prompts, tokens, top: int = 16):
     """One row for every generated position of every sequence: (hidden float32 [n][d], ids int32 [n][top], teacher float32 [n][top], targets int32 [n]).
 
     prompts: the sequences' prompts; tokens: int32 [B][max_new], what they emitted. ids at or past the small model's vocabulary (a large model's padding) are no entries of
-    the losses. Both models' slots 0 .. B - 1 are used, and hold the sequences afterwards.
+    the losses. slm exposes the rows that its LM head multiplies (hidden_tap POST_FINAL_NORM): others are refused. Both models' slots 0 .. B - 1 are used, and hold the sequences afterwards.
     """
+    if slm.cfg.hidden_tap != POST_FINAL_NORM:
+        raise ValueError("the small model exposes hidden rows before the final norm: its LM head does not multiply them")
     slots = list(range(len(prompts)))
     keep = ([], [], [], [])
 
