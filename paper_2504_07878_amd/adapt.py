@@ -44,6 +44,7 @@ def adapt_head(head, hidden, ids, teacher, targets, steps: int = 20, rate: float
     derivative is at most 1/2; T^2 makes up for 1/T twice), with which every step of a float32 head goes down (a bfloat16 head's too, but for its rounding). Rows that do not count for a loss (as
     the losses have it) have no part in any of this, whatever they hold; nor have targets past the head's vocabulary, tokens that only the large model has. Returns (new head in the head's type, losses of the steps as a list of floats). Updates are kept in fp32.
     """
+    head, hidden = head.detach(), hidden.detach()          # (steps of its own, whatever graph they come from)
     plan = losses.VocabLoss(hidden.shape[0], head.shape[1], head.shape[0], hidden.dtype, head.dtype, max_entries=ids.shape[1], device=head.device)
     master, value = head.float().clone(), []
     targets = targets.where(targets < head.shape[0], torch.full_like(targets, -1))
@@ -56,7 +57,8 @@ def adapt_head(head, hidden, ids, teacher, targets, steps: int = 20, rate: float
         rate = 1.0 / curvature if curvature else 0.0        # (no row that counts, or rows of zeros: no gradient either)
     for _ in range(steps):
         w = master.to(head.dtype, copy=True).requires_grad_()
-        loss = share / n_kd * losses.distill(plan, hidden, w, ids, teacher, temperature).sum() + (1 - share) / n_ce * losses.cross_entropy(plan, hidden, w, targets).sum()
+        with torch.enable_grad():
+            loss = share / n_kd * losses.distill(plan, hidden, w, ids, teacher, temperature).sum() + (1 - share) / n_ce * losses.cross_entropy(plan, hidden, w, targets).sum()
         loss.backward()
         master -= rate * w.grad.float()
         value.append(loss.detach())

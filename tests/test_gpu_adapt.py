@@ -116,3 +116,35 @@ def test_targets_past_the_vocabulary_do_not_count():
     given = targets.clone()
     got = adapt.adapt_head(head, hidden, ids, teacher, targets, steps=10)
     assert torch.equal(got[0], want[0]) and got[1] == want[1] and torch.equal(targets, given)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_a_parameter_as_the_head_and_no_grad_around_it(dtype):
+    """The head may be a parameter of the caller's, the rows part of a graph, gradients switched off: the same steps, and no gradient left with the caller."""
+    from paper_2504_07878_amd import adapt
+    head, hidden, ids, teacher, targets = some_rows()
+    head = head.to(dtype)
+    want = adapt.adapt_head(head, hidden, ids, teacher, targets, steps=5)
+    p, rows = torch.nn.Parameter(head.clone()), hidden.clone().requires_grad_()
+    for mode in (torch.enable_grad, torch.no_grad):
+        with mode():
+            got = adapt.adapt_head(p, rows, ids, teacher, targets, steps=5)
+        assert torch.equal(got[0], want[0]) and got[1] == want[1] and not got[0].requires_grad
+        assert p.grad is None and rows.grad is None and torch.equal(p.detach(), head)
+
+
+def test_a_bf16_models_head_learns():
+    """The rows that a bf16 model exposes are fp32, over a bf16 head."""
+    from paper_2504_07878_amd import adapt, joint, synth, tokroute
+    s = synth.TINY.with_(name="tiny-bf16", dtype=synth.BF16, kv_dtype=synth.BF16, threshold=0.5)
+    slm = tokroute.Model(s.asdict(), synth.make_weights(s, SEED), B, 64)
+    llm = tokroute.Model(s.with_(router_hidden=0).asdict(), synth.make_weights(s.with_(router_hidden=0), SEED + 1, std=0.05), B, 64)
+    prompts = [synth.prompt_tokens(SEED, f"adapt{b}", 9 + 5 * b, s.vocab) for b in range(B)]
+    tokens, _ = joint.generate(slm, llm, prompts, NEW)
+    hidden, ids, teacher, targets = adapt.collect(slm, llm, prompts, tokens, top=8)
+    head = slm.dev["tok_emb"]
+    assert hidden.dtype == torch.float32 and head.dtype == torch.bfloat16
+    new, losses = adapt.adapt_head(head, hidden, ids, teacher, targets, steps=100)
+    _, same = adapt.adapt_head(head.float(), hidden, ids, teacher, targets, steps=1)
+    assert abs(losses[0] - same[0]) < 1e-5 * same[0]            # the same head, and losses of the same precision
+    assert new.dtype == torch.bfloat16 and losses[-1] < losses[50] < losses[0]
