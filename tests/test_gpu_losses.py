@@ -543,3 +543,27 @@ def test_the_most_rows_of_the_most_entries(losses, types):
         off = (got.double() - torch.from_numpy(exact).cuda()[row]).abs().max()
         assert float(off) <= tol, (float(off), tol)
     assert (dh[:, 1:] == 0).all()
+
+
+@pytest.mark.parametrize("entries", [0, 5])
+@pytest.mark.parametrize("dim", [448, 430])
+def test_large_blocks_of_the_heads_gradient(losses, dim, entries):
+    """More than 1024 rows, and more than 128 blocks of 256 features x 256 entries, the last of both partly empty; a head that is read as it lies and one that is packed."""
+    t = make(1200, dim, 17001, BF16, BF16, entries=entries, seed=dim + entries)
+    check(call(losses, t, 2.0 if entries else 1.0), t, 2.0 if entries else 1.0)
+
+
+@pytest.mark.parametrize("entries", [0, 5])
+@pytest.mark.parametrize("rows,dim", [(300, 192), (600, 201), (1500, 192), (1500, 201)])
+def test_many_rows_over_the_vocabulary_in_pieces(losses, rows, dim, entries):
+    """Pieces of 2048 entries (the workspace is one for 130000 rows), the last of 300: large blocks that go on from the sums of the pieces before, and parts of the last piece without an entry."""
+    t = make(rows, dim, 4396, BF16, BF16, entries=entries, seed=rows + dim)
+    temperature = 1.5 if entries else 1.0
+    got = call(losses, t, temperature, plan=losses.VocabLoss(130000, dim, 4396, BF16, BF16, max_entries=max(entries, 1)))
+    check(got, t, temperature)
+    whole = call(losses, t, temperature)
+    assert torch.equal(got["loss"], whole["loss"]) and torch.equal(got["lse"], whole["lse"])
+
+
+def test_fp32_rows_over_a_bf16_head_in_a_captured_graph(losses):
+    test_another_stream_and_a_captured_graph(losses, (F32, BF16))
