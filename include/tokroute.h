@@ -298,7 +298,7 @@ int tr_profile_chain(void *hip_stream, int32_t *buf, int32_t workgroups, int32_t
  * grad_loss 0 take no part in the gradients. An id listed twice in a row counts with both shares.
  *
  * Sums, softmax statistics and the losses are 32-bit throughout. Types: hidden and weight both TR_BF16, both TR_F32, or hidden TR_F32 (as tr_out.hidden) over
- * a TR_BF16 head; gradients have the type of what they are to. With bf16 hidden rows the pieces of p - y are rounded to bf16 once.
+ * a TR_BF16 head; gradients have the type of what they are to. With bf16 hidden rows the pieces of grad_loss (p - y) are rounded to bf16 once.
  * The same inputs give the same bits.
  *
  * Errors: TR_ERR_INVALID_ARG, TR_ERR_SHAPE (unsupported types or sizes), TR_ERR_CAPACITY (more rows or entries than configured, workspace too small), before

@@ -11,7 +11,8 @@
 //   turns_kernel    blocks of 256 x 256, for more than 256 rows. 6144 rows x 151936 x 896 (8192, three quarters of them counting) take 1510 us for the softmax, 1.11 PFLOP/s with
 //                   the matrix pipes 52 % busy at 2.0 GHz; 2048 rows x 152064 x 3584 1790 us, 1.25 PFLOP/s, 61 % at 1.9 GHz (a library product of 8192^3: 1.30, of
 //                   4096 x 151936 x 896: 0.98). Bound by power and copies together, 1.6 us a step, and by what lies between two blocks, 5 us: the exponentials.
-//   stream_kernel   blocks of 256 x 64 or 128, for fewer rows. Bound by the head's bytes: 272 MB in 50 us, 5.4 TB/s, what copies reach here.
+//   stream_kernel   blocks of 256 x 64 or 128, for fewer rows. Bound by the head's bytes: 272 MB in 50 us, 5.4 TB/s, what copies reach here. Rows in planes, however many (300 of 500 rows x
+//                   151936 x 896: softmax 250 us, probabilities 268, 0.98 and 0.91 PFLOP/s; on 32-bit instructions, 64 x 64, the probabilities took 872).
 //   block_kernel    blocks of 128 x 128, where there are few blocks, and for the gradient to the head of few rows.
 #include "vocab_loss_epilogues.h"
 #include <algorithm>

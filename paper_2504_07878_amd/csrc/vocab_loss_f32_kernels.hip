@@ -20,8 +20,8 @@ namespace {
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 constexpr int BK = 32, PITCH = BK + 4;       // 16-byte reads of 16 rows meet 16 different places of the 64 banks
 
-// Loads of 16 bytes from any element on (global loads need no alignment here): lines of odd length need them (gradients of 58 rows x 10911 x 1397 over a bf16 head: element
-// by element, under conditions, 252 us, so 121; with 1400 features 97).
+// Loads of 16 bytes from any element on (global loads need no alignment here): lines of odd length need them (probabilities and gradients of 58 rows x 10911 x 1397 over a bf16 head,
+// both on these instructions: element by element, under conditions, 252 us, so 121, 67 of it the gradients; with 1400 features 97).
 typedef f32x4 __attribute__((aligned(2))) loose16;
 
 // four elements of a line from p on, as fp32
