@@ -336,6 +336,68 @@ int tr_cross_entropy_grad(const tr_loss_config *cfg, void *workspace, size_t wor
 int tr_distill_grad(const tr_loss_config *cfg, void *workspace, size_t workspace_bytes, void *hip_stream, const tr_loss_rows *in, const float *lse,
                     const float *grad_loss, const tr_loss_grads *out);
 
+/* ------------------------------------------------------------------ tokens from logits
+ *
+ * The step and the tail give the greedy token. These calls draw tokens from rows of logits (tr_out.logits, or a caller's own), and list a row's largest logits (the teacher's
+ * entries of tr_distill). They need no context.
+ *
+ * The order of a row: larger logit first, of equal ones (-0 and 0 are) the lower id. Logits of -infinity or NaN are no tokens. w[v] = exp((z[v] - max z) / T); where logits are
+ * +infinity they have weight 1 and all others 0.
+ *   top_k keeps the first top_k tokens of the order (0 or less: all); top_p the shortest run of these, from the first on, that has top_p of their weight or more (1 or more, NaN: all);
+ *   min_p those of weight min_p or more (0 or less, NaN: all). What all three keep is kept; the first always is.
+ *   tr_sample: token = the first kept id up to which, by id, the kept weights add up to more than u times the sum of all of them; logprob = log(its weight / that sum).
+ *     u below 0 or NaN counts as 0; at 1 or more the last kept id of any weight is drawn. T of 0 (or less, or NaN): the first of the order, logprob 0.
+ *   tr_top: the first `entries` tokens of the order; ids -1 and values -infinity where a row has fewer.
+ * A row without any token: token -1, logprob 0.
+ * Weights are sums' terms in 64 bits, rounded to units of 2^-(62 - log2 vocab) of the largest (2^-44 at 151936): the same inputs give the same token, whatever else runs.
+ *
+ * Errors: TR_ERR_INVALID_ARG, TR_ERR_SHAPE (unsupported type or sizes), TR_ERR_CAPACITY (more rows or entries than configured, workspace too small), before anything is enqueued;
+ * TR_ERR_HIP. Calls only enqueue, with the device of the stream and of all pointers current. The workspace is cleared (zeros) by the caller once, before its first call, belongs to one configuration, and
+ * calls that share it must be ordered with respect to each other; but for what is cleared nothing in it outlives a call (after TR_ERR_HIP clear it again). rows may be 0. */
+typedef struct tr_pick_config {
+    int32_t max_rows, vocab;      /* 1 .. 2^20 both */
+    int32_t dtype;                /* of the logits: TR_F32 / TR_BF16 */
+} tr_pick_config;
+
+typedef struct tr_pick_rows {     /* DEVICE pointer, aligned to its elements */
+    const void *logits;           /* [rows][vocab], rows contiguous */
+    int64_t stride;               /* elements from row to row, >= vocab */
+    int32_t rows;
+} tr_pick_rows;
+
+/* DEVICE pointers. Each but u may be NULL: then the value below it holds for all rows (checked: temperature >= 0, top_k >= 0, top_p and min_p in [0, 1]). */
+typedef struct tr_sample_how {
+    const float *u;               /* [rows] the random numbers, evenly distributed in [0, 1) */
+    const float *temperatures;    /* [rows] */
+    const int32_t *top_ks;
+    const float *top_ps, *min_ps;
+    float temperature;
+    int32_t top_k;
+    float top_p, min_p;
+} tr_sample_how;
+
+/* Bytes of device workspace (256-byte aligned, owned by the caller) the calls below need; 0 if the configuration is not supported. */
+size_t tr_pick_workspace_bytes(const tr_pick_config *cfg);
+/* token: DEVICE int32 [rows]; logprob: DEVICE float [rows]. */
+int tr_sample(const tr_pick_config *cfg, void *workspace, size_t workspace_bytes, void *hip_stream, const tr_pick_rows *in, const tr_sample_how *how, int32_t *token, float *logprob);
+/* ids: DEVICE int32 [rows][entries]; values: DEVICE float [rows][entries]; entries 1 .. 1024 (more than vocab may be asked for). */
+int tr_top(const tr_pick_config *cfg, void *workspace, size_t workspace_bytes, void *hip_stream, const tr_pick_rows *in, int32_t entries, int32_t *ids, float *values);
+
+/* ------------------------------------------------------------------ the length of many gradients, and its clipping
+ *
+ * norm = sqrt(sum of the squares of all elements of all gradients); tr_grad_clip: out[i] = grads[i] * min(1, max_norm / norm). Squares and sums are 64-bit, in an order that the
+ * sizes alone decide: the same gradients give the same bits. Elements are multiplied in 32 bits and rounded once. Where the norm is infinite or NaN the gradients stay as they are (and
+ * the norm says so).
+ *
+ * n gradients; grads, out, counts, dtypes are HOST arrays [n], read before the call returns: DEVICE pointers (aligned to their elements; of count 0: any), elements (0 .. 2^40), TR_F32 /
+ * TR_BF16. out[i] may be grads[i]: in place; then nothing is written where nothing is to be scaled. Otherwise what is written may overlap nothing of the call (TR_ERR_INVALID_ARG); tr_grad_norm
+ * takes a gradient twice. max_norm >= 0, may be infinite. norm: DEVICE float [1], outside of the gradients.
+ * Workspace (256-byte aligned DEVICE memory), errors and streams: as for tokens from logits above, cleared once in particular. */
+size_t tr_grad_workspace_bytes(void);
+int tr_grad_norm(void *workspace, size_t workspace_bytes, void *hip_stream, int32_t n, const void *const *grads, const int64_t *counts, const int32_t *dtypes, float *norm);
+int tr_grad_clip(void *workspace, size_t workspace_bytes, void *hip_stream, int32_t n, const void *const *grads, void *const *out, const int64_t *counts, const int32_t *dtypes,
+                 float max_norm, float *norm);
+
 const char *tr_last_error(const tr_ctx *ctx);
 
 #ifdef __cplusplus

@@ -1,0 +1,78 @@
+"""The length of many gradients together, and its clipping: the binding of tr_grad_norm and tr_grad_clip (include/tokroute.h).
+
+There is no CPU fallback: without the built library or without a GPU calls raise.
+"""
+from __future__ import annotations
+
+import ctypes as C
+
+import torch
+
+from . import tokroute
+from .tokroute import TokrouteError
+
+_DTYPES = {torch.float32: tokroute.F32, torch.bfloat16: tokroute.BF16}
+
+
+def _dense(t):
+    """Whether a tensor's elements fill one piece of memory, in whatever order of its dimensions."""
+    return t.is_contiguous() or t.permute(sorted(range(t.dim()), key=lambda i: (-t.stride(i), -t.shape[i]))).is_contiguous()
+
+
+class Clipper:
+    """Workspace of the calls. Calls enqueue on the current stream of `device`, whichever device is current; calls of one Clipper on different streams must be ordered by the caller.
+
+    Gradients are float32 or bfloat16 tensors on `device`, of any mixture of sizes, each of elements that fill one piece of memory; None (a parameter without a gradient) is left out.
+    """
+
+    def __init__(self, device="cuda:0"):
+        if not torch.cuda.is_available():
+            raise RuntimeError("tokroute needs a GPU: no CPU path exists")
+        self.lib = tokroute.load_library()
+        self.workspace = torch.zeros(self.lib.tr_grad_workspace_bytes(), dtype=torch.uint8, device=device)
+        self.device = self.workspace.device
+        self._home = torch.cuda.current_stream(self.device)
+
+    # -- helpers
+    def _list(self, grads, what="gradients"):
+        for t in grads:
+            if not (isinstance(t, torch.Tensor) and t.dtype in _DTYPES and t.device == self.device and t.layout == torch.strided and _dense(t)):
+                raise ValueError(f"{what}: float32 or bfloat16 tensors on {self.device}, each of elements that fill one piece of memory")
+        return (C.c_void_p * len(grads))(*[t.data_ptr() for t in grads])
+
+    def _call(self, fn, what, *args):
+        s = torch.cuda.current_stream(self.device)
+        if s != self._home:
+            self.workspace.record_stream(s)    # its memory is not handed on while work of that stream may use it
+        with torch.cuda.device(self.device):   # a default stream is the current device's
+            rc = fn(self.workspace.data_ptr(), self.workspace.numel(), s.cuda_stream, *args)
+        if rc:
+            raise TokrouteError(rc, what)
+
+    def _sizes(self, grads):
+        return (C.c_int64 * len(grads))(*[t.numel() for t in grads]), (C.c_int32 * len(grads))(*[_DTYPES[t.dtype] for t in grads])
+
+    # -- the ABI
+    def norm(self, grads):
+        """Length of all gradients together: a float32 tensor of no dimensions."""
+        grads = [t for t in grads if t is not None]
+        at, norm = self._list(grads), torch.empty((), dtype=torch.float32, device=self.device)
+        self._call(self.lib.tr_grad_norm, "tr_grad_norm", len(grads), at, *self._sizes(grads), norm.data_ptr())
+        return norm
+
+    def clip(self, grads, max_norm: float, out=None):
+        """The same, and the gradients scaled by min(1, max_norm / norm): in place, or into `out` (tensors of the same shapes, types and strides; None where a gradient is None)."""
+        grads = list(grads)
+        out = grads if out is None else list(out)
+        if len(out) != len(grads) or any((a is None) != (b is None) for a, b in zip(grads, out)):
+            raise ValueError("out: a tensor for every gradient")
+        grads, out = [t for t in grads if t is not None], [t for t in out if t is not None]
+        at = self._list(grads)
+        to = at
+        if any(a is not b for a, b in zip(grads, out)):
+            to = self._list(out, "out")
+            if any(a.dtype != b.dtype or a.shape != b.shape or (a.stride() != b.stride() and not (a.is_contiguous() and b.is_contiguous())) for a, b in zip(grads, out)):
+                raise ValueError("out: tensors of the gradients' shapes, types and strides")
+        norm = torch.empty((), dtype=torch.float32, device=self.device)
+        self._call(self.lib.tr_grad_clip, "tr_grad_clip", len(grads), at, to, *self._sizes(grads), max_norm, norm.data_ptr())
+        return norm

@@ -1,0 +1,101 @@
+"""Tokens drawn from rows of logits, and a row's largest logits.
+
+The binding of tr_sample and tr_top (include/tokroute.h states what they compute, and what becomes of infinities, NaN and rows without any token). A `Sampler` keeps the workspace
+that calls share; `Draw` is how `joint.generate` draws. There is no CPU fallback: without the built library or without a GPU calls raise.
+"""
+from __future__ import annotations
+
+import ctypes as C
+from dataclasses import dataclass
+
+import torch
+
+from . import tokroute
+from .tokroute import TokrouteError, tr_pick_config, tr_pick_rows, tr_sample_how
+
+_DTYPES = {torch.float32: tokroute.F32, torch.bfloat16: tokroute.BF16}
+
+
+@dataclass(frozen=True)
+class Draw:
+    """How tokens are drawn: the arguments of `Sampler.sample` of the same names. temperature 0: the largest logit."""
+    temperature: float = 1.0
+    top_k: int = 0
+    top_p: float = 1.0
+    min_p: float = 0.0
+
+
+class Sampler:
+    """Workspace and sizes of calls on up to max_rows rows of `vocab` logits.
+
+    Calls enqueue on the current stream of `device`, whichever device is current; calls of one Sampler on different streams must be ordered by the caller, since they share the workspace.
+    Rows may be strided; each row is contiguous.
+    """
+
+    def __init__(self, max_rows: int, vocab: int, dtype=torch.float32, device="cuda:0"):
+        if not torch.cuda.is_available():
+            raise RuntimeError("tokroute needs a GPU: no CPU path exists")
+        if dtype not in _DTYPES:
+            raise ValueError(f"logits are float32 or bfloat16, not {dtype}")
+        self.lib = tokroute.load_library()
+        self.dtype = dtype
+        self.cfg = tr_pick_config(max_rows, vocab, _DTYPES[dtype])
+        nbytes = self.lib.tr_pick_workspace_bytes(C.byref(self.cfg))
+        if nbytes == 0:
+            raise TokrouteError(tokroute.ERR_SHAPE, "tr_pick_workspace_bytes", "(sizes or types not supported)")
+        self.workspace = torch.zeros(nbytes, dtype=torch.uint8, device=device)
+        self.device = self.workspace.device
+        self._home = torch.cuda.current_stream(self.device)
+
+    # -- helpers
+    def _rows(self, logits):
+        v = self.cfg.vocab
+        if not (isinstance(logits, torch.Tensor) and logits.dtype == self.dtype and logits.device == self.device and logits.dim() == 2 and logits.shape[1] == v
+                and (logits.stride(1) == 1 or v == 1)):
+            raise ValueError(f"logits: a {self.dtype} matrix of {v} columns with contiguous rows on {self.device}")
+        n = logits.shape[0]
+        return tr_pick_rows(logits.data_ptr(), max(logits.stride(0), v) if n <= 1 else logits.stride(0), n)
+
+    def _flat(self, t, what, dtype, shape):
+        if not (isinstance(t, torch.Tensor) and t.dtype == dtype and t.device == self.device and tuple(t.shape) == shape and t.is_contiguous()):
+            raise ValueError(f"{what}: a contiguous {dtype} tensor of shape {shape} on {self.device}")
+        return t.data_ptr()
+
+    def _out(self, t, what, dtype, shape):
+        t = torch.empty(shape, dtype=dtype, device=self.device) if t is None else t
+        return t, self._flat(t, what, dtype, shape)
+
+    def _call(self, fn, what, *args):
+        s = torch.cuda.current_stream(self.device)
+        if s != self._home:
+            self.workspace.record_stream(s)    # its memory is not handed on while work of that stream may use it
+        with torch.cuda.device(self.device):   # a default stream is the current device's
+            rc = fn(C.byref(self.cfg), self.workspace.data_ptr(), self.workspace.numel(), s.cuda_stream, *args)
+        if rc:
+            raise TokrouteError(rc, what)
+
+    # -- the ABI, same names
+    def sample(self, logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, token=None, logprob=None):
+        """(token int32 [n], logprob float32 [n]): one token a row from its random number u (float32 [n] in [0, 1)), and the logarithm of its probability among what the filters keep.
+
+        temperature, top_p, min_p (float32 [n]) and top_k (int32 [n]) are numbers or device tensors with a value a row. token and logprob may be given (written over)."""
+        rows = self._rows(logits)
+        n = rows.rows
+        how = tr_sample_how(self._flat(u, "u", torch.float32, (n,)))
+        for name, value, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
+            if isinstance(value, torch.Tensor):
+                setattr(how, name + "s", self._flat(value, name, dtype, (n,)))
+            else:
+                setattr(how, name, value)
+        token, token_at = self._out(token, "token", torch.int32, (n,))
+        logprob, logprob_at = self._out(logprob, "logprob", torch.float32, (n,))
+        self._call(self.lib.tr_sample, "tr_sample", C.byref(rows), C.byref(how), token_at, logprob_at)
+        return token, logprob
+
+    def top(self, logits, entries: int, ids=None, values=None):
+        """(ids int32 [n][entries], values float32 [n][entries]): the largest logits of each row, in falling order, equal ones by id; -1 and -inf where a row has fewer."""
+        rows = self._rows(logits)
+        ids, ids_at = self._out(ids, "ids", torch.int32, (rows.rows, entries))
+        values, values_at = self._out(values, "values", torch.float32, (rows.rows, entries))
+        self._call(self.lib.tr_top, "tr_top", C.byref(rows), entries, ids_at, values_at)
+        return ids, values

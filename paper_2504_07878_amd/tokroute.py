@@ -25,7 +25,8 @@ KERNEL_FAMILIES = ("setup", "prep", "qkv", "attention", "oproj", "gateup", "down
 
 EXPORTS = ["tr_workspace_bytes", "tr_create", "tr_destroy", "tr_prefill", "tr_decode_step", "tr_decode_step_dev", "tr_decode_step_active", "tr_extend", "tr_tail", "tr_tail_noalloc", "tr_set_threshold",
            "tr_set_mode", "tr_set_shared", "tr_seq_len", "tr_seq_truncate", "tr_seq_fork", "tr_seq_load_kv", "tr_counters_ptr", "tr_profile_enable", "tr_profile_select",
-           "tr_profile_read", "tr_profile_chain", "tr_last_error", "tr_loss_workspace_bytes", "tr_cross_entropy", "tr_cross_entropy_grad", "tr_distill", "tr_distill_grad"]
+           "tr_profile_read", "tr_profile_chain", "tr_last_error", "tr_loss_workspace_bytes", "tr_cross_entropy", "tr_cross_entropy_grad", "tr_distill", "tr_distill_grad",
+           "tr_pick_workspace_bytes", "tr_sample", "tr_top", "tr_grad_workspace_bytes", "tr_grad_norm", "tr_grad_clip"]
 
 
 class tr_config(C.Structure):
@@ -50,6 +51,18 @@ class tr_loss_rows(C.Structure):
 
 class tr_loss_grads(C.Structure):
     _fields_ = [("d_hidden", C.c_void_p), ("d_weight", C.c_void_p), ("d_hidden_stride", C.c_int64), ("d_weight_stride", C.c_int64)]
+
+
+class tr_pick_config(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("max_rows", "vocab", "dtype")]
+
+
+class tr_pick_rows(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("stride", C.c_int64), ("rows", C.c_int32)]
+
+
+class tr_sample_how(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("u", "temperatures", "top_ks", "top_ps", "min_ps")] + [("temperature", C.c_float), ("top_k", C.c_int32), ("top_p", C.c_float), ("min_p", C.c_float)]
 
 
 class tr_weights(C.Structure):
@@ -102,6 +115,13 @@ def load_library():
             f.argtypes = [lc, vp, sz, vp, lr, vp, vp]
         for f in (L.tr_cross_entropy_grad, L.tr_distill_grad):
             f.argtypes = [lc, vp, sz, vp, lr, vp, vp, C.POINTER(tr_loss_grads)]
+        pc, pr = C.POINTER(tr_pick_config), C.POINTER(tr_pick_rows)
+        L.tr_pick_workspace_bytes.argtypes = [pc]; L.tr_pick_workspace_bytes.restype = sz
+        L.tr_sample.argtypes = [pc, vp, sz, vp, pr, C.POINTER(tr_sample_how), vp, vp]
+        L.tr_top.argtypes = [pc, vp, sz, vp, pr, i32, vp, vp]
+        L.tr_grad_workspace_bytes.argtypes = []; L.tr_grad_workspace_bytes.restype = sz
+        L.tr_grad_norm.argtypes = [vp, sz, vp, i32, vp, vp, vp, vp]
+        L.tr_grad_clip.argtypes = [vp, sz, vp, i32, vp, vp, vp, vp, f32, vp]
         L.tr_last_error.argtypes = [vp]; L.tr_last_error.restype = C.c_char_p
         _lib = L
     return _lib
