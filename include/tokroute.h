@@ -352,8 +352,8 @@ int tr_distill_grad(const tr_loss_config *cfg, void *workspace, size_t workspace
  * Weights are sums' terms in 64 bits, rounded to units of 2^-(62 - log2 vocab) of the largest (2^-44 at 151936): the same inputs give the same token, whatever else runs.
  *
  * Errors: TR_ERR_INVALID_ARG, TR_ERR_SHAPE (unsupported type or sizes), TR_ERR_CAPACITY (more rows or entries than configured, workspace too small), before anything is enqueued;
- * TR_ERR_HIP. Calls only enqueue, with the device of the stream and of all pointers current. The workspace is cleared (zeros) by the caller once, before its first call, belongs to one configuration, and
- * calls that share it must be ordered with respect to each other; but for what is cleared nothing in it outlives a call (after TR_ERR_HIP clear it again). rows may be 0. */
+ * TR_ERR_HIP. Calls only enqueue, with the device of the stream and of all pointers current. Calls that share a workspace must be ordered with respect to each other; nothing in it outlives
+ * a call. rows may be 0. */
 typedef struct tr_pick_config {
     int32_t max_rows, vocab;      /* 1 .. 2^20 both */
     int32_t dtype;                /* of the logits: TR_F32 / TR_BF16 */
@@ -392,7 +392,7 @@ int tr_top(const tr_pick_config *cfg, void *workspace, size_t workspace_bytes, v
  * n gradients; grads, out, counts, dtypes are HOST arrays [n], read before the call returns: DEVICE pointers (aligned to their elements; of count 0: any), elements (0 .. 2^40), TR_F32 /
  * TR_BF16. out[i] may be grads[i]: in place; then nothing is written where nothing is to be scaled. Otherwise what is written may overlap nothing of the call (TR_ERR_INVALID_ARG); tr_grad_norm
  * takes a gradient twice. max_norm >= 0, may be infinite. norm: DEVICE float [1], outside of the gradients.
- * Workspace (256-byte aligned DEVICE memory), errors and streams: as for tokens from logits above, cleared once in particular. */
+ * Workspace (256-byte aligned DEVICE memory), errors and streams: as for tokens from logits above. */
 size_t tr_grad_workspace_bytes(void);
 int tr_grad_norm(void *workspace, size_t workspace_bytes, void *hip_stream, int32_t n, const void *const *grads, const int64_t *counts, const int32_t *dtypes, float *norm);
 int tr_grad_clip(void *workspace, size_t workspace_bytes, void *hip_stream, int32_t n, const void *const *grads, void *const *out, const int64_t *counts, const int32_t *dtypes,

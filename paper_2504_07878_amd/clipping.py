@@ -4,7 +4,7 @@ There is no CPU fallback: without the built library or without a GPU calls raise
 """
 from __future__ import annotations
 
-import ctypes as C
+from array import array
 
 import torch
 
@@ -29,35 +29,40 @@ class Clipper:
         if not torch.cuda.is_available():
             raise RuntimeError("tokroute needs a GPU: no CPU path exists")
         self.lib = tokroute.load_library()
-        self.workspace = torch.zeros(self.lib.tr_grad_workspace_bytes(), dtype=torch.uint8, device=device)
+        self.workspace = torch.empty(self.lib.tr_grad_workspace_bytes(), dtype=torch.uint8, device=device)
         self.device = self.workspace.device
         self._home = torch.cuda.current_stream(self.device)
 
     # -- helpers
     def _list(self, grads, what="gradients"):
-        for t in grads:
-            if not (isinstance(t, torch.Tensor) and t.dtype in _DTYPES and t.device == self.device and t.layout == torch.strided and _dense(t)):
-                raise ValueError(f"{what}: float32 or bfloat16 tensors on {self.device}, each of elements that fill one piece of memory")
-        return (C.c_void_p * len(grads))(*[t.data_ptr() for t in grads])
+        """Addresses; a few calls over all tensors rather than several a tensor (hundreds of gradients take longer to look at than to read)."""
+        try:
+            fine = set(map(torch.Tensor.get_device, grads)) <= {self.device.index} and all(map(torch.Tensor.is_contiguous, grads)) and {t.dtype for t in grads} <= _DTYPES.keys()
+        except (TypeError, RuntimeError):       # no tensor, or one of another layout
+            fine = False
+        if not fine and not all(isinstance(t, torch.Tensor) and t.dtype in _DTYPES and t.device == self.device and t.layout == torch.strided and _dense(t) for t in grads):
+            raise ValueError(f"{what}: float32 or bfloat16 tensors on {self.device}, each of elements that fill one piece of memory")
+        return array("q", map(torch.Tensor.data_ptr, grads))
 
-    def _call(self, fn, what, *args):
+    @staticmethod
+    def _sizes(grads):
+        return array("q", map(torch.Tensor.numel, grads)), array("i", [_DTYPES[t.dtype] for t in grads])
+
+    def _call(self, fn, what, arrays, *args):
         s = torch.cuda.current_stream(self.device)
         if s != self._home:
             self.workspace.record_stream(s)    # its memory is not handed on while work of that stream may use it
         with torch.cuda.device(self.device):   # a default stream is the current device's
-            rc = fn(self.workspace.data_ptr(), self.workspace.numel(), s.cuda_stream, *args)
+            rc = fn(self.workspace.data_ptr(), self.workspace.numel(), s.cuda_stream, len(arrays[0]), *[x.buffer_info()[0] for x in arrays], *args)
         if rc:
             raise TokrouteError(rc, what)
-
-    def _sizes(self, grads):
-        return (C.c_int64 * len(grads))(*[t.numel() for t in grads]), (C.c_int32 * len(grads))(*[_DTYPES[t.dtype] for t in grads])
 
     # -- the ABI
     def norm(self, grads):
         """Length of all gradients together: a float32 tensor of no dimensions."""
         grads = [t for t in grads if t is not None]
         at, norm = self._list(grads), torch.empty((), dtype=torch.float32, device=self.device)
-        self._call(self.lib.tr_grad_norm, "tr_grad_norm", len(grads), at, *self._sizes(grads), norm.data_ptr())
+        self._call(self.lib.tr_grad_norm, "tr_grad_norm", [at, *self._sizes(grads)], norm.data_ptr())
         return norm
 
     def clip(self, grads, max_norm: float, out=None):
@@ -74,5 +79,5 @@ class Clipper:
             if any(a.dtype != b.dtype or a.shape != b.shape or (a.stride() != b.stride() and not (a.is_contiguous() and b.is_contiguous())) for a, b in zip(grads, out)):
                 raise ValueError("out: tensors of the gradients' shapes, types and strides")
         norm = torch.empty((), dtype=torch.float32, device=self.device)
-        self._call(self.lib.tr_grad_clip, "tr_grad_clip", len(grads), at, to, *self._sizes(grads), max_norm, norm.data_ptr())
+        self._call(self.lib.tr_grad_clip, "tr_grad_clip", [at, to, *self._sizes(grads)], max_norm, norm.data_ptr())
         return norm

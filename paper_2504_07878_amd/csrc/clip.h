@@ -4,9 +4,10 @@
 
 namespace tr {
 
-// A launch takes up to CLIP_LIST gradients, handed over by value (nothing of a call lies in memory that has to outlive it), as tiles of CLIP_TILE elements numbered through.
-constexpr int CLIP_LIST = 112, CLIP_TILE = 8192;
-constexpr int CLIP_GROUPS = 2048;              // most workgroups of a launch, each with a place for its sum
+// A launch takes up to CLIP_LIST gradients, handed over by value (nothing of a call lies in memory that has to outlive it), as tiles of CLIP_TILE bytes numbered through.
+constexpr int CLIP_LIST = 112, CLIP_TILE = 32768;
+constexpr int CLIP_GROUPS = 2048;              // most workgroups of a launch, each of which leaves a sum
+constexpr int CLIP_SUMS = 4096;                // places for sums in the workspace
 
 struct ClipList {
     const void *in[CLIP_LIST];
@@ -18,17 +19,13 @@ struct ClipList {
 };
 static_assert(sizeof(ClipList) < 4000, "kernel arguments");
 
-struct ClipState {                             // in the workspace; arrived is zero before and after every launch
-    uint32_t arrived;
-    float scale;                               // of the last call
-    double squares;                            // of the lists before
-    char pad[240];
-    double part[CLIP_GROUPS];
-};
+inline int clip_groups(const ClipList &l) { return l.tile[l.n] < CLIP_GROUPS ? (int)l.tile[l.n] : CLIP_GROUPS; }
 
-// Sum of squares of a list, added to those of the lists before (first: there are none). The last list leaves the norm, and the scale for max_norm.
-void launch_clip_squares(hipStream_t s, const ClipList &l, ClipState *state, bool first, bool last, double max_norm, float *norm);
-// out = in * scale
-void launch_clip_scale(hipStream_t s, const ClipList &l, const ClipState *state);
+// Sums of squares of a list, clip_groups of them, from sums[0] on
+void launch_clip_squares(hipStream_t s, const ClipList &l, double *sums);
+// The first n sums: into sums[0], and their root into norm (either may be NULL)
+void launch_clip_join(hipStream_t s, const double *sums, int n, double *to, float *norm);
+// out = in * min(1, max_norm / norm), norm the root of the first n sums, which is left in `norm` (where it is not NULL)
+void launch_clip_scale(hipStream_t s, const ClipList &l, const double *sums, int n, double max_norm, float *norm);
 
 }  // namespace tr

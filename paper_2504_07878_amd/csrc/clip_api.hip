@@ -35,10 +35,28 @@ bool overlap(int n, const void *const *in, void *const *out, const int64_t *coun
     return false;
 }
 
+// f(list) for all gradients that have elements
+template <class F> void lists(int n, const void *const *in, void *const *out, const int64_t *counts, const int32_t *dtypes, F f)
+{
+    ClipList l{};
+    for (int i = 0; i < n; ++i) {
+        if (!counts[i]) continue;
+        const uint64_t bytes = (uint64_t)counts[i] * size_of(dtypes[i]), tiles = (bytes + CLIP_TILE - 1) / CLIP_TILE;
+        if (l.n == CLIP_LIST || l.tile[l.n] + tiles > 0x7fffffffu) {      // (one gradient alone has fewer)
+            f(l);
+            l.n = 0;
+        }
+        l.in[l.n] = in[i]; l.out[l.n] = out ? out[i] : nullptr; l.count[l.n] = counts[i]; l.half[l.n] = dtypes[i] == TR_BF16;
+        l.tile[l.n + 1] = l.tile[l.n] + (uint32_t)tiles;
+        ++l.n;
+    }
+    if (l.n) f(l);
+}
+
 int run(void *ws, size_t ws_bytes, void *stream, int n, const void *const *in, void *const *out, const int64_t *counts, const int32_t *dtypes, double max_norm, float *norm)
 {
     if (!ws || !norm || n < 0 || (n && (!in || !counts || !dtypes))) return TR_ERR_INVALID_ARG;
-    if (ws_bytes < sizeof(ClipState)) return TR_ERR_CAPACITY;
+    if (ws_bytes < CLIP_SUMS * sizeof(double)) return TR_ERR_CAPACITY;
     if ((reinterpret_cast<uintptr_t>(ws) & 255) || (reinterpret_cast<uintptr_t>(norm) & 3) || !(max_norm >= 0)) return TR_ERR_INVALID_ARG;
     for (int i = 0; i < n; ++i) {
         if (dtypes[i] != TR_F32 && dtypes[i] != TR_BF16) return TR_ERR_SHAPE;
@@ -54,26 +72,27 @@ int run(void *ws, size_t ws_bytes, void *stream, int n, const void *const *in, v
         }
     }
     hipStream_t s = (hipStream_t)stream;
-    ClipState *const state = (ClipState *)ws;
-    for (int scale = 0; scale < (out ? 2 : 1); ++scale) {
-        int i = 0;
-        bool first = true;
-        do {
-            ClipList l{};
-            uint64_t tiles = 0;
-            for (; i < n && l.n < CLIP_LIST; ++i) {
-                if (!counts[i]) continue;
-                const uint64_t more = ((uint64_t)counts[i] + CLIP_TILE - 1) / CLIP_TILE;
-                if (tiles + more > 0x7fffffffu) break;        // (one gradient alone has fewer)
-                l.in[l.n] = in[i]; l.out[l.n] = out ? out[i] : nullptr; l.count[l.n] = counts[i]; l.half[l.n] = dtypes[i] == TR_BF16; l.tile[l.n] = (uint32_t)tiles;
-                tiles += more;
-                l.tile[++l.n] = (uint32_t)tiles;
-            }
-            while (i < n && !counts[i]) ++i;
-            if (scale) launch_clip_scale(s, l, state);
-            else launch_clip_squares(s, l, state, first, i >= n, max_norm, norm);
-            first = false;
-        } while (i < n);
+    double *const sums = (double *)ws;
+    int have = 0;                          // sums so far
+    lists(n, in, out, counts, dtypes, [&](const ClipList &l) {
+        if (have + clip_groups(l) > CLIP_SUMS) {
+            launch_clip_join(s, sums, have, sums, nullptr);
+            have = 1;
+        }
+        launch_clip_squares(s, l, sums + have);
+        have += clip_groups(l);
+    });
+    if (!out || !have) launch_clip_join(s, sums, have, nullptr, norm);
+    else {
+        // every workgroup of the scaling adds the sums up by itself, which saves a launch; many are added up once
+        if (have > CLIP_GROUPS) {
+            launch_clip_join(s, sums, have, sums, nullptr);
+            have = 1;
+        }
+        lists(n, in, out, counts, dtypes, [&](const ClipList &l) {
+            launch_clip_scale(s, l, sums, have, max_norm, norm);
+            norm = nullptr;
+        });
     }
     return hipGetLastError() == hipSuccess ? TR_OK : TR_ERR_HIP;
 }
@@ -82,7 +101,7 @@ int run(void *ws, size_t ws_bytes, void *stream, int n, const void *const *in, v
 
 extern "C" {
 
-size_t tr_grad_workspace_bytes(void) { return sizeof(ClipState); }
+size_t tr_grad_workspace_bytes(void) { return CLIP_SUMS * sizeof(double); }
 
 int tr_grad_norm(void *workspace, size_t workspace_bytes, void *hip_stream, int32_t n, const void *const *grads, const int64_t *counts, const int32_t *dtypes, float *norm)
 {

@@ -2,26 +2,11 @@
 // squares would lose gradients below 1e-23 and overflow from 1e19 on.
 #include "clip.h"
 
-#include <algorithm>
-
 namespace tr {
 
 namespace {
 
-constexpr int THREADS = 256;
-
-struct Tile { int of; long long at; int len; };
-
-__device__ __forceinline__ Tile tile_at(const ClipList &l, uint32_t t)
-{
-    int lo = 0, hi = l.n - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (l.tile[mid] <= t) lo = mid; else hi = mid - 1;
-    }
-    const long long at = (long long)(t - l.tile[lo]) * CLIP_TILE, left = l.count[lo] - at;
-    return Tile{lo, at, (int)(left < CLIP_TILE ? left : CLIP_TILE)};
-}
+constexpr int THREADS = 256, WAVES = THREADS / 64, LOADS = CLIP_TILE / 16 / THREADS;
 
 __device__ __forceinline__ float wide(float v) { return v; }
 __device__ __forceinline__ float wide(bf16_t v) { return __uint_as_float((uint32_t)v << 16); }
@@ -32,19 +17,45 @@ __device__ __forceinline__ void put(bf16_t &to, float v)
     __builtin_memcpy(&to, &b, 2);
 }
 
+template <class T> struct Vector { T v[16 / sizeof(T)]; };
+
+// f(gradient, first element, elements) for the tiles of a list that are this workgroup's
+template <class F> __device__ __forceinline__ void each_tile(const ClipList &l, F f)
+{
+    const uint32_t tiles = l.tile[l.n];
+    int i = 0;
+    for (uint32_t t = blockIdx.x; t < tiles; t += gridDim.x) {
+        while (l.tile[i + 1] <= t) ++i;
+        const int size = l.half[i] ? 2 : 4;
+        const long long at = (long long)(t - l.tile[i]) * (CLIP_TILE / size), left = l.count[i] - at;
+        f(i, at, (int)(left < CLIP_TILE / size ? left : CLIP_TILE / size));
+    }
+}
+
 template <class T> __device__ __forceinline__ double squares_of(const T *p, int len)
 {
     constexpr int N = 16 / sizeof(T);
     double sum = 0;
+    const auto add = [&](const Vector<T> &x) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) { const double y = wide(x.v[e]); sum = fma(y, y, sum); }
+    };
+    if (len == CLIP_TILE / (int)sizeof(T)) {          // a whole tile: all its loads at once
+        Vector<T> x[LOADS];
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) __builtin_memcpy(&x[i], p + (i * THREADS + threadIdx.x) * N, 16);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) add(x[i]);
+        return sum;
+    }
     for (int i = threadIdx.x * N; i < len; i += THREADS * N) {
-        T v[N];
-        if (i + N <= len) __builtin_memcpy(v, p + i, 16);
+        Vector<T> x{};
+        if (i + N <= len) __builtin_memcpy(&x, p + i, 16);
         else {
 #pragma unroll
-            for (int e = 0; e < N; ++e) v[e] = i + e < len ? p[i + e] : T(0);
+            for (int e = 0; e < N; ++e) if (i + e < len) x.v[e] = p[i + e];
         }
-#pragma unroll
-        for (int e = 0; e < N; ++e) { const double x = wide(v[e]); sum = fma(x, x, sum); }
+        add(x);
     }
     return sum;
 }
@@ -52,87 +63,93 @@ template <class T> __device__ __forceinline__ double squares_of(const T *p, int 
 __device__ __forceinline__ double sum_of_all(double v, double *s)
 {
     for (int o = 1; o < 64; o *= 2) v += __shfl_xor(v, o);
-    __syncthreads();
     if (threadIdx.x % 64 == 0) s[threadIdx.x / 64] = v;
     __syncthreads();
-    return s[0] + s[1] + s[2] + s[3];
+    v = s[0];
+    for (int w = 1; w < WAVES; ++w) v += s[w];
+    return v;
 }
 
-// bound by memory
-__global__ __launch_bounds__(THREADS) void squares_kernel(ClipList l, ClipState *state, bool first, bool last, double max_norm, float *norm)
+__device__ __forceinline__ double sum_of_sums(const double *sums, int n, double *s)
 {
-    __shared__ double s_sum[THREADS / 64];
-    __shared__ bool s_last;
+    double v = 0;
+    for (int i = threadIdx.x; i < n; i += THREADS) v += sums[i];
+    return sum_of_all(v, s);
+}
+
+// Bound by memory.
+__global__ __launch_bounds__(THREADS) void squares_kernel(ClipList l, double *sums)
+{
+    __shared__ double s[WAVES];
     double sum = 0;
-    const uint32_t tiles = l.tile[l.n];
-    for (uint32_t t = blockIdx.x; t < tiles; t += gridDim.x) {
-        const Tile x = tile_at(l, t);
-        sum += l.half[x.of] ? squares_of((const bf16_t *)l.in[x.of] + x.at, x.len) : squares_of((const float *)l.in[x.of] + x.at, x.len);
-    }
-    sum = sum_of_all(sum, s_sum);
+    each_tile(l, [&](int i, long long at, int len) { sum += l.half[i] ? squares_of((const bf16_t *)l.in[i] + at, len) : squares_of((const float *)l.in[i] + at, len); });
+    sum = sum_of_all(sum, s);
+    if (threadIdx.x == 0) sums[blockIdx.x] = sum;
+}
+
+__global__ __launch_bounds__(THREADS) void join_kernel(const double *sums, int n, double *to, float *norm)
+{
+    __shared__ double s[WAVES];
+    const double sum = sum_of_sums(sums, n, s);      // (behind a barrier: `to` may be one of them)
     if (threadIdx.x == 0) {
-        // past the L2, and there before it is counted: the last to arrive finds them all
-        __hip_atomic_store(&state->part[blockIdx.x], sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        __builtin_amdgcn_s_waitcnt(0);
-        s_last = __hip_atomic_fetch_add(&state->arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
-    }
-    __syncthreads();
-    if (!s_last) return;
-    sum = 0;
-    for (uint32_t i = threadIdx.x; i < gridDim.x; i += THREADS) sum += __hip_atomic_load(&state->part[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    sum = sum_of_all(sum, s_sum);
-    if (threadIdx.x == 0) {
-        state->arrived = 0;
-        if (!first) sum += state->squares;
-        state->squares = sum;
-        if (last) {
-            const double length = sqrt(sum);
-            *norm = (float)length;
-            state->scale = length > max_norm && length < INFINITY ? (float)(max_norm / length) : 1.f;     // (infinity, NaN: 1)
-        }
+        if (to) *to = sum;
+        if (norm) *norm = (float)sqrt(sum);
     }
 }
 
 template <class T> __device__ __forceinline__ void scale_tile(const T *p, T *q, int len, float by)
 {
     constexpr int N = 16 / sizeof(T);
-    for (int i = threadIdx.x * N; i < len; i += THREADS * N) {
-        T v[N];
-        if (i + N <= len) {
-            __builtin_memcpy(v, p + i, 16);
+    const auto scale = [&](Vector<T> &x) {
 #pragma unroll
-            for (int e = 0; e < N; ++e) put(v[e], wide(v[e]) * by);
-            __builtin_memcpy(q + i, v, 16);
+        for (int e = 0; e < N; ++e) put(x.v[e], wide(x.v[e]) * by);
+    };
+    if (len == CLIP_TILE / (int)sizeof(T)) {
+        Vector<T> x[LOADS];
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) __builtin_memcpy(&x[i], p + (i * THREADS + threadIdx.x) * N, 16);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            scale(x[i]);
+            __builtin_memcpy(q + (i * THREADS + threadIdx.x) * N, &x[i], 16);
+        }
+        return;
+    }
+    for (int i = threadIdx.x * N; i < len; i += THREADS * N) {
+        if (i + N <= len) {
+            Vector<T> x;
+            __builtin_memcpy(&x, p + i, 16);
+            scale(x);
+            __builtin_memcpy(q + i, &x, 16);
         } else {
             for (int e = i; e < len; ++e) put(q[e], wide(p[e]) * by);
         }
     }
 }
 
-__global__ __launch_bounds__(THREADS) void scale_kernel(ClipList l, const ClipState *state)
+// Bound by memory.
+__global__ __launch_bounds__(THREADS) void scale_kernel(ClipList l, const double *sums, int n, double max_norm, float *norm)
 {
-    const float by = state->scale;
-    const uint32_t tiles = l.tile[l.n];
-    for (uint32_t t = blockIdx.x; t < tiles; t += gridDim.x) {
-        const Tile x = tile_at(l, t);
-        if (by == 1.f && l.in[x.of] == l.out[x.of]) continue;      // as they are
-        if (l.half[x.of]) scale_tile((const bf16_t *)l.in[x.of] + x.at, (bf16_t *)l.out[x.of] + x.at, x.len, by);
-        else scale_tile((const float *)l.in[x.of] + x.at, (float *)l.out[x.of] + x.at, x.len, by);
-    }
+    __shared__ double s[WAVES];
+    const double length = sqrt(sum_of_sums(sums, n, s));
+    if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)length;
+    const float by = length > max_norm && length < INFINITY ? (float)(max_norm / length) : 1.f;      // (infinity, NaN: 1)
+    each_tile(l, [&](int i, long long at, int len) {
+        if (by == 1.f && l.in[i] == l.out[i]) return;      // as they are
+        if (l.half[i]) scale_tile((const bf16_t *)l.in[i] + at, (bf16_t *)l.out[i] + at, len, by);
+        else scale_tile((const float *)l.in[i] + at, (float *)l.out[i] + at, len, by);
+    });
 }
-
-int groups(const ClipList &l) { return (int)std::max(1u, std::min<uint32_t>(CLIP_GROUPS, l.tile[l.n])); }
 
 }  // namespace
 
-void launch_clip_squares(hipStream_t s, const ClipList &l, ClipState *state, bool first, bool last, double max_norm, float *norm)
-{
-    hipLaunchKernelGGL(squares_kernel, dim3(groups(l)), dim3(THREADS), 0, s, l, state, first, last, max_norm, norm);
-}
+void launch_clip_squares(hipStream_t s, const ClipList &l, double *sums) { hipLaunchKernelGGL(squares_kernel, dim3(clip_groups(l)), dim3(THREADS), 0, s, l, sums); }
 
-void launch_clip_scale(hipStream_t s, const ClipList &l, const ClipState *state)
+void launch_clip_join(hipStream_t s, const double *sums, int n, double *to, float *norm) { hipLaunchKernelGGL(join_kernel, dim3(1), dim3(THREADS), 0, s, sums, n, to, norm); }
+
+void launch_clip_scale(hipStream_t s, const ClipList &l, const double *sums, int n, double max_norm, float *norm)
 {
-    if (l.n) hipLaunchKernelGGL(scale_kernel, dim3(groups(l)), dim3(THREADS), 0, s, l, state);
+    hipLaunchKernelGGL(scale_kernel, dim3(clip_groups(l)), dim3(THREADS), 0, s, l, sums, n, max_norm, norm);
 }
 
 }  // namespace tr

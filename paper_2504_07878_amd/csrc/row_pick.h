@@ -9,11 +9,41 @@ namespace tr {
 
 constexpr int PICK_MAX_ROWS = 1 << 20, PICK_MAX_VOCAB = 1 << 20, PICK_MAX_ENTRIES = 1024;
 
+// A wavefront reads PICK_PART tokens of a row, a workgroup PICK_GROUP. Rows of more than one workgroup meet in the workspace: every part leaves its sum and its largest tokens, from which one
+// workgroup decides. Workspace and launches are for PICK_ROWS rows at a time.
+constexpr int PICK_THREADS = 512, PICK_WAVES = PICK_THREADS / 64, PICK_EACH = 16, PICK_PART = 64 * PICK_EACH, PICK_GROUP = PICK_PART * PICK_WAVES;
+constexpr int PICK_ROWS = 1024;
+constexpr int PICK_LISTED = PICK_THREADS * PICK_EACH;     // most tokens of a row that parts leave, and that the deciding workgroup holds
+constexpr int PICK_PART_LISTED = 64;                      // of one part
+constexpr int PICK_STEPS = 512;                           // of a histogram of masses over the logits of a row
+
+struct alignas(16) PickHead {
+    union { double sum; unsigned long long mass; };   // of the part's weights, relative to its own largest; of what it keeps, in units
+    uint32_t top;          // largest key
+    uint32_t from;         // all the part's tokens of this key or a larger one are listed
+    uint32_t count, pad;   // those
+};
+
+// A row whose filters end below what the parts have listed
+struct alignas(16) PickSearch {
+    uint32_t stage;        // PICK_*
+    uint32_t top_key, least;   // largest key; the smallest that min_p keeps
+    float from, scale;     // logits below `from` in steps of 1 / scale
+    uint32_t found, pad;   // the stage that it turned out to be
+    unsigned long long want;   // mass that it keeps
+};
+enum { PICK_DONE = 0, PICK_STEP = 1,    // the step, then the place in it
+       PICK_LEAST = 2,                  // everything from `least` on
+       PICK_WHOLE = 3 };                // one workgroup looks through the row
+
 struct PickArgs {
     const void *logits;
     long long stride;                // elements from row to row
     int rows, vocab, dtype;          // DT_*
     int unit;                        // masses are in units of 2^-unit: vocab of them stay below 2^63
+    int groups, listed;              // workgroups a row, tokens a part may leave
+    int listed_lanes;                // lanes whose largest token is among them
+    uint32_t listed_inverse;         // 2^32 / listed, rounded up: quotients of numbers below 2^16
     // draws: a number a row, or the value for all
     const float *u, *temperatures, *top_ps, *min_ps;
     const int *top_ks;
@@ -25,8 +55,22 @@ struct PickArgs {
     int entries;
     int32_t *ids;
     float *values;
+    // workspace (rows of more than one workgroup)
+    PickHead *head;                  // [rows][parts]
+    uint2 *list;                     // [rows][parts][listed]: key, id
+    PickSearch *search;              // [rows]
+    unsigned long long *steps;       // [rows][groups][PICK_STEPS]
+    bool searched;                   // there may be rows to search
 };
 
+inline int pick_groups(int vocab) { return (vocab + PICK_GROUP - 1) / PICK_GROUP; }
+inline int pick_listed(int vocab)
+{
+    const int most = PICK_LISTED / (pick_groups(vocab) * PICK_WAVES);
+    return most < PICK_PART_LISTED ? most : PICK_PART_LISTED;
+}
+
+// rows of at most PICK_ROWS
 void launch_sample(hipStream_t s, const PickArgs &a);
 void launch_top(hipStream_t s, const PickArgs &a);
 

@@ -14,7 +14,25 @@ bool config_ok(const tr_pick_config *c)
     return c && c->max_rows >= 1 && c->max_rows <= PICK_MAX_ROWS && c->vocab >= 1 && c->vocab <= PICK_MAX_VOCAB && (c->dtype == TR_F32 || c->dtype == TR_BF16);
 }
 
-size_t workspace_of(const tr_pick_config *) { return 256; }
+size_t up(size_t v) { return (v + 255) / 256 * 256; }
+
+// Rows of one workgroup need none of it but for the smallest size there is.
+struct Plan { size_t head, list, search, steps, total; };
+Plan plan_of(const tr_pick_config *c)
+{
+    Plan p{};
+    const size_t rows = std::min(c->max_rows, PICK_ROWS), groups = pick_groups(c->vocab), parts = rows * groups * PICK_WAVES;
+    p.total = 256;
+    if (groups > 1) {
+        p.list = up(parts * sizeof(PickHead));
+        p.search = p.list + up(parts * pick_listed(c->vocab) * 8);
+        p.steps = p.search + up(rows * sizeof(PickSearch));
+        p.total = p.steps + up(rows * groups * PICK_STEPS * 8);
+    }
+    return p;
+}
+
+size_t workspace_of(const tr_pick_config *c) { return plan_of(c).total; }
 
 // What both calls check; TR_OK, or an error before anything is enqueued.
 int arguments(const tr_pick_config *c, const tr_pick_rows *in, void *ws, size_t ws_bytes, PickArgs &a)
@@ -30,10 +48,34 @@ int arguments(const tr_pick_config *c, const tr_pick_rows *in, void *ws, size_t 
     int bits = 0;
     while ((1 << bits) < c->vocab) ++bits;
     a.unit = std::min(52, 62 - bits);
+    a.groups = pick_groups(c->vocab);
+    a.listed = pick_listed(c->vocab);
+    // of x lanes in 64 whose largest of PICK_EACH tokens is among them, the others' follow: with tokens in any order 64 ln(64 / (64 - x)) tokens, here 0.85 of those that fit
+    a.listed_lanes = std::max(1, (int)(64 * (1 - std::exp(-0.85 * a.listed / 64))));
+    a.listed_inverse = (uint32_t)((((uint64_t)1 << 32) + a.listed - 1) / a.listed);
+    const Plan p = plan_of(c);
+    char *const b = (char *)ws;
+    a.head = (PickHead *)(b + p.head); a.list = (uint2 *)(b + p.list); a.search = (PickSearch *)(b + p.search); a.steps = (unsigned long long *)(b + p.steps);
     return TR_OK;
 }
 
-int enqueued() { return hipGetLastError() == hipSuccess ? TR_OK : TR_ERR_HIP; }
+// PICK_ROWS rows at a time
+template <class Launch> int enqueue(const PickArgs &all, Launch launch)
+{
+    const size_t size = all.dtype == DT_BF16 ? 2 : 4;
+    for (int at = 0; at < all.rows; at += PICK_ROWS) {
+        PickArgs a = all;
+        a.rows = std::min(PICK_ROWS, all.rows - at);
+        a.logits = (const char *)all.logits + (size_t)at * all.stride * size;
+        for (const float **p : {&a.u, &a.temperatures, &a.top_ps, &a.min_ps}) if (*p) *p += at;
+        if (a.top_ks) a.top_ks += at;
+        if (a.token) { a.token += at; a.logprob += at; }
+        if (a.ids) { a.ids += (size_t)at * all.entries; a.values += (size_t)at * all.entries; }
+        launch(a);
+    }
+    return hipGetLastError() == hipSuccess ? TR_OK : TR_ERR_HIP;
+}
+
 bool aligned(const void *p) { return !(reinterpret_cast<uintptr_t>(p) & 3); }
 
 }  // namespace
@@ -57,8 +99,9 @@ int tr_sample(const tr_pick_config *cfg, void *workspace, size_t workspace_bytes
     a.u = how->u; a.temperatures = how->temperatures; a.top_ks = how->top_ks; a.top_ps = how->top_ps; a.min_ps = how->min_ps;
     a.temperature = how->temperature; a.top_k = how->top_k; a.top_p = how->top_p; a.min_p = how->min_p;
     a.token = token; a.logprob = logprob;
-    launch_sample((hipStream_t)hip_stream, a);
-    return enqueued();
+    // (top-k ends within what the parts list but for rows whose largest logits lie oddly; one workgroup searches these)
+    a.searched = a.groups > 1 && (a.top_ps || a.min_ps || a.top_p < 1.f || a.min_p > 0.f) && (a.top_ks || a.top_k == 0);
+    return enqueue(a, [&](const PickArgs &p) { launch_sample((hipStream_t)hip_stream, p); });
 }
 
 int tr_top(const tr_pick_config *cfg, void *workspace, size_t workspace_bytes, void *hip_stream, const tr_pick_rows *in, int32_t entries, int32_t *ids, float *values)
@@ -71,8 +114,7 @@ int tr_top(const tr_pick_config *cfg, void *workspace, size_t workspace_bytes, v
     if (!a.rows) return TR_OK;
     if (!ids || !values) return TR_ERR_INVALID_ARG;
     a.entries = entries; a.ids = ids; a.values = values;
-    launch_top((hipStream_t)hip_stream, a);
-    return enqueued();
+    return enqueue(a, [&](const PickArgs &p) { launch_top((hipStream_t)hip_stream, p); });
 }
 
 }  // extern "C"

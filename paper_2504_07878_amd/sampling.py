@@ -43,7 +43,7 @@ class Sampler:
         nbytes = self.lib.tr_pick_workspace_bytes(C.byref(self.cfg))
         if nbytes == 0:
             raise TokrouteError(tokroute.ERR_SHAPE, "tr_pick_workspace_bytes", "(sizes or types not supported)")
-        self.workspace = torch.zeros(nbytes, dtype=torch.uint8, device=device)
+        self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
         self.device = self.workspace.device
         self._home = torch.cuda.current_stream(self.device)
 
