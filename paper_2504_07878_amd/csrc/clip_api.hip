@@ -35,11 +35,12 @@ bool overlap(int n, const void *const *in, void *const *out, const int64_t *coun
     return false;
 }
 
-// f(list) for all gradients that have elements
-template <class F> void lists(int n, const void *const *in, void *const *out, const int64_t *counts, const int32_t *dtypes, F f)
+// f(list) for all gradients that have elements, from the last on where asked
+template <class F> void lists(bool back, int n, const void *const *in, void *const *out, const int64_t *counts, const int32_t *dtypes, F f)
 {
     ClipList l{};
-    for (int i = 0; i < n; ++i) {
+    for (int k = 0; k < n; ++k) {
+        const int i = back ? n - 1 - k : k;
         if (!counts[i]) continue;
         const uint64_t bytes = (uint64_t)counts[i] * size_of(dtypes[i]), tiles = (bytes + CLIP_TILE - 1) / CLIP_TILE;
         if (l.n == CLIP_LIST || l.tile[l.n] + tiles > 0x7fffffffu) {      // (one gradient alone has fewer)
@@ -74,7 +75,7 @@ int run(void *ws, size_t ws_bytes, void *stream, int n, const void *const *in, v
     hipStream_t s = (hipStream_t)stream;
     double *const sums = (double *)ws;
     int have = 0;                          // sums so far
-    lists(n, in, out, counts, dtypes, [&](const ClipList &l) {
+    lists(false, n, in, out, counts, dtypes, [&](const ClipList &l) {
         if (have + clip_groups(l) > CLIP_SUMS) {
             launch_clip_join(s, sums, have, sums, nullptr);
             have = 1;
@@ -89,7 +90,7 @@ int run(void *ws, size_t ws_bytes, void *stream, int n, const void *const *in, v
             launch_clip_join(s, sums, have, sums, nullptr);
             have = 1;
         }
-        lists(n, in, out, counts, dtypes, [&](const ClipList &l) {
+        lists(true, n, in, out, counts, dtypes, [&](const ClipList &l) {
             launch_clip_scale(s, l, sums, have, max_norm, norm);
             norm = nullptr;
         });

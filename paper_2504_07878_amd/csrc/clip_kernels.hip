@@ -18,16 +18,23 @@ __device__ __forceinline__ void put(bf16_t &to, float v)
 }
 
 template <class T> struct Vector { T v[16 / sizeof(T)]; };
+typedef __attribute__((ext_vector_type(4), aligned(2))) uint32_t u32x4_any;
+template <class T> __device__ __forceinline__ void store_past(T *p, const Vector<T> &x)
+{
+    u32x4_any v;
+    __builtin_memcpy(&v, &x, 16);
+    __builtin_nontemporal_store(v, (u32x4_any *)p);
+}
 
 // f(gradient, first element, elements) for the tiles of a list that are this workgroup's
-template <class F> __device__ __forceinline__ void each_tile(const ClipList &l, F f)
+template <bool BACK, class F> __device__ __forceinline__ void each_tile(const ClipList &l, F f)
 {
     const uint32_t tiles = l.tile[l.n];
     int i = 0;
     for (uint32_t t = blockIdx.x; t < tiles; t += gridDim.x) {
         while (l.tile[i + 1] <= t) ++i;
         const int size = l.half[i] ? 2 : 4;
-        const long long at = (long long)(t - l.tile[i]) * (CLIP_TILE / size), left = l.count[i] - at;
+        const long long at = (long long)(BACK ? l.tile[i + 1] - 1 - t : t - l.tile[i]) * (CLIP_TILE / size), left = l.count[i] - at;
         f(i, at, (int)(left < CLIP_TILE / size ? left : CLIP_TILE / size));
     }
 }
@@ -82,7 +89,7 @@ __global__ __launch_bounds__(THREADS) void squares_kernel(ClipList l, double *su
 {
     __shared__ double s[WAVES];
     double sum = 0;
-    each_tile(l, [&](int i, long long at, int len) { sum += l.half[i] ? squares_of((const bf16_t *)l.in[i] + at, len) : squares_of((const float *)l.in[i] + at, len); });
+    each_tile<false>(l, [&](int i, long long at, int len) { sum += l.half[i] ? squares_of((const bf16_t *)l.in[i] + at, len) : squares_of((const float *)l.in[i] + at, len); });
     sum = sum_of_all(sum, s);
     if (threadIdx.x == 0) sums[blockIdx.x] = sum;
 }
@@ -111,7 +118,7 @@ template <class T> __device__ __forceinline__ void scale_tile(const T *p, T *q, 
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             scale(x[i]);
-            __builtin_memcpy(q + (i * THREADS + threadIdx.x) * N, &x[i], 16);
+            store_past(q + (i * THREADS + threadIdx.x) * N, x[i]);
         }
         return;
     }
@@ -134,7 +141,7 @@ __global__ __launch_bounds__(THREADS) void scale_kernel(ClipList l, const double
     const double length = sqrt(sum_of_sums(sums, n, s));
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)length;
     const float by = length > max_norm && length < INFINITY ? (float)(max_norm / length) : 1.f;      // (infinity, NaN: 1)
-    each_tile(l, [&](int i, long long at, int len) {
+    each_tile<true>(l, [&](int i, long long at, int len) {
         if (by == 1.f && l.in[i] == l.out[i]) return;      // as they are
         if (l.half[i]) scale_tile((const bf16_t *)l.in[i] + at, (bf16_t *)l.out[i] + at, len, by);
         else scale_tile((const float *)l.in[i] + at, (float *)l.out[i] + at, len, by);
