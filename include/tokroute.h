@@ -349,7 +349,7 @@ int tr_distill_grad(const tr_loss_config *cfg, void *workspace, size_t workspace
  *     u below 0 or NaN counts as 0; at 1 or more the last kept id of any weight is drawn. T of 0 (or less, or NaN): the first of the order, logprob 0.
  *   tr_top: the first `entries` tokens of the order; ids -1 and values -infinity where a row has fewer.
  * A row without any token: token -1, logprob 0.
- * Weights are sums' terms in 64 bits, rounded to units of 2^-(62 - log2 vocab) of the largest (2^-44 at 151936): the same inputs give the same token, whatever else runs.
+ * Weights are sums' terms in 64 bits, rounded to units of 2^-(62 - log2 vocab), or 2^-51, of the largest (2^-44 at 151936): the same inputs give the same token, whatever else runs.
  *
  * Errors: TR_ERR_INVALID_ARG, TR_ERR_SHAPE (unsupported type or sizes), TR_ERR_CAPACITY (more rows or entries than configured, workspace too small), before anything is enqueued;
  * TR_ERR_HIP. Calls only enqueue, with the device of the stream and of all pointers current. Calls that share a workspace must be ordered with respect to each other; nothing in it outlives

@@ -43,7 +43,6 @@ struct PickArgs {
     int unit;                        // masses are in units of 2^-unit: vocab of them stay below 2^63
     int groups, listed;              // workgroups a row, tokens a part may leave
     int listed_lanes;                // lanes whose largest token is among them
-    uint32_t listed_inverse;         // 2^32 / listed, rounded up: quotients of numbers below 2^16
     // draws: a number a row, or the value for all
     const float *u, *temperatures, *top_ps, *min_ps;
     const int *top_ks;

@@ -47,16 +47,25 @@ int arguments(const tr_pick_config *c, const tr_pick_rows *in, void *ws, size_t 
     a.logits = in->logits; a.stride = in->stride; a.rows = in->rows; a.vocab = c->vocab; a.dtype = c->dtype == TR_BF16 ? DT_BF16 : DT_F32;
     int bits = 0;
     while ((1 << bits) < c->vocab) ++bits;
-    a.unit = std::min(52, 62 - bits);
+    a.unit = std::min(51, 62 - bits);
     a.groups = pick_groups(c->vocab);
-    a.listed = pick_listed(c->vocab);
-    // of x lanes in 64 whose largest of PICK_EACH tokens is among them, the others' follow: with tokens in any order 64 ln(64 / (64 - x)) tokens, here 0.85 of those that fit
-    a.listed_lanes = std::max(1, (int)(64 * (1 - std::exp(-0.85 * a.listed / 64))));
-    a.listed_inverse = (uint32_t)((((uint64_t)1 << 32) + a.listed - 1) / a.listed);
     const Plan p = plan_of(c);
     char *const b = (char *)ws;
     a.head = (PickHead *)(b + p.head); a.list = (uint2 *)(b + p.list); a.search = (PickSearch *)(b + p.search); a.steps = (unsigned long long *)(b + p.steps);
     return TR_OK;
+}
+
+// Tokens that a part leaves: as many as there is room for, or, where all rows have a top-k, enough for it. A part's largest m are those of a share m / PICK_PART of the row, give or take
+// sqrt(m), and what is known of the row ends with the part that has the least: some 2.7 sqrt(m) below among a hundred parts.
+void list_tokens(PickArgs &a, int top_k)
+{
+    a.listed = pick_listed(a.vocab);
+    if (top_k > 0) {
+        const double want = 1.3 * top_k / (a.groups * PICK_WAVES) + 0.3, root = (2.7 + std::sqrt(2.7 * 2.7 + 4 * want)) / 2;
+        a.listed = (int)std::min<double>(a.listed, std::ceil(root * root / 0.85));
+    }
+    // of x lanes in 64 whose largest of PICK_EACH tokens is among them, the others' follow: with tokens in any order 64 ln(64 / (64 - x)) tokens, here 0.85 of those that fit
+    a.listed_lanes = std::max(1, (int)(64 * (1 - std::exp(-0.85 * a.listed / 64))));
 }
 
 // PICK_ROWS rows at a time
@@ -101,6 +110,7 @@ int tr_sample(const tr_pick_config *cfg, void *workspace, size_t workspace_bytes
     a.token = token; a.logprob = logprob;
     // (top-k ends within what the parts list but for rows whose largest logits lie oddly; one workgroup searches these)
     a.searched = a.groups > 1 && (a.top_ps || a.min_ps || a.top_p < 1.f || a.min_p > 0.f) && (a.top_ks || a.top_k == 0);
+    list_tokens(a, !a.temperatures && !(a.temperature > 0.f) ? 1 : a.top_ks ? 0 : a.top_k);
     return enqueue(a, [&](const PickArgs &p) { launch_sample((hipStream_t)hip_stream, p); });
 }
 
@@ -114,6 +124,7 @@ int tr_top(const tr_pick_config *cfg, void *workspace, size_t workspace_bytes, v
     if (!a.rows) return TR_OK;
     if (!ids || !values) return TR_ERR_INVALID_ARG;
     a.entries = entries; a.ids = ids; a.values = values;
+    list_tokens(a, entries);
     return enqueue(a, [&](const PickArgs &p) { launch_top((hipStream_t)hip_stream, p); });
 }
 
