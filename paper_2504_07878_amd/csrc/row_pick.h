@@ -9,11 +9,12 @@ namespace tr {
 
 constexpr int PICK_MAX_ROWS = 1 << 20, PICK_MAX_VOCAB = 1 << 20, PICK_MAX_ENTRIES = 1024;
 
-// A wavefront reads PICK_PART tokens of a row, a workgroup PICK_GROUP. Rows of more than one workgroup meet in the workspace: every part leaves its sum and its largest tokens, from which one
+// A wavefront reads a part of a row, a workgroup eight of them. Rows of more than one workgroup meet in the workspace: every part leaves its sum and its largest tokens, from which one
 // workgroup decides. Workspace and launches are for PICK_ROWS rows at a time.
-constexpr int PICK_THREADS = 512, PICK_WAVES = PICK_THREADS / 64, PICK_EACH = 16, PICK_PART = 64 * PICK_EACH, PICK_GROUP = PICK_PART * PICK_WAVES;
+constexpr int PICK_THREADS = 512, PICK_WAVES = PICK_THREADS / 64, PICK_PART = 1024, PICK_GROUP = PICK_PART * PICK_WAVES;
+constexpr int PICK_ONE = PICK_GROUP;                      // most tokens of a row that is one workgroup's from the start
 constexpr int PICK_ROWS = 1024;
-constexpr int PICK_LISTED = PICK_THREADS * PICK_EACH;     // most tokens of a row that parts leave, and that the deciding workgroup holds
+constexpr int PICK_LISTED = 8192;                         // most tokens of a row that parts leave, and that the deciding workgroup holds
 constexpr int PICK_PART_LISTED = 64;                      // of one part
 constexpr int PICK_STEPS = 512;                           // of a histogram of masses over the logits of a row
 
@@ -32,9 +33,9 @@ struct alignas(16) PickSearch {
     uint32_t found, pad;   // the stage that it turned out to be
     unsigned long long want;   // mass that it keeps
 };
-enum { PICK_DONE = 0, PICK_STEP = 1,    // the step, then the place in it
-       PICK_LEAST = 2,                  // everything from `least` on
-       PICK_WHOLE = 3 };                // one workgroup looks through the row
+enum { PICK_STEP = 1,      // the step, then the place in it
+       PICK_LEAST = 2,     // everything from `least` on
+       PICK_WHOLE = 3 };   // one workgroup looks through the row
 
 struct PickArgs {
     const void *logits;
@@ -55,17 +56,17 @@ struct PickArgs {
     int32_t *ids;
     float *values;
     // workspace (rows of more than one workgroup)
-    PickHead *head;                  // [rows][parts]
+    PickHead *head;                  // [rows][parts]; NULL: rows of one workgroup
     uint2 *list;                     // [rows][parts][listed]: key, id
     PickSearch *search;              // [rows]
     unsigned long long *steps;       // [rows][groups][PICK_STEPS]
-    bool searched;                   // there may be rows to search
+    uint32_t *queue;                 // [0] how many rows are searched, then which; NULL: none can be
 };
 
 inline int pick_groups(int vocab) { return (vocab + PICK_GROUP - 1) / PICK_GROUP; }
-inline int pick_listed(int vocab)
+inline int pick_listed(int groups)
 {
-    const int most = PICK_LISTED / (pick_groups(vocab) * PICK_WAVES);
+    const int most = PICK_LISTED / (groups * PICK_WAVES);
     return most < PICK_PART_LISTED ? most : PICK_PART_LISTED;
 }
 

@@ -17,17 +17,18 @@ bool config_ok(const tr_pick_config *c)
 size_t up(size_t v) { return (v + 255) / 256 * 256; }
 
 // Rows of one workgroup need none of it but for the smallest size there is.
-struct Plan { size_t head, list, search, steps, total; };
+struct Plan { size_t head, list, search, steps, queue, total; };
 Plan plan_of(const tr_pick_config *c)
 {
     Plan p{};
-    const size_t rows = std::min(c->max_rows, PICK_ROWS), groups = pick_groups(c->vocab), parts = rows * groups * PICK_WAVES;
+    const size_t rows = std::min(c->max_rows, PICK_ROWS), groups = pick_groups(c->vocab);
     p.total = 256;
-    if (groups > 1) {
-        p.list = up(parts * sizeof(PickHead));
-        p.search = p.list + up(parts * pick_listed(c->vocab) * 8);
+    if (c->vocab > PICK_ONE) {
+        p.list = up(rows * groups * PICK_WAVES * sizeof(PickHead));
+        p.search = p.list + up(rows * PICK_LISTED * 8);
         p.steps = p.search + up(rows * sizeof(PickSearch));
-        p.total = p.steps + up(rows * groups * PICK_STEPS * 8);
+        p.queue = p.steps + up(rows * groups * PICK_STEPS * 8);
+        p.total = p.queue + up((rows + 1) * 4);
     }
     return p;
 }
@@ -48,10 +49,12 @@ int arguments(const tr_pick_config *c, const tr_pick_rows *in, void *ws, size_t 
     int bits = 0;
     while ((1 << bits) < c->vocab) ++bits;
     a.unit = std::min(51, 62 - bits);
-    a.groups = pick_groups(c->vocab);
-    const Plan p = plan_of(c);
-    char *const b = (char *)ws;
-    a.head = (PickHead *)(b + p.head); a.list = (uint2 *)(b + p.list); a.search = (PickSearch *)(b + p.search); a.steps = (unsigned long long *)(b + p.steps);
+    if (c->vocab > PICK_ONE) {
+        a.groups = pick_groups(c->vocab);
+        const Plan p = plan_of(c);
+        char *const b = (char *)ws;
+        a.head = (PickHead *)(b + p.head); a.list = (uint2 *)(b + p.list); a.search = (PickSearch *)(b + p.search); a.steps = (unsigned long long *)(b + p.steps); a.queue = (uint32_t *)(b + p.queue);
+    }
     return TR_OK;
 }
 
@@ -59,12 +62,13 @@ int arguments(const tr_pick_config *c, const tr_pick_rows *in, void *ws, size_t 
 // sqrt(m), and what is known of the row ends with the part that has the least: some 2.7 sqrt(m) below among a hundred parts.
 void list_tokens(PickArgs &a, int top_k)
 {
-    a.listed = pick_listed(a.vocab);
+    if (!a.head) return;
+    a.listed = pick_listed(a.groups);
     if (top_k > 0) {
         const double want = 1.3 * top_k / (a.groups * PICK_WAVES) + 0.3, root = (2.7 + std::sqrt(2.7 * 2.7 + 4 * want)) / 2;
         a.listed = (int)std::min<double>(a.listed, std::ceil(root * root / 0.85));
     }
-    // of x lanes in 64 whose largest of PICK_EACH tokens is among them, the others' follow: with tokens in any order 64 ln(64 / (64 - x)) tokens, here 0.85 of those that fit
+    // of x lanes in 64 whose largest of 16 tokens is among them, the others' follow: with tokens in any order 64 ln(64 / (64 - x)) tokens, here 0.85 of those that fit
     a.listed_lanes = std::max(1, (int)(64 * (1 - std::exp(-0.85 * a.listed / 64))));
 }
 
@@ -109,7 +113,7 @@ int tr_sample(const tr_pick_config *cfg, void *workspace, size_t workspace_bytes
     a.temperature = how->temperature; a.top_k = how->top_k; a.top_p = how->top_p; a.min_p = how->min_p;
     a.token = token; a.logprob = logprob;
     // (top-k ends within what the parts list but for rows whose largest logits lie oddly; one workgroup searches these)
-    a.searched = a.groups > 1 && (a.top_ps || a.min_ps || a.top_p < 1.f || a.min_p > 0.f) && (a.top_ks || a.top_k == 0);
+    if (!(a.top_ps || a.min_ps || a.top_p < 1.f || a.min_p > 0.f) || !(a.top_ks || a.top_k == 0)) a.queue = nullptr;
     list_tokens(a, !a.temperatures && !(a.temperature > 0.f) ? 1 : a.top_ks ? 0 : a.top_k);
     return enqueue(a, [&](const PickArgs &p) { launch_sample((hipStream_t)hip_stream, p); });
 }
@@ -124,6 +128,7 @@ int tr_top(const tr_pick_config *cfg, void *workspace, size_t workspace_bytes, v
     if (!a.rows) return TR_OK;
     if (!ids || !values) return TR_ERR_INVALID_ARG;
     a.entries = entries; a.ids = ids; a.values = values;
+    a.queue = nullptr;
     list_tokens(a, entries);
     return enqueue(a, [&](const PickArgs &p) { launch_top((hipStream_t)hip_stream, p); });
 }

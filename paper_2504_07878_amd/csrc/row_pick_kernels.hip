@@ -10,6 +10,7 @@
 // executing them (the same in registers, unrolled: 88 KB of code for decide_kernel, 12.8 us for one row with top-k and top-p).
 #include "row_pick.h"
 
+#include <algorithm>
 #include <float.h>
 
 namespace tr {
@@ -18,12 +19,13 @@ namespace {
 
 typedef unsigned long long u64;
 
-constexpr int THREADS = PICK_THREADS, WAVES = PICK_WAVES, EACH = PICK_EACH;
+constexpr int THREADS = PICK_THREADS, WAVES = PICK_WAVES, EACH = PICK_PART / 64;
 constexpr int BIN_BITS = 11, BINS = 1 << BIN_BITS;
-constexpr int MAX_PARTS = (PICK_MAX_VOCAB + PICK_PART - 1) / PICK_PART;
+constexpr int MAX_PARTS = PICK_MAX_VOCAB / PICK_PART;
+constexpr int PART_STEPS = PICK_PART / THREADS;      // tokens a thread where a workgroup looks through a part
 constexpr int FEW = 256;      // tokens that are compared with each other, all with all
 constexpr uint32_t LOWEST = 0x00800000u, ANY = 0xffffffffu;      // key of the lowest finite logit
-static_assert(MAX_PARTS == 2 * THREADS && PICK_PART == 2 * THREADS && THREADS == 2 * FEW);
+static_assert(MAX_PARTS == 2 * THREADS && PART_STEPS == 2 && THREADS == 2 * FEW);
 
 // Logits as whole numbers in their order. -inf and NaN are no tokens: key 0. (-0 is 0.)
 __device__ __forceinline__ uint32_t key_of(float z)
@@ -146,20 +148,22 @@ __device__ __forceinline__ double evenly(float u) { return fmin(fmax((double)u, 
 
 // ------------------------------------------------------------------ a workgroup's searches
 
-template <int HELD> struct Shared {
+template <int HELD, bool WHOLE = false> struct Shared {
+    static constexpr bool by_place = WHOLE;      // a token's id is its place
     u64 bin[BINS];
     u64 part[WAVES];
     u64 before, at;
     double run;
     double powers[32];
     uint32_t place, top, from, n;
-    int found, first, last, entries;
+    uint32_t first, last;
+    int found, entries;
     union {
         struct { u64 few[FEW], few_mass[FEW]; };
         u64 entry[PICK_MAX_ENTRIES];
         u64 mass[MAX_PARTS];
     };
-    uint32_t key[HELD], id[HELD];      // tokens, key 0: none
+    uint32_t key[HELD], id[WHOLE ? 1 : HELD];      // tokens, key 0: none
 };
 
 // sum of the values of all threads up to this one, and of all
@@ -197,9 +201,9 @@ template <class Each, class S> __device__ __forceinline__ Border border_step(Eac
     for (int i = threadIdx.x; i < BINS; i += THREADS) s.bin[i] = 0;
     if (threadIdx.x == 0) s.found = 0;
     __syncthreads();
-    each([&](uint32_t place, u64 amount) {
+    each([&](uint32_t place, auto amount) {
         const uint32_t d = place - base;
-        if (d <= most) atomicAdd(&s.bin[d >> shift], amount);
+        if (d <= most) atomicAdd(&s.bin[d >> shift], (u64)amount());
     });
     __syncthreads();
     u64 mine[N], sum = 0, total;
@@ -217,11 +221,10 @@ template <class Each, class S> __device__ __forceinline__ Border border_step(Eac
     return s.found ? Border{true, s.place, s.before, s.at} : Border{false, 0, 0, 0};
 }
 
-// The first place up to which the amounts come to `want` (> 0) or more, what lies before it and what at it. each(add) calls add(place, amount) for everything; places are below
-// 2^bits. Eleven bits of the place at a time, by a histogram of amounts. All threads get the answer.
-template <class Each, class S> __device__ __forceinline__ Border find_border(Each each, int bits, u64 want, S &s)
+// The first place up to which the amounts come to `want` (> 0) or more, what lies before it and what at it. each(add) calls add(place, amount) for everything, amount() being what it is; places are below
+// 2^bits. Eleven bits of the place at a time, by a histogram of amounts. All threads get the answer. b: of a step before, which bits are left of.
+template <class Each, class S> __device__ __forceinline__ Border find_border(Each each, int bits, u64 want, S &s, Border b = Border{true, 0, 0, 0})
 {
-    Border b{true, 0, 0, 0};
 #pragma unroll 1
     do {
         const int shift = max(0, bits - BIN_BITS);
@@ -232,14 +235,14 @@ template <class Each, class S> __device__ __forceinline__ Border find_border(Eac
 }
 
 // Where a row's tokens come from: what a workgroup holds, all tokens of keys `from` and above
-template <int HELD> struct Pool {
-    const Shared<HELD> &s;
+template <class S> struct Pool {
+    const S &s;
     uint32_t from, n;
     __device__ __forceinline__ bool all() const { return from <= LOWEST; }
     template <class F> __device__ __forceinline__ void each(F f) const
     {
 #pragma unroll 1
-        for (uint32_t i = threadIdx.x; i < n; i += THREADS) if (const uint32_t key = s.key[i]) f(key, s.id[i]);
+        for (uint32_t i = threadIdx.x; i < n; i += THREADS) if (const uint32_t key = s.key[i]) f(key, S::by_place ? i : s.id[i]);
     }
 };
 
@@ -281,15 +284,19 @@ __device__ __forceinline__ int bits_of(uint32_t v) { return v ? 32 - __clz(v) : 
 __device__ __forceinline__ u64 share_of(float p, u64 sum) { return max(min((u64)ceil(fmax((double)p, 0.0) * (double)sum), sum), 1ull); }
 __device__ __forceinline__ u64 share_of(float p, double weight, double unit) { return max((u64)ceil(fmax((double)p, 0.0) * weight * unit), 1ull); }
 
+// A first step towards the border of top-k or top-p (key places, 2^shift of them), where one was taken
+struct First { Border b; int shift; };
+
 // What the filters keep; false: more than the source knows of. `weight`: of the whole row, for a source that does not hold it all.
-template <class Source, class S> __device__ __forceinline__ bool keep(const Source &src, const Row &r, double weight, int vocab, Kept &kept, S &s)
+template <class Source, class S> __device__ __forceinline__ bool keep(const Source &src, const Row &r, double weight, int vocab, const First &first, Kept &kept, S &s)
 {
-    const int key_bits = bits_of(r.top_key - src.from);
+    const int key_bits = first.b.found ? first.shift : bits_of(r.top_key - src.from);
+    const Border from = first.b.found ? first.b : Border{true, 0, 0, 0};
     bool cut = false;
     u64 ties = 0;                     // 0: all of them
     kept = Kept{LOWEST, ANY};
     if (r.k > 0) {
-        const Border b = find_border([&](auto add) { src.each([&](uint32_t key, uint32_t) { add(r.top_key - key, 1); }); }, key_bits, r.k, s);
+        const Border b = find_border([&](auto add) { src.each([&](uint32_t key, uint32_t) { add(r.top_key - key, [] { return 1; }); }); }, key_bits, r.k, s, from);
         if (!b.found && !src.all()) return false;
         if (b.found) { kept.key = r.top_key - b.place; ties = r.k - b.before < b.at ? r.k - b.before : 0; cut = true; }
     }
@@ -301,7 +308,8 @@ template <class Source, class S> __device__ __forceinline__ bool keep(const Sour
             src.each([&](uint32_t key, uint32_t) { sum += key > kept.key || (key == kept.key && !ties) ? r.mass(key) : 0; });
             want = share_of(r.p, sum_of_all(sum, s) + (ties ? ties * r.mass(kept.key) : 0));
         } else want = share_of(r.p, weight, r.unit);
-        const Border b = find_border([&](auto add) { src.each([&](uint32_t key, uint32_t) { if (key >= least) add(r.top_key - key, r.mass(key)); }); }, key_bits, want, s);
+        const Border b = find_border([&](auto add) { src.each([&](uint32_t key, uint32_t) { if (key >= least) add(r.top_key - key, [&] { return r.mass(key); }); }); },
+                                     cut ? bits_of(r.top_key - least) : key_bits, want, s, cut ? Border{true, 0, 0, 0} : from);
         if (!b.found) return false;
         const uint32_t key = r.top_key - b.place;
         const u64 one = r.mass(key), need = (want - b.before + one - 1) / one;
@@ -317,7 +325,7 @@ template <class Source, class S> __device__ __forceinline__ bool keep(const Sour
         cut = true;
     }
     if (!cut && !src.all()) return false;
-    if (ties) kept.last = find_border([&](auto add) { src.each([&](uint32_t key, uint32_t id) { if (key == kept.key) add(id, 1); }); }, bits_of(vocab - 1), ties, s).place;
+    if (ties) kept.last = find_border([&](auto add) { src.each([&](uint32_t key, uint32_t id) { if (key == kept.key) add(id, [] { return 1; }); }); }, bits_of(vocab - 1), ties, s).place;
     return true;
 }
 
@@ -332,23 +340,23 @@ __device__ __forceinline__ void put_nothing(const PickArgs &a, int r, bool top)
     else if (threadIdx.x == 0) { a.token[r] = -1; a.logprob[r] = 0.f; }
 }
 
-template <class T, class Source, class S> __device__ __forceinline__ bool draw(const Source &src, const PickArgs &a, int r, const T *logits, const Row &row, double weight, S &s)
+template <class T, class Source, class S> __device__ __forceinline__ bool draw(const Source &src, const PickArgs &a, int r, const T *logits, const Row &row, double weight, const First &first, S &s)
 {
     Kept kept;
-    if (!keep(src, row, weight, a.vocab, kept, s)) return false;
+    if (!keep(src, row, weight, a.vocab, first, kept, s)) return false;
     u64 sum = 0;
     src.each([&](uint32_t key, uint32_t id) { sum += kept.has(key, id) ? row.mass(key) : 0; });
     sum = sum_of_all(sum, s);
     const u64 below = min((u64)(evenly(a.u[r]) * (double)sum), sum - 1);
-    const Border b = find_border([&](auto add) { src.each([&](uint32_t key, uint32_t id) { if (kept.has(key, id)) add(id, row.mass(key)); }); }, bits_of(a.vocab - 1), below + 1, s);
+    const Border b = find_border([&](auto add) { src.each([&](uint32_t key, uint32_t id) { if (kept.has(key, id)) add(id, [&] { return row.mass(key); }); }); }, bits_of(a.vocab - 1), below + 1, s);
     if (threadIdx.x == 0) put_draw(a, r, row, b.place, wide(logits[b.place]), (double)sum / row.unit);
     return true;
 }
 
-template <class Source, class S> __device__ __forceinline__ bool list_top(const Source &src, const PickArgs &a, int r, const Row &row, S &s)
+template <class Source, class S> __device__ __forceinline__ bool list_top(const Source &src, const PickArgs &a, int r, const Row &row, const First &first, S &s)
 {
     Kept kept;
-    if (!keep(src, row, 0.0, a.vocab, kept, s)) return false;
+    if (!keep(src, row, 0.0, a.vocab, first, kept, s)) return false;
     __syncthreads();
     for (int i = threadIdx.x; i < PICK_MAX_ENTRIES; i += THREADS) s.entry[i] = ~0ull;
     if (threadIdx.x == 0) s.entries = 0;
@@ -376,7 +384,7 @@ template <class Source, class S> __device__ __forceinline__ bool list_top(const 
 
 // Tokens that a workgroup can compare all with all: those from where top-k or top-p end on, or min-p. Two threads a token add up what comes before it in the order, and then, of what is kept,
 // what comes before it by id. false: more than FEW, or more than the source knows of.
-template <bool TOP, int HELD> __device__ __forceinline__ bool among_few(const Pool<HELD> &src, const PickArgs &a, int r, const Row &row, double weight, Shared<HELD> &s)
+template <bool TOP, class S> __device__ __forceinline__ bool among_few(const Pool<S> &src, const PickArgs &a, int r, const Row &row, double weight, First &first, S &s)
 {
     if (row.k > FEW) return false;
     uint32_t floor = src.from;
@@ -395,8 +403,9 @@ template <bool TOP, int HELD> __device__ __forceinline__ bool among_few(const Po
     if (row.k > 0 || row.p < 1.f) {
         const int bits = bits_of(row.top_key - floor), shift = max(0, bits - BIN_BITS);
         const bool by_count = row.k > 0;
-        const Border b = border_step([&](auto add) { src.each([&](uint32_t key, uint32_t) { if (key >= floor) add(row.top_key - key, by_count ? 1 : row.mass(key)); }); }, 0, bits, shift, 0,
+        const Border b = border_step([&](auto add) { src.each([&](uint32_t key, uint32_t) { if (key >= floor) add(row.top_key - key, [&] { return by_count ? 1 : row.mass(key); }); }); }, 0, bits, shift, 0,
                                      by_count ? (u64)row.k : want, s);
+        first = First{b, shift};
         if (b.found) { floor = row.top_key - min(row.top_key - floor, b.place + ((1u << shift) - 1)); closed = true; }
     }
     if (!closed) return false;
@@ -462,49 +471,57 @@ template <bool TOP, int HELD> __device__ __forceinline__ bool among_few(const Po
 
 struct Found { int at; double before; };
 
-// The first of the values (two a thread, in the threads' order) up to which they add up to more than `want`; where rounding leaves none the last that is no zero. `upto`: sum_upto of a
-// thread's two. Sums in 64 bits in a fixed order.
-template <class S> __device__ __forceinline__ Found first_over(const double (&v)[2], double upto, double want, S &s)
+// The first of the values (N a thread, in the threads' order) up to which they add up to more than `want`; where rounding leaves none the last that is no zero. `before`: sum of the
+// threads' before this one. Sums in 64 bits in a fixed order.
+template <int N, class S> __device__ __forceinline__ Found first_over(const double (&v)[N], double before, double want, S &s)
 {
-    const double run[3] = {upto - (v[0] + v[1]), upto - v[1], upto};
-    if (threadIdx.x == 0) { s.first = 0x7fffffff; s.last = 0; }
-    __syncthreads();
+    double run = before, found_at = before;
+    uint32_t first = ANY, last = 0;
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
+    for (int e = 0; e < N; ++e) {
+        const double from = run;
+        run += v[e];
         if (!(v[e] > 0)) continue;
-        atomicMax(&s.last, (int)threadIdx.x * 2 + e);
-        if (run[e + 1] > want) atomicMin(&s.first, (int)threadIdx.x * 2 + e);
+        const uint32_t i = threadIdx.x * N + e;
+        last = i + 1;
+        if (first != ANY) continue;
+        found_at = from;                                  // (of the first that is over, or of the last)
+        if (run > want) first = i;
     }
+    if (threadIdx.x == 0) { s.first = ANY; s.last = 0; }
+    const uint32_t wave_first = ~wave_max(~first), wave_last = wave_max(last);
     __syncthreads();
-    const int at = min(s.first, s.last);
-    if (at / 2 == (int)threadIdx.x) s.run = run[at % 2];
+    if (threadIdx.x % 64 == 0) { atomicMin(&s.first, wave_first); atomicMax(&s.last, wave_last); }
     __syncthreads();
-    return Found{at, s.run};
+    const uint32_t at = s.first != ANY ? s.first : s.last - 1;
+    if (at / N == threadIdx.x) s.run = found_at;
+    __syncthreads();
+    return Found{(int)at, s.run};
 }
 
-// A draw from a row that nothing is cut from, which more than one workgroup has read in pieces of PICK_PART tokens: the piece by the pieces' weights (two a thread), then the token in it
-template <class T, class S> __device__ __forceinline__ void draw_freely(const PickArgs &a, int r, const T *logits, const Row &row, double (&v)[2], S &s)
+// A draw from a row that nothing is cut from, which more than one workgroup has read in parts that are one piece each: the part by the parts' weights (two a thread), then the token in it
+template <class T, class S> __device__ __forceinline__ void draw_freely(const PickArgs &a, int r, const T *logits, const Row &row, const double (&parts)[2], S &s)
 {
     double total, rest;
-    double upto = sum_upto(v[0] + v[1], total, s);
+    double before = sum_upto(parts[0] + parts[1], total, s) - (parts[0] + parts[1]);
     const double want = evenly(a.u[r]) * total;
-    const Found part = first_over(v, upto, want, s);
-    float z[2];
+    const Found part = first_over(parts, before, want, s);
+    float z[PART_STEPS];
+    double v[PART_STEPS], sum = 0;
+    const int first = part.at * PICK_PART + threadIdx.x * PART_STEPS;
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-        const int id = part.at * PICK_PART + threadIdx.x * 2 + e;
-        z[e] = id < a.vocab ? wide(logits[id]) : -INFINITY;
-    }
+    for (int e = 0; e < PART_STEPS; ++e) z[e] = first + e < a.vocab ? wide(logits[first + e]) : -INFINITY;
 #pragma unroll
-    for (int e = 0; e < 2; ++e) v[e] = z[e] > -INFINITY ? row.weight(z[e]) : 0;
-    upto = sum_upto(v[0] + v[1], rest, s);
-    const Found token = first_over(v, upto, want - part.before, s);
-    if (token.at / 2 == (int)threadIdx.x) put_draw(a, r, row, part.at * PICK_PART + token.at, z[token.at % 2], total);
+    for (int e = 0; e < PART_STEPS; ++e) sum += v[e] = z[e] > -INFINITY ? row.weight(z[e]) : 0;
+    before = sum_upto(sum, rest, s) - sum;
+    const Found token = first_over(v, before, want - part.before, s);
+#pragma unroll
+    for (int e = 0; e < PART_STEPS; ++e) if (token.at == (int)threadIdx.x * PART_STEPS + e) put_draw(a, r, row, first + e, z[e], total);
 }
 
 // ------------------------------------------------------------------ the kernels
 
-// A part of a row: blocks of a load each, `step` apart, in LDS as 32 bits, 16 a lane (-inf: no token). A load past the row's end is moved back, and what it has twice is dropped.
+// A part of a row: blocks of a load each, `step` apart, in LDS as 32 bits, EACH a lane (-inf: no token). A load past the row's end is moved back, and what it has twice is dropped.
 template <class T> struct Part {
     static constexpr int N = 16 / sizeof(T), BLOCKS = EACH / N, BLOCK = 64 * N;
     float (*z)[64][4];           // [EACH / 4][lane][4]
@@ -512,8 +529,7 @@ template <class T> struct Part {
     int vocab;
     __device__ __forceinline__ uint32_t at(int block) const
     {
-        const uint32_t i = first + block * step;
-        return vocab >= N ? min(i, (uint32_t)(vocab - N)) : i;
+        return min(first + block * step, (uint32_t)(vocab - N));
     }
     __device__ __forceinline__ uint32_t id(int e) const { return at(e / N) + e % N; }
     __device__ __forceinline__ float &logit(int e) const { return z[e / 4][threadIdx.x % 64][e % 4]; }
@@ -521,15 +537,8 @@ template <class T> struct Part {
     __device__ __forceinline__ float load(const T *logits)
     {
         T raw[BLOCKS][N];
-        if (vocab >= N) {
 #pragma unroll
-            for (int i = 0; i < BLOCKS; ++i) __builtin_memcpy(raw[i], (const char *)logits + at(i) * (uint32_t)sizeof(T), 16);
-        } else {
-#pragma unroll
-            for (int i = 0; i < BLOCKS; ++i)
-#pragma unroll
-                for (int e = 0; e < N; ++e) raw[i][e] = logits[min(at(i) + e, (uint32_t)vocab - 1)];
-        }
+        for (int i = 0; i < BLOCKS; ++i) __builtin_memcpy(raw[i], (const char *)logits + at(i) * (uint32_t)sizeof(T), 16);
         // (the last lane's last load ends within the row: so do all)
         const bool whole = __builtin_amdgcn_readlane((int)(first + (BLOCKS - 1) * step), 63) + N <= vocab;
         float most = -INFINITY;
@@ -543,7 +552,7 @@ template <class T> struct Part {
             }
             if (!whole) {
 #pragma unroll
-                for (int e = 0; e < N; ++e) if (at(i) + e < first + i * step || at(i) + e >= (uint32_t)vocab) v[e] = -INFINITY;
+                for (int e = 0; e < N; ++e) if (at(i) + e < first + i * step) v[e] = -INFINITY;
             }
 #pragma unroll
             for (int e = 0; e < N; ++e) most = fmaxf(most, v[e]);
@@ -553,7 +562,7 @@ template <class T> struct Part {
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         return most;
     }
-    // f(logit, place) for the lane's 16
+    // f(logit, place) for the lane's
     template <class F> __device__ __forceinline__ void each(F f) const
     {
 #pragma unroll 1
@@ -572,7 +581,7 @@ template <class T> struct Part {
             const int e = __ffs(mask) - 1;
             to[i++] = make_uint2(key_of(logit(e)), id(e));
         }
-        if (lane >= sum && lane < listed) to[lane] = make_uint2(0, 0);
+        for (int l = lane; l < listed; l += 64) if (l >= sum) to[l] = make_uint2(0, 0);
     }
 };
 
@@ -586,6 +595,7 @@ template <class T, bool TOP> __global__ __launch_bounds__(THREADS, 8) void parts
     // Of a row that is cut from, blocks of all parts take turns, so that large logits that lie together are spread over the parts; of one that is drawn from freely a part is one
     // piece, so that its sum is a step of the sums by id.
     using P = Part<T>;
+    if (a.queue && blockIdx.x == 0 && threadIdx.x == 0) a.queue[0] = 0;
     P p{s_z[wave], (uint32_t)part * (row.cut ? P::BLOCK : PICK_PART) + lane * P::N, (uint32_t)(row.cut ? parts * P::BLOCK : P::BLOCK), a.vocab};
     const uint32_t lane_top = key_of(p.load((const T *)a.logits + (long long)r * a.stride));
     if (row.summed) load_powers(s_powers);
@@ -648,7 +658,7 @@ template <int HELD> struct Lists {
             v[e] = i < all ? list[i] : make_uint2(0, 0);
         }
     }
-    __device__ __forceinline__ uint32_t hold(uint32_t least, Shared<HELD> &s) const      // (s.n is zero, behind a barrier)
+    template <class S> __device__ __forceinline__ uint32_t hold(uint32_t least, S &s) const      // (s.n is zero, behind a barrier)
     {
         int n = 0;
 #pragma unroll
@@ -667,13 +677,14 @@ template <int HELD> struct Lists {
 // One workgroup a row. Bound by the latency of a few loads and of some twenty barriers.
 template <class T, bool TOP, bool WHOLE, int HELD> __global__ __launch_bounds__(THREADS) void decide_kernel(PickArgs a)
 {
-    __shared__ Shared<HELD> s;
+    using S = Shared<HELD, WHOLE>;
+    __shared__ S s;
     const int r = blockIdx.x, vocab = a.vocab, parts = a.groups * WAVES;
     const T *const logits = (const T *)a.logits + (long long)r * a.stride;
     Row row = row_of<TOP>(a, r, s.powers);
     if (threadIdx.x == 0) { s.top = 0; s.from = LOWEST; s.n = 0; }
     load_powers(s.powers);
-    Pool<HELD> pool{s, LOWEST, (uint32_t)vocab};
+    Pool<S> pool{s, LOWEST, (uint32_t)vocab};
     double weight = 0;
     if constexpr (WHOLE) {
         constexpr int N = 16 / sizeof(T);
@@ -688,13 +699,13 @@ template <class T, bool TOP, bool WHOLE, int HELD> __global__ __launch_bounds__(
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
                     const uint32_t key = key_of(wide(v[e]));
-                    s.key[at + e] = key; s.id[at + e] = at + e;
+                    s.key[at + e] = key;
                     top = max(top, key);
                 }
             }
         } else if ((int)threadIdx.x < vocab) {
             top = key_of(wide(logits[threadIdx.x]));
-            s.key[threadIdx.x] = top; s.id[threadIdx.x] = threadIdx.x;
+            s.key[threadIdx.x] = top;
         }
         top = wave_max(top);
         if (threadIdx.x % 64 == 0) atomicMax(&s.top, top);
@@ -702,7 +713,6 @@ template <class T, bool TOP, bool WHOLE, int HELD> __global__ __launch_bounds__(
         if (!s.top) { put_nothing(a, r, TOP); return; }
         row.relative_to(s.top);
     } else {
-        if (a.searched && threadIdx.x == 0) a.search[r].stage = PICK_DONE;
         PickHead head[2]{};
 #pragma unroll
         for (int e = 0; e < 2; ++e) if ((int)threadIdx.x * 2 + e < parts) head[e] = a.head[(long long)r * parts + threadIdx.x * 2 + e];
@@ -729,12 +739,13 @@ template <class T, bool TOP, bool WHOLE, int HELD> __global__ __launch_bounds__(
         }
         pool.n = lists.hold(pool.from, s);
     }
-    if (among_few<TOP>(pool, a, r, row, weight, s)) return;
+    First first{};
+    if (among_few<TOP>(pool, a, r, row, weight, first, s)) return;
     if constexpr (TOP) {
-        if (list_top(pool, a, r, row, s)) return;
+        if (list_top(pool, a, r, row, first, s)) return;
     } else {
-        if (draw(pool, a, r, logits, row, weight, s)) return;
-        if (!WHOLE && a.searched && row.k == 0 && row.top < INFINITY && pool.from <= row.top_key) {
+        if (draw(pool, a, r, logits, row, weight, first, s)) return;
+        if (!WHOLE && a.queue && row.k == 0 && row.top < INFINITY && pool.from <= row.top_key) {
             if (threadIdx.x == 0) {
                 PickSearch q{};
                 q.stage = row.p < 1.f ? PICK_STEP : PICK_LEAST;
@@ -746,14 +757,15 @@ template <class T, bool TOP, bool WHOLE, int HELD> __global__ __launch_bounds__(
                 q.scale = (float)((PICK_STEPS - 2) / fmax((double)q.from - least, 1e-30));
                 q.want = share_of(row.p, weight, row.unit);
                 a.search[r] = q;
+                a.queue[1 + atomicAdd(a.queue, 1u)] = r;
             }
             return;
         }
     }
     if constexpr (!WHOLE) {
         const Streamed<T> whole{logits, vocab};
-        if constexpr (TOP) list_top(whole, a, r, row, s);
-        else draw(whole, a, r, logits, row, weight, s);
+        if constexpr (TOP) list_top(whole, a, r, row, First{}, s);
+        else draw(whole, a, r, logits, row, weight, First{}, s);
     }
 }
 
@@ -765,33 +777,37 @@ __device__ __forceinline__ int step_of(float z, const PickSearch &q) { return (i
 // Masses by steps below `from`, in the last place that of everything from it on; what is below all steps is left out
 template <class T> __global__ __launch_bounds__(THREADS, 8) void steps_kernel(PickArgs a)
 {
-    const int r = blockIdx.x / a.groups, group = blockIdx.x % a.groups;
-    const PickSearch q = a.search[r];
-    if (q.stage != PICK_STEP) return;
     __shared__ float s_z[WAVES][EACH / 4][64][4];
     __shared__ double s_powers[32];
     __shared__ u64 step[PICK_STEPS];
     static_assert(PICK_STEPS == THREADS);
-    step[threadIdx.x] = 0;
-    Row row = row_of<false>(a, r, s_powers);
-    row.relative_to(q.top_key);
-    using P = Part<T>;
-    P p{s_z[threadIdx.x / 64], (uint32_t)(group * WAVES + threadIdx.x / 64) * PICK_PART + threadIdx.x % 64 * P::N, P::BLOCK, a.vocab};
-    p.load((const T *)a.logits + (long long)r * a.stride);
     load_powers(s_powers);
-    __syncthreads();
-    u64 above = 0;
-    p.each([&](float z, int) {
-        const int at = z >= q.from ? -1 : step_of(z, q);
-        if (z == -INFINITY || at >= PICK_STEPS - 1) return;
-        const u64 m = row.mass(z);
-        if (at < 0) above += m;
-        else atomicAdd(&step[at], m);
-    });
-    above = wave_sum(above);
-    if (threadIdx.x % 64 == 0) atomicAdd(&step[PICK_STEPS - 1], above);
-    __syncthreads();
-    a.steps[((long long)r * a.groups + group) * PICK_STEPS + threadIdx.x] = step[threadIdx.x];
+    const uint32_t items = a.queue[0] * a.groups;
+#pragma unroll 1
+    for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const int r = a.queue[1 + item / a.groups], group = item % a.groups;
+        const PickSearch q = a.search[r];
+        if (q.stage != PICK_STEP) continue;
+        step[threadIdx.x] = 0;
+        Row row = row_of<false>(a, r, s_powers);
+        row.relative_to(q.top_key);
+        using P = Part<T>;
+        P p{s_z[threadIdx.x / 64], (uint32_t)(group * WAVES + threadIdx.x / 64) * PICK_PART + threadIdx.x % 64 * P::N, P::BLOCK, a.vocab};
+        p.load((const T *)a.logits + (long long)r * a.stride);
+        __syncthreads();
+        u64 above = 0;
+        p.each([&](float z, int) {
+            const int at = z >= q.from ? -1 : step_of(z, q);
+            if (z == -INFINITY || at >= PICK_STEPS - 1) return;
+            const u64 m = row.mass(z);
+            if (at < 0) above += m;
+            else atomicAdd(&step[at], m);
+        });
+        above = wave_sum(above);
+        if (threadIdx.x % 64 == 0) atomicAdd(&step[PICK_STEPS - 1], above);
+        __syncthreads();
+        a.steps[((long long)r * a.groups + group) * PICK_STEPS + threadIdx.x] = step[threadIdx.x];
+    }
 }
 
 // The step that top-p ends in; of each part the mass of what is above it and its tokens in it. Where min-p alone decides, the mass of what it keeps.
@@ -801,55 +817,60 @@ template <class T> __global__ __launch_bounds__(THREADS, 8) void place_kernel(Pi
     __shared__ double s_powers[32];
     __shared__ u64 s_part[WAVES];
     __shared__ int s_step;
-    const int r = blockIdx.x / a.groups, group = blockIdx.x % a.groups, lane = threadIdx.x % 64, wave = threadIdx.x / 64, parts = a.groups * WAVES, part = group * WAVES + wave;
-    const PickSearch q = a.search[r];
-    if (q.stage == PICK_DONE) return;
-    Row row = row_of<false>(a, r, s_powers);
-    row.relative_to(q.top_key);
-    using P = Part<T>;
-    P p{s_z[wave], (uint32_t)part * PICK_PART + lane * P::N, P::BLOCK, a.vocab};
-    p.load((const T *)a.logits + (long long)r * a.stride);
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, parts = a.groups * WAVES;
     load_powers(s_powers);
-    int step = PICK_STEPS;                    // none
-    uint32_t stage = q.stage;
-    if (stage == PICK_STEP) {
-        u64 sum = 0;
-        const u64 *const steps = a.steps + (long long)r * a.groups * PICK_STEPS + threadIdx.x;
+    const uint32_t items = a.queue[0] * a.groups;
+#pragma unroll 1
+    for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const int r = a.queue[1 + item / a.groups], group = item % a.groups, part = group * WAVES + wave;
+        const PickSearch q = a.search[r];
+        Row row = row_of<false>(a, r, s_powers);
+        row.relative_to(q.top_key);
+        using P = Part<T>;
+        P p{s_z[wave], (uint32_t)part * PICK_PART + lane * P::N, P::BLOCK, a.vocab};
+        p.load((const T *)a.logits + (long long)r * a.stride);
+        int step = PICK_STEPS;                    // none
+        uint32_t stage = q.stage;
+        if (stage == PICK_STEP) {
+            u64 sum = 0;
+            const u64 *const steps = a.steps + (long long)r * a.groups * PICK_STEPS + threadIdx.x;
 #pragma unroll 4
-        for (int g = 0; g < a.groups; ++g) sum += steps[g * PICK_STEPS];
-        // (what is above all steps, which the last place holds, comes before them)
-        u64 upto = wave_upto(threadIdx.x == PICK_STEPS - 1 ? 0 : sum, Plus{});
-        if (threadIdx.x == 0) s_step = PICK_STEPS;
-        if (lane == 63) s_part[wave] = wave == WAVES - 1 ? sum : upto;
-        __syncthreads();
-        upto += s_part[WAVES - 1];
+            for (int g = 0; g < a.groups; ++g) sum += steps[g * PICK_STEPS];
+            // (what is above all steps, which the last place holds, comes before them)
+            u64 upto = wave_upto(threadIdx.x == PICK_STEPS - 1 ? 0 : sum, Plus{});
+            __syncthreads();
+            if (threadIdx.x == 0) s_step = PICK_STEPS;
+            if (lane == 63) s_part[wave] = wave == WAVES - 1 ? sum : upto;
+            __syncthreads();
+            upto += s_part[WAVES - 1];
 #pragma unroll
-        for (int w = 0; w < WAVES - 1; ++w) upto += w < wave ? s_part[w] : 0;
-        if (threadIdx.x < PICK_STEPS - 1 && upto - sum < q.want && q.want <= upto) s_step = threadIdx.x;
-        __syncthreads();
-        step = s_step;
-        if (step == PICK_STEPS) stage = PICK_WHOLE;
-        else if (q.least && step_of(logit_of(q.least), q) < step) stage = PICK_LEAST;
+            for (int w = 0; w < WAVES - 1; ++w) upto += w < wave ? s_part[w] : 0;
+            if (threadIdx.x < PICK_STEPS - 1 && upto - sum < q.want && q.want <= upto) s_step = threadIdx.x;
+            __syncthreads();
+            step = s_step;
+            if (step == PICK_STEPS) stage = PICK_WHOLE;
+            else if (q.least && step_of(logit_of(q.least), q) < step) stage = PICK_LEAST;
+        }
+        if (group == 0 && threadIdx.x == 0) a.search[r].found = stage;
+        if (stage == PICK_WHOLE) continue;
+        PickHead head{};
+        const float least = stage == PICK_LEAST ? logit_of(q.least) : q.from;
+        u64 mass = 0;
+        uint32_t mask = 0;
+        p.each([&](float z, int e) {
+            if (z == -INFINITY) return;
+            const int at = stage == PICK_STEP ? step_of(z, q) : PICK_STEPS;
+            if (z >= least || at < step) mass += row.mass(z);
+            else mask |= (uint32_t)(at == step) << e;
+        });
+        head.mass = wave_sum(mass);
+        if (stage == PICK_STEP) {
+            const int upto = wave_upto(__popc(mask), Plus{}), sum = last_lane(upto);
+            head.count = sum;
+            if (sum <= a.listed) p.list(mask, upto, sum, a.listed, a.list + ((long long)r * parts + part) * a.listed);
+        }
+        if (lane == 0) a.head[(long long)r * parts + part] = head;
     }
-    if (group == 0 && threadIdx.x == 0) a.search[r].found = stage;
-    if (stage == PICK_WHOLE) return;
-    PickHead head{};
-    const float least = stage == PICK_LEAST ? logit_of(q.least) : q.from;
-    u64 mass = 0;
-    uint32_t mask = 0;
-    p.each([&](float z, int e) {
-        if (z == -INFINITY) return;
-        const int at = stage == PICK_STEP ? step_of(z, q) : PICK_STEPS;
-        if (z >= least || at < step) mass += row.mass(z);
-        else mask |= (uint32_t)(at == step) << e;
-    });
-    head.mass = wave_sum(mass);
-    if (stage == PICK_STEP) {
-        const int upto = wave_upto(__popc(mask), Plus{}), sum = last_lane(upto);
-        head.count = sum;
-        if (sum <= a.listed) p.list(mask, upto, sum, a.listed, a.list + ((long long)r * parts + part) * a.listed);
-    }
-    if (lane == 0) a.head[(long long)r * parts + part] = head;
 }
 
 // The place in the step, and the draw: the part by the parts' masses, then the token in it
@@ -857,94 +878,109 @@ template <class T> __global__ __launch_bounds__(THREADS) void finish_kernel(Pick
 {
     constexpr int HELD = PICK_LISTED;
     __shared__ Shared<HELD> s;
-    const int r = blockIdx.x, vocab = a.vocab, parts = a.groups * WAVES;
-    const PickSearch q = a.search[r];
-    if (q.stage == PICK_DONE) return;
-    const T *const logits = (const T *)a.logits + (long long)r * a.stride;
-    Row row = row_of<false>(a, r, s.powers);
-    row.relative_to(q.top_key);
-    if (threadIdx.x == 0) s.n = 0;
+    const int vocab = a.vocab, parts = a.groups * WAVES;
     load_powers(s.powers);
-    bool whole = q.found == PICK_WHOLE;
-    u64 v[2] = {0, 0}, above = 0, total, rest;
-    if (!whole) {
-        u64 over = 0;
+    const uint32_t rows = a.queue[0];
+#pragma unroll 1
+    for (uint32_t item = blockIdx.x; item < rows; item += gridDim.x) {
+        const int r = a.queue[1 + item];
+        const PickSearch q = a.search[r];
+        const T *const logits = (const T *)a.logits + (long long)r * a.stride;
+        Row row = row_of<false>(a, r, s.powers);
+        row.relative_to(q.top_key);
+        __syncthreads();
+        if (threadIdx.x == 0) s.n = 0;
+        bool whole = q.found == PICK_WHOLE;
+        u64 above = 0;
+        if (!whole) {
+            u64 over = 0;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int w = threadIdx.x * 2 + e;
+                PickHead head{};
+                if (w < parts) head = a.head[(long long)r * parts + w];
+                s.mass[w] = head.mass;
+                above += head.mass;
+                over += head.count > (uint32_t)a.listed;
+            }
+            whole = sum_of_all(over, s) != 0;
+            above = sum_of_all(above, s);
+        }
+        if (whole) {
+            const Streamed<T> all{logits, vocab};
+            draw(all, a, r, logits, row, 0.0, First{}, s);
+            continue;
+        }
+        Kept kept{q.least, ANY};
+        if (q.found == PICK_STEP) {
+            Lists<HELD> lists;
+            lists.load(a, r, parts);
+            const Pool<Shared<HELD>> pool{s, LOWEST, lists.hold(LOWEST, s)};
+            const Border b = find_border([&](auto add) { pool.each([&](uint32_t key, uint32_t) { add(q.top_key - key, [&] { return row.mass(key); }); }); }, bits_of(q.top_key - LOWEST),
+                                         q.want - above, s);
+            kept.key = q.top_key - b.place;
+            const u64 one = row.mass(kept.key), need = (q.want - above - b.before + one - 1) / one;
+            u64 ties = need < b.at / one ? need : 0;
+            if (q.least > kept.key) { kept.key = q.least; ties = 0; }
+            if (ties) kept.last = find_border([&](auto add) { pool.each([&](uint32_t key, uint32_t id) { if (key == kept.key) add(id, [] { return 1; }); }); }, bits_of(vocab - 1), ties, s).place;
+            __syncthreads();
+            pool.each([&](uint32_t key, uint32_t id) { if (kept.has(key, id)) atomicAdd(&s.mass[id / PICK_PART], row.mass(key)); });
+            __syncthreads();
+        }
+        u64 total, rest;
+        const u64 m[2] = {s.mass[threadIdx.x * 2], s.mass[threadIdx.x * 2 + 1]};
+        u64 run = sum_upto(m[0] + m[1], total, s) - m[0] - m[1];
+        const u64 below = min((u64)(evenly(a.u[r]) * (double)total), total - 1);
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            const int w = threadIdx.x * 2 + e;
-            PickHead head{};
-            if (w < parts) head = a.head[(long long)r * parts + w];
-            s.mass[w] = head.mass;
-            above += head.mass;
-            over += head.count > (uint32_t)a.listed;
+            if (run <= below && below < run + m[e]) { s.place = threadIdx.x * 2 + e; s.before = run; }
+            run += m[e];
         }
-        whole = sum_of_all(over, s) != 0;
-        above = sum_of_all(above, s);
-    }
-    if (whole) {
-        const Streamed<T> all{logits, vocab};
-        draw(all, a, r, logits, row, 0.0, s);
-        return;
-    }
-    Kept kept{q.least, ANY};
-    if (q.found == PICK_STEP) {
-        Lists<HELD> lists;
-        lists.load(a, r, parts);
-        const Pool<HELD> pool{s, LOWEST, lists.hold(LOWEST, s)};
-        const Border b = find_border([&](auto add) { pool.each([&](uint32_t key, uint32_t) { add(q.top_key - key, row.mass(key)); }); }, bits_of(q.top_key - LOWEST), q.want - above, s);
-        kept.key = q.top_key - b.place;
-        const u64 one = row.mass(kept.key), need = (q.want - above - b.before + one - 1) / one;
-        u64 ties = need < b.at / one ? need : 0;
-        if (q.least > kept.key) { kept.key = q.least; ties = 0; }
-        if (ties) kept.last = find_border([&](auto add) { pool.each([&](uint32_t key, uint32_t id) { if (key == kept.key) add(id, 1); }); }, bits_of(vocab - 1), ties, s).place;
         __syncthreads();
-        pool.each([&](uint32_t key, uint32_t id) { if (kept.has(key, id)) atomicAdd(&s.mass[id / PICK_PART], row.mass(key)); });
-        __syncthreads();
-    }
-    v[0] = s.mass[threadIdx.x * 2]; v[1] = s.mass[threadIdx.x * 2 + 1];
-    u64 run = sum_upto(v[0] + v[1], total, s) - v[0] - v[1];
-    const u64 below = min((u64)(evenly(a.u[r]) * (double)total), total - 1);
+        const int first = s.place * PICK_PART + threadIdx.x * PART_STEPS;
+        const u64 left = below - s.before;
+        float z[PART_STEPS];
+        u64 v[PART_STEPS], sum = 0;
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-        if (run <= below && below < run + v[e]) { s.place = threadIdx.x * 2 + e; s.before = run; }
-        run += v[e];
-    }
-    __syncthreads();
-    const uint32_t first = s.place * PICK_PART;
-    const u64 left = below - s.before;
-    float z[2];
+        for (int e = 0; e < PART_STEPS; ++e) z[e] = first + e < vocab ? wide(logits[first + e]) : -INFINITY;
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-        const uint32_t id = first + threadIdx.x * 2 + e;
-        z[e] = id < (uint32_t)vocab ? wide(logits[id]) : -INFINITY;
-        const uint32_t key = key_of(z[e]);
-        v[e] = key && kept.has(key, id) ? row.mass(key) : 0;
-    }
-    run = sum_upto(v[0] + v[1], rest, s) - v[0] - v[1];
+        for (int e = 0; e < PART_STEPS; ++e) {
+            const uint32_t key = key_of(z[e]);
+            sum += v[e] = key && kept.has(key, first + e) ? row.mass(key) : 0;
+        }
+        run = sum_upto(sum, rest, s) - sum;
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-        if (run <= left && left < run + v[e]) put_draw(a, r, row, first + threadIdx.x * 2 + e, z[e], (double)total / row.unit);
-        run += v[e];
+        for (int e = 0; e < PART_STEPS; ++e) {
+            if (run <= left && left < run + v[e]) put_draw(a, r, row, first + e, z[e], (double)total / row.unit);
+            run += v[e];
+        }
+    }
+}
+
+template <class T, bool TOP> void launch_parts(hipStream_t s, const PickArgs &a)
+{
+    const unsigned all = (unsigned)a.rows * a.groups;
+    hipLaunchKernelGGL((parts_kernel<T, TOP>), dim3(all), dim3(THREADS), 0, s, a);
+    if (a.groups * WAVES * a.listed <= 4096) hipLaunchKernelGGL((decide_kernel<T, TOP, false, 4096>), dim3(a.rows), dim3(THREADS), 0, s, a);
+    else hipLaunchKernelGGL((decide_kernel<T, TOP, false, PICK_LISTED>), dim3(a.rows), dim3(THREADS), 0, s, a);
+    if constexpr (!TOP) {
+        if (!a.queue) return;
+        // rows of the queue, which the host does not know: as many workgroups as run at once, which are soon gone where it is empty
+        hipLaunchKernelGGL(steps_kernel<T>, dim3(std::min(all, 1024u)), dim3(THREADS), 0, s, a);
+        hipLaunchKernelGGL(place_kernel<T>, dim3(std::min(all, 1024u)), dim3(THREADS), 0, s, a);
+        hipLaunchKernelGGL(finish_kernel<T>, dim3(std::min(a.rows, 256)), dim3(THREADS), 0, s, a);
     }
 }
 
 template <class T, bool TOP> void launch(hipStream_t s, const PickArgs &a)
 {
-    const dim3 rows(a.rows), all((unsigned)a.rows * a.groups), threads(THREADS);
-    if (a.groups == 1) {
-        if (a.vocab <= 2048 * 2) hipLaunchKernelGGL((decide_kernel<T, TOP, true, 4096>), rows, threads, 0, s, a);
+    const dim3 rows(a.rows), threads(THREADS);
+    if (!a.head) {
+        if (a.vocab <= 4096) hipLaunchKernelGGL((decide_kernel<T, TOP, true, 4096>), rows, threads, 0, s, a);
         else hipLaunchKernelGGL((decide_kernel<T, TOP, true, 8192>), rows, threads, 0, s, a);
         return;
     }
-    hipLaunchKernelGGL((parts_kernel<T, TOP>), all, threads, 0, s, a);
-    if (a.groups * WAVES * a.listed <= 4096) hipLaunchKernelGGL((decide_kernel<T, TOP, false, 4096>), rows, threads, 0, s, a);
-    else hipLaunchKernelGGL((decide_kernel<T, TOP, false, 8192>), rows, threads, 0, s, a);
-    if constexpr (!TOP) {
-        if (!a.searched) return;
-        hipLaunchKernelGGL(steps_kernel<T>, all, threads, 0, s, a);
-        hipLaunchKernelGGL(place_kernel<T>, all, threads, 0, s, a);
-        hipLaunchKernelGGL(finish_kernel<T>, rows, threads, 0, s, a);
-    }
+    launch_parts<T, TOP>(s, a);
 }
 
 }  // namespace

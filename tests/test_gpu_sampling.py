@@ -235,13 +235,23 @@ def test_other_streams_and_graphs(sampling):
             check_top(z, 7, ids, values)
 
 
-def test_many_rows_and_none(sampling):
-    n, v = 3000, 77
-    s = sampling.Sampler(n, v)
-    z, u = logits_of("peaked", n, v, 101), torch.rand(n, device="cuda", generator=rng(102))
-    token, lp = s.sample(z, u, top_k=9, top_p=0.8)
-    check(z[::37], u[::37], dict(top_k=9, top_p=0.8), token[::37], lp[::37])
-    assert s.sample(z[:0], u[:0])[0].shape == (0,) and s.top(z[:0], 3)[0].shape == (0, 3)
+def test_no_rows(sampling):
+    s = sampling.Sampler(4, 77)
+    z, u = torch.zeros((0, 77), device="cuda"), torch.zeros(0, device="cuda")
+    assert s.sample(z, u)[0].shape == (0,) and s.top(z, 3)[0].shape == (0, 3)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n, v", [(3000, 77), (1030, 9000), (600, 20001), (300, 40003)])
+def test_many_rows(sampling, n, v, dtype):
+    """More than one launch takes, and more than one wavefront of 1024 tokens each for all of them."""
+    s, some = sampling.Sampler(n, v, dtype), slice(n % 7, None, 41)
+    for kind, how in (("peaked", dict(top_k=9, top_p=0.8)), ("flat", dict(top_p=0.9)), ("flat", {}), ("ties", dict(min_p=0.05)), ("peaked", dict(top_p=0.95, temperature=1.2))):
+        z, u = logits_of(kind, n, v, 101, dtype), torch.rand(n, device="cuda", generator=rng(102))
+        token, lp = s.sample(z, u, **how)
+        check(z[some], u[some], how, token[some], lp[some])
+    ids, values = s.top(z, 33)
+    check_top(z[some], 33, ids[some], values[some])
 
 
 def test_a_long_row(sampling):
