@@ -76,12 +76,21 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v) { return last_lane(wave
 
 // ------------------------------------------------------------------ weights
 
-// 2^(j / 32)
-__device__ const double POWERS[32] = {
-    1.0, 1.0218971486541166, 1.0442737824274138, 1.0671404006768237, 1.0905077326652577, 1.1143867425958924, 1.1387886347566916, 1.1637248587775775,
-    1.189207115002721, 1.215247359980469, 1.241857812073484, 1.2690509571917332, 1.2968395546510096, 1.3252366431597413, 1.3542555469368927, 1.383909881963832,
-    1.4142135623730951, 1.4451808069770467, 1.4768261459394993, 1.5091644275934228, 1.5422108254079407, 1.5759808451078865, 1.6104903319492543, 1.645755478153965,
-    1.681792830507429, 1.718619298122478, 1.7562521603732995, 1.7947090750031072, 1.8340080864093424, 1.8741676341103, 1.9152065613971474, 1.9571441241754002};
+// 2^(j / 32) as 64-bit words, less j << 47: with k << 47 added, k = 32 e + j, the word of 2^(k / 32)
+__device__ const uint2 POWERS[32] = {
+    {0x00000000, 0x3ff00000}, {0xd3158574, 0x3fefd9b0}, {0x6cf9890f, 0x3fefb558}, {0xd0125b51, 0x3fef9301}, {0x3c7d517b, 0x3fef72b8}, {0x3168b9aa, 0x3fef5487},
+    {0x6e756238, 0x3fef387a}, {0xf51fdee1, 0x3fef1e9d}, {0x0a31b715, 0x3fef06fe}, {0x373aa9cb, 0x3feef1a7}, {0x4c123422, 0x3feedea6}, {0x6061892d, 0x3feece08},
+    {0xd5362a27, 0x3feebfda}, {0x569d4f82, 0x3feeb42b}, {0xdd485429, 0x3feeab07}, {0xb03a5585, 0x3feea47e}, {0x667f3bcd, 0x3feea09e}, {0xe8ec5f74, 0x3fee9f75},
+    {0x73eb0187, 0x3feea114}, {0x994cce13, 0x3feea589}, {0x422aa0db, 0x3feeace5}, {0xb0cdc5e5, 0x3feeb737}, {0x82a3f090, 0x3feec491}, {0xb23e255d, 0x3feed503},
+    {0x995ad3ad, 0x3feee89f}, {0xf2fb5e47, 0x3feeff76}, {0xdd85529c, 0x3fef199b}, {0xdcef9069, 0x3fef3720}, {0xdcfba487, 0x3fef5818}, {0x337b9b5f, 0x3fef7c97},
+    {0xa2a490da, 0x3fefa4af}, {0x5b6e4540, 0x3fefd076}};
+
+// a constant in scalar registers: an operand of a multiply-add there, where the compiler would copy it to vector registers every time
+__device__ __forceinline__ double uniform(double v)
+{
+    asm("" : "+s"(v));
+    return v;
+}
 
 // What a row's user set, and what weights are relative to
 struct Row {
@@ -90,28 +99,31 @@ struct Row {
     bool cut, summed;         // some filter is set; the parts' sums are wanted
     double top, per, unit;    // largest logit, 32 log2(e) / T, 2^a.unit
     uint32_t top_key;
-    const double *powers;     // in LDS: 32 entries are one to each pair of banks
+    const uint2 *powers;      // in LDS: 32 entries are one to each pair of banks
     // exp((z - top) / T) = 2^(x / 32), x = k + f, |f| <= 1/2: 2^(k / 32) from the table, 2^(f / 32) - 1 = f q(f), q interpolated at four Chebyshev nodes (1.6e-13 off at most). 64 bits
     // are for the borders: a share that top-p ends at, or a draw, that is off by 1e-8 of all takes another token once in a hundred rows of a hundred thousand even tokens.
-    __device__ __forceinline__ double weight(float z) const
+    __device__ __forceinline__ double weight(float z) const { return top == INFINITY ? infinite_weight(z) : finite_weight(z); }
+    __device__ __forceinline__ double infinite_weight(float z) const { return z == INFINITY ? 1.0 : 0.0; }
+    __device__ __forceinline__ double finite_weight(float z) const
     {
-        if (top == INFINITY) return z == INFINITY ? 1.0 : 0.0;
         constexpr double WHOLE = 6755399441055744.0;      // 3 2^51: what is added to it is rounded to a whole number
         const double x = fmax(((double)z - top) * per, -32000.0), n = x + WHOLE, f = x - (n - WHOLE);
-        const int k = (int)(uint32_t)__double_as_longlong(n);
-        const double q = fma(fma(fma(9.172598566029335e-09, f, 1.6938609067364198e-06), f, 0.00023459619820112603), f, 0.021660849392187844);
-        const double power = powers[k & 31], scaled = __hiloint2double(__double2hiint(power) + ((k >> 5) << 20), __double2loint(power));
-        return fma(scaled, q * f, scaled);
+        const uint32_t k = (uint32_t)__double_as_longlong(n);
+        const double q = fma(fma(fma(uniform(9.172598566029335e-09), f, uniform(1.6938609067364198e-06)), f, uniform(0.00023459619820112603)), f, uniform(0.021660849392187844));
+        const uint2 word = powers[k & 31];
+        const double power = __hiloint2double((int)(word.y + (k << 15)), (int)word.x);
+        return fma(power, q * f, power);
     }
     // in units (2^51 of them at most: rounded by adding 2^52)
-    __device__ __forceinline__ u64 mass(float z) const { return (u64)__double_as_longlong(fma(weight(z), unit, 4503599627370496.0)) & 0xfffffffffffffull; }
+    __device__ __forceinline__ u64 in_units(double w) const { return (u64)__double_as_longlong(fma(w, unit, 4503599627370496.0)) & 0xfffffffffffffull; }
+    __device__ __forceinline__ u64 mass(float z) const { return in_units(weight(z)); }
     __device__ __forceinline__ u64 mass(uint32_t key) const { return mass(logit_of(key)); }
     __device__ __forceinline__ void relative_to(uint32_t key) { top_key = key; top = logit_of(key); }
 };
 
-__device__ __forceinline__ void load_powers(double *powers) { if (threadIdx.x % 64 < 32) powers[threadIdx.x % 64] = POWERS[threadIdx.x % 64]; }      // (every wavefront all of them)
+__device__ __forceinline__ void load_powers(uint2 *powers) { if (threadIdx.x % 64 < 32) powers[threadIdx.x % 64] = POWERS[threadIdx.x % 64]; }      // (every wavefront all of them)
 
-template <bool TOP> __device__ __forceinline__ Row row_of(const PickArgs &a, int r, const double *powers)
+template <bool TOP> __device__ __forceinline__ Row row_of(const PickArgs &a, int r, const uint2 *powers)
 {
     Row row{};
     row.t = 1.f; row.p = 1.f;
@@ -154,7 +166,7 @@ template <int HELD, bool WHOLE = false> struct Shared {
     u64 part[WAVES];
     u64 before, at;
     double run;
-    double powers[32];
+    uint2 powers[32];
     uint32_t place, top, from, n;
     uint32_t first, last;
     int found, entries;
@@ -589,7 +601,7 @@ template <class T> struct Part {
 template <class T, bool TOP> __global__ __launch_bounds__(THREADS, 8) void parts_kernel(PickArgs a)
 {
     __shared__ float s_z[WAVES][EACH / 4][64][4];
-    __shared__ double s_powers[32];
+    __shared__ uint2 s_powers[32];
     const int r = blockIdx.x / a.groups, lane = threadIdx.x % 64, wave = threadIdx.x / 64, parts = a.groups * WAVES, part = (blockIdx.x % a.groups) * WAVES + wave;
     Row row = row_of<TOP>(a, r, s_powers);
     // Of a row that is cut from, blocks of all parts take turns, so that large logits that lie together are spread over the parts; of one that is drawn from freely a part is one
@@ -604,7 +616,8 @@ template <class T, bool TOP> __global__ __launch_bounds__(THREADS, 8) void parts
     if (row.summed && head.top) {
         row.relative_to(head.top);
         double sum = 0;
-        p.each([&](float z, int) { sum += row.weight(z); });
+        if (row.top < INFINITY) p.each([&](float z, int) { sum += row.finite_weight(z); });
+        else p.each([&](float z, int) { sum += row.infinite_weight(z); });
         head.sum = wave_sum(sum);
     }
     if (row.cut) {
@@ -778,7 +791,7 @@ __device__ __forceinline__ int step_of(float z, const PickSearch &q) { return (i
 template <class T> __global__ __launch_bounds__(THREADS, 8) void steps_kernel(PickArgs a)
 {
     __shared__ float s_z[WAVES][EACH / 4][64][4];
-    __shared__ double s_powers[32];
+    __shared__ uint2 s_powers[32];
     __shared__ u64 step[PICK_STEPS];
     static_assert(PICK_STEPS == THREADS);
     load_powers(s_powers);
@@ -799,7 +812,7 @@ template <class T> __global__ __launch_bounds__(THREADS, 8) void steps_kernel(Pi
         p.each([&](float z, int) {
             const int at = z >= q.from ? -1 : step_of(z, q);
             if (z == -INFINITY || at >= PICK_STEPS - 1) return;
-            const u64 m = row.mass(z);
+            const u64 m = row.in_units(row.finite_weight(z));
             if (at < 0) above += m;
             else atomicAdd(&step[at], m);
         });
@@ -814,7 +827,7 @@ template <class T> __global__ __launch_bounds__(THREADS, 8) void steps_kernel(Pi
 template <class T> __global__ __launch_bounds__(THREADS, 8) void place_kernel(PickArgs a)
 {
     __shared__ float s_z[WAVES][EACH / 4][64][4];
-    __shared__ double s_powers[32];
+    __shared__ uint2 s_powers[32];
     __shared__ u64 s_part[WAVES];
     __shared__ int s_step;
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, parts = a.groups * WAVES;
@@ -860,7 +873,7 @@ template <class T> __global__ __launch_bounds__(THREADS, 8) void place_kernel(Pi
         p.each([&](float z, int e) {
             if (z == -INFINITY) return;
             const int at = stage == PICK_STEP ? step_of(z, q) : PICK_STEPS;
-            if (z >= least || at < step) mass += row.mass(z);
+            if (z >= least || at < step) mass += row.in_units(row.finite_weight(z));
             else mask |= (uint32_t)(at == step) << e;
         });
         head.mass = wave_sum(mass);
