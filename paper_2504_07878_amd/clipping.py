@@ -31,7 +31,7 @@ class Clipper:
         self.lib = tokroute.load_library()
         self.workspace = torch.empty(self.lib.tr_grad_workspace_bytes(), dtype=torch.uint8, device=device)
         self.device = self.workspace.device
-        self._home = torch.cuda.current_stream(self.device)
+        self._home = torch.cuda.current_stream(self.device).cuda_stream
 
     # -- helpers
     def _list(self, grads, what="gradients"):
@@ -49,11 +49,11 @@ class Clipper:
         return array("q", map(torch.Tensor.numel, grads)), array("i", [_DTYPES[t.dtype] for t in grads])
 
     def _call(self, fn, what, arrays, *args):
-        s = torch.cuda.current_stream(self.device)
-        if s != self._home:
-            self.workspace.record_stream(s)    # its memory is not handed on while work of that stream may use it
-        with torch.cuda.device(self.device):   # a default stream is the current device's
-            rc = fn(self.workspace.data_ptr(), self.workspace.numel(), s.cuda_stream, len(arrays[0]), *[x.buffer_info()[0] for x in arrays], *args)
+        stream = tokroute.raw_stream(self.device.index)
+        if stream != self._home:
+            self.workspace.record_stream(torch.cuda.current_stream(self.device))    # its memory is not handed on while work of that stream may use it
+        with tokroute.on_device(self.device.index):      # a default stream is the current device's
+            rc = fn(self.workspace.data_ptr(), self.workspace.numel(), stream, len(arrays[0]), *[x.buffer_info()[0] for x in arrays], *args)
         if rc:
             raise TokrouteError(rc, what)
 

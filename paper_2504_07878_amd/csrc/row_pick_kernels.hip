@@ -20,12 +20,15 @@ namespace {
 typedef unsigned long long u64;
 
 constexpr int THREADS = PICK_THREADS, WAVES = PICK_WAVES, EACH = PICK_PART / 64;
-constexpr int BIN_BITS = 11, BINS = 1 << BIN_BITS;
+constexpr int DECIDERS = 512;      // threads of a workgroup that decides on a row (1024: 9.6 instead of 7.8 us for one row)
+constexpr int BIN_BITS = 9, BINS = 1 << BIN_BITS;
+static_assert(BINS == DECIDERS);
 constexpr int MAX_PARTS = PICK_MAX_VOCAB / PICK_PART;
-constexpr int PART_STEPS = PICK_PART / THREADS;      // tokens a thread where a workgroup looks through a part
-constexpr int FEW = 256;      // tokens that are compared with each other, all with all
+constexpr int FEW = 256, FEW_PLACES = 128;      // tokens that are compared with each other, all with all, instead of all that is left to do, or of a step (5 us among 250)
+constexpr int LESS = 2048;    // tokens that are put together once a search has left so few
 constexpr uint32_t LOWEST = 0x00800000u, ANY = 0xffffffffu;      // key of the lowest finite logit
-static_assert(MAX_PARTS == 2 * THREADS && PART_STEPS == 2 && THREADS == 2 * FEW);
+constexpr int PER = PICK_PART / DECIDERS;      // tokens of a part, or parts of a row, a thread
+static_assert(MAX_PARTS == PICK_PART);
 
 // Logits as whole numbers in their order. -inf and NaN are no tokens: key 0. (-0 is 0.)
 __device__ __forceinline__ uint32_t key_of(float z)
@@ -49,6 +52,12 @@ template <int C, int ROWS, class V> __device__ __forceinline__ V lanes_before(V 
         const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, C, ROWS, 0xf, false), hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(x >> 32), C, ROWS, 0xf, false);
         return __builtin_bit_cast(V, (u64)hi << 32 | lo);
     }
+}
+// v of another lane (quad_perm, row_half_mirror, row_mirror)
+template <int C> __device__ __forceinline__ u64 lanes_from(u64 v)
+{
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, C, 0xf, 0xf, false), hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), C, 0xf, 0xf, false);
+    return (u64)hi << 32 | lo;
 }
 // join of the values of all lanes up to this one; zero is the join's neutral value
 template <class V, class Join> __device__ __forceinline__ V wave_upto(V v, Join join)
@@ -163,19 +172,20 @@ __device__ __forceinline__ double evenly(float u) { return fmin(fmax((double)u, 
 template <int HELD, bool WHOLE = false> struct Shared {
     static constexpr bool by_place = WHOLE;      // a token's id is its place
     u64 bin[BINS];
-    u64 part[WAVES];
+    u64 part[DECIDERS / 64];
     u64 before, at;
     double run;
     uint2 powers[32];
-    uint32_t place, top, from, n;
+    uint32_t place, top, from, n, most, least;
     uint32_t first, last;
     int found, entries;
+    u64 few[FEW], few_mass[FEW];
     union {
-        struct { u64 few[FEW], few_mass[FEW]; };
         u64 entry[PICK_MAX_ENTRIES];
         u64 mass[MAX_PARTS];
     };
-    uint32_t key[HELD], id[WHOLE ? 1 : HELD];      // tokens, key 0: none
+    uint32_t key[HELD + LESS], id[(WHOLE ? 0 : HELD) + LESS];      // tokens, key 0: none; behind them those that a first step has left
+    static constexpr int held = HELD, ids = WHOLE ? 0 : HELD;
 };
 
 // sum of the values of all threads up to this one, and of all
@@ -188,7 +198,7 @@ template <class V, class S> __device__ __forceinline__ V sum_upto(V v, V &total,
     __syncthreads();
     V run = 0, before = 0;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
+    for (int w = 0; w < DECIDERS / 64; ++w) {
         if (w == (int)threadIdx.x / 64) before = run;
         run += __builtin_bit_cast(V, s.part[w]);
     }
@@ -208,53 +218,130 @@ struct Border { bool found; uint32_t place; u64 before, at; };
 template <class Each, class S> __device__ __forceinline__ Border border_step(Each each, uint32_t base, int bits, int shift, u64 before, u64 want, S &s)
 {
     const uint32_t most = bits >= 32 ? ANY : (1u << bits) - 1;
-    constexpr int N = BINS / THREADS;
     __syncthreads();
-    for (int i = threadIdx.x; i < BINS; i += THREADS) s.bin[i] = 0;
+    s.bin[threadIdx.x] = 0;
     if (threadIdx.x == 0) s.found = 0;
     __syncthreads();
-    each([&](uint32_t place, auto amount) {
-        const uint32_t d = place - base;
-        if (d <= most) atomicAdd(&s.bin[d >> shift], (u64)amount());
-    });
+    each([&](uint32_t place) { return place - base <= most; }, [&](uint32_t place, u64 amount) { atomicAdd(&s.bin[(place - base) >> shift], amount); });
     __syncthreads();
-    u64 mine[N], sum = 0, total;
-#pragma unroll
-    for (int e = 0; e < N; ++e) sum += mine[e] = s.bin[threadIdx.x * N + e];
-    u64 run = before + sum_upto(sum, total, s) - sum;
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-        if (run < want && want <= run + mine[e]) {      // (for one thread and one bin at most)
-            s.found = 1; s.before = run; s.at = mine[e]; s.place = base + ((uint32_t)(threadIdx.x * N + e) << shift);
-        }
-        run += mine[e];
+    u64 total;
+    const u64 mine = s.bin[threadIdx.x], upto = before + sum_upto(mine, total, s);
+    if (upto - mine < want && want <= upto) {      // (for one thread at most)
+        s.found = 1; s.before = upto - mine; s.at = mine; s.place = base + (threadIdx.x << shift);
     }
     __syncthreads();
     return s.found ? Border{true, s.place, s.before, s.at} : Border{false, 0, 0, 0};
 }
 
-// The first place up to which the amounts come to `want` (> 0) or more, what lies before it and what at it. each(add) calls add(place, amount) for everything, amount() being what it is; places are below
-// 2^bits. Eleven bits of the place at a time, by a histogram of amounts. All threads get the answer. b: of a step before, which bits are left of.
-template <class Each, class S> __device__ __forceinline__ Border find_border(Each each, int bits, u64 want, S &s, Border b = Border{true, 0, 0, 0})
+// Few tokens compared with each other, all with all: a team of 2 to 16 neighbouring lanes for each, as many as there are lanes for
+struct Team {
+    int lanes, token, lane;
+    __device__ __forceinline__ explicit Team(int n) : lanes(n <= DECIDERS / 16 ? 16 : n <= DECIDERS / 8 ? 8 : n <= DECIDERS / 4 ? 4 : 2), token((int)threadIdx.x / lanes), lane((int)threadIdx.x % lanes) {}
+    // f(j) for the lane's share of the tokens to compare with
+    template <class F> __device__ __forceinline__ void each(int n, F f) const
+    {
+        if (token < n)
+#pragma unroll 4
+            for (int j = lane; j < n; j += lanes) f(j);
+    }
+    __device__ __forceinline__ u64 sum(u64 v) const
+    {
+        v += lanes_from<0xb1>(v);                      // lane ^ 1
+        if (lanes >= 4) v += lanes_from<0x4e>(v);      // lane ^ 2
+        if (lanes >= 8) v += lanes_from<0x141>(v);     // the other four of eight
+        if (lanes >= 16) v += lanes_from<0x140>(v);    // the other eight of sixteen
+        return v;
+    }
+    __device__ __forceinline__ int sum(int v) const { return (int)sum((u64)v); }
+};
+
+// The first place up to which the amounts come to `want` (> 0) or more, what lies before it and what at it. each(in, put) calls put(place, amount) for everything whose place in(place) names; places are below
+// 2^bits. Nine bits of the place at a time, by a histogram of amounts, until the step that holds the place has so few of everything that they can be compared all with all. All threads
+// get the answer. b: of a step before, which bits are left of.
+template <class Each, class S> __device__ __forceinline__ Border find_border(Each each, int bits, u64 want, S &s, Border b = Border{true, 0, 0, 0}, bool stepped = false)
 {
 #pragma unroll 1
-    do {
-        const int shift = max(0, bits - BIN_BITS);
-        b = border_step(each, b.place, bits, shift, b.before, want, s);
-        bits = shift;
-    } while (bits > 0 && b.found);
-    return b;
+    for (;;) {
+        if (!stepped) {
+            const int shift = max(0, bits - BIN_BITS);
+            b = border_step(each, b.place, bits, shift, b.before, want, s);
+            bits = shift;
+        }
+        if (!b.found || bits == 0) return b;
+        stepped = false;
+        const uint32_t most = (1u << bits) - 1;
+        if (threadIdx.x == 0) s.entries = 0;
+        __syncthreads();
+        each([&](uint32_t place) { return place - b.place <= most; }, [&](uint32_t place, u64 amount) {
+            const int i = atomicAdd(&s.entries, 1);
+            if (i < FEW_PLACES) { s.few[i] = place; s.few_mass[i] = amount; }
+        });
+        __syncthreads();
+        const int n = s.entries;
+        if (n > FEW_PLACES) continue;
+        const Team team(n);
+        const int i = team.token;
+        const uint32_t place = i < n ? (uint32_t)s.few[i] : 0;
+        u64 before = 0, at = 0;
+        team.each(n, [&](int j) {
+            const uint32_t other = (uint32_t)s.few[j];
+            const u64 amount = s.few_mass[j];
+            before += other < place ? amount : 0;
+            at += other == place ? amount : 0;
+        });
+        before = b.before + team.sum(before);
+        at = team.sum(at);
+        if (i < n && before < want && want <= before + at) { s.place = place; s.before = before; s.at = at; }      // (the same from all that are equal)
+        __syncthreads();
+        return Border{true, s.place, s.before, s.at};
+    }
 }
 
-// Where a row's tokens come from: what a workgroup holds, all tokens of keys `from` and above
+// Where a row's tokens come from. tally(in, amount, put) calls put(key, id, amount(key)) for the tokens that in(key, id) names.
+// What a workgroup holds, all tokens of keys `from` and above: four at a time, so that their amounts are computed side by side
 template <class S> struct Pool {
-    const S &s;
+    S &s;
     uint32_t from, n;
+    bool less = false;      // those behind the others
     __device__ __forceinline__ bool all() const { return from <= LOWEST; }
-    template <class F> __device__ __forceinline__ void each(F f) const
+    template <class In, class Amount, class Put> __device__ __forceinline__ void tally(In in, Amount amount, Put put) const
     {
+        constexpr int N = 4;
+        const uint32_t *const keys = s.key + (less ? S::held : 0), *const ids = s.id + (less ? S::ids : 0);
 #pragma unroll 1
-        for (uint32_t i = threadIdx.x; i < n; i += THREADS) if (const uint32_t key = s.key[i]) f(key, S::by_place ? i : s.id[i]);
+        for (uint32_t first = threadIdx.x; first < n; first += N * DECIDERS) {
+            uint32_t key[N], id[N];
+            u64 v[N];
+            bool ok[N];
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const uint32_t i = first + e * DECIDERS, at = i < n ? i : first;
+                key[e] = i < n ? keys[at] : 0;
+                id[e] = S::by_place && !less ? at : ids[at];
+            }
+#pragma unroll
+            for (int e = 0; e < N; ++e) ok[e] = (key[e] != 0) & in(key[e], id[e]);
+            if (__any(ok[0] | ok[1] | ok[2] | ok[3])) {
+#pragma unroll
+                for (int e = 0; e < N; ++e) v[e] = amount(key[e]);
+#pragma unroll
+                for (int e = 0; e < N; ++e) if (ok[e]) put(key[e], id[e], v[e]);
+            }
+        }
+    }
+    // Only the tokens that in(key, id) names from here on, where they are few enough
+    template <class In> __device__ __forceinline__ void lessen(In in)
+    {
+        if (less) return;
+        __syncthreads();
+        if (threadIdx.x == 0) s.entries = 0;
+        __syncthreads();
+        tally(in, [](uint32_t) { return 0; }, [&](uint32_t key, uint32_t id, u64) {
+            const int i = atomicAdd(&s.entries, 1);
+            if (i < LESS) { s.key[S::held + i] = key; s.id[S::ids + i] = id; }
+        });
+        __syncthreads();
+        if (s.entries <= LESS) { less = true; n = s.entries; }
     }
 };
 
@@ -264,11 +351,12 @@ template <class T> struct Streamed {
     int vocab;
     static constexpr uint32_t from = LOWEST;
     __device__ __forceinline__ bool all() const { return true; }
-    template <class F> __device__ __forceinline__ void each(F f) const
+    template <class In> __device__ __forceinline__ void lessen(In) {}
+    template <class In, class Amount, class Put> __device__ __forceinline__ void tally(In in, Amount amount, Put put) const
     {
         constexpr int N = 16 / sizeof(T);
 #pragma unroll 1
-        for (int i = threadIdx.x * N; i < vocab; i += THREADS * N) {
+        for (int i = threadIdx.x * N; i < vocab; i += DECIDERS * N) {
             T v[N];
             if (i + N <= vocab) __builtin_memcpy(v, row + i, 16);
             else {
@@ -278,7 +366,7 @@ template <class T> struct Streamed {
 #pragma unroll
             for (int e = 0; e < N; ++e) {
                 const uint32_t key = i + e < vocab ? key_of(wide(v[e])) : 0;
-                if (key) f(key, (uint32_t)(i + e));
+                if (key && in(key, (uint32_t)(i + e))) put(key, (uint32_t)(i + e), (u64)amount(key));
             }
         }
     }
@@ -287,7 +375,8 @@ template <class T> struct Streamed {
 // What is kept of a row: all keys above `key`, and of those equal to it ids up to `last`
 struct Kept {
     uint32_t key, last;
-    __device__ __forceinline__ bool has(uint32_t k, uint32_t id) const { return k > key || (k == key && id <= last); }
+    u64 mass;             // 0: not known
+    __device__ __forceinline__ bool has(uint32_t k, uint32_t id) const { return (k > key) | ((k == key) & (id <= last)); }
 };
 
 __device__ __forceinline__ int bits_of(uint32_t v) { return v ? 32 - __clz(v) : 1; }
@@ -296,51 +385,6 @@ __device__ __forceinline__ int bits_of(uint32_t v) { return v ? 32 - __clz(v) : 
 __device__ __forceinline__ u64 share_of(float p, u64 sum) { return max(min((u64)ceil(fmax((double)p, 0.0) * (double)sum), sum), 1ull); }
 __device__ __forceinline__ u64 share_of(float p, double weight, double unit) { return max((u64)ceil(fmax((double)p, 0.0) * weight * unit), 1ull); }
 
-// A first step towards the border of top-k or top-p (key places, 2^shift of them), where one was taken
-struct First { Border b; int shift; };
-
-// What the filters keep; false: more than the source knows of. `weight`: of the whole row, for a source that does not hold it all.
-template <class Source, class S> __device__ __forceinline__ bool keep(const Source &src, const Row &r, double weight, int vocab, const First &first, Kept &kept, S &s)
-{
-    const int key_bits = first.b.found ? first.shift : bits_of(r.top_key - src.from);
-    const Border from = first.b.found ? first.b : Border{true, 0, 0, 0};
-    bool cut = false;
-    u64 ties = 0;                     // 0: all of them
-    kept = Kept{LOWEST, ANY};
-    if (r.k > 0) {
-        const Border b = find_border([&](auto add) { src.each([&](uint32_t key, uint32_t) { add(r.top_key - key, [] { return 1; }); }); }, key_bits, r.k, s, from);
-        if (!b.found && !src.all()) return false;
-        if (b.found) { kept.key = r.top_key - b.place; ties = r.k - b.before < b.at ? r.k - b.before : 0; cut = true; }
-    }
-    if (r.p < 1.f) {
-        const uint32_t least = max(kept.key, src.from);
-        u64 want;
-        if (cut || src.all()) {
-            u64 sum = 0;
-            src.each([&](uint32_t key, uint32_t) { sum += key > kept.key || (key == kept.key && !ties) ? r.mass(key) : 0; });
-            want = share_of(r.p, sum_of_all(sum, s) + (ties ? ties * r.mass(kept.key) : 0));
-        } else want = share_of(r.p, weight, r.unit);
-        const Border b = find_border([&](auto add) { src.each([&](uint32_t key, uint32_t) { if (key >= least) add(r.top_key - key, [&] { return r.mass(key); }); }); },
-                                     cut ? bits_of(r.top_key - least) : key_bits, want, s, cut ? Border{true, 0, 0, 0} : from);
-        if (!b.found) return false;
-        const uint32_t key = r.top_key - b.place;
-        const u64 one = r.mass(key), need = (want - b.before + one - 1) / one;
-        if (key != kept.key || !ties || need < ties) ties = need < b.at / one ? need : 0;
-        kept.key = key;
-        cut = true;
-    }
-    if (r.m > 0.f) {
-        const uint32_t least = least_key(r);
-        if (!cut && least < src.from) return false;
-        if (least > kept.key) { kept.key = least; ties = 0; }
-        if (r.m > 1.f) ties = 1;
-        cut = true;
-    }
-    if (!cut && !src.all()) return false;
-    if (ties) kept.last = find_border([&](auto add) { src.each([&](uint32_t key, uint32_t id) { if (key == kept.key) add(id, [] { return 1; }); }); }, bits_of(vocab - 1), ties, s).place;
-    return true;
-}
-
 __device__ __forceinline__ void put_draw(const PickArgs &a, int r, const Row &row, uint32_t id, float z, double total)
 {
     a.token[r] = (int)id;
@@ -348,59 +392,138 @@ __device__ __forceinline__ void put_draw(const PickArgs &a, int r, const Row &ro
 }
 __device__ __forceinline__ void put_nothing(const PickArgs &a, int r, bool top)
 {
-    if (top) for (int i = threadIdx.x; i < a.entries; i += THREADS) { a.ids[(long long)r * a.entries + i] = -1; a.values[(long long)r * a.entries + i] = -INFINITY; }
+    if (top) for (int i = threadIdx.x; i < a.entries; i += DECIDERS) { a.ids[(long long)r * a.entries + i] = -1; a.values[(long long)r * a.entries + i] = -INFINITY; }
     else if (threadIdx.x == 0) { a.token[r] = -1; a.logprob[r] = 0.f; }
 }
 
-template <class T, class Source, class S> __device__ __forceinline__ bool draw(const Source &src, const PickArgs &a, int r, const T *logits, const Row &row, double weight, const First &first, S &s)
-{
-    Kept kept;
-    if (!keep(src, row, weight, a.vocab, first, kept, s)) return false;
-    u64 sum = 0;
-    src.each([&](uint32_t key, uint32_t id) { sum += kept.has(key, id) ? row.mass(key) : 0; });
-    sum = sum_of_all(sum, s);
-    const u64 below = min((u64)(evenly(a.u[r]) * (double)sum), sum - 1);
-    const Border b = find_border([&](auto add) { src.each([&](uint32_t key, uint32_t id) { if (kept.has(key, id)) add(id, [&] { return row.mass(key); }); }); }, bits_of(a.vocab - 1), below + 1, s);
-    if (threadIdx.x == 0) put_draw(a, r, row, b.place, wide(logits[b.place]), (double)sum / row.unit);
-    return true;
-}
+// A first step towards the border of top-k or top-p, where one was taken: key places from b.place on, less than 2^shift of them
+struct First { Border b; int shift; u64 want; };
 
-template <class Source, class S> __device__ __forceinline__ bool list_top(const Source &src, const PickArgs &a, int r, const Row &row, const First &first, S &s)
+// What the filters keep, listed in order (TOP) or drawn from; false: more than the source knows of. `weight`: of the whole row, for a source that does not hold it all.
+// Searches follow each other: where top-k ends, where top-p does, which of equal tokens are kept, which token is drawn. One piece of code is all of them.
+template <bool TOP, class Source, class S> __device__ __forceinline__ bool search(Source &src, const PickArgs &a, int r, const Row &row, double weight, const First &first, S &s)
 {
-    Kept kept;
-    if (!keep(src, row, 0.0, a.vocab, first, kept, s)) return false;
-    __syncthreads();
-    for (int i = threadIdx.x; i < PICK_MAX_ENTRIES; i += THREADS) s.entry[i] = ~0ull;
-    if (threadIdx.x == 0) s.entries = 0;
-    __syncthreads();
-    src.each([&](uint32_t key, uint32_t id) { if (kept.has(key, id)) s.entry[atomicAdd(&s.entries, 1)] = (u64)~key << 32 | id; });
-    __syncthreads();
-    const int n = s.entries;
+    enum { BY_COUNT, BY_MASS, KEPT, BY_TIE, BY_DRAW };
+    Kept kept{LOWEST, ANY, 0};
+    bool cut = false, stepped = first.b.found;
+    u64 ties = 0, equal = 0, want = 0, sum = 0;      // ties 0: all of them, of `equal` ones
+    int mode = row.k > 0 ? BY_COUNT : row.p < 1.f ? BY_MASS : KEPT;
 #pragma unroll 1
-    for (int size = 2; size < 2 * n; size *= 2)
-#pragma unroll 1
-        for (int step = size / 2; step; step /= 2) {
-            __syncthreads();
-            const int x = (threadIdx.x / step) * 2 * step + threadIdx.x % step, y = x + step;
-            const u64 v = s.entry[x], w = s.entry[y];
-            if ((v > w) == !(x & size)) { s.entry[x] = w; s.entry[y] = v; }
+    for (;;) {
+        if (mode == KEPT) {
+            if (row.m > 0.f) {
+                const uint32_t least = least_key(row);
+                if (!cut && least < src.from) return false;
+                if (least > kept.key) { kept.key = least; ties = 0; kept.mass = 0; }
+                if (row.m > 1.f) { ties = 1; equal = ANY; kept.mass = 0; }
+                cut = true;
+            }
+            if (!cut && !src.all()) return false;
+            mode = ties ? BY_TIE : BY_DRAW;
         }
-    __syncthreads();
-    for (int i = threadIdx.x; i < a.entries; i += THREADS) {
-        const u64 e = s.entry[i];
-        a.ids[(long long)r * a.entries + i] = e == ~0ull ? -1 : (int)(uint32_t)e;
-        a.values[(long long)r * a.entries + i] = e == ~0ull ? -INFINITY : logit_of(~(uint32_t)(e >> 32));
+        if (TOP && mode == BY_DRAW) break;
+        const uint32_t least = max(kept.key, src.from);
+        const bool by_key = mode == BY_COUNT || mode == BY_MASS, by_mass = mode == BY_MASS || mode == BY_DRAW;
+        if (mode == BY_COUNT) want = row.k;
+        if (mode == BY_TIE) want = ties;
+        if (by_mass) {
+            if (mode == BY_MASS && stepped) want = first.want;
+            else if (mode == BY_MASS && !cut && !src.all()) want = share_of(row.p, weight, row.unit);
+            else {
+                sum = kept.mass;
+                if (!sum) {
+                    const bool some = mode == BY_MASS && ties;      // of the equal ones: which is not known yet
+                    src.tally([&](uint32_t key, uint32_t id) { return kept.has(key, id) & !(some & (key == kept.key)); }, [&](uint32_t key) { return row.mass(key); },
+                              [&](uint32_t, uint32_t, u64 m) { sum += m; });
+                    sum = sum_of_all(sum, s) + (mode == BY_MASS && ties ? ties * row.mass(kept.key) : 0);
+                }
+                want = mode == BY_MASS ? share_of(row.p, sum) : min((u64)(evenly(a.u[r]) * (double)sum), sum - 1) + 1;
+            }
+        }
+        const bool few = mode == BY_TIE && equal <= FEW_PLACES;      // no step is needed to get to them
+        const int bits = stepped ? first.shift : bits_of(by_key ? row.top_key - least : (uint32_t)a.vocab - 1);
+        // what is looked through: keys above `over` and ids of it up to `last`, no keys above `most`
+        const uint32_t over = by_key ? least : kept.key, last = mode == BY_DRAW ? kept.last : ANY, most = mode == BY_TIE ? kept.key : ANY, key_bits = by_key ? ANY : 0;
+        const auto place = [&](uint32_t key, uint32_t id) { return (key_bits & (row.top_key - key)) | (~key_bits & id); };
+        const Border b = find_border([&](auto in, auto put) {
+            src.tally([&](uint32_t key, uint32_t id) { return ((key > over) | ((key == over) & (id <= last))) & (key <= most) & in(place(key, id)); },
+                      [&](uint32_t key) { return by_mass ? row.mass(key) : 1; }, [&](uint32_t key, uint32_t id, u64 m) { put(place(key, id), m); });
+        }, bits, want, s, stepped ? first.b : Border{true, 0, 0, 0}, stepped | few);
+        stepped = false;
+        if (mode == BY_COUNT) {
+            if (!b.found && !src.all()) return false;
+            if (b.found) {
+                kept.key = row.top_key - b.place; equal = b.at; ties = want - b.before < b.at ? want - b.before : 0; cut = true;
+                if (!TOP) src.lessen([&](uint32_t key, uint32_t) { return key >= kept.key; });
+            }
+            mode = row.p < 1.f ? BY_MASS : KEPT;
+        } else if (mode == BY_MASS) {
+            if (!b.found) {
+                if (!(row.m > 0.f && least_key(row) >= src.from)) return false;
+                mode = KEPT;      // (min-p ends before)
+                continue;
+            }
+            const uint32_t key = row.top_key - b.place;
+            const u64 one = row.mass(key), need = (want - b.before + one - 1) / one;
+            equal = b.at / one;
+            if (key != kept.key || !ties || need < ties) ties = need < equal ? need : 0;
+            kept.key = key;
+            kept.mass = ties ? b.before + ties * one : b.before + b.at;
+            cut = true;
+            mode = KEPT;
+        } else if (mode == BY_TIE) {
+            kept.last = b.place;
+            mode = BY_DRAW;
+        } else {
+            // (its logit: what the draw was from)
+            src.tally([&](uint32_t, uint32_t id) { return id == b.place; }, [](uint32_t) { return 0; },
+                      [&](uint32_t key, uint32_t id, u64) { put_draw(a, r, row, id, logit_of(key), (double)sum / row.unit); });
+            return true;
+        }
+    }
+    if constexpr (TOP) {
+        __syncthreads();
+        for (int i = threadIdx.x; i < PICK_MAX_ENTRIES; i += DECIDERS) s.entry[i] = ~0ull;
+        if (threadIdx.x == 0) s.entries = 0;
+        __syncthreads();
+        src.tally([&](uint32_t key, uint32_t id) { return kept.has(key, id); }, [](uint32_t) { return 0; },
+                  [&](uint32_t key, uint32_t id, u64) { s.entry[atomicAdd(&s.entries, 1)] = (u64)~key << 32 | id; });
+        __syncthreads();
+        const int n = s.entries;
+#pragma unroll 1
+        for (int size = 2; size < 2 * n; size *= 2)
+#pragma unroll 1
+            for (int step = size / 2; step; step /= 2) {
+                __syncthreads();
+                if (threadIdx.x >= PICK_MAX_ENTRIES / 2) continue;
+                const int x = (threadIdx.x / step) * 2 * step + threadIdx.x % step, y = x + step;
+                const u64 v = s.entry[x], w = s.entry[y];
+                if ((v > w) == !(x & size)) { s.entry[x] = w; s.entry[y] = v; }
+            }
+        __syncthreads();
+        for (int i = threadIdx.x; i < a.entries; i += DECIDERS) {
+            const u64 e = s.entry[i];
+            a.ids[(long long)r * a.entries + i] = e == ~0ull ? -1 : (int)(uint32_t)e;
+            a.values[(long long)r * a.entries + i] = e == ~0ull ? -INFINITY : logit_of(~(uint32_t)(e >> 32));
+        }
     }
     return true;
 }
 
-// Tokens that a workgroup can compare all with all: those from where top-k or top-p end on, or min-p. Two threads a token add up what comes before it in the order, and then, of what is kept,
+// One workgroup looks through a row in memory, as often as it takes.
+template <class T, bool TOP, class S> __device__ __forceinline__ void whole_row(const PickArgs &a, int r, const Row &row, S &s)
+{
+    Streamed<T> all{(const T *)a.logits + (long long)r * a.stride, a.vocab};
+    search<TOP>(all, a, r, row, 0.0, First{}, s);
+}
+
+// Tokens that a workgroup can compare all with all: those from where top-k or top-p end on, or min-p. A team of lanes a token adds up what comes before it in the order, and then, of what is kept,
 // what comes before it by id. false: more than FEW, or more than the source knows of.
-template <bool TOP, class S> __device__ __forceinline__ bool among_few(const Pool<S> &src, const PickArgs &a, int r, const Row &row, double weight, First &first, S &s)
+template <bool TOP, class S> __device__ __forceinline__ bool among_few(Pool<S> &src, const PickArgs &a, int r, const Row &row, double weight, uint32_t low, First &first, S &s)
 {
     if (row.k > FEW) return false;
-    uint32_t floor = src.from;
-    bool closed = src.all();
+    uint32_t floor = max(src.from, low);
+    bool closed = floor <= LOWEST;
     const uint32_t least = row.m > 0.f ? least_key(row) : 0;
     if (row.m > 0.f && least >= floor && !(row.p < 1.f && row.k > 0)) { floor = least; closed = true; }      // (top-p's is a share of all that top-k keeps)
     u64 want = 0;
@@ -408,93 +531,100 @@ template <bool TOP, class S> __device__ __forceinline__ bool among_few(const Poo
         if (!src.all()) want = share_of(row.p, weight, row.unit);
         else {
             u64 sum = 0;
-            src.each([&](uint32_t key, uint32_t) { sum += row.mass(key); });
+            src.tally([](uint32_t, uint32_t) { return true; }, [&](uint32_t key) { return row.mass(key); }, [&](uint32_t, uint32_t, u64 m) { sum += m; });
             want = share_of(row.p, sum_of_all(sum, s));
         }
     }
-    if (row.k > 0 || row.p < 1.f) {
-        const int bits = bits_of(row.top_key - floor), shift = max(0, bits - BIN_BITS);
+    // steps of equal width down to the floor (keys are denser the nearer logits are to zero)
+    const bool by_step = (row.k > 0 || row.p < 1.f) && row.top < INFINITY;
+    const float high = logit_of(row.top_key), scale = (BINS - 1) / fmaxf(high - logit_of(floor), FLT_MIN);
+    const auto step = [&](uint32_t key) { return (uint32_t)fminf((high - logit_of(key)) * scale, (float)BINS); };
+    uint32_t last = ANY;
+    if (by_step) {
         const bool by_count = row.k > 0;
-        const Border b = border_step([&](auto add) { src.each([&](uint32_t key, uint32_t) { if (key >= floor) add(row.top_key - key, [&] { return by_count ? 1 : row.mass(key); }); }); }, 0, bits, shift, 0,
-                                     by_count ? (u64)row.k : want, s);
-        first = First{b, shift};
-        if (b.found) { floor = row.top_key - min(row.top_key - floor, b.place + ((1u << shift) - 1)); closed = true; }
+        const Border b = border_step([&](auto in, auto put) {
+            src.tally([&](uint32_t key, uint32_t) { return (key >= floor) & in(step(key)); }, [&](uint32_t key) { return by_count ? 1 : row.mass(key); },
+                      [&](uint32_t key, uint32_t, u64 m) { put(step(key), m); });
+        }, 0, BIN_BITS, 0, 0, by_count ? (u64)row.k : want, s);
+        if (b.found) { last = b.place; closed = true; first.b = b; first.want = want; }
     }
     if (!closed) return false;
     __syncthreads();
-    if (threadIdx.x == 0) s.entries = 0;
+    if (threadIdx.x == 0) { s.entries = 0; s.most = 0; s.least = ANY; }
     __syncthreads();
-    src.each([&](uint32_t key, uint32_t id) {
-        if (key < floor) return;
+    src.tally([&](uint32_t key, uint32_t) { return (key >= floor) & (!by_step | (step(key) <= last)); }, [](uint32_t) { return 0; }, [&](uint32_t key, uint32_t id, u64) {
         const int i = atomicAdd(&s.entries, 1);
         if (i < FEW) s.few[i] = (u64)~key << 32 | id;
+        if (i < LESS) { s.key[S::held + i] = key; s.id[S::ids + i] = id; }
+        if (by_step && step(key) == last) { atomicMax(&s.most, key); atomicMin(&s.least, key); }
     });
     __syncthreads();
     const int n = s.entries;
-    if (n > FEW) return false;
-    const int i = threadIdx.x / 2, half = threadIdx.x % 2;
+    if (n > FEW) {
+        // the border is in the step's keys
+        if (first.b.found) { first.shift = bits_of(s.most - s.least); first.b.place = row.top_key - s.most; }
+        if (n <= LESS) { src.less = true; src.n = n; }
+        return false;
+    }
+    const Team team(n);
+    const int i = team.token;
+    const bool speaks = i < n && team.lane == 0;
     const u64 mine = i < n ? s.few[i] : ~0ull;
     const uint32_t key = ~(uint32_t)(mine >> 32), id = (uint32_t)mine;
     if constexpr (TOP) {
         int rank = 0;
-        if (i < n)
-#pragma unroll 4
-            for (int j = half; j < n; j += 2) rank += s.few[j] < mine;
-        rank += __shfl_xor(rank, 1);
-        if (i < n && half == 0 && rank < a.entries) {
+        team.each(n, [&](int j) { rank += s.few[j] < mine; });
+        rank = team.sum(rank);
+        if (speaks && rank < a.entries) {
             a.ids[(long long)r * a.entries + rank] = (int)id;
             a.values[(long long)r * a.entries + rank] = logit_of(key);
         }
-        for (int e = n + threadIdx.x; e < a.entries; e += THREADS) { a.ids[(long long)r * a.entries + e] = -1; a.values[(long long)r * a.entries + e] = -INFINITY; }
+        for (int e = n + threadIdx.x; e < a.entries; e += DECIDERS) { a.ids[(long long)r * a.entries + e] = -1; a.values[(long long)r * a.entries + e] = -INFINITY; }
         return true;
     }
     const u64 own = i < n ? row.mass(key) : 0;
-    if (i < n && half == 0) s.few_mass[i] = own;
+    if (speaks) s.few_mass[i] = own;
     __syncthreads();
     int rank = 0;
     u64 before = 0;
-    if (i < n)
-#pragma unroll 4
-        for (int j = half; j < n; j += 2) {
-            const bool less = s.few[j] < mine;
-            rank += less;
-            before += less ? s.few_mass[j] : 0;
-        }
-    rank += __shfl_xor(rank, 1);
-    before += __shfl_xor(before, 1);
+    team.each(n, [&](int j) {
+        const bool less = s.few[j] < mine;
+        rank += less;
+        before += less ? s.few_mass[j] : 0;
+    });
+    rank = team.sum(rank);
+    before = team.sum(before);
     bool kept = i < n && (row.k == 0 || rank < row.k);
     if (row.p < 1.f) {
-        if (row.k > 0) want = share_of(row.p, sum_of_all(kept && half == 0 ? own : (u64)0, s));
+        if (row.k > 0) want = share_of(row.p, sum_of_all(kept && speaks ? own : (u64)0, s));
         kept = kept && before < want;
     }
     if (row.m > 0.f) kept = kept && (rank == 0 || (key >= least && !(row.m > 1.f)));
-    const u64 sum = sum_of_all(kept && half == 0 ? own : (u64)0, s);
-    if (i < n && half == 0) s.few_mass[i] = kept ? own : 0;
+    const u64 sum = sum_of_all(kept && speaks ? own : (u64)0, s);
+    if (speaks) s.few_mass[i] = kept ? own : 0;
     __syncthreads();
     const u64 below = min((u64)(evenly(a.u[r]) * (double)sum), sum - 1);
     before = 0;
-    if (kept)
-#pragma unroll 4
-        for (int j = half; j < n; j += 2) before += (uint32_t)s.few[j] < id ? s.few_mass[j] : 0;
-    before += __shfl_xor(before, 1);
-    if (kept && half == 0 && before <= below && below < before + own) put_draw(a, r, row, id, logit_of(key), (double)sum / row.unit);
+    team.each(n, [&](int j) { before += (uint32_t)s.few[j] < id ? s.few_mass[j] : 0; });
+    before = team.sum(before);
+    if (kept && speaks && before <= below && below < before + own) put_draw(a, r, row, id, logit_of(key), (double)sum / row.unit);
     return true;
 }
 
 struct Found { int at; double before; };
 
-// The first of the values (N a thread, in the threads' order) up to which they add up to more than `want`; where rounding leaves none the last that is no zero. `before`: sum of the
+// The first of the values (PER a thread, in the threads' order) up to which they add up to more than `want`; where rounding leaves none the last that is no zero. `before`: sum of the
 // threads' before this one. Sums in 64 bits in a fixed order.
-template <int N, class S> __device__ __forceinline__ Found first_over(const double (&v)[N], double before, double want, S &s)
+template <class S> __device__ __forceinline__ Found first_over(const double (&v)[PER], double before, double want, S &s)
 {
     double run = before, found_at = before;
     uint32_t first = ANY, last = 0;
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
+    for (int e = 0; e < PER; ++e) {
         const double from = run;
         run += v[e];
         if (!(v[e] > 0)) continue;
-        const uint32_t i = threadIdx.x * N + e;
+        const uint32_t i = threadIdx.x * PER + e;
         last = i + 1;
         if (first != ANY) continue;
         found_at = from;                                  // (of the first that is over, or of the last)
@@ -506,29 +636,32 @@ template <int N, class S> __device__ __forceinline__ Found first_over(const doub
     if (threadIdx.x % 64 == 0) { atomicMin(&s.first, wave_first); atomicMax(&s.last, wave_last); }
     __syncthreads();
     const uint32_t at = s.first != ANY ? s.first : s.last - 1;
-    if (at / N == threadIdx.x) s.run = found_at;
+    if (at / PER == threadIdx.x) s.run = found_at;
     __syncthreads();
     return Found{(int)at, s.run};
 }
 
-// A draw from a row that nothing is cut from, which more than one workgroup has read in parts that are one piece each: the part by the parts' weights (two a thread), then the token in it
-template <class T, class S> __device__ __forceinline__ void draw_freely(const PickArgs &a, int r, const T *logits, const Row &row, const double (&parts)[2], S &s)
+// A draw from a row that nothing is cut from, which more than one workgroup has read in parts that are one piece each: the part by the parts' weights, then the token in it
+template <class T, class S> __device__ __forceinline__ void draw_freely(const PickArgs &a, int r, const T *logits, const Row &row, const double (&parts)[PER], S &s)
 {
-    double total, rest;
-    double before = sum_upto(parts[0] + parts[1], total, s) - (parts[0] + parts[1]);
+    double total, rest, sum = 0;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) sum += parts[e];
+    double before = sum_upto(sum, total, s) - sum;
     const double want = evenly(a.u[r]) * total;
     const Found part = first_over(parts, before, want, s);
-    float z[PART_STEPS];
-    double v[PART_STEPS], sum = 0;
-    const int first = part.at * PICK_PART + threadIdx.x * PART_STEPS;
+    float z[PER];
+    double v[PER];
+    const int first = part.at * PICK_PART + threadIdx.x * PER;
 #pragma unroll
-    for (int e = 0; e < PART_STEPS; ++e) z[e] = first + e < a.vocab ? wide(logits[first + e]) : -INFINITY;
+    for (int e = 0; e < PER; ++e) z[e] = first + e < a.vocab ? wide(logits[first + e]) : -INFINITY;
+    sum = 0;
 #pragma unroll
-    for (int e = 0; e < PART_STEPS; ++e) sum += v[e] = z[e] > -INFINITY ? row.weight(z[e]) : 0;
+    for (int e = 0; e < PER; ++e) sum += v[e] = z[e] > -INFINITY ? row.weight(z[e]) : 0;
     before = sum_upto(sum, rest, s) - sum;
     const Found token = first_over(v, before, want - part.before, s);
 #pragma unroll
-    for (int e = 0; e < PART_STEPS; ++e) if (token.at == (int)threadIdx.x * PART_STEPS + e) put_draw(a, r, row, first + e, z[e], total);
+    for (int e = 0; e < PER; ++e) if (token.at == (int)threadIdx.x * PER + e) put_draw(a, r, row, first + e, z[e], total);
 }
 
 // ------------------------------------------------------------------ the kernels
@@ -660,53 +793,61 @@ template <class T, bool TOP> __global__ __launch_bounds__(THREADS, 8) void parts
 
 // the parts' lists, `listed` a part, into a workgroup's pool: those of keys `least` and above
 template <int HELD> struct Lists {
-    uint2 v[HELD / THREADS];
+    uint2 v[HELD / DECIDERS];
     __device__ __forceinline__ void load(const PickArgs &a, int r, int parts)
     {
         const uint2 *const list = a.list + (long long)r * parts * a.listed;
         const uint32_t all = parts * a.listed;
 #pragma unroll
-        for (int e = 0; e < HELD / THREADS; ++e) {
-            const uint32_t i = e * THREADS + threadIdx.x;
+        for (int e = 0; e < HELD / DECIDERS; ++e) {
+            const uint32_t i = e * DECIDERS + threadIdx.x;
             v[e] = i < all ? list[i] : make_uint2(0, 0);
         }
     }
-    template <class S> __device__ __forceinline__ uint32_t hold(uint32_t least, S &s) const      // (s.n is zero, behind a barrier)
+    template <class S> __device__ __forceinline__ uint32_t hold(uint32_t least, S &s, uint32_t *lowest = nullptr) const      // (s.n is zero, behind a barrier)
     {
         int n = 0;
 #pragma unroll
-        for (int e = 0; e < HELD / THREADS; ++e) n += v[e].x && v[e].x >= least;
+        for (int e = 0; e < HELD / DECIDERS; ++e) n += v[e].x && v[e].x >= least;
         const int upto = wave_upto(n, Plus{});
         uint32_t at = 0;
         if (threadIdx.x % 64 == 63) at = atomicAdd(&s.n, (uint32_t)upto);
         at = last_lane(at) + upto - n;
+        if (lowest) {
+            uint32_t low = ANY;
 #pragma unroll
-        for (int e = 0; e < HELD / THREADS; ++e) if (v[e].x && v[e].x >= least) { s.key[at] = v[e].x; s.id[at++] = v[e].y; }
+            for (int e = 0; e < HELD / DECIDERS; ++e) low = v[e].x ? min(low, v[e].x) : low;
+            low = ~wave_max(~low);
+            if (threadIdx.x % 64 == 0) atomicMin(lowest, low);
+        }
+#pragma unroll
+        for (int e = 0; e < HELD / DECIDERS; ++e) if (v[e].x && v[e].x >= least) { s.key[at] = v[e].x; s.id[at++] = v[e].y; }
         __syncthreads();
         return s.n;
     }
 };
 
 // One workgroup a row. Bound by the latency of a few loads and of some twenty barriers.
-template <class T, bool TOP, bool WHOLE, int HELD> __global__ __launch_bounds__(THREADS) void decide_kernel(PickArgs a)
+template <class T, bool TOP, bool WHOLE, int HELD> __global__ __launch_bounds__(DECIDERS) void decide_kernel(PickArgs a)
 {
     using S = Shared<HELD, WHOLE>;
     __shared__ S s;
     const int r = blockIdx.x, vocab = a.vocab, parts = a.groups * WAVES;
     const T *const logits = (const T *)a.logits + (long long)r * a.stride;
     Row row = row_of<TOP>(a, r, s.powers);
-    if (threadIdx.x == 0) { s.top = 0; s.from = LOWEST; s.n = 0; }
+    if (threadIdx.x == 0) { s.top = 0; s.from = LOWEST; s.n = 0; s.least = ANY; }
     load_powers(s.powers);
     Pool<S> pool{s, LOWEST, (uint32_t)vocab};
     double weight = 0;
+    uint32_t low = LOWEST;
     if constexpr (WHOLE) {
         constexpr int N = 16 / sizeof(T);
         __syncthreads();
         uint32_t top = 0;
         if (vocab >= N) {
 #pragma unroll
-            for (int i = 0; i < HELD / THREADS / N; ++i) {
-                const int at = min((i * THREADS + (int)threadIdx.x) * N, vocab - N);      // (some twice, the same)
+            for (int i = 0; i < (HELD + DECIDERS * N - 1) / (DECIDERS * N); ++i) {
+                const int at = min((i * DECIDERS + (int)threadIdx.x) * N, vocab - N);      // (some twice, the same)
                 T v[N];
                 __builtin_memcpy(v, logits + at, 16);
 #pragma unroll
@@ -720,19 +861,25 @@ template <class T, bool TOP, bool WHOLE, int HELD> __global__ __launch_bounds__(
             top = key_of(wide(logits[threadIdx.x]));
             s.key[threadIdx.x] = top;
         }
+        // as many tokens as there are threads with tokens are not below the least of the threads' largest: few filters end below that
+        const uint32_t least = ~wave_max(top ? ~top : 0);
         top = wave_max(top);
-        if (threadIdx.x % 64 == 0) atomicMax(&s.top, top);
+        if (threadIdx.x % 64 == 0) { atomicMax(&s.top, top); atomicMin(&s.least, least); }
         __syncthreads();
         if (!s.top) { put_nothing(a, r, TOP); return; }
         row.relative_to(s.top);
+        if (vocab > FEW) low = s.least;
     } else {
-        PickHead head[2]{};
+        PickHead head[PER]{};
 #pragma unroll
-        for (int e = 0; e < 2; ++e) if ((int)threadIdx.x * 2 + e < parts) head[e] = a.head[(long long)r * parts + threadIdx.x * 2 + e];
+        for (int e = 0; e < PER; ++e) if ((int)threadIdx.x * PER + e < parts) head[e] = a.head[(long long)r * parts + threadIdx.x * PER + e];
         Lists<HELD> lists;
         if (row.cut) lists.load(a, r, parts);
         __syncthreads();
-        const uint32_t top = wave_max(max(head[0].top, head[1].top)), from = wave_max(max(head[0].from, head[1].from));
+        uint32_t top = 0, from = 0;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) { top = max(top, head[e].top); from = max(from, head[e].from); }
+        top = wave_max(top); from = wave_max(from);
         if (threadIdx.x % 64 == 0) { atomicMax(&s.top, top); atomicMax(&s.from, from); }
         __syncthreads();
         if (!s.top) { put_nothing(a, r, TOP); return; }
@@ -740,24 +887,22 @@ template <class T, bool TOP, bool WHOLE, int HELD> __global__ __launch_bounds__(
         pool.from = s.from;
         if constexpr (!TOP) {
             if (row.summed) {
-                double v[2];
+                double v[PER], sum = 0;
 #pragma unroll
-                for (int e = 0; e < 2; ++e) v[e] = head[e].top ? head[e].sum * row.weight(logit_of(head[e].top)) : 0;
+                for (int e = 0; e < PER; ++e) sum += v[e] = head[e].top ? head[e].sum * row.weight(logit_of(head[e].top)) : 0;
                 if (!row.cut) {
                     draw_freely(a, r, logits, row, v, s);
                     return;
                 }
-                weight = sum_of_all(v[0] + v[1], s);
+                weight = sum_of_all(sum, s);
             }
         }
         pool.n = lists.hold(pool.from, s);
     }
     First first{};
-    if (among_few<TOP>(pool, a, r, row, weight, first, s)) return;
-    if constexpr (TOP) {
-        if (list_top(pool, a, r, row, first, s)) return;
-    } else {
-        if (draw(pool, a, r, logits, row, weight, first, s)) return;
+    if (among_few<TOP>(pool, a, r, row, weight, low, first, s)) return;
+    if (search<TOP>(pool, a, r, row, weight, first, s)) return;
+    if constexpr (!TOP) {
         if (!WHOLE && a.queue && row.k == 0 && row.top < INFINITY && pool.from <= row.top_key) {
             if (threadIdx.x == 0) {
                 PickSearch q{};
@@ -775,11 +920,7 @@ template <class T, bool TOP, bool WHOLE, int HELD> __global__ __launch_bounds__(
             return;
         }
     }
-    if constexpr (!WHOLE) {
-        const Streamed<T> whole{logits, vocab};
-        if constexpr (TOP) list_top(whole, a, r, row, First{}, s);
-        else draw(whole, a, r, logits, row, weight, First{}, s);
-    }
+    if constexpr (!WHOLE) whole_row<T, TOP>(a, r, row, s);
 }
 
 // ------------------------------------------------------------------ rows that are searched
@@ -787,13 +928,15 @@ template <class T, bool TOP, bool WHOLE, int HELD> __global__ __launch_bounds__(
 // The step of a logit below `from`; larger logits are in no later step
 __device__ __forceinline__ int step_of(float z, const PickSearch &q) { return (int)fminf((q.from - z) * q.scale, (float)PICK_STEPS); }
 
+constexpr int STEP_COPIES = THREADS / PICK_STEPS;      // of the histogram, for neighbouring lanes: even tokens meet in few steps
+
 // Masses by steps below `from`, in the last place that of everything from it on; what is below all steps is left out
 template <class T> __global__ __launch_bounds__(THREADS, 8) void steps_kernel(PickArgs a)
 {
     __shared__ float s_z[WAVES][EACH / 4][64][4];
     __shared__ uint2 s_powers[32];
-    __shared__ u64 step[PICK_STEPS];
-    static_assert(PICK_STEPS == THREADS);
+    __shared__ u64 step[STEP_COPIES][PICK_STEPS + 1];
+    static_assert(STEP_COPIES * PICK_STEPS == THREADS);
     load_powers(s_powers);
     const uint32_t items = a.queue[0] * a.groups;
 #pragma unroll 1
@@ -801,7 +944,7 @@ template <class T> __global__ __launch_bounds__(THREADS, 8) void steps_kernel(Pi
         const int r = a.queue[1 + item / a.groups], group = item % a.groups;
         const PickSearch q = a.search[r];
         if (q.stage != PICK_STEP) continue;
-        step[threadIdx.x] = 0;
+        step[threadIdx.x / PICK_STEPS][threadIdx.x % PICK_STEPS] = 0;
         Row row = row_of<false>(a, r, s_powers);
         row.relative_to(q.top_key);
         using P = Part<T>;
@@ -814,12 +957,18 @@ template <class T> __global__ __launch_bounds__(THREADS, 8) void steps_kernel(Pi
             if (z == -INFINITY || at >= PICK_STEPS - 1) return;
             const u64 m = row.in_units(row.finite_weight(z));
             if (at < 0) above += m;
-            else atomicAdd(&step[at], m);
+            else atomicAdd(&step[threadIdx.x % STEP_COPIES][at], m);
         });
         above = wave_sum(above);
-        if (threadIdx.x % 64 == 0) atomicAdd(&step[PICK_STEPS - 1], above);
+        if (threadIdx.x % 64 == 0) atomicAdd(&step[0][PICK_STEPS - 1], above);
         __syncthreads();
-        a.steps[((long long)r * a.groups + group) * PICK_STEPS + threadIdx.x] = step[threadIdx.x];
+        if (threadIdx.x < PICK_STEPS) {
+            u64 sum = 0;
+#pragma unroll
+            for (int c = 0; c < STEP_COPIES; ++c) sum += step[c][threadIdx.x];
+            a.steps[((long long)r * a.groups + group) * PICK_STEPS + threadIdx.x] = sum;
+        }
+        __syncthreads();
     }
 }
 
@@ -828,7 +977,7 @@ template <class T> __global__ __launch_bounds__(THREADS, 8) void place_kernel(Pi
 {
     __shared__ float s_z[WAVES][EACH / 4][64][4];
     __shared__ uint2 s_powers[32];
-    __shared__ u64 s_part[WAVES];
+    __shared__ u64 s_sum[STEP_COPIES][PICK_STEPS];
     __shared__ int s_step;
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, parts = a.groups * WAVES;
     load_powers(s_powers);
@@ -845,20 +994,35 @@ template <class T> __global__ __launch_bounds__(THREADS, 8) void place_kernel(Pi
         int step = PICK_STEPS;                    // none
         uint32_t stage = q.stage;
         if (stage == PICK_STEP) {
+            const int at = threadIdx.x % PICK_STEPS, quarter = threadIdx.x / PICK_STEPS;
+            const u64 *const steps = a.steps + (long long)r * a.groups * PICK_STEPS + at;
             u64 sum = 0;
-            const u64 *const steps = a.steps + (long long)r * a.groups * PICK_STEPS + threadIdx.x;
 #pragma unroll 4
-            for (int g = 0; g < a.groups; ++g) sum += steps[g * PICK_STEPS];
-            // (what is above all steps, which the last place holds, comes before them)
-            u64 upto = wave_upto(threadIdx.x == PICK_STEPS - 1 ? 0 : sum, Plus{});
+            for (int g = quarter; g < a.groups; g += STEP_COPIES) sum += steps[g * PICK_STEPS];
             __syncthreads();
+            s_sum[quarter][at] = sum;
             if (threadIdx.x == 0) s_step = PICK_STEPS;
-            if (lane == 63) s_part[wave] = wave == WAVES - 1 ? sum : upto;
             __syncthreads();
-            upto += s_part[WAVES - 1];
+            if (wave == 0) {
+                // (what is above all steps, which the last place holds, comes before them)
+                u64 v[PICK_STEPS / 64];
 #pragma unroll
-            for (int w = 0; w < WAVES - 1; ++w) upto += w < wave ? s_part[w] : 0;
-            if (threadIdx.x < PICK_STEPS - 1 && upto - sum < q.want && q.want <= upto) s_step = threadIdx.x;
+                for (int e = 0; e < PICK_STEPS / 64; ++e) {
+                    v[e] = 0;
+#pragma unroll
+                    for (int c = 0; c < STEP_COPIES; ++c) v[e] += s_sum[c][lane * (PICK_STEPS / 64) + e];
+                }
+                u64 run = last_lane(v[PICK_STEPS / 64 - 1]), mine = 0;
+                if (lane == 63) v[PICK_STEPS / 64 - 1] = 0;
+#pragma unroll
+                for (int e = 0; e < PICK_STEPS / 64; ++e) mine += v[e];
+                run += wave_upto(mine, Plus{}) - mine;
+#pragma unroll
+                for (int e = 0; e < PICK_STEPS / 64; ++e) {
+                    if (run < q.want && q.want <= run + v[e]) s_step = lane * (PICK_STEPS / 64) + e;
+                    run += v[e];
+                }
+            }
             __syncthreads();
             step = s_step;
             if (step == PICK_STEPS) stage = PICK_WHOLE;
@@ -887,7 +1051,7 @@ template <class T> __global__ __launch_bounds__(THREADS, 8) void place_kernel(Pi
 }
 
 // The place in the step, and the draw: the part by the parts' masses, then the token in it
-template <class T> __global__ __launch_bounds__(THREADS) void finish_kernel(PickArgs a)
+template <class T> __global__ __launch_bounds__(DECIDERS) void finish_kernel(PickArgs a)
 {
     constexpr int HELD = PICK_LISTED;
     __shared__ Shared<HELD> s;
@@ -902,14 +1066,16 @@ template <class T> __global__ __launch_bounds__(THREADS) void finish_kernel(Pick
         Row row = row_of<false>(a, r, s.powers);
         row.relative_to(q.top_key);
         __syncthreads();
-        if (threadIdx.x == 0) s.n = 0;
+        if (threadIdx.x == 0) { s.n = 0; s.from = ANY; }
         bool whole = q.found == PICK_WHOLE;
+        Lists<HELD> lists;
+        if (q.found == PICK_STEP) lists.load(a, r, parts);
         u64 above = 0;
         if (!whole) {
             u64 over = 0;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int w = threadIdx.x * 2 + e;
+            for (int e = 0; e < PER; ++e) {
+                const int w = threadIdx.x * PER + e;
                 PickHead head{};
                 if (w < parts) head = a.head[(long long)r * parts + w];
                 s.mass[w] = head.mass;
@@ -920,50 +1086,56 @@ template <class T> __global__ __launch_bounds__(THREADS) void finish_kernel(Pick
             above = sum_of_all(above, s);
         }
         if (whole) {
-            const Streamed<T> all{logits, vocab};
-            draw(all, a, r, logits, row, 0.0, First{}, s);
+            whole_row<T, false>(a, r, row, s);
             continue;
         }
-        Kept kept{q.least, ANY};
+        Kept kept{q.least, ANY, 0};
         if (q.found == PICK_STEP) {
-            Lists<HELD> lists;
-            lists.load(a, r, parts);
-            const Pool<Shared<HELD>> pool{s, LOWEST, lists.hold(LOWEST, s)};
-            const Border b = find_border([&](auto add) { pool.each([&](uint32_t key, uint32_t) { add(q.top_key - key, [&] { return row.mass(key); }); }); }, bits_of(q.top_key - LOWEST),
-                                         q.want - above, s);
-            kept.key = q.top_key - b.place;
+            const Pool<Shared<HELD>> pool{s, LOWEST, lists.hold(LOWEST, s, &s.from)};      // (and the smallest of them)
+            const uint32_t high = key_of(q.from);
+            const auto mass = [&](uint32_t key) { return row.in_units(row.finite_weight(logit_of(key))); };
+            const Border b = find_border([&](auto in, auto put) {
+                pool.tally([&](uint32_t key, uint32_t) { return in(high - key); }, mass, [&](uint32_t key, uint32_t, u64 m) { put(high - key, m); });
+            }, bits_of(high - s.from), q.want - above, s);
+            kept.key = high - b.place;
             const u64 one = row.mass(kept.key), need = (q.want - above - b.before + one - 1) / one;
-            u64 ties = need < b.at / one ? need : 0;
+            const u64 equal = b.at / one;
+            u64 ties = need < equal ? need : 0;
             if (q.least > kept.key) { kept.key = q.least; ties = 0; }
-            if (ties) kept.last = find_border([&](auto add) { pool.each([&](uint32_t key, uint32_t id) { if (key == kept.key) add(id, [] { return 1; }); }); }, bits_of(vocab - 1), ties, s).place;
+            if (ties) kept.last = find_border([&](auto in, auto put) {
+                pool.tally([&](uint32_t key, uint32_t id) { return (key == kept.key) & in(id); }, [](uint32_t) { return 1; }, [&](uint32_t, uint32_t id, u64 m) { put(id, m); });
+            }, bits_of(vocab - 1), ties, s, Border{true, 0, 0, 0}, equal <= FEW_PLACES).place;
             __syncthreads();
-            pool.each([&](uint32_t key, uint32_t id) { if (kept.has(key, id)) atomicAdd(&s.mass[id / PICK_PART], row.mass(key)); });
+            pool.tally([&](uint32_t key, uint32_t id) { return kept.has(key, id); }, mass, [&](uint32_t, uint32_t id, u64 m) { atomicAdd(&s.mass[id / PICK_PART], m); });
             __syncthreads();
         }
-        u64 total, rest;
-        const u64 m[2] = {s.mass[threadIdx.x * 2], s.mass[threadIdx.x * 2 + 1]};
-        u64 run = sum_upto(m[0] + m[1], total, s) - m[0] - m[1];
+        // the part, then the token in it
+        u64 total, sum = 0, part[PER];
+#pragma unroll
+        for (int e = 0; e < PER; ++e) sum += part[e] = s.mass[threadIdx.x * PER + e];
+        u64 run = sum_upto(sum, total, s) - sum;
         const u64 below = min((u64)(evenly(a.u[r]) * (double)total), total - 1);
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            if (run <= below && below < run + m[e]) { s.place = threadIdx.x * 2 + e; s.before = run; }
-            run += m[e];
+        for (int e = 0; e < PER; ++e) {
+            if (run <= below && below < run + part[e]) { s.place = threadIdx.x * PER + e; s.before = run; }
+            run += part[e];
         }
         __syncthreads();
-        const int first = s.place * PICK_PART + threadIdx.x * PART_STEPS;
+        const int first = s.place * PICK_PART + threadIdx.x * PER;
         const u64 left = below - s.before;
-        float z[PART_STEPS];
-        u64 v[PART_STEPS], sum = 0;
+        float z[PER];
+        u64 v[PER], rest;
 #pragma unroll
-        for (int e = 0; e < PART_STEPS; ++e) z[e] = first + e < vocab ? wide(logits[first + e]) : -INFINITY;
+        for (int e = 0; e < PER; ++e) z[e] = first + e < vocab ? wide(logits[first + e]) : -INFINITY;
+        sum = 0;
 #pragma unroll
-        for (int e = 0; e < PART_STEPS; ++e) {
+        for (int e = 0; e < PER; ++e) {
             const uint32_t key = key_of(z[e]);
-            sum += v[e] = key && kept.has(key, first + e) ? row.mass(key) : 0;
+            sum += v[e] = key && kept.has(key, first + e) ? row.in_units(row.finite_weight(z[e])) : 0;
         }
         run = sum_upto(sum, rest, s) - sum;
 #pragma unroll
-        for (int e = 0; e < PART_STEPS; ++e) {
+        for (int e = 0; e < PER; ++e) {
             if (run <= left && left < run + v[e]) put_draw(a, r, row, first + e, z[e], (double)total / row.unit);
             run += v[e];
         }
@@ -974,20 +1146,20 @@ template <class T, bool TOP> void launch_parts(hipStream_t s, const PickArgs &a)
 {
     const unsigned all = (unsigned)a.rows * a.groups;
     hipLaunchKernelGGL((parts_kernel<T, TOP>), dim3(all), dim3(THREADS), 0, s, a);
-    if (a.groups * WAVES * a.listed <= 4096) hipLaunchKernelGGL((decide_kernel<T, TOP, false, 4096>), dim3(a.rows), dim3(THREADS), 0, s, a);
-    else hipLaunchKernelGGL((decide_kernel<T, TOP, false, PICK_LISTED>), dim3(a.rows), dim3(THREADS), 0, s, a);
+    if (a.groups * WAVES * a.listed <= 4096) hipLaunchKernelGGL((decide_kernel<T, TOP, false, 4096>), dim3(a.rows), dim3(DECIDERS), 0, s, a);
+    else hipLaunchKernelGGL((decide_kernel<T, TOP, false, PICK_LISTED>), dim3(a.rows), dim3(DECIDERS), 0, s, a);
     if constexpr (!TOP) {
         if (!a.queue) return;
         // rows of the queue, which the host does not know: as many workgroups as run at once, which are soon gone where it is empty
         hipLaunchKernelGGL(steps_kernel<T>, dim3(std::min(all, 1024u)), dim3(THREADS), 0, s, a);
         hipLaunchKernelGGL(place_kernel<T>, dim3(std::min(all, 1024u)), dim3(THREADS), 0, s, a);
-        hipLaunchKernelGGL(finish_kernel<T>, dim3(std::min(a.rows, 256)), dim3(THREADS), 0, s, a);
+        hipLaunchKernelGGL(finish_kernel<T>, dim3(std::min(a.rows, 256)), dim3(DECIDERS), 0, s, a);
     }
 }
 
 template <class T, bool TOP> void launch(hipStream_t s, const PickArgs &a)
 {
-    const dim3 rows(a.rows), threads(THREADS);
+    const dim3 rows(a.rows), threads(DECIDERS);
     if (!a.head) {
         if (a.vocab <= 4096) hipLaunchKernelGGL((decide_kernel<T, TOP, true, 4096>), rows, threads, 0, s, a);
         else hipLaunchKernelGGL((decide_kernel<T, TOP, true, 8192>), rows, threads, 0, s, a);

@@ -45,7 +45,7 @@ class Sampler:
             raise TokrouteError(tokroute.ERR_SHAPE, "tr_pick_workspace_bytes", "(sizes or types not supported)")
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
         self.device = self.workspace.device
-        self._home = torch.cuda.current_stream(self.device)
+        self._home = torch.cuda.current_stream(self.device).cuda_stream
 
     # -- helpers
     def _rows(self, logits):
@@ -53,24 +53,20 @@ class Sampler:
         if not (isinstance(logits, torch.Tensor) and logits.dtype == self.dtype and logits.device == self.device and logits.dim() == 2 and logits.shape[1] == v
                 and (logits.stride(1) == 1 or v == 1)):
             raise ValueError(f"logits: a {self.dtype} matrix of {v} columns with contiguous rows on {self.device}")
-        n = logits.shape[0]
-        return tr_pick_rows(logits.data_ptr(), max(logits.stride(0), v) if n <= 1 else logits.stride(0), n)
+        n, stride = logits.shape[0], logits.stride(0)
+        return tr_pick_rows(logits.data_ptr(), max(stride, v) if n <= 1 else stride, n)
 
     def _flat(self, t, what, dtype, shape):
-        if not (isinstance(t, torch.Tensor) and t.dtype == dtype and t.device == self.device and tuple(t.shape) == shape and t.is_contiguous()):
+        if not (isinstance(t, torch.Tensor) and t.dtype == dtype and t.device == self.device and t.shape == shape and t.is_contiguous()):
             raise ValueError(f"{what}: a contiguous {dtype} tensor of shape {shape} on {self.device}")
         return t.data_ptr()
 
-    def _out(self, t, what, dtype, shape):
-        t = torch.empty(shape, dtype=dtype, device=self.device) if t is None else t
-        return t, self._flat(t, what, dtype, shape)
-
     def _call(self, fn, what, *args):
-        s = torch.cuda.current_stream(self.device)
-        if s != self._home:
-            self.workspace.record_stream(s)    # its memory is not handed on while work of that stream may use it
-        with torch.cuda.device(self.device):   # a default stream is the current device's
-            rc = fn(C.byref(self.cfg), self.workspace.data_ptr(), self.workspace.numel(), s.cuda_stream, *args)
+        stream = tokroute.raw_stream(self.device.index)
+        if stream != self._home:
+            self.workspace.record_stream(torch.cuda.current_stream(self.device))    # its memory is not handed on while work of that stream may use it
+        with tokroute.on_device(self.device.index):      # a default stream is the current device's
+            rc = fn(C.byref(self.cfg), self.workspace.data_ptr(), self.workspace.numel(), stream, *args)
         if rc:
             raise TokrouteError(rc, what)
 
@@ -80,22 +76,23 @@ class Sampler:
 
         temperature, top_p, min_p (float32 [n]) and top_k (int32 [n]) are numbers or device tensors with a value a row. token and logprob may be given (written over)."""
         rows = self._rows(logits)
-        n = rows.rows
-        how = tr_sample_how(self._flat(u, "u", torch.float32, (n,)))
+        shape = (rows.rows,)
+        how = tr_sample_how(self._flat(u, "u", torch.float32, shape), None, None, None, None, 1.0, 0, 1.0, 0.0)
         for name, value, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
             if isinstance(value, torch.Tensor):
-                setattr(how, name + "s", self._flat(value, name, dtype, (n,)))
+                setattr(how, name + "s", self._flat(value, name, dtype, shape))
             else:
                 setattr(how, name, value)
-        token, token_at = self._out(token, "token", torch.int32, (n,))
-        logprob, logprob_at = self._out(logprob, "logprob", torch.float32, (n,))
-        self._call(self.lib.tr_sample, "tr_sample", C.byref(rows), C.byref(how), token_at, logprob_at)
+        token = torch.empty(shape, dtype=torch.int32, device=self.device) if token is None else token
+        logprob = torch.empty(shape, dtype=torch.float32, device=self.device) if logprob is None else logprob
+        self._call(self.lib.tr_sample, "tr_sample", C.byref(rows), C.byref(how), self._flat(token, "token", torch.int32, shape), self._flat(logprob, "logprob", torch.float32, shape))
         return token, logprob
 
     def top(self, logits, entries: int, ids=None, values=None):
         """(ids int32 [n][entries], values float32 [n][entries]): the largest logits of each row, in falling order, equal ones by id; -1 and -inf where a row has fewer."""
         rows = self._rows(logits)
-        ids, ids_at = self._out(ids, "ids", torch.int32, (rows.rows, entries))
-        values, values_at = self._out(values, "values", torch.float32, (rows.rows, entries))
-        self._call(self.lib.tr_top, "tr_top", C.byref(rows), entries, ids_at, values_at)
+        shape = (rows.rows, entries)
+        ids = torch.empty(shape, dtype=torch.int32, device=self.device) if ids is None else ids
+        values = torch.empty(shape, dtype=torch.float32, device=self.device) if values is None else values
+        self._call(self.lib.tr_top, "tr_top", C.byref(rows), entries, self._flat(ids, "ids", torch.int32, shape), self._flat(values, "values", torch.float32, shape))
         return ids, values

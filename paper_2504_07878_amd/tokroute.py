@@ -6,6 +6,7 @@ fallback: if the library is missing or no GPU is present, calls raise.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 
@@ -125,6 +126,19 @@ def load_library():
         L.tr_last_error.argtypes = [vp]; L.tr_last_error.restype = C.c_char_p
         _lib = L
     return _lib
+
+
+def raw_stream(index: int) -> int:
+    """Handle of the current stream of a device (0.1 us; `torch.cuda.current_stream` makes an object first, 1.9 us)."""
+    return torch._C._cuda_getCurrentRawStream(index)
+
+
+_HERE = contextlib.nullcontext()
+
+
+def on_device(index: int):
+    """Makes a device current, where it is not (which `torch.cuda.device` finds out in 1.3 us, this in 0.2)."""
+    return _HERE if torch.cuda.current_device() == index else torch.cuda.device(index)
 
 
 class TokrouteError(RuntimeError):
