@@ -10,7 +10,7 @@ from __future__ import annotations
 import numpy as np
 import torch
 
-from . import losses
+from . import clipping, losses, sampling
 from .tokroute import POST_FINAL_NORM
 
 
@@ -24,9 +24,12 @@ def collect(slm, llm, prompts, tokens, top: int = 16):
         raise ValueError("the small model exposes hidden rows before the final norm: its LM head does not multiply them")
     slots = list(range(len(prompts)))
     keep = ([], [], [], [])
+    vocab = llm.shape["vocab"]
+    listed = top <= sampling.MOST_ENTRIES and vocab <= sampling.MOST_VOCAB      # (more entries than the losses take are listed by PyTorch)
+    sampler = sampling.Sampler(len(prompts), vocab, device=llm.device) if listed else None
 
     def take(small, large, targets):
-        value, index = large.logits.topk(top, 1)
+        index, value = sampler.top(large.logits, top) if listed else large.logits.topk(top, 1)[::-1]
         for to, x in zip(keep, (small.hidden, index.int(), value, torch.from_numpy(np.ascontiguousarray(targets, dtype=np.int32)).to(value.device))):
             to.append(x)
 
@@ -36,13 +39,14 @@ def collect(slm, llm, prompts, tokens, top: int = 16):
     return tuple(torch.cat(x) for x in keep)
 
 
-def adapt_head(head, hidden, ids, teacher, targets, steps: int = 20, rate: float = None, share: float = 0.5, temperature: float = 2.0):
+def adapt_head(head, hidden, ids, teacher, targets, steps: int = 20, rate: float = None, share: float = 0.5, temperature: float = 2.0, max_norm: float = None):
     """Gradient descent on the LM head [vocab][d] (float32 or bfloat16): `share` of the loss is distillation, the rest cross entropy, both means over the rows that count.
 
     hidden: float32 as `collect` gives them, or bfloat16, with which the gradients over a bfloat16 head run on bf16 matrix instructions, several times as fast.
     rate: None takes 1 / (mean |hidden|^2 / 2), each loss's mean over its own rows that count, by its share: the inverse of a bound on the curvature of the loss in the head (a softmax's second
     derivative is at most 1/2; T^2 makes up for 1/T twice), with which every step of a float32 head goes down (a bfloat16 head's too, but for its rounding). Rows that do not count for a loss (as
-    the losses have it) have no part in any of this, whatever they hold; nor have targets past the head's vocabulary, tokens that only the large model has. Returns (new head in the head's type, losses of the steps as a list of floats). Updates are kept in fp32.
+    the losses have it) have no part in any of this, whatever they hold; nor have targets past the head's vocabulary, tokens that only the large model has. max_norm: a longer gradient is scaled to that
+    length (rows that say something else than the rest then move the head no further than others). Returns (new head in the head's type, losses of the steps as a list of floats). Updates are kept in fp32.
     """
     head, hidden = head.detach(), hidden.detach()          # (steps of its own, whatever graph they come from)
     plan = losses.VocabLoss(hidden.shape[0], head.shape[1], head.shape[0], hidden.dtype, head.dtype, max_entries=ids.shape[1], device=head.device)
@@ -55,11 +59,14 @@ def adapt_head(head, hidden, ids, teacher, targets, steps: int = 20, rate: float
         mean_ce, mean_kd = (float(square.where(on, torch.zeros_like(square)).sum()) / n for on, n in ((count_ce, n_ce), (count_kd, n_kd)))
         curvature = (share * mean_kd + (1 - share) * mean_ce) / 2
         rate = 1.0 / curvature if curvature else 0.0        # (no row that counts, or rows of zeros: no gradient either)
+    clipper = None if max_norm is None else clipping.Clipper(head.device)
     for _ in range(steps):
         w = master.to(head.dtype, copy=True).requires_grad_()
         with torch.enable_grad():
             loss = share / n_kd * losses.distill(plan, hidden, w, ids, teacher, temperature).sum() + (1 - share) / n_ce * losses.cross_entropy(plan, hidden, w, targets).sum()
         loss.backward()
+        if clipper is not None:
+            clipper.clip([w.grad], max_norm)
         master -= rate * w.grad.float()
         value.append(loss.detach())
     return master.to(head.dtype), torch.stack(value).tolist() if value else []

@@ -7,16 +7,50 @@ request (Figure 2) never recompute a prefix (the prototype of Section 4.1 has no
 
 This module is host control flow only: every tensor operation runs in the library's kernels, called through the C ABI
 binding. One device-to-host copy of the flags and tokens per step decides which sequences call the large model.
+
+Tokens are greedy, or drawn (`sampling.Draw`) from given random numbers, one for every position of every sequence: the same numbers give the same
+draws whatever the schedule. The router's flags do not depend on it.
 """
 from __future__ import annotations
+
+from dataclasses import asdict
 
 import numpy as np
 
 NEEDED = ("token", "flag")     # all the host loop reads back per step: 8 bytes per sequence
 
 
-def generate(slm, llm, prompts, max_new: int):
-    """Greedy joint decoding of len(prompts) sequences (slot b of both models serves sequence b).
+class _Tokens:
+    """What becomes of a call's outputs: nothing where tokens are greedy, drawn tokens in the greedy ones' place otherwise. vocab: ids from it on are drawn by nobody."""
+
+    def __init__(self, model, rows, vocab, draw, numbers):
+        self.wanted, self.vocab = draw is not None, vocab
+        if self.wanted:
+            from . import sampling
+            self.sampler, self.draw, self.numbers = sampling.Sampler(rows, vocab, device=model.device), asdict(draw), numbers
+
+    def __call__(self, out, sequences, positions):
+        """Row i of the outputs is sequences[i]'s token at positions[i]."""
+        if self.wanted and self.numbers.shape[1]:
+            self.sampler.sample(out.logits[:, :self.vocab], self.numbers[sequences, positions], token=out.token, **self.draw)
+        return out
+
+
+def _choosers(slm, llm, rows, max_new, draw, numbers):
+    """One for each model; the large one's padding past the small one's vocabulary is not drawn."""
+    if draw is None:
+        return _Tokens(slm, rows, 0, None, None), _Tokens(llm, rows, 0, None, None)
+    numbers = np.asarray(numbers, dtype=np.float32)
+    if numbers.shape != (rows, max_new):
+        raise ValueError(f"numbers: one for every sequence and new token, [{rows}][{max_new}]")
+    import torch
+    numbers = torch.from_numpy(numbers.copy()).to(slm.device)
+    v = slm.shape["vocab"]
+    return _Tokens(slm, rows, v, draw, numbers), _Tokens(llm, rows, min(v, llm.shape["vocab"]), draw, numbers)
+
+
+def generate(slm, llm, prompts, max_new: int, draw=None, numbers=None):
+    """Joint decoding of len(prompts) sequences (slot b of both models serves sequence b), greedy or, with a `sampling.Draw`, drawn from numbers [B][max_new] in [0, 1).
 
     slm: tokroute.Model with a router; llm: tokroute.Model of the large model (its own outputs are used, its router
     fields ignored). Returns (tokens int32 [B][max_new], routed bool [B][max_new]): routed[b][t] says the large model
@@ -28,18 +62,19 @@ def generate(slm, llm, prompts, max_new: int):
     llm_len = [0] * B                      # tokens of seq[b] the large model's cache holds
     tokens = np.zeros((B, max_new), np.int32)
     routed = np.zeros((B, max_new), bool)
-    out = slm.prefill(slots, prompts).cpu(NEEDED)
+    small, large = _choosers(slm, llm, B, max_new, draw, numbers)
+    out = small(slm.prefill(slots, prompts, want_logits=small.wanted), slots, [0] * B).cpu(NEEDED)
     for t in range(max_new):
         tok = out.token.astype(np.int32).copy()
         flagged = [b for b in slots if out.flag[b]]
         first = [b for b in flagged if llm_len[b] == 0]
         later = [b for b in flagged if llm_len[b] > 0]
         if first:
-            lo = llm.prefill(first, [seq[b] for b in first]).cpu(("token",))
+            lo = large(llm.prefill(first, [seq[b] for b in first], want_logits=large.wanted), first, [t] * len(first)).cpu(("token",))
             for i, b in enumerate(first):
                 tok[b] = lo.token[i]
         if later:
-            lo = llm.extend(later, [seq[b][llm_len[b]:] for b in later]).cpu(("token",))
+            lo = large(llm.extend(later, [seq[b][llm_len[b]:] for b in later], want_logits=large.wanted), later, [t] * len(later)).cpu(("token",))
             for i, b in enumerate(later):
                 tok[b] = lo.token[i]
         for b in flagged:
@@ -49,11 +84,11 @@ def generate(slm, llm, prompts, max_new: int):
             seq[b].append(int(tok[b]))
         tokens[:, t] = tok
         if t + 1 < max_new:
-            out = slm.decode_step(slots, tok).cpu(NEEDED)
+            out = small(slm.decode_step(slots, tok, want_logits=small.wanted), slots, [t + 1] * B).cpu(NEEDED)
     return tokens, routed
 
 
-def generate_overlapped(slm, llm, prompts, max_new: int):
+def generate_overlapped(slm, llm, prompts, max_new: int, draw=None, numbers=None):
     """The same decoding as `generate`, sequence by sequence, scheduled for throughput: a flagged sequence waits for the
     large model while the others keep decoding.
 
@@ -93,10 +128,11 @@ def generate_overlapped(slm, llm, prompts, max_new: int):
             else:
                 emit(b, out.token[i], False)
 
+    small, large = _choosers(slm, llm, B, max_new, draw, numbers)
     start, was_shared = torch.cuda.current_stream(), slm.shared
     s_small.wait_stream(start); s_large.wait_stream(start)
     with torch.cuda.stream(s_small):
-        take(list(range(B)), slm.prefill(list(range(B)), prompts).cpu(NEEDED, stream_only=True))
+        take(list(range(B)), small(slm.prefill(list(range(B)), prompts, want_logits=small.wanted), list(range(B)), [0] * B).cpu(NEEDED, stream_only=True))
     while inflight or pending or any(running):
         if inflight and (inflight[2].query() or not any(running)):
             bs, _, ev = inflight
@@ -111,10 +147,10 @@ def generate_overlapped(slm, llm, prompts, max_new: int):
             keep = []
             with torch.cuda.stream(s_large):
                 if first:
-                    keep.append(llm.prefill(first, [seq[b] for b in first]))
+                    keep.append(large(llm.prefill(first, [seq[b] for b in first], want_logits=large.wanted), first, [done[b] for b in first]))
                     host_tok[:len(first)].copy_(keep[-1].token[:len(first)], non_blocking=True)
                 if later:
-                    keep.append(llm.extend(later, [seq[b][llm_len[b]:] for b in later]))
+                    keep.append(large(llm.extend(later, [seq[b][llm_len[b]:] for b in later], want_logits=large.wanted), later, [done[b] for b in later]))
                     host_tok[len(first):len(first) + len(later)].copy_(keep[-1].token[:len(later)], non_blocking=True)
                 ev = torch.cuda.Event()
                 ev.record(s_large)
@@ -124,7 +160,7 @@ def generate_overlapped(slm, llm, prompts, max_new: int):
         if run:
             slm.set_shared(was_shared or inflight is not None)
             with torch.cuda.stream(s_small):
-                take(run, slm.decode_step(run, next_tok[run]).cpu(NEEDED, stream_only=True))
+                take(run, small(slm.decode_step(run, next_tok[run], want_logits=small.wanted), run, [done[b] for b in run]).cpu(NEEDED, stream_only=True))
     slm.set_shared(was_shared)
     start.wait_stream(s_small); start.wait_stream(s_large)
     return tokens, routed

@@ -13,6 +13,8 @@ import torch
 from . import tokroute
 from .tokroute import TokrouteError, tr_pick_config, tr_pick_rows, tr_sample_how
 
+MOST_ENTRIES, MOST_VOCAB = 1024, 1 << 20     # that tr_top lists, and that the calls take
+
 _DTYPES = {torch.float32: tokroute.F32, torch.bfloat16: tokroute.BF16}
 
 

@@ -60,3 +60,20 @@ def check_draw(z, u, t, k, p, m, token, logprob):
     before, upto = w[:i].sum() / total, w[:i + 1].sum() / total
     want = math.log(w[i] / total)
     return before - eps <= u and (u <= upto + eps) and abs(logprob - want) <= 2.0 ** -24 * abs(want) + 2 * eps
+
+
+def near_draw(z, u, t, k, p, m, token, slack):
+    """Whether a token is the draw from logits that make shares differ by a part `slack` of themselves: one that is kept, or next to the last that is, whose stretch is at most `slack` from u
+    (sums up to it differ by that part; what is or is not kept at the border makes as much)."""
+    kept, w = kept_of(z, t, k, p, m)
+    order = order_of(z)
+    more = order[:len(kept) + 2]                     # the border may lie a token further on
+    weights = np.exp(logs_of(z, more, t))
+    for last in {max(1, len(kept) - 1), len(kept), min(len(kept) + 1, len(order))}:
+        by_id = np.argsort(more[:last])
+        ids, share = more[:last][by_id], weights[:last][by_id] / weights[:last].sum()
+        upto = np.cumsum(share)
+        at = np.flatnonzero(ids == token)
+        if len(at) and upto[at[0]] - share[at[0]] - slack <= u <= upto[at[0]] + slack:
+            return True
+    return False

@@ -1,0 +1,98 @@
+"""Sequences drawn by both models, the large one's largest logits around them, and the small one's head fitted to them with clipped gradients: the run that tokens from logits, the losses and
+clipping are for."""
+import numpy as np
+import pytest
+import torch
+
+import picks
+
+pytestmark = pytest.mark.gpu
+SEED, B, NEW = 7878, 5, 14
+
+
+@pytest.fixture(scope="module")
+def models():
+    from paper_2504_07878_amd import synth, tokroute
+    s = synth.TINY.with_(threshold=0.5)
+    big = synth.TINY.with_(name="tiny-large", n_layers=3, vocab=s.vocab + 64, router_hidden=0)      # the large model's vocabulary is padded further
+    slm = tokroute.Model(s.asdict(), synth.make_weights(s, SEED, std=0.05), B, 64)
+    llm = tokroute.Model(big.asdict(), synth.make_weights(big, SEED + 1, std=0.05), B, 64)
+    prompts = [synth.prompt_tokens(SEED, f"drawn{b}", 5 + 7 * b, s.vocab) for b in range(B)]
+    numbers = np.random.Generator(np.random.Philox(SEED)).random((B, NEW), dtype=np.float32)
+    return s, slm, llm, prompts, numbers
+
+
+def loops():
+    from paper_2504_07878_amd import joint
+    return joint.generate, joint.generate_overlapped
+
+
+@pytest.mark.parametrize("overlapped", [0, 1])
+def test_temperature_zero_is_greedy(models, overlapped):
+    from paper_2504_07878_amd import sampling
+    s, slm, llm, prompts, numbers = models
+    run = loops()[overlapped]
+    tokens, routed = run(slm, llm, prompts, NEW)
+    drawn, routed2 = run(slm, llm, prompts, NEW, draw=sampling.Draw(temperature=0.0), numbers=numbers)
+    assert np.array_equal(tokens, drawn) and np.array_equal(routed, routed2) and routed.any() and not routed.all()
+
+
+@pytest.mark.parametrize("how", [dict(temperature=0.9), dict(top_k=20, temperature=1.1), dict(min_p=0.3), dict(top_p=0.6)])
+@pytest.mark.parametrize("overlapped", [0, 1])
+def test_every_token_is_the_draw_of_its_number(models, overlapped, how):
+    """Each position again, from the whole prefix by a prompt, with the model that the router chose. Logits of a prompt and of a step agree within 1e-4 of their size, here below 5: two
+    of them differ by 1e-3 at most, T being 0.9 or more weights by 1.2e-3 of themselves, and shares by twice that."""
+    from paper_2504_07878_amd import sampling
+    s, slm, llm, prompts, numbers = models
+    draw = sampling.Draw(**how)
+    tokens, routed = loops()[overlapped](slm, llm, prompts, NEW, draw=draw, numbers=numbers)
+    assert routed.any() and not routed.all() and (tokens >= 0).all() and (tokens < s.vocab).all()
+    for b in range(B):
+        for t in range(0, NEW, 3):
+            seq = list(prompts[b]) + tokens[b, :t].tolist()
+            model = llm if routed[b, t] else slm
+            z = model.prefill([0], [seq], want_logits=True).cpu().logits[0, :s.vocab]
+            assert np.abs(z).max() < 5
+            settings = float(np.float32(draw.temperature)), draw.top_k, float(np.float32(draw.top_p)), float(np.float32(draw.min_p))
+            assert picks.near_draw(z, numbers[b, t], *settings, tokens[b, t], 2.4e-3), (b, t)
+
+
+def test_the_same_numbers_the_same_tokens(models):
+    from paper_2504_07878_amd import joint, sampling
+    s, slm, llm, prompts, numbers = models
+    draw = sampling.Draw(temperature=0.8, top_p=0.9)
+    first, _ = joint.generate(slm, llm, prompts, NEW, draw=draw, numbers=numbers)
+    again, _ = joint.generate(slm, llm, prompts, NEW, draw=draw, numbers=numbers)
+    other, _ = joint.generate(slm, llm, prompts, NEW, draw=draw, numbers=1 - numbers)
+    assert np.array_equal(first, again) and not np.array_equal(first, other)
+
+
+def test_drawn_sequences_to_a_new_head(models):
+    """The run as a whole: draws, rows with the teacher's largest logits, and steps of clipped gradients."""
+    from paper_2504_07878_amd import adapt, joint, sampling
+    s, slm, llm, prompts, numbers = models
+    tokens, _ = joint.generate(slm, llm, prompts, NEW, draw=sampling.Draw(temperature=0.9, top_p=0.95), numbers=numbers)
+    hidden, ids, teacher, targets = adapt.collect(slm, llm, prompts, tokens, top=12)
+    assert ids.dtype == torch.int32 and ids.shape == teacher.shape == (B * NEW, 12)
+    logits = llm.prefill(list(range(B)), prompts, want_logits=True).logits
+    for row, i, v in zip(logits.cpu().numpy(), ids[:B].cpu().numpy(), teacher[:B].cpu().numpy()):
+        assert np.array_equal(i, picks.order_of(row)[:12]) and np.array_equal(v, row[i])
+    head = slm.dev["tok_emb"]
+    free, _ = adapt.adapt_head(head, hidden, ids, teacher, targets, steps=1, rate=0.25)
+    length = float((free.double() - head.double()).norm()) / 0.25      # of the gradient
+    for part in (0.1, 0.75):
+        new, losses = adapt.adapt_head(head, hidden, ids, teacher, targets, steps=1, rate=0.25, max_norm=part * length)
+        # fp32 products and sums of a step round by 2^-24 of the head's entries, sqrt(entries) of them together
+        slack = 3 * 2.0 ** -24 * float(head.double().norm()) / 0.25
+        assert abs(float((new.double() - head.double()).norm()) / 0.25 - part * length) <= 1e-5 * length + slack and len(losses) == 1
+    same, _ = adapt.adapt_head(head, hidden, ids, teacher, targets, steps=1, rate=0.25, max_norm=2 * length)
+    assert torch.equal(same, free)
+    assert len(adapt.adapt_head(head, hidden, ids, teacher, targets, steps=5, max_norm=0.5 * length)[1]) == 5
+
+
+def test_more_entries_than_the_losses_take(models):
+    """As before they could be listed: by PyTorch."""
+    from paper_2504_07878_amd import adapt
+    s, slm, llm, prompts, numbers = models
+    hidden, ids, teacher, targets = adapt.collect(slm, llm, prompts, np.ones((B, 1), np.int32), top=1100)
+    assert ids.shape == teacher.shape == (B, 1100) and (teacher[:, :-1] >= teacher[:, 1:]).all()
