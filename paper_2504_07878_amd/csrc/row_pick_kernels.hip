@@ -396,7 +396,7 @@ __device__ __forceinline__ void put_nothing(const PickArgs &a, int r, bool top)
     else if (threadIdx.x == 0) { a.token[r] = -1; a.logprob[r] = 0.f; }
 }
 
-// A first step towards the border of top-k or top-p, where one was taken: key places from b.place on, less than 2^shift of them
+// A first step towards the border of top-k or top-p, where one was taken: key places from b.place on, less than 2^shift of them; top-p's share, where it was computed (0: not)
 struct First { Border b; int shift; u64 want; };
 
 // What the filters keep, listed in order (TOP) or drawn from; false: more than the source knows of. `weight`: of the whole row, for a source that does not hold it all.
@@ -408,6 +408,7 @@ template <bool TOP, class Source, class S> __device__ __forceinline__ bool searc
     bool cut = false, stepped = first.b.found;
     u64 ties = 0, equal = 0, want = 0, sum = 0;      // ties 0: all of them, of `equal` ones
     int mode = row.k > 0 ? BY_COUNT : row.p < 1.f ? BY_MASS : KEPT;
+    const bool ended = row.m > 0.f && least_key(row) >= src.from;      // by min-p, if by nothing else before
 #pragma unroll 1
     for (;;) {
         if (mode == KEPT) {
@@ -427,7 +428,7 @@ template <bool TOP, class Source, class S> __device__ __forceinline__ bool searc
         if (mode == BY_COUNT) want = row.k;
         if (mode == BY_TIE) want = ties;
         if (by_mass) {
-            if (mode == BY_MASS && stepped) want = first.want;
+            if (mode == BY_MASS && !cut && first.want) want = first.want;
             else if (mode == BY_MASS && !cut && !src.all()) want = share_of(row.p, weight, row.unit);
             else {
                 sum = kept.mass;
@@ -451,7 +452,7 @@ template <bool TOP, class Source, class S> __device__ __forceinline__ bool searc
         }, bits, want, s, stepped ? first.b : Border{true, 0, 0, 0}, stepped | few);
         stepped = false;
         if (mode == BY_COUNT) {
-            if (!b.found && !src.all()) return false;
+            if (!b.found && !src.all() && !(ended && !(row.p < 1.f))) return false;
             if (b.found) {
                 kept.key = row.top_key - b.place; equal = b.at; ties = want - b.before < b.at ? want - b.before : 0; cut = true;
                 if (!TOP) src.lessen([&](uint32_t key, uint32_t) { return key >= kept.key; });
@@ -459,8 +460,8 @@ template <bool TOP, class Source, class S> __device__ __forceinline__ bool searc
             mode = row.p < 1.f ? BY_MASS : KEPT;
         } else if (mode == BY_MASS) {
             if (!b.found) {
-                if (!(row.m > 0.f && least_key(row) >= src.from)) return false;
-                mode = KEPT;      // (min-p ends before)
+                if (!ended) return false;
+                mode = KEPT;
                 continue;
             }
             const uint32_t key = row.top_key - b.place;
@@ -546,7 +547,8 @@ template <bool TOP, class S> __device__ __forceinline__ bool among_few(Pool<S> &
             src.tally([&](uint32_t key, uint32_t) { return (key >= floor) & in(step(key)); }, [&](uint32_t key) { return by_count ? 1 : row.mass(key); },
                       [&](uint32_t key, uint32_t, u64 m) { put(step(key), m); });
         }, 0, BIN_BITS, 0, 0, by_count ? (u64)row.k : want, s);
-        if (b.found) { last = b.place; closed = true; first.b = b; first.want = want; }
+        first.want = want;
+        if (b.found) { last = b.place; closed = true; first.b = b; }
     }
     if (!closed) return false;
     __syncthreads();

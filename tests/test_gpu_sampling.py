@@ -8,7 +8,8 @@ import picks
 pytestmark = pytest.mark.gpu
 SIZES = (1, 2, 7, 63, 65, 255, 1000, 2049, 4096, 5003, 16384, 16385, 40001, 151936, 152064)
 SETTINGS = [dict(), dict(temperature=0.7), dict(top_k=1), dict(top_k=5), dict(top_k=50, temperature=0.8), dict(top_p=0.9), dict(top_p=0.5, temperature=1.3), dict(min_p=0.05),
-            dict(top_k=40, top_p=0.95, min_p=0.02, temperature=0.6), dict(temperature=0.0), dict(top_p=0.0), dict(min_p=1.0), dict(top_k=1000, top_p=0.999)]
+            dict(top_k=40, top_p=0.95, min_p=0.02, temperature=0.6), dict(temperature=0.0), dict(top_p=0.0), dict(min_p=1.0), dict(top_k=1000, top_p=0.999),
+            dict(top_p=0.95, min_p=0.02), dict(top_p=0.999, min_p=0.2), dict(top_p=0.9999, min_p=0.001), dict(top_k=700, min_p=0.05), dict(top_k=3000, min_p=0.02), dict(top_k=700, top_p=0.99, min_p=0.01)]
 NAMES = ("temperature", "top_k", "top_p", "min_p")
 NONE = dict(temperature=1.0, top_k=0, top_p=1.0, min_p=0.0)
 
