@@ -70,7 +70,7 @@ inline int pick_listed(int groups)
     return most < PICK_PART_LISTED ? most : PICK_PART_LISTED;
 }
 
-// rows of at most PICK_ROWS
+// PICK_ROWS rows at most where a.head is there
 void launch_sample(hipStream_t s, const PickArgs &a);
 void launch_top(hipStream_t s, const PickArgs &a);
 

@@ -72,13 +72,14 @@ void list_tokens(PickArgs &a, int top_k)
     a.listed_lanes = std::max(1, (int)(64 * (1 - std::exp(-0.85 * a.listed / 64))));
 }
 
-// PICK_ROWS rows at a time
+// PICK_ROWS rows at a time where they meet in the workspace
 template <class Launch> int enqueue(const PickArgs &all, Launch launch)
 {
     const size_t size = all.dtype == DT_BF16 ? 2 : 4;
-    for (int at = 0; at < all.rows; at += PICK_ROWS) {
+    const int most = all.head ? PICK_ROWS : PICK_MAX_ROWS;
+    for (int at = 0; at < all.rows; at += most) {
         PickArgs a = all;
-        a.rows = std::min(PICK_ROWS, all.rows - at);
+        a.rows = std::min(most, all.rows - at);
         a.logits = (const char *)all.logits + (size_t)at * all.stride * size;
         for (const float **p : {&a.u, &a.temperatures, &a.top_ps, &a.min_ps}) if (*p) *p += at;
         if (a.top_ks) a.top_ks += at;

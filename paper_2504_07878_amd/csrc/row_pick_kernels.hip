@@ -269,7 +269,7 @@ template <class Each, class S> __device__ __forceinline__ Border find_border(Eac
         }
         if (!b.found || bits == 0) return b;
         stepped = false;
-        const uint32_t most = (1u << bits) - 1;
+        const uint32_t most = bits >= 32 ? ANY : (1u << bits) - 1;
         if (threadIdx.x == 0) s.entries = 0;
         __syncthreads();
         each([&](uint32_t place) { return place - b.place <= most; }, [&](uint32_t place, u64 amount) {

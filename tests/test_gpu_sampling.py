@@ -124,6 +124,22 @@ def test_masks_infinities_and_nan(sampling, v, how):
         check_top(z, k, *s.top(z, k))
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("v, left", [(2153, 0.3), (30843, 0.01), (30092, 0.02), (151936, 0.005)])
+def test_few_tokens_among_masked_ones(sampling, v, left, dtype):
+    """Most of a row is -inf, some of the rest the type's lowest value: the tokens that are left lie in a vanishing part of the row's range, on both sides of 0."""
+    n, s = 6, sampling.Sampler(6, v, dtype)
+    for kind in ("flat", "peaked", "ties"):
+        z, g = logits_of(kind, n, v, 35, dtype), rng(36)
+        z = z.masked_fill(torch.rand((n, v), device="cuda", generator=g) > left, float("-inf"))
+        z[:, ::3] = torch.finfo(dtype).min
+        u = torch.rand(n, device="cuda", generator=g)
+        for how in (dict(top_p=0.9), dict(top_p=0.9, temperature=5.0), dict(top_k=50), dict(top_k=300, top_p=0.99), dict(min_p=0.01), dict()):
+            check(z, u, how, *s.sample(z, u, **how))
+        for k in (50, 300):
+            check_top(z, k, *s.top(z, k))
+
+
 @pytest.mark.parametrize("v", [1003, 40001])
 def test_settings_of_their_own_for_every_row(sampling, v):
     t = torch.tensor([0.0, 1e-30, 0.5, 1.0, 1.5, float("inf"), -1.0, float("nan"), 1.0, 1.0, 1.0, 1.0, 1.0, 1.0], device="cuda")
