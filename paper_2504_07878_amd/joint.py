@@ -27,7 +27,7 @@ class _Tokens:
         self.wanted, self.vocab = draw is not None, vocab
         if self.wanted:
             from . import sampling
-            self.sampler, self.draw, self.numbers = sampling.Sampler(rows, vocab, device=model.device), asdict(draw), numbers
+            self.sampler, self.draw, self.numbers = sampling.Sampler(rows, vocab, device=model.device), asdict(draw), numbers.to(model.device)
 
     def __call__(self, out, sequences, positions):
         """Row i of the outputs is sequences[i]'s token at positions[i]."""
@@ -44,7 +44,7 @@ def _choosers(slm, llm, rows, max_new, draw, numbers):
     if numbers.shape != (rows, max_new):
         raise ValueError(f"numbers: one for every sequence and new token, [{rows}][{max_new}]")
     import torch
-    numbers = torch.from_numpy(numbers.copy()).to(slm.device)
+    numbers = torch.from_numpy(numbers.copy())
     v = slm.shape["vocab"]
     return _Tokens(slm, rows, v, draw, numbers), _Tokens(llm, rows, min(v, llm.shape["vocab"]), draw, numbers)
 

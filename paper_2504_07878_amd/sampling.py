@@ -6,6 +6,7 @@ that calls share; `Draw` is how `joint.generate` draws. There is no CPU fallback
 from __future__ import annotations
 
 import ctypes as C
+import operator
 from dataclasses import dataclass
 
 import torch
@@ -16,6 +17,11 @@ from .tokroute import TokrouteError, tr_pick_config, tr_pick_rows, tr_sample_how
 MOST_ENTRIES, MOST_VOCAB = 1024, 1 << 20     # that tr_top lists, and that the calls take
 
 _DTYPES = {torch.float32: tokroute.F32, torch.bfloat16: tokroute.BF16}
+
+
+def _int32(v):
+    """A number beyond 32 bits as the nearest that has them, which the library judges (ctypes would take its last 32 bits)."""
+    return max(min(operator.index(v), 2**31 - 1), -2**31)
 
 
 @dataclass(frozen=True)
@@ -41,7 +47,7 @@ class Sampler:
             raise ValueError(f"logits are float32 or bfloat16, not {dtype}")
         self.lib = tokroute.load_library()
         self.dtype = dtype
-        self.cfg = tr_pick_config(max_rows, vocab, _DTYPES[dtype])
+        self.cfg = tr_pick_config(_int32(max_rows), _int32(vocab), _DTYPES[dtype])
         nbytes = self.lib.tr_pick_workspace_bytes(C.byref(self.cfg))
         if nbytes == 0:
             raise TokrouteError(tokroute.ERR_SHAPE, "tr_pick_workspace_bytes", "(sizes or types not supported)")
@@ -56,7 +62,7 @@ class Sampler:
                 and (logits.stride(1) == 1 or v == 1)):
             raise ValueError(f"logits: a {self.dtype} matrix of {v} columns with contiguous rows on {self.device}")
         n, stride = logits.shape[0], logits.stride(0)
-        return tr_pick_rows(logits.data_ptr(), max(stride, v) if n <= 1 else stride, n)
+        return tr_pick_rows(logits.data_ptr(), max(stride, v) if n <= 1 else stride, _int32(n))
 
     def _flat(self, t, what, dtype, shape):
         if not (isinstance(t, torch.Tensor) and t.dtype == dtype and t.device == self.device and t.shape == shape and t.is_contiguous()):
@@ -84,7 +90,7 @@ class Sampler:
             if isinstance(value, torch.Tensor):
                 setattr(how, name + "s", self._flat(value, name, dtype, shape))
             else:
-                setattr(how, name, value)
+                setattr(how, name, _int32(value) if dtype == torch.int32 else value)
         token = torch.empty(shape, dtype=torch.int32, device=self.device) if token is None else token
         logprob = torch.empty(shape, dtype=torch.float32, device=self.device) if logprob is None else logprob
         self._call(self.lib.tr_sample, "tr_sample", C.byref(rows), C.byref(how), self._flat(token, "token", torch.int32, shape), self._flat(logprob, "logprob", torch.float32, shape))
@@ -92,6 +98,8 @@ class Sampler:
 
     def top(self, logits, entries: int, ids=None, values=None):
         """(ids int32 [n][entries], values float32 [n][entries]): the largest logits of each row, in falling order, equal ones by id; -1 and -inf where a row has fewer."""
+        if entries > MOST_ENTRIES:
+            raise TokrouteError(tokroute.ERR_CAPACITY, "tr_top", f"(more than {MOST_ENTRIES} entries)")
         rows = self._rows(logits)
         shape = (rows.rows, entries)
         ids = torch.empty(shape, dtype=torch.int32, device=self.device) if ids is None else ids

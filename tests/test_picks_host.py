@@ -97,3 +97,19 @@ def test_clipping_is_refused_before_anything_is_enqueued(tr):
     for grads, out, counts in (([a, a], [a, a], [10, 10]), ([a, a + 36], [a, a + 36], [10, 10]), ([a], [a + 4], [10]), ([a, b], [b, a], [10, 10]), ([a, b], [b + 4000, b], [10, 1001]),
                                ([a, b], [a + 4096, a + 4100], [2, 2]), ([a, a + 400, b], [a, a + 400, a + 396], [100, 100, 1])):
         assert call(grads, out, counts, [0] * len(grads))[0] == bad, (grads, out, counts)
+
+
+@pytest.mark.parametrize("top_k, passed", [(7, 7), (np.int64(7), 7), (2**31, 2**31 - 1), (2**32 + 1, 2**31 - 1), (-2**32 + 1, -2**31)])
+def test_numbers_beyond_32_bits_are_not_cut_off(tr, top_k, passed):
+    import torch
+    from paper_2504_07878_amd import sampling
+    s = object.__new__(sampling.Sampler)                  # (without a GPU)
+    s.dtype, s.device, s.cfg, s.lib, got = torch.float32, torch.device("cpu"), tr.tr_pick_config(4, 10, tr.F32), tr.load_library(), []
+    s._call = lambda fn, what, rows, how, *out: got.append(how._obj.top_k)
+    s.sample(torch.zeros(4, 10), torch.zeros(4), top_k=top_k)
+    assert got == [passed]
+    for entries in (1025, 2**32 + 1):
+        with pytest.raises(tr.TokrouteError) as e:
+            s.top(torch.zeros(0, 10), entries)
+        assert e.value.code == tr.ERR_CAPACITY
+    assert s._rows(torch.zeros(1, 10).expand(2**32 + 1, 10)).rows == 2**31 - 1       # more than any Sampler is for
