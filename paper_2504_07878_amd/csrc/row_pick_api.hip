@@ -58,18 +58,25 @@ int arguments(const tr_pick_config *c, const tr_pick_rows *in, void *ws, size_t 
     return TR_OK;
 }
 
-// Tokens that a part leaves: as many as there is room for, or, where all rows have a top-k, enough for it. A part's largest m are those of a share m / PICK_PART of the row, give or take
-// sqrt(m), and what is known of the row ends with the part that has the least: some 2.7 sqrt(m) below among a hundred parts.
+// Tokens that a part leaves: as many as there is room for, or, where all rows have a top-k, enough for it. What is known of a row ends where the first part ends, so that each has to leave its
+// share: with tokens in any order a part has L or more of the row's largest top_k by Poisson's distribution of top_k / parts, and one row in a hundred may have such a part (which then is
+// read again, 10 us more for it; one row in a million: 1 us more for every call at top-k 16 to 64).
 void list_tokens(PickArgs &a, int top_k)
 {
     if (!a.head) return;
-    a.listed = pick_listed(a.groups);
+    const int most = pick_listed(a.groups), parts = a.groups * PICK_WAVES;
+    // of x lanes in 64 whose largest of 16 tokens is among them, the others' follow
+    const auto tokens = [](int x) { const double t = 64 * std::log(64.0 / (64 - x)); return (int)std::ceil(t + 3.5 * std::sqrt(t - x)) + 1; };
+    int lanes = 63;
     if (top_k > 0) {
-        const double want = 1.3 * top_k / (a.groups * PICK_WAVES) + 0.3, root = (2.7 + std::sqrt(2.7 * 2.7 + 4 * want)) / 2;
-        a.listed = (int)std::min<double>(a.listed, std::ceil(root * root / 0.85));
+        const double mean = (double)top_k / parts;
+        int least = 0;
+        for (double p = std::exp(-mean); least < 55 && (least <= mean || p * parts > 1e-2); p *= mean / least) ++least;
+        lanes = std::min(lanes, least * 4 / 3);      // (a part takes more than 3/4 of them)
     }
-    // of x lanes in 64 whose largest of 16 tokens is among them, the others' follow: with tokens in any order 64 ln(64 / (64 - x)) tokens, here 0.85 of those that fit
-    a.listed_lanes = std::max(1, (int)(64 * (1 - std::exp(-0.85 * a.listed / 64))));
+    while (lanes > 1 && tokens(lanes) > most) --lanes;
+    a.listed_lanes = lanes;
+    a.listed = std::min(most, tokens(lanes));
 }
 
 // PICK_ROWS rows at a time where they meet in the workspace

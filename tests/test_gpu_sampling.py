@@ -125,6 +125,24 @@ def test_masks_infinities_and_nan(sampling, v, how):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("v, pad", [(8193, 1), (30011, 0), (151936, 3)])
+def test_large_logits_that_lie_together(sampling, v, pad, dtype):
+    """Runs of neighbouring ids that are far above the rest, one run or several, longer and shorter than top-k, at the row's ends too; in one row at equal logits."""
+    z = logits_of("flat", 8, v + pad, 41)[:, :v]
+    for row, (begin, length) in enumerate(((0, 30), (v - 40, 40), (v // 2, 300), (77, 1500), (v // 3, 4000), (0, v), (v // 2, 700), (v // 4, 256))):
+        z[row, begin:begin + length] += 9
+    z[6, v // 2:v // 2 + 700] = 9.5
+    z[7, v // 2:v // 2 + 256] += 20
+    z[7, v - 300:] += 7
+    z, u = z.to(dtype), torch.rand(8, device="cuda", generator=rng(42))
+    s = sampling.Sampler(8, v, dtype)
+    for k in (5, 50, 400, 1000):
+        for how in (dict(top_k=k), dict(top_k=k, top_p=0.9, temperature=2.0), dict(top_k=torch.full((8,), k, dtype=torch.int32, device="cuda"), top_p=0.95, min_p=0.01)):
+            check(z, u, how, *s.sample(z, u, **how))
+        check_top(z, k, *s.top(z, k))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("v, left", [(2153, 0.3), (30843, 0.01), (30092, 0.02), (151936, 0.005)])
 def test_few_tokens_among_masked_ones(sampling, v, left, dtype):
     """Most of a row is -inf, some of the rest the type's lowest value: the tokens that are left lie in a vanishing part of the row's range, on both sides of 0."""
