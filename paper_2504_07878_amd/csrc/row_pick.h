@@ -15,7 +15,7 @@ constexpr int PICK_THREADS = 512, PICK_WAVES = PICK_THREADS / 64, PICK_PART = 10
 constexpr int PICK_ONE = PICK_GROUP;                      // most tokens of a row that is one workgroup's from the start
 constexpr int PICK_ROWS = 1024;
 constexpr int PICK_LISTED = 8192;                         // most tokens of a row that parts leave, and that the deciding workgroup holds
-constexpr int PICK_PART_LISTED = 64;                      // of one part
+constexpr int PICK_PART_LISTED = 128;                     // of one part
 constexpr int PICK_STEPS = 256;                           // of a histogram of masses over the logits of a row
 
 struct alignas(16) PickHead {
