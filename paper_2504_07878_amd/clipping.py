@@ -11,6 +11,7 @@ import torch
 from . import tokroute
 from .tokroute import TokrouteError
 
+_type_of = torch.Tensor.dtype.__get__
 _DTYPES = {torch.float32: tokroute.F32, torch.bfloat16: tokroute.BF16}
 
 
@@ -34,19 +35,21 @@ class Clipper:
         self._home = torch.cuda.current_stream(self.device).cuda_stream
 
     # -- helpers
-    def _list(self, grads, what="gradients"):
-        """Addresses; a few calls over all tensors rather than several a tensor (hundreds of gradients take longer to look at than to read)."""
+    def _look(self, grads, what="gradients"):
+        """Addresses, and the types there are; a few calls over all tensors rather than several a tensor (hundreds of gradients take longer to look at than to read)."""
         try:
-            fine = set(map(torch.Tensor.get_device, grads)) <= {self.device.index} and all(map(torch.Tensor.is_contiguous, grads)) and {t.dtype for t in grads} <= _DTYPES.keys()
+            kinds = set(map(_type_of, grads))
+            fine = kinds <= _DTYPES.keys() and set(map(torch.Tensor.get_device, grads)) <= {self.device.index} and all(map(torch.Tensor.is_contiguous, grads))
         except (TypeError, RuntimeError):       # no tensor, or one of another layout
             fine = False
         if not fine and not all(isinstance(t, torch.Tensor) and t.dtype in _DTYPES and t.device == self.device and t.layout == torch.strided and _dense(t) for t in grads):
             raise ValueError(f"{what}: float32 or bfloat16 tensors on {self.device}, each of elements that fill one piece of memory")
-        return array("q", map(torch.Tensor.data_ptr, grads))
+        return array("q", list(map(torch.Tensor.data_ptr, grads))), kinds
 
     @staticmethod
-    def _sizes(grads):
-        return array("q", map(torch.Tensor.numel, grads)), array("i", [_DTYPES[t.dtype] for t in grads])
+    def _sizes(grads, kinds):
+        types = [_DTYPES[kind] for kind in kinds] * len(grads) if len(kinds) == 1 else [_DTYPES[t.dtype] for t in grads]
+        return array("q", list(map(torch.Tensor.numel, grads))), array("i", types)
 
     def _call(self, fn, what, arrays, *args):
         stream = tokroute.raw_stream(self.device.index)
@@ -61,8 +64,8 @@ class Clipper:
     def norm(self, grads):
         """Length of all gradients together: a float32 tensor of no dimensions."""
         grads = [t for t in grads if t is not None]
-        at, norm = self._list(grads), torch.empty((), dtype=torch.float32, device=self.device)
-        self._call(self.lib.tr_grad_norm, "tr_grad_norm", [at, *self._sizes(grads)], norm.data_ptr())
+        (at, kinds), norm = self._look(grads), torch.empty((), dtype=torch.float32, device=self.device)
+        self._call(self.lib.tr_grad_norm, "tr_grad_norm", [at, *self._sizes(grads, kinds)], norm.data_ptr())
         return norm
 
     def clip(self, grads, max_norm: float, out=None):
@@ -72,12 +75,12 @@ class Clipper:
         if len(out) != len(grads) or any((a is None) != (b is None) for a, b in zip(grads, out)):
             raise ValueError("out: a tensor for every gradient")
         grads, out = [t for t in grads if t is not None], [t for t in out if t is not None]
-        at = self._list(grads)
+        at, kinds = self._look(grads)
         to = at
         if any(a is not b for a, b in zip(grads, out)):
-            to = self._list(out, "out")
+            to, _ = self._look(out, "out")
             if any(a.dtype != b.dtype or a.shape != b.shape or (a.stride() != b.stride() and not (a.is_contiguous() and b.is_contiguous())) for a, b in zip(grads, out)):
                 raise ValueError("out: tensors of the gradients' shapes, types and strides")
         norm = torch.empty((), dtype=torch.float32, device=self.device)
-        self._call(self.lib.tr_grad_clip, "tr_grad_clip", [at, to, *self._sizes(grads)], max_norm, norm.data_ptr())
+        self._call(self.lib.tr_grad_clip, "tr_grad_clip", [at, to, *self._sizes(grads, kinds)], max_norm, norm.data_ptr())
         return norm
