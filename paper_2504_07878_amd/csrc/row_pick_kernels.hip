@@ -118,10 +118,9 @@ struct Row {
         constexpr double WHOLE = 6755399441055744.0;      // 3 2^51: what is added to it is rounded to a whole number
         const double x = fmax(((double)z - top) * per, -32000.0), n = x + WHOLE, f = x - (n - WHOLE);
         const uint32_t k = (uint32_t)__double_as_longlong(n);
-        const double q = fma(fma(fma(uniform(9.172598566029335e-09), f, uniform(1.6938609067364198e-06)), f, uniform(0.00023459619820112603)), f, uniform(0.021660849392187844));
+        const double q = fma(fma(fma(fma(uniform(9.172598566029335e-09), f, uniform(1.6938609067364198e-06)), f, uniform(0.00023459619820112603)), f, uniform(0.021660849392187844)), f, 1.0);
         const uint2 word = powers[k & 31];
-        const double power = __hiloint2double((int)(word.y + (k << 15)), (int)word.x);
-        return fma(power, q * f, power);
+        return __hiloint2double((int)(word.y + (k << 15)), (int)word.x) * q;
     }
     // in units (2^51 of them at most: rounded by adding 2^52)
     __device__ __forceinline__ u64 in_units(double w) const { return (u64)__double_as_longlong(fma(w, unit, 4503599627370496.0)) & 0xfffffffffffffull; }
@@ -670,7 +669,7 @@ template <class T, class S> __device__ __forceinline__ void draw_freely(const Pi
 
 // ------------------------------------------------------------------ the kernels
 
-// A part of a row: blocks of a load each, `step` apart, in LDS as 32 bits, EACH a lane (-inf: no token). A load past the row's end is moved back, and what it has twice is dropped.
+// A part of a row: blocks of a load each, `step` apart, in LDS as 32 bits, EACH a lane (-inf, NaN: no token). A load past the row's end is moved back, and what it has twice is dropped.
 template <class T> struct Part {
     static constexpr int N = 16 / sizeof(T), BLOCKS = EACH / N, BLOCK = 64 * N;
     float (*z)[64][4];           // [EACH / 4][lane][4]
@@ -695,10 +694,7 @@ template <class T> struct Part {
         for (int i = 0; i < BLOCKS; ++i) {
             float v[N];
 #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                v[e] = wide(raw[i][e]);
-                v[e] = v[e] > -INFINITY ? v[e] : -INFINITY;
-            }
+            for (int e = 0; e < N; ++e) v[e] = wide(raw[i][e]);
             if (!whole) {
 #pragma unroll
                 for (int e = 0; e < N; ++e) if (at(i) + e < first + i * step) v[e] = -INFINITY;
@@ -978,7 +974,7 @@ template <class T, bool TOP, bool WHOLE, int HELD> __global__ __launch_bounds__(
 
 // ------------------------------------------------------------------ rows that are searched
 
-// The step of a logit below `from`; larger logits are in no later step
+// The step of a logit below `from`; larger logits are in no later step, and what is no token is in none
 __device__ __forceinline__ int step_of(float z, const PickSearch &q) { return (int)fminf((q.from - z) * q.scale, (float)PICK_STEPS); }
 
 constexpr int STEP_COPIES = THREADS / PICK_STEPS;      // of the histogram, for neighbouring lanes: even tokens meet in few steps
@@ -1007,7 +1003,7 @@ template <class T> __global__ __launch_bounds__(THREADS, 8) void steps_kernel(Pi
         u64 above = 0;
         p.each([&](float z, int) {
             const int at = z >= q.from ? -1 : step_of(z, q);
-            if (z == -INFINITY || at >= PICK_STEPS - 1) return;
+            if (at >= PICK_STEPS - 1) return;                        // (-inf and NaN too)
             const u64 m = row.in_units(row.finite_weight(z));
             if (at < 0) above += m;
             else atomicAdd(&step[threadIdx.x % STEP_COPIES][at], m);
@@ -1088,8 +1084,7 @@ template <class T> __global__ __launch_bounds__(THREADS, 8) void place_kernel(Pi
         u64 mass = 0;
         uint32_t mask = 0;
         p.each([&](float z, int e) {
-            if (z == -INFINITY) return;
-            const int at = stage == PICK_STEP ? step_of(z, q) : PICK_STEPS;
+            const int at = stage == PICK_STEP ? step_of(z, q) : PICK_STEPS;      // (-inf, NaN: PICK_STEPS)
             if (z >= least || at < step) mass += row.in_units(row.finite_weight(z));
             else mask |= (uint32_t)(at == step) << e;
         });
