@@ -4,7 +4,8 @@
 
 namespace tr {
 
-// A launch takes up to CLIP_LIST gradients, handed over by value (nothing of a call lies in memory that has to outlive it), as tiles of CLIP_TILE bytes numbered through.
+// A launch takes up to CLIP_LIST gradients (as many as 4 KB of arguments hold), handed over by value (nothing of a call lies in memory that has to outlive it), as tiles of CLIP_TILE bytes
+// numbered through: eight loads of 16 bytes a thread in flight (norm of 494 million bf16 elements 188 us, with four 209, with sixteen the same).
 constexpr int CLIP_LIST = 112, CLIP_TILE = 32768;
 constexpr int CLIP_GROUPS = 2048;              // most workgroups of a launch, each of which leaves a sum
 constexpr int CLIP_SUMS = 4096;                // places for sums in the workspace

@@ -730,7 +730,8 @@ template <class T> struct Part {
     }
 };
 
-// Bound by its instructions: some 40 a token and lane where sums are wanted, half of them 64-bit ones for the weight.
+// Bound by its instructions where sums are wanted: 35 a token and lane with the list, 22 without, half of them 64-bit ones for the weight (256 rows of 152064 bf16 logits 44 us, 64 free fp32 rows 12).
+// Without sums 13, bound by memory (1024 rows of 151936 fp32 logits 107 us, 5.8 TB/s). 16 tokens a lane: with 32 fewer wavefronts wait for the loads at once.
 template <class T, bool TOP> __global__ __launch_bounds__(THREADS, 8) void parts_kernel(PickArgs a)
 {
     __shared__ float s_z[WAVES][EACH / 4][64][4];
@@ -867,7 +868,7 @@ template <class T, int HELD, class S> __device__ __forceinline__ bool mend(const
     return true;
 }
 
-// One workgroup a row. Bound by the latency of a few loads and of some twenty barriers.
+// One workgroup a row. Bound by the latency of a few loads and of some twenty barriers: one row of 151936 8.3 us, the largest 16 of 64 rows 6, 256 rows with top-p, which ends among thousands, 31.
 template <class T, bool TOP, bool WHOLE, int HELD> __global__ __launch_bounds__(DECIDERS) void decide_kernel(PickArgs a)
 {
     using S = Shared<HELD, WHOLE>;
@@ -979,6 +980,7 @@ __device__ __forceinline__ int step_of(float z, const PickSearch &q) { return (i
 
 constexpr int STEP_COPIES = THREADS / PICK_STEPS;      // of the histogram, for neighbouring lanes: even tokens meet in few steps
 
+// Bound by the 64-bit LDS atomics (32 rows of 151936 11 us; a third to half of the LDS cycles are conflicts).
 // Masses by steps below `from`, in the last place that of everything from it on; what is below all steps is left out
 template <class T> __global__ __launch_bounds__(THREADS, 8) void steps_kernel(PickArgs a)
 {
@@ -1021,6 +1023,7 @@ template <class T> __global__ __launch_bounds__(THREADS, 8) void steps_kernel(Pi
     }
 }
 
+// Bound by its instructions and by the latency before them (32 rows of 151936 14 us).
 // The step that top-p ends in; of each part the mass of what is above it and its tokens in it. Where min-p alone decides, the mass of what it keeps.
 template <class T> __global__ __launch_bounds__(THREADS, 8) void place_kernel(PickArgs a)
 {
@@ -1098,7 +1101,7 @@ template <class T> __global__ __launch_bounds__(THREADS, 8) void place_kernel(Pi
     }
 }
 
-// The place in the step, and the draw: the part by the parts' masses, then the token in it
+// The place in the step, and the draw: the part by the parts' masses, then the token in it. One workgroup a row, bound by latency (32 rows 16 us).
 template <class T> __global__ __launch_bounds__(DECIDERS) void finish_kernel(PickArgs a)
 {
     constexpr int HELD = PICK_LISTED;
