@@ -36,7 +36,7 @@ class Clipper:
 
     # -- helpers
     def _look(self, grads, what="gradients"):
-        """Addresses, and the types there are; a few calls over all tensors rather than several a tensor (hundreds of gradients take longer to look at than to read)."""
+        """Addresses, the types there are, and whether all are contiguous; a few calls over all tensors rather than several a tensor (hundreds of gradients take longer to look at than to read)."""
         try:
             kinds = set(map(_type_of, grads))
             fine = kinds <= _DTYPES.keys() and set(map(torch.Tensor.get_device, grads)) <= {self.device.index} and all(map(torch.Tensor.is_contiguous, grads))
@@ -44,7 +44,7 @@ class Clipper:
             fine = False
         if not fine and not all(isinstance(t, torch.Tensor) and t.dtype in _DTYPES and t.device == self.device and t.layout == torch.strided and _dense(t) for t in grads):
             raise ValueError(f"{what}: float32 or bfloat16 tensors on {self.device}, each of elements that fill one piece of memory")
-        return array("q", list(map(torch.Tensor.data_ptr, grads))), kinds
+        return array("q", list(map(torch.Tensor.data_ptr, grads))), kinds, fine
 
     @staticmethod
     def _sizes(grads, kinds):
@@ -64,22 +64,24 @@ class Clipper:
     def norm(self, grads):
         """Length of all gradients together: a float32 tensor of no dimensions."""
         grads = [t for t in grads if t is not None]
-        (at, kinds), norm = self._look(grads), torch.empty((), dtype=torch.float32, device=self.device)
+        (at, kinds, _), norm = self._look(grads), torch.empty((), dtype=torch.float32, device=self.device)
         self._call(self.lib.tr_grad_norm, "tr_grad_norm", [at, *self._sizes(grads, kinds)], norm.data_ptr())
         return norm
 
     def clip(self, grads, max_norm: float, out=None):
         """The same, and the gradients scaled by min(1, max_norm / norm): in place, or into `out` (tensors of the same shapes, types and strides; None where a gradient is None)."""
-        grads = list(grads)
-        out = grads if out is None else list(out)
-        if len(out) != len(grads) or any((a is None) != (b is None) for a, b in zip(grads, out)):
+        all_grads = list(grads)
+        all_out = all_grads if out is None else list(out)
+        grads, out = [t for t in all_grads if t is not None], [t for t in all_out if t is not None]
+        if len(all_out) != len(all_grads) or len(out) != len(grads) or (len(grads) < len(all_grads) and any((a is None) != (b is None) for a, b in zip(all_grads, all_out))):
             raise ValueError("out: a tensor for every gradient")
-        grads, out = [t for t in grads if t is not None], [t for t in out if t is not None]
-        at, kinds = self._look(grads)
+        at, kinds, plain = self._look(grads)
         to = at
         if any(a is not b for a, b in zip(grads, out)):
-            to, _ = self._look(out, "out")
-            if any(a.dtype != b.dtype or a.shape != b.shape or (a.stride() != b.stride() and not (a.is_contiguous() and b.is_contiguous())) for a, b in zip(grads, out)):
+            to, out_kinds, out_plain = self._look(out, "out")
+            same = list(map(torch.Tensor.size, grads)) == list(map(torch.Tensor.size, out)) and kinds == out_kinds
+            if not same or (len(kinds) > 1 and any(a.dtype != b.dtype for a, b in zip(grads, out))) or (
+                    not (plain and out_plain) and any(a.stride() != b.stride() and not (a.is_contiguous() and b.is_contiguous()) for a, b in zip(grads, out))):
                 raise ValueError("out: tensors of the gradients' shapes, types and strides")
         norm = torch.empty((), dtype=torch.float32, device=self.device)
         self._call(self.lib.tr_grad_clip, "tr_grad_clip", [at, to, *self._sizes(grads, kinds)], max_norm, norm.data_ptr())
