@@ -58,11 +58,11 @@ class Sampler:
     # -- helpers
     def _rows(self, logits):
         v = self.cfg.vocab
-        if not (isinstance(logits, torch.Tensor) and logits.dtype == self.dtype and logits.device == self.device and logits.dim() == 2 and logits.shape[1] == v
-                and (logits.stride(1) == 1 or v == 1)):
+        fine = isinstance(logits, torch.Tensor) and logits.dtype == self.dtype and logits.device == self.device and logits.dim() == 2
+        (n, columns), (stride, along) = (logits.shape, logits.stride()) if fine else ((0, 0), (0, 0))
+        if columns != v or (along != 1 and v > 1):
             raise ValueError(f"logits: a {self.dtype} matrix of {v} columns with contiguous rows on {self.device}")
-        n, stride = logits.shape[0], logits.stride(0)
-        return tr_pick_rows(logits.data_ptr(), max(stride, v) if n <= 1 else stride, _int32(n))
+        return tr_pick_rows(logits.data_ptr(), max(stride, v) if n <= 1 else stride, n if n < 2**31 else 2**31 - 1)      # (more than any Sampler is for)
 
     def _flat(self, t, what, dtype, shape):
         if not (isinstance(t, torch.Tensor) and t.dtype == dtype and t.device == self.device and t.shape == shape and t.is_contiguous()):
@@ -85,15 +85,32 @@ class Sampler:
         temperature, top_p, min_p (float32 [n]) and top_k (int32 [n]) are numbers or device tensors with a value a row. token and logprob may be given (written over)."""
         rows = self._rows(logits)
         shape = (rows.rows,)
-        how = tr_sample_how(self._flat(u, "u", torch.float32, shape), None, None, None, None, 1.0, 0, 1.0, 0.0)
-        for name, value, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
-            if isinstance(value, torch.Tensor):
-                setattr(how, name + "s", self._flat(value, name, dtype, shape))
-            else:
-                setattr(how, name, _int32(value) if dtype == torch.int32 else value)
-        token = torch.empty(shape, dtype=torch.int32, device=self.device) if token is None else token
-        logprob = torch.empty(shape, dtype=torch.float32, device=self.device) if logprob is None else logprob
-        self._call(self.lib.tr_sample, "tr_sample", C.byref(rows), C.byref(how), self._flat(token, "token", torch.int32, shape), self._flat(logprob, "logprob", torch.float32, shape))
+        how = tr_sample_how(self._flat(u, "u", torch.float32, shape))
+        if isinstance(temperature, torch.Tensor):
+            how.temperatures = self._flat(temperature, "temperature", torch.float32, shape)
+        else:
+            how.temperature = temperature
+        if isinstance(top_k, torch.Tensor):
+            how.top_ks = self._flat(top_k, "top_k", torch.int32, shape)
+        else:
+            how.top_k = _int32(top_k)
+        if isinstance(top_p, torch.Tensor):
+            how.top_ps = self._flat(top_p, "top_p", torch.float32, shape)
+        else:
+            how.top_p = top_p
+        if isinstance(min_p, torch.Tensor):
+            how.min_ps = self._flat(min_p, "min_p", torch.float32, shape)
+        else:
+            how.min_p = min_p
+        if token is None:
+            token = torch.empty_like(u, dtype=torch.int32)
+        else:
+            self._flat(token, "token", torch.int32, shape)
+        if logprob is None:
+            logprob = torch.empty_like(u)
+        else:
+            self._flat(logprob, "logprob", torch.float32, shape)
+        self._call(self.lib.tr_sample, "tr_sample", C.byref(rows), C.byref(how), token.data_ptr(), logprob.data_ptr())
         return token, logprob
 
     def top(self, logits, entries: int, ids=None, values=None):
@@ -102,7 +119,13 @@ class Sampler:
             raise TokrouteError(tokroute.ERR_CAPACITY, "tr_top", f"(more than {MOST_ENTRIES} entries)")
         rows = self._rows(logits)
         shape = (rows.rows, entries)
-        ids = torch.empty(shape, dtype=torch.int32, device=self.device) if ids is None else ids
-        values = torch.empty(shape, dtype=torch.float32, device=self.device) if values is None else values
-        self._call(self.lib.tr_top, "tr_top", C.byref(rows), entries, self._flat(ids, "ids", torch.int32, shape), self._flat(values, "values", torch.float32, shape))
+        if ids is None:
+            ids = logits.new_empty(shape, dtype=torch.int32)
+        else:
+            self._flat(ids, "ids", torch.int32, shape)
+        if values is None:
+            values = logits.new_empty(shape, dtype=torch.float32)
+        else:
+            self._flat(values, "values", torch.float32, shape)
+        self._call(self.lib.tr_top, "tr_top", C.byref(rows), entries, ids.data_ptr(), values.data_ptr())
         return ids, values
