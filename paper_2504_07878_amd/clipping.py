@@ -69,7 +69,8 @@ class Clipper:
         return norm
 
     def clip(self, grads, max_norm: float, out=None):
-        """The same, and the gradients scaled by min(1, max_norm / norm): in place, or into `out` (tensors of the same shapes, types and strides; None where a gradient is None)."""
+        """The same, and the gradients scaled by min(1, max_norm / norm): in place, or into `out` (tensors of the same types, shapes and strides, None where a gradient is None;
+        where all are contiguous those of as many elements will do)."""
         all_grads = list(grads)
         all_out = all_grads if out is None else list(out)
         grads, out = [t for t in all_grads if t is not None], [t for t in all_out if t is not None]
@@ -79,10 +80,13 @@ class Clipper:
         to = at
         if any(a is not b for a, b in zip(grads, out)):
             to, out_kinds, out_plain = self._look(out, "out")
-            same = list(map(torch.Tensor.size, grads)) == list(map(torch.Tensor.size, out)) and kinds == out_kinds
-            if not same or (len(kinds) > 1 and any(a.dtype != b.dtype for a, b in zip(grads, out))) or (
-                    not (plain and out_plain) and any(a.stride() != b.stride() and not (a.is_contiguous() and b.is_contiguous()) for a, b in zip(grads, out))):
-                raise ValueError("out: tensors of the gradients' shapes, types and strides")
+            alike = kinds == out_kinds and (len(kinds) <= 1 or list(map(_type_of, grads)) == list(map(_type_of, out)))
+            if plain and out_plain:
+                alike = alike and list(map(torch.Tensor.numel, grads)) == list(map(torch.Tensor.numel, out))
+            else:
+                alike = alike and all(a.shape == b.shape and (a.stride() == b.stride() or (a.is_contiguous() and b.is_contiguous())) for a, b in zip(grads, out))
+            if not alike:
+                raise ValueError("out: tensors of the gradients' types, shapes and strides")
         norm = torch.empty((), dtype=torch.float32, device=self.device)
         self._call(self.lib.tr_grad_clip, "tr_grad_clip", [at, to, *self._sizes(grads, kinds)], max_norm, norm.data_ptr())
         return norm

@@ -58,6 +58,12 @@ int arguments(const tr_pick_config *c, const tr_pick_rows *in, void *ws, size_t 
     return TR_OK;
 }
 
+// Room for the tokens that go with x lanes in 64 whose largest of 16 is among them: t = 64 log(64 / (64 - x)) of tokens in any order, give or take sqrt(t - x)
+struct Room {
+    int of[64] = {};
+    Room() { for (int x = 1; x < 64; ++x) { const double t = 64 * std::log(64.0 / (64 - x)); of[x] = (int)std::ceil(t + 3.5 * std::sqrt(t - x)) + 1; } }
+};
+
 // Tokens that a part leaves: as many as there is room for, or, where all rows have a top-k, enough for it. What is known of a row ends where the first part ends, so that each has to leave its
 // share: with tokens in any order a part has L or more of the row's largest top_k by Poisson's distribution of top_k / parts, and one row in a hundred may have such a part (which then is
 // read again, 10 us more for it; one row in a million: 1 us more for every call at top-k 16 to 64).
@@ -66,8 +72,7 @@ void list_tokens(PickArgs &a, int top_k)
     if (!a.head) return;
     // (without top-k half of it: of 64 flat rows of 20000 top-p 0.9 and min-p 0.05 take 34 instead of 45 us, while the largest 1000 take 31 instead of 68 with all of it)
     const int most = top_k > 0 || a.top_ks ? pick_listed(a.groups) : std::min(pick_listed(a.groups), PICK_PART_LISTED / 2), parts = a.groups * PICK_WAVES;
-    // of x lanes in 64 whose largest of 16 tokens is among them, the others' follow
-    const auto tokens = [](int x) { const double t = 64 * std::log(64.0 / (64 - x)); return (int)std::ceil(t + 3.5 * std::sqrt(t - x)) + 1; };
+    static const Room room;
     int lanes = 63;
     if (top_k > 0) {
         const double mean = (double)top_k / parts;
@@ -75,9 +80,9 @@ void list_tokens(PickArgs &a, int top_k)
         for (double p = std::exp(-mean); least < 63 && (least <= mean || p * parts > 1e-2); p *= mean / least) ++least;
         lanes = std::min(lanes, least * 4 / 3);      // (a part takes more than 3/4 of them)
     }
-    while (lanes > 1 && tokens(lanes) > most) --lanes;
+    while (lanes > 1 && room.of[lanes] > most) --lanes;
     a.listed_lanes = lanes;
-    a.listed = std::min(most, tokens(lanes));
+    a.listed = std::min(most, room.of[lanes]);
 }
 
 // PICK_ROWS rows at a time where they meet in the workspace

@@ -98,6 +98,20 @@ def test_alignment_order_of_dimensions_and_what_lies_beside(clipping):
         assert not to[:5].any()
 
 
+def test_into_tensors_of_other_shapes(clipping):
+    """Contiguous ones of as many elements: a bucket's rows. Types are one by one the same, and orders of dimensions are not mixed."""
+    c, grads = clipping.Clipper(), some([(33, 70), 9, (3, 4, 5)], (torch.float32, torch.bfloat16, torch.float32))
+    out = [torch.zeros(t.numel(), device="cuda", dtype=t.dtype) for t in grads]
+    check([a.view(b.shape) for a, b in zip(out, grads)], grads, c.clip(grads, 0.5, out=out), 0.5)
+    turned = [t.clone() for t in grads]
+    turned[0] = torch.zeros((70, 33), device="cuda").t()
+    for bad in ([out[1], out[0], out[2]], [out[0], out[1].float(), out[2].bfloat16()], turned, [out[0][:-1], out[1], out[2]]):
+        before = [t.clone() for t in bad]
+        with pytest.raises(ValueError):
+            c.clip(grads, 0.5, out=bad)
+        assert all(torch.equal(a, b) for a, b in zip(bad, before))
+
+
 def test_the_same_gradient_twice(clipping):
     t = some([1000], (torch.float32,))[0]
     c = clipping.Clipper()
