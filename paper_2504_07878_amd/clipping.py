@@ -47,9 +47,9 @@ class Clipper:
         return array("q", list(map(torch.Tensor.data_ptr, grads))), kinds, fine
 
     @staticmethod
-    def _sizes(grads, kinds):
+    def _sizes(grads, kinds, counts):
         types = [_DTYPES[kind] for kind in kinds] * len(grads) if len(kinds) == 1 else [_DTYPES[t.dtype] for t in grads]
-        return array("q", list(map(torch.Tensor.numel, grads))), array("i", types)
+        return array("q", counts), array("i", types)
 
     def _call(self, fn, what, arrays, *args):
         stream = tokroute.raw_stream(self.device.index)
@@ -65,7 +65,7 @@ class Clipper:
         """Length of all gradients together: a float32 tensor of no dimensions."""
         grads = [t for t in grads if t is not None]
         (at, kinds, _), norm = self._look(grads), torch.empty((), dtype=torch.float32, device=self.device)
-        self._call(self.lib.tr_grad_norm, "tr_grad_norm", [at, *self._sizes(grads, kinds)], norm.data_ptr())
+        self._call(self.lib.tr_grad_norm, "tr_grad_norm", [at, *self._sizes(grads, kinds, list(map(torch.Tensor.numel, grads)))], norm.data_ptr())
         return norm
 
     def clip(self, grads, max_norm: float, out=None):
@@ -77,16 +77,16 @@ class Clipper:
         if len(all_out) != len(all_grads) or len(out) != len(grads) or (len(grads) < len(all_grads) and any((a is None) != (b is None) for a, b in zip(all_grads, all_out))):
             raise ValueError("out: a tensor for every gradient")
         at, kinds, plain = self._look(grads)
-        to = at
+        to, counts = at, list(map(torch.Tensor.numel, grads))
         if any(a is not b for a, b in zip(grads, out)):
             to, out_kinds, out_plain = self._look(out, "out")
             alike = kinds == out_kinds and (len(kinds) <= 1 or list(map(_type_of, grads)) == list(map(_type_of, out)))
             if plain and out_plain:
-                alike = alike and list(map(torch.Tensor.numel, grads)) == list(map(torch.Tensor.numel, out))
+                alike = alike and counts == list(map(torch.Tensor.numel, out))
             else:
                 alike = alike and all(a.shape == b.shape and (a.stride() == b.stride() or (a.is_contiguous() and b.is_contiguous())) for a, b in zip(grads, out))
             if not alike:
                 raise ValueError("out: tensors of the gradients' types, shapes and strides")
         norm = torch.empty((), dtype=torch.float32, device=self.device)
-        self._call(self.lib.tr_grad_clip, "tr_grad_clip", [at, to, *self._sizes(grads, kinds)], max_norm, norm.data_ptr())
+        self._call(self.lib.tr_grad_clip, "tr_grad_clip", [at, to, *self._sizes(grads, kinds, counts)], max_norm, norm.data_ptr())
         return norm
