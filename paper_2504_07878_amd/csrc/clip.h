@@ -5,9 +5,13 @@
 namespace tr {
 
 // A launch takes up to CLIP_LIST gradients (as many as 4 KB of arguments hold), handed over by value (nothing of a call lies in memory that has to outlive it), as tiles of CLIP_TILE bytes
-// numbered through: eight loads of 16 bytes a thread in flight (norm of 494 million bf16 elements 188 us, with four 209, with sixteen the same).
+// numbered through: eight loads of 16 bytes a thread in flight (norm of 494 million bf16 elements, read through the caches, 188 us, with four 209, with sixteen the same).
 constexpr int CLIP_LIST = 112, CLIP_TILE = 32768;
 constexpr int CLIP_GROUPS = 2048;              // most workgroups of a launch, each of which leaves a sum
+// What is read once, or not again before it has left the last-level cache, is read past the caches (norm of 494 million bf16 elements 158 instead of 187 us; after another buffer was written,
+// whose lines the loads would throw out, 175 instead of 255). Bytes at the end of the gradients that the cache is left for between the two passes of clipping (clip of 272 MB
+// 124 us, of 2 GB 987; with 128 MB 130 and 996, with 256 MB 128 and 987, without any 132 and 993; all read through the caches 130 and 1094):
+constexpr uint64_t CLIP_KEEP = 192 << 20;
 constexpr int CLIP_SUMS = 4096;                // places for sums in the workspace
 
 struct ClipList {
@@ -17,6 +21,7 @@ struct ClipList {
     uint32_t tile[CLIP_LIST + 1];              // first tile of each; the last one's end
     unsigned char half[CLIP_LIST];             // bf16
     int n;
+    uint32_t past;                             // tiles before this one are read past the caches; backwards those from this one on
 };
 static_assert(sizeof(ClipList) < 4000, "kernel arguments");
 

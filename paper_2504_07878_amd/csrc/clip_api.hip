@@ -75,7 +75,15 @@ int run(void *ws, size_t ws_bytes, void *stream, int n, const void *const *in, v
     hipStream_t s = (hipStream_t)stream;
     double *const sums = (double *)ws;
     int have = 0;                          // sums so far
-    lists(false, n, in, out, counts, dtypes, [&](const ClipList &l) {
+    // tiles that are read again while the cache may still have them, the last ones, and those before them
+    uint64_t kept = 0, past = 0;
+    for (int i = 0; i < n; ++i) past += ((uint64_t)counts[i] * size_of(dtypes[i]) + CLIP_TILE - 1) / CLIP_TILE;
+    if (out) kept = std::min<uint64_t>(past, CLIP_KEEP / CLIP_TILE);
+    past -= kept;
+    uint64_t left = past;
+    lists(false, n, in, out, counts, dtypes, [&](ClipList &l) {
+        l.past = (uint32_t)std::min<uint64_t>(left, l.tile[l.n]);
+        left -= l.past;
         if (have + clip_groups(l) > CLIP_SUMS) {
             launch_clip_join(s, sums, have, sums, nullptr);
             have = 1;
@@ -90,7 +98,9 @@ int run(void *ws, size_t ws_bytes, void *stream, int n, const void *const *in, v
             launch_clip_join(s, sums, have, sums, nullptr);
             have = 1;
         }
-        lists(true, n, in, out, counts, dtypes, [&](const ClipList &l) {
+        lists(true, n, in, out, counts, dtypes, [&](ClipList &l) {
+            l.past = (uint32_t)std::min<uint64_t>(kept, l.tile[l.n]);
+            kept -= l.past;
             launch_clip_scale(s, l, sums, have, max_norm, norm);
             norm = nullptr;
         });

@@ -26,7 +26,26 @@ template <class T> __device__ __forceinline__ void store_past(T *p, const Vector
     __builtin_nontemporal_store(v, (u32x4_any *)p);
 }
 
-// f(gradient, first element, elements) for the tiles of a list that are this workgroup's
+template <class T> __device__ __forceinline__ Vector<T> load_past(const T *p)
+{
+    const u32x4_any v = __builtin_nontemporal_load((const u32x4_any *)p);
+    Vector<T> x;
+    __builtin_memcpy(&x, &v, 16);
+    return x;
+}
+
+// a whole tile, all its loads at once
+template <bool PAST, class T> __device__ __forceinline__ void load_tile(Vector<T> (&x)[LOADS], const T *p)
+{
+    constexpr int N = 16 / sizeof(T);
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+        if constexpr (PAST) x[i] = load_past(p + (i * THREADS + threadIdx.x) * N);
+        else __builtin_memcpy(&x[i], p + (i * THREADS + threadIdx.x) * N, 16);
+    }
+}
+
+// f(gradient, first element, elements, whether to read past the caches) for the tiles of a list that are this workgroup's
 template <bool BACK, class F> __device__ __forceinline__ void each_tile(const ClipList &l, F f)
 {
     const uint32_t tiles = l.tile[l.n];
@@ -35,11 +54,11 @@ template <bool BACK, class F> __device__ __forceinline__ void each_tile(const Cl
         while (l.tile[i + 1] <= t) ++i;
         const int size = l.half[i] ? 2 : 4;
         const long long at = (long long)(BACK ? l.tile[i + 1] - 1 - t : t - l.tile[i]) * (CLIP_TILE / size), left = l.count[i] - at;
-        f(i, at, (int)(left < CLIP_TILE / size ? left : CLIP_TILE / size));
+        f(i, at, (int)(left < CLIP_TILE / size ? left : CLIP_TILE / size), BACK ? t >= l.past : t < l.past);
     }
 }
 
-template <class T> __device__ __forceinline__ double squares_of(const T *p, int len)
+template <bool PAST, class T> __device__ __forceinline__ double squares_of(const T *p, int len)
 {
     constexpr int N = 16 / sizeof(T);
     double sum = 0;
@@ -47,10 +66,9 @@ template <class T> __device__ __forceinline__ double squares_of(const T *p, int 
 #pragma unroll
         for (int e = 0; e < N; ++e) { const double y = wide(x.v[e]); sum = fma(y, y, sum); }
     };
-    if (len == CLIP_TILE / (int)sizeof(T)) {          // a whole tile: all its loads at once
+    if (len == CLIP_TILE / (int)sizeof(T)) {
         Vector<T> x[LOADS];
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) __builtin_memcpy(&x[i], p + (i * THREADS + threadIdx.x) * N, 16);
+        load_tile<PAST>(x, p);
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) add(x[i]);
         return sum;
@@ -84,12 +102,15 @@ __device__ __forceinline__ double sum_of_sums(const double *sums, int n, double 
     return sum_of_all(v, s);
 }
 
-// Bound by memory: 5.57 TB/s for 494 million bf16 elements, in three launches.
+// Bound by memory: 494 million bf16 elements at 6.3 TB/s, 5.6 where none of them is in the last-level cache.
 __global__ __launch_bounds__(THREADS) void squares_kernel(ClipList l, double *sums)
 {
     __shared__ double s[WAVES];
     double sum = 0;
-    each_tile<false>(l, [&](int i, long long at, int len) { sum += l.half[i] ? squares_of((const bf16_t *)l.in[i] + at, len) : squares_of((const float *)l.in[i] + at, len); });
+    each_tile<false>(l, [&](int i, long long at, int len, bool past) {
+        if (l.half[i]) sum += past ? squares_of<true>((const bf16_t *)l.in[i] + at, len) : squares_of<false>((const bf16_t *)l.in[i] + at, len);
+        else sum += past ? squares_of<true>((const float *)l.in[i] + at, len) : squares_of<false>((const float *)l.in[i] + at, len);
+    });
     sum = sum_of_all(sum, s);
     if (threadIdx.x == 0) sums[blockIdx.x] = sum;
 }
@@ -104,7 +125,7 @@ __global__ __launch_bounds__(THREADS) void join_kernel(const double *sums, int n
     }
 }
 
-template <class T> __device__ __forceinline__ void scale_tile(const T *p, T *q, int len, float by)
+template <bool PAST, class T> __device__ __forceinline__ void scale_tile(const T *p, T *q, int len, float by)
 {
     constexpr int N = 16 / sizeof(T);
     const auto scale = [&](Vector<T> &x) {
@@ -113,8 +134,7 @@ template <class T> __device__ __forceinline__ void scale_tile(const T *p, T *q, 
     };
     if (len == CLIP_TILE / (int)sizeof(T)) {
         Vector<T> x[LOADS];
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) __builtin_memcpy(&x[i], p + (i * THREADS + threadIdx.x) * N, 16);
+        load_tile<PAST>(x, p);
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             scale(x[i]);
@@ -135,17 +155,21 @@ template <class T> __device__ __forceinline__ void scale_tile(const T *p, T *q, 
 }
 
 // Bound by memory: what was squared last is scaled first, as it may still be in the last-level cache, and stores go past it. (136 million bf16 elements into a buffer, squares included: 165 us
-// forwards, 153 backwards, 127 with such stores.)
+// forwards, 153 backwards, 127 with such stores, 124 with loads as clip.h has them.)
 __global__ __launch_bounds__(THREADS) void scale_kernel(ClipList l, const double *sums, int n, double max_norm, float *norm)
 {
     __shared__ double s[WAVES];
     const double length = sqrt(sum_of_sums(sums, n, s));
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)length;
     const float by = length > max_norm && length < INFINITY ? (float)(max_norm / length) : 1.f;      // (infinity, NaN: 1)
-    each_tile<true>(l, [&](int i, long long at, int len) {
+    each_tile<true>(l, [&](int i, long long at, int len, bool past) {
         if (by == 1.f && l.in[i] == l.out[i]) return;      // as they are
-        if (l.half[i]) scale_tile((const bf16_t *)l.in[i] + at, (bf16_t *)l.out[i] + at, len, by);
-        else scale_tile((const float *)l.in[i] + at, (float *)l.out[i] + at, len, by);
+        const auto scale = [&](const auto *p, auto *q) {
+            if (past) scale_tile<true>(p + at, q + at, len, by);
+            else scale_tile<false>(p + at, q + at, len, by);
+        };
+        if (l.half[i]) scale((const bf16_t *)l.in[i], (bf16_t *)l.out[i]);
+        else scale((const float *)l.in[i], (float *)l.out[i]);
     });
 }
 
