@@ -16,6 +16,7 @@ constexpr int PICK_ONE = PICK_GROUP;                      // most tokens of a ro
 constexpr int PICK_ROWS = 1024;
 constexpr int PICK_LISTED = 8192;                         // most tokens of a row that parts leave, and that the deciding workgroup holds
 constexpr int PICK_PART_LISTED = 128;                     // of one part
+constexpr size_t PICK_KEEP = 192 << 20;                   // bytes of logits that a last-level cache may still hold when they are read again
 constexpr int PICK_STEPS = 256;                           // of a histogram of masses over the logits of a row (256 rows of 152064, some of them flat: 127 us, with 128 steps 131, with 512 133)
 
 struct alignas(16) PickHead {
@@ -44,6 +45,9 @@ struct PickArgs {
     int unit;                        // masses are in units of 2^-unit: vocab of them stay below 2^63
     int groups, listed;              // workgroups a row, tokens a part may leave
     int listed_lanes;                // lanes whose largest token is among them
+    // Logits are read past the caches where nothing reads them again, or where they do not fit (the largest 64 of 1024 rows of 151936: 119 instead of 125 us, after they were written 122 instead
+    // of 189; where rows may be searched 256 bf16 rows take 127 through the caches and 129 past them)
+    bool past;
     // draws: a number a row, or the value for all
     const float *u, *temperatures, *top_ps, *min_ps;
     const int *top_ks;

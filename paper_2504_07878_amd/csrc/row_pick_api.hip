@@ -93,6 +93,7 @@ template <class Launch> int enqueue(const PickArgs &all, Launch launch)
     for (int at = 0; at < all.rows; at += most) {
         PickArgs a = all;
         a.rows = std::min(most, all.rows - at);
+        a.past = !a.queue || a.rows * (size_t)a.vocab * size > PICK_KEEP;
         a.logits = (const char *)all.logits + (size_t)at * all.stride * size;
         for (const float **p : {&a.u, &a.temperatures, &a.top_ps, &a.min_ps}) if (*p) *p += at;
         if (a.top_ks) a.top_ks += at;

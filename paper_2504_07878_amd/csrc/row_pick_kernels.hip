@@ -18,6 +18,7 @@ namespace tr {
 namespace {
 
 typedef unsigned long long u64;
+typedef __attribute__((ext_vector_type(4), aligned(2))) uint32_t u32x4_any;
 
 constexpr int THREADS = PICK_THREADS, WAVES = PICK_WAVES, EACH = PICK_PART / 64;
 constexpr int DECIDERS = 512;      // threads of a workgroup that decides on a row (1024: 9.6 instead of 7.8 us for one row)
@@ -682,11 +683,17 @@ template <class T> struct Part {
     __device__ __forceinline__ uint32_t id(int e) const { return at(e / N) + e % N; }
     __device__ __forceinline__ float &logit(int e) const { return z[e / 4][threadIdx.x % 64][e % 4]; }
     // returns the largest of the lane's
-    __device__ __forceinline__ float load(const T *logits)
+    template <bool PAST = false> __device__ __forceinline__ float load(const T *logits)
     {
         T raw[BLOCKS][N];
 #pragma unroll
-        for (int i = 0; i < BLOCKS; ++i) __builtin_memcpy(raw[i], (const char *)logits + at(i) * (uint32_t)sizeof(T), 16);
+        for (int i = 0; i < BLOCKS; ++i) {
+            const char *const p = (const char *)logits + at(i) * (uint32_t)sizeof(T);
+            u32x4_any v;
+            if constexpr (PAST) v = __builtin_nontemporal_load((const u32x4_any *)p);
+            else __builtin_memcpy(&v, p, 16);
+            __builtin_memcpy(raw[i], &v, 16);
+        }
         // (the last lane's last load ends within the row: so do all)
         const bool whole = __builtin_amdgcn_readlane((int)(first + (BLOCKS - 1) * step), 63) + N <= vocab;
         float most = -INFINITY;
@@ -732,7 +739,7 @@ template <class T> struct Part {
 
 // Bound by its instructions where sums are wanted: 35 a token and lane with the list, 22 without, half of them 64-bit ones for the weight (256 rows of 152064 bf16 logits 44 us, 64 free fp32 rows 12).
 // Without sums 13, bound by memory (1024 rows of 151936 fp32 logits 107 us, 5.8 TB/s). 16 tokens a lane: with 32 fewer wavefronts wait for the loads at once.
-template <class T, bool TOP> __global__ __launch_bounds__(THREADS, 8) void parts_kernel(PickArgs a)
+template <class T, bool TOP, bool PAST> __global__ __launch_bounds__(THREADS, 8) void parts_kernel(PickArgs a)
 {
     __shared__ float s_z[WAVES][EACH / 4][64][4];
     __shared__ uint2 s_powers[32];
@@ -743,7 +750,7 @@ template <class T, bool TOP> __global__ __launch_bounds__(THREADS, 8) void parts
     using P = Part<T>;
     if (a.queue && blockIdx.x == 0 && threadIdx.x == 0) a.queue[0] = 0;
     P p{s_z[wave], (uint32_t)part * (row.cut ? P::BLOCK : PICK_PART) + lane * P::N, (uint32_t)(row.cut ? parts * P::BLOCK : P::BLOCK), a.vocab};
-    const uint32_t lane_top = key_of(p.load((const T *)a.logits + (long long)r * a.stride));
+    const uint32_t lane_top = key_of(p.template load<PAST>((const T *)a.logits + (long long)r * a.stride));
     if (row.summed) load_powers(s_powers);
     PickHead head{};
     head.top = wave_max(lane_top);
@@ -1196,7 +1203,8 @@ template <class T> __global__ __launch_bounds__(DECIDERS) void finish_kernel(Pic
 template <class T, bool TOP> void launch_parts(hipStream_t s, const PickArgs &a)
 {
     const unsigned all = (unsigned)a.rows * a.groups;
-    hipLaunchKernelGGL((parts_kernel<T, TOP>), dim3(all), dim3(THREADS), 0, s, a);
+    if (a.past) hipLaunchKernelGGL((parts_kernel<T, TOP, true>), dim3(all), dim3(THREADS), 0, s, a);
+    else hipLaunchKernelGGL((parts_kernel<T, TOP, false>), dim3(all), dim3(THREADS), 0, s, a);
     if (a.groups * WAVES * a.listed <= 4096) hipLaunchKernelGGL((decide_kernel<T, TOP, false, 4096>), dim3(a.rows), dim3(DECIDERS), 0, s, a);
     else hipLaunchKernelGGL((decide_kernel<T, TOP, false, PICK_LISTED>), dim3(a.rows), dim3(DECIDERS), 0, s, a);
     if constexpr (!TOP) {
