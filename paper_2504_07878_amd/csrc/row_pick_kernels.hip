@@ -738,7 +738,7 @@ template <class T> struct Part {
 };
 
 // Bound by its instructions where sums are wanted: 35 a token and lane with the list, 22 without, half of them 64-bit ones for the weight (256 rows of 152064 bf16 logits 44 us, 64 free fp32 rows 12).
-// Without sums 13, bound by memory (1024 rows of 151936 fp32 logits 107 us, 5.8 TB/s). 16 tokens a lane: with 32 fewer wavefronts wait for the loads at once.
+// Without sums 13, bound by memory (1024 rows of 151936 fp32 logits 104 us, 6 TB/s). 16 tokens a lane: with 32 fewer wavefronts wait for the loads at once.
 template <class T, bool TOP, bool PAST> __global__ __launch_bounds__(THREADS, 8) void parts_kernel(PickArgs a)
 {
     __shared__ float s_z[WAVES][EACH / 4][64][4];
