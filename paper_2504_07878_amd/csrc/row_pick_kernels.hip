@@ -266,7 +266,7 @@ template <class Each, class S> __device__ __forceinline__ Border find_border(Eac
             const int shift = max(0, bits - BIN_BITS);
             b = border_step(each, b.place, bits, shift, b.before, want, s);
             bits = shift;
-        }
+        } else __syncthreads();      // (others may still read what the caller counted in s.entries)
         if (!b.found || bits == 0) return b;
         stepped = false;
         const uint32_t most = bits >= 32 ? ANY : (1u << bits) - 1;

@@ -1,0 +1,69 @@
+"""The kernels of draws, largest logits, gradient norm and clipping on the CPU (lockstep.py), no GPU needed: wavefronts that get ahead of each other, and ends of the ranges that are the same on either."""
+import numpy as np
+import pytest
+
+import lockstep
+import picks
+
+
+@pytest.fixture(scope="module")
+def host(tmp_path_factory):
+    return lockstep.build(str(tmp_path_factory.mktemp("lanes")))
+
+
+def rows_of(kind, n, v, seed, half=False):
+    """peaked: a body and a few tokens far above it; flat: a body alone; ties: a body in steps of 1/8; together: the largest are neighbours; equal: one value; masked: most is -inf. half: bits of bfloat16."""
+    g = np.random.Generator(np.random.Philox(seed))
+    z = g.standard_normal((n, v), dtype=np.float32)
+    if kind == "peaked":
+        z = z * 2 + np.where(g.random((n, v)) < 20 / v, g.uniform(6, 14, (n, v)), 0)
+    elif kind == "ties":
+        z = np.round(z * 8) / 8
+    elif kind == "together":
+        z[:, v // 3:v // 3 + 700] += 9
+    elif kind == "equal":
+        z[:] = 1.5
+    elif kind == "masked":
+        z[g.random((n, v)) < 0.97] = -np.inf
+        z[0] = -np.inf
+    z = np.ascontiguousarray(z, dtype=np.float32)
+    return (z.view(np.uint32) >> 16).astype(np.uint16) if half else z
+
+
+def values(z):
+    return (z.astype(np.uint32) << 16).view(np.float32) if z.dtype == np.uint16 else z
+
+
+def check(z, u, how, token, logprob):
+    how = dict(temperature=1.0, top_k=0, top_p=1.0, min_p=0.0) | how
+    t, p, m = (float(np.float32(how[x])) for x in ("temperature", "top_p", "min_p"))
+    for i, row in enumerate(values(z)):
+        assert picks.check_draw(row, u[i], t, how["top_k"], p, m, token[i], logprob[i]), (i, how, u[i], token[i], logprob[i])
+
+
+# what each reaches: filters that end among few tokens, among more than are compared all with all (top-p 0.9, top-k 100 of neighbours), among equal ones (ties at top-k's border, a few or many), below
+# what the parts of a row have listed (flat rows, through the queue), and nothing cut
+SETTINGS = [dict(), dict(top_k=20), dict(top_p=0.9), dict(top_k=200, top_p=0.95), dict(top_k=700), dict(min_p=0.05), dict(top_k=700, min_p=0.01), dict(top_p=0.99, min_p=0.02, temperature=1.5), dict(top_p=0.999),
+            dict(temperature=0.0)]
+
+
+@pytest.mark.parametrize("order", lockstep.ORDERS)
+@pytest.mark.parametrize("kind", ["peaked", "flat", "ties", "together", "equal", "masked"])
+@pytest.mark.parametrize("v", [257, 3001, 9001, 20001])
+def test_a_wavefront_that_is_ahead_of_the_others_changes_no_draw(host, v, kind, order):
+    for i, how in enumerate(SETTINGS):
+        z, u = rows_of(kind, 3, v, 100 * v + i, half=i % 3 == 2), np.random.Generator(np.random.Philox(i)).random(3, dtype=np.float32)
+        check(z, u, how, *host.sample(z, u, order, **how))
+
+
+@pytest.mark.parametrize("order", lockstep.ORDERS)
+@pytest.mark.parametrize("kind", ["peaked", "flat", "ties", "together", "equal", "masked"])
+@pytest.mark.parametrize("v", [257, 3001, 20001])
+def test_a_wavefront_that_is_ahead_of_the_others_changes_no_list(host, v, kind, order):
+    for k in (5, 60, 300, 1000):
+        z = rows_of(kind, 2, v, v + k, half=k == 60)
+        ids, got = host.top(z, k, order)
+        for row, i, x in zip(values(z), ids, got):
+            want = picks.order_of(row)[:k]
+            assert np.array_equal(i, np.concatenate([want, np.full(k - len(want), -1)]))
+            assert np.array_equal(x, np.concatenate([row[want], np.full(k - len(want), -np.inf, np.float32)]))
