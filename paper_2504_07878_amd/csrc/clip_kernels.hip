@@ -160,8 +160,9 @@ __global__ __launch_bounds__(THREADS) void scale_kernel(ClipList l, const double
 {
     __shared__ double s[WAVES];
     const double length = sqrt(sum_of_sums(sums, n, s));
-    if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)length;
-    const float by = length > max_norm && length < INFINITY ? (float)(max_norm / length) : 1.f;      // (infinity, NaN: 1)
+    const float said = (float)length;
+    if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = said;
+    const float by = length > max_norm && said < INFINITY ? (float)(max_norm / length) : 1.f;      // (infinity, lengths that 32 bits do not hold, NaN: 1)
     each_tile<true>(l, [&](int i, long long at, int len, bool past) {
         if (by == 1.f && l.in[i] == l.out[i]) return;      // as they are
         const auto scale = [&](const auto *p, auto *q) {

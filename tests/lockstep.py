@@ -70,3 +70,18 @@ class Library:
     def launches(self, part):
         """Launches of kernels of that name in the last call."""
         return self.lib.lanes_launches(part.encode())
+
+    def clip(self, grads, max_norm, out=None, order=0):
+        """grads: flat arrays, float32 or the bit patterns of bfloat16 (uint16); out: the same. None: in place; max_norm None: the norm alone."""
+        n, tr = len(grads), self.tr
+        at = lambda arrays: (C.c_void_p * n)(*[x.ctypes.data for x in arrays])   # noqa: E731
+        counts, types = (C.c_int64 * n)(*[x.size for x in grads]), (C.c_int32 * n)(*[tr.BF16 if x.dtype == np.uint16 else tr.F32 for x in grads])
+        ws, norm = room(self.lib.tr_grad_workspace_bytes()), np.full(1, 77, np.float32)
+        ends = C.c_void_p(ws.ctypes.data), C.c_size_t(ws.nbytes), None, n, at(grads)
+        self.lib.lanes_order(order)
+        self.lib.lanes_launches(None)
+        if max_norm is None:
+            self._done(self.lib.tr_grad_norm(*ends, counts, types, C.c_void_p(norm.ctypes.data)))
+        else:
+            self._done(self.lib.tr_grad_clip(*ends, at(grads if out is None else out), counts, types, C.c_float(max_norm), C.c_void_p(norm.ctypes.data)))
+        return norm[0]

@@ -78,6 +78,14 @@ def test_gradients_that_are_not_finite_stay_as_they_are(clipping, bad):
     assert all(torch.equal(a.nan_to_num(5.0), b.nan_to_num(5.0)) for a, b in zip(mine, grads))
 
 
+def test_gradients_whose_norm_is_beyond_32_bits_stay_as_they_are(clipping):
+    """100 elements of 2^127 are 2^130 long: the norm that the call reports is infinite."""
+    grads = [torch.full((100,), 2.0 ** 127, device="cuda"), torch.ones(33, device="cuda", dtype=torch.bfloat16)]
+    mine, out, c = [t.clone() for t in grads], [torch.full_like(t, 7) for t in grads], clipping.Clipper()
+    assert float(c.clip(mine, 1.0)) == float(c.clip(grads, 1.0, out=out)) == float("inf")
+    assert all(torch.equal(a, b) and torch.equal(a, x) for a, b, x in zip(mine, out, grads))
+
+
 def test_alignment_order_of_dimensions_and_what_lies_beside(clipping):
     c = clipping.Clipper()
     for dtype in (torch.float32, torch.bfloat16):

@@ -67,3 +67,20 @@ def test_a_wavefront_that_is_ahead_of_the_others_changes_no_list(host, v, kind, 
             want = picks.order_of(row)[:k]
             assert np.array_equal(i, np.concatenate([want, np.full(k - len(want), -1)]))
             assert np.array_equal(x, np.concatenate([row[want], np.full(k - len(want), -np.inf, np.float32)]))
+
+
+def halved(x):
+    """Bits of bfloat16, of values that have them."""
+    return (np.ascontiguousarray(x, dtype=np.float32).view(np.uint32) >> 16).astype(np.uint16)
+
+
+@pytest.mark.parametrize("inside", [False, True])
+def test_gradients_whose_norm_is_beyond_32_bits_stay_as_they_are(host, inside):
+    """The norm that the call reports says which case it is: infinite (100 elements of 2^127 are 2^130 long), and nothing is scaled."""
+    grads = [np.full(100, 2.0 ** 127, np.float32), halved(np.full(33, -1.5)), np.ones(7, np.float32)]
+    before, out = [x.copy() for x in grads], None if inside else [np.full_like(x, 7) for x in grads]
+    assert host.clip(grads, 1.0, out) == np.inf
+    assert all(np.array_equal(a, b) for a, b in zip(grads if inside else out, before))
+    # at the last length that 32 bits hold they are
+    grads = [np.full(2, 2.0 ** 127, np.float32)]
+    assert host.clip(grads, 1.0) == np.float32(2.0 ** 127.5) and np.allclose(grads[0], 0.5 ** 0.5, rtol=2 ** -22, atol=0)
