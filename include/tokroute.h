@@ -386,7 +386,7 @@ int tr_top(const tr_pick_config *cfg, void *workspace, size_t workspace_bytes, v
 /* ------------------------------------------------------------------ the length of many gradients, and its clipping
  *
  * norm = sqrt(sum of the squares of all elements of all gradients); tr_grad_clip: out[i] = grads[i] * min(1, max_norm / norm). Squares and sums are 64-bit, in an order that the
- * sizes alone decide: the same gradients give the same bits. Elements are multiplied in 32 bits and rounded once. Where the norm that the call reports
+ * sizes alone decide: the same gradients give the same bits. The scale has 24 bits, however small it is; elements are multiplied in 32 bits and rounded once. Where the norm that the call reports
  * is infinite (a length that 32 bits do not hold is) or NaN the gradients stay as they are.
  *
  * n gradients; grads, out, counts, dtypes are HOST arrays [n], read before the call returns: DEVICE pointers (aligned to their elements; of count 0: any), elements (0 .. 2^40), TR_F32 /

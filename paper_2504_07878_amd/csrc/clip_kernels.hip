@@ -2,6 +2,8 @@
 // squares would lose gradients below 1e-23 and overflow from 1e19 on.
 #include "clip.h"
 
+#include <float.h>
+
 namespace tr {
 
 namespace {
@@ -125,12 +127,20 @@ __global__ __launch_bounds__(THREADS) void join_kernel(const double *sums, int n
     }
 }
 
-template <bool PAST, class T> __device__ __forceinline__ void scale_tile(const T *p, T *q, int len, float by)
+// by * 2^shift: a scale below 2^-126 keeps all its bits
+struct Scale {
+    float by;
+    int shift;
+    __device__ __forceinline__ float operator()(float v) const { return ldexpf(v * by, shift); }
+    __device__ __forceinline__ bool none() const { return by == 1.f && shift == 0; }
+};
+
+template <bool PAST, class T> __device__ __forceinline__ void scale_tile(const T *p, T *q, int len, Scale by)
 {
     constexpr int N = 16 / sizeof(T);
     const auto scale = [&](Vector<T> &x) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) put(x.v[e], wide(x.v[e]) * by);
+        for (int e = 0; e < N; ++e) put(x.v[e], by(wide(x.v[e])));
     };
     if (len == CLIP_TILE / (int)sizeof(T)) {
         Vector<T> x[LOADS];
@@ -149,7 +159,7 @@ template <bool PAST, class T> __device__ __forceinline__ void scale_tile(const T
             scale(x);
             __builtin_memcpy(q + i, &x, 16);
         } else {
-            for (int e = i; e < len; ++e) put(q[e], wide(p[e]) * by);
+            for (int e = i; e < len; ++e) put(q[e], by(wide(p[e])));
         }
     }
 }
@@ -162,9 +172,12 @@ __global__ __launch_bounds__(THREADS) void scale_kernel(ClipList l, const double
     const double length = sqrt(sum_of_sums(sums, n, s));
     const float said = (float)length;
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = said;
-    const float by = length > max_norm && said < INFINITY ? (float)(max_norm / length) : 1.f;      // (infinity, lengths that 32 bits do not hold, NaN: 1)
+    double ratio = length > max_norm && said < INFINITY ? max_norm / length : 1.0;      // (infinity, lengths that 32 bits do not hold, NaN: 1)
+    int shift = 0;
+    if (ratio < FLT_MIN) ratio = frexp(ratio, &shift);
+    const Scale by{(float)ratio, shift};
     each_tile<true>(l, [&](int i, long long at, int len, bool past) {
-        if (by == 1.f && l.in[i] == l.out[i]) return;      // as they are
+        if (by.none() && l.in[i] == l.out[i]) return;      // as they are
         const auto scale = [&](const auto *p, auto *q) {
             if (past) scale_tile<true>(p + at, q + at, len, by);
             else scale_tile<false>(p + at, q + at, len, by);

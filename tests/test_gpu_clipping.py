@@ -86,6 +86,15 @@ def test_gradients_whose_norm_is_beyond_32_bits_stay_as_they_are(clipping):
     assert all(torch.equal(a, b) and torch.equal(a, x) for a, b, x in zip(mine, out, grads))
 
 
+@pytest.mark.parametrize("max_norm, size", [(1e-8, 1e37), (1e-30, 1e15), (3e-38, 2e30), (1e-44, 1e36)])
+def test_scales_below_what_32_bits_hold(clipping, max_norm, size):
+    """max_norm / norm is subnormal in 32 bits, or zero, where the products are not. Results below 2^-126 are off by half of 2^-149 (bfloat16: 2^-133) twice at most: `tiny` of check. max_norm
+    is the float32 that it is handed over as."""
+    grads, max_norm = [x * size for x in some([(300, 70), 11], (torch.float32, torch.bfloat16), scale=0.01)], float(np.float32(max_norm))
+    mine = [t.clone() for t in grads]
+    check(mine, grads, clipping.Clipper().clip(mine, max_norm), max_norm)
+
+
 def test_alignment_order_of_dimensions_and_what_lies_beside(clipping):
     c = clipping.Clipper()
     for dtype in (torch.float32, torch.bfloat16):

@@ -84,3 +84,21 @@ def test_gradients_whose_norm_is_beyond_32_bits_stay_as_they_are(host, inside):
     # at the last length that 32 bits hold they are
     grads = [np.full(2, 2.0 ** 127, np.float32)]
     assert host.clip(grads, 1.0) == np.float32(2.0 ** 127.5) and np.allclose(grads[0], 0.5 ** 0.5, rtol=2 ** -22, atol=0)
+
+
+@pytest.mark.parametrize("max_norm, size", [(1e-8, 1e37), (1e-3, 3e37), (1e-30, 1e15), (3e-38, 2e30), (1e-44, 1e38), (0.25, 2e37)])
+def test_scales_below_what_32_bits_hold(host, max_norm, size):
+    """max_norm / norm is subnormal in 32 bits, or zero, where the products are not. The scale and the product are rounded to 24 bits, bfloat16 to 8 then; results below 2^-126 are off by half
+    of 2^-149 (bfloat16: 2^-133) twice. max_norm is the float32 that it is handed over as."""
+    g = np.random.Generator(np.random.Philox(5))
+    grads = [(g.uniform(-1, 1, 300) * size).astype(np.float32), halved(g.uniform(-1, 1, 77) * size), np.array([0.0, -0.0, 1e-30, size], np.float32)]
+    wide = [values(x).astype(np.float64) for x in grads]
+    length, max_norm = np.sqrt(sum((x * x).sum() for x in wide)), float(np.float32(max_norm))
+    out = [np.full_like(x, 7) for x in grads]
+    held = length <= np.finfo(np.float32).max          # (two of the lengths are beyond 32 bits)
+    norm = host.clip(grads, max_norm, out)
+    assert abs(norm / length - 1) <= 2.0 ** -23 if held else norm == np.inf
+    for got, x in zip(out, wide):
+        want, half = x * (max_norm / length if held else 1.0), got.dtype == np.uint16
+        off = np.abs(values(got).astype(np.float64) - want)
+        assert (off <= np.abs(want) * ((2.0 ** -8 if half else 0) + 3.1 * 2.0 ** -24) + (2.0 ** -133 if half else 0) + 2.0 ** -149).all()
