@@ -125,7 +125,7 @@ int tr_sample(const tr_pick_config *cfg, void *workspace, size_t workspace_bytes
     if (!a.rows) return TR_OK;
     if (!how->u || !token || !logprob) return TR_ERR_INVALID_ARG;
     a.u = how->u; a.temperatures = how->temperatures; a.top_ks = how->top_ks; a.top_ps = how->top_ps; a.min_ps = how->min_ps;
-    a.temperature = how->temperature; a.top_k = how->top_k; a.top_p = how->top_p; a.min_p = how->min_p;
+    a.temperature = how->temperature; a.top_k = how->top_k < a.vocab ? how->top_k : 0; a.top_p = how->top_p; a.min_p = how->min_p;
     a.token = token; a.logprob = logprob;
     // (top-k ends within what the parts list but for rows whose largest logits lie oddly; one workgroup searches these)
     if (!(a.top_ps || a.min_ps || a.top_p < 1.f || a.min_p > 0.f) || !(a.top_ks || a.top_k == 0)) a.queue = nullptr;

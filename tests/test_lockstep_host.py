@@ -102,3 +102,15 @@ def test_scales_below_what_32_bits_hold(host, max_norm, size):
         want, half = x * (max_norm / length if held else 1.0), got.dtype == np.uint16
         off = np.abs(values(got).astype(np.float64) - want)
         assert (off <= np.abs(want) * ((2.0 ** -8 if half else 0) + 3.1 * 2.0 ** -24) + (2.0 ** -133 if half else 0) + 2.0 ** -149).all()
+
+
+@pytest.mark.parametrize("how", [dict(top_p=0.9), dict(min_p=0.01), dict(top_p=0.95, min_p=0.001)])
+@pytest.mark.parametrize("more", [0, 1, 2**31 - 1 - 9001])
+def test_a_top_k_of_all_tokens_is_none(host, how, more):
+    """Flat rows go the way that they go without top-k, read by all workgroups rather than by one."""
+    z, u = rows_of("flat", 3, 9001, 3), np.float32([0.1, 0.5, 0.9])
+    without = host.sample(z, u, **how)
+    assert host.launches("steps_kernel") == 1
+    got = host.sample(z, u, **how, top_k=9001 + more)
+    assert host.launches("steps_kernel") == 1 and all(np.array_equal(a, b) for a, b in zip(got, without))
+    check(z, u, how, *got)
