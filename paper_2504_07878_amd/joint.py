@@ -30,9 +30,14 @@ class _Tokens:
             self.sampler, self.draw, self.numbers = sampling.Sampler(rows, vocab, device=model.device), asdict(draw), numbers.to(model.device)
 
     def __call__(self, out, sequences, positions):
-        """Row i of the outputs is sequences[i]'s token at positions[i]."""
-        if self.wanted and self.numbers.shape[1]:
-            self.sampler.sample(out.logits[:, :self.vocab], self.numbers[sequences, positions], token=out.token, **self.draw)
+        """Row i of the outputs is sequences[i]'s token at positions[i]. Only enqueues: the host does not wait for the call that the outputs are of."""
+        count = self.numbers.shape[1] if self.wanted else 0
+        if count:
+            import torch
+            at = torch.empty(len(sequences), dtype=torch.int64, pin_memory=True)     # (from pageable memory the copy would wait for the stream)
+            at.numpy()[:] = [b * count + t for b, t in zip(sequences, positions)]
+            u = self.numbers.view(-1).index_select(0, at.to(self.numbers.device, non_blocking=True))
+            self.sampler.sample(out.logits[:, :self.vocab], u, token=out.token, **self.draw)
         return out
 
 

@@ -67,6 +67,29 @@ def test_the_same_numbers_the_same_tokens(models):
     assert np.array_equal(first, again) and not np.array_equal(first, other)
 
 
+def test_a_draw_does_not_wait_for_the_model(models):
+    """The host goes on while the call whose logits are drawn from is still at work (here: products behind it on its stream that take a tenth of a second), as the overlapped schedule needs."""
+    from paper_2504_07878_amd import joint, sampling
+    s, slm, llm, prompts, numbers = models
+    _, large = joint._choosers(slm, llm, B, NEW, sampling.Draw(temperature=0.9), numbers)
+    side, busy, to = torch.cuda.Stream(), torch.zeros((8192, 8192), device="cuda", dtype=torch.bfloat16), torch.empty((8192, 8192), device="cuda", dtype=torch.bfloat16)
+    tokens, waits = [], []
+    side.wait_stream(torch.cuda.current_stream())
+    for products in (1, 200):      # once for what is allocated
+        with torch.cuda.stream(side):
+            out = llm.prefill(list(range(B)), prompts, want_logits=True)
+            for _ in range(products):
+                torch.mm(busy, busy, out=to)
+            done = torch.cuda.Event()
+            done.record()
+            large(out, list(range(B)), [3] * B)
+        waits.append(done.query())
+        side.synchronize()
+        tokens.append(out.token.cpu())
+    assert not waits[1]
+    assert torch.equal(*tokens)
+
+
 def test_drawn_sequences_to_a_new_head(models):
     """The run as a whole: draws, rows with the teacher's largest logits, and steps of clipped gradients."""
     from paper_2504_07878_amd import adapt, joint, sampling
