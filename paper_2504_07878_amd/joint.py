@@ -136,36 +136,38 @@ def generate_overlapped(slm, llm, prompts, max_new: int, draw=None, numbers=None
     small, large = _choosers(slm, llm, B, max_new, draw, numbers)
     start, was_shared = torch.cuda.current_stream(), slm.shared
     s_small.wait_stream(start); s_large.wait_stream(start)
-    with torch.cuda.stream(s_small):
-        take(list(range(B)), small(slm.prefill(list(range(B)), prompts, want_logits=small.wanted), list(range(B)), [0] * B).cpu(NEEDED, stream_only=True))
-    while inflight or pending or any(running):
-        if inflight and (inflight[2].query() or not any(running)):
-            bs, _, ev = inflight
-            ev.synchronize()
-            for i, b in enumerate(bs):
-                llm_len[b] = len(seq[b])
-                emit(b, int(host_tok[i]), True)
-            inflight = None
-        if not inflight and pending:
-            first = [b for b in pending if llm_len[b] == 0]
-            later = [b for b in pending if llm_len[b] > 0]
-            keep = []
-            with torch.cuda.stream(s_large):
-                if first:
-                    keep.append(large(llm.prefill(first, [seq[b] for b in first], want_logits=large.wanted), first, [done[b] for b in first]))
-                    host_tok[:len(first)].copy_(keep[-1].token[:len(first)], non_blocking=True)
-                if later:
-                    keep.append(large(llm.extend(later, [seq[b][llm_len[b]:] for b in later], want_logits=large.wanted), later, [done[b] for b in later]))
-                    host_tok[len(first):len(first) + len(later)].copy_(keep[-1].token[:len(later)], non_blocking=True)
-                ev = torch.cuda.Event()
-                ev.record(s_large)
-            inflight = (first + later, keep, ev)
-            pending = []
-        run = [b for b in range(B) if running[b]]
-        if run:
-            slm.set_shared(was_shared or inflight is not None)
-            with torch.cuda.stream(s_small):
-                take(run, small(slm.decode_step(run, next_tok[run], want_logits=small.wanted), run, [done[b] for b in run]).cpu(NEEDED, stream_only=True))
-    slm.set_shared(was_shared)
-    start.wait_stream(s_small); start.wait_stream(s_large)
+    try:
+        with torch.cuda.stream(s_small):
+            take(list(range(B)), small(slm.prefill(list(range(B)), prompts, want_logits=small.wanted), list(range(B)), [0] * B).cpu(NEEDED, stream_only=True))
+        while inflight or pending or any(running):
+            if inflight and (inflight[2].query() or not any(running)):
+                bs, _, ev = inflight
+                ev.synchronize()
+                for i, b in enumerate(bs):
+                    llm_len[b] = len(seq[b])
+                    emit(b, int(host_tok[i]), True)
+                inflight = None
+            if not inflight and pending:
+                first = [b for b in pending if llm_len[b] == 0]
+                later = [b for b in pending if llm_len[b] > 0]
+                keep = []
+                with torch.cuda.stream(s_large):
+                    if first:
+                        keep.append(large(llm.prefill(first, [seq[b] for b in first], want_logits=large.wanted), first, [done[b] for b in first]))
+                        host_tok[:len(first)].copy_(keep[-1].token[:len(first)], non_blocking=True)
+                    if later:
+                        keep.append(large(llm.extend(later, [seq[b][llm_len[b]:] for b in later], want_logits=large.wanted), later, [done[b] for b in later]))
+                        host_tok[len(first):len(first) + len(later)].copy_(keep[-1].token[:len(later)], non_blocking=True)
+                    ev = torch.cuda.Event()
+                    ev.record(s_large)
+                inflight = (first + later, keep, ev)
+                pending = []
+            run = [b for b in range(B) if running[b]]
+            if run:
+                slm.set_shared(was_shared or inflight is not None)
+                with torch.cuda.stream(s_small):
+                    take(run, small(slm.decode_step(run, next_tok[run], want_logits=small.wanted), run, [done[b] for b in run]).cpu(NEEDED, stream_only=True))
+    finally:                               # (after an error too: what is under way ends before what the caller enqueues next)
+        slm.set_shared(was_shared)
+        start.wait_stream(s_small); start.wait_stream(s_large)
     return tokens, routed

@@ -90,6 +90,42 @@ def test_a_draw_does_not_wait_for_the_model(models):
     assert torch.equal(*tokens)
 
 
+def test_an_error_leaves_the_streams_joined(models, monkeypatch):
+    """A step fails while the large model is at work (products behind its call take a tenth of a second): what the caller enqueues next comes after that, and the small model is as it was."""
+    from paper_2504_07878_amd import joint
+    s, slm, llm, prompts, numbers = models
+    busy, to = (torch.zeros((8192, 8192), device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    made, stream, prefill = [], torch.cuda.Stream, llm.prefill
+
+    def streams(*a, **k):
+        x = stream(*a, **k)
+        made.extend([] if a or k else [x])      # (current streams are made with their handle)
+        return x
+
+    def large(*a, **k):
+        out = prefill(*a, **k)
+        for _ in range(200):
+            torch.mm(busy, busy, out=to)
+        return out
+
+    def step(*a, **k):
+        assert slm.shared
+        raise RuntimeError("this step fails")
+
+    assert not slm.shared
+    monkeypatch.setattr(torch.cuda, "Stream", streams)
+    monkeypatch.setattr(llm, "prefill", large)
+    monkeypatch.setattr(slm, "decode_step", step)
+    with pytest.raises(RuntimeError, match="this step fails"):
+        joint.generate_overlapped(slm, llm, prompts, NEW)
+    after = torch.cuda.Event()
+    after.record()
+    after.synchronize()
+    there = [x.query() for x in made]
+    torch.cuda.synchronize()
+    assert there == [True, True] and not slm.shared
+
+
 def test_drawn_sequences_to_a_new_head(models):
     """The run as a whole: draws, rows with the teacher's largest logits, and steps of clipped gradients."""
     from paper_2504_07878_amd import adapt, joint, sampling
