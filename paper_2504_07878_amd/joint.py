@@ -41,6 +41,11 @@ class _Tokens:
         return out
 
 
+def _drawn(tokens):
+    if np.any(np.asarray(tokens) < 0):
+        raise ValueError("a row of logits holds no token to draw: all of them are -inf or NaN")
+
+
 def _choosers(slm, llm, rows, max_new, draw, numbers):
     """One for each model; the large one's padding past the small one's vocabulary is not drawn."""
     if draw is None:
@@ -59,7 +64,7 @@ def generate(slm, llm, prompts, max_new: int, draw=None, numbers=None):
 
     slm: tokroute.Model with a router; llm: tokroute.Model of the large model (its own outputs are used, its router
     fields ignored). Returns (tokens int32 [B][max_new], routed bool [B][max_new]): routed[b][t] says the large model
-    produced tokens[b][t].
+    produced tokens[b][t]. A row of logits that are all -inf or NaN has no token to draw: ValueError.
     """
     B = len(prompts)
     slots = list(range(B))
@@ -82,6 +87,7 @@ def generate(slm, llm, prompts, max_new: int, draw=None, numbers=None):
             lo = large(llm.extend(later, [seq[b][llm_len[b]:] for b in later], want_logits=large.wanted), later, [t] * len(later)).cpu(("token",))
             for i, b in enumerate(later):
                 tok[b] = lo.token[i]
+        _drawn(tok)
         for b in flagged:
             llm_len[b] = len(seq[b])
             routed[b, t] = True
@@ -118,6 +124,7 @@ def generate_overlapped(slm, llm, prompts, max_new: int, draw=None, numbers=None
     inflight = None                        # (sequences, output objects kept alive, event)
 
     def emit(b, tok, by_large):
+        _drawn(tok)
         tokens[b, done[b]] = tok
         routed[b, done[b]] = by_large
         seq[b].append(int(tok))

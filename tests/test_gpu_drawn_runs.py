@@ -126,6 +126,25 @@ def test_an_error_leaves_the_streams_joined(models, monkeypatch):
     assert there == [True, True] and not slm.shared
 
 
+@pytest.mark.parametrize("new", [1, 4])
+@pytest.mark.parametrize("overlapped", [0, 1])
+def test_rows_without_any_token_end_the_run(models, overlapped, new):
+    """A large model whose logits are NaN: the run ends with an error, at its last position too."""
+    from paper_2504_07878_amd import sampling, synth, tokroute
+    s, slm, llm, prompts, numbers = models
+    weights = synth.make_weights(s, SEED, std=0.05)
+    weights["final_norm"] = np.full_like(weights["final_norm"], np.nan)
+    broken = tokroute.Model(s.with_(router_hidden=0).asdict(), weights, B, 64)
+    scores = np.sort(slm.prefill(list(range(B)), prompts).cpu().score)
+    slm.set_threshold(float(scores[B // 2]))      # some of the prompts' tokens are the large model's
+    try:
+        with pytest.raises(ValueError, match="no token"):
+            loops()[overlapped](slm, broken, prompts, new, draw=sampling.Draw(temperature=0.9), numbers=numbers[:, :new])
+        assert not slm.shared
+    finally:
+        slm.set_threshold(s.threshold)
+
+
 def test_drawn_sequences_to_a_new_head(models):
     """The run as a whole: draws, rows with the teacher's largest logits, and steps of clipped gradients."""
     from paper_2504_07878_amd import adapt, joint, sampling
