@@ -25,7 +25,7 @@ def collect(slm, llm, prompts, tokens, top: int = 16):
     slots = list(range(len(prompts)))
     keep = ([], [], [], [])
     vocab = llm.shape["vocab"]
-    listed = top <= sampling.MOST_ENTRIES and vocab <= sampling.MOST_VOCAB      # (more entries than the losses take are listed by PyTorch)
+    listed = 1 <= top <= sampling.MOST_ENTRIES and vocab <= sampling.MOST_VOCAB      # (more entries than the losses take, or none, are listed by PyTorch)
     sampler = sampling.Sampler(len(prompts), vocab, device=llm.device) if listed else None
 
     def take(small, large, targets):
