@@ -7,6 +7,7 @@ from __future__ import annotations
 from array import array
 
 import torch
+from torch.autograd.graph import increment_version
 
 from . import tokroute
 from .tokroute import TokrouteError
@@ -89,4 +90,5 @@ class Clipper:
                 raise ValueError("out: tensors of the gradients' types, shapes and strides")
         norm = torch.empty((), dtype=torch.float32, device=self.device)
         self._call(self.lib.tr_grad_clip, "tr_grad_clip", [at, to, *self._sizes(grads, kinds, counts)], max_norm, norm.data_ptr())
+        increment_version(out)      # autograd sees what is written over
         return norm

@@ -10,6 +10,7 @@ import operator
 from dataclasses import dataclass
 
 import torch
+from torch.autograd.graph import increment_version
 
 from . import tokroute
 from .tokroute import TokrouteError, tr_pick_config, tr_pick_rows, tr_sample_how
@@ -84,7 +85,7 @@ class Sampler:
 
         temperature, top_p, min_p (float32 [n]) and top_k (int32 [n]) are numbers or device tensors with a value a row. token and logprob may be given (written over)."""
         rows = self._rows(logits)
-        shape = (rows.rows,)
+        shape, given = (rows.rows,), [t for t in (token, logprob) if t is not None]
         how = tr_sample_how(self._flat(u, "u", torch.float32, shape))
         if isinstance(temperature, torch.Tensor):
             how.temperatures = self._flat(temperature, "temperature", torch.float32, shape)
@@ -111,6 +112,7 @@ class Sampler:
         else:
             self._flat(logprob, "logprob", torch.float32, shape)
         self._call(self.lib.tr_sample, "tr_sample", C.byref(rows), C.byref(how), token.data_ptr(), logprob.data_ptr())
+        increment_version(given)      # autograd sees what is written over
         return token, logprob
 
     def top(self, logits, entries: int, ids=None, values=None):
@@ -118,7 +120,7 @@ class Sampler:
         if entries > MOST_ENTRIES:
             raise TokrouteError(tokroute.ERR_CAPACITY, "tr_top", f"(more than {MOST_ENTRIES} entries)")
         rows = self._rows(logits)
-        shape = (rows.rows, entries)
+        shape, given = (rows.rows, entries), [t for t in (ids, values) if t is not None]
         if ids is None:
             ids = logits.new_empty(shape, dtype=torch.int32)
         else:
@@ -128,4 +130,5 @@ class Sampler:
         else:
             self._flat(values, "values", torch.float32, shape)
         self._call(self.lib.tr_top, "tr_top", C.byref(rows), entries, ids.data_ptr(), values.data_ptr())
+        increment_version(given)
         return ids, values

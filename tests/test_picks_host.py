@@ -113,3 +113,31 @@ def test_numbers_beyond_32_bits_are_not_cut_off(tr, top_k, passed):
             s.top(torch.zeros(0, 10), entries)
         assert e.value.code == tr.ERR_CAPACITY
     assert s._rows(torch.zeros(1, 10).expand(2**32 + 1, 10)).rows == 2**31 - 1       # more than any Sampler is for
+
+
+def test_autograd_sees_what_is_written_over(tr):
+    """A tensor that a graph has kept, and that a call has written over since, is no gradient of it any more: the backward pass says so, as after PyTorch's own calls."""
+    import torch
+    from types import SimpleNamespace
+    from paper_2504_07878_amd import clipping, sampling
+    cpu, noted = torch.device("cpu"), []                  # (without a GPU)
+    c, s = object.__new__(clipping.Clipper), object.__new__(sampling.Sampler)
+    c.device, c.lib = cpu, SimpleNamespace(tr_grad_clip=None)
+    s.dtype, s.device, s.cfg, s.lib = torch.float32, cpu, tr.tr_pick_config(4, 10, tr.F32), SimpleNamespace(tr_sample=None, tr_top=None)
+    c._call = s._call = lambda *a: noted.append(a)
+    w, z, u = torch.ones(4, requires_grad=True), torch.zeros(4, 10), torch.zeros(4)
+    wide = torch.ones(4, 3, requires_grad=True)
+    calls = [(w, lambda t: c.clip([t], 1.0)), (w, lambda t: c.clip([torch.zeros(4)], 1.0, out=[t])), (w, lambda t: c.clip([None, t], 1.0)), (w, lambda t: s.sample(z, u, logprob=t)), (wide, lambda t: s.top(z, 3, values=t))]
+    for x, write in calls:
+        kept = torch.ones_like(x).detach()
+        y = (x * kept).sum()
+        write(kept)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.backward()
+    assert len(noted) == len(calls)
+    with torch.inference_mode():
+        c.clip([torch.ones(3)], 1.0)                      # (keeps no count)
+    same = torch.ones(4)
+    y = (w * same).sum()
+    c.clip([same], 1.0, out=[torch.zeros(4)])             # what is only read is still what it was
+    y.backward()
