@@ -350,6 +350,7 @@ int tr_distill_grad(const tr_loss_config *cfg, void *workspace, size_t workspace
  *   tr_top: the first `entries` tokens of the order; ids -1 and values -infinity where a row has fewer.
  * A row without any token: token -1, logprob 0.
  * Weights are sums' terms in 64 bits, rounded to units of 2^-(62 - log2 vocab), or 2^-51, of the largest (2^-44 at 151936): the same inputs give the same token, whatever else runs.
+ * (Where nothing is cut from more than 8192 logits sums are not rounded to units, and u counts as 2^-45 at least and 1 - 2^-45 at most: what adds up to less at either end of the ids is not drawn.)
  *
  * Errors: TR_ERR_INVALID_ARG, TR_ERR_SHAPE (unsupported type or sizes), TR_ERR_CAPACITY (more rows or entries than configured, workspace too small), before anything is enqueued;
  * TR_ERR_HIP. Calls only enqueue, with the device of the stream and of all pointers current. Calls that share a workspace must be ordered with respect to each other; nothing in it outlives

@@ -652,7 +652,9 @@ template <class T, class S> __device__ __forceinline__ void draw_freely(const Pi
 #pragma unroll
     for (int e = 0; e < PER; ++e) sum += parts[e];
     double before = sum_upto(sum, total, s) - sum;
-    const double want = evenly(a.u[r]) * total;
+    // (the first and the last tokens may weigh nothing beside the others, where weights in units are 0)
+    constexpr double END = 0x1p-45;
+    const double want = fmin(fmax(evenly(a.u[r]), END), 1 - END) * total;
     const Found part = first_over(parts, before, want, s);
     float z[PER];
     double v[PER];

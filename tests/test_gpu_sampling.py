@@ -181,6 +181,16 @@ def test_random_numbers_at_the_ends(sampling, v, how):
         check(z, u, how, *sampling.Sampler(len(u), v).sample(z, u, **how))
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("v", [1000, 40001, 151936])
+def test_numbers_at_the_ends_draw_nothing_without_weight(sampling, v, dtype):
+    """0 and numbers that 32 bits round to 1: at low temperatures nearly all tokens have no weight that 64 bits hold beside the largest, the first and the last ids too."""
+    u = torch.tensor([0.0, 1e-20, 2.0 ** -24, 1 - 2.0 ** -24, 1.0, 5.0], device="cuda")
+    z, s = (2 * logits_of("flat", 1, v, 52)).to(dtype).expand(len(u), v), sampling.Sampler(len(u), v, dtype)
+    for t in (1.0, 0.1, 0.01, 1e-3, 1e-30):
+        check(z, u, dict(temperature=t), *s.sample(z.contiguous(), u, temperature=t))
+
+
 def test_equal_logits_are_drawn_by_place(sampling):
     """All weights are 1: u takes the token at floor(u V), and filters keep the lowest ids."""
     v = 40000

@@ -114,3 +114,14 @@ def test_a_top_k_of_all_tokens_is_none(host, how, more):
     got = host.sample(z, u, **how, top_k=9001 + more)
     assert host.launches("steps_kernel") == 1 and all(np.array_equal(a, b) for a, b in zip(got, without))
     check(z, u, how, *got)
+
+
+ENDS = np.float32([0.0, 1e-20, 2.0 ** -24, 1 - 2.0 ** -24, 1.0, 5.0])
+
+
+@pytest.mark.parametrize("temperature", [1.0, 0.1, 0.01, 1e-3, 1e-30])
+@pytest.mark.parametrize("v", [3001, 9001, 20001])
+def test_numbers_at_the_ends_draw_nothing_without_weight(host, v, temperature):
+    """0 and numbers that 32 bits round to 1: at low temperatures nearly all tokens have no weight that 64 bits hold beside the largest, the first and the last ids too."""
+    z = np.repeat(2 * rows_of("flat", 1, v, 7), len(ENDS), 0)
+    check(z, ENDS, dict(temperature=temperature), *host.sample(z, ENDS, temperature=temperature))
