@@ -203,3 +203,35 @@ def test_refusals(clipping):
             c.clip([t], bad)
         assert e.value.code == tokroute.ERR_INVALID_ARG
     assert (t == 1).all()
+
+
+LARGE = [(500 + i % 7, 901) if i % 5 else (i % 31 + 1,) for i in range(490)] + [(151936, 11), 7]
+LARGE[40:40] = [(0,), (20000, 1003)]
+
+
+@pytest.mark.parametrize("by", [0.37, 1.5])
+@pytest.mark.parametrize("dtypes", [(torch.float32,), (torch.bfloat16,), (torch.bfloat16, torch.float32, torch.bfloat16)], ids=["f32", "bf16", "both"])
+def test_more_sums_than_one_join_and_more_bytes_than_the_cache(clipping, dtypes, by):
+    """A large model's gradients: four lists that fill all workgroups of a launch (8192 sums, joined on the way twice, and before the scaling) and a fifth, 390 MB in bf16 and 770 MB in fp32, of which the
+    last 192 MB are read through the caches, from a gradient's middle on; sizes that are no whole number of tiles, some small ones between them. Element by element."""
+    grads, c = some(LARGE, dtypes, seed=9), clipping.Clipper()
+    want = float(np.sqrt(sum(float(t.double().square().sum()) for t in grads)))
+    max_norm = float(np.float32(by * want))
+    scale = min(1.0, max_norm / want)
+    out = [torch.full_like(t, 7) for t in grads]
+    norms = [c.norm(grads), c.clip(grads, max_norm, out=out)]
+    for t, x in zip(out, grads):
+        y = x.double() * scale
+        assert ((t.double() - y).abs() <= y.abs() * ((EPS[t.dtype] if t.dtype != torch.float32 else 0) + 3.1 * EPS[torch.float32]) + torch.finfo(t.dtype).tiny * EPS[t.dtype] * 2).all()
+        assert by < 1 or torch.equal(t, x)
+    norms.append(c.clip(grads, max_norm))
+    assert all(torch.equal(a, b) for a, b in zip(grads, out))
+    assert abs(float(norms[0]) / want - 1) <= 2.0 ** -23 and torch.equal(norms[0], norms[1]) and torch.equal(norms[0], norms[2])
+
+
+@pytest.mark.parametrize("dtypes", [(torch.float32,), (torch.bfloat16, torch.float32)], ids=["f32", "both"])
+def test_the_norm_of_many_lists(clipping, dtypes):
+    """As those of test_the_same_bits_every_time, some 3200 sums, against 64 bits."""
+    grads = some([(1500, 896), 896, 77, (300, 300)] * 40, dtypes)
+    norm, want = clipping.Clipper().norm(grads), float(np.sqrt(sum(float(t.double().square().sum()) for t in grads)))
+    assert abs(float(norm) / want - 1) <= 2.0 ** -23

@@ -125,3 +125,19 @@ def test_numbers_at_the_ends_draw_nothing_without_weight(host, v, temperature):
     """0 and numbers that 32 bits round to 1: at low temperatures nearly all tokens have no weight that 64 bits hold beside the largest, the first and the last ids too."""
     z = np.repeat(2 * rows_of("flat", 1, v, 7), len(ENDS), 0)
     check(z, ENDS, dict(temperature=temperature), *host.sample(z, ENDS, temperature=temperature))
+
+
+@pytest.mark.parametrize("order", lockstep.ORDERS)
+def test_clipping_of_several_lists(host, order):
+    """Two lists and a half, one of the gradients of several tiles: in place as into others, and the norm alone."""
+    g = np.random.Generator(np.random.Philox(9))
+    grads = [(g.standard_normal(30011 if i == 130 else i % 37, dtype=np.float32)) for i in range(290)]
+    grads = [halved(x) if i % 3 == 1 else x for i, x in enumerate(grads)]
+    wide = [values(x).astype(np.float64) for x in grads]
+    length = np.sqrt(sum((x * x).sum() for x in wide))
+    max_norm, out = float(np.float32(0.37 * length)), [np.full_like(x, 7) for x in grads]
+    norms = [host.clip(grads, None, order=order), host.clip(grads, max_norm, out, order), host.clip(grads, max_norm, order=order)]
+    assert norms[0] == norms[1] == norms[2] and abs(norms[0] / length - 1) <= 2.0 ** -23
+    for a, b, x in zip(grads, out, wide):
+        want = x * (max_norm / length)
+        assert np.array_equal(a, b) and (np.abs(values(b) - want) <= np.abs(want) * ((2.0 ** -8 if b.dtype == np.uint16 else 0) + 3.1 * 2.0 ** -24)).all()
