@@ -86,7 +86,8 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v) { return last_lane(wave
 
 // ------------------------------------------------------------------ weights
 
-// 2^(j / 32) as 64-bit words, less j << 47: with k << 47 added, k = 32 e + j, the word of 2^(k / 32)
+// The exponential by a table and a short polynomial is P. T. P. Tang's method (Table-driven implementation of the exponential function in IEEE floating-point arithmetic, ACM Transactions on
+// Mathematical Software 15, 1989), with values of its own: 2^(j / 32) as 64-bit words, less j << 47, so that with k << 47 added, k = 32 e + j, it is the word of 2^(k / 32)
 __device__ const uint2 POWERS[32] = {
     {0x00000000, 0x3ff00000}, {0xd3158574, 0x3fefd9b0}, {0x6cf9890f, 0x3fefb558}, {0xd0125b51, 0x3fef9301}, {0x3c7d517b, 0x3fef72b8}, {0x3168b9aa, 0x3fef5487},
     {0x6e756238, 0x3fef387a}, {0xf51fdee1, 0x3fef1e9d}, {0x0a31b715, 0x3fef06fe}, {0x373aa9cb, 0x3feef1a7}, {0x4c123422, 0x3feedea6}, {0x6061892d, 0x3feece08},

@@ -8,8 +8,10 @@ request (Figure 2) never recompute a prefix (the prototype of Section 4.1 has no
 This module is host control flow only: every tensor operation runs in the library's kernels, called through the C ABI
 binding. One device-to-host copy of the flags and tokens per step decides which sequences call the large model.
 
-Tokens are greedy, or drawn (`sampling.Draw`) from given random numbers, one for every position of every sequence: the same numbers give the same
-draws whatever the schedule. The router's flags do not depend on it.
+Tokens are greedy, or drawn (`sampling.Draw`) from given random numbers, one for every position of every sequence,
+whatever the schedule. Schedules batch sequences differently, which leaves other last bits in the logits: their draws
+differ where a number lies that near to the border between two tokens (and where a score does to the threshold), and
+nowhere else; the same call gives the same tokens. Whether a position is routed does not depend on its number.
 """
 from __future__ import annotations
 

@@ -67,6 +67,32 @@ def test_the_same_numbers_the_same_tokens(models):
     assert np.array_equal(first, again) and not np.array_equal(first, other)
 
 
+@pytest.mark.parametrize("how", [dict(temperature=0.9), dict(temperature=1.0, top_p=0.8), dict(top_k=20)])
+def test_schedules_draw_the_same_but_next_to_a_border(models, how):
+    """Sequence by sequence, up to where the schedules first differ, if they do: there the number is next to the border between both tokens (logits differ by 1e-3 at most, as above), or the score
+    next to the threshold."""
+    from paper_2504_07878_amd import joint, sampling
+    s, slm, llm, prompts, numbers = models
+    draw = sampling.Draw(**how)
+    (tokens, routed), (other, routed2) = (run(slm, llm, prompts, NEW, draw=draw, numbers=numbers) for run in loops())
+    settings = float(np.float32(draw.temperature)), draw.top_k, float(np.float32(draw.top_p)), float(np.float32(draw.min_p))
+    same = 0
+    for b in range(B):
+        differ = np.flatnonzero((tokens[b] != other[b]) | (routed[b] != routed2[b]))
+        t = int(differ[0]) if len(differ) else NEW
+        same += t
+        if t == NEW:
+            continue
+        seq = list(prompts[b]) + tokens[b, :t].tolist()
+        if routed[b, t] != routed2[b, t]:
+            assert abs(float(slm.prefill([0], [seq]).cpu().score[0]) - s.threshold) < 1e-4
+            continue
+        z = (llm if routed[b, t] else slm).prefill([0], [seq], want_logits=True).cpu().logits[0, :s.vocab]
+        for token in (tokens[b, t], other[b, t]):
+            assert picks.near_draw(z, numbers[b, t], *settings, token, 2.4e-3)
+    assert same >= B * NEW // 2      # (a number is within 2.4e-3 of a border between the 20 to 4000 tokens' stretches now and then; fp32 logits are a hundred times nearer than that)
+
+
 def test_a_draw_does_not_wait_for_the_model(models):
     """The host goes on while the call whose logits are drawn from is still at work (here: products behind it on its stream that take a tenth of a second), as the overlapped schedule needs."""
     from paper_2504_07878_amd import joint, sampling
