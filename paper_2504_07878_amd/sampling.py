@@ -70,6 +70,10 @@ class Sampler:
             raise ValueError(f"{what}: a contiguous {dtype} tensor of shape {shape} on {self.device}")
         return t.data_ptr()
 
+    def _over(self, t, what, dtype, shape):
+        self._flat(t, what, dtype, shape)
+        increment_version(t)      # autograd sees what is written over
+
     def _call(self, fn, what, *args):
         stream = tokroute.raw_stream(self.device.index)
         if stream != self._home:
@@ -85,7 +89,7 @@ class Sampler:
 
         temperature, top_p, min_p (float32 [n]) and top_k (int32 [n]) are numbers or device tensors with a value a row. token and logprob may be given (written over)."""
         rows = self._rows(logits)
-        shape, given = (rows.rows,), [t for t in (token, logprob) if t is not None]
+        shape = (rows.rows,)
         how = tr_sample_how(self._flat(u, "u", torch.float32, shape))
         if isinstance(temperature, torch.Tensor):
             how.temperatures = self._flat(temperature, "temperature", torch.float32, shape)
@@ -106,13 +110,12 @@ class Sampler:
         if token is None:
             token = torch.empty_like(u, dtype=torch.int32)
         else:
-            self._flat(token, "token", torch.int32, shape)
+            self._over(token, "token", torch.int32, shape)
         if logprob is None:
             logprob = torch.empty_like(u)
         else:
-            self._flat(logprob, "logprob", torch.float32, shape)
+            self._over(logprob, "logprob", torch.float32, shape)
         self._call(self.lib.tr_sample, "tr_sample", C.byref(rows), C.byref(how), token.data_ptr(), logprob.data_ptr())
-        increment_version(given)      # autograd sees what is written over
         return token, logprob
 
     def top(self, logits, entries: int, ids=None, values=None):
@@ -120,15 +123,14 @@ class Sampler:
         if entries > MOST_ENTRIES:
             raise TokrouteError(tokroute.ERR_CAPACITY, "tr_top", f"(more than {MOST_ENTRIES} entries)")
         rows = self._rows(logits)
-        shape, given = (rows.rows, entries), [t for t in (ids, values) if t is not None]
+        shape = (rows.rows, entries)
         if ids is None:
             ids = logits.new_empty(shape, dtype=torch.int32)
         else:
-            self._flat(ids, "ids", torch.int32, shape)
+            self._over(ids, "ids", torch.int32, shape)
         if values is None:
             values = logits.new_empty(shape, dtype=torch.float32)
         else:
-            self._flat(values, "values", torch.float32, shape)
+            self._over(values, "values", torch.float32, shape)
         self._call(self.lib.tr_top, "tr_top", C.byref(rows), entries, ids.data_ptr(), values.data_ptr())
-        increment_version(given)
         return ids, values
