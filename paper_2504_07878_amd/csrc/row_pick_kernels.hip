@@ -878,7 +878,7 @@ template <class T, int HELD, class S> __device__ __forceinline__ bool mend(const
     return true;
 }
 
-// One workgroup a row. Bound by the latency of a few loads and of some twenty barriers: one row of 151936 8.3 us, the largest 16 of 64 rows 6, 256 rows with top-p, which ends among thousands, 31.
+// One workgroup a row. Bound by the latency of a few loads and of some twenty barriers: one row of 151936 8.3 us, the largest 16 of 64 rows 6, 256 rows with top-p, which ends among thousands, 32.
 template <class T, bool TOP, bool WHOLE, int HELD> __global__ __launch_bounds__(DECIDERS) void decide_kernel(PickArgs a)
 {
     using S = Shared<HELD, WHOLE>;
