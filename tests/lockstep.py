@@ -16,7 +16,7 @@ def build(to):
     lanes, csrc = os.path.join(ROOT, "tests", "lanes"), os.path.join(ROOT, "paper_2504_07878_amd", "csrc")
     sources = [os.path.join(lanes, "lanes.cpp")] + [os.path.join(csrc, f"{x}.hip") for x in ("row_pick_api", "row_pick_kernels", "clip_api", "clip_kernels")]
     objects = [os.path.join(to, os.path.basename(s) + ".o") for s in sources]
-    flags = ["-x", "c++", "-std=c++17", "-O1", "-mfma", "-ffp-contract=off", "-fPIC", "-I", lanes]
+    flags = ["-x", "c++", "-std=c++17", "-O1", "-ffp-contract=off", "-fPIC", "-I", lanes]
     for p in [subprocess.Popen([CXX, *flags, "-c", s, "-o", o]) for s, o in zip(sources, objects)]:
         assert p.wait() == 0
     path = os.path.join(to, "liblanes.so")
