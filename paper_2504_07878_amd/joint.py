@@ -42,10 +42,9 @@ class _Tokens:
             self.sampler.sample(out.logits[:, :self.vocab], u, token=out.token, **self.draw)
         return out
 
-
-def _drawn(tokens):
-    if np.any(np.asarray(tokens) < 0):
-        raise ValueError("a row of logits holds no token to draw: all of them are -inf or NaN")
+    def drawn(self, tokens):
+        if self.wanted and np.any(np.asarray(tokens) < 0):
+            raise ValueError("a row of logits holds no token to draw: all of them are -inf or NaN")
 
 
 def _choosers(slm, llm, rows, max_new, draw, numbers):
@@ -89,7 +88,7 @@ def generate(slm, llm, prompts, max_new: int, draw=None, numbers=None):
             lo = large(llm.extend(later, [seq[b][llm_len[b]:] for b in later], want_logits=large.wanted), later, [t] * len(later)).cpu(("token",))
             for i, b in enumerate(later):
                 tok[b] = lo.token[i]
-        _drawn(tok)
+        small.drawn(tok)
         for b in flagged:
             llm_len[b] = len(seq[b])
             routed[b, t] = True
@@ -126,7 +125,7 @@ def generate_overlapped(slm, llm, prompts, max_new: int, draw=None, numbers=None
     inflight = None                        # (sequences, output objects kept alive, event)
 
     def emit(b, tok, by_large):
-        _drawn(tok)
+        small.drawn(tok)
         tokens[b, done[b]] = tok
         routed[b, done[b]] = by_large
         seq[b].append(int(tok))
